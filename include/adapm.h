@@ -287,6 +287,108 @@ adapm_status adapm_sgns_step(adapm_ctx* ctx, uint32_t worker, const uint32_t* ce
                              uint32_t n_ctx, uint32_t n_neg, uint32_t vocab, uint32_t dim,
                              float lr, double* loss_out);
 
+/* ---- token embeddings --------------------------------------------------- */
+/* A model whose token embedding lives in the store and whose other layers run
+ * elsewhere uses these around its own forward and backward pass: look the
+ * rows of a batch up (adapm_embed), sum the gradient rows of equal tokens
+ * (adapm_embed_grad), take the norm over these and every other gradient
+ * (adapm_grad_norm), clip (adapm_clip_grads), and apply the summed rows
+ * (adapm_push_grads).  The paper has no counterpart; reads and writes follow
+ * adapm_pull and adapm_push (replica of the worker, else main). */
+
+#define ADAPM_F32 0
+#define ADAPM_F16 1
+#define ADAPM_BF16 2
+
+/* outer x inner token ids; id (o, i) is ids[o * outer_stride + i *
+ * inner_stride] (a host array has no gaps: inner_stride 1, outer_stride
+ * inner).  id_bits 32: ids are keys, as everywhere; 64: signed.  An id outside
+ * [0, num_keys) is reported as ADAPM_ERANGE by adapm_wait and treated as
+ * padding.  With has_pad, ids equal to pad (any value) are padding: they have
+ * a row of zeros and no gradient. */
+typedef struct {
+  const void* ids;
+  int32_t id_bits;
+  int32_t has_pad;
+  int64_t pad;
+  uint64_t outer, inner;
+  int64_t outer_stride, inner_stride;
+} adapm_tokens;
+
+/* The rows that belong to an adapm_tokens: row (o, i) begins at element
+ * o * outer_stride + i * inner_stride of data (a host array has no gaps); its
+ * elements, of `type` (ADAPM_F32, _F16, _BF16), follow each other. */
+typedef struct {
+  void* data;
+  int32_t type;
+  int64_t outer_stride, inner_stride;
+} adapm_rows;
+
+/* One gradient: `count` elements of `type` without gaps, aligned to one
+ * element.  With live (a device word; NULL: none), only the first
+ * min(count, *live * row_len) count: the rows of adapm_embed_grad, whose
+ * number only the device knows. */
+typedef struct {
+  void* data;
+  uint64_t count;
+  const uint32_t* live;
+  uint32_t row_len;
+  int32_t type;
+} adapm_tensor;
+
+/* out(t) = scale * the first `dim` floats of the worker's value of token t
+ * (1 <= dim <= value_len), computed in fp32 and rounded once to out's type.
+ * A row whose replica has a pending update counts it, as in adapm_pull.
+ * Rows of out must not overlap (ADAPM_EINVAL where two strides make them). */
+adapm_status adapm_embed(adapm_ctx* ctx, uint32_t worker, const adapm_tokens* tokens, uint32_t dim,
+                         float scale, const adapm_rows* out);
+
+/* The gradient of adapm_embed by tokens: keys receives the distinct tokens of
+ * the batch in ascending order, without padding, *count their number, and row
+ * u of rows (dim floats each, no gaps) scale times the sum of the rows of
+ * grad that belong to keys[u].  Both have room for outer * inner entries; keys
+ * behind the last are 0xFFFFFFFF, rows behind it are left as they are.
+ * grad may repeat rows (strides of 0).  Sums are fp32 in order of appearance
+ * within fixed chunks of the sorted batch, chunk sums in chunk order:
+ * deterministic for a given input.  The store is neither read nor written;
+ * tokens that the worker has signalled (adapm_intent) are grouped by that
+ * intent's plan, as in adapm_push.  keys, rows and count are device or host
+ * arrays. */
+adapm_status adapm_embed_grad(adapm_ctx* ctx, uint32_t worker, const adapm_tokens* tokens, uint32_t dim,
+                              float scale, const adapm_rows* grad, uint32_t* keys, float* rows,
+                              uint32_t* count);
+
+/* *norm (a float, device or host) = |scale| * the Euclidean norm over all
+ * elements of the n gradients; device arrays.  Squares are summed in fp32
+ * over at most 64 elements and in fp64 above, and in fp64 throughout where
+ * fp32 squares would overflow or vanish.  An infinity or a NaN anywhere shows
+ * in the norm.  Deterministic. */
+adapm_status adapm_grad_norm(adapm_ctx* ctx, const adapm_tensor* grads, uint64_t n, float scale,
+                             float* norm);
+
+/* outs[t] = round(scale * f * grads[t]) for every t, f = 1 if *norm <=
+ * max_norm, else max_norm / *norm (a NaN norm makes every element NaN, an
+ * infinite one 0, or NaN where it came from).  *norm is a device float, as
+ * adapm_grad_norm leaves it, so nothing waits on the host.  outs[t] has
+ * grads[t]'s count and a type of its own; its live and row_len are not used.
+ * It is grads[t]'s own memory (same type) or does not overlap any gradient.
+ * outs = NULL: in place, and nothing moves when scale * f is 1. */
+adapm_status adapm_clip_grads(adapm_ctx* ctx, const adapm_tensor* grads, const adapm_tensor* outs, uint64_t n,
+                              float scale, float max_norm, const float* norm);
+
+/* Apply n gradient rows of `dim` floats (no gaps) to the worker's values of
+ * `keys`, as adapm_embed_grad leaves them: ascending, each at most once,
+ * 0xFFFFFFFF skipped (a key that is not above the one before it is skipped
+ * and reported as ADAPM_ESTATE by adapm_wait, one >= num_keys as
+ * ADAPM_ERANGE).  With g = scale * f * rows[u], f from norm and max_norm as in
+ * adapm_clip_grads (norm = NULL: 1), the pushed row is -lr * g in the first
+ * dim floats, or with adagrad (value_len = 2 * dim, dim a multiple of 4)
+ * [-lr * g / sqrt(a + g*g + eps) | g*g], a the accumulators before the call.
+ * Written as adapm_push writes its sums, without a sort. */
+adapm_status adapm_push_grads(adapm_ctx* ctx, uint32_t worker, const uint32_t* keys, const float* rows,
+                              uint64_t n, uint32_t dim, int adagrad, float lr, float eps, float scale,
+                              float max_norm, const float* norm);
+
 /* ---- inspection (synchronising; for tests and tools) ------------------ */
 adapm_status adapm_clock(adapm_ctx* ctx, uint32_t worker, int64_t* out);
 

@@ -7,6 +7,8 @@ GPU or on the host (pinned or not) or numpy arrays; keys are passed as
 kernels; if the library is missing this module raises instead of falling
 back to anything else.
 """
+import collections
+import contextlib
 import ctypes
 import os
 
@@ -28,6 +30,7 @@ EXPORTS = [
     "adapm_refcounts", "adapm_owners", "adapm_poisson_quantile", "adapm_read_main", "adapm_get_stats", "adapm_profile_enable",
     "adapm_profile_read", "adapm_kernel_launches", "adapm_push_noalloc", "adapm_last_error",
     "adapm_debug_fail_next_barrier", "adapm_debug_fail_next_launch",
+    "adapm_embed", "adapm_embed_grad", "adapm_grad_norm", "adapm_clip_grads", "adapm_push_grads",
 ]
 
 
@@ -75,6 +78,25 @@ class Stats(ctypes.Structure):
     ]
 
 
+F32, F16, BF16 = range(3)
+
+
+class _Tokens(ctypes.Structure):
+    _fields_ = [("ids", ctypes.c_void_p), ("id_bits", ctypes.c_int32), ("has_pad", ctypes.c_int32),
+                ("pad", ctypes.c_int64), ("outer", ctypes.c_uint64), ("inner", ctypes.c_uint64),
+                ("outer_stride", ctypes.c_int64), ("inner_stride", ctypes.c_int64)]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("type", ctypes.c_int32), ("outer_stride", ctypes.c_int64),
+                ("inner_stride", ctypes.c_int64)]
+
+
+class _Tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("count", ctypes.c_uint64), ("live", ctypes.c_void_p),
+                ("row_len", ctypes.c_uint32), ("type", ctypes.c_int32)]
+
+
 class AdaPMError(RuntimeError):
     def __init__(self, status, message):
         super().__init__(f"{STATUS_NAMES.get(status, status)}: {message}")
@@ -120,6 +142,11 @@ def load(path=LIB_PATH):
         "adapm_push_noalloc": [P, U32, P, U64, P],
         "adapm_debug_fail_next_barrier": [P],
         "adapm_debug_fail_next_launch": [P],
+        "adapm_embed": [P, U32, P, U32, F, P],
+        "adapm_embed_grad": [P, U32, P, U32, F, P, P, P, P],
+        "adapm_grad_norm": [P, P, U64, F, P],
+        "adapm_clip_grads": [P, P, P, U64, F, F, P],
+        "adapm_push_grads": [P, U32, P, P, U64, U32, I, F, F, F, F, P],
     }
     for name, args in sig.items():
         fn = getattr(L, name)
@@ -205,6 +232,81 @@ def _out_ptr(t):
         return t.ctypes.data if t.size else None
     assert t.is_contiguous()
     return t.data_ptr() if t.numel() else None
+
+
+# -- token embeddings --------------------------------------------------------------
+_float_types = {}   # torch dtype -> element type of the ABI
+
+
+def _type_of(dtype):
+    if not _float_types:
+        torch = _torch()
+        _float_types.update({torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16})
+    if dtype not in _float_types:
+        raise ValueError(f"rows and gradients are float32, float16 or bfloat16, not {dtype}")
+    return _float_types[dtype]
+
+
+def _one_stride(shape, strides):
+    """The step that walks these dimensions in order, None if there is none (0 where nothing is stepped over)."""
+    step, size = 0, 1
+    for n, s in zip(reversed(shape), reversed(strides)):
+        if n == 1:
+            continue
+        if size > 1 and s != step * size:
+            return None
+        if size == 1:
+            step = s
+        size *= n
+    return step
+
+
+def _two_levels(shape, *strides):
+    """(outer, inner, (outer stride, inner stride) of each), or None: an outer and an inner step for all of them."""
+    for cut in range(len(shape) + 1):
+        steps = [(_one_stride(shape[:cut], s[:cut]), _one_stride(shape[cut:], s[cut:])) for s in strides]
+        if all(a is not None and b is not None for a, b in steps):
+            outer = inner = 1
+            for n in shape[:cut]:
+                outer *= n
+            for n in shape[cut:]:
+                inner *= n
+            return (outer, inner, *steps)
+    return None
+
+
+class RowGrads(collections.namedtuple("RowGrads", ["keys", "rows", "count"])):
+    """Gradient rows of distinct keys (adapm_embed_grad): keys (int32, ascending, then -1), rows (float32, one per
+    key) and count (int32, one element: how many of them there are)."""
+
+    __slots__ = ()
+
+
+class GradList:
+    """Gradients for grad_norm and clip_grads: CUDA tensors without gaps (float32, float16, bfloat16) and RowGrads.
+    A program whose gradient buffers stay can make its list once; the list keeps its tensors alive."""
+
+    def __init__(self, grads):
+        self.grads = list(grads)
+        self.array = (_Tensor * max(1, len(self.grads)))()
+        self.n = len(self.grads)
+        for a, g in zip(self.array, self.grads):
+            rows = g
+            if isinstance(g, RowGrads):
+                rows = g.rows
+                a.live, a.row_len = g.count.data_ptr(), rows.shape[-1]
+            if not rows.is_cuda or not rows.is_contiguous():
+                raise ValueError("gradients are CUDA tensors without gaps")
+            a.data, a.count, a.type = rows.data_ptr(), rows.numel(), _type_of(rows.dtype)
+
+
+def _check_norm(norm):
+    if norm is not None and (not norm.is_cuda or norm.dtype != _torch().float32 or norm.numel() != 1):
+        raise ValueError("norm is a float32 scalar on the GPU")
+
+
+def _grad_list(grads):
+    return grads if isinstance(grads, GradList) else GradList(grads)
 
 
 def poisson_quantile(lam, p):
@@ -361,6 +463,122 @@ class ParameterManager:
         self._check(self._lib.adapm_sgns_step(self._h, worker, c.ptr, x.ptr, ng.ptr, c.n, n_ctx,
                                               n_neg, vocab, dim, lr, lp))
         return lo
+
+    # -- token embeddings --------------------------------------------------------
+    def _on_stream(self):
+        """Temporaries and new outputs are made on, and belong to, the library's stream."""
+        torch = _torch()
+        if torch.cuda.current_stream() == self.stream:
+            return contextlib.nullcontext()
+        return torch.cuda.stream(self.stream)
+
+    def _tokens(self, tokens, pad, rows, what):
+        """The descriptors of tokens and of the rows (..., dim) that belong to them, and what keeps both alive."""
+        torch = _torch()
+        if isinstance(tokens, (np.ndarray, list, tuple)):
+            tokens = torch.from_numpy(np.ascontiguousarray(np.asarray(tokens, dtype=np.int64)))
+        if tokens.dtype != torch.int32 and tokens.dtype != torch.int64:
+            if tokens.is_floating_point() or tokens.is_complex() or tokens.dtype == torch.bool:
+                raise ValueError(f"tokens are integers, not {tokens.dtype}")
+            with self._on_stream():
+                tokens = tokens.to(torch.int64)
+        if rows.shape[:-1] != tokens.shape:
+            raise ValueError(f"{what} must have shape {(*tokens.shape, 'dim')}, not {tuple(rows.shape)}")
+        n, dim = tokens.numel(), rows.shape[-1]
+        if tokens.is_contiguous() and rows.is_contiguous():
+            outer, inner, ts, rs = 1, n, (n, 1), (n * dim, dim)
+        else:
+            if dim > 1 and rows.stride(-1) != 1:
+                if what == "out":
+                    raise ValueError("elements of a row of out must follow each other")
+                with self._on_stream():
+                    rows = rows.contiguous()
+            got = _two_levels(tokens.shape, tokens.stride(), rows.stride()[:-1])
+            if got is None:
+                with self._on_stream():
+                    tokens = tokens.contiguous()
+                got = _two_levels(tokens.shape, tokens.stride(), rows.stride()[:-1])
+            if got is None:
+                if what == "out":
+                    raise ValueError("out's rows are not reached by an outer and an inner stride")
+                with self._on_stream():
+                    rows = rows.contiguous()
+                got = _two_levels(tokens.shape, tokens.stride(), rows.stride()[:-1])
+            outer, inner, ts, rs = got
+        t = _Tokens(tokens.data_ptr(), 32 if tokens.dtype == torch.int32 else 64, pad is not None,
+                    0 if pad is None else int(pad), outer, inner, ts[0], ts[1])
+        return t, _Rows(rows.data_ptr(), _type_of(rows.dtype), rs[0], rs[1]), tokens, rows
+
+    def embed(self, worker, tokens, dim=None, scale=1.0, pad=None, out=None, dtype=None):
+        """scale * the first dim floats of the worker's value of every token, as (*tokens.shape, dim) in dtype
+        (float32 unless given, or out's).  Tokens: int32 or int64, any shape, strided or not; pad: the token whose
+        rows are zeros."""
+        torch = _torch()
+        if out is None:
+            shape = tokens.shape if hasattr(tokens, "shape") else np.shape(tokens)
+            on_gpu = isinstance(tokens, torch.Tensor) and tokens.is_cuda
+            with self._on_stream():
+                out = torch.empty((*shape, self.D if dim is None else dim), dtype=dtype or torch.float32,
+                                  device="cuda" if on_gpu else "cpu", pin_memory=not on_gpu)
+        elif (dim is not None and out.shape[-1] != dim) or (dtype is not None and out.dtype != dtype):
+            raise ValueError("out has another dim or dtype")
+        t, r, tokens, _ = self._tokens(tokens, pad, out, "out")
+        self._check(self._lib.adapm_embed(self._h, worker, ctypes.byref(t), out.shape[-1], scale, ctypes.byref(r)))
+        return out
+
+    def embed_grad(self, worker, tokens, grad, scale=1.0, pad=None, out=None):
+        """RowGrads of the distinct tokens: scale times the sum of the rows of grad (*tokens.shape, dim) that belong
+        to each.  out: RowGrads with room for tokens.numel() keys and rows."""
+        torch = _torch()
+        t, r, tokens, grad = self._tokens(tokens, pad, grad, "grad")
+        n, dim = tokens.numel(), grad.shape[-1]
+        if out is None:
+            where = {"device": "cuda"} if grad.is_cuda else {"device": "cpu", "pin_memory": True}
+            with self._on_stream():
+                out = RowGrads(torch.empty(n, dtype=torch.int32, **where), torch.empty((n, dim), **where),
+                               torch.empty(1, dtype=torch.int32, **where))
+        elif (out.keys.numel() < n or out.rows.numel() < n * dim or out.count.numel() < 1
+              or out.keys.dtype != torch.int32 or out.rows.dtype != torch.float32 or out.count.dtype != torch.int32
+              or (n > 0 and out.rows.shape[-1] != dim)):
+            raise ValueError("out needs int32 keys, float32 rows of dim elements for every token, and an int32 count")
+        self._check(self._lib.adapm_embed_grad(self._h, worker, ctypes.byref(t), dim, scale, ctypes.byref(r),
+                                               _out_ptr(out.keys), _out_ptr(out.rows), _out_ptr(out.count)))
+        return out
+
+    def grad_norm(self, grads, scale=1.0, out=None):
+        """|scale| times the Euclidean norm over all elements of grads (a GradList, or what makes one), as a float32
+        scalar on the GPU."""
+        g = _grad_list(grads)
+        if out is None:
+            torch = _torch()
+            with self._on_stream():
+                out = torch.empty((), dtype=torch.float32, device="cuda")
+        self._check(self._lib.adapm_grad_norm(self._h, g.array, g.n, scale, out.data_ptr()))
+        return out
+
+    def clip_grads(self, grads, norm, max_norm, scale=1.0, out=None):
+        """scale * min(1, max_norm / norm) times every gradient, in place or into out (a GradList, or what makes one).
+        norm: a float32 scalar on the GPU, as grad_norm returns it for the same scale."""
+        g = _grad_list(grads)
+        o = None if out is None else _grad_list(out)
+        if o is not None and o.n != g.n:
+            raise ValueError("out needs a tensor for every gradient")
+        _check_norm(norm)
+        self._check(self._lib.adapm_clip_grads(self._h, g.array, None if o is None else o.array, g.n, scale, max_norm,
+                                               norm.data_ptr()))
+
+    def push_grads(self, worker, keys, rows, lr, adagrad=False, eps=1e-8, scale=1.0, norm=None,
+                   max_norm=float("inf")):
+        """Update the worker's values of distinct ascending keys (-1: none) by their gradient rows, as embed_grad
+        leaves both: SGD, or AdaGrad on [theta | a] rows, after clipping to max_norm by norm."""
+        with contextlib.nullcontext() if _plain_tensor(keys, 1) and _plain_tensor(rows, 2) else self._on_stream():
+            k, r = _keys(keys), _floats(rows)
+        dim = rows.shape[-1]
+        if r.n != k.n * dim:
+            raise ValueError("rows must hold a row for every key")
+        _check_norm(norm)
+        self._check(self._lib.adapm_push_grads(self._h, worker, k.ptr, r.ptr, k.n, dim, int(bool(adagrad)), lr, eps,
+                                               scale, max_norm, None if norm is None else norm.data_ptr()))
 
     # -- inspection ------------------------------------------------------------
     def clock(self, worker):

@@ -15,7 +15,9 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libadapm.so")
-SOURCES = ["sort.cu", "sort_small.cu", "store.cu", "pull_bulk.cu", "push.cu", "push_factors.cu", "advance.cu", "copied.cu", "steps.cu", "capi.cu", "noalloc.cu"]
+SOURCES = ["sort.cu", "sort_small.cu", "store.cu", "pull_bulk.cu", "push.cu", "push_factors.cu", "advance.cu", "copied.cu", "steps.cu", "capi.cu", "noalloc.cu",
+           "embed.cu", "embed_sort.cu", "embed_grad.cu", "embed_grad_f32.cu", "embed_grad_f16.cu", "embed_grad_bf16.cu",
+           "push_grads.cu", "grads.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ARCH + ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]
 

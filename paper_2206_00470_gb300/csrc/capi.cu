@@ -22,6 +22,7 @@
 
 #include "adapm.h"
 #include "blocks.h"
+#include "embed.cuh"
 #include "internal.cuh"
 #include "store_launch.cuh"
 
@@ -806,6 +807,107 @@ cudaError_t close_list(adapm_ctx* ctx, uint32_t w, int64_t id) {
   return e;
 }
 
+// ---- token embeddings --------------------------------------------------------
+bool float_type(int32_t type) { return type == ADAPM_F32 || type == ADAPM_F16 || type == ADAPM_BF16; }
+size_t type_bytes(int32_t type) { return type == ADAPM_F32 ? 4 : 2; }
+
+// Checks of the tokens and their rows that adapm_embed and adapm_embed_grad
+// share; n: the number of tokens.
+adapm_status check_tokens(adapm_ctx* ctx, uint32_t worker, const adapm_tokens* t, uint32_t dim, const adapm_rows* r,
+                          uint64_t* n) {
+  if (worker >= ctx->s.W) return fail(ctx, ADAPM_EINVAL, "worker %u >= %u", worker, ctx->s.W);
+  if (!t || !r) return fail(ctx, ADAPM_EINVAL, "null tokens or rows");
+  if (t->id_bits != 32 && t->id_bits != 64) return fail(ctx, ADAPM_EINVAL, "ids have 32 or 64 bits, not %d", t->id_bits);
+  if (!float_type(r->type)) return fail(ctx, ADAPM_EINVAL, "unknown element type %d", r->type);
+  if (dim == 0 || dim > ctx->s.D) return fail(ctx, ADAPM_EINVAL, "dim %u: need 1 .. value_len %u", dim, ctx->s.D);
+  if (t->outer > kMaxN || t->inner > kMaxN || t->outer * t->inner > kMaxN)
+    return fail(ctx, ADAPM_EINVAL, "more than 2^31 tokens");
+  *n = t->outer * t->inner;
+  if (*n > 0 && (!t->ids || !r->data)) return fail(ctx, ADAPM_EINVAL, "null ids or rows");
+  if (*n > 0 && (reinterpret_cast<uintptr_t>(t->ids) % (t->id_bits / 8) != 0 ||
+                 reinterpret_cast<uintptr_t>(r->data) % type_bytes(r->type) != 0))
+    return fail(ctx, ADAPM_EINVAL, "ids or rows are not aligned to their type");
+  return ADAPM_OK;
+}
+
+// Whether element (o, i) is at (o * inner + i) * step.
+bool no_gaps(const adapm_tokens* t, int64_t outer_stride, int64_t inner_stride, int64_t step) {
+  return (t->inner <= 1 || inner_stride == step) && (t->outer <= 1 || outer_stride == (int64_t)t->inner * step);
+}
+
+// The ids on the device; `owned` is freed after the call's kernels.
+adapm_status stage_tokens(adapm_ctx* ctx, const adapm_tokens* t, uint64_t n, TokenView* v, char** owned) {
+  const size_t size = t->id_bits / 8;
+  v->flat = no_gaps(t, t->outer_stride, t->inner_stride, 1);
+  if (!v->flat && !is_device_ptr(t->ids)) return fail(ctx, ADAPM_EINVAL, "ids on the host must have no gaps");
+  Input<char> in;
+  CK(stage_in(ctx, static_cast<const char*>(t->ids), n * size, &in));
+  v->ids = in.dev;
+  *owned = in.owned;
+  v->wide = t->id_bits == 64;
+  v->has_pad = t->has_pad != 0;
+  v->pad = v->wide ? t->pad : (int64_t)(uint32_t)t->pad;   // (32-bit ids are unsigned)
+  v->inner = (uint32_t)t->inner;
+  v->outer_stride = t->outer_stride;
+  v->inner_stride = t->inner_stride;
+  v->n = n;
+  return ADAPM_OK;
+}
+
+RowView row_view(const adapm_tokens* t, const adapm_rows* r, void* dev) {
+  RowView v{};
+  v.data = static_cast<char*>(dev);
+  v.type = r->type;
+  v.inner = (uint32_t)t->inner;
+  v.outer_stride = r->outer_stride;
+  v.inner_stride = r->inner_stride;
+  // one step from each row to the next
+  v.flat = t->outer <= 1 || t->inner <= 1 || r->outer_stride == (int64_t)t->inner * r->inner_stride;
+  if (t->inner <= 1) v.inner_stride = r->outer_stride;
+  return v;
+}
+
+// Whether no two of the rows share an element.
+bool rows_apart(const adapm_tokens* t, const adapm_rows* r, uint32_t dim) {
+  uint64_t n0 = t->inner, n1 = t->outer;
+  int64_t s0 = r->inner_stride, s1 = r->outer_stride;
+  if (n0 <= 1) s0 = dim;
+  if (n1 <= 1) s1 = s0;
+  if (n1 > 1 && n0 > 1 && s1 < s0) {
+    std::swap(n0, n1);
+    std::swap(s0, s1);
+  }
+  if (n0 <= 1) return n1 <= 1 || s1 >= (int64_t)dim;
+  return s0 >= (int64_t)dim && (n1 <= 1 || s1 >= (int64_t)(n0 - 1) * s0 + (int64_t)dim);
+}
+
+adapm_status check_tensors(adapm_ctx* ctx, const adapm_tensor* t, uint64_t n, const char* what) {
+  if (n > 0 && !t) return fail(ctx, ADAPM_EINVAL, "null %s", what);
+  if (n > (1u << 24)) return fail(ctx, ADAPM_EINVAL, "more than 2^24 %s", what);
+  for (uint64_t i = 0; i < n; ++i) {
+    const unsigned long long at = i;
+    if (!float_type(t[i].type)) return fail(ctx, ADAPM_EINVAL, "%s[%llu]: unknown element type %d", what, at, t[i].type);
+    if (t[i].count == 0) continue;
+    if (!t[i].data || t[i].count > (1ull << 48)) return fail(ctx, ADAPM_EINVAL, "%s[%llu]: bad data/count", what, at);
+    if (reinterpret_cast<uintptr_t>(t[i].data) % type_bytes(t[i].type) != 0)
+      return fail(ctx, ADAPM_EINVAL, "%s[%llu] is not aligned to its type", what, at);
+    if (!is_device_ptr(t[i].data) || (t[i].live && !is_device_ptr(t[i].live)))
+      return fail(ctx, ADAPM_EINVAL, "%s[%llu] is not a device array", what, at);
+  }
+  return ADAPM_OK;
+}
+
+GradTensor grad_tensor(const adapm_tensor& t) {
+  GradTensor g{};
+  g.in = static_cast<const char*>(t.data);
+  g.out = static_cast<char*>(t.data);
+  g.live = t.live;
+  g.count = t.count;
+  g.row_len = t.row_len;
+  g.type = g.out_type = (uint8_t)t.type;
+  return g;
+}
+
 }  // namespace
 
 bool adapm::ctx_view(adapm_ctx* ctx, CtxView* out) {
@@ -1281,6 +1383,8 @@ adapm_status adapm_wait(adapm_ctx* ctx) {
   if (errors & ERR_REFCOUNT) return fail(ctx, ADAPM_ESTATE, "intent refcount overflow");
   if (errors & ERR_INTERNAL)
     return fail(ctx, ADAPM_ESTATE, "an index in the library's own state was out of range (element skipped)");
+  if (errors & ERR_KEY_ORDER)
+    return fail(ctx, ADAPM_ESTATE, "the keys of a row update were not distinct and ascending (some skipped)");
   return ADAPM_OK;
 }
 
@@ -1456,6 +1560,247 @@ adapm_status adapm_sgns_step(adapm_ctx* ctx, uint32_t worker, const uint32_t* ce
     pool_free(ctx, p);
   if (st != ADAPM_OK) return st;
   return check_launch(ctx, "sgns_step");
+}
+
+adapm_status adapm_embed(adapm_ctx* ctx, uint32_t worker, const adapm_tokens* tokens, uint32_t dim, float scale,
+                         const adapm_rows* out) {
+  adapm_status st = check_ctx(ctx);
+  if (st != ADAPM_OK) return st;
+  uint64_t n = 0;
+  st = check_tokens(ctx, worker, tokens, dim, out, &n);
+  if (st != ADAPM_OK) return st;
+  if (n == 0) return ADAPM_OK;
+  if (!rows_apart(tokens, out, dim)) return fail(ctx, ADAPM_EINVAL, "rows of out overlap");
+  const bool on_device = is_device_ptr(out->data);
+  if (!on_device && !no_gaps(tokens, out->outer_stride, out->inner_stride, dim))
+    return fail(ctx, ADAPM_EINVAL, "rows on the host must have no gaps");
+  TokenView tv{};
+  char* ids = nullptr;
+  st = stage_tokens(ctx, tokens, n, &tv, &ids);
+  if (st != ADAPM_OK) return st;
+  st = early_make(ctx, worker);
+  if (st != ADAPM_OK) return st;
+  ProfScope ps(ctx, 2);
+  CK(stage_join(ctx));
+  Output<char> o;
+  if (on_device) o.dev = static_cast<char*>(out->data);
+  else CK(stage_out(ctx, static_cast<char*>(out->data), n * dim * type_bytes(out->type), &o));
+  {
+    ProfScope pk(ctx, 7);
+    launch_embed(ctx->s, worker, tv, dim, scale, row_view(tokens, out, o.dev), ctx->sms, ctx->stream);
+  }
+  CK(finish_out(ctx, &o));
+  pool_free(ctx, ids);
+  return check_launch(ctx, "embed");
+}
+
+adapm_status adapm_embed_grad(adapm_ctx* ctx, uint32_t worker, const adapm_tokens* tokens, uint32_t dim, float scale,
+                              const adapm_rows* grad, uint32_t* keys, float* rows, uint32_t* count) {
+  adapm_status st = check_ctx(ctx);
+  if (st != ADAPM_OK) return st;
+  uint64_t n = 0;
+  st = check_tokens(ctx, worker, tokens, dim, grad, &n);
+  if (st != ADAPM_OK) return st;
+  if (!count || (n > 0 && (!keys || !rows))) return fail(ctx, ADAPM_EINVAL, "null keys, rows or count");
+  ProfScope ps(ctx, 5);
+  Output<uint32_t> oc;
+  CK(stage_out(ctx, count, 1, &oc));
+  if (n == 0) {
+    CK(cudaMemsetAsync(oc.dev, 0, sizeof(uint32_t), ctx->stream));
+    CK(finish_out(ctx, &oc));
+    return ADAPM_OK;
+  }
+  const bool on_device = is_device_ptr(grad->data);
+  if (!on_device && !no_gaps(tokens, grad->outer_stride, grad->inner_stride, dim))
+    return fail(ctx, ADAPM_EINVAL, "rows on the host must have no gaps");
+  TokenView tv{};
+  char* ids = nullptr;
+  st = stage_tokens(ctx, tokens, n, &tv, &ids);
+  if (st != ADAPM_OK) return st;
+  Input<char> ig;
+  if (on_device) ig.dev = static_cast<const char*>(grad->data);
+  else CK(stage_in(ctx, static_cast<const char*>(grad->data), n * dim * type_bytes(grad->type), &ig));
+  CK(stage_join(ctx));
+  Output<uint32_t> ok;
+  Output<float> orows;
+  CK(stage_out(ctx, keys, n, &ok));
+  CK(stage_out(ctx, rows, n * dim, &orows));
+  GradArgs a{};
+  a.n = n;
+  a.K = ctx->s.K;
+  a.grad = row_view(tokens, grad, const_cast<char*>(ig.dev));
+  a.dim = dim;
+  a.scale = scale;
+  a.keys = ok.dev;
+  a.rows = orows.dev;
+  a.count = oc.dev;
+  a.st = ctx->dstate;
+  a.pad_key = kNoKey;
+  IntentList* plan = find_plan(ctx, worker, n);
+  const bool count_sort = !plan && n <= kCountSort;
+  // padding that is a valid key is sorted like one (an intent that lists it
+  // then still matches, and the chunks are cut alike) and left out of the sums
+  if (tv.has_pad && tv.pad >= 0 && tv.pad < (int64_t)ctx->s.K) {
+    a.pad_key = (uint32_t)tv.pad;
+    tv.has_pad = false;
+  }
+  // 32-bit ids without gaps are keys as they are, and padding of all ones no key
+  const bool as_is = !tv.wide && tv.flat && (!tv.has_pad || (uint32_t)tv.pad == kNoKey);
+  uint32_t *ka = nullptr, *kb = nullptr, *va = nullptr, *vb = nullptr, *hist = nullptr, *copied = nullptr;
+  CK(pool_alloc(ctx, &ka, n));
+  CK(pool_alloc(ctx, &va, n));
+  if (count_sort) {
+    launch_count_sort(tv, ctx->s.K, ka, va, ctx->dstate, ctx->stream);
+    a.skeys = ka;
+    a.spos = va;
+  } else {
+    const uint32_t* raw = static_cast<const uint32_t*>(tv.ids);
+    if (!as_is) {
+      CK(pool_alloc(ctx, &copied, n));
+      launch_copy_tokens(tv, ctx->s.K, copied, ctx->dstate, ctx->sms, ctx->stream);
+      raw = copied;
+    }
+    uint32_t seq = 0;
+    if (plan) {
+      plan->plan_used = true;
+      if (plan->ready) CK(cudaStreamWaitEvent(ctx->stream, plan->ready, 0));   // (null: made on this stream)
+      if (++ctx->plan_seq == 0) ctx->plan_seq = 1;
+      seq = ctx->plan_seq;
+      ctx->planned_pushes += 1;
+    }
+    CK(pool_alloc(ctx, &kb, n));
+    CK(pool_alloc(ctx, &vb, n));
+    CK(pool_alloc(ctx, &hist, sort_scratch_words(n, ctx->bits, ctx->sms)));
+    uint32_t *sk = nullptr, *sp = nullptr;
+    CK(sort_keys(raw, n, ctx->s.K, !as_is || tv.has_pad, ctx->bits, ka, kb, va, vb, hist, ctx->sms, ctx->dstate,
+                 &ctx->bar_base, nullptr, nullptr, ctx->stream, &sk, &sp, plan ? plan->px : nullptr,
+                 plan ? &ctx->dstate->plan_miss : nullptr, seq, ctx_sort_by(ctx, n)));
+    a.skeys = sk;
+    a.spos = sp;
+    if (plan) {
+      a.skeys = plan->psk;
+      a.spos = plan->psp;
+      a.alt_keys = sk;
+      a.alt_pos = sp;
+      a.plan_word = &ctx->dstate->plan_miss;
+      a.plan_seq = seq;
+    }
+  }
+  const GradPlan p = grad_plan(a, ctx->sms);
+  a.chunk = p.chunk;
+  uint32_t *heads = nullptr, *crossing = nullptr;
+  float* parts = nullptr;
+  if (p.count_heads) CK(pool_alloc(ctx, &heads, p.spans));
+  CK(pool_alloc(ctx, &crossing, p.spans));
+  CK(pool_alloc(ctx, &parts, 2 * p.spans * dim));
+  a.heads = heads;
+  a.crossing = crossing;
+  a.parts = parts;
+  launch_embed_grad(a, p, ctx->stream);
+  CK(finish_out(ctx, &ok));
+  CK(finish_out(ctx, &orows));
+  CK(finish_out(ctx, &oc));
+  for (void* q : {(void*)ka, (void*)kb, (void*)va, (void*)vb, (void*)hist, (void*)copied, (void*)heads,
+                  (void*)crossing, (void*)parts, (void*)ids, (void*)ig.owned})
+    pool_free(ctx, q);
+  return check_launch(ctx, "embed_grad");
+}
+
+adapm_status adapm_grad_norm(adapm_ctx* ctx, const adapm_tensor* grads, uint64_t n, float scale, float* norm) {
+  adapm_status st = check_ctx(ctx);
+  if (st != ADAPM_OK) return st;
+  st = check_tensors(ctx, grads, n, "grads");
+  if (st != ADAPM_OK) return st;
+  if (!norm) return fail(ctx, ADAPM_EINVAL, "null norm");
+  std::vector<GradTensor> t;
+  try {
+    t.reserve(n);
+  } catch (...) {
+    return fail(ctx, ADAPM_ENOMEM, "no host memory for %llu tensors", (unsigned long long)n);
+  }
+  for (uint64_t i = 0; i < n; ++i) t.push_back(grad_tensor(grads[i]));
+  ProfScope ps(ctx, 5);
+  Output<float> o;
+  CK(stage_out(ctx, norm, 1, &o));
+  double* part = nullptr;
+  CK(pool_alloc(ctx, &part, norm_scratch_doubles(n, ctx->sms)));
+  launch_grad_norm(t.data(), n, scale, part, o.dev, ctx->dstate, ctx->sms, ctx->stream);
+  pool_free(ctx, part);
+  CK(finish_out(ctx, &o));
+  return check_launch(ctx, "grad_norm");
+}
+
+adapm_status adapm_clip_grads(adapm_ctx* ctx, const adapm_tensor* grads, const adapm_tensor* outs, uint64_t n,
+                              float scale, float max_norm, const float* norm) {
+  adapm_status st = check_ctx(ctx);
+  if (st != ADAPM_OK) return st;
+  st = check_tensors(ctx, grads, n, "grads");
+  if (st == ADAPM_OK && outs) st = check_tensors(ctx, outs, n, "outs");
+  if (st != ADAPM_OK) return st;
+  if (!norm || !is_device_ptr(norm)) return fail(ctx, ADAPM_EINVAL, "norm is not a device word");
+  if (!(max_norm >= 0.f)) return fail(ctx, ADAPM_EINVAL, "max_norm must not be negative");
+  std::vector<GradTensor> t;
+  try {
+    t.reserve(n);
+  } catch (...) {
+    return fail(ctx, ADAPM_ENOMEM, "no host memory for %llu tensors", (unsigned long long)n);
+  }
+  for (uint64_t i = 0; i < n; ++i) {
+    t.push_back(grad_tensor(grads[i]));
+    if (!outs) continue;
+    const unsigned long long at = i;
+    if (outs[i].count != grads[i].count) return fail(ctx, ADAPM_EINVAL, "outs[%llu] has another count", at);
+    if (outs[i].data == grads[i].data && outs[i].type != grads[i].type && grads[i].count > 0)
+      return fail(ctx, ADAPM_EINVAL, "outs[%llu] is its gradient in another type", at);
+    t.back().out = static_cast<char*>(outs[i].data);
+    t.back().out_type = (uint8_t)outs[i].type;
+  }
+  if (n == 0) return ADAPM_OK;
+  ProfScope ps(ctx, 5);
+  launch_clip_grads(t.data(), n, scale, max_norm, norm, outs == nullptr, ctx->sms, ctx->stream);
+  return check_launch(ctx, "clip_grads");
+}
+
+adapm_status adapm_push_grads(adapm_ctx* ctx, uint32_t worker, const uint32_t* keys, const float* rows, uint64_t n,
+                              uint32_t dim, int adagrad, float lr, float eps, float scale, float max_norm,
+                              const float* norm) {
+  adapm_status st = check_ctx(ctx);
+  if (st != ADAPM_OK) return st;
+  if (worker >= ctx->s.W) return fail(ctx, ADAPM_EINVAL, "worker %u >= %u", worker, ctx->s.W);
+  if (n > kMaxN || (n > 0 && (!keys || !rows))) return fail(ctx, ADAPM_EINVAL, "bad pointers/n");
+  if (dim == 0 || (adagrad ? 2 * (uint64_t)dim != ctx->s.D : dim > ctx->s.D))
+    return fail(ctx, ADAPM_EINVAL, "dim %u does not match value_len %u", dim, ctx->s.D);
+  // (theta and accumulators are read and written as float4 halves of a row)
+  if (adagrad && dim % 4 != 0) return fail(ctx, ADAPM_EINVAL, "dim %u: need a multiple of 4 with AdaGrad", dim);
+  if (norm && !is_device_ptr(norm)) return fail(ctx, ADAPM_EINVAL, "norm is not a device word");
+  if (norm && !(max_norm >= 0.f)) return fail(ctx, ADAPM_EINVAL, "max_norm must not be negative");
+  if (n == 0) return ADAPM_OK;
+  Input<uint32_t> ik;
+  Input<float> ir;
+  CK(stage_in(ctx, keys, n, &ik));
+  CK(stage_in(ctx, rows, n * dim, &ir));
+  CK(stage_join(ctx));
+  st = early_make(ctx, worker);
+  if (st != ADAPM_OK) return st;
+  RowUpdate u{};
+  u.keys = ik.dev;
+  u.rows = ir.dev;
+  u.n = n;
+  u.dim = dim;
+  u.worker = worker;
+  u.adagrad = adagrad != 0;
+  u.lr = lr;
+  u.eps = eps;
+  u.scale = scale;
+  u.max_norm = max_norm;
+  u.norm = norm;
+  {
+    ProfScope ps(ctx, 3);
+    launch_push_grads(ctx->s, u, ctx->sms, ctx->stream);
+  }
+  pool_free(ctx, ik.owned);
+  pool_free(ctx, ir.owned);
+  return check_launch(ctx, "push_grads");
 }
 
 adapm_status adapm_clock(adapm_ctx* ctx, uint32_t worker, int64_t* out) {

@@ -1,0 +1,462 @@
+// embed_grad: the gradient of an embedding lookup by sorted tokens.
+//
+//   rows[u] = scale * sum of grad[p] over the positions p with key keys[u]
+//
+// The (key, position) pairs come sorted.  They are cut into spans, a block
+// each, and a span into chunks, a row group each: a group walks its chunk's
+// rows with several loads in flight, keeps the running sum of the current key
+// in registers (fp32), and writes the sum of a key whose rows lie inside the
+// chunk straight to its place.  Keys cut by a chunk's end leave partial sums
+// in shared memory that the block adds in chunk order; keys that run past a
+// span leave theirs in memory and grad_combine adds them in span order.  So
+// each row is read once, each sum written once, a hot token's rows are spread
+// over many groups, and the order of every sum is fixed by the input alone.
+//
+// Where a sum goes: the index of its key among the distinct ones, which is the
+// number of keys that begin before it.  Per span that number comes from
+// grad_heads (one launch over the sorted keys, whose last block sums the
+// spans' counts up).
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "embed.cuh"
+#include "rowgroup.cuh"
+
+namespace adapm {
+
+namespace {
+
+constexpr int kGradSpan = 2048;   // sorted rows staged per block, at most
+
+// V elements of type T as they travel.
+template <int BYTES>
+struct Raw;
+template <>
+struct Raw<16> {
+  using type = uint4;
+};
+template <>
+struct Raw<8> {
+  using type = uint2;
+};
+template <>
+struct Raw<4> {
+  using type = uint32_t;
+};
+template <>
+struct Raw<2> {
+  using type = uint16_t;
+};
+template <class T, int V>
+using RawOf = typename Raw<(int)sizeof(T) * V>::type;
+
+__device__ __forceinline__ float as_float(float v) { return v; }
+__device__ __forceinline__ float as_float(__half v) { return __half2float(v); }
+__device__ __forceinline__ float as_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+
+template <class T, int V>
+__device__ __forceinline__ void add_raw(float (&sum)[V], const RawOf<T, V>& raw) {
+  const T* x = reinterpret_cast<const T*>(&raw);
+#pragma unroll
+  for (int j = 0; j < V; ++j) sum[j] += as_float(x[j]);
+}
+template <class T, int V>
+__device__ __forceinline__ void set_raw(float (&sum)[V], const RawOf<T, V>& raw) {
+  const T* x = reinterpret_cast<const T*>(&raw);
+#pragma unroll
+  for (int j = 0; j < V; ++j) sum[j] = as_float(x[j]);
+}
+// V floats to or from a row that begins on a multiple of min(V, 4) floats.
+template <int V>
+__device__ __forceinline__ void put_floats(float* p, const float (&x)[V], float scale) {
+  if constexpr (V % 4 == 0) {
+#pragma unroll
+    for (int j = 0; j < V; j += 4)
+      *reinterpret_cast<float4*>(p + j) =
+          make_float4(x[j] * scale, x[j + 1] * scale, x[j + 2] * scale, x[j + 3] * scale);
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j) p[j] = x[j] * scale;
+  }
+}
+template <int V>
+__device__ __forceinline__ void add_floats(float (&x)[V], const float* p) {
+  if constexpr (V % 4 == 0) {
+#pragma unroll
+    for (int j = 0; j < V; j += 4) {
+      const float4 v = *reinterpret_cast<const float4*>(p + j);
+      x[j] += v.x;
+      x[j + 1] += v.y;
+      x[j + 2] += v.z;
+      x[j + 3] += v.w;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j) x[j] += p[j];
+  }
+}
+
+// Whether a sort before gave up, or which arrays hold the sorted pairs.
+__device__ __forceinline__ bool grad_resolve(GradArgs& a) {
+  if (sort_failed(a.st)) return false;
+  if (a.plan_word != nullptr && *a.plan_word == a.plan_seq) {
+    a.skeys = a.alt_keys;
+    a.spos = a.alt_pos;
+  }
+  return true;
+}
+__device__ __forceinline__ bool grad_valid(const GradArgs& a, uint32_t k) { return k < a.K && k != a.pad_key; }
+
+// heads[b] = distinct keys that begin in spans before b; *count = all.
+__global__ void __launch_bounds__(kThreads) grad_heads_kernel(const GradArgs args, uint32_t span, uint32_t spans) {
+  after_previous();
+  GradArgs a = args;
+  if (!grad_resolve(a)) return;
+  __shared__ bool last;
+  for (uint32_t b = blockIdx.x; b < spans; b += gridDim.x) {
+    const uint64_t p0 = (uint64_t)b * span;
+    const uint64_t p1 = p0 + span < a.n ? p0 + span : a.n;
+    uint32_t heads = 0, unused = 0;
+    for (uint64_t p = p0 + threadIdx.x; p < p1; p += kThreads) {
+      const uint32_t k = a.skeys[p];
+      heads += grad_valid(a, k) && (p == 0 || a.skeys[p - 1] != k) ? 1u : 0u;
+    }
+    block_sum2(heads, unused);
+    if (threadIdx.x == 0) a.heads[b] = heads;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) {
+    __threadfence();
+    last = atomicAdd(&a.st->grad_done, 1u) == gridDim.x - 1;
+    __threadfence();
+  }
+  __syncthreads();
+  if (!last) return;
+  uint32_t run = 0;
+  for (uint32_t b0 = 0; b0 < spans; b0 += kThreads) {
+    const uint32_t b = b0 + threadIdx.x;
+    uint32_t h = b < spans ? __ldcg(a.heads + b) : 0u, unused = 0, total, none;
+    block_exclusive_scan2(h, unused, total, none);
+    if (b < spans) a.heads[b] = run + h;
+    run += total;
+  }
+  if (threadIdx.x == 0) {
+    *a.count = run;
+    a.st->grad_done = 0u;
+  }
+}
+
+// Dynamic shared memory of grad_sum: head and tail piece of every chunk, then
+// the span's keys (with the one before and the one after), rows and flags.
+template <int C, int V>
+constexpr size_t grad_smem() {
+  return 2 * (size_t)kThreads * C * V * sizeof(float) +
+         kGradSpan * (sizeof(int64_t) + sizeof(uint32_t) + sizeof(uint8_t)) + (kGradSpan + 2) * sizeof(uint32_t);
+}
+
+// Row flags: the first of its key in its chunk; the last of its key, or of the
+// chunk; the key begins in the chunk; it ends at this row; the row counts.
+constexpr uint8_t kBegin = 1, kEnd = 2, kStarted = 4, kLast = 8, kCounts = 16;
+
+template <class T, int V, int G, int C, int R>
+__global__ void __launch_bounds__(kThreads, C * V >= 24 ? 2 : 3) grad_sum_kernel(const GradArgs args) {
+  after_previous();
+  GradArgs a = args;
+  if (!grad_resolve(a)) return;
+  constexpr int NG = kThreads / G;
+  const uint32_t CH = a.chunk, span = NG * CH;
+  extern __shared__ __align__(16) unsigned char dsm[];
+  float* ph = reinterpret_cast<float*>(dsm);                 // head piece of each chunk
+  float* pt = ph + kThreads * C * V;                         // tail piece of each chunk
+  int64_t* so = reinterpret_cast<int64_t*>(pt + kThreads * C * V);   // first element of each row
+  uint32_t* su = reinterpret_cast<uint32_t*>(so + kGradSpan);        // index of its key among the distinct ones
+  uint32_t* sk = su + kGradSpan;                             // sk[0]: key before the span; sk[1 + len]: after it
+  uint8_t* sf = reinterpret_cast<uint8_t*>(sk + kGradSpan + 2);
+  const int lane = threadIdx.x & (G - 1);
+  const uint32_t gi = threadIdx.x / G;
+  const uint32_t nv = (a.dim + V - 1) / V;
+  const T* grad = reinterpret_cast<const T*>(a.grad.data);
+  const uint64_t P0 = (uint64_t)blockIdx.x * span;
+  const uint32_t len = (uint32_t)(a.n - P0 < (uint64_t)span ? a.n - P0 : span);
+  for (uint32_t i = threadIdx.x; i < len; i += kThreads) sk[1 + i] = a.skeys[P0 + i];
+  if (threadIdx.x == 0) {
+    sk[0] = P0 > 0 ? a.skeys[P0 - 1] : kNoKey;
+    sk[1 + len] = P0 + len < a.n ? a.skeys[P0 + len] : kNoKey;
+  }
+  uint32_t first, total;   // distinct keys that begin before the span; in all
+  if (a.heads != nullptr) {
+    first = a.heads[blockIdx.x];
+    total = *a.count;
+  } else {
+    __shared__ uint32_t both[2];
+    uint32_t below = 0, all = 0;
+    for (uint64_t p = threadIdx.x; p < a.n; p += kThreads) {
+      const uint32_t k = a.skeys[p];
+      const uint32_t h = grad_valid(a, k) && (p == 0 || a.skeys[p - 1] != k) ? 1u : 0u;
+      all += h;
+      if (p < P0) below += h;
+    }
+    block_sum2(below, all);
+    if (threadIdx.x == 0) {
+      both[0] = below;
+      both[1] = all;
+      if (blockIdx.x == 0) *a.count = all;
+    }
+    __syncthreads();
+    first = both[0];
+    total = both[1];
+  }
+  __syncthreads();
+  bool wrong = false;
+  for (uint32_t i0 = 0; i0 < len; i0 += kThreads) {   // block-uniform
+    const uint32_t i = i0 + threadIdx.x;
+    const bool in = i < len;
+    const uint32_t k = in ? sk[1 + i] : kNoKey;
+    const bool counts = in && grad_valid(a, k);
+    const uint32_t head = counts && sk[i] != k ? 1u : 0u;   // (sk[0] is kNoKey in front of the first)
+    uint32_t before = head, unused = 0, heads, none;
+    block_exclusive_scan2(before, unused, heads, none);
+    if (in) {
+      uint8_t f = 0;
+      const uint32_t pos = a.spos[P0 + i];
+      if (counts && pos < a.n) {
+        const uint32_t cs = i - i % CH, ce = cs + CH < len ? cs + CH : len;
+        const bool ends = sk[2 + i] != k;
+        f = kCounts | (head || i == cs ? kBegin : 0) | (ends || i + 1 == ce ? kEnd : 0) |
+            (sk[cs] != k ? kStarted : 0) | (ends ? kLast : 0);
+        so[i] = row_offset(a.grad, pos);
+      } else if (counts || (k >= a.K && k != kNoKey)) {
+        wrong = true;
+      }
+      sf[i] = f;
+      const uint32_t u = first + before + head - 1;
+      su[i] = u;
+      if (head) a.keys[u] = k;
+      if (i + 1 == len) a.crossing[blockIdx.x] = u;
+      if (P0 + i >= total) a.keys[P0 + i] = kNoKey;
+    }
+    first += heads;
+  }
+  if (__syncthreads_or(wrong) && threadIdx.x == 0) set_error(a.st, ERR_INTERNAL);
+  const uint32_t p0 = gi * CH < len ? gi * CH : len;
+  const uint32_t p1 = p0 + CH < len ? p0 + CH : len;
+  float run[C][V];
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+#pragma unroll
+    for (int j = 0; j < V; ++j) run[c][j] = 0.f;
+  for (uint32_t p = p0; p < p1; p += R) {
+    RawOf<T, V> d[R][C];
+    uint8_t f[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      f[r] = p + r < p1 ? sf[p + r] : 0;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const uint32_t q = lane + c * G;
+        if ((f[r] & kCounts) && q < nv)
+          d[r][c] = *reinterpret_cast<const RawOf<T, V>*>(grad + so[p + r] + (int64_t)q * V);
+        else
+          d[r][c] = RawOf<T, V>{};
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (!(f[r] & kCounts)) continue;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        if (f[r] & kBegin) set_raw<T, V>(run[c], d[r][c]);
+        else add_raw<T, V>(run[c], d[r][c]);
+      }
+      if (!(f[r] & kEnd)) continue;
+      if ((f[r] & (kStarted | kLast)) == (kStarted | kLast)) {
+        float* row = a.rows + (uint64_t)su[p + r] * a.dim;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          const uint32_t q = lane + c * G;
+          if (q < nv) put_floats<V>(row + q * V, run[c], a.scale);
+        }
+      } else {   // a chunk has at most one head and one tail piece
+        float* piece = ((f[r] & kStarted) ? pt : ph) + gi * G * C * V;
+#pragma unroll
+        for (int c = 0; c < C; ++c) put_floats<V>(piece + (lane + c * G) * V, run[c], 1.f);
+      }
+    }
+  }
+  __syncthreads();
+  // A key that begins in chunk gi and goes on is summed here by group gi: its
+  // tail piece, then the head pieces of the chunks it covers.
+  const uint32_t nch = (len + CH - 1) / CH;
+  auto chunk_end = [&](uint32_t m) { return (m + 1) * CH < len ? (m + 1) * CH : len; };
+  auto walk = [&](uint32_t m, uint32_t kk, bool& out) {   // last chunk from m on that kk covers; past the span?
+    while (true) {
+      const uint32_t e = chunk_end(m);
+      const bool through = sk[e] == kk && sk[1 + e] == kk;
+      if (!through || m + 1 >= nch) {
+        out = through;
+        return m;
+      }
+      ++m;
+    }
+  };
+  auto add_pieces = [&](uint32_t m0, uint32_t m1) {
+    for (uint32_t m = m0; m <= m1; ++m)
+#pragma unroll
+      for (int c = 0; c < C; ++c) add_floats<V>(run[c], ph + (m * G * C + lane + c * G) * V);
+  };
+  auto put_row = [&](float* row, float scale) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const uint32_t q = lane + c * G;
+      if (q < nv) put_floats<V>(row + q * V, run[c], scale);
+    }
+  };
+  auto zero_run = [&]() {
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int j = 0; j < V; ++j) run[c][j] = 0.f;
+  };
+  if (gi < nch) {
+    const uint32_t kl = sk[p1];   // the chunk's last row
+    if (grad_valid(a, kl) && sk[1 + p1] == kl && sk[p0] != kl) {
+      bool out = true;
+      const uint32_t m1 = gi + 1 < nch ? walk(gi + 1, kl, out) : gi;
+      zero_run();
+#pragma unroll
+      for (int c = 0; c < C; ++c) add_floats<V>(run[c], pt + (gi * G * C + lane + c * G) * V);
+      add_pieces(gi + 1, m1);
+      if (out) put_row(a.parts + (2 * (uint64_t)blockIdx.x + 1) * a.dim, 1.f);
+      else put_row(a.rows + (uint64_t)su[p1 - 1] * a.dim, a.scale);
+    }
+  }
+  if (gi == 0 && sk[0] == sk[1] && grad_valid(a, sk[1])) {   // the span's first key began before it
+    bool out = false;
+    const uint32_t m1 = walk(0, sk[1], out);
+    zero_run();
+    add_pieces(0, m1);
+    put_row(a.parts + 2 * (uint64_t)blockIdx.x * a.dim, 1.f);
+  }
+}
+
+// Keys that run past a span: the tail piece of the span where one begins plus
+// the head pieces of the spans that it continues into, in order.  One block
+// per span, a thread per column.
+__global__ void __launch_bounds__(kThreads) grad_combine_kernel(const GradArgs args, uint32_t span, uint32_t spans) {
+  after_previous();
+  GradArgs a = args;
+  if (!grad_resolve(a)) return;
+  for (uint32_t b = blockIdx.x; b + 1 < spans; b += gridDim.x) {   // block-uniform
+    const uint64_t st = (uint64_t)b * span, en = st + span;
+    const uint32_t kl = a.skeys[en - 1];
+    if (!grad_valid(a, kl) || a.skeys[en] != kl) continue;
+    if (st > 0 && a.skeys[st - 1] == kl) continue;   // it began in an earlier span
+    // the last span whose first row has the key: those after b that do are a prefix
+    uint32_t lo = b + 1;
+    for (uint32_t m0 = b + 2; m0 < spans; m0 += kThreads) {
+      const uint32_t m = m0 + threadIdx.x;
+      const int same = __syncthreads_count(m < spans && a.skeys[(uint64_t)m * span] == kl);
+      lo += (uint32_t)same;
+      if (same < kThreads) break;
+    }
+    float* row = a.rows + (uint64_t)a.crossing[b] * a.dim;
+    for (uint32_t c = threadIdx.x; c < a.dim; c += kThreads) {
+      float sum = a.parts[(2 * (uint64_t)b + 1) * a.dim + c];
+      for (uint32_t m = b + 1; m <= lo; ++m) sum += a.parts[2 * (uint64_t)m * a.dim + c];
+      row[c] = sum * a.scale;
+    }
+  }
+}
+
+// Lanes per row group and vectors of a row per lane.
+template <int V, class F>
+void dispatch_grad(uint32_t nv, F&& f) {
+  if (nv <= 4) f(std::integral_constant<int, 4>{}, std::integral_constant<int, 1>{});
+  else if (nv <= 8) f(std::integral_constant<int, 8>{}, std::integral_constant<int, 1>{});
+  else if (nv <= 16) f(std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{});
+  else if (nv <= 32) f(std::integral_constant<int, 32>{}, std::integral_constant<int, 1>{});
+  else if (nv <= 64) f(std::integral_constant<int, 32>{}, std::integral_constant<int, 2>{});
+  else if (nv <= 96) f(std::integral_constant<int, 32>{}, std::integral_constant<int, 3>{});
+  else if (V >= 8 || nv <= 128) f(std::integral_constant<int, 32>{}, std::integral_constant<int, 4>{});
+  else if constexpr (V < 8) {
+    if (V >= 4 || nv <= 256) f(std::integral_constant<int, 32>{}, std::integral_constant<int, 8>{});
+    else if constexpr (V < 4) {
+      if (nv <= 512) f(std::integral_constant<int, 32>{}, std::integral_constant<int, 16>{});
+      else f(std::integral_constant<int, 32>{}, std::integral_constant<int, 32>{});
+    }
+  }
+}
+
+// Elements a lane loads at a time: the most that every row's start and length
+// are a multiple of.
+template <class T>
+int grad_vector(const GradArgs& a) {
+  for (int v = 16 / (int)sizeof(T); v >= 4; v /= 2) {
+    if (reinterpret_cast<uintptr_t>(a.grad.data) % (v * sizeof(T)) == 0 && a.dim % v == 0 &&
+        a.grad.inner_stride % v == 0 && (a.grad.flat || a.grad.outer_stride % v == 0) &&
+        reinterpret_cast<uintptr_t>(a.rows) % 16 == 0)
+      return v;
+  }
+  return 1;
+}
+
+template <class T, class F>
+void dispatch_grad_args(const GradArgs& a, F&& f) {
+  const int v = grad_vector<T>(a);
+  auto by_v = [&](auto Vc) {
+    constexpr int V = decltype(Vc)::value;
+    dispatch_grad<V>((a.dim + V - 1) / V, [&](auto Gc, auto Cc) { f(Vc, Gc, Cc); });
+  };
+  if constexpr (sizeof(T) == 2)
+    if (v == 8) return by_v(std::integral_constant<int, 8>{});
+  if (v >= 4) return by_v(std::integral_constant<int, 4>{});
+  by_v(std::integral_constant<int, 1>{});
+}
+
+template <class T>
+GradPlan grad_plan_typed(const GradArgs& a, int sms) {
+  GradPlan p{};
+  dispatch_grad_args<T>(a, [&](auto Vc, auto Gc, auto Cc) {
+    constexpr int V = decltype(Vc)::value, G = decltype(Gc)::value, C = decltype(Cc)::value;
+    constexpr uint64_t NG = kThreads / G, most = kGradSpan / NG;
+    // one span per resident block, or as few full waves of them as spans allow
+    const uint64_t groups = NG * (uint64_t)sms * (C * V >= 24 ? 2 : 3);
+    const uint64_t waves = (a.n + groups * most - 1) / (groups * most);
+    uint64_t ch = (a.n + groups * waves - 1) / (groups * waves);
+    if (ch < 4) ch = 4;
+    if (ch > most) ch = most;
+    p.chunk = (uint32_t)ch;
+    p.spans = (a.n + NG * ch - 1) / (NG * ch);
+  });
+  p.count_heads = a.n > kCountSort;
+  return p;
+}
+
+template <class T>
+void launch_grad_typed(const GradArgs& a, const GradPlan& p, cudaStream_t stream) {
+  dispatch_grad_args<T>(a, [&](auto Vc, auto Gc, auto Cc) {
+    constexpr int V = decltype(Vc)::value, G = decltype(Gc)::value, C = decltype(Cc)::value;
+    constexpr int R = 8 / C > 0 ? 8 / C : 1;
+    const uint32_t span = p.chunk * (kThreads / G), spans = (uint32_t)p.spans;
+    note_launches((p.count_heads ? 1 : 0) + (spans > 1 ? 2 : 1));
+    if (p.count_heads)
+      launch_after(grad_heads_kernel, spans < 1024 ? spans : 1024u, kThreads, 0, stream, a, span, spans);
+    constexpr size_t smem = grad_smem<C, V>();
+    // the kernel's dynamic shared-memory limit is a per-device attribute
+    static bool attr_set[64] = {false};
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (dev < 0 || dev >= 64 || !attr_set[dev]) {
+      cudaFuncSetAttribute(grad_sum_kernel<T, V, G, C, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+      if (dev >= 0 && dev < 64) attr_set[dev] = true;
+    }
+    launch_after(grad_sum_kernel<T, V, G, C, R>, spans, kThreads, smem, stream, a);
+    if (spans > 1)
+      launch_after(grad_combine_kernel, spans < 2048 ? spans : 2048u, kThreads, 0, stream, a, span, spans);
+  });
+}
+
+}  // namespace
+}  // namespace adapm

@@ -40,6 +40,7 @@ enum ErrBits : uint32_t {
   ERR_TIMEOUT = 8u,     // a bounded wait on another block gave up
   ERR_INTERNAL = 16u,   // an index read from the library's own scratch or lists was out of
                         // range: the element was skipped instead of accessed
+  ERR_KEY_ORDER = 32u,  // the keys of a row update are not distinct and ascending
 };
 
 struct DevState {
@@ -62,6 +63,8 @@ struct DevState {
   uint32_t sync_done;     // blocks of a sync that finished (0 between syncs)
   uint32_t ev_done;       // blocks of the closing events launch that finished (0 between advances)
   uint32_t loss_done;     // blocks of a training step that finished (0 between steps)
+  uint32_t grad_done;     // blocks of embed_grad's key count that finished (0 between calls)
+  uint32_t norm_done;     // blocks of a gradient norm that finished (0 between calls)
   unsigned long long push_rows;       // rows pushed (cumulative)
   unsigned long long push_unique;     // distinct keys over all pushes (cumulative)
   unsigned long long sync_keys;       // keys merged by sync (cumulative)
