@@ -73,7 +73,7 @@ struct GradArgs {
   float* rows;        // out
   uint32_t* count;    // out
   uint32_t chunk;     // rows a group sums, of a span of (groups per block) chunks
-  uint32_t* heads;    // per span: distinct keys that begin in spans before it; null: counted where they are needed
+  uint32_t* heads;    // per span: distinct keys that begin in it; null: counted where they are needed
   uint32_t* crossing; // per span: index of the key whose rows run past its end
   float* parts;       // per span: a head and a tail row of `dim` floats
   DevState* st;

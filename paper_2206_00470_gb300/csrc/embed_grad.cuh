@@ -13,13 +13,15 @@
 // over many groups, and the order of every sum is fixed by the input alone.
 //
 // Where a sum goes: the index of its key among the distinct ones, which is the
-// number of keys that begin before it.  Per span that number comes from
-// grad_heads (one launch over the sorted keys, whose last block sums the
-// spans' counts up).
+// number of keys that begin before it: grad_heads counts those of each span,
+// and a block of grad_sum adds the counts of the spans before its own (of a few
+// thousand keys it counts them itself, which saves the launch).
 #pragma once
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
+
+#include <algorithm>
 
 #include "embed.cuh"
 #include "rowgroup.cuh"
@@ -29,6 +31,7 @@ namespace adapm {
 namespace {
 
 constexpr int kGradSpan = 2048;   // sorted rows staged per block, at most
+constexpr int kGradBlocks = 3;    // grad_sum blocks per SM
 
 // V elements of type T as they travel.
 template <int BYTES>
@@ -109,43 +112,56 @@ __device__ __forceinline__ bool grad_resolve(GradArgs& a) {
 }
 __device__ __forceinline__ bool grad_valid(const GradArgs& a, uint32_t k) { return k < a.K && k != a.pad_key; }
 
-// heads[b] = distinct keys that begin in spans before b; *count = all.
-__global__ void __launch_bounds__(kThreads) grad_heads_kernel(const GradArgs args, uint32_t span, uint32_t spans) {
+// heads[b] = distinct keys that begin in span b.
+__global__ void __launch_bounds__(kThreads) grad_heads_kernel(const GradArgs args, uint32_t span) {
   after_previous();
   GradArgs a = args;
   if (!grad_resolve(a)) return;
-  __shared__ bool last;
-  for (uint32_t b = blockIdx.x; b < spans; b += gridDim.x) {
-    const uint64_t p0 = (uint64_t)b * span;
-    const uint64_t p1 = p0 + span < a.n ? p0 + span : a.n;
-    uint32_t heads = 0, unused = 0;
-    for (uint64_t p = p0 + threadIdx.x; p < p1; p += kThreads) {
-      const uint32_t k = a.skeys[p];
-      heads += grad_valid(a, k) && (p == 0 || a.skeys[p - 1] != k) ? 1u : 0u;
+  const uint64_t p0 = (uint64_t)blockIdx.x * span;
+  const uint64_t p1 = p0 + span < a.n ? p0 + span : a.n;
+  uint32_t heads = 0, unused = 0;
+  for (uint64_t p = p0 + threadIdx.x; p < p1; p += kThreads) {
+    const uint32_t k = a.skeys[p];
+    heads += grad_valid(a, k) && (p == 0 || a.skeys[p - 1] != k) ? 1u : 0u;
+  }
+  block_sum2(heads, unused);
+  if (threadIdx.x == 0) a.heads[blockIdx.x] = heads;
+}
+
+// Distinct keys that begin before span b, and in all (to every thread of the
+// block): from the spans' counts, or from the keys themselves where there are
+// few.
+__device__ __forceinline__ uint2 grad_ranks(const GradArgs& a, uint32_t b, uint32_t spans, uint64_t P0) {
+  __shared__ uint2 both;
+  uint32_t below = 0, all = 0;
+  if (a.heads != nullptr) {
+    for (uint32_t m = threadIdx.x; m < spans; m += kThreads) {
+      const uint32_t h = a.heads[m];
+      all += h;
+      if (m < b) below += h;
     }
-    block_sum2(heads, unused);
-    if (threadIdx.x == 0) a.heads[b] = heads;
-    __syncthreads();
+  } else {
+    const uint32_t n = (uint32_t)a.n;
+    auto count = [&](uint32_t p, uint32_t k, uint32_t prev) {
+      const uint32_t h = grad_valid(a, k) && prev != k ? 1u : 0u;
+      all += h;
+      if (p < P0) below += h;
+    };
+#pragma unroll 4
+    for (uint32_t p = 4 * threadIdx.x; p + 4 <= n; p += 4 * kThreads) {
+      const uint4 v = *reinterpret_cast<const uint4*>(a.skeys + p);
+      count(p, v.x, p > 0 ? a.skeys[p - 1] : kNoKey);
+      count(p + 1, v.y, v.x);
+      count(p + 2, v.z, v.y);
+      count(p + 3, v.w, v.z);
+    }
+    const uint32_t p = n / 4 * 4 + threadIdx.x;
+    if (p < n) count(p, a.skeys[p], p > 0 ? a.skeys[p - 1] : kNoKey);
   }
-  if (threadIdx.x == 0) {
-    __threadfence();
-    last = atomicAdd(&a.st->grad_done, 1u) == gridDim.x - 1;
-    __threadfence();
-  }
+  block_sum2(below, all);
+  if (threadIdx.x == 0) both = make_uint2(below, all);
   __syncthreads();
-  if (!last) return;
-  uint32_t run = 0;
-  for (uint32_t b0 = 0; b0 < spans; b0 += kThreads) {
-    const uint32_t b = b0 + threadIdx.x;
-    uint32_t h = b < spans ? __ldcg(a.heads + b) : 0u, unused = 0, total, none;
-    block_exclusive_scan2(h, unused, total, none);
-    if (b < spans) a.heads[b] = run + h;
-    run += total;
-  }
-  if (threadIdx.x == 0) {
-    *a.count = run;
-    a.st->grad_done = 0u;
-  }
+  return both;
 }
 
 // Dynamic shared memory of grad_sum: head and tail piece of every chunk, then
@@ -160,8 +176,10 @@ constexpr size_t grad_smem() {
 // chunk; the key begins in the chunk; it ends at this row; the row counts.
 constexpr uint8_t kBegin = 1, kEnd = 2, kStarted = 4, kLast = 8, kCounts = 16;
 
+// Blocks of one span are next to each other, one per tile of columns.
 template <class T, int V, int G, int C, int R>
-__global__ void __launch_bounds__(kThreads, C * V >= 24 ? 2 : 3) grad_sum_kernel(const GradArgs args) {
+__global__ void __launch_bounds__(kThreads, kGradBlocks) grad_sum_kernel(const GradArgs args, uint32_t spans,
+                                                                         uint32_t tiles, uint32_t tile) {
   after_previous();
   GradArgs a = args;
   if (!grad_resolve(a)) return;
@@ -176,39 +194,22 @@ __global__ void __launch_bounds__(kThreads, C * V >= 24 ? 2 : 3) grad_sum_kernel
   uint8_t* sf = reinterpret_cast<uint8_t*>(sk + kGradSpan + 2);
   const int lane = threadIdx.x & (G - 1);
   const uint32_t gi = threadIdx.x / G;
-  const uint32_t nv = (a.dim + V - 1) / V;
-  const T* grad = reinterpret_cast<const T*>(a.grad.data);
-  const uint64_t P0 = (uint64_t)blockIdx.x * span;
+  const uint32_t b = blockIdx.x / tiles, q0 = (blockIdx.x - b * tiles) * tile;   // first vector of the tile
+  const uint32_t nv = (a.dim + V - 1) / V - q0 < tile ? (a.dim + V - 1) / V - q0 : tile;
+  const T* grad = reinterpret_cast<const T*>(a.grad.data) + q0 * V;
+  float* rows = a.rows + q0 * V;
+  float* parts = a.parts + q0 * V;
+  const uint64_t P0 = (uint64_t)b * span;
   const uint32_t len = (uint32_t)(a.n - P0 < (uint64_t)span ? a.n - P0 : span);
   for (uint32_t i = threadIdx.x; i < len; i += kThreads) sk[1 + i] = a.skeys[P0 + i];
   if (threadIdx.x == 0) {
     sk[0] = P0 > 0 ? a.skeys[P0 - 1] : kNoKey;
     sk[1 + len] = P0 + len < a.n ? a.skeys[P0 + len] : kNoKey;
   }
-  uint32_t first, total;   // distinct keys that begin before the span; in all
-  if (a.heads != nullptr) {
-    first = a.heads[blockIdx.x];
-    total = *a.count;
-  } else {
-    __shared__ uint32_t both[2];
-    uint32_t below = 0, all = 0;
-    for (uint64_t p = threadIdx.x; p < a.n; p += kThreads) {
-      const uint32_t k = a.skeys[p];
-      const uint32_t h = grad_valid(a, k) && (p == 0 || a.skeys[p - 1] != k) ? 1u : 0u;
-      all += h;
-      if (p < P0) below += h;
-    }
-    block_sum2(below, all);
-    if (threadIdx.x == 0) {
-      both[0] = below;
-      both[1] = all;
-      if (blockIdx.x == 0) *a.count = all;
-    }
-    __syncthreads();
-    first = both[0];
-    total = both[1];
-  }
-  __syncthreads();
+  const uint2 ranks = grad_ranks(a, b, spans, P0);   // (a barrier: the keys are staged)
+  uint32_t first = ranks.x;
+  const uint32_t total = ranks.y;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.count = total;
   bool wrong = false;
   for (uint32_t i0 = 0; i0 < len; i0 += kThreads) {   // block-uniform
     const uint32_t i = i0 + threadIdx.x;
@@ -233,9 +234,11 @@ __global__ void __launch_bounds__(kThreads, C * V >= 24 ? 2 : 3) grad_sum_kernel
       sf[i] = f;
       const uint32_t u = first + before + head - 1;
       su[i] = u;
-      if (head) a.keys[u] = k;
-      if (i + 1 == len) a.crossing[blockIdx.x] = u;
-      if (P0 + i >= total) a.keys[P0 + i] = kNoKey;
+      if (q0 == 0) {
+        if (head) a.keys[u] = k;
+        if (i + 1 == len) a.crossing[b] = u;
+        if (P0 + i >= total) a.keys[P0 + i] = kNoKey;
+      }
     }
     first += heads;
   }
@@ -272,7 +275,7 @@ __global__ void __launch_bounds__(kThreads, C * V >= 24 ? 2 : 3) grad_sum_kernel
       }
       if (!(f[r] & kEnd)) continue;
       if ((f[r] & (kStarted | kLast)) == (kStarted | kLast)) {
-        float* row = a.rows + (uint64_t)su[p + r] * a.dim;
+        float* row = rows + (uint64_t)su[p + r] * a.dim;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
           const uint32_t q = lane + c * G;
@@ -328,8 +331,8 @@ __global__ void __launch_bounds__(kThreads, C * V >= 24 ? 2 : 3) grad_sum_kernel
 #pragma unroll
       for (int c = 0; c < C; ++c) add_floats<V>(run[c], pt + (gi * G * C + lane + c * G) * V);
       add_pieces(gi + 1, m1);
-      if (out) put_row(a.parts + (2 * (uint64_t)blockIdx.x + 1) * a.dim, 1.f);
-      else put_row(a.rows + (uint64_t)su[p1 - 1] * a.dim, a.scale);
+      if (out) put_row(parts + (2 * (uint64_t)b + 1) * a.dim, 1.f);
+      else put_row(rows + (uint64_t)su[p1 - 1] * a.dim, a.scale);
     }
   }
   if (gi == 0 && sk[0] == sk[1] && grad_valid(a, sk[1])) {   // the span's first key began before it
@@ -337,55 +340,100 @@ __global__ void __launch_bounds__(kThreads, C * V >= 24 ? 2 : 3) grad_sum_kernel
     const uint32_t m1 = walk(0, sk[1], out);
     zero_run();
     add_pieces(0, m1);
-    put_row(a.parts + 2 * (uint64_t)blockIdx.x * a.dim, 1.f);
+    put_row(parts + 2 * (uint64_t)b * a.dim, 1.f);
   }
 }
 
 // Keys that run past a span: the tail piece of the span where one begins plus
-// the head pieces of the spans that it continues into, in order.  One block
-// per span, a thread per column.
-__global__ void __launch_bounds__(kThreads) grad_combine_kernel(const GradArgs args, uint32_t span, uint32_t spans) {
+// the head pieces of the spans that it continues into.  A block per span and
+// tile of 32 vectors; its warps take the head pieces in strides, in increasing
+// order and several in flight, then the warps' sums are added in warp order.
+template <int V>
+__global__ void __launch_bounds__(kThreads) grad_combine_kernel(const GradArgs args, uint32_t span, uint32_t spans,
+                                                                uint32_t tiles) {
   after_previous();
   GradArgs a = args;
   if (!grad_resolve(a)) return;
-  for (uint32_t b = blockIdx.x; b + 1 < spans; b += gridDim.x) {   // block-uniform
-    const uint64_t st = (uint64_t)b * span, en = st + span;
-    const uint32_t kl = a.skeys[en - 1];
-    if (!grad_valid(a, kl) || a.skeys[en] != kl) continue;
-    if (st > 0 && a.skeys[st - 1] == kl) continue;   // it began in an earlier span
-    // the last span whose first row has the key: those after b that do are a prefix
-    uint32_t lo = b + 1;
-    for (uint32_t m0 = b + 2; m0 < spans; m0 += kThreads) {
-      const uint32_t m = m0 + threadIdx.x;
-      const int same = __syncthreads_count(m < spans && a.skeys[(uint64_t)m * span] == kl);
-      lo += (uint32_t)same;
-      if (same < kThreads) break;
+  constexpr int NW = kThreads / 32, UB = 8;
+  __shared__ float part[NW][32 * V];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+  const uint32_t b = blockIdx.x / tiles, c0 = ((blockIdx.x - b * tiles) * 32 + lane) * V;
+  const uint64_t st = (uint64_t)b * span, en = st + span;
+  // the keys around the span's end and before its start, and the first keys of
+  // the spans after it, in one latency
+  const uint32_t kl = a.skeys[en - 1], kn = a.skeys[en], kb = st > 0 ? a.skeys[st - 1] : kNoKey;
+  uint32_t kf = b + 1 + threadIdx.x < spans ? a.skeys[(uint64_t)(b + 1 + threadIdx.x) * span] : kNoKey;
+  const uint32_t u = a.crossing[b];
+  if (!grad_valid(a, kl) || kn != kl || kb == kl) return;   // (uniform) none, or it began in an earlier span
+  // the last span whose first row has the key: those after b that do are a prefix
+  uint32_t lo = b;
+  for (uint32_t m0 = b + 1; m0 < spans; m0 += kThreads) {
+    if (m0 > b + 1) kf = m0 + threadIdx.x < spans ? a.skeys[(uint64_t)(m0 + threadIdx.x) * span] : kNoKey;
+    const int same = __syncthreads_count(kf == kl);
+    lo += (uint32_t)same;
+    if (same < kThreads) break;
+  }
+  float sum[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) sum[j] = 0.f;
+  if (c0 < a.dim) {
+    for (uint32_t m0 = b + 1 + warp; m0 <= lo; m0 += NW * UB) {
+      float x[UB][V];
+#pragma unroll
+      for (int r = 0; r < UB; ++r) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[r][j] = 0.f;
+        if (m0 + r * NW <= lo) add_floats<V>(x[r], a.parts + 2 * (uint64_t)(m0 + r * NW) * a.dim + c0);
+      }
+#pragma unroll
+      for (int r = 0; r < UB; ++r)
+#pragma unroll
+        for (int j = 0; j < V; ++j) sum[j] += x[r][j];
     }
-    float* row = a.rows + (uint64_t)a.crossing[b] * a.dim;
-    for (uint32_t c = threadIdx.x; c < a.dim; c += kThreads) {
-      float sum = a.parts[(2 * (uint64_t)b + 1) * a.dim + c];
-      for (uint32_t m = b + 1; m <= lo; ++m) sum += a.parts[2 * (uint64_t)m * a.dim + c];
-      row[c] = sum * a.scale;
-    }
+  }
+#pragma unroll
+  for (int j = 0; j < V; ++j) part[warp][j * 32 + lane] = sum[j];
+  __syncthreads();
+  if (warp == 0 && c0 < a.dim) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum[j] = 0.f;
+    add_floats<V>(sum, a.parts + (2 * (uint64_t)b + 1) * a.dim + c0);
+#pragma unroll
+    for (int w = 0; w < NW; ++w)
+#pragma unroll
+      for (int j = 0; j < V; ++j) sum[j] += part[w][j * 32 + lane];
+    put_floats<V>(a.rows + (uint64_t)u * a.dim + c0, sum, a.scale);
   }
 }
 
-// Lanes per row group and vectors of a row per lane.
+// Columns are cut into tiles of at most 32 * most_vectors(V) vectors, so that a
+// lane's sums and the rows it has in flight leave registers for kGradBlocks
+// blocks per SM.  Few rows take one vector per lane (more, shorter blocks).
+constexpr int most_vectors(int V) { return V == 8 ? 2 : (V == 4 ? 4 : 8); }
+constexpr uint64_t kFewRows = 4096;
+
+struct GradTiles {
+  uint32_t tiles, tile;   // of so many vectors
+};
+template <int V>
+GradTiles grad_tiles(const GradArgs& a) {
+  const uint32_t nv = (a.dim + V - 1) / V, most = 32 * (a.n <= kFewRows ? 1 : most_vectors(V));
+  const uint32_t tiles = (nv + most - 1) / most;
+  return {tiles, (nv + tiles - 1) / tiles};
+}
+
+// Lanes per row group and vectors of a tile's row per lane.
 template <int V, class F>
-void dispatch_grad(uint32_t nv, F&& f) {
-  if (nv <= 4) f(std::integral_constant<int, 4>{}, std::integral_constant<int, 1>{});
-  else if (nv <= 8) f(std::integral_constant<int, 8>{}, std::integral_constant<int, 1>{});
-  else if (nv <= 16) f(std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{});
-  else if (nv <= 32) f(std::integral_constant<int, 32>{}, std::integral_constant<int, 1>{});
-  else if (nv <= 64) f(std::integral_constant<int, 32>{}, std::integral_constant<int, 2>{});
-  else if (nv <= 96) f(std::integral_constant<int, 32>{}, std::integral_constant<int, 3>{});
-  else if (V >= 8 || nv <= 128) f(std::integral_constant<int, 32>{}, std::integral_constant<int, 4>{});
+void dispatch_grad(uint32_t tile, F&& f) {
+  if (tile <= 4) f(std::integral_constant<int, 4>{}, std::integral_constant<int, 1>{});
+  else if (tile <= 8) f(std::integral_constant<int, 8>{}, std::integral_constant<int, 1>{});
+  else if (tile <= 16) f(std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{});
+  else if (tile <= 32) f(std::integral_constant<int, 32>{}, std::integral_constant<int, 1>{});
+  else if (tile <= 64) f(std::integral_constant<int, 32>{}, std::integral_constant<int, 2>{});
   else if constexpr (V < 8) {
-    if (V >= 4 || nv <= 256) f(std::integral_constant<int, 32>{}, std::integral_constant<int, 8>{});
-    else if constexpr (V < 4) {
-      if (nv <= 512) f(std::integral_constant<int, 32>{}, std::integral_constant<int, 16>{});
-      else f(std::integral_constant<int, 32>{}, std::integral_constant<int, 32>{});
-    }
+    if (V >= 4 && tile <= 96) f(std::integral_constant<int, 32>{}, std::integral_constant<int, 3>{});
+    else if (tile <= 128) f(std::integral_constant<int, 32>{}, std::integral_constant<int, 4>{});
+    else if constexpr (V < 4) f(std::integral_constant<int, 32>{}, std::integral_constant<int, 8>{});
   }
 }
 
@@ -406,8 +454,8 @@ template <class T, class F>
 void dispatch_grad_args(const GradArgs& a, F&& f) {
   const int v = grad_vector<T>(a);
   auto by_v = [&](auto Vc) {
-    constexpr int V = decltype(Vc)::value;
-    dispatch_grad<V>((a.dim + V - 1) / V, [&](auto Gc, auto Cc) { f(Vc, Gc, Cc); });
+    const GradTiles t = grad_tiles<decltype(Vc)::value>(a);
+    dispatch_grad<decltype(Vc)::value>(t.tile, [&](auto Gc, auto Cc) { f(Vc, Gc, Cc, t); });
   };
   if constexpr (sizeof(T) == 2)
     if (v == 8) return by_v(std::integral_constant<int, 8>{});
@@ -418,14 +466,13 @@ void dispatch_grad_args(const GradArgs& a, F&& f) {
 template <class T>
 GradPlan grad_plan_typed(const GradArgs& a, int sms) {
   GradPlan p{};
-  dispatch_grad_args<T>(a, [&](auto Vc, auto Gc, auto Cc) {
-    constexpr int V = decltype(Vc)::value, G = decltype(Gc)::value, C = decltype(Cc)::value;
-    constexpr uint64_t NG = kThreads / G, most = kGradSpan / NG;
+  dispatch_grad_args<T>(a, [&](auto, auto Gc, auto, GradTiles t) {
+    constexpr uint64_t NG = kThreads / decltype(Gc)::value, most = kGradSpan / NG;
     // one span per resident block, or as few full waves of them as spans allow
-    const uint64_t groups = NG * (uint64_t)sms * (C * V >= 24 ? 2 : 3);
+    const uint64_t groups = NG * std::max<uint64_t>(1, (uint64_t)sms * kGradBlocks / t.tiles);
     const uint64_t waves = (a.n + groups * most - 1) / (groups * most);
     uint64_t ch = (a.n + groups * waves - 1) / (groups * waves);
-    if (ch < 4) ch = 4;
+    if (ch < 8) ch = 8;
     if (ch > most) ch = most;
     p.chunk = (uint32_t)ch;
     p.spans = (a.n + NG * ch - 1) / (NG * ch);
@@ -436,13 +483,12 @@ GradPlan grad_plan_typed(const GradArgs& a, int sms) {
 
 template <class T>
 void launch_grad_typed(const GradArgs& a, const GradPlan& p, cudaStream_t stream) {
-  dispatch_grad_args<T>(a, [&](auto Vc, auto Gc, auto Cc) {
+  dispatch_grad_args<T>(a, [&](auto Vc, auto Gc, auto Cc, GradTiles t) {
     constexpr int V = decltype(Vc)::value, G = decltype(Gc)::value, C = decltype(Cc)::value;
-    constexpr int R = 8 / C > 0 ? 8 / C : 1;
+    constexpr int R = 8 / C;
     const uint32_t span = p.chunk * (kThreads / G), spans = (uint32_t)p.spans;
     note_launches((p.count_heads ? 1 : 0) + (spans > 1 ? 2 : 1));
-    if (p.count_heads)
-      launch_after(grad_heads_kernel, spans < 1024 ? spans : 1024u, kThreads, 0, stream, a, span, spans);
+    if (p.count_heads) launch_after(grad_heads_kernel, spans, kThreads, 0, stream, a, span);
     constexpr size_t smem = grad_smem<C, V>();
     // the kernel's dynamic shared-memory limit is a per-device attribute
     static bool attr_set[64] = {false};
@@ -452,9 +498,11 @@ void launch_grad_typed(const GradArgs& a, const GradPlan& p, cudaStream_t stream
       cudaFuncSetAttribute(grad_sum_kernel<T, V, G, C, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
       if (dev >= 0 && dev < 64) attr_set[dev] = true;
     }
-    launch_after(grad_sum_kernel<T, V, G, C, R>, spans, kThreads, smem, stream, a);
-    if (spans > 1)
-      launch_after(grad_combine_kernel, spans < 2048 ? spans : 2048u, kThreads, 0, stream, a, span, spans);
+    launch_after(grad_sum_kernel<T, V, G, C, R>, spans * t.tiles, kThreads, smem, stream, a, spans, t.tiles, t.tile);
+    if (spans > 1) {
+      const uint32_t tiles = (a.dim + 32 * V - 1) / (32 * V);
+      launch_after(grad_combine_kernel<V>, (spans - 1) * tiles, kThreads, 0, stream, a, span, spans, tiles);
+    }
   });
 }
 

@@ -118,43 +118,40 @@ __device__ __forceinline__ void load_unit(const char* p0, const char* p1, const 
 
 // Sum of the unit's squares of one lane: fp32 over its 32 or 64 elements,
 // which errs by a few parts in 10^7 at most, unless squares overflow or
-// vanish there: then again in fp64.
-template <int TYPE>
-__device__ __forceinline__ double unit_squares(const uint4 (&v)[kLoads]) {
-  constexpr int E = TYPE == ADAPM_F32 ? 4 : 8;
-  float sum = 0.f;
-#pragma unroll
-  for (int i = 0; i < kLoads; ++i) {
-    float x[8];
-    unpack<TYPE>(v[i], x);
-#pragma unroll
-    for (int j = 0; j < E; ++j) sum = fmaf(x[j], x[j], sum);
-  }
-  if (sum > 1e-25f && sum < 1e37f) return (double)sum;
-  uint32_t any = 0;
-#pragma unroll
-  for (int i = 0; i < kLoads; ++i) any |= v[i].x | v[i].y | v[i].z | v[i].w;
-  if ((any & (TYPE == ADAPM_F32 ? 0x7FFFFFFFu : 0x7FFF7FFFu)) == 0u) return 0.0;   // zeros, as untouched rows have
-  double s = 0.0;
-#pragma unroll
-  for (int i = 0; i < kLoads; ++i) {
-    float x[8];
-    unpack<TYPE>(v[i], x);
-#pragma unroll
-    for (int j = 0; j < E; ++j) s += (double)x[j] * (double)x[j];
-  }
-  return s;
-}
-
+// vanish there: then again in fp64, from memory (the words need not be kept
+// for that, which would cost the usual case registers).
 template <int TYPE>
 __device__ __forceinline__ double norm_unit(const GradTensor& t, uint32_t k) {
+  constexpr int E = TYPE == ADAPM_F32 ? 4 : 8;
   const char* p0 = t.in;
   const char* p1 = p0 + live_count(t) * (TYPE == ADAPM_F32 ? 4 : 2);
   const char* at = p0 - (reinterpret_cast<uintptr_t>(p0) & 15) + (uint64_t)k * kUnit;
   if (at >= p1) return 0.0;
   uint4 v[kLoads];
   load_unit<TYPE>(p0, p1, at, v);
-  return unit_squares<TYPE>(v);
+  float sum[2] = {0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    float x[8];
+    unpack<TYPE>(v[i], x);
+#pragma unroll
+    for (int j = 0; j < E; ++j) sum[i & 1] = fmaf(x[j], x[j], sum[i & 1]);
+  }
+  const float both = sum[0] + sum[1];
+  if (both > 1e-25f && both < 1e37f) return (double)both;
+  double s = 0.0;
+#pragma unroll 1
+  for (int i = 0; i < kLoads; ++i) {
+    const char* w = at + (i * 32 + (threadIdx.x & 31)) * 16;
+    constexpr int S = 16 / E;
+#pragma unroll 1
+    for (int j = 0; j < E; ++j) {
+      const char* e = w + j * S;
+      const double x = e >= p0 && e < p1 ? (double)load_one<TYPE>(e) : 0.0;
+      s += x * x;
+    }
+  }
+  return s;
 }
 
 // part: one sum per block of every launch of the call; the last block of the

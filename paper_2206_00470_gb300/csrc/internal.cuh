@@ -63,7 +63,6 @@ struct DevState {
   uint32_t sync_done;     // blocks of a sync that finished (0 between syncs)
   uint32_t ev_done;       // blocks of the closing events launch that finished (0 between advances)
   uint32_t loss_done;     // blocks of a training step that finished (0 between steps)
-  uint32_t grad_done;     // blocks of embed_grad's key count that finished (0 between calls)
   uint32_t norm_done;     // blocks of a gradient norm that finished (0 between calls)
   unsigned long long push_rows;       // rows pushed (cumulative)
   unsigned long long push_unique;     // distinct keys over all pushes (cumulative)
