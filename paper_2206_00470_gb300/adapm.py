@@ -167,9 +167,15 @@ def kernel_launches():
     return v.value
 
 
+_torch_module = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
 _torch_types = None   # (Tensor, int32, float32), once torch is needed
@@ -235,6 +241,7 @@ def _out_ptr(t):
 
 
 # -- token embeddings --------------------------------------------------------------
+_NOTHING = contextlib.nullcontext()
 _float_types = {}   # torch dtype -> element type of the ABI
 
 
@@ -263,6 +270,8 @@ def _one_stride(shape, strides):
 
 def _two_levels(shape, *strides):
     """(outer, inner, (outer stride, inner stride) of each), or None: an outer and an inner step for all of them."""
+    if len(shape) == 1:
+        return (1, shape[0], *((0, s[0]) for s in strides))
     for cut in range(len(shape) + 1):
         steps = [(_one_stride(shape[:cut], s[:cut]), _one_stride(shape[cut:], s[cut:])) for s in strides]
         if all(a is not None and b is not None for a, b in steps):
@@ -361,6 +370,10 @@ class ParameterManager:
         if st != OK:
             raise AdaPMError(st, "adapm_create failed")
         self._h = h
+        self._handle = stream.cuda_stream
+        self._device = torch.device("cuda", torch.cuda.current_device())
+        self._t, self._r = _Tokens(), _Rows()   # refilled by every call that takes tokens
+        self._t_ref, self._r_ref = ctypes.byref(self._t), ctypes.byref(self._r)
 
     # -- plumbing ------------------------------------------------------------
     def _check(self, st):
@@ -381,6 +394,8 @@ class ParameterManager:
 
     def _new_rows(self, n, like):
         torch = _torch()
+        if isinstance(like, torch.Tensor) and like.is_cuda:
+            return torch.empty((n, self.D), dtype=torch.float32, device=like.device)
         if isinstance(like, np.ndarray):
             return np.empty((n, self.D), dtype=np.float32)
         dev = like.device if like is not None and hasattr(like, "device") else torch.device("cuda")
@@ -468,46 +483,58 @@ class ParameterManager:
     def _on_stream(self):
         """Temporaries and new outputs are made on, and belong to, the library's stream."""
         torch = _torch()
-        if torch.cuda.current_stream() == self.stream:
-            return contextlib.nullcontext()
+        if torch._C._cuda_getCurrentRawStream(self._device.index) == self._handle:
+            return _NOTHING
         return torch.cuda.stream(self.stream)
 
-    def _tokens(self, tokens, pad, rows, what):
-        """The descriptors of tokens and of the rows (..., dim) that belong to them, and what keeps both alive."""
+    def _describe(self, tokens, pad, rows, what):
+        """Fills the descriptors of tokens and of the rows (..., dim) that belong to them; returns the two, or the
+        temporaries that stand for them."""
         torch = _torch()
-        if isinstance(tokens, (np.ndarray, list, tuple)):
+        if not isinstance(tokens, torch.Tensor):
             tokens = torch.from_numpy(np.ascontiguousarray(np.asarray(tokens, dtype=np.int64)))
-        if tokens.dtype != torch.int32 and tokens.dtype != torch.int64:
+        wide = tokens.dtype is torch.int64
+        if not wide and tokens.dtype is not torch.int32:
             if tokens.is_floating_point() or tokens.is_complex() or tokens.dtype == torch.bool:
                 raise ValueError(f"tokens are integers, not {tokens.dtype}")
             with self._on_stream():
                 tokens = tokens.to(torch.int64)
-        if rows.shape[:-1] != tokens.shape:
-            raise ValueError(f"{what} must have shape {(*tokens.shape, 'dim')}, not {tuple(rows.shape)}")
-        n, dim = tokens.numel(), rows.shape[-1]
-        if tokens.is_contiguous() and rows.is_contiguous():
-            outer, inner, ts, rs = 1, n, (n, 1), (n * dim, dim)
+            wide = True
+        shape, *row_shape, dim = tokens.shape, *rows.shape
+        if tuple(shape) != tuple(row_shape):
+            raise ValueError(f"{what} must have shape {(*shape, 'dim')}, not {tuple(rows.shape)}")
+        steps = rows.stride()
+        if dim > 1 and steps[-1] != 1:
+            if what == "out":
+                raise ValueError("elements of a row of out must follow each other")
+            with self._on_stream():
+                rows = rows.contiguous()
+            steps = rows.stride()
+        t, r = self._t, self._r
+        if len(shape) == 2:
+            t.outer, t.inner = shape
+            t.outer_stride, t.inner_stride = tokens.stride()
+            r.outer_stride, r.inner_stride, _ = steps
         else:
-            if dim > 1 and rows.stride(-1) != 1:
-                if what == "out":
-                    raise ValueError("elements of a row of out must follow each other")
-                with self._on_stream():
-                    rows = rows.contiguous()
-            got = _two_levels(tokens.shape, tokens.stride(), rows.stride()[:-1])
+            got = _two_levels(shape, tokens.stride(), steps[:-1])
             if got is None:
                 with self._on_stream():
                     tokens = tokens.contiguous()
-                got = _two_levels(tokens.shape, tokens.stride(), rows.stride()[:-1])
+                got = _two_levels(shape, tokens.stride(), steps[:-1])
             if got is None:
                 if what == "out":
                     raise ValueError("out's rows are not reached by an outer and an inner stride")
                 with self._on_stream():
                     rows = rows.contiguous()
-                got = _two_levels(tokens.shape, tokens.stride(), rows.stride()[:-1])
-            outer, inner, ts, rs = got
-        t = _Tokens(tokens.data_ptr(), 32 if tokens.dtype == torch.int32 else 64, pad is not None,
-                    0 if pad is None else int(pad), outer, inner, ts[0], ts[1])
-        return t, _Rows(rows.data_ptr(), _type_of(rows.dtype), rs[0], rs[1]), tokens, rows
+                got = _two_levels(shape, tokens.stride(), rows.stride()[:-1])
+            t.outer, t.inner, (t.outer_stride, t.inner_stride), (r.outer_stride, r.inner_stride) = got
+        t.ids, t.id_bits = tokens.data_ptr(), 64 if wide else 32
+        if pad is None:
+            t.has_pad = 0
+        else:
+            t.has_pad, t.pad = 1, pad
+        r.data, r.type = rows.data_ptr(), _type_of(rows.dtype)
+        return tokens, rows
 
     def embed(self, worker, tokens, dim=None, scale=1.0, pad=None, out=None, dtype=None):
         """scale * the first dim floats of the worker's value of every token, as (*tokens.shape, dim) in dtype
@@ -519,21 +546,22 @@ class ParameterManager:
             on_gpu = isinstance(tokens, torch.Tensor) and tokens.is_cuda
             with self._on_stream():
                 out = torch.empty((*shape, self.D if dim is None else dim), dtype=dtype or torch.float32,
-                                  device="cuda" if on_gpu else "cpu", pin_memory=not on_gpu)
+                                  device=self._device if on_gpu else "cpu", pin_memory=not on_gpu)
         elif (dim is not None and out.shape[-1] != dim) or (dtype is not None and out.dtype != dtype):
             raise ValueError("out has another dim or dtype")
-        t, r, tokens, _ = self._tokens(tokens, pad, out, "out")
-        self._check(self._lib.adapm_embed(self._h, worker, ctypes.byref(t), out.shape[-1], scale, ctypes.byref(r)))
+        keep = self._describe(tokens, pad, out, "out")   # (until the call has taken its arguments)
+        self._check(self._lib.adapm_embed(self._h, worker, self._t_ref, out.shape[-1], scale, self._r_ref))
+        del keep
         return out
 
     def embed_grad(self, worker, tokens, grad, scale=1.0, pad=None, out=None):
         """RowGrads of the distinct tokens: scale times the sum of the rows of grad (*tokens.shape, dim) that belong
         to each.  out: RowGrads with room for tokens.numel() keys and rows."""
         torch = _torch()
-        t, r, tokens, grad = self._tokens(tokens, pad, grad, "grad")
+        tokens, grad = self._describe(tokens, pad, grad, "grad")
         n, dim = tokens.numel(), grad.shape[-1]
         if out is None:
-            where = {"device": "cuda"} if grad.is_cuda else {"device": "cpu", "pin_memory": True}
+            where = {"device": self._device} if grad.is_cuda else {"device": "cpu", "pin_memory": True}
             with self._on_stream():
                 out = RowGrads(torch.empty(n, dtype=torch.int32, **where), torch.empty((n, dim), **where),
                                torch.empty(1, dtype=torch.int32, **where))
@@ -541,8 +569,8 @@ class ParameterManager:
               or out.keys.dtype != torch.int32 or out.rows.dtype != torch.float32 or out.count.dtype != torch.int32
               or (n > 0 and out.rows.shape[-1] != dim)):
             raise ValueError("out needs int32 keys, float32 rows of dim elements for every token, and an int32 count")
-        self._check(self._lib.adapm_embed_grad(self._h, worker, ctypes.byref(t), dim, scale, ctypes.byref(r),
-                                               _out_ptr(out.keys), _out_ptr(out.rows), _out_ptr(out.count)))
+        self._check(self._lib.adapm_embed_grad(self._h, worker, self._t_ref, dim, scale, self._r_ref, _out_ptr(out.keys),
+                                               _out_ptr(out.rows), _out_ptr(out.count)))
         return out
 
     def grad_norm(self, grads, scale=1.0, out=None):
@@ -552,7 +580,7 @@ class ParameterManager:
         if out is None:
             torch = _torch()
             with self._on_stream():
-                out = torch.empty((), dtype=torch.float32, device="cuda")
+                out = torch.empty((), dtype=torch.float32, device=self._device)
         self._check(self._lib.adapm_grad_norm(self._h, g.array, g.n, scale, out.data_ptr()))
         return out
 
@@ -571,7 +599,7 @@ class ParameterManager:
                    max_norm=float("inf")):
         """Update the worker's values of distinct ascending keys (-1: none) by their gradient rows, as embed_grad
         leaves both: SGD, or AdaGrad on [theta | a] rows, after clipping to max_norm by norm."""
-        with contextlib.nullcontext() if _plain_tensor(keys, 1) and _plain_tensor(rows, 2) else self._on_stream():
+        with _NOTHING if _plain_tensor(keys, 1) and _plain_tensor(rows, 2) else self._on_stream():
             k, r = _keys(keys), _floats(rows)
         dim = rows.shape[-1]
         if r.n != k.n * dim:

@@ -881,7 +881,45 @@ bool rows_apart(const adapm_tokens* t, const adapm_rows* r, uint32_t dim) {
   return s0 >= (int64_t)dim && (n1 <= 1 || s1 >= (int64_t)(n0 - 1) * s0 + (int64_t)dim);
 }
 
+// Whether pointers are on the device, for a list of them: those inside an
+// allocation already asked for need not be asked for again (a query takes 0.1
+// us, a list of a model's gradients hundreds of them).
+class DevicePointers {
+ public:
+  bool has(const void* p) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+    for (const Range& r : known_)
+      if (at - r.base < r.size) return true;
+    if (!is_device_ptr(p)) return false;
+    using Fn = int (*)(unsigned long long*, size_t*, unsigned long long);   // cuMemGetAddressRange
+    static const Fn range = [] {
+      void* f = nullptr;
+      cudaDriverEntryPointQueryResult got;
+      if (cudaGetDriverEntryPointByVersion("cuMemGetAddressRange", &f, 12000, cudaEnableDefault, &got) != cudaSuccess ||
+          got != cudaDriverEntryPointSuccess) {
+        cudaGetLastError();
+        f = nullptr;
+      }
+      return reinterpret_cast<Fn>(f);
+    }();
+    unsigned long long base = 0;
+    size_t size = 0;
+    if (range && range(&base, &size, at) == 0) known_[next_++ % kRanges] = Range{(uintptr_t)base, size};
+    return true;
+  }
+
+ private:
+  static constexpr int kRanges = 4;
+  struct Range {
+    uintptr_t base = 0;
+    size_t size = 0;
+  };
+  Range known_[kRanges];
+  unsigned next_ = 0;
+};
+
 adapm_status check_tensors(adapm_ctx* ctx, const adapm_tensor* t, uint64_t n, const char* what) {
+  DevicePointers device;
   if (n > 0 && !t) return fail(ctx, ADAPM_EINVAL, "null %s", what);
   if (n > (1u << 24)) return fail(ctx, ADAPM_EINVAL, "more than 2^24 %s", what);
   for (uint64_t i = 0; i < n; ++i) {
@@ -891,7 +929,7 @@ adapm_status check_tensors(adapm_ctx* ctx, const adapm_tensor* t, uint64_t n, co
     if (!t[i].data || t[i].count > (1ull << 48)) return fail(ctx, ADAPM_EINVAL, "%s[%llu]: bad data/count", what, at);
     if (reinterpret_cast<uintptr_t>(t[i].data) % type_bytes(t[i].type) != 0)
       return fail(ctx, ADAPM_EINVAL, "%s[%llu] is not aligned to its type", what, at);
-    if (!is_device_ptr(t[i].data) || (t[i].live && !is_device_ptr(t[i].live)))
+    if (!device.has(t[i].data) || (t[i].live && !device.has(t[i].live)))
       return fail(ctx, ADAPM_EINVAL, "%s[%llu] is not a device array", what, at);
   }
   return ADAPM_OK;
@@ -1653,6 +1691,14 @@ adapm_status adapm_embed_grad(adapm_ctx* ctx, uint32_t worker, const adapm_token
     launch_count_sort(tv, ctx->s.K, ka, va, ctx->dstate, ctx->stream);
     a.skeys = ka;
     a.spos = va;
+  } else if (!plan && n <= kTokenSort) {
+    CK(pool_alloc(ctx, &kb, n));
+    CK(pool_alloc(ctx, &vb, n));
+    CK(pool_alloc(ctx, &hist, token_sort_words(n, ctx->bits)));
+    uint32_t *const k2[2] = {ka, kb}, *const p2[2] = {va, vb};
+    const int which = token_sort(tv, ctx->s.K, ctx->bits, k2, p2, hist, ctx->dstate, ctx->stream);
+    a.skeys = k2[which];
+    a.spos = p2[which];
   } else {
     const uint32_t* raw = static_cast<const uint32_t*>(tv.ids);
     if (!as_is) {

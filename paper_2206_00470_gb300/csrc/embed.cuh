@@ -30,17 +30,23 @@ struct RowView {
 };
 
 #ifdef __CUDACC__
-// The key of token t: kNoKey for padding, kBadKey for an id that is none.
-__device__ __forceinline__ uint32_t token_key(const TokenView& v, uint64_t t, uint64_t K) {
-  int64_t at = (int64_t)t;
-  if (!v.flat) {
-    const uint32_t o = (uint32_t)t / v.inner, i = (uint32_t)t - o * v.inner;
-    at = (int64_t)o * v.outer_stride + (int64_t)i * v.inner_stride;
-  }
-  const int64_t id = v.wide ? static_cast<const int64_t*>(v.ids)[at]
-                            : (int64_t)static_cast<const uint32_t*>(v.ids)[at];
+// Where token t's id is, the id, and its key: kNoKey for padding, kBadKey for an
+// id that is none.
+__device__ __forceinline__ int64_t token_at(const TokenView& v, uint32_t t) {
+  if (v.flat) return t;
+  const uint32_t o = t / v.inner, i = t - o * v.inner;
+  return (int64_t)o * v.outer_stride + (int64_t)i * v.inner_stride;
+}
+__device__ __forceinline__ int64_t token_id(const TokenView& v, uint32_t t) {
+  const int64_t at = token_at(v, t);
+  return v.wide ? static_cast<const int64_t*>(v.ids)[at] : (int64_t)static_cast<const uint32_t*>(v.ids)[at];
+}
+__device__ __forceinline__ uint32_t id_key(const TokenView& v, int64_t id, uint64_t K) {
   if (v.has_pad && id == v.pad) return kNoKey;
   return id >= 0 && id < (int64_t)K ? (uint32_t)id : kBadKey;
+}
+__device__ __forceinline__ uint32_t token_key(const TokenView& v, uint64_t t, uint64_t K) {
+  return id_key(v, token_id(v, (uint32_t)t), K);
 }
 // First element of the row of token t.
 __device__ __forceinline__ int64_t row_offset(const RowView& v, uint32_t t) {
@@ -91,9 +97,19 @@ void launch_embed_grad(const GradArgs& a, const GradPlan& p, cudaStream_t stream
 void launch_copy_tokens(const TokenView& t, uint64_t K, uint32_t* out, DevState* st, int sms, cudaStream_t stream);
 // Stable sort of a few tokens' keys with their positions by counting, for
 // each, the keys that go before it; bad ids sort as padding and are reported.
-constexpr uint64_t kCountSort = 8192;
+constexpr uint64_t kCountSort = 6144;
 void launch_count_sort(const TokenView& t, uint64_t K, uint32_t* skeys, uint32_t* spos, DevState* st,
                        cudaStream_t stream);
+
+// Stable sort of up to kTokenSort tokens' keys by their low `bits` bits with
+// their positions.  keys / pos: two arrays of n each; the result is in those
+// whose index is returned.  scratch: token_sort_words(n, bits) words.  Bad ids sort as
+// padding and are reported.
+constexpr int kTokenBits = 8;
+constexpr uint64_t kTokenSort = 1u << 17;
+size_t token_sort_words(uint64_t n, int bits);
+int token_sort(const TokenView& t, uint64_t K, int bits, uint32_t* const* keys, uint32_t* const* pos,
+               uint32_t* scratch, DevState* st, cudaStream_t stream);
 
 // ---- update by gradient rows --------------------------------------------------
 struct RowUpdate {

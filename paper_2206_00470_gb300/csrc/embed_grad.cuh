@@ -31,7 +31,7 @@ namespace adapm {
 namespace {
 
 constexpr int kGradSpan = 2048;   // sorted rows staged per block, at most
-constexpr int kGradBlocks = 3;    // grad_sum blocks per SM
+constexpr int kGradBlocks = 2;    // grad_sum blocks per SM
 
 // V elements of type T as they travel.
 template <int BYTES>
@@ -128,48 +128,45 @@ __global__ void __launch_bounds__(kThreads) grad_heads_kernel(const GradArgs arg
   if (threadIdx.x == 0) a.heads[blockIdx.x] = heads;
 }
 
-// Distinct keys that begin before span b, and in all (to every thread of the
-// block): from the spans' counts, or from the keys themselves where there are
-// few.
-__device__ __forceinline__ uint2 grad_ranks(const GradArgs& a, uint32_t b, uint32_t spans, uint64_t P0) {
-  __shared__ uint2 both;
-  uint32_t below = 0, all = 0;
+// A thread's share of the distinct keys that begin before span b, and in all:
+// from the spans' counts, or from the keys themselves where there are few.
+__device__ __forceinline__ void grad_ranks(const GradArgs& a, uint32_t b, uint32_t spans, uint64_t P0, uint32_t& below,
+                                           uint32_t& all) {
+  below = all = 0;
   if (a.heads != nullptr) {
+#pragma unroll 4
     for (uint32_t m = threadIdx.x; m < spans; m += kThreads) {
       const uint32_t h = a.heads[m];
       all += h;
       if (m < b) below += h;
     }
-  } else {
-    const uint32_t n = (uint32_t)a.n;
-    auto count = [&](uint32_t p, uint32_t k, uint32_t prev) {
-      const uint32_t h = grad_valid(a, k) && prev != k ? 1u : 0u;
-      all += h;
-      if (p < P0) below += h;
-    };
-#pragma unroll 4
-    for (uint32_t p = 4 * threadIdx.x; p + 4 <= n; p += 4 * kThreads) {
-      const uint4 v = *reinterpret_cast<const uint4*>(a.skeys + p);
-      count(p, v.x, p > 0 ? a.skeys[p - 1] : kNoKey);
-      count(p + 1, v.y, v.x);
-      count(p + 2, v.z, v.y);
-      count(p + 3, v.w, v.z);
-    }
-    const uint32_t p = n / 4 * 4 + threadIdx.x;
-    if (p < n) count(p, a.skeys[p], p > 0 ? a.skeys[p - 1] : kNoKey);
+    return;
   }
-  block_sum2(below, all);
-  if (threadIdx.x == 0) both = make_uint2(below, all);
-  __syncthreads();
-  return both;
+  const uint32_t n = (uint32_t)a.n;
+  auto count = [&](uint32_t p, uint32_t k, uint32_t prev) {
+    const uint32_t h = grad_valid(a, k) && prev != k ? 1u : 0u;
+    all += h;
+    if (p < P0) below += h;
+  };
+#pragma unroll 4
+  for (uint32_t p = 4 * threadIdx.x; p + 4 <= n; p += 4 * kThreads) {
+    const uint4 v = *reinterpret_cast<const uint4*>(a.skeys + p);
+    count(p, v.x, p > 0 ? a.skeys[p - 1] : kNoKey);
+    count(p + 1, v.y, v.x);
+    count(p + 2, v.z, v.y);
+    count(p + 3, v.w, v.z);
+  }
+  const uint32_t p = n / 4 * 4 + threadIdx.x;
+  if (p < n) count(p, a.skeys[p], p > 0 ? a.skeys[p - 1] : kNoKey);
 }
 
-// Dynamic shared memory of grad_sum: head and tail piece of every chunk, then
-// the span's keys (with the one before and the one after), rows and flags.
+// Dynamic shared memory of grad_sum: the head piece of every chunk, then the
+// span's keys (with the one before and the one after), rows and flags.  What it
+// takes, L1 lacks for the loads in flight.
 template <int C, int V>
 constexpr size_t grad_smem() {
-  return 2 * (size_t)kThreads * C * V * sizeof(float) +
-         kGradSpan * (sizeof(int64_t) + sizeof(uint32_t) + sizeof(uint8_t)) + (kGradSpan + 2) * sizeof(uint32_t);
+  return (size_t)kThreads * C * V * sizeof(float) +
+         kGradSpan * (2 * sizeof(uint32_t) + sizeof(uint8_t)) + (kGradSpan + 2) * sizeof(uint32_t);
 }
 
 // Row flags: the first of its key in its chunk; the last of its key, or of the
@@ -187,9 +184,8 @@ __global__ void __launch_bounds__(kThreads, kGradBlocks) grad_sum_kernel(const G
   const uint32_t CH = a.chunk, span = NG * CH;
   extern __shared__ __align__(16) unsigned char dsm[];
   float* ph = reinterpret_cast<float*>(dsm);                 // head piece of each chunk
-  float* pt = ph + kThreads * C * V;                         // tail piece of each chunk
-  int64_t* so = reinterpret_cast<int64_t*>(pt + kThreads * C * V);   // first element of each row
-  uint32_t* su = reinterpret_cast<uint32_t*>(so + kGradSpan);        // index of its key among the distinct ones
+  uint32_t* sp = reinterpret_cast<uint32_t*>(ph + kThreads * C * V);   // position of each row
+  uint32_t* su = sp + kGradSpan;                             // index of its key among the distinct ones
   uint32_t* sk = su + kGradSpan;                             // sk[0]: key before the span; sk[1 + len]: after it
   uint8_t* sf = reinterpret_cast<uint8_t*>(sk + kGradSpan + 2);
   const int lane = threadIdx.x & (G - 1);
@@ -201,46 +197,87 @@ __global__ void __launch_bounds__(kThreads, kGradBlocks) grad_sum_kernel(const G
   float* parts = a.parts + q0 * V;
   const uint64_t P0 = (uint64_t)b * span;
   const uint32_t len = (uint32_t)(a.n - P0 < (uint64_t)span ? a.n - P0 : span);
-  for (uint32_t i = threadIdx.x; i < len; i += kThreads) sk[1 + i] = a.skeys[P0 + i];
+  // the span's keys and positions, and the counts in front of it, in one
+  // latency; then one scan: a row's rank is the heads of the rounds and warps
+  // before it plus those of the lanes before
+  constexpr int NR = kGradSpan / kThreads, NW = kThreads / 32;
+  __shared__ uint32_t heads[NR * NW], sums[2][NW];
+  const int lane32 = threadIdx.x & 31, warp = threadIdx.x / 32;
+  uint32_t pos[NR];
+#pragma unroll
+  for (int j = 0; j < NR; ++j) {
+    const uint32_t i = j * kThreads + threadIdx.x;
+    pos[j] = i < len ? a.spos[P0 + i] : 0u;
+    if (i < len) sk[1 + i] = a.skeys[P0 + i];
+  }
   if (threadIdx.x == 0) {
     sk[0] = P0 > 0 ? a.skeys[P0 - 1] : kNoKey;
     sk[1 + len] = P0 + len < a.n ? a.skeys[P0 + len] : kNoKey;
   }
-  const uint2 ranks = grad_ranks(a, b, spans, P0);   // (a barrier: the keys are staged)
-  uint32_t first = ranks.x;
-  const uint32_t total = ranks.y;
-  if (blockIdx.x == 0 && threadIdx.x == 0) *a.count = total;
-  bool wrong = false;
-  for (uint32_t i0 = 0; i0 < len; i0 += kThreads) {   // block-uniform
-    const uint32_t i = i0 + threadIdx.x;
-    const bool in = i < len;
-    const uint32_t k = in ? sk[1 + i] : kNoKey;
-    const bool counts = in && grad_valid(a, k);
-    const uint32_t head = counts && sk[i] != k ? 1u : 0u;   // (sk[0] is kNoKey in front of the first)
-    uint32_t before = head, unused = 0, heads, none;
-    block_exclusive_scan2(before, unused, heads, none);
-    if (in) {
-      uint8_t f = 0;
-      const uint32_t pos = a.spos[P0 + i];
-      if (counts && pos < a.n) {
-        const uint32_t cs = i - i % CH, ce = cs + CH < len ? cs + CH : len;
-        const bool ends = sk[2 + i] != k;
-        f = kCounts | (head || i == cs ? kBegin : 0) | (ends || i + 1 == ce ? kEnd : 0) |
-            (sk[cs] != k ? kStarted : 0) | (ends ? kLast : 0);
-        so[i] = row_offset(a.grad, pos);
-      } else if (counts || (k >= a.K && k != kNoKey)) {
-        wrong = true;
-      }
-      sf[i] = f;
-      const uint32_t u = first + before + head - 1;
-      su[i] = u;
-      if (q0 == 0) {
-        if (head) a.keys[u] = k;
-        if (i + 1 == len) a.crossing[b] = u;
-        if (P0 + i >= total) a.keys[P0 + i] = kNoKey;
-      }
+  uint32_t below, all;
+  grad_ranks(a, b, spans, P0, below, all);
+  below = __reduce_add_sync(0xFFFFFFFFu, below);
+  all = __reduce_add_sync(0xFFFFFFFFu, all);
+  if (lane32 == 0) {
+    sums[0][warp] = below;
+    sums[1][warp] = all;
+  }
+  __syncthreads();
+  uint32_t head[NR];   // lanes of the warp whose row is the first of its key
+#pragma unroll
+  for (int j = 0; j < NR; ++j) {
+    const uint32_t i = j * kThreads + threadIdx.x;
+    const bool h = i < len && grad_valid(a, sk[1 + i]) && sk[i] != sk[1 + i];   // (sk[0] is kNoKey in front of the first)
+    head[j] = __ballot_sync(0xFFFFFFFFu, h);
+    if (lane32 == 0) heads[j * NW + warp] = __popc(head[j]);
+  }
+  __syncthreads();
+  if (warp == 0) {   // exclusive scan of the NR * NW counts, two a lane
+    static_assert(NR * NW == 64, "");
+    const uint32_t h0 = heads[2 * lane32], h1 = heads[2 * lane32 + 1];
+    uint32_t x = h0 + h1;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+      if (lane32 >= o) x += y;
     }
-    first += heads;
+    heads[2 * lane32] = x - h0 - h1;
+    heads[2 * lane32 + 1] = x - h1;
+  }
+  uint32_t first = 0, total = 0;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    first += sums[0][w];
+    total += sums[1][w];
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.count = total;
+  __syncthreads();
+  bool wrong = false;
+#pragma unroll
+  for (int j = 0; j < NR; ++j) {
+    const uint32_t i = j * kThreads + threadIdx.x;
+    if (i >= len) break;
+    const uint32_t k = sk[1 + i];
+    const bool counts = grad_valid(a, k), begins = (head[j] >> lane32) & 1u;
+    uint8_t f = 0;
+    if (counts && pos[j] < a.n) {
+      const uint32_t cs = i - i % CH, ce = cs + CH < len ? cs + CH : len;
+      const bool ends = sk[2 + i] != k;
+      f = kCounts | (begins || i == cs ? kBegin : 0) | (ends || i + 1 == ce ? kEnd : 0) |
+          (sk[cs] != k ? kStarted : 0) | (ends ? kLast : 0);
+      sp[i] = pos[j];
+    } else if (counts || (k >= a.K && k != kNoKey)) {
+      wrong = true;
+    }
+    sf[i] = f;
+    // heads up to and including this row, less one
+    const uint32_t u = first + heads[j * NW + warp] + __popc(head[j] & (0xFFFFFFFFu >> (31 - lane32))) - 1;
+    su[i] = u;
+    if (q0 == 0) {
+      if (begins) a.keys[u] = k;
+      if (i + 1 == len) a.crossing[b] = u;
+      if (P0 + i >= total) a.keys[P0 + i] = kNoKey;
+    }
   }
   if (__syncthreads_or(wrong) && threadIdx.x == 0) set_error(a.st, ERR_INTERNAL);
   const uint32_t p0 = gi * CH < len ? gi * CH : len;
@@ -250,21 +287,22 @@ __global__ void __launch_bounds__(kThreads, kGradBlocks) grad_sum_kernel(const G
   for (int c = 0; c < C; ++c)
 #pragma unroll
     for (int j = 0; j < V; ++j) run[c][j] = 0.f;
-  for (uint32_t p = p0; p < p1; p += R) {
-    RawOf<T, V> d[R][C];
-    uint8_t f[R];
+  auto fetch = [&](uint32_t p, uint8_t (&f)[R], RawOf<T, V> (&d)[R][C]) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       f[r] = p + r < p1 ? sf[p + r] : 0;
+      const T* row = grad + (f[r] & kCounts ? row_offset(a.grad, sp[p + r]) : 0);
 #pragma unroll
       for (int c = 0; c < C; ++c) {
         const uint32_t q = lane + c * G;
         if ((f[r] & kCounts) && q < nv)
-          d[r][c] = *reinterpret_cast<const RawOf<T, V>*>(grad + so[p + r] + (int64_t)q * V);
+          d[r][c] = *reinterpret_cast<const RawOf<T, V>*>(row + q * V);
         else
           d[r][c] = RawOf<T, V>{};
       }
     }
+  };
+  auto add = [&](uint32_t p, const uint8_t (&f)[R], const RawOf<T, V> (&d)[R][C]) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       if (!(f[r] & kCounts)) continue;
@@ -281,16 +319,21 @@ __global__ void __launch_bounds__(kThreads, kGradBlocks) grad_sum_kernel(const G
           const uint32_t q = lane + c * G;
           if (q < nv) put_floats<V>(row + q * V, run[c], a.scale);
         }
-      } else {   // a chunk has at most one head and one tail piece
-        float* piece = ((f[r] & kStarted) ? pt : ph) + gi * G * C * V;
+      } else if (!(f[r] & kStarted)) {   // the chunk's head piece (a tail piece stays in the registers)
 #pragma unroll
-        for (int c = 0; c < C; ++c) put_floats<V>(piece + (lane + c * G) * V, run[c], 1.f);
+        for (int c = 0; c < C; ++c) put_floats<V>(ph + (gi * G * C + lane + c * G) * V, run[c], 1.f);
       }
     }
+  };
+  for (uint32_t p = p0; p < p1; p += R) {
+    uint8_t f[R];
+    RawOf<T, V> d[R][C];
+    fetch(p, f, d);
+    add(p, f, d);
   }
   __syncthreads();
   // A key that begins in chunk gi and goes on is summed here by group gi: its
-  // tail piece, then the head pieces of the chunks it covers.
+  // tail piece (the running sum), then the head pieces of the chunks it covers.
   const uint32_t nch = (len + CH - 1) / CH;
   auto chunk_end = [&](uint32_t m) { return (m + 1) * CH < len ? (m + 1) * CH : len; };
   auto walk = [&](uint32_t m, uint32_t kk, bool& out) {   // last chunk from m on that kk covers; past the span?
@@ -316,20 +359,11 @@ __global__ void __launch_bounds__(kThreads, kGradBlocks) grad_sum_kernel(const G
       if (q < nv) put_floats<V>(row + q * V, run[c], scale);
     }
   };
-  auto zero_run = [&]() {
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-      for (int j = 0; j < V; ++j) run[c][j] = 0.f;
-  };
   if (gi < nch) {
     const uint32_t kl = sk[p1];   // the chunk's last row
     if (grad_valid(a, kl) && sk[1 + p1] == kl && sk[p0] != kl) {
       bool out = true;
       const uint32_t m1 = gi + 1 < nch ? walk(gi + 1, kl, out) : gi;
-      zero_run();
-#pragma unroll
-      for (int c = 0; c < C; ++c) add_floats<V>(run[c], pt + (gi * G * C + lane + c * G) * V);
       add_pieces(gi + 1, m1);
       if (out) put_row(parts + (2 * (uint64_t)b + 1) * a.dim, 1.f);
       else put_row(rows + (uint64_t)su[p1 - 1] * a.dim, a.scale);
@@ -338,7 +372,10 @@ __global__ void __launch_bounds__(kThreads, kGradBlocks) grad_sum_kernel(const G
   if (gi == 0 && sk[0] == sk[1] && grad_valid(a, sk[1])) {   // the span's first key began before it
     bool out = false;
     const uint32_t m1 = walk(0, sk[1], out);
-    zero_run();
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int j = 0; j < V; ++j) run[c][j] = 0.f;
     add_pieces(0, m1);
     put_row(parts + 2 * (uint64_t)b * a.dim, 1.f);
   }

@@ -1,6 +1,7 @@
 // Keys of a batch of tokens, without gaps or sorted with their positions, for
 // embed_grad.
 #include "embed.cuh"
+#include "radix.cuh"
 #include "rowgroup.cuh"
 
 namespace adapm {
@@ -21,81 +22,298 @@ __global__ void __launch_bounds__(kThreads) copy_tokens_kernel(const TokenView t
 
 // Position of key i in the stable order: the keys below it, and those equal
 // to it that come first.  Every block counts for kOwn keys against all n,
-// staged in shared memory kTile at a time: kSlices threads share the others of
-// kPer keys, four a load.  n^2 comparisons over the whole GPU in one launch and
-// without a wait between blocks, where a radix sort of so few keys is a chain
-// of passes in one block.
-constexpr int kPer = 2, kSlices = 16, kOwn = kThreads / kSlices * kPer, kTile = 4096;
+// staged in shared memory: kSlices threads share the others of kPer keys, four
+// a load.  n^2 comparisons over the whole GPU in one launch and without a wait
+// between blocks, where a radix sort of so few keys is a chain of passes.
+// Bound by latency up to 2,000 tokens (4 us), by the comparisons above: 4,096
+// tokens 6.7 us, 6,000 10 us, 8,192 15 us (token sort: 12, 12.5, 12 us and the
+// launch of grad_heads).
+constexpr int kThreadsC = 256, kPer = 2, kSlices = 32, kOwn = kThreadsC / kSlices * kPer;
 
-__global__ void __launch_bounds__(kThreads) count_sort_kernel(const TokenView t, uint64_t K, uint32_t* skeys,
+__global__ void __launch_bounds__(kThreadsC) count_sort_kernel(const TokenView t, uint64_t K, uint32_t* skeys,
                                                               uint32_t* spos, DevState* st) {
   after_previous();
-  constexpr int NO = kThreads / kSlices;   // threads that hold different keys
-  __shared__ __align__(16) uint32_t tile[kTile];
+  constexpr int NO = kThreadsC / kSlices;   // threads that hold different keys
+  __shared__ __align__(16) uint32_t all[kCountSort];
   __shared__ uint32_t cnt[kSlices][kOwn];
   const uint32_t n = (uint32_t)t.n;
   const int o = threadIdx.x % NO, part = threadIdx.x / NO;
-  const uint32_t own0 = blockIdx.x * kOwn;
-  uint32_t mine[kPer], before[kPer];
   bool bad = false;
+  constexpr int B = 8;   // ids in flight per thread
+  for (uint32_t j0 = threadIdx.x; j0 < n; j0 += B * kThreadsC) {
+    int64_t id[B];
+    if (t.wide) {
+#pragma unroll
+      for (int e = 0; e < B; ++e)
+        id[e] = j0 + e * kThreadsC < n ? static_cast<const int64_t*>(t.ids)[token_at(t, j0 + e * kThreadsC)] : 0;
+    } else {
+#pragma unroll
+      for (int e = 0; e < B; ++e)
+        id[e] = j0 + e * kThreadsC < n ? static_cast<const uint32_t*>(t.ids)[token_at(t, j0 + e * kThreadsC)] : 0;
+    }
+#pragma unroll
+    for (int e = 0; e < B; ++e) {
+      const uint32_t k = id_key(t, id[e], K);
+      if (j0 + e * kThreadsC >= n) break;
+      bad |= k == kBadKey;
+      all[j0 + e * kThreadsC] = k == kBadKey ? kNoKey : k;
+    }
+  }
+  __syncthreads();
+  // the block's own keys [a, b), the thread's among them
+  const uint32_t a = blockIdx.x * kOwn, b = a + kOwn < n ? a + kOwn : n;
+  uint32_t mine[kPer], before[kPer];
 #pragma unroll
   for (int q = 0; q < kPer; ++q) {
-    const uint32_t i = own0 + q * NO + o;
-    mine[q] = i < n ? token_key(t, i, K) : kNoKey;
-    bad |= mine[q] == kBadKey;
-    if (mine[q] == kBadKey) mine[q] = kNoKey;
+    mine[q] = a + q * NO + o < n ? all[a + q * NO + o] : kNoKey;
     before[q] = 0;
   }
-  for (uint32_t t0 = 0; t0 < n; t0 += kTile) {
-    const uint32_t len = n - t0 < (uint32_t)kTile ? n - t0 : (uint32_t)kTile;
-    __syncthreads();
+  // keys [lo, hi), lo a multiple of four: those below mine, or (in front of the
+  // block's own) not above it
+  auto count = [&](uint32_t lo, uint32_t hi, bool equal) {
+    const uint32_t whole = lo + (hi - lo) / 4 * 4;
 #pragma unroll 4
-    for (uint32_t j = threadIdx.x; j < len; j += kThreads) {
-      const uint32_t k = token_key(t, t0 + j, K);
-      tile[j] = k == kBadKey ? kNoKey : k;
+    for (uint32_t j = lo + 4 * part; j < whole; j += 4 * kSlices) {
+      const uint4 v = *reinterpret_cast<const uint4*>(all + j);
+      const uint32_t k[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int q = 0; q < kPer; ++q) before[q] += equal ? (k[e] <= mine[q]) : (k[e] < mine[q]);
     }
-    __syncthreads();
-    // keys [lo, hi) of the tile, a multiple of four from lo: below mine, or
-    // (before the block's own) not above it
-    auto count = [&](uint32_t lo, uint32_t hi, bool equal) {
-      const uint32_t whole = lo + (hi - lo) / 4 * 4;
-#pragma unroll 4
-      for (uint32_t j = lo + 4 * part; j < whole; j += 4 * kSlices) {
-        const uint4 v = *reinterpret_cast<const uint4*>(tile + j);
-        const uint32_t k[4] = {v.x, v.y, v.z, v.w};
+    for (uint32_t j = whole + part; j < hi; j += kSlices)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
+      for (int q = 0; q < kPer; ++q) before[q] += equal ? (all[j] <= mine[q]) : (all[j] < mine[q]);
+  };
+  count(0, a, true);
+  if (b < n) count(b, n, false);   // (b is then a multiple of kOwn)
+  for (uint32_t j = a + part; j < b; j += kSlices)
 #pragma unroll
-          for (int q = 0; q < kPer; ++q) before[q] += equal ? (k[e] <= mine[q]) : (k[e] < mine[q]);
-      }
-      for (uint32_t j = whole + part; j < hi; j += kSlices)
-#pragma unroll
-        for (int q = 0; q < kPer; ++q) before[q] += equal ? (tile[j] <= mine[q]) : (tile[j] < mine[q]);
-    };
-    // (own0 and the tiles' starts are multiples of kOwn)
-    const uint32_t a = own0 < t0 ? 0u : (own0 - t0 < len ? own0 - t0 : len);
-    const uint32_t b = own0 + kOwn < t0 ? 0u : (own0 + kOwn - t0 < len ? own0 + kOwn - t0 : len);
-    count(0, a, true);
-    count(b, len, false);
-    for (uint32_t j = a + part; j < b; j += kSlices)
-#pragma unroll
-      for (int q = 0; q < kPer; ++q) {
-        const uint32_t i = own0 + q * NO + o;
-        before[q] += tile[j] < mine[q] || (tile[j] == mine[q] && t0 + j < i);
-      }
-  }
+    for (int q = 0; q < kPer; ++q) before[q] += all[j] < mine[q] || (all[j] == mine[q] && j < a + q * NO + o);
 #pragma unroll
   for (int q = 0; q < kPer; ++q) cnt[part][q * NO + o] = before[q];
   __syncthreads();
-  if (threadIdx.x < kOwn && own0 + threadIdx.x < n) {
+  if (threadIdx.x < kOwn && a + threadIdx.x < n) {
     uint32_t at = 0;
 #pragma unroll
     for (int p = 0; p < kSlices; ++p) at += cnt[p][threadIdx.x];
-    const uint32_t k = token_key(t, own0 + threadIdx.x, K);
-    skeys[at] = k == kBadKey ? kNoKey : k;
-    spos[at] = own0 + threadIdx.x;
+    skeys[at] = all[a + threadIdx.x];
+    spos[at] = a + threadIdx.x;
   }
+  if (blockIdx.x == 0 && __syncthreads_or(bad) && threadIdx.x == 0) set_error(st, ERR_KEY_RANGE);
+}
+
+// ---------------------------------------------------------------------------
+// Token sort: a stable radix sort of up to kTokenSort tokens in one launch per
+// pass of kTokenBits bits and one in front.  Every block owns a tile of
+// consecutive items and finds the places of its own from a table (digit x
+// tile) of the items that every tile holds, by summing the table's rows: no
+// scan launch, no wait between blocks.  While it moves its items it counts
+// them into the next pass's table (packed 16-bit counts; a tile holds at most
+// 1024).  The first pass reads the tokens themselves, in whatever layout they
+// have.  All of it is latency: a launch takes 3.5 to 6 us.
+//
+// Grid sort (sort.cu) -> this, tokens of 1M keys: 16,384 26 -> 13 us, 65,536
+// 31 -> 19 us, 131,072 31 -> 24 us; more tiles make the rows long: 262,144 27
+// to 35 us there, 35 to 42 here.  (Digits of 10 bits and tiles of 2048 took 17,
+// 22 and 27 us.)
+// ---------------------------------------------------------------------------
+constexpr int kThreadsT = 1 << kTokenBits, kWarpsT = kThreadsT / 32;   // a thread per digit
+constexpr uint32_t kTilesMost = 128;
+
+struct TokenPass {
+  const uint32_t* keys;   // null: the tokens
+  const uint32_t* pos;
+  uint32_t* keys_out;
+  uint32_t* pos_out;
+  const uint16_t* table;  // counts of this pass's digits
+  uint32_t* next;         // packed counts of the next pass's, null: none
+  uint32_t n, tiles, stride;   // stride: tiles of a table row, a multiple of eight
+  int shift, bits, next_bits;
+};
+
+// The items of a thread: warp w owns ITEMS * 32 consecutive ones, 32 a round.
+template <int ITEMS>
+__device__ __forceinline__ uint32_t item_at(uint32_t tile0, int it) {
+  return tile0 + ((threadIdx.x / 32) * ITEMS + it) * 32 + (threadIdx.x & 31);
+}
+template <int ITEMS>
+__device__ __forceinline__ bool load_tokens(const TokenView& t, uint64_t K, uint32_t tile0, uint32_t (&key)[ITEMS]) {
+  int64_t id[ITEMS];
+  const uint32_t n = (uint32_t)t.n;
+  if (t.wide) {
+#pragma unroll
+    for (int it = 0; it < ITEMS; ++it) {
+      const uint32_t i = item_at<ITEMS>(tile0, it);
+      id[it] = i < n ? static_cast<const int64_t*>(t.ids)[token_at(t, i)] : 0;
+    }
+  } else {
+#pragma unroll
+    for (int it = 0; it < ITEMS; ++it) {
+      const uint32_t i = item_at<ITEMS>(tile0, it);
+      id[it] = i < n ? static_cast<const uint32_t*>(t.ids)[token_at(t, i)] : 0;
+    }
+  }
+  bool bad = false;
+#pragma unroll
+  for (int it = 0; it < ITEMS; ++it) {
+    key[it] = id_key(t, id[it], K);
+    if (key[it] == kBadKey) {
+      key[it] = kNoKey;
+      bad = true;
+    }
+  }
+  return bad;
+}
+
+// The first pass's table, and the next ones cleared.
+template <int ITEMS>
+__global__ void __launch_bounds__(kThreadsT) token_count_kernel(const TokenView t, uint64_t K, uint16_t* table,
+                                                                uint32_t* clear, uint32_t clear_words, uint32_t stride,
+                                                                int bits, DevState* st) {
+  after_previous();
+  extern __shared__ __align__(16) unsigned char dsm[];
+  uint32_t* cnt = reinterpret_cast<uint32_t*>(dsm);
+  const uint32_t digits = 1u << bits, tile0 = blockIdx.x * (kThreadsT * ITEMS);
+  for (uint32_t i = blockIdx.x * kThreadsT + threadIdx.x; i < clear_words; i += gridDim.x * kThreadsT) clear[i] = 0u;
+  uint32_t key[ITEMS];
+  const bool bad = load_tokens<ITEMS>(t, K, tile0, key);
+  for (uint32_t d = threadIdx.x; d < digits; d += kThreadsT) cnt[d] = 0u;
+  __syncthreads();
+#pragma unroll
+  for (int it = 0; it < ITEMS; ++it) {
+    const bool in = item_at<ITEMS>(tile0, it) < (uint32_t)t.n;
+    const uint32_t d = in ? key[it] & (digits - 1) : digits;
+    const uint32_t peers = __match_any_sync(0xFFFFFFFFu, d);
+    if (in && (peers & lanemask_lt()) == 0u) atomicAdd(cnt + d, (uint32_t)__popc(peers));
+  }
+  __syncthreads();
+  for (uint32_t d = threadIdx.x; d < digits; d += kThreadsT) table[d * stride + blockIdx.x] = (uint16_t)cnt[d];
+  if (blockIdx.x == 0)   // tiles of the row that do not exist
+    for (uint32_t d = threadIdx.x; d < digits; d += kThreadsT)
+      for (uint32_t b = gridDim.x; b < stride; ++b) table[d * stride + b] = 0;
   if (__syncthreads_or(bad) && threadIdx.x == 0) set_error(st, ERR_KEY_RANGE);
+}
+
+// Dynamic shared memory of token_pass: the digits' places, then the warps'
+// digit counts.
+size_t token_smem(int bits) { return ((size_t)4 + 2 * kWarpsT) << bits; }
+
+template <int ITEMS>
+__global__ void __launch_bounds__(kThreadsT) token_pass_kernel(const TokenView t, uint64_t K, const TokenPass p) {
+  after_previous();
+  extern __shared__ __align__(16) unsigned char dsm[];
+  const uint32_t digits = 1u << p.bits;
+  uint32_t* place = reinterpret_cast<uint32_t*>(dsm);
+  uint16_t* wcnt = reinterpret_cast<uint16_t*>(place + digits);   // [warp][digit]
+  __shared__ uint32_t scan[kWarpsT];
+  const uint32_t tile0 = blockIdx.x * (kThreadsT * ITEMS);
+  const int warp = threadIdx.x / 32;
+  uint32_t key[ITEMS], pos[ITEMS], rank[ITEMS];
+  if (p.keys == nullptr) {
+    load_tokens<ITEMS>(t, K, tile0, key);
+#pragma unroll
+    for (int it = 0; it < ITEMS; ++it) pos[it] = item_at<ITEMS>(tile0, it);
+  } else {
+#pragma unroll
+    for (int it = 0; it < ITEMS; ++it) {
+      const uint32_t i = item_at<ITEMS>(tile0, it);
+      key[it] = i < p.n ? p.keys[i] : kNoKey;
+      pos[it] = i < p.n ? p.pos[i] : 0u;
+    }
+  }
+  // items of the thread's digit: anywhere, and in the tiles before this one
+  uint32_t all = 0, before = 0;
+  if (threadIdx.x < digits) {
+    const uint4* row = reinterpret_cast<const uint4*>(p.table + (uint64_t)threadIdx.x * p.stride);
+#pragma unroll 8
+    for (uint32_t q = 0; q < p.stride / 8; ++q) {
+      const uint4 v = row[q];
+      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t b = 8 * q + 2 * e, lo = w[e] & 0xFFFFu, hi = w[e] >> 16;
+        all += lo + hi;
+        before += (b < blockIdx.x ? lo : 0u) + (b + 1 < blockIdx.x ? hi : 0u);
+      }
+    }
+  }
+  for (uint32_t i = threadIdx.x; i < digits * kWarpsT / 2; i += kThreadsT) reinterpret_cast<uint32_t*>(wcnt)[i] = 0u;
+  __syncthreads();
+  // ranks within the warp
+  uint32_t peers[ITEMS];
+#pragma unroll
+  for (int it = 0; it < ITEMS; ++it)
+    peers[it] = digit_peers((key[it] >> p.shift) & (digits - 1), item_at<ITEMS>(tile0, it) < p.n, p.bits);
+#pragma unroll
+  for (int it = 0; it < ITEMS; ++it) {
+    const bool in = item_at<ITEMS>(tile0, it) < p.n;
+    uint16_t* c = wcnt + warp * digits + ((key[it] >> p.shift) & (digits - 1));
+    const uint32_t have = in ? *c : 0u;
+    rank[it] = have + __popc(peers[it] & lanemask_lt());
+    __syncwarp();
+    if (in && (peers[it] & lanemask_lt()) == 0u) *c = (uint16_t)(have + __popc(peers[it]));
+    __syncwarp();
+  }
+  // where the digit's items of this tile go: behind those of lower digits and
+  // of the tiles before, warp by warp
+  uint32_t total;
+  const uint32_t base = block_exclusive_scan<kThreadsT>(all, &total, scan);   // (a barrier: the warps' counts are final)
+  if (threadIdx.x < digits) {
+    uint32_t h[kWarpsT], run = 0;
+#pragma unroll
+    for (int w = 0; w < kWarpsT; ++w) h[w] = wcnt[w * digits + threadIdx.x];
+#pragma unroll
+    for (int w = 0; w < kWarpsT; ++w) {
+      wcnt[w * digits + threadIdx.x] = (uint16_t)run;
+      run += h[w];
+    }
+    place[threadIdx.x] = base + before;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int it = 0; it < ITEMS; ++it) {
+    const bool in = item_at<ITEMS>(tile0, it) < p.n;
+    const uint32_t d = (key[it] >> p.shift) & (digits - 1);
+    const uint32_t at = in ? place[d] + wcnt[warp * digits + d] + rank[it] : 0u;
+    if (in) {
+      p.keys_out[at] = key[it];
+      p.pos_out[at] = pos[it];
+    }
+    if (p.next != nullptr) {
+      const uint32_t nd = (key[it] >> (p.shift + p.bits)) & ((1u << p.next_bits) - 1);
+      const uint32_t cell = in ? nd * p.stride + at / (kThreadsT * ITEMS) : 0xFFFFFFFFu;
+      const uint32_t peers = __match_any_sync(0xFFFFFFFFu, cell);
+      if (in && (peers & lanemask_lt()) == 0u) atomicAdd(p.next + cell / 2, (uint32_t)__popc(peers) << (16 * (cell & 1)));
+    }
+  }
+}
+
+template <int ITEMS>
+int token_sort_items(const TokenView& t, uint64_t K, int bits, uint32_t* const* keys, uint32_t* const* pos,
+                             uint32_t* scratch, DevState* st, cudaStream_t stream) {
+  const int passes = (bits + kTokenBits - 1) / kTokenBits, each = (bits + passes - 1) / passes;
+  const uint32_t tiles = (uint32_t)((t.n + kThreadsT * ITEMS - 1) / (kThreadsT * ITEMS)), stride = (tiles + 7) / 8 * 8;
+  const uint32_t words = (stride << each) / 2;   // of a table
+  note_launches(1 + passes);
+  launch_after(token_count_kernel<ITEMS>, tiles, kThreadsT, sizeof(uint32_t) << each, stream, t, K,
+               reinterpret_cast<uint16_t*>(scratch), scratch + words, (uint32_t)(passes - 1) * words, stride, each, st);
+  for (int i = 0; i < passes; ++i) {
+    TokenPass p{};
+    p.keys = i == 0 ? nullptr : keys[(i - 1) & 1];
+    p.pos = i == 0 ? nullptr : pos[(i - 1) & 1];
+    p.keys_out = keys[i & 1];
+    p.pos_out = pos[i & 1];
+    p.table = reinterpret_cast<const uint16_t*>(scratch + i * words);
+    p.next = i + 1 < passes ? scratch + (i + 1) * words : nullptr;
+    p.n = (uint32_t)t.n;
+    p.tiles = tiles;
+    p.stride = stride;
+    p.shift = i * each;
+    p.bits = p.next_bits = each;
+    launch_after(token_pass_kernel<ITEMS>, tiles, kThreadsT, token_smem(each), stream, t, K, p);
+  }
+  return (passes - 1) & 1;
 }
 
 }  // namespace
@@ -108,7 +326,22 @@ void launch_copy_tokens(const TokenView& t, uint64_t K, uint32_t* out, DevState*
 void launch_count_sort(const TokenView& t, uint64_t K, uint32_t* skeys, uint32_t* spos, DevState* st,
                        cudaStream_t stream) {
   note_launches(1);
-  launch_after(count_sort_kernel, (unsigned)((t.n + kOwn - 1) / kOwn), kThreads, 0, stream, t, K, skeys, spos, st);
+  launch_after(count_sort_kernel, (unsigned)((t.n + kOwn - 1) / kOwn), kThreadsC, 0, stream, t, K, skeys, spos, st);
+}
+
+// Tiles of 512 tokens, or twice that where they would be too many.
+int token_items(uint64_t n) { return n <= (uint64_t)kTilesMost * kThreadsT * 2 ? 2 : 4; }
+
+size_t token_sort_words(uint64_t n, int bits) {
+  const int passes = (bits + kTokenBits - 1) / kTokenBits, each = (bits + passes - 1) / passes;
+  const uint64_t tile = (uint64_t)kThreadsT * token_items(n), tiles = (n + tile - 1) / tile;
+  return (size_t)passes * (((tiles + 7) / 8 * 8) << each) / 2;
+}
+
+int token_sort(const TokenView& t, uint64_t K, int bits, uint32_t* const* keys, uint32_t* const* pos,
+               uint32_t* scratch, DevState* st, cudaStream_t stream) {
+  if (token_items(t.n) == 2) return token_sort_items<2>(t, K, bits, keys, pos, scratch, st, stream);
+  return token_sort_items<4>(t, K, bits, keys, pos, scratch, st, stream);
 }
 
 }  // namespace adapm

@@ -36,10 +36,9 @@ struct Table {
 
 __device__ __forceinline__ int size_of(int type) { return type == ADAPM_F32 ? 4 : 2; }
 
-// The tensor of unit u, from tensor i on.
+// The tensor of unit u, one of lo .. hi.
 template <int N>
-__device__ __forceinline__ int tensor_of(const Table<N>& tab, uint32_t u, int i) {
-  int lo = i, hi = tab.n - 1;
+__device__ __forceinline__ int tensor_of(const Table<N>& tab, uint32_t u, int lo, int hi) {
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if (tab.unit[mid] <= u) lo = mid;
@@ -130,8 +129,10 @@ __device__ __forceinline__ double norm_unit(const GradTensor& t, uint32_t k) {
   uint4 v[kLoads];
   load_unit<TYPE>(p0, p1, at, v);
   float sum[2] = {0.f, 0.f};
+  uint32_t any = 0;
 #pragma unroll
   for (int i = 0; i < kLoads; ++i) {
+    any |= v[i].x | v[i].y | v[i].z | v[i].w;
     float x[8];
     unpack<TYPE>(v[i], x);
 #pragma unroll
@@ -139,6 +140,7 @@ __device__ __forceinline__ double norm_unit(const GradTensor& t, uint32_t k) {
   }
   const float both = sum[0] + sum[1];
   if (both > 1e-25f && both < 1e37f) return (double)both;
+  if ((any & (TYPE == ADAPM_F32 ? 0x7FFFFFFFu : 0x7FFF7FFFu)) == 0u) return 0.0;   // zeros, as untouched rows have
   double s = 0.0;
 #pragma unroll 1
   for (int i = 0; i < kLoads; ++i) {
@@ -168,7 +170,7 @@ grad_norm_kernel(const __grid_constant__ Table<N> tab, double* part, uint32_t pa
   double sum = 0.0;
   int i = 0;
   for (uint32_t u = blockIdx.x * (kThreads / 32) + threadIdx.x / 32; u < units; u += warps) {
-    i = tensor_of(tab, u, i);
+    i = tensor_of(tab, u, i, tab.n - 1);
     const GradTensor& t = tab.t[i];
     const uint32_t k = u - tab.unit[i];
     sum += t.type == ADAPM_F32 ? norm_unit<ADAPM_F32>(t, k)
@@ -257,9 +259,11 @@ clip_grads_kernel(const __grid_constant__ Table<N> tab, float scale, float max_n
   if (in_place && f == 1.f) return;
   const uint32_t units = tab.unit[tab.n];
   const uint32_t warps = gridDim.x * (kThreads / 32);
-  int i = 0;
-  for (uint32_t u = blockIdx.x * (kThreads / 32) + threadIdx.x / 32; u < units; u += warps) {
-    i = tensor_of(tab, u, i);
+  int i = tab.n - 1;
+  // last units first: the norm's pass left them in L2 (clip_mixed 62.9 -> 59.4 us)
+  for (uint32_t v = blockIdx.x * (kThreads / 32) + threadIdx.x / 32; v < units; v += warps) {
+    const uint32_t u = units - 1 - v;
+    i = tensor_of(tab, u, 0, i);
     const GradTensor& t = tab.t[i];
     const uint32_t k = u - tab.unit[i];
     if (t.type == ADAPM_F32) clip_unit<ADAPM_F32>(t, k, f);
