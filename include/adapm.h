@@ -37,17 +37,19 @@
  *     row for it is zero), ADAPM_ENOMEM when replica_capacity is exhausted
  *     (the replicas of that call are not created and reads of those keys go
  *     to the main copy), ADAPM_ESTATE for a refcount overflow (more than
- *     65535 overlapping intents of one worker on one key).  ADAPM_ETIMEOUT
+ *     65535 overlapping intents of one worker on one key) or gradient rows
+ *     whose keys are out of order (adapm_push_grads).  ADAPM_ETIMEOUT
  *     reports that a bounded device-side wait gave up: the key sort of a
- *     push runs as one cooperative launch whose blocks meet at grid
- *     barriers, and a barrier wait is limited.  Work enqueued after such a failure does not
- *     touch the store, and the context is unusable afterwards (destroy it).
+ *     push (or of a large embedding gradient) runs as one cooperative launch
+ *     whose blocks meet at grid barriers, and a barrier wait is limited.  Work
+ *     enqueued after such a failure does not touch the store, and the context
+ *     is unusable afterwards (destroy it).
  *   - ADAPM_ECUDA reports a CUDA runtime error; the context is then unusable.
  *   - Stream capture.  While the library stream records a CUDA graph, calls
  *     with device (or pinned host) arrays that pull, push (adapm_push_noalloc
- *     too), take a training step or sync are recorded, and every launch of the
- *     graph repeats them on the arrays and state it finds; such pushes use no
- *     push plan.
+ *     too), take a training step or sync are recorded, like the token-embedding
+ *     calls, and every launch of the graph repeats them on the arrays and state
+ *     it finds; such pushes and embedding gradients use no push plan.
  *     adapm_intent, adapm_advance_clock and (with ADAPM_ACT_ADAPTIVE)
  *     adapm_sync move the host's clocks and intents, which a launch cannot
  *     repeat: they return ADAPM_EINVAL and change nothing.  Make the first
@@ -427,13 +429,15 @@ typedef struct {
   uint64_t capacity;
   uint64_t created, destroyed;
   uint64_t last_push_unique; /* distinct keys of the last push */
-  uint64_t push_rows;        /* rows pushed, cumulative (training steps included) */
+  uint64_t push_rows;        /* rows pushed, cumulative (training steps included; the rows of
+                                adapm_push_grads, whose number the device knows, are not) */
   uint64_t push_unique;      /* distinct keys per push, summed over pushes */
   uint64_t sync_keys;        /* keys merged by sync, cumulative */
   uint64_t sync_replicas;    /* replicas refreshed by sync, cumulative */
   uint64_t relocations;      /* owner changes, cumulative (relocation only) */
   uint64_t sync_refreshed;   /* replica values written by sync, cumulative */
-  uint64_t planned_pushes;   /* pushes that checked a push plan (see adapm_intent), cumulative */
+  uint64_t planned_pushes;   /* pushes (and embedding gradients) that checked a push plan (see
+                                adapm_intent), cumulative */
   uint64_t plan_misses;      /* of those, pushes whose keys differed, so they sorted, cumulative */
   uint64_t early_advances;   /* advances whose refcount events ran early, cumulative */
   uint64_t early_undone;     /* early events undone (the advance's intents changed), cumulative */
@@ -443,8 +447,10 @@ adapm_status adapm_get_stats(adapm_ctx* ctx, adapm_stats* out);
 
 /* Per-operation device time: when enabled, every call records CUDA events
  * around its work on the library stream.  Operations: 0 intent, 1 advance,
- * 2 pull, 3 push, 4 sync, 5 training-step compute (without its push),
- * 6 push gather-scatter kernel alone, 7 pull gather kernel alone.
+ * 2 pull (adapm_embed too), 3 push (adapm_push_grads too), 4 sync,
+ * 5 training-step compute (without its push; the embedding's gradient, the
+ * gradient norm and clipping too), 6 push gather-scatter kernel alone,
+ * 7 pull gather kernel alone (or adapm_embed's).
  * adapm_profile_read synchronises and returns the summed milliseconds and
  * call counts since the last read (arrays of ADAPM_NUM_OPS). */
 #define ADAPM_NUM_OPS 8
@@ -459,10 +465,11 @@ adapm_status adapm_kernel_launches(uint64_t* out);
 const char* adapm_last_error(adapm_ctx* ctx);
 
 /* Fault injection for tests of the bounded device waits (no GPU fault is
- * involved): the next push of this context sorts its keys in a launch whose
- * first grid barrier waits for arrivals that never come.  That wait gives up
- * after about a second, the push leaves the store untouched, and
- * adapm_wait returns ADAPM_ETIMEOUT; the context is unusable afterwards,
+ * involved): the next push of this context (or embedding gradient that sorts
+ * like one: of more than 131,072 tokens, or of signalled ones) sorts its keys
+ * in a launch whose first grid barrier waits for arrivals that never come.
+ * That wait gives up after about a second, the push leaves the store (the
+ * gradient its outputs) untouched, and adapm_wait returns ADAPM_ETIMEOUT; the context is unusable afterwards,
  * other contexts are unaffected. */
 adapm_status adapm_debug_fail_next_barrier(adapm_ctx* ctx);
 

@@ -1736,10 +1736,11 @@ adapm_status adapm_embed_grad(adapm_ctx* ctx, uint32_t worker, const adapm_token
   a.chunk = p.chunk;
   uint32_t *heads = nullptr, *crossing = nullptr;
   float* parts = nullptr;
-  if (p.count_heads) CK(pool_alloc(ctx, &heads, p.spans));
+  if (p.count_heads) CK(pool_alloc(ctx, &heads, p.spans + 1));
   CK(pool_alloc(ctx, &crossing, p.spans));
   CK(pool_alloc(ctx, &parts, 2 * p.spans * dim));
   a.heads = heads;
+  a.scanned = p.scan_heads;
   a.crossing = crossing;
   a.parts = parts;
   launch_embed_grad(a, p, ctx->stream);

@@ -80,6 +80,7 @@ struct GradArgs {
   uint32_t* count;    // out
   uint32_t chunk;     // rows a group sums, of a span of (groups per block) chunks
   uint32_t* heads;    // per span: distinct keys that begin in it; null: counted where they are needed
+  bool scanned;       // heads holds sums: per span the keys that begin before it, then all
   uint32_t* crossing; // per span: index of the key whose rows run past its end
   float* parts;       // per span: a head and a tail row of `dim` floats
   DevState* st;
@@ -87,7 +88,8 @@ struct GradArgs {
 struct GradPlan {     // sizes of a batch's scratch
   uint32_t chunk;
   uint64_t spans;
-  bool count_heads;   // heads is needed
+  bool count_heads;   // heads is needed,
+  bool scan_heads;    // summed up by a launch of its own
 };
 GradPlan grad_plan(const GradArgs& a, int sms);
 void launch_embed_grad(const GradArgs& a, const GradPlan& p, cudaStream_t stream);

@@ -32,6 +32,7 @@ namespace {
 
 constexpr int kGradSpan = 2048;   // sorted rows staged per block, at most
 constexpr int kGradBlocks = 2;    // grad_sum blocks per SM
+constexpr uint64_t kSpansSummed = 2048;   // spans whose counts every block of grad_sum sums up itself
 
 // V elements of type T as they travel.
 template <int BYTES>
@@ -128,11 +129,35 @@ __global__ void __launch_bounds__(kThreads) grad_heads_kernel(const GradArgs arg
   if (threadIdx.x == 0) a.heads[blockIdx.x] = heads;
 }
 
+// Very many spans: their counts summed up by one block, so that grad_sum need
+// not read all of them.  heads[b] becomes the keys that begin before span b,
+// heads[spans] all.
+__global__ void __launch_bounds__(kThreads) grad_scan_kernel(const GradArgs args, uint32_t spans) {
+  after_previous();
+  if (sort_failed(args.st)) return;
+  uint32_t run = 0;
+  for (uint32_t b0 = 0; b0 < spans; b0 += kThreads) {
+    const uint32_t b = b0 + threadIdx.x;
+    uint32_t h = b < spans ? args.heads[b] : 0u, unused = 0, total, none;
+    block_exclusive_scan2(h, unused, total, none);
+    if (b < spans) args.heads[b] = run + h;
+    run += total;
+  }
+  if (threadIdx.x == 0) args.heads[spans] = run;
+}
+
 // A thread's share of the distinct keys that begin before span b, and in all:
 // from the spans' counts, or from the keys themselves where there are few.
 __device__ __forceinline__ void grad_ranks(const GradArgs& a, uint32_t b, uint32_t spans, uint64_t P0, uint32_t& below,
                                            uint32_t& all) {
   below = all = 0;
+  if (a.scanned) {
+    if (threadIdx.x == 0) {
+      below = a.heads[b];
+      all = a.heads[spans];
+    }
+    return;
+  }
   if (a.heads != nullptr) {
 #pragma unroll 4
     for (uint32_t m = threadIdx.x; m < spans; m += kThreads) {
@@ -515,6 +540,7 @@ GradPlan grad_plan_typed(const GradArgs& a, int sms) {
     p.spans = (a.n + NG * ch - 1) / (NG * ch);
   });
   p.count_heads = a.n > kCountSort;
+  p.scan_heads = p.spans > kSpansSummed;
   return p;
 }
 
@@ -524,8 +550,9 @@ void launch_grad_typed(const GradArgs& a, const GradPlan& p, cudaStream_t stream
     constexpr int V = decltype(Vc)::value, G = decltype(Gc)::value, C = decltype(Cc)::value;
     constexpr int R = 8 / C;
     const uint32_t span = p.chunk * (kThreads / G), spans = (uint32_t)p.spans;
-    note_launches((p.count_heads ? 1 : 0) + (spans > 1 ? 2 : 1));
+    note_launches((p.count_heads ? 1 : 0) + (p.scan_heads ? 1 : 0) + (spans > 1 ? 2 : 1));
     if (p.count_heads) launch_after(grad_heads_kernel, spans, kThreads, 0, stream, a, span);
+    if (p.scan_heads) launch_after(grad_scan_kernel, 1, kThreads, 0, stream, a, spans);
     constexpr size_t smem = grad_smem<C, V>();
     // the kernel's dynamic shared-memory limit is a per-device attribute
     static bool attr_set[64] = {false};

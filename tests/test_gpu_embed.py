@@ -245,6 +245,19 @@ def test_gradient_of_large_batches(gpu_lib, n, dim):
     check_grad(gpu_lib, 70_000, zipf(n, 70_000, n, 0.9), dim, torch.float16, dyadic=True)
 
 
+def test_gradient_of_more_spans_than_a_block_sums(gpu_lib):
+    check_grad(gpu_lib, 3_000_000, zipf(5_000_000, 3_000_000, 4, 0.7), 4, torch.float32, ids=torch.int32, dyadic=True)
+
+
+# either side of where another sort takes over, and of where its tiles grow
+@pytest.mark.parametrize("n", [6143, 6144, 6145, 65_536, 65_537, 131_071, 131_072, 131_073])
+@pytest.mark.parametrize("K", [3, 256, 257, 65_536, 1_000_000, 20_000_000])
+def test_gradient_by_every_sort(gpu_lib, n, K):
+    t = zipf(n, K, n, 0.4)
+    t[::11] = -1
+    check_grad(gpu_lib, K, t, 4, torch.bfloat16, ids=torch.int32 if n % 2 else torch.int64, pad=-1, dyadic=True)
+
+
 @pytest.mark.parametrize("n", [100, 30_000])
 @pytest.mark.parametrize("ids", [torch.int32, torch.int64])
 @pytest.mark.parametrize("pad", [0, 17, -1, -100, 10 ** 6])
@@ -460,6 +473,27 @@ def test_update_of_the_first_floats_of_a_row(gpu_lib, D, dim):
     pm.close()
 
 
+@pytest.mark.parametrize("dim", [4, 64])
+def test_rows_that_begin_between_vectors(gpu_lib, dim):
+    """Gradient rows, and the rows of sums, whose first element is on no vector boundary."""
+    K, n = 80, 300
+    init = table(K, dim)
+    pm = make(gpu_lib, init)
+    t = zipf(n, K)
+    x = torch.randn(n * dim + 1, device="cuda")[1:].view(n, dim)
+    out = gpu_lib.RowGrads(torch.empty(n, dtype=torch.int32, device="cuda"),
+                           torch.zeros(n * dim + 1, device="cuda")[1:].view(n, dim),
+                           torch.empty(1, dtype=torch.int32, device="cuda"))
+    pm.embed_grad(0, torch.from_numpy(t).cuda(), x, out=out)
+    pm.push_grads(0, out.keys, out.rows, 0.5)
+    pm.wait()
+    keys, sums, mags, m = plain_grad(t, x.double().cpu().numpy(), 1.0)
+    check_row_grads(out, keys, sums, 1.01 * (m[:, None] + 1) * U * mags)
+    want, bound = plain_update(init[keys], out.rows[:len(keys)].cpu().numpy(), dim, 0.5, 1.0, False, 0.0)
+    assert (np.abs(pm.read_main(keys) - want) <= bound).all()
+    pm.close()
+
+
 def test_update_equals_a_push_of_the_formed_rows(gpu_lib):
     """The same bits as adapm_push of -lr * g, in every replica state, over several clocks."""
     K, D, W, n = 500, 24, 3, 120
@@ -576,6 +610,21 @@ def test_refusals(gpu_lib):
     assert np.array_equal(pm.read_main(np.arange(20)), table(20, 16))
     pm.close()
     pm6.close()
+
+
+def test_a_sort_that_gives_up_leaves_the_outputs(gpu_lib):
+    """The bounded wait of a large batch's sort runs out (host hook, no GPU fault): ADAPM_ETIMEOUT, nothing written."""
+    pm = make(gpu_lib, table(1000, 8))
+    n = 140_000
+    g = gpu_lib.RowGrads(torch.full((n,), 7, dtype=torch.int32, device="cuda"), torch.full((n, 8), 5.0, device="cuda"),
+                         torch.full((1,), 3, dtype=torch.int32, device="cuda"))
+    pm.debug_fail_next_barrier()
+    pm.embed_grad(0, torch.from_numpy(zipf(n, 1000)).cuda(), torch.ones(n, 8, device="cuda"), out=g)
+    with pytest.raises(gpu_lib.AdaPMError) as e:
+        pm.wait()
+    assert e.value.status == gpu_lib.ETIMEOUT
+    assert (g.keys == 7).all() and (g.rows == 5.0).all() and int(g.count) == 3
+    pm.close()
 
 
 def test_calls_on_a_stream_of_their_own(gpu_lib):
