@@ -878,7 +878,7 @@ bool rows_apart(const adapm_tokens* t, const adapm_rows* r, uint32_t dim) {
     std::swap(s0, s1);
   }
   if (n0 <= 1) return n1 <= 1 || s1 >= (int64_t)dim;
-  return s0 >= (int64_t)dim && (n1 <= 1 || s1 >= (int64_t)(n0 - 1) * s0 + (int64_t)dim);
+  return s0 >= (int64_t)dim && (n1 <= 1 || s1 >= (__int128)(n0 - 1) * s0 + dim);
 }
 
 // Whether pointers are on the device, for a list of them: those inside an

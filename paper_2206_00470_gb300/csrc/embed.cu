@@ -11,6 +11,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <algorithm>
+
 #include "adapm.h"
 #include "embed.cuh"
 #include "rowgroup.cuh"
@@ -67,104 +69,91 @@ __device__ __forceinline__ void load8(const float4* p, float4& a, float4& b) {
                : "l"(p));
 }
 
-// A lane takes units of W float4 of a row, U of them.  W = 2 (16-bit rows of a
-// multiple of eight elements): 256-bit loads and 128-bit stores, half as many
-// of each (262,144 rows of 1024 floats out of a table in L2, where the stores
-// are what counts, 97 -> 93 us).  Rows per group and round: four to eight
-// float4 per lane in flight, at three blocks per SM (64 x 4096 rows of 1024
-// floats: 157 us with as many registers as the compiler likes, 147 at three
-// blocks, 151 at four).
-constexpr int embed_rows(int U, int W) {
-  return W == 2 ? (U == 1 ? 2 : 1) : (U == 1 ? 4 : (U == 2 ? 2 : 1));
+__device__ __forceinline__ void store8(float* p, float4 a, float4 b) {
+  asm volatile("st.global.cs.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(a.x), "f"(a.y), "f"(a.z),
+               "f"(a.w), "f"(b.x), "f"(b.y), "f"(b.z), "f"(b.w)
+               : "memory");
 }
 
-template <class T, int W, int G, int U, int R>
-__global__ void __launch_bounds__(kThreads, U * W == 1 ? 5 : 3)
-embed_kernel(Store s, uint32_t w, const TokenView tv, uint32_t dim, float scale, const RowView ov, bool vec) {
+// A warp takes a batch of up to 32 tokens: a lane per token for what a token
+// needs (its id, two divisions for strided ones, map entry, state, addresses),
+// then the warp's row groups for the rows, which learn the addresses from the
+// lane that has them.  (Every lane of a row group working that out for itself is
+// a hundred instructions per row: 2^20 rows of 100 floats 196 us, now 141.)  The
+// block scheduler hands the batches out: warps that take one after the other
+// (two to four times as many blocks as are resident) lose up to a tenth on wide
+// rows.
+//
+// A lane moves units of W float4 of a row, U of them.  W = 2 (rows of a multiple
+// of eight elements): 256-bit loads, 256-bit or (16-bit types) 128-bit stores,
+// half as many of each (2^20 rows of 64 floats 106 us, now 75).  Blocks per SM,
+// by what the registers hold and what was fastest: 2^20 rows of 100 floats 171
+// us at five, 142 at eight; 2^18 of 300 floats 104 at four, 110 at five; 64 x
+// 4096 of 1024 147 at three, 151 at four.
+constexpr int embed_blocks_per_sm(int U, int W) { return U == 1 ? 8 : (U * W <= 3 ? 4 : 3); }
+// Tokens per batch, at most.
+constexpr uint32_t embed_batch(int U) { return U == 1 ? 32 : 4; }
+
+template <class T, int W, int G, int U>
+__global__ void __launch_bounds__(kThreads, embed_blocks_per_sm(U, W))
+embed_kernel(Store s, uint32_t w, const TokenView tv, uint32_t per, uint32_t dim, float scale, const RowView ov,
+             bool vec) {
   after_previous();
-  constexpr int C = U * W;
-  const int lane = threadIdx.x & (G - 1);
-  const uint64_t g = group_id<G>(), ng = group_count<G>();
-  const uint32_t n4 = (dim + 3) >> 2;
-  const uint64_t n = tv.n;
-  const int32_t* mapw = s.map + (uint64_t)w * s.K;
+  constexpr int C = U * W, GW = 32 / G;
+  const uint32_t lane32 = threadIdx.x & 31, lane = lane32 & (G - 1), sub = lane32 / G;
+  const uint32_t n4 = (dim + 3) >> 2, n = (uint32_t)tv.n;
+  const uint64_t base = ((uint64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32) * per;
+  if (base >= n) return;   // warp-uniform
+  const uint32_t cnt = n - base < per ? (uint32_t)(n - base) : per;
+  const uint32_t k = lane32 < cnt ? token_key(tv, base + lane32, s.K) : kNoKey;
   s.par = s.st->par;
   const bool mapped = s.st->live != 0;   // without replicas every map entry is -1
-  const uint64_t step = ng * R;
-  bool bad = false;
+  const float4 *src = nullptr, *add = nullptr;
+  if (k < s.K) src = row_source(s, mapped ? s.map[(uint64_t)w * s.K + k] : -1, k, &add);
+  else if (k == kBadKey) set_error(s.st, ERR_KEY_RANGE);
+  T* out = reinterpret_cast<T*>(ov.data) + (lane32 < cnt ? row_offset(ov, (uint32_t)base + lane32) : 0);
+  const bool adds = __any_sync(0xFFFFFFFFu, add != nullptr);
   auto col_of = [&](int c) { return W * (uint32_t)(lane + c / W * G) + c % W; };
-  auto load_keys = [&](uint64_t b, uint32_t (&k)[R]) {
-#pragma unroll
-    for (int r = 0; r < R; ++r) k[r] = b + r < n ? token_key(tv, b + r, s.K) : kNoKey;
+  auto of_token = [&](const void* p, uint32_t t) {   // what the lane of token t has
+    return __shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(p), t & 31);
   };
-  auto load_slots = [&](const uint32_t (&k)[R], int32_t (&sl)[R]) {
-#pragma unroll
-    for (int r = 0; r < R; ++r) sl[r] = mapped && k[r] < s.K ? mapw[k[r]] : -1;
-  };
-  uint64_t base = g * R;
-  uint32_t k0[R], k1[R];
-  int32_t sl0[R];
-  load_keys(base, k0);
-  load_keys(base + step, k1);
-  load_slots(k0, sl0);
-  for (; base < n; base += step) {
-    const float4* src[R];
-    const float4* add[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      src[r] = add[r] = nullptr;
-      if (k0[r] < s.K) src[r] = row_source(s, sl0[r], k0[r], &add[r]);
-      else if (k0[r] == kBadKey) bad = true;
-    }
-    float4 v[R][C];
+  for (uint32_t j = 0; j < cnt; j += GW) {
+    const uint32_t t = j + sub;
+    const float4* from = reinterpret_cast<const float4*>(of_token(src, t));
+    T* row = reinterpret_cast<T*>(of_token(out, t));
+    float4 v[C];
 #pragma unroll
     for (int c = 0; c < C; c += W) {
       const uint32_t col = col_of(c);
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-#pragma unroll
-        for (int j = 0; j < W; ++j) v[r][c + j] = f4zero();
-        if (src[r] == nullptr || col >= n4) continue;
-        if constexpr (W == 2) load8(src[r] + col, v[r][c], v[r][c + 1]);
-        else v[r][c] = src[r][col];
-      }
+      for (int q = 0; q < W; ++q) v[c + q] = f4zero();
+      if (t >= cnt || from == nullptr || col >= n4) continue;
+      if constexpr (W == 2) load8(from + col, v[c], v[c + 1]);
+      else v[c] = from[col];
     }
+    if (adds) {
+      const float4* more = reinterpret_cast<const float4*>(of_token(add, t));
 #pragma unroll
-    for (int r = 0; r < R; ++r)
-      if (add[r] != nullptr)
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-          const uint32_t col = col_of(c);
-          if (col < n4) v[r][c] = f4add(v[r][c], add[r][col]);
-        }
-    int32_t sl1[R];
-    uint32_t k2[R];
-    load_slots(k1, sl1);
-    load_keys(base + 2 * step, k2);
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      if (base + r >= n) break;
-      T* row = reinterpret_cast<T*>(ov.data) + row_offset(ov, (uint32_t)(base + r));
-#pragma unroll
-      for (int c = 0; c < C; c += W) {
+      for (int c = 0; c < C; ++c) {
         const uint32_t col = col_of(c);
-        if (col >= n4) continue;
-        if constexpr (W == 2) {
-          const uint2 a = pack4(f4scale(v[r][c], scale), T()), b = pack4(f4scale(v[r][c + 1], scale), T());
-          __stcs(reinterpret_cast<uint4*>(row + 4 * col), make_uint4(a.x, a.y, b.x, b.y));
-        } else {
-          put4(row, 4 * col, dim, f4scale(v[r][c], scale), vec);
-        }
+        if (t < cnt && more != nullptr && col < n4) v[c] = f4add(v[c], more[col]);
       }
     }
+    if (t >= cnt) continue;
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      k0[r] = k1[r];
-      sl0[r] = sl1[r];
-      k1[r] = k2[r];
+    for (int c = 0; c < C; c += W) {
+      const uint32_t col = col_of(c);
+      if (col >= n4) continue;
+      if constexpr (W == 2 && sizeof(T) == 4) {
+        store8(row + 4 * col, f4scale(v[c], scale), f4scale(v[c + 1], scale));
+      } else if constexpr (W == 2) {
+        const uint2 x = pack4(f4scale(v[c], scale), T()), y = pack4(f4scale(v[c + 1], scale), T());
+        __stcs(reinterpret_cast<uint4*>(row + 4 * col), make_uint4(x.x, x.y, y.x, y.y));
+      } else {
+        put4(row, 4 * col, dim, f4scale(v[c], scale), vec);
+      }
     }
   }
-  if (bad && lane == 0) set_error(s.st, ERR_KEY_RANGE);
 }
 
 // Whether every row begins on a multiple of `elements` elements.
@@ -177,24 +166,28 @@ template <class T>
 void launch_typed(const Store& s, uint32_t w, const TokenView& t, uint32_t dim, float scale, const RowView& out,
                   int sms, cudaStream_t stream) {
   auto go = [&](auto Wc, auto Gc, auto Uc) {
-    constexpr int W = decltype(Wc)::value, G = decltype(Gc)::value, U = decltype(Uc)::value, R = embed_rows(U, W);
-    launch_after(embed_kernel<T, W, G, U, R>, grid_for((t.n + R - 1) / R, G, sms), kThreads, 0, stream, s, w, t, dim,
-                 scale, out, rows_aligned(out, sizeof(T), 4));
+    constexpr int W = decltype(Wc)::value, G = decltype(Gc)::value, U = decltype(Uc)::value;
+    // few tokens: batches (of whole rounds of the warp's groups) that give every resident warp some (of six
+    // blocks per SM: 24 x 1023 rows of 256 5.3 us, of eight 5.8)
+    constexpr uint64_t round = 32 / G, most = std::max<uint64_t>(round, embed_batch(U));
+    const uint64_t warps = (uint64_t)sms * std::min(embed_blocks_per_sm(U, W), 6) * (kThreads / 32);
+    const uint64_t per = std::min<uint64_t>(most, ((t.n + warps - 1) / warps + round - 1) / round * round);
+    const uint64_t blocks = (t.n + per * (kThreads / 32) - 1) / (per * (kThreads / 32));
+    launch_after(embed_kernel<T, W, G, U>, (unsigned)blocks, kThreads, 0, stream, s, w, t, (uint32_t)per, dim, scale,
+                 out, rows_aligned(out, sizeof(T), 4));
   };
   using std::integral_constant;
-  if constexpr (sizeof(T) == 2) {
-    if (dim % 8 == 0 && s.D % 8 == 0 && rows_aligned(out, sizeof(T), 8)) {
-      const integral_constant<int, 2> two{};
-      const uint32_t units = dim / 8;
-      if (units <= 4) go(two, integral_constant<int, 4>{}, integral_constant<int, 1>{});
-      else if (units <= 8) go(two, integral_constant<int, 8>{}, integral_constant<int, 1>{});
-      else if (units <= 16) go(two, integral_constant<int, 16>{}, integral_constant<int, 1>{});
-      else if (units <= 32) go(two, integral_constant<int, 32>{}, integral_constant<int, 1>{});
-      else if (units <= 64) go(two, integral_constant<int, 32>{}, integral_constant<int, 2>{});
-      else if (units <= 96) go(two, integral_constant<int, 32>{}, integral_constant<int, 3>{});
-      else go(two, integral_constant<int, 32>{}, integral_constant<int, 4>{});
-      return;
-    }
+  if (dim % 8 == 0 && s.D % 8 == 0 && rows_aligned(out, sizeof(T), 8)) {
+    const integral_constant<int, 2> two{};
+    const uint32_t units = dim / 8;
+    if (units <= 4) go(two, integral_constant<int, 4>{}, integral_constant<int, 1>{});
+    else if (units <= 8) go(two, integral_constant<int, 8>{}, integral_constant<int, 1>{});
+    else if (units <= 16) go(two, integral_constant<int, 16>{}, integral_constant<int, 1>{});
+    else if (units <= 32) go(two, integral_constant<int, 32>{}, integral_constant<int, 1>{});
+    else if (units <= 64) go(two, integral_constant<int, 32>{}, integral_constant<int, 2>{});
+    else if (units <= 96) go(two, integral_constant<int, 32>{}, integral_constant<int, 3>{});
+    else go(two, integral_constant<int, 32>{}, integral_constant<int, 4>{});
+    return;
   }
   dispatch_gc((dim + 3) / 4, [&](auto Gc, auto Cc) { go(integral_constant<int, 1>{}, Gc, Cc); });
 }

@@ -25,9 +25,10 @@ __global__ void __launch_bounds__(kThreads) copy_tokens_kernel(const TokenView t
 // staged in shared memory: kSlices threads share the others of kPer keys, four
 // a load.  n^2 comparisons over the whole GPU in one launch and without a wait
 // between blocks, where a radix sort of so few keys is a chain of passes.
-// Bound by latency up to 2,000 tokens (4 us), by the comparisons above: 4,096
-// tokens 6.7 us, 6,000 10 us, 8,192 15 us (token sort: 12, 12.5, 12 us and the
-// launch of grad_heads).
+// Bound by latency up to 2,000 tokens (3.8 us), by the comparisons above: 4,096
+// tokens 6.1 us, 6,000 9.5 us, 8,192 15 us.  The token sort below takes 12 us
+// for any of these and needs grad_heads' launch; one block's sort (sort_small)
+// 9, 13.5, 20 and 21 us.
 constexpr int kThreadsC = 256, kPer = 2, kSlices = 32, kOwn = kThreadsC / kSlices * kPer;
 
 __global__ void __launch_bounds__(kThreadsC) count_sort_kernel(const TokenView t, uint64_t K, uint32_t* skeys,
@@ -113,10 +114,10 @@ __global__ void __launch_bounds__(kThreadsC) count_sort_kernel(const TokenView t
 // 1024).  The first pass reads the tokens themselves, in whatever layout they
 // have.  All of it is latency: a launch takes 3.5 to 6 us.
 //
-// Grid sort (sort.cu) -> this, tokens of 1M keys: 16,384 26 -> 13 us, 65,536
-// 31 -> 19 us, 131,072 31 -> 24 us; more tiles make the rows long: 262,144 27
-// to 35 us there, 35 to 42 here.  (Digits of 10 bits and tiles of 2048 took 17,
-// 22 and 27 us.)
+// Grid sort (sort.cu) -> this, tokens of 1M keys: 16,384 26 -> 12.7 us, 65,536
+// 31 -> 17.8 us, 131,072 31 -> 24 us; more tiles make the rows long: 262,144 34
+// us there, 35 to 42 here.  (Digits of 10 bits and tiles of 2048 took 17, 22 and
+// 27 us.)
 // ---------------------------------------------------------------------------
 constexpr int kThreadsT = 1 << kTokenBits, kWarpsT = kThreadsT / 32;   // a thread per digit
 constexpr uint32_t kTilesMost = 128;

@@ -494,10 +494,11 @@ def test_rows_that_begin_between_vectors(gpu_lib, dim):
     pm.close()
 
 
-def test_update_equals_a_push_of_the_formed_rows(gpu_lib):
+@pytest.mark.parametrize("refresh", [False, True])
+def test_update_equals_a_push_of_the_formed_rows(gpu_lib, refresh):
     """The same bits as adapm_push of -lr * g, in every replica state, over several clocks."""
     K, D, W, n = 500, 24, 3, 120
-    a, b = (make(gpu_lib, table(K, D), W) for _ in range(2))
+    a, b = (make(gpu_lib, table(K, D), W, delta_refresh=refresh) for _ in range(2))
     rng = np.random.default_rng(2)
     for clock in range(6):
         for w in range(W):
