@@ -466,7 +466,7 @@ const char* adapm_last_error(adapm_ctx* ctx);
 
 /* Fault injection for tests of the bounded device waits (no GPU fault is
  * involved): the next push of this context (or embedding gradient that sorts
- * like one: of more than 131,072 tokens, or of signalled ones) sorts its keys
+ * like one: of more than 2^19 tokens, or of signalled ones) sorts its keys
  * in a launch whose first grid barrier waits for arrivals that never come.
  * That wait gives up after about a second, the push leaves the store (the
  * gradient its outputs) untouched, and adapm_wait returns ADAPM_ETIMEOUT; the context is unusable afterwards,

@@ -111,16 +111,16 @@ __global__ void __launch_bounds__(kThreadsC) count_sort_kernel(const TokenView t
 // tile) of the items that every tile holds, by summing the table's rows: no
 // scan launch, no wait between blocks.  While it moves its items it counts
 // them into the next pass's table (packed 16-bit counts; a tile holds at most
-// 1024).  The first pass reads the tokens themselves, in whatever layout they
-// have.  All of it is latency: a launch takes 3.5 to 6 us.
+// 4096).  The first pass reads the tokens themselves, in whatever layout they
+// have.  Bound by the latency of its launches, 3.5 to 8 us each.
 //
-// Grid sort (sort.cu) -> this, tokens of 1M keys: 16,384 26 -> 12.7 us, 65,536
-// 31 -> 17.8 us, 131,072 31 -> 24 us; more tiles make the rows long: 262,144 34
-// us there, 35 to 42 here.  (Digits of 10 bits and tiles of 2048 took 17, 22 and
-// 27 us.)
+// Grid sort (sort.cu) -> this, tokens of 1M keys: 16,384 26 -> 13 us, 65,536
+// 31 -> 17.5, 131,072 31 -> 21, 262,144 34 -> 26, 524,288 50 -> 40; 2^20, in
+// tiles of 8192, 69 both.  (Digits of 10 bits take longer per launch than they
+// save launches: 65,536 22 us, of 11 bits 24.)
 // ---------------------------------------------------------------------------
-constexpr int kThreadsT = 1 << kTokenBits, kWarpsT = kThreadsT / 32;   // a thread per digit
 constexpr uint32_t kTilesMost = 128;
+static_assert(256 >= 1 << kTokenBits, "a thread per digit");
 
 struct TokenPass {
   const uint32_t* keys;   // null: the tokens
@@ -168,18 +168,18 @@ __device__ __forceinline__ bool load_tokens(const TokenView& t, uint64_t K, uint
 }
 
 // The first pass's table, and the next ones cleared.
-template <int ITEMS>
-__global__ void __launch_bounds__(kThreadsT) token_count_kernel(const TokenView t, uint64_t K, uint16_t* table,
+template <int NT, int ITEMS>
+__global__ void __launch_bounds__(NT) token_count_kernel(const TokenView t, uint64_t K, uint16_t* table,
                                                                 uint32_t* clear, uint32_t clear_words, uint32_t stride,
                                                                 int bits, DevState* st) {
   after_previous();
   extern __shared__ __align__(16) unsigned char dsm[];
   uint32_t* cnt = reinterpret_cast<uint32_t*>(dsm);
-  const uint32_t digits = 1u << bits, tile0 = blockIdx.x * (kThreadsT * ITEMS);
-  for (uint32_t i = blockIdx.x * kThreadsT + threadIdx.x; i < clear_words; i += gridDim.x * kThreadsT) clear[i] = 0u;
+  const uint32_t digits = 1u << bits, tile0 = blockIdx.x * (NT * ITEMS);
+  for (uint32_t i = blockIdx.x * NT + threadIdx.x; i < clear_words; i += gridDim.x * NT) clear[i] = 0u;
   uint32_t key[ITEMS];
   const bool bad = load_tokens<ITEMS>(t, K, tile0, key);
-  for (uint32_t d = threadIdx.x; d < digits; d += kThreadsT) cnt[d] = 0u;
+  for (uint32_t d = threadIdx.x; d < digits; d += NT) cnt[d] = 0u;
   __syncthreads();
 #pragma unroll
   for (int it = 0; it < ITEMS; ++it) {
@@ -189,26 +189,31 @@ __global__ void __launch_bounds__(kThreadsT) token_count_kernel(const TokenView 
     if (in && (peers & lanemask_lt()) == 0u) atomicAdd(cnt + d, (uint32_t)__popc(peers));
   }
   __syncthreads();
-  for (uint32_t d = threadIdx.x; d < digits; d += kThreadsT) table[d * stride + blockIdx.x] = (uint16_t)cnt[d];
+  for (uint32_t d = threadIdx.x; d < digits; d += NT) table[d * stride + blockIdx.x] = (uint16_t)cnt[d];
   if (blockIdx.x == 0)   // tiles of the row that do not exist
-    for (uint32_t d = threadIdx.x; d < digits; d += kThreadsT)
+    for (uint32_t d = threadIdx.x; d < digits; d += NT)
       for (uint32_t b = gridDim.x; b < stride; ++b) table[d * stride + b] = 0;
   if (__syncthreads_or(bad) && threadIdx.x == 0) set_error(st, ERR_KEY_RANGE);
 }
 
-// Dynamic shared memory of token_pass: the digits' places, then the warps'
-// digit counts.
-size_t token_smem(int bits) { return ((size_t)4 + 2 * kWarpsT) << bits; }
+// Dynamic shared memory of token_pass: the digits' places, the warps' digit
+// counts, and the tile in order, so that a digit's items leave in one run
+// (131,072 tokens 17 to 23 us so, 19 to 26 item by item; 262,144 22 to 29, 25
+// to 35).
+template <int NT, int ITEMS>
+size_t token_smem(int bits) {
+  return (((size_t)4 + NT / 16) << bits) + (size_t)NT * ITEMS * 8;
+}
 
-template <int ITEMS>
-__global__ void __launch_bounds__(kThreadsT) token_pass_kernel(const TokenView t, uint64_t K, const TokenPass p) {
+template <int NT, int ITEMS>
+__global__ void __launch_bounds__(NT) token_pass_kernel(const TokenView t, uint64_t K, const TokenPass p) {
   after_previous();
   extern __shared__ __align__(16) unsigned char dsm[];
   const uint32_t digits = 1u << p.bits;
   uint32_t* place = reinterpret_cast<uint32_t*>(dsm);
   uint16_t* wcnt = reinterpret_cast<uint16_t*>(place + digits);   // [warp][digit]
-  __shared__ uint32_t scan[kWarpsT];
-  const uint32_t tile0 = blockIdx.x * (kThreadsT * ITEMS);
+  __shared__ uint32_t scan[(NT / 32)];
+  const uint32_t tile0 = blockIdx.x * (NT * ITEMS);
   const int warp = threadIdx.x / 32;
   uint32_t key[ITEMS], pos[ITEMS], rank[ITEMS];
   if (p.keys == nullptr) {
@@ -239,7 +244,7 @@ __global__ void __launch_bounds__(kThreadsT) token_pass_kernel(const TokenView t
       }
     }
   }
-  for (uint32_t i = threadIdx.x; i < digits * kWarpsT / 2; i += kThreadsT) reinterpret_cast<uint32_t*>(wcnt)[i] = 0u;
+  for (uint32_t i = threadIdx.x; i < digits * (NT / 32) / 2; i += NT) reinterpret_cast<uint32_t*>(wcnt)[i] = 0u;
   __syncthreads();
   // ranks within the warp
   uint32_t peers[ITEMS];
@@ -259,45 +264,70 @@ __global__ void __launch_bounds__(kThreadsT) token_pass_kernel(const TokenView t
   // where the digit's items of this tile go: behind those of lower digits and
   // of the tiles before, warp by warp
   uint32_t total;
-  const uint32_t base = block_exclusive_scan<kThreadsT>(all, &total, scan);   // (a barrier: the warps' counts are final)
+  const uint32_t base = block_exclusive_scan<NT>(all, &total, scan);   // (a barrier: the warps' counts are final)
+  uint32_t h[NT / 32], mine = 0;
+#pragma unroll
+  for (int w = 0; w < NT / 32; ++w) {
+    h[w] = threadIdx.x < digits ? wcnt[w * digits + threadIdx.x] : 0u;
+    mine += h[w];
+  }
+  const uint32_t first = block_exclusive_scan<NT>(mine, &total, scan);   // in the ordered tile
   if (threadIdx.x < digits) {
-    uint32_t h[kWarpsT], run = 0;
+    uint32_t run = first;
 #pragma unroll
-    for (int w = 0; w < kWarpsT; ++w) h[w] = wcnt[w * digits + threadIdx.x];
-#pragma unroll
-    for (int w = 0; w < kWarpsT; ++w) {
+    for (int w = 0; w < NT / 32; ++w) {
       wcnt[w * digits + threadIdx.x] = (uint16_t)run;
       run += h[w];
     }
-    place[threadIdx.x] = base + before;
+    place[threadIdx.x] = base + before - first;   // (of the ordered tile's begin)
   }
   __syncthreads();
+  uint32_t* tk = reinterpret_cast<uint32_t*>(wcnt + digits * (NT / 32));
+  uint32_t* tp = tk + NT * ITEMS;
 #pragma unroll
-  for (int it = 0; it < ITEMS; ++it) {
-    const bool in = item_at<ITEMS>(tile0, it) < p.n;
-    const uint32_t d = (key[it] >> p.shift) & (digits - 1);
-    const uint32_t at = in ? place[d] + wcnt[warp * digits + d] + rank[it] : 0u;
+  for (int it = 0; it < ITEMS; ++it)
+    if (item_at<ITEMS>(tile0, it) < p.n) {
+      const uint32_t i = wcnt[warp * digits + ((key[it] >> p.shift) & (digits - 1))] + rank[it];
+      tk[i] = key[it];
+      tp[i] = pos[it];
+    }
+  __syncthreads();
+  const uint32_t len = p.n - tile0 < (uint32_t)(NT * ITEMS) ? p.n - tile0 : (uint32_t)(NT * ITEMS);
+  for (uint32_t i0 = 0; i0 < len; i0 += NT) {   // block-uniform
+    const uint32_t i = i0 + threadIdx.x;
+    const bool in = i < len;
+    const uint32_t k = in ? tk[i] : 0u;
+    const uint32_t at = in ? place[(k >> p.shift) & (digits - 1)] + i : 0u;
     if (in) {
-      p.keys_out[at] = key[it];
-      p.pos_out[at] = pos[it];
+      p.keys_out[at] = k;
+      p.pos_out[at] = tp[i];
     }
     if (p.next != nullptr) {
-      const uint32_t nd = (key[it] >> (p.shift + p.bits)) & ((1u << p.next_bits) - 1);
-      const uint32_t cell = in ? nd * p.stride + at / (kThreadsT * ITEMS) : 0xFFFFFFFFu;
-      const uint32_t peers = __match_any_sync(0xFFFFFFFFu, cell);
-      if (in && (peers & lanemask_lt()) == 0u) atomicAdd(p.next + cell / 2, (uint32_t)__popc(peers) << (16 * (cell & 1)));
+      const uint32_t nd = (k >> (p.shift + p.bits)) & ((1u << p.next_bits) - 1);
+      const uint32_t cell = in ? nd * p.stride + at / (NT * ITEMS) : 0xFFFFFFFFu;
+      const uint32_t same = __match_any_sync(0xFFFFFFFFu, cell);
+      if (in && (same & lanemask_lt()) == 0u) atomicAdd(p.next + cell / 2, (uint32_t)__popc(same) << (16 * (cell & 1)));
     }
   }
 }
 
-template <int ITEMS>
+template <int NT, int ITEMS>
 int token_sort_items(const TokenView& t, uint64_t K, int bits, uint32_t* const* keys, uint32_t* const* pos,
                              uint32_t* scratch, DevState* st, cudaStream_t stream) {
   const int passes = (bits + kTokenBits - 1) / kTokenBits, each = (bits + passes - 1) / passes;
-  const uint32_t tiles = (uint32_t)((t.n + kThreadsT * ITEMS - 1) / (kThreadsT * ITEMS)), stride = (tiles + 7) / 8 * 8;
+  const uint32_t tiles = (uint32_t)((t.n + NT * ITEMS - 1) / (NT * ITEMS)), stride = (tiles + 7) / 8 * 8;
   const uint32_t words = (stride << each) / 2;   // of a table
+  // the kernel's dynamic shared-memory limit is a per-device attribute
+  static bool attr_set[64] = {false};
+  int dev = 0;
+  cudaGetDevice(&dev);
+  if (token_smem<NT, ITEMS>(kTokenBits) > 48 * 1024 && (dev < 0 || dev >= 64 || !attr_set[dev])) {
+    cudaFuncSetAttribute(token_pass_kernel<NT, ITEMS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                         (int)token_smem<NT, ITEMS>(kTokenBits));
+    if (dev >= 0 && dev < 64) attr_set[dev] = true;
+  }
   note_launches(1 + passes);
-  launch_after(token_count_kernel<ITEMS>, tiles, kThreadsT, sizeof(uint32_t) << each, stream, t, K,
+  launch_after(token_count_kernel<NT, ITEMS>, tiles, NT, sizeof(uint32_t) << each, stream, t, K,
                reinterpret_cast<uint16_t*>(scratch), scratch + words, (uint32_t)(passes - 1) * words, stride, each, st);
   for (int i = 0; i < passes; ++i) {
     TokenPass p{};
@@ -312,7 +342,7 @@ int token_sort_items(const TokenView& t, uint64_t K, int bits, uint32_t* const* 
     p.stride = stride;
     p.shift = i * each;
     p.bits = p.next_bits = each;
-    launch_after(token_pass_kernel<ITEMS>, tiles, kThreadsT, token_smem(each), stream, t, K, p);
+    launch_after(token_pass_kernel<NT, ITEMS>, tiles, NT, token_smem<NT, ITEMS>(each), stream, t, K, p);
   }
   return (passes - 1) & 1;
 }
@@ -330,19 +360,27 @@ void launch_count_sort(const TokenView& t, uint64_t K, uint32_t* skeys, uint32_t
   launch_after(count_sort_kernel, (unsigned)((t.n + kOwn - 1) / kOwn), kThreadsC, 0, stream, t, K, skeys, spos, st);
 }
 
-// Tiles of 512 tokens, or twice that where they would be too many.
-int token_items(uint64_t n) { return n <= (uint64_t)kTilesMost * kThreadsT * 2 ? 2 : 4; }
+// Tiles of 512 tokens, doubled until there are at most kTilesMost.
+uint32_t token_tile(uint64_t n) {
+  uint32_t tile = 512;
+  while ((uint64_t)tile * kTilesMost < n) tile *= 2;
+  return tile;
+}
 
 size_t token_sort_words(uint64_t n, int bits) {
   const int passes = (bits + kTokenBits - 1) / kTokenBits, each = (bits + passes - 1) / passes;
-  const uint64_t tile = (uint64_t)kThreadsT * token_items(n), tiles = (n + tile - 1) / tile;
+  const uint64_t tile = token_tile(n), tiles = (n + tile - 1) / tile;
   return (size_t)passes * (((tiles + 7) / 8 * 8) << each) / 2;
 }
 
 int token_sort(const TokenView& t, uint64_t K, int bits, uint32_t* const* keys, uint32_t* const* pos,
                uint32_t* scratch, DevState* st, cudaStream_t stream) {
-  if (token_items(t.n) == 2) return token_sort_items<2>(t, K, bits, keys, pos, scratch, st, stream);
-  return token_sort_items<4>(t, K, bits, keys, pos, scratch, st, stream);
+  switch (token_tile(t.n)) {
+    case 512: return token_sort_items<256, 2>(t, K, bits, keys, pos, scratch, st, stream);
+    case 1024: return token_sort_items<256, 4>(t, K, bits, keys, pos, scratch, st, stream);
+    case 2048: return token_sort_items<512, 4>(t, K, bits, keys, pos, scratch, st, stream);
+    default: return token_sort_items<512, 8>(t, K, bits, keys, pos, scratch, st, stream);
+  }
 }
 
 }  // namespace adapm

@@ -250,7 +250,8 @@ def test_gradient_of_more_spans_than_a_block_sums(gpu_lib):
 
 
 # either side of where another sort takes over, and of where its tiles grow
-@pytest.mark.parametrize("n", [6143, 6144, 6145, 65_536, 65_537, 131_071, 131_072, 131_073])
+@pytest.mark.parametrize("n", [6143, 6144, 6145, 65_536, 65_537, 131_071, 131_072, 131_073, 262_145,
+                               524_288, 524_289])
 @pytest.mark.parametrize("K", [3, 256, 257, 65_536, 1_000_000, 20_000_000])
 def test_gradient_by_every_sort(gpu_lib, n, K):
     t = zipf(n, K, n, 0.4)
@@ -614,13 +615,15 @@ def test_refusals(gpu_lib):
 
 
 def test_a_sort_that_gives_up_leaves_the_outputs(gpu_lib):
-    """The bounded wait of a large batch's sort runs out (host hook, no GPU fault): ADAPM_ETIMEOUT, nothing written."""
+    """The bounded wait of a signalled batch's sort runs out (host hook, no GPU fault): ADAPM_ETIMEOUT, nothing written."""
     pm = make(gpu_lib, table(1000, 8))
-    n = 140_000
+    n = 20_000
+    t = torch.from_numpy(zipf(n, 1000)).cuda()
+    pm.intent(0, t, 0, 5)
     g = gpu_lib.RowGrads(torch.full((n,), 7, dtype=torch.int32, device="cuda"), torch.full((n, 8), 5.0, device="cuda"),
                          torch.full((1,), 3, dtype=torch.int32, device="cuda"))
     pm.debug_fail_next_barrier()
-    pm.embed_grad(0, torch.from_numpy(zipf(n, 1000)).cuda(), torch.ones(n, 8, device="cuda"), out=g)
+    pm.embed_grad(0, t, torch.ones(n, 8, device="cuda"), out=g)
     with pytest.raises(gpu_lib.AdaPMError) as e:
         pm.wait()
     assert e.value.status == gpu_lib.ETIMEOUT
