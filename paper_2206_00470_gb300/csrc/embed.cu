@@ -6,8 +6,8 @@
 // rounding to 16 bits on the way, so that the fp32 rows never travel.  Bound by
 // memory: 4 dim bytes in per distinct token (repeats come from L2), dim
 // elements out per token.  64 x 4096 tokens of 62,000 distinct ones, rows of
-// 1024, bf16 out: 142 us, 5.6 TB/s of those bytes; 64 x 2048 distinct rows, fp32
-// out, 160 us, 6.7 TB/s.
+// 1024, bf16 out: 139 us, 5.7 TB/s of those bytes; 64 x 2048 tokens of 250,000
+// at random, fp32 out, 157 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -88,8 +88,7 @@ __device__ __forceinline__ void store8(float* p, float4 a, float4 b) {
 // of eight elements): 256-bit loads, 256-bit or (16-bit types) 128-bit stores,
 // half as many of each (2^20 rows of 64 floats 106 us, now 75).  Blocks per SM,
 // by what the registers hold and what was fastest: 2^20 rows of 100 floats 171
-// us at five, 142 at eight; 2^18 of 300 floats 104 at four, 110 at five; 64 x
-// 4096 of 1024 147 at three, 151 at four.
+// us at five, 142 at eight; 2^18 of 300 floats 104 at four, 110 at five.
 constexpr int embed_blocks_per_sm(int U, int W) { return U == 1 ? 8 : (U * W <= 3 ? 4 : 3); }
 // Tokens per batch, at most.
 constexpr uint32_t embed_batch(int U) { return U == 1 ? 32 : 4; }
