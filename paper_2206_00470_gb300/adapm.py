@@ -246,12 +246,14 @@ _float_types = {}   # torch dtype -> element type of the ABI
 
 
 def _type_of(dtype):
-    if not _float_types:
+    known = _float_types.get(dtype)
+    if known is None:
         torch = _torch()
         _float_types.update({torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16})
-    if dtype not in _float_types:
-        raise ValueError(f"rows and gradients are float32, float16 or bfloat16, not {dtype}")
-    return _float_types[dtype]
+        if dtype not in _float_types:
+            raise ValueError(f"rows and gradients are float32, float16 or bfloat16, not {dtype}")
+        known = _float_types[dtype]
+    return known
 
 
 def _one_stride(shape, strides):
@@ -310,7 +312,7 @@ class GradList:
 
 
 def _check_norm(norm):
-    if norm is not None and (not norm.is_cuda or norm.dtype != _torch().float32 or norm.numel() != 1):
+    if norm is not None and not (norm.is_cuda and norm.dtype is _torch().float32 and norm.numel() == 1):
         raise ValueError("norm is a float32 scalar on the GPU")
 
 
@@ -500,11 +502,11 @@ class ParameterManager:
             with self._on_stream():
                 tokens = tokens.to(torch.int64)
             wide = True
-        shape, *row_shape, dim = tokens.shape, *rows.shape
-        if tuple(shape) != tuple(row_shape):
-            raise ValueError(f"{what} must have shape {(*shape, 'dim')}, not {tuple(rows.shape)}")
+        shape, row_shape = tokens.shape, rows.shape
+        if not row_shape or row_shape[:-1] != shape:
+            raise ValueError(f"{what} must have shape {(*shape, 'dim')}, not {tuple(row_shape)}")
         steps = rows.stride()
-        if dim > 1 and steps[-1] != 1:
+        if steps[-1] != 1 and row_shape[-1] > 1:
             if what == "out":
                 raise ValueError("elements of a row of out must follow each other")
             with self._on_stream():
@@ -556,7 +558,7 @@ class ParameterManager:
 
     def embed_grad(self, worker, tokens, grad, scale=1.0, pad=None, out=None):
         """RowGrads of the distinct tokens: scale times the sum of the rows of grad (*tokens.shape, dim) that belong
-        to each.  out: RowGrads with room for tokens.numel() keys and rows."""
+        to each.  out: RowGrads with room for tokens.numel() keys and rows, of which the result is the front."""
         torch = _torch()
         tokens, grad = self._describe(tokens, pad, grad, "grad")
         n, dim = tokens.numel(), grad.shape[-1]
@@ -571,6 +573,8 @@ class ParameterManager:
             raise ValueError("out needs int32 keys, float32 rows of dim elements for every token, and an int32 count")
         self._check(self._lib.adapm_embed_grad(self._h, worker, self._t_ref, dim, scale, self._r_ref, _out_ptr(out.keys),
                                                _out_ptr(out.rows), _out_ptr(out.count)))
+        if out.keys.numel() != n or out.rows.numel() != n * dim:   # (what lies behind is another batch's)
+            out = RowGrads(out.keys.view(-1)[:n], out.rows.view(-1)[:n * dim].view(n, dim), out.count)
         return out
 
     def grad_norm(self, grads, scale=1.0, out=None):
@@ -599,14 +603,18 @@ class ParameterManager:
                    max_norm=float("inf")):
         """Update the worker's values of distinct ascending keys (-1: none) by their gradient rows, as embed_grad
         leaves both: SGD, or AdaGrad on [theta | a] rows, after clipping to max_norm by norm."""
-        with _NOTHING if _plain_tensor(keys, 1) and _plain_tensor(rows, 2) else self._on_stream():
-            k, r = _keys(keys), _floats(rows)
+        if _plain_tensor(keys, 1) and _plain_tensor(rows, 2):
+            k, r, n, m = keys.data_ptr(), rows.data_ptr(), keys.numel(), rows.numel()   # (0 for none: a null pointer)
+        else:
+            with self._on_stream():
+                keep = _keys(keys), _floats(rows)
+            (k, n), (r, m) = ((a.ptr, a.n) for a in keep)
         dim = rows.shape[-1]
-        if r.n != k.n * dim:
+        if m != n * dim:
             raise ValueError("rows must hold a row for every key")
         _check_norm(norm)
-        self._check(self._lib.adapm_push_grads(self._h, worker, k.ptr, r.ptr, k.n, dim, int(bool(adagrad)), lr, eps,
-                                               scale, max_norm, None if norm is None else norm.data_ptr()))
+        self._check(self._lib.adapm_push_grads(self._h, worker, k, r, n, dim, bool(adagrad), lr, eps, scale, max_norm,
+                                               None if norm is None else norm.data_ptr()))
 
     # -- inspection ------------------------------------------------------------
     def clock(self, worker):

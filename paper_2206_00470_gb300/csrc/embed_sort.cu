@@ -129,7 +129,7 @@ struct TokenPass {
   uint32_t* pos_out;
   const uint16_t* table;  // counts of this pass's digits
   uint32_t* next;         // packed counts of the next pass's, null: none
-  uint32_t n, tiles, stride;   // stride: tiles of a table row, a multiple of eight
+  uint32_t n, stride;     // stride: tiles of a table row, a multiple of eight
   int shift, bits, next_bits;
 };
 
@@ -338,7 +338,6 @@ int token_sort_items(const TokenView& t, uint64_t K, int bits, uint32_t* const* 
     p.table = reinterpret_cast<const uint16_t*>(scratch + i * words);
     p.next = i + 1 < passes ? scratch + (i + 1) * words : nullptr;
     p.n = (uint32_t)t.n;
-    p.tiles = tiles;
     p.stride = stride;
     p.shift = i * each;
     p.bits = p.next_bits = each;

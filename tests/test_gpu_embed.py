@@ -474,6 +474,26 @@ def test_update_of_the_first_floats_of_a_row(gpu_lib, D, dim):
     pm.close()
 
 
+def test_buffers_of_a_larger_batch(gpu_lib):
+    """The last, smaller batch in the buffers of the others: nothing of theirs is updated again."""
+    K, D = 50, 8
+    init = table(K, D)
+    pm = make(gpu_lib, init)
+    ones = torch.ones(20, D, device="cuda")
+    buf = pm.embed_grad(0, torch.arange(20, 40, device="cuda"), ones)
+    g = pm.embed_grad(0, torch.tensor([3, 3, 1], device="cuda"), ones[:3], out=buf)
+    assert g.keys.shape == (3,) and g.rows.shape == (3, D)
+    norm = pm.grad_norm([g])
+    pm.push_grads(0, g.keys, g.rows, 1.0)
+    pm.wait()
+    want = init.copy()
+    want[1] -= 1
+    want[3] -= 2
+    assert np.array_equal(pm.read_main(np.arange(K)), want)
+    assert abs(float(norm) - np.sqrt(5 * D)) < 1e-5
+    pm.close()
+
+
 @pytest.mark.parametrize("dim", [4, 64])
 def test_rows_that_begin_between_vectors(gpu_lib, dim):
     """Gradient rows, and the rows of sums, whose first element is on no vector boundary."""
