@@ -374,7 +374,9 @@ adapm_status adapm_grad_norm(adapm_ctx* ctx, const adapm_tensor* grads, uint64_t
  * adapm_grad_norm leaves it, so nothing waits on the host.  outs[t] has
  * grads[t]'s count and a type of its own; its live and row_len are not used.
  * It is grads[t]'s own memory (same type) or does not overlap any gradient.
- * outs = NULL: in place, and nothing moves when scale * f is 1. */
+ * outs = NULL: in place, and nothing moves when scale * f is 1.  (A tensor
+ * that is listed twice counts twice in the norm, and must not be clipped in
+ * place.) */
 adapm_status adapm_clip_grads(adapm_ctx* ctx, const adapm_tensor* grads, const adapm_tensor* outs, uint64_t n,
                               float scale, float max_norm, const float* norm);
 

@@ -107,7 +107,7 @@ void launch_count_sort(const TokenView& t, uint64_t K, uint32_t* skeys, uint32_t
 // their positions.  keys / pos: two arrays of n each; the result is in those
 // whose index is returned.  scratch: token_sort_words(n, bits) words.  Bad ids sort as
 // padding and are reported.
-constexpr int kTokenBits = 8;
+constexpr int kTokenBits = 9;   // of a pass, at most
 constexpr uint64_t kTokenSort = 1u << 19;
 size_t token_sort_words(uint64_t n, int bits);
 int token_sort(const TokenView& t, uint64_t K, int bits, uint32_t* const* keys, uint32_t* const* pos,

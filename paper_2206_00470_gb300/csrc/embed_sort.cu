@@ -114,13 +114,12 @@ __global__ void __launch_bounds__(kThreadsC) count_sort_kernel(const TokenView t
 // 4096).  The first pass reads the tokens themselves, in whatever layout they
 // have.  Bound by the latency of its launches, 3.5 to 8 us each.
 //
-// Grid sort (sort.cu) -> this, tokens of 1M keys: 16,384 26 -> 13 us, 65,536
-// 31 -> 17.5, 131,072 31 -> 21, 262,144 34 -> 26, 524,288 50 -> 40; 2^20, in
-// tiles of 8192, 69 both.  (Digits of 10 bits take longer per launch than they
-// save launches: 65,536 22 us, of 11 bits 24.)
+// Grid sort (sort.cu) -> this, tokens of 1M keys: 16,384 26 -> 13.5 us, 65,536
+// 31 -> 18, 131,072 31 -> 21, 262,144 34 -> 28, 524,288 50 -> 40; of 250,000
+// keys 524,288 37 -> 34; 2^20, in tiles of 8192, 69 both.  (Digits of 10 bits
+// take longer per launch than they save launches: 65,536 22 us, of 11 bits 24.)
 // ---------------------------------------------------------------------------
 constexpr uint32_t kTilesMost = 128;
-static_assert(256 >= 1 << kTokenBits, "a thread per digit");
 
 struct TokenPass {
   const uint32_t* keys;   // null: the tokens
@@ -228,10 +227,16 @@ __global__ void __launch_bounds__(NT) token_pass_kernel(const TokenView t, uint6
       pos[it] = i < p.n ? p.pos[i] : 0u;
     }
   }
-  // items of the thread's digit: anywhere, and in the tiles before this one
-  uint32_t all = 0, before = 0;
-  if (threadIdx.x < digits) {
-    const uint4* row = reinterpret_cast<const uint4*>(p.table + (uint64_t)threadIdx.x * p.stride);
+  // items of the thread's digits (the next ones to each other): anywhere, and in
+  // the tiles before this one
+  constexpr int J = (1 << kTokenBits) / NT > 1 ? (1 << kTokenBits) / NT : 1;
+  const uint32_t per = digits > (uint32_t)NT ? J : 1, d0 = threadIdx.x * per;
+  uint32_t all[J], before[J];
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    all[j] = before[j] = 0;
+    if (j >= (int)per || d0 + j >= digits) continue;
+    const uint4* row = reinterpret_cast<const uint4*>(p.table + (uint64_t)(d0 + j) * p.stride);
 #pragma unroll 8
     for (uint32_t q = 0; q < p.stride / 8; ++q) {
       const uint4 v = row[q];
@@ -239,8 +244,8 @@ __global__ void __launch_bounds__(NT) token_pass_kernel(const TokenView t, uint6
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const uint32_t b = 8 * q + 2 * e, lo = w[e] & 0xFFFFu, hi = w[e] >> 16;
-        all += lo + hi;
-        before += (b < blockIdx.x ? lo : 0u) + (b + 1 < blockIdx.x ? hi : 0u);
+        all[j] += lo + hi;
+        before[j] += (b < blockIdx.x ? lo : 0u) + (b + 1 < blockIdx.x ? hi : 0u);
       }
     }
   }
@@ -263,23 +268,29 @@ __global__ void __launch_bounds__(NT) token_pass_kernel(const TokenView t, uint6
   }
   // where the digit's items of this tile go: behind those of lower digits and
   // of the tiles before, warp by warp
-  uint32_t total;
-  const uint32_t base = block_exclusive_scan<NT>(all, &total, scan);   // (a barrier: the warps' counts are final)
-  uint32_t h[NT / 32], mine = 0;
+  uint32_t sum = 0, total;
 #pragma unroll
-  for (int w = 0; w < NT / 32; ++w) {
-    h[w] = threadIdx.x < digits ? wcnt[w * digits + threadIdx.x] : 0u;
-    mine += h[w];
-  }
-  const uint32_t first = block_exclusive_scan<NT>(mine, &total, scan);   // in the ordered tile
-  if (threadIdx.x < digits) {
-    uint32_t run = first;
+  for (int j = 0; j < J; ++j) sum += all[j];
+  uint32_t base = block_exclusive_scan<NT>(sum, &total, scan);   // (a barrier: the warps' counts are final)
+  uint32_t h[J][NT / 32], mine = 0;
+#pragma unroll
+  for (int j = 0; j < J; ++j)
 #pragma unroll
     for (int w = 0; w < NT / 32; ++w) {
-      wcnt[w * digits + threadIdx.x] = (uint16_t)run;
-      run += h[w];
+      h[j][w] = j < (int)per && d0 + j < digits ? wcnt[w * digits + d0 + j] : 0u;
+      mine += h[j][w];
     }
-    place[threadIdx.x] = base + before - first;   // (of the ordered tile's begin)
+  uint32_t run = block_exclusive_scan<NT>(mine, &total, scan);   // in the ordered tile
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    if (j >= (int)per || d0 + j >= digits) continue;
+    place[d0 + j] = base + before[j] - run;   // (of the ordered tile's begin)
+    base += all[j];
+#pragma unroll
+    for (int w = 0; w < NT / 32; ++w) {
+      wcnt[w * digits + d0 + j] = (uint16_t)run;
+      run += h[j][w];
+    }
   }
   __syncthreads();
   uint32_t* tk = reinterpret_cast<uint32_t*>(wcnt + digits * (NT / 32));
@@ -311,10 +322,20 @@ __global__ void __launch_bounds__(NT) token_pass_kernel(const TokenView t, uint6
   }
 }
 
+// Passes of a sort by `bits` bits: of up to 9 bits while the table is short (up
+// to 16,384 tokens) or a thread has one digit of it all the same (tiles of 512
+// threads), else of up to 8.  17 and 18 bits, two passes against three: 8,192
+// tokens 10 and 12 us, 16,384 12.5 and 13.5, 262,144 26 and 28, 524,288 34 and
+// 42; but 65,536 21 and 18, 131,072 23 and 20.
+int token_passes(uint64_t n, int bits) {
+  const int most = n <= 16384 || n > 131072 ? kTokenBits : 8;
+  return (bits + most - 1) / most;
+}
+
 template <int NT, int ITEMS>
 int token_sort_items(const TokenView& t, uint64_t K, int bits, uint32_t* const* keys, uint32_t* const* pos,
-                             uint32_t* scratch, DevState* st, cudaStream_t stream) {
-  const int passes = (bits + kTokenBits - 1) / kTokenBits, each = (bits + passes - 1) / passes;
+                     uint32_t* scratch, DevState* st, cudaStream_t stream) {
+  const int passes = token_passes(t.n, bits), each = (bits + passes - 1) / passes;
   const uint32_t tiles = (uint32_t)((t.n + NT * ITEMS - 1) / (NT * ITEMS)), stride = (tiles + 7) / 8 * 8;
   const uint32_t words = (stride << each) / 2;   // of a table
   // the kernel's dynamic shared-memory limit is a per-device attribute
@@ -367,7 +388,7 @@ uint32_t token_tile(uint64_t n) {
 }
 
 size_t token_sort_words(uint64_t n, int bits) {
-  const int passes = (bits + kTokenBits - 1) / kTokenBits, each = (bits + passes - 1) / passes;
+  const int passes = token_passes(n, bits), each = (bits + passes - 1) / passes;
   const uint64_t tile = token_tile(n), tiles = (n + tile - 1) / tile;
   return (size_t)passes * (((tiles + 7) / 8 * 8) << each) / 2;
 }
