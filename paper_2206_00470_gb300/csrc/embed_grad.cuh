@@ -508,13 +508,13 @@ void dispatch_grad(uint32_t tile, F&& f) {
 }
 
 // Elements a lane loads at a time: the most that every row's start and length
-// are a multiple of.
+// are a multiple of.  (Sums of four and more are written as vectors.)
 template <class T>
 int grad_vector(const GradArgs& a) {
-  for (int v = 16 / (int)sizeof(T); v >= 4; v /= 2) {
+  for (int v = 16 / (int)sizeof(T); v > 1; v /= 2) {
     if (reinterpret_cast<uintptr_t>(a.grad.data) % (v * sizeof(T)) == 0 && a.dim % v == 0 &&
         a.grad.inner_stride % v == 0 && (a.grad.flat || a.grad.outer_stride % v == 0) &&
-        reinterpret_cast<uintptr_t>(a.rows) % 16 == 0)
+        (v < 4 || reinterpret_cast<uintptr_t>(a.rows) % 16 == 0))
       return v;
   }
   return 1;
@@ -530,6 +530,7 @@ void dispatch_grad_args(const GradArgs& a, F&& f) {
   if constexpr (sizeof(T) == 2)
     if (v == 8) return by_v(std::integral_constant<int, 8>{});
   if (v >= 4) return by_v(std::integral_constant<int, 4>{});
+  if (v == 2) return by_v(std::integral_constant<int, 2>{});
   by_v(std::integral_constant<int, 1>{});
 }
 
