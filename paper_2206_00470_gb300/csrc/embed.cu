@@ -43,13 +43,29 @@ __device__ __forceinline__ __nv_bfloat16 round_to<__nv_bfloat16>(float v) {
   return __float2bfloat16_rn(v);
 }
 
-// Up to four elements of a row from column c; `vec`: rows begin on a multiple
-// of four elements.
+__device__ __forceinline__ uint32_t pack2(float x, float y, __half) {
+  const __half2 a = __floats2half2_rn(x, y);
+  return *reinterpret_cast<const uint32_t*>(&a);
+}
+__device__ __forceinline__ uint32_t pack2(float x, float y, __nv_bfloat16) {
+  const __nv_bfloat162 a = __floats2bfloat162_rn(x, y);
+  return *reinterpret_cast<const uint32_t*>(&a);
+}
+__device__ __forceinline__ float2 pack2(float x, float y, float) { return make_float2(x, y); }
+
+// Up to four elements of a row from column c; rows begin on a multiple of
+// `align` (4, 2 or 1) elements.
 template <class T>
-__device__ __forceinline__ void put4(T* row, uint32_t c, uint32_t dim, float4 v, bool vec) {
-  if (vec && c + 4 <= dim) {
+__device__ __forceinline__ void put4(T* row, uint32_t c, uint32_t dim, float4 v, int align) {
+  if (align == 4 && c + 4 <= dim) {
     auto p = pack4(v, T());
     __stcs(reinterpret_cast<decltype(p)*>(row + c), p);
+    return;
+  }
+  if (align == 2 && c + 4 <= dim) {
+    auto p = pack2(v.x, v.y, T()), q = pack2(v.z, v.w, T());
+    *reinterpret_cast<decltype(p)*>(row + c) = p;
+    *reinterpret_cast<decltype(p)*>(row + c + 2) = q;
     return;
   }
   const float x[4] = {v.x, v.y, v.z, v.w};
@@ -96,7 +112,7 @@ constexpr uint32_t embed_batch(int U) { return U == 1 ? 32 : 4; }
 template <class T, int W, int G, int U>
 __global__ void __launch_bounds__(kThreads, embed_blocks_per_sm(U, W))
 embed_kernel(Store s, uint32_t w, const TokenView tv, uint32_t per, uint32_t dim, float scale, const RowView ov,
-             bool vec) {
+             int align) {
   after_previous();
   constexpr int C = U * W, GW = 32 / G;
   const uint32_t lane32 = threadIdx.x & 31, lane = lane32 & (G - 1), sub = lane32 / G;
@@ -149,7 +165,7 @@ embed_kernel(Store s, uint32_t w, const TokenView tv, uint32_t per, uint32_t dim
         const uint2 x = pack4(f4scale(v[c], scale), T()), y = pack4(f4scale(v[c + 1], scale), T());
         __stcs(reinterpret_cast<uint4*>(row + 4 * col), make_uint4(x.x, x.y, y.x, y.y));
       } else {
-        put4(row, 4 * col, dim, f4scale(v[c], scale), vec);
+        put4(row, 4 * col, dim, f4scale(v[c], scale), align);
       }
     }
   }
@@ -173,7 +189,7 @@ void launch_typed(const Store& s, uint32_t w, const TokenView& t, uint32_t dim, 
     const uint64_t per = std::min<uint64_t>(most, ((t.n + warps - 1) / warps + round - 1) / round * round);
     const uint64_t blocks = (t.n + per * (kThreads / 32) - 1) / (per * (kThreads / 32));
     launch_after(embed_kernel<T, W, G, U>, (unsigned)blocks, kThreads, 0, stream, s, w, t, (uint32_t)per, dim, scale,
-                 out, rows_aligned(out, sizeof(T), 4));
+                 out, rows_aligned(out, sizeof(T), 4) ? 4 : (rows_aligned(out, sizeof(T), 2) ? 2 : 1));
   };
   using std::integral_constant;
   if (dim % 8 == 0 && s.D % 8 == 0 && rows_aligned(out, sizeof(T), 8)) {
