@@ -355,7 +355,7 @@ adapm_status adapm_embed(adapm_ctx* ctx, uint32_t worker, const adapm_tokens* to
  * deterministic for a given input.  The store is neither read nor written;
  * tokens that the worker has signalled (adapm_intent) are grouped by that
  * intent's plan, as in adapm_push.  keys, rows and count are device or host
- * arrays. */
+ * arrays (rows of a host array behind the last are set to 0). */
 adapm_status adapm_embed_grad(adapm_ctx* ctx, uint32_t worker, const adapm_tokens* tokens, uint32_t dim,
                               float scale, const adapm_rows* grad, uint32_t* keys, float* rows,
                               uint32_t* count);

@@ -811,6 +811,11 @@ cudaError_t close_list(adapm_ctx* ctx, uint32_t w, int64_t id) {
 bool float_type(int32_t type) { return type == ADAPM_F32 || type == ADAPM_F16 || type == ADAPM_BF16; }
 size_t type_bytes(int32_t type) { return type == ADAPM_F32 ? 4 : 2; }
 
+// Whether element (o, i) is at (o * inner + i) * step.
+bool no_gaps(const adapm_tokens* t, int64_t outer_stride, int64_t inner_stride, int64_t step) {
+  return (t->inner <= 1 || inner_stride == step) && (t->outer <= 1 || outer_stride == (int64_t)t->inner * step);
+}
+
 // Checks of the tokens and their rows that adapm_embed and adapm_embed_grad
 // share; n: the number of tokens.
 adapm_status check_tokens(adapm_ctx* ctx, uint32_t worker, const adapm_tokens* t, uint32_t dim, const adapm_rows* r,
@@ -827,19 +832,18 @@ adapm_status check_tokens(adapm_ctx* ctx, uint32_t worker, const adapm_tokens* t
   if (*n > 0 && (reinterpret_cast<uintptr_t>(t->ids) % (t->id_bits / 8) != 0 ||
                  reinterpret_cast<uintptr_t>(r->data) % type_bytes(r->type) != 0))
     return fail(ctx, ADAPM_EINVAL, "ids or rows are not aligned to their type");
+  // (host arrays are copied whole)
+  if (*n > 0 && !no_gaps(t, t->outer_stride, t->inner_stride, 1) && !is_device_ptr(t->ids))
+    return fail(ctx, ADAPM_EINVAL, "ids on the host must have no gaps");
+  if (*n > 0 && !no_gaps(t, r->outer_stride, r->inner_stride, dim) && !is_device_ptr(r->data))
+    return fail(ctx, ADAPM_EINVAL, "rows on the host must have no gaps");
   return ADAPM_OK;
-}
-
-// Whether element (o, i) is at (o * inner + i) * step.
-bool no_gaps(const adapm_tokens* t, int64_t outer_stride, int64_t inner_stride, int64_t step) {
-  return (t->inner <= 1 || inner_stride == step) && (t->outer <= 1 || outer_stride == (int64_t)t->inner * step);
 }
 
 // The ids on the device; `owned` is freed after the call's kernels.
 adapm_status stage_tokens(adapm_ctx* ctx, const adapm_tokens* t, uint64_t n, TokenView* v, char** owned) {
   const size_t size = t->id_bits / 8;
   v->flat = no_gaps(t, t->outer_stride, t->inner_stride, 1);
-  if (!v->flat && !is_device_ptr(t->ids)) return fail(ctx, ADAPM_EINVAL, "ids on the host must have no gaps");
   Input<char> in;
   CK(stage_in(ctx, static_cast<const char*>(t->ids), n * size, &in));
   v->ids = in.dev;
@@ -1609,9 +1613,6 @@ adapm_status adapm_embed(adapm_ctx* ctx, uint32_t worker, const adapm_tokens* to
   if (st != ADAPM_OK) return st;
   if (n == 0) return ADAPM_OK;
   if (!rows_apart(tokens, out, dim)) return fail(ctx, ADAPM_EINVAL, "rows of out overlap");
-  const bool on_device = is_device_ptr(out->data);
-  if (!on_device && !no_gaps(tokens, out->outer_stride, out->inner_stride, dim))
-    return fail(ctx, ADAPM_EINVAL, "rows on the host must have no gaps");
   TokenView tv{};
   char* ids = nullptr;
   st = stage_tokens(ctx, tokens, n, &tv, &ids);
@@ -1621,8 +1622,7 @@ adapm_status adapm_embed(adapm_ctx* ctx, uint32_t worker, const adapm_tokens* to
   ProfScope ps(ctx, 2);
   CK(stage_join(ctx));
   Output<char> o;
-  if (on_device) o.dev = static_cast<char*>(out->data);
-  else CK(stage_out(ctx, static_cast<char*>(out->data), n * dim * type_bytes(out->type), &o));
+  CK(stage_out(ctx, static_cast<char*>(out->data), n * dim * type_bytes(out->type), &o));
   {
     ProfScope pk(ctx, 7);
     launch_embed(ctx->s, worker, tv, dim, scale, row_view(tokens, out, o.dev), ctx->sms, ctx->stream);
@@ -1648,21 +1648,20 @@ adapm_status adapm_embed_grad(adapm_ctx* ctx, uint32_t worker, const adapm_token
     CK(finish_out(ctx, &oc));
     return ADAPM_OK;
   }
-  const bool on_device = is_device_ptr(grad->data);
-  if (!on_device && !no_gaps(tokens, grad->outer_stride, grad->inner_stride, dim))
-    return fail(ctx, ADAPM_EINVAL, "rows on the host must have no gaps");
   TokenView tv{};
   char* ids = nullptr;
   st = stage_tokens(ctx, tokens, n, &tv, &ids);
   if (st != ADAPM_OK) return st;
   Input<char> ig;
-  if (on_device) ig.dev = static_cast<const char*>(grad->data);
-  else CK(stage_in(ctx, static_cast<const char*>(grad->data), n * dim * type_bytes(grad->type), &ig));
+  CK(stage_in(ctx, static_cast<const char*>(grad->data), n * dim * type_bytes(grad->type), &ig));
   CK(stage_join(ctx));
   Output<uint32_t> ok;
   Output<float> orows;
   CK(stage_out(ctx, keys, n, &ok));
   CK(stage_out(ctx, rows, n * dim, &orows));
+  // (host arrays are copied whole, with what the call leaves as it is)
+  if (ok.host) CK(cudaMemsetAsync(ok.dev, 0xFF, n * sizeof(uint32_t), ctx->stream));
+  if (orows.host) CK(cudaMemsetAsync(orows.dev, 0, n * dim * sizeof(float), ctx->stream));
   GradArgs a{};
   a.n = n;
   a.K = ctx->s.K;

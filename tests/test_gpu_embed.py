@@ -180,6 +180,19 @@ def test_lookup_with_early_events_and_on_the_host(gpu_lib):
     pm.wait()
     keys, counts = np.unique(t.numpy(), return_counts=True)
     check_row_grads(g, keys, np.repeat(counts[:, None], D, 1).astype(np.float64), 0.0)
+    assert not g.rows[len(keys):].any()
+    pm.close()
+
+
+def test_host_arrays_with_gaps_are_refused_whatever_else_is_on_the_host(gpu_lib):
+    pm = make(gpu_lib, table(20, 8))
+    t, x = torch.arange(12).reshape(3, 4), torch.ones(3, 4, 16)
+    for call in (lambda: pm.embed(0, t[:, :3].clone(), out=x[:, :3, :8]), lambda: pm.embed(0, t[:, :3], out=torch.ones(3, 3, 8)),
+                 lambda: pm.embed_grad(0, t, x[:, :, :8]), lambda: pm.embed_grad(0, t[:, :3], torch.ones(3, 3, 8))):
+        with pytest.raises(gpu_lib.AdaPMError) as e:
+            call()
+        assert e.value.status == gpu_lib.EINVAL and "gaps" in str(e.value)
+    pm.wait()
     pm.close()
 
 
