@@ -22,7 +22,9 @@
  *     Host inputs are copied to the device before the call's kernels (pinned
  *     ones on a copy stream of the library's, so that the copy overlaps the
  *     kernels of earlier calls; the library stream waits for it); a host
- *     output is filled by a device-to-host copy on the library stream.
+ *     output is filled by a device-to-host copy on the library stream (a
+ *     later call that takes the same array as an input copies it in behind
+ *     that).
  *   - Calls are ordered on the library stream and return once their work is
  *     enqueued.  Device and pinned host arrays are read and written in
  *     stream order: keep inputs unchanged, and read outputs only, after

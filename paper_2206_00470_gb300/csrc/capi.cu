@@ -92,6 +92,13 @@ struct WorkerState {
   } early;
 };
 
+// A pinned host array that a call fills: done is recorded behind its copy
+// (null: a recorded call, which fills it whenever the graph is launched).
+struct HostWrite {
+  uintptr_t begin, end;
+  cudaEvent_t done;
+};
+
 }  // namespace
 
 struct adapm_ctx {
@@ -125,7 +132,8 @@ struct adapm_ctx {
   // mark (an event on `stream` with the bytes staged before it) is taken at
   // each staging call; while more than kStageAhead bytes are staged beyond
   // the oldest mark, copy_in waits for that mark, which bounds the staging
-  // memory in flight.
+  // memory in flight.  An input that an earlier call may still have to fill (a
+  // pinned output of its) is copied on `stream` instead, behind that call.
   cudaStream_t copy_in = nullptr;
   cudaMemPool_t stage_pool = nullptr;
   cudaEvent_t staged = nullptr;
@@ -134,6 +142,8 @@ struct adapm_ctx {
   std::vector<cudaEvent_t> spare_marks;
   uint64_t stage_unmarked = 0;   // bytes staged since the last mark
   uint64_t stage_live = 0;       // bytes staged since the oldest mark
+  std::vector<HostWrite> host_writes;   // outputs that may not have arrived yet
+  size_t host_writes_swept = 64;        // more of them than this: those that have arrived are forgotten
   // Push plans are sorted on plan_stream (lowest priority, so its blocks
   // take what the library stream leaves), with scratch from plan_pool, which
   // never makes one stream wait for the other on its own.
@@ -310,6 +320,51 @@ void pool_free(adapm_ctx* ctx, void* p) {
   if (p) ctx->blocks.give(PoolMem{ctx->pool, ctx->stream}, p);
 }
 
+// Forgets a host array that has been filled.
+void forget_host_write(adapm_ctx* ctx, size_t i) {
+  ctx->spare_ready.push_back(ctx->host_writes[i].done);
+  ctx->host_writes[i] = ctx->host_writes.back();
+  ctx->host_writes.pop_back();
+}
+
+bool host_write_done(const HostWrite& h) {
+  if (h.done == nullptr) return false;
+  const cudaError_t q = cudaEventQuery(h.done);
+  if (q == cudaErrorNotReady && cudaPeekAtLastError() == cudaErrorNotReady) cudaGetLastError();
+  return q == cudaSuccess;
+}
+
+// Behind the copy on `stream` that fills a pinned host array.
+cudaError_t note_host_write(adapm_ctx* ctx, const void* p, uint64_t bytes) {
+  const HostWrite h{reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes, nullptr};
+  for (HostWrite& k : ctx->host_writes) {   // (a program's buffers are the same ones in every step)
+    if (k.begin != h.begin || k.end != h.end || (k.done == nullptr) != ctx->capturing) continue;
+    return ctx->capturing ? cudaSuccess : cudaEventRecord(k.done, ctx->stream);
+  }
+  try {
+    if (ctx->host_writes.size() >= ctx->host_writes_swept) {
+      for (size_t i = ctx->host_writes.size(); i-- > 0;)
+        if (host_write_done(ctx->host_writes[i])) forget_host_write(ctx, i);
+      ctx->host_writes_swept = std::max<size_t>(64, 2 * ctx->host_writes.size());
+    }
+    ctx->host_writes.push_back(h);
+  } catch (...) {
+    return cudaErrorMemoryAllocation;
+  }
+  if (ctx->capturing) return cudaSuccess;
+  cudaError_t e = take_ready_event(ctx, &ctx->host_writes.back().done);
+  if (e == cudaSuccess) e = cudaEventRecord(ctx->host_writes.back().done, ctx->stream);
+  return e;
+}
+
+// Whether a call before this one may still have to fill a part of the array.
+bool host_write_queued(adapm_ctx* ctx, const void* p, uint64_t bytes) {
+  const uintptr_t begin = reinterpret_cast<uintptr_t>(p), end = begin + bytes;
+  for (const HostWrite& h : ctx->host_writes)
+    if (h.begin < end && begin < h.end && !host_write_done(h)) return true;
+  return false;
+}
+
 // Device view of an input array; copies host arrays in.
 template <class T>
 struct Input {
@@ -329,7 +384,8 @@ cudaError_t stage_in(adapm_ctx* ctx, const T* p, size_t count, Input<T>* in) {
     return cudaSuccess;
   }
   const uint64_t bytes = count * sizeof(T);
-  if (kind == MemKind::PinnedHost && !ctx->capturing) {   // (a graph records its copies on `stream`)
+  // (a graph records its copies on `stream`, and what an earlier call writes there is read behind it)
+  if (kind == MemKind::PinnedHost && !ctx->capturing && !host_write_queued(ctx, p, bytes)) {
     cudaError_t e = ensure_copy_in(ctx);
     if (e == cudaSuccess) e = stage_mark(ctx, bytes);
     if (e != cudaSuccess) return e;
@@ -364,16 +420,19 @@ struct Output {
   T* dev = nullptr;
   T* host = nullptr;
   size_t count = 0;
+  bool pinned = false;
 };
 
 template <class T>
 cudaError_t stage_out(adapm_ctx* ctx, T* p, size_t count, Output<T>* o) {
   o->count = count;
-  if (count == 0 || is_device_ptr(p)) {
+  const MemKind kind = count == 0 ? MemKind::Device : mem_kind(p);
+  if (kind == MemKind::Device) {
     o->dev = p;
     return cudaSuccess;
   }
   o->host = p;
+  o->pinned = kind == MemKind::PinnedHost;
   return pool_alloc(ctx, &o->dev, count);
 }
 
@@ -383,6 +442,7 @@ cudaError_t finish_out(adapm_ctx* ctx, Output<T>* o) {
   cudaError_t e = cudaMemcpyAsync(o->host, o->dev, o->count * sizeof(T), cudaMemcpyDeviceToHost,
                                   ctx->stream);
   pool_free(ctx, o->dev);
+  if (e == cudaSuccess && o->pinned) e = note_host_write(ctx, o->host, o->count * sizeof(T));
   return e;
 }
 
@@ -1124,6 +1184,8 @@ adapm_status adapm_destroy(adapm_ctx* ctx) {
     if (kv.second.listed) cudaEventDestroy(kv.second.listed);
   }
   for (auto e : ctx->spare_ready) cudaEventDestroy(e);
+  for (auto& h : ctx->host_writes)
+    if (h.done) cudaEventDestroy(h.done);
   ctx->blocks.release(cudaFree);
   ctx->plan_blocks.release(cudaFree);
   Store& s = ctx->s;
