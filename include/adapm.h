@@ -388,8 +388,9 @@ adapm_status adapm_clip_grads(adapm_ctx* ctx, const adapm_tensor* grads, const a
  * and reported as ADAPM_ESTATE by adapm_wait, one >= num_keys as
  * ADAPM_ERANGE).  With g = scale * f * rows[u], f from norm and max_norm as in
  * adapm_clip_grads (norm = NULL: 1), the pushed row is -lr * g in the first
- * dim floats, or with adagrad (value_len = 2 * dim, dim a multiple of 4)
- * [-lr * g / sqrt(a + g*g + eps) | g*g], a the accumulators before the call.
+ * dim floats (nothing is added to the others, whatever f is), or with adagrad
+ * (value_len = 2 * dim, dim a multiple of 4) [-lr * g / sqrt(a + g*g + eps) |
+ * g*g], a the accumulators before the call.
  * Written as adapm_push writes its sums, without a sort. */
 adapm_status adapm_push_grads(adapm_ctx* ctx, uint32_t worker, const uint32_t* keys, const float* rows,
                               uint64_t n, uint32_t dim, int adagrad, float lr, float eps, float scale,

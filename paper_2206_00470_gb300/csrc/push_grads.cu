@@ -26,6 +26,13 @@ __device__ __forceinline__ float4 get4(const float* row, uint32_t c, uint32_t di
   return make_float4(x[0], x[1], x[2], x[3]);
 }
 
+// Elements c .. c + 3 of a row; those behind the gradient's dim become -0, which
+// changes no value it is added to (0 times a NaN or infinite factor would).
+__device__ __forceinline__ float4 keep_dim(float4 v, uint32_t c, uint32_t dim) {
+  return make_float4(c < dim ? v.x : -0.f, c + 1 < dim ? v.y : -0.f, c + 2 < dim ? v.z : -0.f,
+                     c + 3 < dim ? v.w : -0.f);
+}
+
 // Blocks per SM that the registers are cut for: 400,003 AdaGrad rows of 2 x 256
 // floats (C = 4) 363 us at two, 325 at three, 327 at four; 500,000 of 2 x 100
 // (C = 2) 284 at three, 229 at four, 254 at five; 300,000 SGD rows of 300 (C =
@@ -104,7 +111,7 @@ __global__ void __launch_bounds__(kThreads, update_blocks_per_sm(C)) push_grads_
           d[r][c] = ada_theta4(g, d[r][CT + c], u.lr, u.eps);
           d[r][CT + c] = f4square(g);
         } else {
-          d[r][c] = f4mul(g, -u.lr);
+          d[r][c] = keep_dim(f4mul(g, -u.lr), 4 * (lane + c * G), u.dim);
         }
       }
       apply_sum<G, C, SRC>(s, k[r], t[r], d[r], lane, gmask);

@@ -487,6 +487,42 @@ def test_update_of_the_first_floats_of_a_row(gpu_lib, D, dim):
     pm.close()
 
 
+@pytest.mark.parametrize("held", [False, True])
+@pytest.mark.parametrize("bad", ["nan norm", "infinite norm", "nan scale", "infinite lr", "nan row"])
+@pytest.mark.parametrize("D,dim", [(52, 50), (64, 32), (12, 9), (12, 1), (300, 100), (1024, 516), (1024, 999)])
+def test_update_leaves_what_lies_behind_dim(gpu_lib, D, dim, bad, held):
+    """Factors and rows that are no numbers reach the first dim floats only, zeros of either sign included."""
+    K, n = 60, 25
+    init = table(K, D)
+    init[::2, dim:] = 0.0
+    init[1::2, dim + 1:] = -0.0
+    pm = make(gpu_lib, init)
+    keys = np.arange(1, 2 * n, 2)
+    dk = torch.from_numpy(keys).cuda()
+    if held:
+        pm.intent(0, dk, 0, 9)
+    rows = torch.ones(n, dim, device="cuda")
+    kw = dict(norm=torch.tensor({"nan norm": np.nan, "infinite norm": np.inf}.get(bad, 2.0), device="cuda"), max_norm=1.0)
+    lr = np.inf if bad == "infinite lr" else 0.5
+    if bad == "nan scale":
+        kw["scale"] = float("nan")
+    if bad == "nan row":
+        rows[:, 0] = float("nan")
+    for times in range(3):   # (a replica's first push, its second, and later ones are written differently)
+        pm.push_grads(0, dk, rows, lr, **kw)
+        got = pm.pull(0, torch.arange(K, device="cuda")).cpu().numpy()
+        pm.wait()
+        assert np.array_equal(got[:, dim:].view(np.uint32), init[:, dim:].view(np.uint32)), times
+        if bad != "infinite norm":
+            assert not np.isfinite(got[keys, 0]).any()
+        else:
+            assert np.array_equal(got[keys, :dim], init[keys, :dim])
+    pm.sync()
+    got = pm.read_main(np.arange(K))
+    assert np.array_equal(got[:, dim:].view(np.uint32), init[:, dim:].view(np.uint32))
+    pm.close()
+
+
 def test_buffers_of_a_larger_batch(gpu_lib):
     """The last, smaller batch in the buffers of the others: nothing of theirs is updated again."""
     K, D = 50, 8
