@@ -308,8 +308,9 @@ adapm_status adapm_sgns_step(adapm_ctx* ctx, uint32_t worker, const uint32_t* ce
  * inner_stride] (a host array has no gaps: inner_stride 1, outer_stride
  * inner).  id_bits 32: ids are keys, as everywhere; 64: signed.  An id outside
  * [0, num_keys) is reported as ADAPM_ERANGE by adapm_wait and treated as
- * padding.  With has_pad, ids equal to pad (any value) are padding: they have
- * a row of zeros and no gradient. */
+ * padding.  With has_pad, ids equal to pad are padding: they have a row of
+ * zeros and no gradient.  pad may be any value, a key or not; 32-bit ids equal
+ * a pad of [-2^31, 2^32) by its low 32 bits, and no other. */
 typedef struct {
   const void* ids;
   int32_t id_bits;

@@ -531,7 +531,7 @@ class ParameterManager:
                 got = _two_levels(shape, tokens.stride(), rows.stride()[:-1])
             t.outer, t.inner, (t.outer_stride, t.inner_stride), (r.outer_stride, r.inner_stride) = got
         t.ids, t.id_bits = tokens.data_ptr(), 64 if wide else 32
-        if pad is None:
+        if pad is None or not -2 ** 63 <= pad < 2 ** 63:   # (no id equals a larger one; a field would be cut)
             t.has_pad = 0
         else:
             t.has_pad, t.pad = 1, pad

@@ -909,8 +909,9 @@ adapm_status stage_tokens(adapm_ctx* ctx, const adapm_tokens* t, uint64_t n, Tok
   v->ids = in.dev;
   *owned = in.owned;
   v->wide = t->id_bits == 64;
-  v->has_pad = t->has_pad != 0;
-  v->pad = v->wide ? t->pad : (int64_t)(uint32_t)t->pad;   // (32-bit ids are unsigned)
+  // 32-bit ids are unsigned (a negative pad is given as signed); what has more bits equals none of them
+  v->has_pad = t->has_pad != 0 && (v->wide || (t->pad >= INT32_MIN && t->pad <= (int64_t)UINT32_MAX));
+  v->pad = v->wide ? t->pad : (int64_t)(uint32_t)t->pad;
   v->inner = (uint32_t)t->inner;
   v->outer_stride = t->outer_stride;
   v->inner_stride = t->inner_stride;

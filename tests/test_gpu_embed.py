@@ -100,6 +100,25 @@ def test_padding_has_zero_rows_and_is_no_error(gpu_lib, ids, pad):
     pm.close()
 
 
+@pytest.mark.parametrize("ids", [torch.int32, torch.int64])
+@pytest.mark.parametrize("pad", [2 ** 32, 2 ** 32 + 3, -2 ** 32 + 3, -2 ** 31 - 1, 2 ** 40 + 7, -2 ** 63, 2 ** 63 - 1,
+                                 2 ** 64, 2 ** 64 + 3, -2 ** 64 + 7])
+def test_padding_that_no_id_can_equal_pads_nothing(gpu_lib, ids, pad):
+    """A pad beyond the ids' type is none of them: not the token that its low bits spell."""
+    K, D, n = 50, 12, 200
+    init = table(K, D)
+    pm = make(gpu_lib, init)
+    t = torch.from_numpy(zipf(n, K)).to(ids)
+    t[::5], t[1::5] = pad & 31, 0
+    got = pm.embed(0, t.cuda(), scale=3.0, pad=pad)
+    g = pm.embed_grad(0, t.cuda(), torch.ones(n, D, device="cuda"), pad=pad)
+    pm.wait()
+    assert torch.equal(got.cpu(), torch.from_numpy(init)[t.long()] * 3.0)
+    keys, counts = np.unique(t.numpy(), return_counts=True)
+    check_row_grads(g, keys, np.repeat(counts[:, None], D, 1).astype(np.float64), 0.0)
+    pm.close()
+
+
 @pytest.mark.parametrize("ids,bad", [(torch.int32, 50), (torch.int32, -1), (torch.int64, 50), (torch.int64, -1),
                                      (torch.int64, 2 ** 32), (torch.int64, 2 ** 32 + 3), (torch.int64, -2 ** 40)])
 @pytest.mark.parametrize("n", [40, 20_000])
