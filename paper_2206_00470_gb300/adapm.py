@@ -579,12 +579,13 @@ class ParameterManager:
 
     def grad_norm(self, grads, scale=1.0, out=None):
         """|scale| times the Euclidean norm over all elements of grads (a GradList, or what makes one), as a float32
-        scalar on the GPU."""
-        g = _grad_list(grads)
+        scalar on the GPU, or into out (a float32 scalar, on the host too)."""
+        g, torch = _grad_list(grads), _torch()
         if out is None:
-            torch = _torch()
             with self._on_stream():
                 out = torch.empty((), dtype=torch.float32, device=self._device)
+        elif out.dtype is not torch.float32 or out.numel() != 1:
+            raise ValueError("out is a float32 scalar")
         self._check(self._lib.adapm_grad_norm(self._h, g.array, g.n, scale, out.data_ptr()))
         return out
 

@@ -983,6 +983,9 @@ class DevicePointers {
   unsigned next_ = 0;
 };
 
+// A float that a kernel reads or writes as one.
+bool norm_aligned(const float* norm) { return reinterpret_cast<uintptr_t>(norm) % sizeof(float) == 0; }
+
 adapm_status check_tensors(adapm_ctx* ctx, const adapm_tensor* t, uint64_t n, const char* what) {
   DevicePointers device;
   if (n > 0 && !t) return fail(ctx, ADAPM_EINVAL, "null %s", what);
@@ -1820,7 +1823,7 @@ adapm_status adapm_grad_norm(adapm_ctx* ctx, const adapm_tensor* grads, uint64_t
   if (st != ADAPM_OK) return st;
   st = check_tensors(ctx, grads, n, "grads");
   if (st != ADAPM_OK) return st;
-  if (!norm) return fail(ctx, ADAPM_EINVAL, "null norm");
+  if (!norm || !norm_aligned(norm)) return fail(ctx, ADAPM_EINVAL, "norm is null or not aligned");
   std::vector<GradTensor> t;
   try {
     t.reserve(n);
@@ -1846,7 +1849,8 @@ adapm_status adapm_clip_grads(adapm_ctx* ctx, const adapm_tensor* grads, const a
   st = check_tensors(ctx, grads, n, "grads");
   if (st == ADAPM_OK && outs) st = check_tensors(ctx, outs, n, "outs");
   if (st != ADAPM_OK) return st;
-  if (!norm || !is_device_ptr(norm)) return fail(ctx, ADAPM_EINVAL, "norm is not a device word");
+  if (!norm || !norm_aligned(norm) || !is_device_ptr(norm))
+    return fail(ctx, ADAPM_EINVAL, "norm is not a device word");
   if (!(max_norm >= 0.f)) return fail(ctx, ADAPM_EINVAL, "max_norm must not be negative");
   std::vector<GradTensor> t;
   try {
@@ -1881,7 +1885,8 @@ adapm_status adapm_push_grads(adapm_ctx* ctx, uint32_t worker, const uint32_t* k
     return fail(ctx, ADAPM_EINVAL, "dim %u does not match value_len %u", dim, ctx->s.D);
   // (theta and accumulators are read and written as float4 halves of a row)
   if (adagrad && dim % 4 != 0) return fail(ctx, ADAPM_EINVAL, "dim %u: need a multiple of 4 with AdaGrad", dim);
-  if (norm && !is_device_ptr(norm)) return fail(ctx, ADAPM_EINVAL, "norm is not a device word");
+  if (norm && (!norm_aligned(norm) || !is_device_ptr(norm)))
+    return fail(ctx, ADAPM_EINVAL, "norm is not a device word");
   if (norm && !(max_norm >= 0.f)) return fail(ctx, ADAPM_EINVAL, "max_norm must not be negative");
   if (n == 0) return ADAPM_OK;
   Input<uint32_t> ik;

@@ -57,6 +57,38 @@ def test_norms_are_gpu_scalars():
     adapm._check_norm(None)
 
 
+class Recorder:
+    """Stands for the library: every call is noted and answered with ADAPM_OK."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        return lambda *args: self.calls.append((name, args)) or adapm.OK
+
+
+@pytest.fixture
+def manager():
+    """The binding's half of a manager."""
+    pm = adapm.ParameterManager.__new__(adapm.ParameterManager)
+    pm._lib, pm._h, pm.D = Recorder(), None, 8
+    pm._t, pm._r = adapm._Tokens(), adapm._Rows()
+    pm._t_ref, pm._r_ref = adapm.ctypes.byref(pm._t), adapm.ctypes.byref(pm._r)
+    return pm
+
+
+@pytest.mark.parametrize("out", [torch.zeros((), dtype=torch.float16), torch.zeros(3, dtype=torch.bfloat16)[1],
+                                 torch.zeros((), dtype=torch.float64), torch.zeros((), dtype=torch.int32),
+                                 torch.zeros(2), torch.zeros(0), torch.zeros(8, dtype=torch.uint8)[1]])
+def test_a_norm_goes_into_one_float(manager, out):
+    with pytest.raises(ValueError):
+        manager.grad_norm([], out=out)
+    assert not manager._lib.calls
+    for fits in (torch.zeros(()), torch.zeros(5)[3], torch.zeros(1, 1)):
+        assert manager.grad_norm([], out=fits) is fits
+        assert manager._lib.calls.pop()[1][-1] == fits.data_ptr()
+
+
 def test_types():
     assert [adapm._type_of(t) for t in (torch.float32, torch.float16, torch.bfloat16)] == [0, 1, 2]
     with pytest.raises(ValueError):

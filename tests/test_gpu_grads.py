@@ -201,6 +201,29 @@ def test_more_than_2_to_the_32_elements(gpu_lib, pm):
     assert int((t != 0).sum()) == 3
 
 
+def test_norms_that_are_no_aligned_float_are_refused(gpu_lib, pm):
+    x, buf = torch.ones(10, device="cuda"), torch.zeros(8, device="cuda", dtype=torch.bfloat16)
+    row, key = torch.zeros(1, 4, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    for out in (buf[0], buf[1], x.double()[0], x[:2]):
+        with pytest.raises(ValueError):
+            pm.grad_norm([x], out=out)
+    import ctypes
+    lib = gpu_lib.load()
+    t = gpu_lib._Tensor(x.data_ptr(), 10, None, 0, 0)
+    for off in (1, 2, 3):
+        at = buf.data_ptr() + off
+        assert lib.adapm_grad_norm(pm._h, ctypes.byref(t), 1, 1.0, at) == gpu_lib.EINVAL
+        assert lib.adapm_clip_grads(pm._h, ctypes.byref(t), None, 1, 1.0, 1.0, at) == gpu_lib.EINVAL
+        assert lib.adapm_push_grads(pm._h, 0, key.data_ptr(), row.data_ptr(), 1, 4, 0, 0.1, 0.0, 1.0, 1.0,
+                                    at) == gpu_lib.EINVAL
+    host, scalar = torch.zeros(()).pin_memory(), torch.zeros(3, device="cuda")
+    pm.grad_norm([x], out=host)
+    pm.grad_norm([x], out=scalar[1])
+    pm.wait()
+    assert not buf.any() and scalar.tolist() == [0.0, float(host), 0.0] and abs(float(host) - math.sqrt(10)) < 1e-6
+    assert (x == 1).all()
+
+
 def test_refusals(gpu_lib, pm):
     x = torch.ones(10, device="cuda")
     norm = pm.grad_norm([x])
