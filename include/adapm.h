@@ -298,7 +298,8 @@ adapm_status adapm_sgns_step(adapm_ctx* ctx, uint32_t worker, const uint32_t* ce
  * (adapm_embed_grad), take the norm over these and every other gradient
  * (adapm_grad_norm), clip (adapm_clip_grads), and apply the summed rows
  * (adapm_push_grads).  The paper has no counterpart; reads and writes follow
- * adapm_pull and adapm_push (replica of the worker, else main). */
+ * adapm_pull and adapm_push (replica of the worker, else main).  Arrays are
+ * aligned to their elements (ADAPM_EINVAL otherwise). */
 
 #define ADAPM_F32 0
 #define ADAPM_F16 1

@@ -983,8 +983,8 @@ class DevicePointers {
   unsigned next_ = 0;
 };
 
-// A float that a kernel reads or writes as one.
-bool norm_aligned(const float* norm) { return reinterpret_cast<uintptr_t>(norm) % sizeof(float) == 0; }
+// Words that a kernel reads or writes as such.
+bool word_aligned(const void* p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; }
 
 adapm_status check_tensors(adapm_ctx* ctx, const adapm_tensor* t, uint64_t n, const char* what) {
   DevicePointers device;
@@ -995,7 +995,7 @@ adapm_status check_tensors(adapm_ctx* ctx, const adapm_tensor* t, uint64_t n, co
     if (!float_type(t[i].type)) return fail(ctx, ADAPM_EINVAL, "%s[%llu]: unknown element type %d", what, at, t[i].type);
     if (t[i].count == 0) continue;
     if (!t[i].data || t[i].count > (1ull << 48)) return fail(ctx, ADAPM_EINVAL, "%s[%llu]: bad data/count", what, at);
-    if (reinterpret_cast<uintptr_t>(t[i].data) % type_bytes(t[i].type) != 0)
+    if (reinterpret_cast<uintptr_t>(t[i].data) % type_bytes(t[i].type) != 0 || !word_aligned(t[i].live))
       return fail(ctx, ADAPM_EINVAL, "%s[%llu] is not aligned to its type", what, at);
     if (!device.has(t[i].data) || (t[i].live && !device.has(t[i].live)))
       return fail(ctx, ADAPM_EINVAL, "%s[%llu] is not a device array", what, at);
@@ -1706,6 +1706,8 @@ adapm_status adapm_embed_grad(adapm_ctx* ctx, uint32_t worker, const adapm_token
   st = check_tokens(ctx, worker, tokens, dim, grad, &n);
   if (st != ADAPM_OK) return st;
   if (!count || (n > 0 && (!keys || !rows))) return fail(ctx, ADAPM_EINVAL, "null keys, rows or count");
+  if (!word_aligned(count) || (n > 0 && (!word_aligned(keys) || !word_aligned(rows))))
+    return fail(ctx, ADAPM_EINVAL, "keys, rows or count are not aligned to their type");
   ProfScope ps(ctx, 5);
   Output<uint32_t> oc;
   CK(stage_out(ctx, count, 1, &oc));
@@ -1823,7 +1825,7 @@ adapm_status adapm_grad_norm(adapm_ctx* ctx, const adapm_tensor* grads, uint64_t
   if (st != ADAPM_OK) return st;
   st = check_tensors(ctx, grads, n, "grads");
   if (st != ADAPM_OK) return st;
-  if (!norm || !norm_aligned(norm)) return fail(ctx, ADAPM_EINVAL, "norm is null or not aligned");
+  if (!norm || !word_aligned(norm)) return fail(ctx, ADAPM_EINVAL, "norm is null or not aligned");
   std::vector<GradTensor> t;
   try {
     t.reserve(n);
@@ -1849,7 +1851,7 @@ adapm_status adapm_clip_grads(adapm_ctx* ctx, const adapm_tensor* grads, const a
   st = check_tensors(ctx, grads, n, "grads");
   if (st == ADAPM_OK && outs) st = check_tensors(ctx, outs, n, "outs");
   if (st != ADAPM_OK) return st;
-  if (!norm || !norm_aligned(norm) || !is_device_ptr(norm))
+  if (!norm || !word_aligned(norm) || !is_device_ptr(norm))
     return fail(ctx, ADAPM_EINVAL, "norm is not a device word");
   if (!(max_norm >= 0.f)) return fail(ctx, ADAPM_EINVAL, "max_norm must not be negative");
   std::vector<GradTensor> t;
@@ -1881,11 +1883,13 @@ adapm_status adapm_push_grads(adapm_ctx* ctx, uint32_t worker, const uint32_t* k
   if (st != ADAPM_OK) return st;
   if (worker >= ctx->s.W) return fail(ctx, ADAPM_EINVAL, "worker %u >= %u", worker, ctx->s.W);
   if (n > kMaxN || (n > 0 && (!keys || !rows))) return fail(ctx, ADAPM_EINVAL, "bad pointers/n");
+  if (n > 0 && (!word_aligned(keys) || !word_aligned(rows)))
+    return fail(ctx, ADAPM_EINVAL, "keys or rows are not aligned to their type");
   if (dim == 0 || (adagrad ? 2 * (uint64_t)dim != ctx->s.D : dim > ctx->s.D))
     return fail(ctx, ADAPM_EINVAL, "dim %u does not match value_len %u", dim, ctx->s.D);
   // (theta and accumulators are read and written as float4 halves of a row)
   if (adagrad && dim % 4 != 0) return fail(ctx, ADAPM_EINVAL, "dim %u: need a multiple of 4 with AdaGrad", dim);
-  if (norm && (!norm_aligned(norm) || !is_device_ptr(norm)))
+  if (norm && (!word_aligned(norm) || !is_device_ptr(norm)))
     return fail(ctx, ADAPM_EINVAL, "norm is not a device word");
   if (norm && !(max_norm >= 0.f)) return fail(ctx, ADAPM_EINVAL, "max_norm must not be negative");
   if (n == 0) return ADAPM_OK;

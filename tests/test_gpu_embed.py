@@ -702,6 +702,31 @@ def test_refusals(gpu_lib):
     pm6.close()
 
 
+def test_arrays_between_words_are_refused(gpu_lib):
+    pm = make(gpu_lib, table(20, 16))
+    t, x = torch.arange(6, device="cuda"), torch.ones(6, 16, device="cuda")
+    g = pm.embed_grad(0, t, x)
+    pm.wait()
+    kept = [a.clone() for a in g]
+    import ctypes
+    lib = gpu_lib.load()
+    tok = gpu_lib._Tokens(t.data_ptr(), 64, 0, 0, 1, 6, 6, 1)
+    row = gpu_lib._Rows(x.data_ptr(), 0, 96, 16)
+    ptr = [a.data_ptr() for a in g]
+    for off in (1, 2, 3):
+        for i in range(3):
+            at = [p + off * (j == i) for j, p in enumerate(ptr)]
+            assert lib.adapm_embed_grad(pm._h, 0, ctypes.byref(tok), 16, 1.0, ctypes.byref(row), *at) == gpu_lib.EINVAL
+        for keys, rows in ((ptr[0] + off, ptr[1]), (ptr[0], ptr[1] + off)):
+            assert lib.adapm_push_grads(pm._h, 0, keys, rows, 5, 16, 0, 0.1, 0.0, 1.0, 1.0, None) == gpu_lib.EINVAL
+        live = gpu_lib._Tensor(ptr[1], 96, ptr[2] + off, 16, 0)
+        assert lib.adapm_grad_norm(pm._h, ctypes.byref(live), 1, 1.0, x.data_ptr()) == gpu_lib.EINVAL
+    pm.wait()
+    assert all(torch.equal(a, b) for a, b in zip(g, kept)) and (x == 1).all()
+    assert np.array_equal(pm.read_main(np.arange(20)), table(20, 16))
+    pm.close()
+
+
 def test_a_sort_that_gives_up_leaves_the_outputs(gpu_lib):
     """The bounded wait of a signalled batch's sort runs out (host hook, no GPU fault): ADAPM_ETIMEOUT, nothing written."""
     pm = make(gpu_lib, table(1000, 8))
