@@ -178,6 +178,41 @@ def test_lookup_reads_what_pull_reads_in_every_replica_state(gpu_lib, relocate, 
     pm.close()
 
 
+@pytest.mark.parametrize("D", [8, 64, 200, 256, 600, 1024])
+@pytest.mark.parametrize("relocate,refresh", [(False, False), (True, False), (False, True)])
+def test_wide_loads_read_what_pull_reads_in_every_replica_state(gpu_lib, D, relocate, refresh):
+    """Rows of a multiple of eight floats: aliases, pending updates, replicas with values of their own, folded ones."""
+    K, W = 90, 2
+    pm = make(gpu_lib, table(K, D), W, relocate=relocate, delta_refresh=refresh)
+    rng = np.random.default_rng(D)
+    every = torch.arange(K, device="cuda")
+
+    def same():
+        for w in range(W):
+            rows = pm.pull(w, every)
+            for dtype in TYPES:
+                got = pm.embed(w, every, scale=0.5, dtype=dtype)
+                pm.wait()
+                assert torch.equal(got, (rows * 0.5).to(dtype))
+
+    same()
+    for clock in range(3):
+        for w in range(W):
+            pm.intent(w, torch.from_numpy(rng.integers(0, K, size=50)).cuda(), clock, clock + 2)
+            for times in range(3):
+                keys = torch.from_numpy(rng.integers(0, K, size=40)).cuda()
+                pm.push(w, keys, torch.from_numpy(rng.normal(size=(40, D)).astype(np.float32)).cuda())
+                same()
+        if clock == 1:
+            pm.sync()
+            same()
+        for w in range(W):
+            pm.advance_clock(w)
+            same()
+    assert not np.array_equal(pm.read_main(np.arange(K)), table(K, D))
+    pm.close()
+
+
 def test_lookup_with_early_events_and_on_the_host(gpu_lib):
     """A lookup is a worker's first access of a clock as a pull is; host ids and rows are taken as everywhere."""
     K, D = 200, 16
@@ -395,6 +430,37 @@ def test_gradient_takes_an_intents_plan(gpu_lib, n, ids):
     assert st["planned_pushes"] == 6 and st["plan_misses"] >= 2 and plain.stats()["planned_pushes"] == 0
     pm.close()
     plain.close()
+
+
+@pytest.mark.parametrize("n", [3000, 20_000, 600_000])   # (by counting, by the token sort, by the push's sort)
+@pytest.mark.parametrize("ids", [torch.int32, torch.int64])
+@pytest.mark.parametrize("view", ["flat", "shifted", "transposed", "host"])
+def test_a_signalled_batch_hits_its_plan_and_another_misses(gpu_lib, n, ids, view):
+    """Each call's own count of plans looked up and missed, whatever layout and type the tokens have."""
+    K, dim = 700, 4
+
+    def batch(seed):
+        t = torch.from_numpy(zipf(n // 8 * 8 + 8, K, seed)).to(ids).reshape(8, -1).cuda()
+        return {"flat": t[:, :n // 8].contiguous(), "shifted": t[:, :-1], "transposed": t[:, 1:].t(),
+                "host": t[:, :-1].contiguous().cpu()}[view]
+
+    pm = make(gpu_lib, np.zeros((K, dim), np.float32))
+    t, other = batch(1), batch(2)
+    pm.intent(0, t, 0, 5)
+    pm.wait()
+    grad = torch.ones((*t.shape, dim), device="cuda")
+    planned = missed = 0
+    for tokens, hit in ((t, True), (other, False), (t, True)):
+        for pad in (None, -1, K, int(t[0, 0]), int(other[0, 0])):   # (no token's, or a valid one's)
+            g = pm.embed_grad(0, tokens, grad, pad=pad)
+            pm.wait()
+            st = pm.stats()
+            planned, missed = planned + 1, missed + (not hit)
+            assert st["planned_pushes"] == planned and st["plan_misses"] == missed
+            keys, counts = np.unique(tokens.cpu().numpy(), return_counts=True)
+            keep = keys != pad
+            check_row_grads(g, keys[keep], np.repeat(counts[keep][:, None], dim, 1).astype(np.float64), 0.0)
+    pm.close()
 
 
 def test_gradient_is_the_same_every_time(gpu_lib):
