@@ -55,6 +55,27 @@ def test_lookup_is_the_scaled_rounded_row(gpu_lib, dtype, D, dim, n):
     pm.close()
 
 
+# either end of every width that the kernel has lanes and loads for, rows of a multiple of eight elements or not
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim", [8, 32, 40, 64, 72, 128, 136, 256, 264, 512, 520, 640, 768, 776, 1024,
+                                 2, 14, 18, 31, 33, 62, 66, 127, 129, 254, 258, 381, 386, 449, 510, 514, 767, 770, 1021])
+def test_lookup_of_every_width(gpu_lib, dtype, dim):
+    K, D = 97, -(-dim // 8) * 8
+    init = table(K, D)
+    pm = make(gpu_lib, init)
+    for n in (3, 70, 30_000):   # (a warp's batch: one round of rows, some, as many as it takes)
+        t = zipf(n, K, n)
+        want = (torch.from_numpy(init[:, :dim]) * np.float32(-0.3)).to(dtype)[torch.from_numpy(t)]
+        buf = torch.full((n * dim + 8,), 9.0, device="cuda", dtype=dtype)
+        for first in (0, 1, 2, 4):   # rows that begin on every vector boundary and between them
+            buf.fill_(9.0)
+            pm.embed(0, torch.from_numpy(t).cuda(), dim, scale=-0.3, out=buf[first:first + n * dim].view(n, dim))
+            pm.wait()
+            assert torch.equal(buf[first:first + n * dim].view(n, dim).cpu(), want)
+            assert (buf[:first] == 9.0).all() and (buf[first + n * dim:] == 9.0).all()
+    pm.close()
+
+
 def test_lookup_of_strided_tokens_into_strided_rows(gpu_lib):
     K, D, dim = 1000, 64, 60
     init = table(K, D)

@@ -182,6 +182,32 @@ def test_rows_whose_number_the_device_knows(gpu_lib, pm):
         assert bool(g.rows[live:].isnan().all())
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_rows_whose_number_the_device_knows_into_others(gpu_lib, pm, dtype):
+    rows, count = torch.randn(40, 21, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    keys = torch.zeros(40, dtype=torch.int32, device="cuda")
+    for live in (0, 1, 13, 40, 41):
+        count.fill_(live)
+        src, dst = rows.clone(), torch.full((40, 21), 5.0, device="cuda", dtype=dtype)
+        src[live:] = float("nan")
+        more, out = torch.randn(77, device="cuda").to(dtype), torch.empty(77, device="cuda")
+        want = norm64([rows[:live], more])
+        g = gpu_lib.RowGrads(keys, src, count)
+        norm = pm.grad_norm([g, more])
+        # (the rows' number is the gradient's: the target's own is not looked at)
+        for target in (dst, gpu_lib.RowGrads(keys, dst, torch.full_like(count, 3))):
+            dst.fill_(5.0)
+            pm.clip_grads([g, more], norm, want / 4, out=[target, out])
+            pm.wait()
+            ut, tiny = TYPES[dtype]
+            y = rows[:live].double() / 4
+            assert ((dst[:live].double() - y).abs() <= y.abs() * (ut + 40 * U) + tiny).all()
+            assert (dst[live:] == 5.0).all()
+            assert ((out.double() - more.double() / 4).abs() <= more.double().abs() * 40 * U).all()
+        assert abs(float(norm) - want) <= 33 * U * want
+        assert torch.equal(src[:live], rows[:live]) and bool(src[live:].isnan().all())
+
+
 def test_the_same_every_time(gpu_lib, pm):
     t = [torch.randn(1_000_003, device="cuda"), torch.randn(500_000, device="cuda").to(torch.bfloat16)]
     norms = [pm.grad_norm(t) for _ in range(5)]
