@@ -388,12 +388,17 @@ adapm_status adapm_clip_grads(adapm_ctx* ctx, const adapm_tensor* grads, const a
  * `keys`, as adapm_embed_grad leaves them: ascending, each at most once,
  * 0xFFFFFFFF skipped (a key that is not above the one before it is skipped
  * and reported as ADAPM_ESTATE by adapm_wait, one >= num_keys as
- * ADAPM_ERANGE).  With g = scale * f * rows[u], f from norm and max_norm as in
+ * ADAPM_ERANGE).  Only neighbours are compared: where a list that is out of
+ * order holds a key twice with others between, the values of that key are
+ * undefined afterwards, every worker's; those of keys listed once are as said
+ * here.  With g = scale * f * rows[u], f from norm and max_norm as in
  * adapm_clip_grads (norm = NULL: 1), the pushed row is -lr * g in the first
  * dim floats (nothing is added to the others, whatever f is), or with adagrad
  * (value_len = 2 * dim, dim a multiple of 4) [-lr * g / sqrt(a + g*g + eps) |
- * g*g], a the accumulators before the call.
- * Written as adapm_push writes its sums, without a sort. */
+ * g*g], a the accumulators before the call.  Written as adapm_push writes its
+ * sums, without a sort.  No update is skipped for what the norm is: a NaN
+ * norm makes the updated floats NaN; an infinite one makes g zero, and NaN
+ * where the row itself is infinite or NaN. */
 adapm_status adapm_push_grads(adapm_ctx* ctx, uint32_t worker, const uint32_t* keys, const float* rows,
                               uint64_t n, uint32_t dim, int adagrad, float lr, float eps, float scale,
                               float max_norm, const float* norm);

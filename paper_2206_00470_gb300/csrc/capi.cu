@@ -1492,7 +1492,8 @@ adapm_status adapm_wait(adapm_ctx* ctx) {
   if (errors & ERR_INTERNAL)
     return fail(ctx, ADAPM_ESTATE, "an index in the library's own state was out of range (element skipped)");
   if (errors & ERR_KEY_ORDER)
-    return fail(ctx, ADAPM_ESTATE, "the keys of a row update were not distinct and ascending (some skipped)");
+    return fail(ctx, ADAPM_ESTATE, "the keys of a row update were not distinct and ascending (some are skipped, "
+                "those listed twice are undefined)");
   return ADAPM_OK;
 }
 

@@ -629,6 +629,26 @@ def test_update_leaves_what_lies_behind_dim(gpu_lib, D, dim, bad, held):
     pm.close()
 
 
+@pytest.mark.parametrize("adagrad", [False, True])
+def test_update_by_an_infinite_norm(gpu_lib, adagrad):
+    """Nothing changes but where an infinity or a NaN came from."""
+    K, dim = 30, 12
+    init = np.abs(table(K, 2 * dim if adagrad else dim)) + 0.1
+    pm = make(gpu_lib, init)
+    rows = torch.ones(8, dim, device="cuda")
+    rows[2, 5], rows[6, 0] = float("inf"), float("nan")
+    pm.push_grads(0, torch.arange(3, 11, device="cuda"), rows, 0.5, adagrad=adagrad,
+                  norm=torch.tensor(float("inf"), device="cuda"), max_norm=1.0)
+    pm.wait()
+    want = init.copy()
+    for k, c in ((5, 5), (9, 0)):
+        want[k, c] = float("nan")
+        if adagrad:
+            want[k, dim + c] = float("nan")
+    assert np.array_equal(pm.read_main(np.arange(K)), want, equal_nan=True)
+    pm.close()
+
+
 def test_buffers_of_a_larger_batch(gpu_lib):
     """The last, smaller batch in the buffers of the others: nothing of theirs is updated again."""
     K, D = 50, 8
