@@ -358,7 +358,10 @@ adapm_status adapm_embed(adapm_ctx* ctx, uint32_t worker, const adapm_tokens* to
  * within fixed chunks of the sorted batch, chunk sums in chunk order:
  * deterministic for a given input.  The store is neither read nor written;
  * tokens that the worker has signalled (adapm_intent) are grouped by that
- * intent's plan, as in adapm_push.  keys, rows and count are device or host
+ * intent's plan, as in adapm_push.  (An intent takes no padding: a batch whose
+ * pad is no key of the store cannot be signalled whole, and without its padding
+ * has another number of keys.  Such a batch is sorted by this call; pad with a
+ * key to use the plan.)  keys, rows and count are device or host
  * arrays (rows of a host array behind the last are set to 0). */
 adapm_status adapm_embed_grad(adapm_ctx* ctx, uint32_t worker, const adapm_tokens* tokens, uint32_t dim,
                               float scale, const adapm_rows* grad, uint32_t* keys, float* rows,

@@ -104,7 +104,9 @@ __device__ __forceinline__ void store8(float* p, float4 a, float4 b) {
 // of eight elements): 256-bit loads, 256-bit or (16-bit types) 128-bit stores,
 // half as many of each (2^20 rows of 64 floats 106 us, now 75).  Blocks per SM,
 // by what the registers hold and what was fastest: 2^20 rows of 100 floats 171
-// us at five, 142 at eight; 2^18 of 300 floats 104 at four, 110 at five.
+// us at five, 142 at eight; 2^18 of 300 floats 104 at four, 110 at five.  At eight
+// the kernels of W = 2, U = 1 spill one word of a thread (G = 32: four) to local
+// memory.
 constexpr int embed_blocks_per_sm(int U, int W) { return U == 1 ? 8 : (U * W <= 3 ? 4 : 3); }
 // Tokens per batch, at most.
 constexpr uint32_t embed_batch(int U) { return U == 1 ? 32 : 4; }

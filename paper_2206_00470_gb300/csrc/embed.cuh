@@ -1,4 +1,4 @@
-// Token embeddings: what the entry points (embed_api.cu) hand to the kernels of
+// Token embeddings: what the entry points (capi.cu) hand to the kernels of
 // embed.cu, embed_sort.cu, embed_grad.cuh, push_grads.cu and grads.cu.
 #pragma once
 

@@ -12,7 +12,7 @@
 // each row is read once, each sum written once, a hot token's rows are spread
 // over many groups, and the order of every sum is fixed by the input alone.
 // Bound by memory where rows are many (64 x 4096 rows of 1024 bf16 elements of
-// 62,000 tokens: grad_sum 126 us, 6.3 TB/s; the sort in front 30, the rest 9),
+// 62,000 tokens: grad_sum 126 us, 6.3 TB/s; the sort in front 26, the rest 8),
 // by the latency of its launches where they are few (3 x 2003 rows of 200:
 // sort 10, grad_sum 6.6, grad_combine 3 us).
 //

@@ -322,9 +322,11 @@ __global__ void __launch_bounds__(NT) token_pass_kernel(const TokenView t, uint6
   }
 }
 
-// Passes of a sort by `bits` bits: of up to 9 bits while the table is short (up
-// to 16,384 tokens) or a thread has one digit of it all the same (tiles of 512
-// threads), else of up to 8.  17 and 18 bits, two passes against three: 8,192
+// Passes of a sort by `bits` bits.  Every thread of a block sums its digits' rows
+// of the table, a load per eight tiles.  A pass of 9 bits has two digits per
+// thread of a block of 256, so its sums are twice a pass of 8 bits' where rows
+// are long; up to 16,384 tokens a row is four loads at most, and above 131,072 a
+// block has 512 threads, a digit each: 9 bits there, else up to 8.  17 and 18 bits, two passes against three: 8,192
 // tokens 10 and 12 us, 16,384 12.5 and 13.5, 262,144 26 and 28, 524,288 34 and
 // 42; but 65,536 21 and 18, 131,072 23 and 20.
 int token_passes(uint64_t n, int bits) {
