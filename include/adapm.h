@@ -406,6 +406,98 @@ adapm_status adapm_push_grads(adapm_ctx* ctx, uint32_t worker, const uint32_t* k
                               uint64_t n, uint32_t dim, int adagrad, float lr, float eps, float scale,
                               float max_norm, const float* norm);
 
+/* ---- dense layers of a token model ----------------------------------------- */
+/* What such a model runs between adapm_embed and adapm_embed_grad: layer norm,
+ * and the loss that distils a teacher's top logits, each with its gradient.
+ * They neither read nor write the store and belong to no worker; they run on
+ * the library stream like every call, and are recorded in a graph like one.
+ * Arrays are device arrays, aligned to their elements (ADAPM_EINVAL
+ * otherwise).  Sums are fp32 in a fixed order: results are deterministic. */
+
+/* outer x inner rows of `dim` elements; row (o, i) of an adapm_rows begins at
+ * element o * outer_stride + i * inner_stride.  At most 2^31 rows, dim from 1
+ * to 2^31. */
+typedef struct {
+  uint64_t outer, inner;
+  uint32_t dim;
+} adapm_shape;
+
+/* `dim` elements without gaps. */
+typedef struct {
+  void* data;
+  int32_t type;
+} adapm_vector;
+
+/* out = (x - m) r weight + bias for every row, m its mean, r = 1 / sqrt(v +
+ * eps), v its variance (the mean of the squared differences from m).  weight
+ * and bias (NULL: ones, zeros) have types of their own.  stats (NULL: not
+ * wanted) receives m and r of every row, two floats a row without gaps.
+ * Computed in fp32, rounded once to out's type.  out is x's own memory (same
+ * type and strides) or does not overlap it; its rows must not overlap each
+ * other (ADAPM_EINVAL where two strides make them).  eps must not be
+ * negative.  An infinity or NaN makes its own row NaN, no other. */
+adapm_status adapm_layer_norm(adapm_ctx* ctx, const adapm_shape* shape, const adapm_rows* x,
+                              const adapm_vector* weight, const adapm_vector* bias, float eps,
+                              const adapm_rows* out, float* stats);
+
+/* The gradient of adapm_layer_norm.  x, weight: as given there; stats: as left
+ * there; grad: the gradient of out.  With h = (x - m) r and g = grad * weight
+ * (elementwise) every row of dx is r (g - mean(g) - h mean(g h)); dweight is
+ * the sum over rows of grad * h, dbias that of grad (zeros without rows).  dx,
+ * dweight and dbias may each be NULL (not wanted); dx is the memory of x or
+ * of grad (same type and strides) or overlaps neither. */
+adapm_status adapm_layer_norm_grad(adapm_ctx* ctx, const adapm_shape* shape, const adapm_rows* x,
+                                   const adapm_rows* grad, const float* stats, const adapm_vector* weight,
+                                   const adapm_rows* dx, const adapm_vector* dweight, const adapm_vector* dbias);
+
+/* A teacher's largest logits: `top` (id, logit) pairs per row, in any order,
+ * without gaps (row (o, i) is pair list o * inner + i).  ids are signed, of 32
+ * or 64 bits.  A pair with id -1, or whose logit is -infinity, is no entry (so
+ * that lists may be shorter); one with another id outside the vocabulary is
+ * none either, and reported as ADAPM_ERANGE by adapm_wait.  Entries with the
+ * same id count as one each.  top is at most 1024. */
+typedef struct {
+  const void* ids;
+  int32_t id_bits;
+  const void* logits;
+  int32_t type;
+  uint32_t top;
+} adapm_teacher;
+
+/* One token id per row, signed, of 32 or 64 bits, without gaps.  With has_pad,
+ * ids equal to pad are no label (32-bit ids equal a pad of [-2^31, 2^32) by its
+ * low 32 bits, and no other); an id outside the vocabulary is none either, and
+ * reported as ADAPM_ERANGE by adapm_wait. */
+typedef struct {
+  const void* ids;
+  int32_t id_bits;
+  int32_t has_pad;
+  int64_t pad;
+} adapm_labels;
+
+/* The loss of every row of student logits s (dim is the vocabulary) against a
+ * teacher's list and a label, and its gradient.  With p the softmax of the
+ * list's logits / T (over its entries alone), q the softmax of s / T and c that
+ * of s, T = temperature > 0:
+ *   loss = soft T^2 sum_j p_j (ln p_j - ln q_id_j) + hard (-ln c_label)
+ *   grad_v = scale weights[row] (soft T (q_v - sum of p_j with id_j = v)
+ *                                + hard (c_v - [v = label]))
+ * A row without entries has no first term, a row without a label (labels NULL,
+ * or padding) no second; a row with neither has loss 0 and a gradient of
+ * zeros, whatever its logits hold.  soft = 0 or a NULL teacher: no first term
+ * anywhere, hard = 0: no second.  An entry with p_j = 0 adds nothing to the
+ * loss.  Logits of -infinity have probability 0 (a row of nothing else is NaN,
+ * as are rows with +infinity or NaN).  loss: one float a row, without scale
+ * and weights.  weights (one float a row; NULL: ones) and grad (NULL: not
+ * wanted) may be left out.  grad has the logits' type and is their own memory
+ * (same strides) or does not overlap them; its rows must not overlap each
+ * other.  Computed in fp32 from one reading of the logits; a gradient is
+ * rounded once to its type. */
+adapm_status adapm_distill(adapm_ctx* ctx, const adapm_shape* shape, const adapm_rows* logits,
+                           const adapm_teacher* teacher, float temperature, float soft,
+                           const adapm_labels* labels, float hard, float scale, const float* weights,
+                           const adapm_rows* grad, float* loss);
+
 /* ---- inspection (synchronising; for tests and tools) ------------------ */
 adapm_status adapm_clock(adapm_ctx* ctx, uint32_t worker, int64_t* out);
 
@@ -464,7 +556,7 @@ adapm_status adapm_get_stats(adapm_ctx* ctx, adapm_stats* out);
  * around its work on the library stream.  Operations: 0 intent, 1 advance,
  * 2 pull (adapm_embed too), 3 push (adapm_push_grads too), 4 sync,
  * 5 training-step compute (without its push; the embedding's gradient, the
- * gradient norm and clipping too), 6 push gather-scatter kernel alone,
+ * gradient norm and clipping, and the dense layers too), 6 push gather-scatter kernel alone,
  * 7 pull gather kernel alone (or adapm_embed's).
  * adapm_profile_read synchronises and returns the summed milliseconds and
  * call counts since the last read (arrays of ADAPM_NUM_OPS). */

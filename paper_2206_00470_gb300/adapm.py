@@ -31,6 +31,7 @@ EXPORTS = [
     "adapm_profile_read", "adapm_kernel_launches", "adapm_push_noalloc", "adapm_last_error",
     "adapm_debug_fail_next_barrier", "adapm_debug_fail_next_launch",
     "adapm_embed", "adapm_embed_grad", "adapm_grad_norm", "adapm_clip_grads", "adapm_push_grads",
+    "adapm_layer_norm", "adapm_layer_norm_grad", "adapm_distill",
 ]
 
 
@@ -97,6 +98,24 @@ class _Tensor(ctypes.Structure):
                 ("row_len", ctypes.c_uint32), ("type", ctypes.c_int32)]
 
 
+class _Shape(ctypes.Structure):
+    _fields_ = [("outer", ctypes.c_uint64), ("inner", ctypes.c_uint64), ("dim", ctypes.c_uint32)]
+
+
+class _Vector(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("type", ctypes.c_int32)]
+
+
+class _Teacher(ctypes.Structure):
+    _fields_ = [("ids", ctypes.c_void_p), ("id_bits", ctypes.c_int32), ("logits", ctypes.c_void_p),
+                ("type", ctypes.c_int32), ("top", ctypes.c_uint32)]
+
+
+class _Labels(ctypes.Structure):
+    _fields_ = [("ids", ctypes.c_void_p), ("id_bits", ctypes.c_int32), ("has_pad", ctypes.c_int32),
+                ("pad", ctypes.c_int64)]
+
+
 class AdaPMError(RuntimeError):
     def __init__(self, status, message):
         super().__init__(f"{STATUS_NAMES.get(status, status)}: {message}")
@@ -147,6 +166,9 @@ def load(path=LIB_PATH):
         "adapm_grad_norm": [P, P, U64, F, P],
         "adapm_clip_grads": [P, P, P, U64, F, F, P],
         "adapm_push_grads": [P, U32, P, P, U64, U32, I, F, F, F, F, P],
+        "adapm_layer_norm": [P, P, P, P, P, F, P, P],
+        "adapm_layer_norm_grad": [P, P, P, P, P, P, P, P, P],
+        "adapm_distill": [P, P, P, P, F, F, P, F, F, P, P, P],
     }
     for name, args in sig.items():
         fn = getattr(L, name)
@@ -320,6 +342,27 @@ def _grad_list(grads):
     return grads if isinstance(grads, GradList) else GradList(grads)
 
 
+# -- dense layers ------------------------------------------------------------------
+class NormGrads(collections.namedtuple("NormGrads", ["x", "weight", "bias"])):
+    """Gradients of a layer norm's input, weight and bias (adapm_layer_norm_grad); None where one is not wanted."""
+
+    __slots__ = ()
+
+
+class _Dense:
+    """Descriptors that the calls on dense layers refill (making one anew takes longer than filling it)."""
+
+    __slots__ = ("shape", "rows", "vectors", "teacher", "labels", "shape_ref", "rows_ref", "vectors_ref",
+                 "teacher_ref", "labels_ref")
+
+    def __init__(self):
+        self.shape, self.teacher, self.labels = _Shape(), _Teacher(), _Labels()
+        self.rows, self.vectors = [_Rows() for _ in range(3)], [_Vector() for _ in range(3)]
+        for name in ("shape", "teacher", "labels"):
+            setattr(self, name + "_ref", ctypes.byref(getattr(self, name)))
+        self.rows_ref, self.vectors_ref = [ctypes.byref(r) for r in self.rows], [ctypes.byref(v) for v in self.vectors]
+
+
 def poisson_quantile(lam, p):
     """The p quantile of Poisson(lam) as the library's adaptive action timing computes it (host only)."""
     out = ctypes.c_int64()
@@ -376,6 +419,7 @@ class ParameterManager:
         self._device = torch.device("cuda", torch.cuda.current_device())
         self._t, self._r = _Tokens(), _Rows()   # refilled by every call that takes tokens
         self._t_ref, self._r_ref = ctypes.byref(self._t), ctypes.byref(self._r)
+        self._d = _Dense()
 
     # -- plumbing ------------------------------------------------------------
     def _check(self, st):
@@ -616,6 +660,176 @@ class ParameterManager:
         _check_norm(norm)
         self._check(self._lib.adapm_push_grads(self._h, worker, k, r, n, dim, bool(adagrad), lr, eps, scale, max_norm,
                                                None if norm is None else norm.data_ptr()))
+
+    # -- dense layers --------------------------------------------------------------
+    def _gpu(self, t, what, dtype=None):
+        if not t.is_cuda or t.device.index != self._device.index:
+            raise ValueError(f"{what} is a tensor on {self._device}, not on {t.device}")
+        if dtype is not None and t.dtype is not dtype:
+            raise ValueError(f"{what} is {dtype}, not {t.dtype}")
+        return t
+
+    def _dense_rows(self, named):
+        """Fills the shape and a descriptor of rows for each (tensor, name, written): all (..., dim), of one shape.
+        Inputs that no outer and inner stride reach are copied; returns the tensors."""
+        first = named[0][0]
+        shape, flat = first.shape, True
+        if not shape:
+            raise ValueError(f"{named[0][1]} needs a dimension")
+        tensors = []
+        for t, what, written in named:
+            self._gpu(t, what)
+            if t.shape != shape:
+                raise ValueError(f"{what} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+            if shape[-1] > 1 and t.stride(-1) != 1 and t.numel() > 0:
+                if written:
+                    raise ValueError(f"elements of a row of {what} must follow each other")
+                with self._on_stream():
+                    t = t.contiguous()
+            flat = flat and t.is_contiguous()
+            tensors.append(t)
+        d, dim = self._d, shape[-1]
+        d.shape.dim = dim
+        if flat:
+            d.shape.outer, d.shape.inner = 1, (first.numel() // dim if dim else 0)
+            steps = [(0, dim)] * len(tensors)
+        else:
+            got = _two_levels(shape[:-1], *(t.stride()[:-1] for t in tensors))
+            if got is None:   # (outputs stay as they are)
+                with self._on_stream():
+                    tensors = [t if w else t.contiguous() for t, (_, _, w) in zip(tensors, named)]
+                got = _two_levels(shape[:-1], *(t.stride()[:-1] for t in tensors))
+            if got is None:
+                raise ValueError("rows of the output are not reached by an outer and an inner stride")
+            d.shape.outer, d.shape.inner, *steps = got
+        for r, t, (outer, inner) in zip(d.rows, tensors, steps):
+            r.data, r.type, r.outer_stride, r.inner_stride = t.data_ptr(), _type_of(t.dtype), outer, inner
+        return tensors
+
+    def _dense_vector(self, i, t, dim, what):
+        """The descriptor of a vector of dim elements (None: none)."""
+        if t is None:
+            return None
+        if self._gpu(t, what).numel() != dim or not t.is_contiguous():
+            raise ValueError(f"{what} holds {dim} elements without gaps")
+        v = self._d.vectors[i]
+        v.data, v.type = t.data_ptr(), _type_of(t.dtype)
+        return self._d.vectors_ref[i]
+
+    def layer_norm(self, x, weight=None, bias=None, eps=1e-5, out=None, dtype=None, stats=None):
+        """(x - mean) / sqrt(variance + eps) * weight + bias for every row of x (..., dim), in dtype (x's unless
+        given, or out's).  stats (float32, two per row): receives every row's mean and reciprocal deviation, which
+        layer_norm_grad needs.  out may be x."""
+        torch, d = _torch(), self._d
+        if out is None:
+            with self._on_stream():
+                out = torch.empty(x.shape, dtype=dtype or x.dtype, device=self._device)
+        elif dtype is not None and out.dtype != dtype:
+            raise ValueError("out has another dtype")
+        keep = self._dense_rows(((x, "x", False), (out, "out", True)))
+        dim = x.shape[-1]
+        w, b = self._dense_vector(0, weight, dim, "weight"), self._dense_vector(1, bias, dim, "bias")
+        if stats is not None:
+            self._check_stats(stats, x)
+        self._check(self._lib.adapm_layer_norm(self._h, d.shape_ref, d.rows_ref[0], w, b, eps, d.rows_ref[1],
+                                               None if stats is None else stats.data_ptr()))
+        del keep
+        return out
+
+    def _check_stats(self, stats, x):
+        self._gpu(stats, "stats", _torch().float32)
+        if stats.numel() != 2 * (x.numel() // max(1, x.shape[-1])) or not stats.is_contiguous():
+            raise ValueError("stats holds two elements for every row, without gaps")
+
+    def layer_norm_grad(self, x, grad, stats, weight=None, bias=None, out=None):
+        """NormGrads of layer_norm(x, weight, ..., stats=stats) for the gradient of its output: of x in x's dtype, of
+        the weight (unless None) in the weight's, and of the bias (bias=True, and by default with a weight) in the
+        weight's.  out: NormGrads to fill, None for those not wanted; its x may be x or grad."""
+        torch, d = _torch(), self._d
+        dim = x.shape[-1] if x.dim() else 0
+        if out is None:
+            like = torch.float32 if weight is None else weight.dtype
+            with self._on_stream():
+                dw, db = (torch.empty(dim, dtype=like, device=self._device) if want else None
+                          for want in (weight is not None, weight is not None if bias is None else bias))
+                out = NormGrads(torch.empty(x.shape, dtype=x.dtype, device=self._device), dw, db)
+        rows = [(x, "x", False), (grad, "grad", False)]
+        if out.x is not None:
+            rows.append((out.x, "out.x", True))
+        keep = self._dense_rows(rows)
+        self._check_stats(stats, x)
+        w, dw, db = (self._dense_vector(i, t, dim, what) for i, (t, what) in
+                     enumerate(((weight, "weight"), (out.weight, "out.weight"), (out.bias, "out.bias"))))
+        self._check(self._lib.adapm_layer_norm_grad(self._h, d.shape_ref, d.rows_ref[0], d.rows_ref[1], stats.data_ptr(),
+                                                    w, None if out.x is None else d.rows_ref[2], dw, db))
+        del keep
+        return out
+
+    def _ids(self, t, count, what):
+        """Signed ids without gaps, and their bits."""
+        torch = _torch()
+        if t.dtype is not torch.int32 and t.dtype is not torch.int64:
+            raise ValueError(f"{what} are int32 or int64, not {t.dtype}")
+        if self._gpu(t, what).numel() != count:
+            raise ValueError(f"{what}: {count} are needed, not {t.numel()}")
+        if not t.is_contiguous():
+            with self._on_stream():
+                t = t.contiguous()
+        return t, 32 if t.dtype is torch.int32 else 64
+
+    def distill(self, logits, ids=None, teacher=None, temperature=1.0, soft=1.0, labels=None, hard=0.0, pad=None,
+                scale=1.0, weights=None, grad=None, loss=None):
+        """The loss of every row of student logits (..., vocabulary) against a teacher's top logits and labels:
+        soft T^2 KL(softmax(teacher / T) || softmax(logits / T)) + hard * cross entropy, as float32 (...).
+
+        ids, teacher    (..., top): the vocabulary ids (int32 or int64; -1: no entry) of the teacher's top logits
+        labels, pad     (...): token ids; those equal to pad are none
+        grad            a tensor like the logits (or the logits themselves) that receives scale * weights * the
+                        gradient of the loss; weights: float32, one factor per row"""
+        torch, d = _torch(), self._d
+        lead = logits.shape[:-1]
+        rows = [(logits, "logits", False)]
+        if grad is not None:
+            rows.append((grad, "grad", True))
+        keep = [self._dense_rows(rows)]
+        n = logits.numel() // max(1, logits.shape[-1])
+        t = y = None
+        if teacher is not None or ids is not None:
+            if teacher is None or ids is None or teacher.shape != ids.shape or teacher.shape[:-1] != lead:
+                raise ValueError(f"ids and teacher both have shape {(*lead, 'top')}")
+            top = teacher.shape[-1]
+            at, d.teacher.id_bits = self._ids(ids, n * top, "ids")
+            if not self._gpu(teacher, "teacher").is_contiguous():
+                with self._on_stream():
+                    teacher = teacher.contiguous()
+            d.teacher.ids, d.teacher.logits, d.teacher.top = at.data_ptr(), teacher.data_ptr(), top
+            d.teacher.type = _type_of(teacher.dtype)
+            keep.append((at, teacher))
+            t = d.teacher_ref
+        if labels is not None:
+            if labels.shape != lead:
+                raise ValueError(f"labels must have shape {tuple(lead)}, not {tuple(labels.shape)}")
+            at, d.labels.id_bits = self._ids(labels, n, "labels")
+            d.labels.ids = at.data_ptr()
+            if pad is None or not -2 ** 63 <= pad < 2 ** 63:
+                d.labels.has_pad = 0
+            else:
+                d.labels.has_pad, d.labels.pad = 1, pad
+            keep.append(at)
+            y = d.labels_ref
+        if weights is not None and (self._gpu(weights, "weights", torch.float32).numel() != n
+                                    or not weights.is_contiguous()):
+            raise ValueError("weights holds one element for every row, without gaps")
+        if loss is None:
+            with self._on_stream():
+                loss = torch.empty(lead, dtype=torch.float32, device=self._device)
+        elif self._gpu(loss, "loss", torch.float32).numel() != n or not loss.is_contiguous():
+            raise ValueError("loss holds one element for every row, without gaps")
+        self._check(self._lib.adapm_distill(self._h, d.shape_ref, d.rows_ref[0], t, temperature, soft, y, hard, scale,
+                                            None if weights is None else weights.data_ptr(),
+                                            None if grad is None else d.rows_ref[1], loss.data_ptr()))
+        del keep
+        return loss
 
     # -- inspection ------------------------------------------------------------
     def clock(self, worker):

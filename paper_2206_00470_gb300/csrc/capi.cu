@@ -22,6 +22,7 @@
 
 #include "adapm.h"
 #include "blocks.h"
+#include "dense.cuh"
 #include "embed.cuh"
 #include "internal.cuh"
 #include "store_launch.cuh"
@@ -1003,6 +1004,60 @@ adapm_status check_tensors(adapm_ctx* ctx, const adapm_tensor* t, uint64_t n, co
   return ADAPM_OK;
 }
 
+// ---- dense layers --------------------------------------------------------------
+// Arrays of a shape's rows: their pointers, types, strides and places.
+adapm_status check_shape(adapm_ctx* ctx, const adapm_shape* s, uint64_t* n) {
+  if (!s) return fail(ctx, ADAPM_EINVAL, "null shape");
+  if (s->dim == 0 || s->dim > kMaxN) return fail(ctx, ADAPM_EINVAL, "dim %u: need 1 .. 2^31", s->dim);
+  if (s->outer > kMaxN || s->inner > kMaxN || s->outer * s->inner > kMaxN)
+    return fail(ctx, ADAPM_EINVAL, "more than 2^31 rows");
+  *n = s->outer * s->inner;
+  return ADAPM_OK;
+}
+
+adapm_status check_array(adapm_ctx* ctx, DevicePointers& device, const void* p, size_t align, const char* what) {
+  if (!p) return fail(ctx, ADAPM_EINVAL, "null %s", what);
+  if (reinterpret_cast<uintptr_t>(p) % align != 0) return fail(ctx, ADAPM_EINVAL, "%s is not aligned to its type", what);
+  if (!device.has(p)) return fail(ctx, ADAPM_EINVAL, "%s is not a device array", what);
+  return ADAPM_OK;
+}
+
+adapm_status check_rows(adapm_ctx* ctx, DevicePointers& device, const adapm_rows* r, uint64_t n, const char* what) {
+  if (!r) return fail(ctx, ADAPM_EINVAL, "null %s", what);
+  if (!float_type(r->type)) return fail(ctx, ADAPM_EINVAL, "%s: unknown element type %d", what, r->type);
+  return n == 0 ? ADAPM_OK : check_array(ctx, device, r->data, type_bytes(r->type), what);
+}
+
+// (a vector may be left out: null)
+adapm_status check_vector(adapm_ctx* ctx, DevicePointers& device, const adapm_vector* v, const char* what) {
+  if (!v) return ADAPM_OK;
+  if (!float_type(v->type)) return fail(ctx, ADAPM_EINVAL, "%s: unknown element type %d", what, v->type);
+  return check_array(ctx, device, v->data, type_bytes(v->type), what);
+}
+
+// The shape's rows as the rows of as many tokens.
+adapm_tokens tokens_of(const adapm_shape* s) {
+  adapm_tokens t{};
+  t.outer = s->outer;
+  t.inner = s->inner;
+  return t;
+}
+
+// Rows that are written: apart from each other, and another array's own
+// memory only as that array is laid out.
+adapm_status check_written(adapm_ctx* ctx, const adapm_shape* s, const adapm_rows* r, const adapm_rows* in, const char* what) {
+  const adapm_tokens t = tokens_of(s);
+  if (!rows_apart(&t, r, s->dim)) return fail(ctx, ADAPM_EINVAL, "rows of %s overlap", what);
+  if (r->data == in->data && (r->type != in->type || (s->outer > 1 && r->outer_stride != in->outer_stride) ||
+                              (s->inner > 1 && r->inner_stride != in->inner_stride)))
+    return fail(ctx, ADAPM_EINVAL, "%s is an input's memory in another type or layout", what);
+  return ADAPM_OK;
+}
+
+VectorView vector_view(const adapm_vector* v) {
+  return v ? VectorView{static_cast<char*>(v->data), v->type} : VectorView{nullptr, ADAPM_F32};
+}
+
 GradTensor grad_tensor(const adapm_tensor& t) {
   GradTensor g{};
   g.in = static_cast<const char*>(t.data);
@@ -1920,6 +1975,147 @@ adapm_status adapm_push_grads(adapm_ctx* ctx, uint32_t worker, const uint32_t* k
   pool_free(ctx, ik.owned);
   pool_free(ctx, ir.owned);
   return check_launch(ctx, "push_grads");
+}
+
+adapm_status adapm_layer_norm(adapm_ctx* ctx, const adapm_shape* shape, const adapm_rows* x, const adapm_vector* weight,
+                              const adapm_vector* bias, float eps, const adapm_rows* out, float* stats) {
+  adapm_status st = check_ctx(ctx);
+  if (st != ADAPM_OK) return st;
+  DevicePointers device;
+  uint64_t n = 0;
+  st = check_shape(ctx, shape, &n);
+  if (st == ADAPM_OK) st = check_rows(ctx, device, x, n, "x");
+  if (st == ADAPM_OK) st = check_rows(ctx, device, out, n, "out");
+  if (st == ADAPM_OK) st = check_vector(ctx, device, weight, "weight");
+  if (st == ADAPM_OK) st = check_vector(ctx, device, bias, "bias");
+  if (st == ADAPM_OK && stats && n > 0) st = check_array(ctx, device, stats, 2 * sizeof(float), "stats");
+  if (st != ADAPM_OK) return st;
+  if (!(eps >= 0.f)) return fail(ctx, ADAPM_EINVAL, "eps must not be negative");
+  if (n == 0) return ADAPM_OK;
+  st = check_written(ctx, shape, out, x, "out");
+  if (st != ADAPM_OK) return st;
+  const adapm_tokens t = tokens_of(shape);
+  NormArgs a{};
+  a.n = n;
+  a.dim = shape->dim;
+  a.x = row_view(&t, x, x->data);
+  a.out = row_view(&t, out, out->data);
+  a.weight = vector_view(weight);
+  a.bias = vector_view(bias);
+  a.eps = eps;
+  a.stats = stats;
+  ProfScope ps(ctx, 5);
+  launch_layer_norm(a, ctx->sms, ctx->stream);
+  return check_launch(ctx, "layer_norm");
+}
+
+adapm_status adapm_layer_norm_grad(adapm_ctx* ctx, const adapm_shape* shape, const adapm_rows* x, const adapm_rows* grad,
+                                   const float* stats, const adapm_vector* weight, const adapm_rows* dx,
+                                   const adapm_vector* dweight, const adapm_vector* dbias) {
+  adapm_status st = check_ctx(ctx);
+  if (st != ADAPM_OK) return st;
+  DevicePointers device;
+  uint64_t n = 0;
+  st = check_shape(ctx, shape, &n);
+  if (st == ADAPM_OK) st = check_rows(ctx, device, x, n, "x");
+  if (st == ADAPM_OK) st = check_rows(ctx, device, grad, n, "grad");
+  if (st == ADAPM_OK && dx) st = check_rows(ctx, device, dx, n, "dx");
+  if (st == ADAPM_OK) st = check_vector(ctx, device, weight, "weight");
+  if (st == ADAPM_OK) st = check_vector(ctx, device, dweight, "dweight");
+  if (st == ADAPM_OK) st = check_vector(ctx, device, dbias, "dbias");
+  if (st == ADAPM_OK && n > 0) st = check_array(ctx, device, stats, 2 * sizeof(float), "stats");
+  if (st == ADAPM_OK && n > 0 && dx) st = check_written(ctx, shape, dx, x, "dx");
+  if (st == ADAPM_OK && n > 0 && dx) st = check_written(ctx, shape, dx, grad, "dx");
+  if (st != ADAPM_OK) return st;
+  ProfScope ps(ctx, 5);
+  if (n == 0) {
+    for (const adapm_vector* v : {dweight, dbias})
+      if (v) CK(cudaMemsetAsync(v->data, 0, (size_t)shape->dim * type_bytes(v->type), ctx->stream));
+    return check_launch(ctx, "layer_norm_grad");
+  }
+  if (!dx && !dweight && !dbias) return ADAPM_OK;
+  const adapm_tokens t = tokens_of(shape);
+  NormArgs a{};
+  a.n = n;
+  a.dim = shape->dim;
+  a.x = row_view(&t, x, x->data);
+  a.grad = row_view(&t, grad, grad->data);
+  if (dx) a.out = row_view(&t, dx, dx->data);
+  a.weight = vector_view(weight);
+  a.dweight = vector_view(dweight);
+  a.dbias = vector_view(dbias);
+  a.stats = const_cast<float*>(stats);
+  const size_t floats = norm_grad_scratch(a, ctx->sms);
+  if (floats > 0) CK(pool_alloc(ctx, &a.parts, floats));
+  launch_layer_norm_grad(a, ctx->sms, ctx->stream);
+  pool_free(ctx, a.parts);
+  return check_launch(ctx, "layer_norm_grad");
+}
+
+adapm_status adapm_distill(adapm_ctx* ctx, const adapm_shape* shape, const adapm_rows* logits, const adapm_teacher* teacher,
+                           float temperature, float soft, const adapm_labels* labels, float hard, float scale,
+                           const float* weights, const adapm_rows* grad, float* loss) {
+  adapm_status st = check_ctx(ctx);
+  if (st != ADAPM_OK) return st;
+  DevicePointers device;
+  uint64_t n = 0;
+  st = check_shape(ctx, shape, &n);
+  if (st == ADAPM_OK) st = check_rows(ctx, device, logits, n, "logits");
+  if (st == ADAPM_OK && grad) st = check_rows(ctx, device, grad, n, "grad");
+  if (st != ADAPM_OK) return st;
+  if (!(temperature > 0.f) || !std::isfinite(temperature))
+    return fail(ctx, ADAPM_EINVAL, "the temperature is a positive number, not %g", (double)temperature);
+  if (!std::isfinite(soft) || !std::isfinite(hard)) return fail(ctx, ADAPM_EINVAL, "soft or hard is not a number");
+  if (grad && grad->type != logits->type) return fail(ctx, ADAPM_EINVAL, "grad has another type than the logits");
+  if (teacher) {
+    if (teacher->id_bits != 32 && teacher->id_bits != 64)
+      return fail(ctx, ADAPM_EINVAL, "ids have 32 or 64 bits, not %d", teacher->id_bits);
+    if (!float_type(teacher->type)) return fail(ctx, ADAPM_EINVAL, "teacher: unknown element type %d", teacher->type);
+    if (teacher->top > kMaxTop) return fail(ctx, ADAPM_EINVAL, "%u entries a row: at most %u", teacher->top, kMaxTop);
+    if (n > 0 && teacher->top > 0) st = check_array(ctx, device, teacher->ids, teacher->id_bits / 8, "the teacher's ids");
+    if (st == ADAPM_OK && n > 0 && teacher->top > 0)
+      st = check_array(ctx, device, teacher->logits, type_bytes(teacher->type), "the teacher's logits");
+  }
+  if (st == ADAPM_OK && labels) {
+    if (labels->id_bits != 32 && labels->id_bits != 64)
+      return fail(ctx, ADAPM_EINVAL, "labels have 32 or 64 bits, not %d", labels->id_bits);
+    if (n > 0) st = check_array(ctx, device, labels->ids, labels->id_bits / 8, "labels");
+  }
+  if (st == ADAPM_OK && n > 0 && weights) st = check_array(ctx, device, weights, sizeof(float), "weights");
+  if (st == ADAPM_OK && n > 0) st = check_array(ctx, device, loss, sizeof(float), "loss");
+  if (st != ADAPM_OK) return st;
+  if (n == 0) return ADAPM_OK;
+  if (grad) st = check_written(ctx, shape, grad, logits, "grad");
+  if (st != ADAPM_OK) return st;
+  const adapm_tokens t = tokens_of(shape);
+  DistillArgs a{};
+  a.n = n;
+  a.vocab = shape->dim;
+  a.logits = row_view(&t, logits, logits->data);
+  if (grad) a.grad = row_view(&t, grad, grad->data);
+  if (teacher && soft != 0.f) {
+    a.ids = teacher->ids;
+    a.teacher = teacher->logits;
+    a.wide = teacher->id_bits == 64;
+    a.top = teacher->top;
+    a.teacher_type = teacher->type;
+  }
+  if (labels && hard != 0.f) {
+    a.labels = labels->ids;
+    a.wide_labels = labels->id_bits == 64;
+    a.has_pad = labels->has_pad != 0 && (a.wide_labels || (labels->pad >= INT32_MIN && labels->pad <= (int64_t)UINT32_MAX));
+    a.pad = a.wide_labels ? labels->pad : (int64_t)(int32_t)(uint32_t)labels->pad;
+  }
+  a.temperature = temperature;
+  a.soft = soft;
+  a.hard = hard;
+  a.scale = scale;
+  a.weights = weights;
+  a.loss = loss;
+  a.st = ctx->dstate;
+  ProfScope ps(ctx, 5);
+  launch_distill(a, ctx->sms, ctx->stream);
+  return check_launch(ctx, "distill");
 }
 
 adapm_status adapm_clock(adapm_ctx* ctx, uint32_t worker, int64_t* out) {
