@@ -408,7 +408,8 @@ adapm_status adapm_push_grads(adapm_ctx* ctx, uint32_t worker, const uint32_t* k
 
 /* ---- dense layers of a token model ----------------------------------------- */
 /* What such a model runs between adapm_embed and adapm_embed_grad: layer norm,
- * and the loss that distils a teacher's top logits, each with its gradient.
+ * matrix products with their epilogue, and the loss that distils a teacher's
+ * top logits, each with its gradient.
  * They neither read nor write the store and belong to no worker; they run on
  * the library stream like every call, and are recorded in a graph like one.
  * Arrays are device arrays, aligned to their elements (ADAPM_EINVAL
@@ -449,6 +450,55 @@ adapm_status adapm_layer_norm(adapm_ctx* ctx, const adapm_shape* shape, const ad
 adapm_status adapm_layer_norm_grad(adapm_ctx* ctx, const adapm_shape* shape, const adapm_rows* x,
                                    const adapm_rows* grad, const float* stats, const adapm_vector* weight,
                                    const adapm_rows* dx, const adapm_vector* dweight, const adapm_vector* dbias);
+
+/* Element (i, j) is at i * row_stride + j * col_stride of data. */
+typedef struct {
+  void* data;
+  int32_t type;
+  int64_t row_stride, col_stride;
+} adapm_matrix;
+
+/* A dense layer: `rows` inputs of `ins` elements, as many outputs of `outs`. */
+typedef struct {
+  uint64_t rows;
+  uint32_t ins, outs;
+} adapm_layer;
+
+/* Activations: none, max(z, 0), z Phi(z) with the normal distribution's Phi,
+ * the same with Phi(z) as 1/2 (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))),
+ * z / (1 + e^-z), tanh z. */
+#define ADAPM_ACTIVATION_NONE 0
+#define ADAPM_ACTIVATION_RELU 1
+#define ADAPM_ACTIVATION_GELU 2
+#define ADAPM_ACTIVATION_GELU_TANH 3
+#define ADAPM_ACTIVATION_SILU 4
+#define ADAPM_ACTIVATION_TANH 5
+
+/* z = x weight + bias, out = act(z) + residual.  x (rows x ins) and weight (ins
+ * x outs, so a weight that is stored by output has row_stride 1) are of one
+ * 16-bit type, with any strides that are not negative; bias (outs elements;
+ * NULL: zeros) has a type of its own; residual (NULL: zeros), out and pre are
+ * rows x outs with col_stride 1.  pre (NULL: not wanted) receives z in x's
+ * type, for the backward pass.  out is of x's type or fp32, residual has out's
+ * type and may be its memory.  Products are summed and all else is computed in
+ * fp32, each output is rounded once.  rows, ins and outs are at most 2^31, ins
+ * and outs not 0.  Operands whose rows (or columns) do not begin on 16 bytes
+ * are copied to scratch memory first. */
+adapm_status adapm_linear(adapm_ctx* ctx, const adapm_layer* shape, const adapm_matrix* x,
+                          const adapm_matrix* weight, const adapm_vector* bias, int32_t activation,
+                          const adapm_matrix* residual, const adapm_matrix* out, const adapm_matrix* pre);
+
+/* The gradient of adapm_linear for grad, that of out: with dz = grad act'(z), dx
+ * = dz weight^T, dweight = x^T dz, dbias = the sum over rows of dz (zeros
+ * without rows); the residual's gradient is grad.  pre is z as left there
+ * (NULL where the activation is ADAPM_ACTIVATION_NONE).  grad and pre have x's type;
+ * dz is rounded to it for the products, not for dbias.  relu'(0) is 0.  dx
+ * (rows x ins, col_stride 1) and dweight (ins x outs, one stride 1) are of x's
+ * type or fp32; they and dbias may be NULL (not wanted) and overlap nothing. */
+adapm_status adapm_linear_grad(adapm_ctx* ctx, const adapm_layer* shape, const adapm_matrix* x,
+                               const adapm_matrix* weight, const adapm_matrix* grad, const adapm_matrix* pre,
+                               int32_t activation, const adapm_matrix* dx, const adapm_matrix* dweight,
+                               const adapm_vector* dbias);
 
 /* A teacher's largest logits: `top` (id, logit) pairs per row, in any order,
  * without gaps (row (o, i) is pair list o * inner + i).  ids are signed, of 32

@@ -31,7 +31,7 @@ EXPORTS = [
     "adapm_profile_read", "adapm_kernel_launches", "adapm_push_noalloc", "adapm_last_error",
     "adapm_debug_fail_next_barrier", "adapm_debug_fail_next_launch",
     "adapm_embed", "adapm_embed_grad", "adapm_grad_norm", "adapm_clip_grads", "adapm_push_grads",
-    "adapm_layer_norm", "adapm_layer_norm_grad", "adapm_distill",
+    "adapm_layer_norm", "adapm_layer_norm_grad", "adapm_linear", "adapm_linear_grad", "adapm_distill",
 ]
 
 
@@ -106,6 +106,15 @@ class _Vector(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("type", ctypes.c_int32)]
 
 
+class _Matrix(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("type", ctypes.c_int32), ("row_stride", ctypes.c_int64),
+                ("col_stride", ctypes.c_int64)]
+
+
+class _Layer(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_uint64), ("ins", ctypes.c_uint32), ("outs", ctypes.c_uint32)]
+
+
 class _Teacher(ctypes.Structure):
     _fields_ = [("ids", ctypes.c_void_p), ("id_bits", ctypes.c_int32), ("logits", ctypes.c_void_p),
                 ("type", ctypes.c_int32), ("top", ctypes.c_uint32)]
@@ -168,6 +177,8 @@ def load(path=LIB_PATH):
         "adapm_push_grads": [P, U32, P, P, U64, U32, I, F, F, F, F, P],
         "adapm_layer_norm": [P, P, P, P, P, F, P, P],
         "adapm_layer_norm_grad": [P, P, P, P, P, P, P, P, P],
+        "adapm_linear": [P, P, P, P, P, ctypes.c_int32, P, P, P],
+        "adapm_linear_grad": [P, P, P, P, P, P, ctypes.c_int32, P, P, P],
         "adapm_distill": [P, P, P, P, F, F, P, F, F, P, P, P],
     }
     for name, args in sig.items():
@@ -349,18 +360,35 @@ class NormGrads(collections.namedtuple("NormGrads", ["x", "weight", "bias"])):
     __slots__ = ()
 
 
+class LinearGrads(collections.namedtuple("LinearGrads", ["x", "weight", "bias"])):
+    """Gradients of a dense layer's input, weight and bias (adapm_linear_grad); None where one is not wanted."""
+
+    __slots__ = ()
+
+
+ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4, "tanh": 5}
+
+
+def _activation(name):
+    if name not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {sorted(a for a in ACTIVATIONS if a)}")
+    return ACTIVATIONS[name]
+
+
 class _Dense:
     """Descriptors that the calls on dense layers refill (making one anew takes longer than filling it)."""
 
-    __slots__ = ("shape", "rows", "vectors", "teacher", "labels", "shape_ref", "rows_ref", "vectors_ref",
-                 "teacher_ref", "labels_ref")
+    __slots__ = ("shape", "layer", "rows", "matrices", "vectors", "teacher", "labels", "shape_ref", "layer_ref",
+                 "rows_ref", "matrices_ref", "vectors_ref", "teacher_ref", "labels_ref")
 
     def __init__(self):
-        self.shape, self.teacher, self.labels = _Shape(), _Teacher(), _Labels()
+        self.shape, self.layer, self.teacher, self.labels = _Shape(), _Layer(), _Teacher(), _Labels()
         self.rows, self.vectors = [_Rows() for _ in range(3)], [_Vector() for _ in range(3)]
-        for name in ("shape", "teacher", "labels"):
+        self.matrices = [_Matrix() for _ in range(6)]
+        for name in ("shape", "layer", "teacher", "labels"):
             setattr(self, name + "_ref", ctypes.byref(getattr(self, name)))
-        self.rows_ref, self.vectors_ref = [ctypes.byref(r) for r in self.rows], [ctypes.byref(v) for v in self.vectors]
+        for name in ("rows", "vectors", "matrices"):
+            setattr(self, name + "_ref", [ctypes.byref(a) for a in getattr(self, name)])
 
 
 def poisson_quantile(lam, p):
@@ -763,6 +791,80 @@ class ParameterManager:
         self._check(self._lib.adapm_layer_norm_grad(self._h, d.shape_ref, d.rows_ref[0], d.rows_ref[1], stats.data_ptr(),
                                                     w, None if out.x is None else d.rows_ref[2], dw, db))
         del keep
+        return out
+
+    def _matrix(self, i, t, shape, what, written=False):
+        """The descriptor of (..., columns) as rows of columns, of which there are shape[0]; an input whose rows are
+        not one step apart is copied.  Returns the descriptor and the tensor that it describes."""
+        if t is None:
+            return None, None
+        rows, columns = shape
+        self._gpu(t, what)
+        if t.shape[-1:] != (columns,) or t.numel() != rows * columns:
+            raise ValueError(f"{what} must be (..., {columns}) with {rows} rows, not {tuple(t.shape)}")
+        step = columns if t.is_contiguous() else (t.stride(0) if t.dim() == 2
+                                                  else _one_stride(t.shape[:-1], t.stride()[:-1]))
+        if step is None:
+            if written:
+                raise ValueError(f"rows of {what} are not one step apart")
+            with self._on_stream():
+                t = t.contiguous()
+            step = columns
+        m = self._d.matrices[i]
+        m.data, m.type, m.row_stride, m.col_stride = t.data_ptr(), _type_of(t.dtype), step, t.stride(-1)
+        return self._d.matrices_ref[i], t
+
+    def _layer(self, x, weight):
+        if weight.dim() != 2 or x.dim() < 1 or x.shape[-1] != weight.shape[0]:
+            raise ValueError(f"x (..., ins) and weight (ins, outs) do not fit: {tuple(x.shape)}, {tuple(weight.shape)}")
+        layer = self._d.layer
+        layer.ins, layer.outs = weight.shape
+        layer.rows = n = x.numel() // max(1, layer.ins)
+        return n, layer.ins, layer.outs
+
+    def linear(self, x, weight, bias=None, activation=None, residual=None, out=None, dtype=None, pre=None):
+        """activation(x weight + bias) + residual for x (..., ins) and weight (ins, outs), both float16 or bfloat16,
+        as (..., outs) in dtype (x's unless given, or out's; or float32).  A weight stored by output is passed as its
+        .t().  activation: "relu", "gelu", "gelu_tanh", "silu", "tanh" or None.  pre (x's dtype): receives
+        x weight + bias, which linear_grad needs with an activation.  out may be the residual."""
+        torch, d = _torch(), self._d
+        n, ins, outs = self._layer(x, weight)
+        if out is None:
+            with self._on_stream():
+                out = torch.empty((*x.shape[:-1], outs), dtype=dtype or x.dtype, device=self._device)
+        elif dtype is not None and out.dtype != dtype:
+            raise ValueError("out has another dtype")
+        xm, x = self._matrix(0, x, (n, ins), "x")
+        wm, weight = self._matrix(1, weight, (ins, outs), "weight")
+        rm, residual = self._matrix(2, residual, (n, outs), "residual")
+        om, out = self._matrix(3, out, (n, outs), "out", True)
+        pm, pre = self._matrix(4, pre, (n, outs), "pre", True)
+        b = self._dense_vector(0, bias, outs, "bias")
+        self._check(self._lib.adapm_linear(self._h, d.layer_ref, xm, wm, b, _activation(activation), rm, om, pm))
+        return out
+
+    def linear_grad(self, x, weight, grad, pre=None, activation=None, bias=None, out=None):
+        """LinearGrads of linear(x, weight, ..., pre=pre) for grad, the gradient of its output (that of the residual is
+        grad itself): of x and weight in their dtype, the weight's stored as the weight is, and of the bias (bias=True,
+        and by default) in the weight's.  out: LinearGrads to fill, None for those not wanted."""
+        torch, d = _torch(), self._d
+        n, ins, outs = self._layer(x, weight)
+        kind = _activation(activation)
+        if kind and pre is None:
+            raise ValueError("an activation's gradient needs pre, what linear left there")
+        if out is None:
+            with self._on_stream():
+                out = LinearGrads(torch.empty(x.shape, dtype=x.dtype, device=self._device),
+                                  torch.empty_like(weight),
+                                  torch.empty(outs, dtype=weight.dtype, device=self._device) if bias in (None, True) else None)
+        xm, x = self._matrix(0, x, (n, ins), "x")
+        wm, weight = self._matrix(1, weight, (ins, outs), "weight")
+        gm, grad = self._matrix(2, grad, (n, outs), "grad")
+        pm, pre = self._matrix(3, pre if kind else None, (n, outs), "pre")
+        dx, _ = self._matrix(4, out.x, (n, ins), "out.x", True)
+        dw, _ = self._matrix(5, out.weight, (ins, outs), "out.weight", True)
+        db = self._dense_vector(0, out.bias, outs, "out.bias")
+        self._check(self._lib.adapm_linear_grad(self._h, d.layer_ref, xm, wm, gm, pm, kind, dx, dw, db))
         return out
 
     def _ids(self, t, count, what):

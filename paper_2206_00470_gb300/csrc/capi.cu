@@ -1054,6 +1054,43 @@ adapm_status check_written(adapm_ctx* ctx, const adapm_shape* s, const adapm_row
   return ADAPM_OK;
 }
 
+// A matrix of rows x columns; one that is written has its elements apart, along one stride of 1.
+adapm_status check_matrix(adapm_ctx* ctx, DevicePointers& device, const adapm_matrix* m, uint64_t rows, uint64_t columns,
+                          const char* what) {
+  if (!m) return fail(ctx, ADAPM_EINVAL, "null %s", what);
+  if (!float_type(m->type)) return fail(ctx, ADAPM_EINVAL, "%s: unknown element type %d", what, m->type);
+  if ((rows > 1 && m->row_stride < 0) || (columns > 1 && m->col_stride < 0))
+    return fail(ctx, ADAPM_EINVAL, "%s has negative strides", what);
+  return rows == 0 ? ADAPM_OK : check_array(ctx, device, m->data, type_bytes(m->type), what);
+}
+adapm_status check_written_matrix(adapm_ctx* ctx, const adapm_matrix* m, uint64_t rows, uint64_t columns, bool either,
+                                  const char* what) {
+  const bool by_row = (columns <= 1 || m->col_stride == 1) && (rows <= 1 || m->row_stride >= (int64_t)columns);
+  const bool by_col = (rows <= 1 || m->row_stride == 1) && (columns <= 1 || m->col_stride >= (int64_t)rows);
+  if (by_row || (either && by_col)) return ADAPM_OK;
+  return fail(ctx, ADAPM_EINVAL, "%s: need rows%s of neighbouring elements that do not overlap", what, either ? " or columns" : "");
+}
+
+// What both calls on a dense layer check.
+adapm_status check_layer(adapm_ctx* ctx, DevicePointers& device, const adapm_layer* s, const adapm_matrix* x,
+                         const adapm_matrix* weight, int32_t activation) {
+  if (!s) return fail(ctx, ADAPM_EINVAL, "null shape");
+  if (s->rows > kMaxN || s->ins == 0 || s->ins > kMaxN || s->outs == 0 || s->outs > kMaxN)
+    return fail(ctx, ADAPM_EINVAL, "rows, ins and outs: at most 2^31, ins and outs not 0");
+  if (activation < ADAPM_ACTIVATION_NONE || activation > ADAPM_ACTIVATION_TANH)
+    return fail(ctx, ADAPM_EINVAL, "unknown activation %d", activation);
+  adapm_status st = check_matrix(ctx, device, x, s->rows, s->ins, "x");
+  if (st == ADAPM_OK) st = check_matrix(ctx, device, weight, s->ins, s->outs, "weight");
+  if (st != ADAPM_OK) return st;
+  if (x->type == ADAPM_F32 || weight->type != x->type)
+    return fail(ctx, ADAPM_EINVAL, "x and weight are of one 16-bit type");
+  return ADAPM_OK;
+}
+
+MatrixView matrix_view(const adapm_matrix* m) {
+  return m ? MatrixView{static_cast<char*>(m->data), m->type, m->row_stride, m->col_stride} : MatrixView{nullptr, ADAPM_F32, 0, 0};
+}
+
 VectorView vector_view(const adapm_vector* v) {
   return v ? VectorView{static_cast<char*>(v->data), v->type} : VectorView{nullptr, ADAPM_F32};
 }
@@ -2050,6 +2087,109 @@ adapm_status adapm_layer_norm_grad(adapm_ctx* ctx, const adapm_shape* shape, con
   launch_layer_norm_grad(a, ctx->sms, ctx->stream);
   pool_free(ctx, a.parts);
   return check_launch(ctx, "layer_norm_grad");
+}
+
+adapm_status adapm_linear(adapm_ctx* ctx, const adapm_layer* shape, const adapm_matrix* x, const adapm_matrix* weight,
+                          const adapm_vector* bias, int32_t activation, const adapm_matrix* residual,
+                          const adapm_matrix* out, const adapm_matrix* pre) {
+  adapm_status st = check_ctx(ctx);
+  if (st != ADAPM_OK) return st;
+  DevicePointers device;
+  st = check_layer(ctx, device, shape, x, weight, activation);
+  if (st != ADAPM_OK) return st;
+  const uint64_t n = shape->rows;
+  st = check_matrix(ctx, device, out, n, shape->outs, "out");
+  if (st == ADAPM_OK) st = check_written_matrix(ctx, out, n, shape->outs, false, "out");
+  if (st == ADAPM_OK && pre) st = check_matrix(ctx, device, pre, n, shape->outs, "pre");
+  if (st == ADAPM_OK && pre) st = check_written_matrix(ctx, pre, n, shape->outs, false, "pre");
+  if (st == ADAPM_OK && residual) st = check_matrix(ctx, device, residual, n, shape->outs, "residual");
+  if (st == ADAPM_OK) st = check_vector(ctx, device, bias, "bias");
+  if (st != ADAPM_OK) return st;
+  if (out->type != x->type && out->type != ADAPM_F32) return fail(ctx, ADAPM_EINVAL, "out is of x's type or fp32");
+  if (pre && pre->type != x->type) return fail(ctx, ADAPM_EINVAL, "pre is of x's type");
+  if (residual && (residual->type != out->type || (shape->outs > 1 && residual->col_stride != 1)))
+    return fail(ctx, ADAPM_EINVAL, "residual is of out's type, elements of a row next to each other");
+  if (residual && n > 1 && residual->data == out->data && residual->row_stride != out->row_stride)
+    return fail(ctx, ADAPM_EINVAL, "out is the residual's memory in another layout");
+  if (n > 0 && (out->data == x->data || out->data == weight->data || (pre && (pre->data == out->data || pre->data == x->data))))
+    return fail(ctx, ADAPM_EINVAL, "out or pre is the memory of another array");
+  if (n == 0) return ADAPM_OK;
+  LinearArgs a{};
+  a.rows = n;
+  a.ins = shape->ins;
+  a.outs = shape->outs;
+  a.x = matrix_view(x);
+  a.weight = matrix_view(weight);
+  a.bias = vector_view(bias);
+  a.residual = matrix_view(residual);
+  a.out = matrix_view(out);
+  a.pre = matrix_view(pre);
+  a.activation = activation;
+  a.st = ctx->dstate;
+  ProfScope ps(ctx, 5);
+  char* scratch = nullptr;
+  const size_t bytes = linear_scratch(a, ctx->sms);
+  if (bytes > 0) CK(pool_alloc(ctx, &scratch, bytes));
+  CK(launch_linear(a, scratch, ctx->sms, ctx->stream));
+  pool_free(ctx, scratch);
+  return check_launch(ctx, "linear");
+}
+
+adapm_status adapm_linear_grad(adapm_ctx* ctx, const adapm_layer* shape, const adapm_matrix* x, const adapm_matrix* weight,
+                               const adapm_matrix* grad, const adapm_matrix* pre, int32_t activation,
+                               const adapm_matrix* dx, const adapm_matrix* dweight, const adapm_vector* dbias) {
+  adapm_status st = check_ctx(ctx);
+  if (st != ADAPM_OK) return st;
+  DevicePointers device;
+  st = check_layer(ctx, device, shape, x, weight, activation);
+  if (st != ADAPM_OK) return st;
+  const uint64_t n = shape->rows;
+  st = check_matrix(ctx, device, grad, n, shape->outs, "grad");
+  if (st == ADAPM_OK && activation != ADAPM_ACTIVATION_NONE) st = check_matrix(ctx, device, pre, n, shape->outs, "pre");
+  if (st == ADAPM_OK && dx) st = check_matrix(ctx, device, dx, n, shape->ins, "dx");
+  if (st == ADAPM_OK && dx) st = check_written_matrix(ctx, dx, n, shape->ins, false, "dx");
+  if (st == ADAPM_OK && dweight) st = check_matrix(ctx, device, dweight, shape->ins, shape->outs, "dweight");
+  if (st == ADAPM_OK && dweight) st = check_written_matrix(ctx, dweight, shape->ins, shape->outs, true, "dweight");
+  if (st == ADAPM_OK) st = check_vector(ctx, device, dbias, "dbias");
+  if (st != ADAPM_OK) return st;
+  if (grad->type != x->type || (activation != ADAPM_ACTIVATION_NONE && pre->type != x->type))
+    return fail(ctx, ADAPM_EINVAL, "grad and pre are of x's type");
+  for (const adapm_matrix* m : {dx, dweight})
+    if (m && m->type != x->type && m->type != ADAPM_F32) return fail(ctx, ADAPM_EINVAL, "dx and dweight are of x's type or fp32");
+  if (n > 0 && dx && (dx->data == x->data || dx->data == grad->data || (dweight && dx->data == dweight->data)))
+    return fail(ctx, ADAPM_EINVAL, "dx is the memory of another array");
+  if (dweight && dweight->data == weight->data) return fail(ctx, ADAPM_EINVAL, "dweight is the memory of weight");
+  ProfScope ps(ctx, 5);
+  if (n == 0) {
+    if (dweight) {
+      const bool by_row = shape->outs <= 1 || dweight->col_stride == 1;
+      const size_t size = type_bytes(dweight->type);
+      const size_t lines = by_row ? shape->ins : shape->outs, width = (by_row ? shape->outs : shape->ins) * size;
+      const size_t pitch = lines <= 1 ? width : (size_t)(by_row ? dweight->row_stride : dweight->col_stride) * size;
+      CK(cudaMemset2DAsync(dweight->data, pitch, 0, width, lines, ctx->stream));
+    }
+    if (dbias) CK(cudaMemsetAsync(dbias->data, 0, (size_t)shape->outs * type_bytes(dbias->type), ctx->stream));
+    return check_launch(ctx, "linear_grad");
+  }
+  LinearArgs a{};
+  a.rows = n;
+  a.ins = shape->ins;
+  a.outs = shape->outs;
+  a.x = matrix_view(x);
+  a.weight = matrix_view(weight);
+  a.grad = matrix_view(grad);
+  if (activation != ADAPM_ACTIVATION_NONE) a.pre = matrix_view(pre);
+  a.activation = activation;
+  a.dx = matrix_view(dx);
+  a.dweight = matrix_view(dweight);
+  a.dbias = vector_view(dbias);
+  a.st = ctx->dstate;
+  char* scratch = nullptr;
+  const size_t bytes = linear_grad_scratch(a, ctx->sms);
+  if (bytes > 0) CK(pool_alloc(ctx, &scratch, bytes));
+  CK(launch_linear_grad(a, scratch, ctx->sms, ctx->stream));
+  pool_free(ctx, scratch);
+  return check_launch(ctx, "linear_grad");
 }
 
 adapm_status adapm_distill(adapm_ctx* ctx, const adapm_shape* shape, const adapm_rows* logits, const adapm_teacher* teacher,

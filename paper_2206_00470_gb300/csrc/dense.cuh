@@ -63,6 +63,32 @@ inline void launch_distill(const DistillArgs& a, int sms, cudaStream_t stream) {
   else launch_distill_bf16(a, sms, stream);
 }
 
+// ---- matrix products (linear.cu) ----------------------------------------------------
+// Element (i, j) is at i * row_stride + j * col_stride.
+struct MatrixView {
+  char* data;
+  int type;
+  int64_t row_stride, col_stride;
+};
+struct LinearArgs {
+  uint64_t rows;
+  uint32_t ins, outs;
+  MatrixView x, weight;      // rows x ins, ins x outs, of one 16-bit type
+  VectorView bias;           // null data: none
+  MatrixView residual, out, pre;   // rows x outs, col_stride 1; null data: none
+  int activation;            // ADAPM_ACTIVATION_*
+  // backward: the gradient of out, and what is wanted of x, weight, bias
+  MatrixView grad, dx, dweight;
+  VectorView dbias;
+  DevState* st;
+};
+// Bytes of scratch; the launches take a pointer to that many (aligned to 256),
+// and return a CUDA error of their host side.
+size_t linear_scratch(const LinearArgs& a, int sms);
+cudaError_t launch_linear(const LinearArgs& a, char* scratch, int sms, cudaStream_t stream);
+size_t linear_grad_scratch(const LinearArgs& a, int sms);
+cudaError_t launch_linear_grad(const LinearArgs& a, char* scratch, int sms, cudaStream_t stream);
+
 #ifdef __CUDACC__
 namespace {
 

@@ -1,0 +1,151 @@
+// A product of two matrices of a 16-bit type on the tensor cores, for
+// linear.cu: what its kernel is given, and the pieces of it that speak to the
+// hardware.
+#pragma once
+
+#include <cuda.h>
+
+#include "dense.cuh"
+
+namespace adapm {
+
+// What becomes of element (r, c) of a product: z = sum + bias[c]; pre = z;
+// out = act(z) + residual.
+struct Epilogue {
+  VectorView bias;
+  MatrixView residual, out, pre;
+  int activation;
+};
+
+// D[m][n] = sum over k of A[m][k] B[n][k], in tiles of 128 x bn, k in blocks of
+// 64 (128 bytes, the width of a swizzled row of shared memory).
+constexpr uint32_t kTileM = 128, kBlockK = 64;
+struct GemmArgs {
+  CUtensorMap a, b;
+  bool a_across, b_across;   // stored with m (n) contiguous instead of k
+  bool turned;               // D is the product's transpose: m counts its columns
+  uint32_t m, n;
+  uint32_t bn, stages;
+  uint32_t tiles_m, tiles_n;
+  uint32_t k_blocks, splits, per_split;   // blocks of k: all, parts they are summed in, of one part
+  bool bf16;
+  float* parts;              // splits > 1: the parts' sums, each laid out like the product without gaps
+  Epilogue e;
+  DevState* st;
+};
+
+#ifdef __CUDACC__
+namespace {
+
+__device__ __forceinline__ uint32_t shared_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void barrier_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void barrier_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile(
+      "{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+      : "=r"(done)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return done != 0;
+}
+__device__ __forceinline__ uint64_t now_ns() {
+  uint64_t t;
+  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+  return t;
+}
+// Waits for a phase of a barrier, two seconds at most; false: it gave up.
+__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity) {
+  if (barrier_try(bar, parity)) return true;
+  const uint64_t start = now_ns();
+  for (uint32_t i = 1;; ++i) {
+    if (barrier_try(bar, parity)) return true;
+    if ((i & 63u) == 0u && now_ns() - start > 2000000000ull) return false;
+  }
+}
+
+__device__ __forceinline__ void copy_tile(uint32_t to, const CUtensorMap* map, int x, int y, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(to),
+      "l"(map), "r"(x), "r"(y), "r"(bar)
+      : "memory");
+}
+
+// A tile in shared memory as the tensor cores see it: rows of 128 bytes,
+// swizzled, eight of them 1024 bytes.  Stored with k contiguous, groups of
+// eight rows follow each other; stored across, a row is 64 elements of m at
+// one k, groups of eight k follow each other, and the next 64 of m are a box
+// of kBlockK rows further on.
+__device__ __forceinline__ uint64_t tile_descriptor(uint32_t at, bool across) {
+  const uint64_t leading = across ? kBlockK * 128 : 16, stride = 1024;
+  return (uint64_t)((at & 0x3FFFFu) >> 4) | ((leading >> 4) << 16) | ((stride >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+// From one group of 16 k to the next, in units of the descriptor's address.
+__device__ __forceinline__ uint32_t tile_step(bool across) { return (across ? 16 * 128 : 16 * 2) >> 4; }
+
+__device__ __forceinline__ uint32_t mma_shape(bool bf16, bool a_across, bool b_across, uint32_t n) {
+  return (1u << 4) | ((bf16 ? 1u : 0u) << 7) | ((bf16 ? 1u : 0u) << 10) | ((a_across ? 1u : 0u) << 15) |
+         ((b_across ? 1u : 0u) << 16) | ((n >> 3) << 17) | ((kTileM >> 4) << 24);
+}
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, bool add) {
+  asm volatile(
+      "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a),
+      "l"(b), "r"(shape), "r"((uint32_t)add)
+      : "memory");
+}
+// The barrier is arrived at once all products issued before are done.
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+// Warp-wide: `columns` (a power of two, 32 to 512) of tensor memory.
+__device__ __forceinline__ void tmem_take(uint32_t* at, uint32_t columns) {
+  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(shared_at(at)), "r"(columns) : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+}
+__device__ __forceinline__ void tmem_give(uint32_t at, uint32_t columns) {
+  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns));
+}
+// Warp-wide: 32 (16) columns of the lane's row, waited for (in one statement:
+// nothing may use the registers before the wait).
+__device__ __forceinline__ void tmem_load(uint32_t at, float (&v)[32]) {
+  uint32_t r[32];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+        "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+        "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(at)
+      : "memory");
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_load16(uint32_t at, float (&v)[16]) {
+  uint32_t r[16];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(at)
+      : "memory");
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+}  // namespace
+#endif
+
+}  // namespace adapm
