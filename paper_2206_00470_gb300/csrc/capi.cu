@@ -2254,7 +2254,15 @@ adapm_status adapm_distill(adapm_ctx* ctx, const adapm_shape* shape, const adapm
   a.loss = loss;
   a.st = ctx->dstate;
   ProfScope ps(ctx, 5);
+  char *tasks = nullptr, *entries = nullptr;
+  CK(pool_alloc(ctx, &tasks, n * (kTaskBytes + kRowSumBytes)));
+  if (a.top > 0) CK(pool_alloc(ctx, &entries, n * a.top * kEntryBytes));
+  a.tasks = tasks;
+  a.sums = tasks + n * kTaskBytes;
+  a.entries = entries;
   launch_distill(a, ctx->sms, ctx->stream);
+  pool_free(ctx, tasks);
+  pool_free(ctx, entries);
   return check_launch(ctx, "distill");
 }
 

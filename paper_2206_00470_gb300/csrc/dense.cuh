@@ -51,8 +51,10 @@ struct DistillArgs {
   float temperature, soft, hard, scale;
   const float* weights;  // n factors of the gradient's rows, null: ones
   float* loss;           // n
+  void *tasks, *sums, *entries;   // scratch: n, n and n * top of them
   DevState* st;
 };
+constexpr size_t kTaskBytes = 16, kRowSumBytes = 12, kEntryBytes = 12;
 // The kernels of one type of logits (a translation unit each).
 void launch_distill_f32(const DistillArgs& a, int sms, cudaStream_t stream);
 void launch_distill_f16(const DistillArgs& a, int sms, cudaStream_t stream);
@@ -94,6 +96,20 @@ namespace {
 
 __device__ __forceinline__ float bf16_low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_high(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+// fn(type) for a type known when compiled, or (TYPE -1) for the one known at run
+// time: the branch stands outside of fn's loops, so that their loads go out together.
+template <int T>
+struct Type {
+  static constexpr int value = T;
+};
+template <int TYPE, class F>
+__device__ __forceinline__ void by_type(int type, F&& fn) {
+  if constexpr (TYPE >= 0) fn(Type<TYPE>());
+  else if (type == ADAPM_F32) fn(Type<ADAPM_F32>());
+  else if (type == ADAPM_BF16) fn(Type<ADAPM_BF16>());
+  else fn(Type<ADAPM_F16>());
+}
 
 // One element of a type known at run time.
 __device__ __forceinline__ float load_as(const char* p, int type, int64_t i) {

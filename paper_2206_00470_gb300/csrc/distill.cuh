@@ -1,5 +1,5 @@
 // Distillation from a teacher's top logits: the loss of every row of student
-// logits and its gradient, in one pass over them.
+// logits and its gradient.
 //
 // Row r has student logits s_v, a list of (id_j, t_j), and perhaps a label y:
 //
@@ -7,15 +7,17 @@
 //   loss = soft T^2 sum_j p_j (ln p_j - ln q_id_j) + hard (-ln c_y)
 //   grad_v = f (soft T (q_v - sum_{id_j = v} p_j) + hard (c_v - [v = y])),  f = scale weights[r]
 //
-// A row is read once and kept in registers, packed as it came: eight 16-byte
-// words a thread, 512 threads a block, and where that is too little the blocks
-// of a cluster take a slice of the row each and exchange their warps' maxima
-// and sums through shared memory.  Every warp sums relative to its own maximum,
-// so one exchange per row is enough.  The dense part of the gradient is
-// written from the registers; warp 0, which has read the list and the logits
-// at its ids meanwhile, then writes the few elements that the list and the
-// label change.
-// Bound by memory: a read and a write of the logits.
+// Three launches.  distill_lists, a warp per row: the list's p, one entry for
+// all that share an id, and the logits at its ids and at the label.
+// distill_rows: sums of exponentials of each row and the part of the gradient
+// that every element has, from one reading.  distill_marks, a warp per row:
+// the loss, and the few elements that list and label change.
+//
+// distill_rows keeps a row in registers, packed as it came: eight 16-byte
+// words a thread, and where a block is too small the blocks of a cluster take
+// a slice of the row each and exchange their warps' sums through shared
+// memory.  Every warp sums relative to its own maximum, so one exchange per row
+// is enough.  Bound by memory: a read and a write of the logits.
 #pragma once
 
 #include <cooperative_groups.h>
@@ -149,165 +151,313 @@ __device__ __forceinline__ uint4 pack_word(const float (&y)[Word<TYPE>::kElement
     return make_uint4(pack2<TYPE>(y[0], y[1]), pack2<TYPE>(y[2], y[3]), pack2<TYPE>(y[4], y[5]), pack2<TYPE>(y[6], y[7]));
 }
 
-// Maximum, and sums of exp((s - max) / T) and of exp(s - max), of some logits.
-struct Sums {
+// What distill_lists finds out about a row.
+struct RowTask {
+  float plogp;      // sum of p ln p over the list
+  float label_s;    // the label's logit
+  int32_t label;    // -1: none
+  int32_t some;     // whether the list has entries
+};
+// What distill_rows finds out: largest logit, and sums of exp((s - max) / T)
+// and (distill_two) of exp(s - max).
+struct RowSums {
   float max, t, one;
 };
-__device__ __forceinline__ float finite_shift(float m) { return m == -INFINITY ? 0.f : m; }
+// An entry: the p of all that share its id, and the id's logit.
+struct Entry {
+  uint32_t id;   // kNoKey: none, or another one speaks for it
+  float p, s;
+};
+
+static_assert(sizeof(RowTask) == kTaskBytes && sizeof(RowSums) == kRowSumBytes && sizeof(Entry) == kEntryBytes);
 
 __device__ __forceinline__ int64_t id_at(const void* ids, bool wide, uint64_t i) {
   return wide ? static_cast<const int64_t*>(ids)[i] : (int64_t)static_cast<const int32_t*>(ids)[i];
 }
+__device__ __forceinline__ float lanes_max(float x) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, o));
+  return x;
+}
+
+constexpr int kListWarps = 4;
+
+// Shared memory: for every warp the ids and the table of slots (`table`, a
+// power of two of at least twice as many) that finds those listed twice.
+template <int TYPE>
+__global__ void __launch_bounds__(kListWarps * 32)
+distill_lists_kernel(const __grid_constant__ DistillArgs a, uint32_t table) {
+  after_previous();
+  extern __shared__ uint32_t lists[];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint32_t* const l_id = lists + warp * (2 * a.top + table);
+  uint32_t* const l_slot = l_id + a.top;
+  uint32_t* const l_table = l_slot + a.top;
+  Entry* const entries = static_cast<Entry*>(a.entries);
+  for (uint64_t row = (uint64_t)blockIdx.x * kListWarps + warp; row < a.n; row += (uint64_t)gridDim.x * kListWarps) {
+    const char* const logits = a.logits.data + row_offset(a.logits, (uint32_t)row) * Word<TYPE>::kSize;
+    RowTask task{0.f, 0.f, -1, 0};
+    bool bad = false;
+    if (a.labels != nullptr) {
+      const int64_t y = id_at(a.labels, a.wide_labels, row);
+      if (!(a.has_pad && y == a.pad)) {
+        if (y >= 0 && y < (int64_t)a.vocab) task.label = (int32_t)y;
+        else bad = true;
+      }
+      if (task.label >= 0) task.label_s = load_as(logits, TYPE, task.label);
+    }
+    if (a.top > 0) {
+      for (uint32_t j = lane; j < table; j += 32) l_table[j] = kEmpty;
+      // T ln p_j = t_j - t_max - T ln(sum)
+      float largest = -INFINITY;
+      for (uint32_t j = lane; j < a.top; j += 32) {
+        const uint64_t at = row * a.top + j;
+        const int64_t id = id_at(a.ids, a.wide, at);
+        const float t = load_as(static_cast<const char*>(a.teacher), a.teacher_type, at);
+        const bool here = id >= 0 && id < (int64_t)a.vocab && t != -INFINITY;
+        bad = bad || id >= (int64_t)a.vocab || id < -1;
+        l_id[j] = here ? (uint32_t)id : kNoKey;
+        if (here) {
+          task.some = 1;
+          largest = fmaxf(largest, t);
+        }
+      }
+      __syncwarp();
+      largest = lanes_max(largest);
+      task.some = __any_sync(0xFFFFFFFFu, task.some);
+      const float per_t = kLog2E / a.temperature, inv_t = 1.f / a.temperature;
+      bool doubled = false;
+      float sum = 0.f;
+      for (uint32_t j = lane; j < a.top; j += 32) {
+        const uint32_t id = l_id[j];
+        if (id == kNoKey) continue;
+        sum += exp2_of((load_as(static_cast<const char*>(a.teacher), a.teacher_type, row * a.top + j) - largest) * per_t);
+        // the first entry of an id speaks for all (the table has twice as many slots as there are entries)
+        uint32_t h = (id * 2654435761u) & (table - 1);
+        while (true) {
+          const uint32_t old = atomicCAS(&l_table[h], kEmpty, j);
+          if (old == kEmpty) break;
+          if (l_id[old] == id) {
+            atomicMin(&l_table[h], j);
+            doubled = true;
+            break;
+          }
+          h = (h + 1) & (table - 1);
+        }
+        l_slot[j] = h;
+      }
+      __syncwarp();
+      doubled = __any_sync(0xFFFFFFFFu, doubled);
+      sum = lanes_sum(sum, 32);
+      const float log_sum = logf(sum);
+      for (uint32_t j = lane; j < a.top; j += 32) {
+        const uint64_t at = row * a.top + j;
+        Entry e{l_id[j], 0.f, 0.f};
+        if (e.id != kNoKey) {
+          auto d_of = [&](uint32_t i) { return load_as(static_cast<const char*>(a.teacher), a.teacher_type, row * a.top + i) - largest; };
+          const float d = d_of(j);
+          e.p = exp2_of(d * per_t) / sum;
+          e.s = load_as(logits, TYPE, e.id);
+          if (e.p != 0.f) task.plogp += e.p * (d * inv_t - log_sum);
+          if (doubled) {
+            if (l_table[l_slot[j]] != j) {
+              e.id = kNoKey;
+            } else {
+              for (uint32_t i = j + 1; i < a.top; ++i)
+                if (l_id[i] == e.id) e.p += exp2_of(d_of(i) * per_t) / sum;
+            }
+          }
+        }
+        entries[at] = e;
+      }
+      task.plogp = lanes_sum(task.plogp, 32);
+      __syncwarp();
+    }
+    if (bad) set_error(a.st, ERR_KEY_RANGE);
+    if (lane == 0) static_cast<RowTask*>(a.tasks)[row] = task;
+  }
+}
+
+// Coefficients of a row's two exponentials in its gradient.
+struct RowScale {
+  float t, one;
+};
+__device__ __forceinline__ RowScale row_scale(const DistillArgs& a, uint64_t row, const RowTask& task, const RowSums& sums, bool two) {
+  const float f = a.weights != nullptr ? a.scale * a.weights[row] : a.scale;
+  const float soft = task.some ? a.soft * a.temperature * f : 0.f, hard = task.label >= 0 ? a.hard * f : 0.f;
+  if (two) return RowScale{soft / sums.t, hard / sums.one};
+  return RowScale{(soft + hard) / sums.t, 0.f};
+}
+
+// ---- two floats at a time ------------------------------------------------------
+__device__ __forceinline__ uint64_t pair_of(float x, float y) {
+  return (uint64_t)__float_as_uint(x) | ((uint64_t)__float_as_uint(y) << 32);
+}
+__device__ __forceinline__ float2 floats_of(uint64_t v) { return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))); }
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+// The elements of a word, two by two.
+template <int TYPE>
+__device__ __forceinline__ uint64_t pair_at(const uint4& v, int j) {
+  if constexpr (TYPE == ADAPM_F32) {
+    return j == 0 ? ((uint64_t)v.x | ((uint64_t)v.y << 32)) : ((uint64_t)v.z | ((uint64_t)v.w << 32));
+  } else {
+    const uint32_t w = j == 0 ? v.x : (j == 1 ? v.y : (j == 2 ? v.z : v.w));
+    const float2 f = unpack2<TYPE>(w);
+    return pair_of(f.x, f.y);
+  }
+}
+template <int TYPE>
+__device__ __forceinline__ float largest_of(const uint4& v) {
+  if constexpr (TYPE == ADAPM_F32) {
+    return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+  } else {
+    using H = typename std::conditional<TYPE == ADAPM_BF16, __nv_bfloat162, __half2>::type;
+    auto h = [](uint32_t w) { return *reinterpret_cast<const H*>(&w); };
+    const H m = __hmax2(__hmax2(h(v.x), h(v.y)), __hmax2(h(v.z), h(v.w)));
+    const float2 f = unpack2<TYPE>(*reinterpret_cast<const uint32_t*>(&m));
+    return fmaxf(f.x, f.y);
+  }
+}
+// Where max c is this large, logits are taken relative to the largest before
+// they are multiplied (which would lose too much, or overflow).  Those within
+// the exponential's range of it share its leading bits, so their differences
+// are exact in 16 bits too.
+constexpr float kHuge = 1e5f;
+template <int TYPE>
+__device__ __forceinline__ void take_off(uint4& v, float max) {
+  uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if constexpr (TYPE == ADAPM_F32) {
+      w[j] = __float_as_uint(__uint_as_float(w[j]) - max);
+    } else {
+      const float2 f = unpack2<TYPE>(w[j]);
+      w[j] = pack2<TYPE>(f.x - max, f.y - max);
+    }
+  }
+  v = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// 2^(s c - k) with k = max c, rounded, is off by the rounding of k alone; times
+// this it is 2^((s - max) c).
+__device__ __forceinline__ float unround(float max, float c) {
+  const float k = max * c;
+  return exp2_of(-fmaf(max, c, -k));
+}
 
 // Blocks per SM that the registers allow: 32 of a thread hold eight words.
 constexpr int resident_blocks(int threads, int words) { return (words == 8 ? 1024 : 1536) / threads; }
-
-// What a row has to learn from.
-struct RowTask {
-  int64_t label;    // -1: none
-  bool listed;      // the list has an id
-};
-__device__ __forceinline__ RowTask row_task(const DistillArgs& a, uint64_t row) {
-  RowTask t{-1, false};
-  if (a.labels != nullptr) {
-    const int64_t y = id_at(a.labels, a.wide_labels, row);
-    if (!(a.has_pad && y == a.pad)) {
-      if (y >= 0 && y < (int64_t)a.vocab) t.label = y;
-      else if (threadIdx.x == 0) set_error(a.st, ERR_KEY_RANGE);
-    }
-  }
-  // (the first 32 entries say it nearly always)
-  const int lane = threadIdx.x & 31;
-  for (uint32_t j0 = 0; j0 < a.top && !t.listed; j0 += 32) {
-    const int64_t id = j0 + lane < a.top ? id_at(a.ids, a.wide, row * a.top + j0 + lane) : -1;
-    t.listed = __any_sync(0xFFFFFFFFu, id >= 0 && id < (int64_t)a.vocab);
-  }
-  return t;
-}
+__device__ __forceinline__ float finite_shift(float m) { return m == -INFINITY ? 0.f : m; }
 
 // NV words a thread in registers (0: the row is read again for its gradient).
 // TWO: sums at both temperatures.  Launched in clusters of `split` blocks per row.
 template <int TYPE, int THREADS, int NV, bool TWO>
 __global__ void __launch_bounds__(THREADS, resident_blocks(THREADS, NV))
-distill_kernel(const __grid_constant__ DistillArgs a, int split, uint32_t table) {
+distill_rows_kernel(const __grid_constant__ DistillArgs a, int split) {
   after_previous();
   constexpr int E = Word<TYPE>::kElements, WARPS = THREADS / 32, KEPT = NV > 0 ? NV : 1;
-  __shared__ Sums sums[2][kMaxCluster * WARPS];
-  __shared__ float teacher_part[2][4];   // whether there are entries, largest t, sum of exponentials
-  extern __shared__ uint32_t lists[];    // warp 0: id, t, s, slot of every entry; the table
-  uint32_t* const l_id = lists;
-  float* const l_t = reinterpret_cast<float*>(lists + a.top);
-  float* const l_s = l_t + a.top;
-  uint32_t* const l_slot = lists + 3 * a.top;
-  uint32_t* const l_table = lists + 4 * a.top;
+  __shared__ RowSums sums[2][kMaxCluster * WARPS];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int rank = split > 1 ? (int)(blockIdx.x % split) : 0;
   const uint64_t rows = gridDim.x / split;
-  const float per_t = kLog2E / a.temperature;             // exp((s - m) / T) = 2^((s - m) per_t)
-  const float per = a.top > 0 ? per_t : kLog2E;           // the one temperature of a row without TWO
+  // exp((s - m) / T) = 2^((s - m) per); the one temperature of a row without TWO
+  const float per = a.top > 0 ? kLog2E / a.temperature : kLog2E;
+  const RowTask* const tasks = static_cast<const RowTask*>(a.tasks);
   uint64_t row = blockIdx.x / split;
-  RowTask next = row < a.n ? row_task(a, row) : RowTask{-1, false};
+  RowTask next = tasks[row < a.n ? row : 0];
   for (int turn = 0; row < a.n; row += rows, turn ^= 1) {
     const RowTask task = next;
-    const bool live = task.listed || task.label >= 0;
+    const bool live = task.some || task.label >= 0;
     const RowWords b = row_words<TYPE>(a.logits, row, a.vocab);
     const uint32_t slice = (b.words + split - 1) / split;
     const uint32_t w0 = rank * slice, w1 = min(b.words, w0 + slice);
     uint4 v[KEPT];
-    float label_s = 0.f;   // the label's logit (warp 0)
-    Sums mine{-INFINITY, 0.f, 0.f};
-    if (live) {
-      if constexpr (NV > 0) {
+    RowSums mine{-INFINITY, 0.f, 0.f};
+    if (live && NV > 0) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-          const uint32_t w = w0 + i * THREADS + threadIdx.x;
-          v[i] = make_uint4(Word<TYPE>::kNone, Word<TYPE>::kNone, Word<TYPE>::kNone, Word<TYPE>::kNone);
-          if (w < w1) v[i] = load_word<TYPE>(b, a.vocab, w);
-        }
+      for (int i = 0; i < KEPT; ++i) {
+        const uint32_t w = w0 + i * THREADS + threadIdx.x;
+        v[i] = make_uint4(Word<TYPE>::kNone, Word<TYPE>::kNone, Word<TYPE>::kNone, Word<TYPE>::kNone);
+        if (w < w1) v[i] = load_word<TYPE>(b, a.vocab, w);
       }
     }
-    if (row + rows < a.n) next = row_task(a, row + rows);
+    if (row + rows < a.n) next = tasks[row + rows];
     if (live) {
-      if (warp == 0) {
-        // the list: ids, teacher and student logits; its largest t and sum
-        float tm = -INFINITY;
-        bool bad = false;
-        for (uint32_t j = lane; j < a.top; j += 32) {
-          const uint64_t at = row * a.top + j;
-          const int64_t id = id_at(a.ids, a.wide, at);
-          float t = load_as(static_cast<const char*>(a.teacher), a.teacher_type, at);
-          const bool here = id >= 0 && id < (int64_t)a.vocab && t != -INFINITY;
-          bad = bad || (id >= (int64_t)a.vocab) || id < -1;
-          l_id[j] = here ? (uint32_t)id : kNoKey;
-          l_t[j] = here ? t : -INFINITY;
-          l_s[j] = here ? load_as(b.base, TYPE, b.head + id) : 0.f;
-          if (here) tm = fmaxf(tm, t);
-        }
-        if (task.label >= 0) label_s = load_as(b.base, TYPE, b.head + task.label);
-        if (bad) set_error(a.st, ERR_KEY_RANGE);
-        for (uint32_t j = lane; j < table; j += 32) l_table[j] = kEmpty;
+      // sums of 2^(s c - k), two by two; k = max c
+      auto add = [&](const uint4& word, uint64_t c, uint64_t minus_k, uint64_t& to) {
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) tm = fmaxf(tm, __shfl_xor_sync(0xFFFFFFFFu, tm, o));
-        float ts = 0.f;
-        bool some = false;
-        for (uint32_t j = lane; j < a.top; j += 32) {
-          if (l_id[j] == kNoKey) continue;
-          some = true;
-          ts += exp2_of((l_t[j] - tm) * per_t);
-        }
-        some = __any_sync(0xFFFFFFFFu, some);
-        ts = lanes_sum(ts, 32);
-        if (lane == 0) {
-          teacher_part[turn][0] = some ? 1.f : 0.f;
-          teacher_part[turn][1] = tm;
-          teacher_part[turn][2] = ts;
-        }
-      }
-      // the warp's largest logit, then its sums relative to it
-      auto largest = [&](const uint4& word) {
-        float x[E];
-        unpack_word<TYPE>(word, x);
-#pragma unroll
-        for (int j = 0; j < E; ++j) mine.max = fmaxf(mine.max, x[j]);
-      };
-      auto add = [&](const uint4& word, float shift) {
-        float x[E];
-        unpack_word<TYPE>(word, x);
-#pragma unroll
-        for (int j = 0; j < E; ++j) {
-          const float d = x[j] - shift;
-          mine.t += exp2_of(d * per);
-          if (TWO) mine.one += exp2_of(d * kLog2E);
+        for (int j = 0; j < E / 2; ++j) {
+          const float2 d = floats_of(fma_pair(pair_at<TYPE>(word, j), c, minus_k));
+          to = add_pair(to, pair_of(exp2_of(d.x), exp2_of(d.y)));
         }
       };
+      uint64_t st = 0, so = 0;
       if constexpr (NV > 0) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) largest(v[i]);
+        for (int i = 0; i < NV; ++i) mine.max = fmaxf(mine.max, largest_of<TYPE>(v[i]));
+        mine.max = lanes_max(mine.max);
+        float shift = finite_shift(mine.max);
+        const bool huge = fabsf(shift * kLog2E) > kHuge || fabsf(shift * per) > kHuge;
+        if (huge) {
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) mine.max = fmaxf(mine.max, __shfl_xor_sync(0xFFFFFFFFu, mine.max, o));
-        const float shift = finite_shift(mine.max);
+          for (int i = 0; i < NV; ++i) take_off<TYPE>(v[i], shift);
+        }
+        const float k = huge ? 0.f : shift;
+        const uint64_t c = pair_of(per, per), m = pair_of(-(k * per), -(k * per));
 #pragma unroll
-        for (int i = 0; i < NV; ++i) add(v[i], shift);
+        for (int i = 0; i < NV; ++i) add(v[i], c, m, st);
+        if (TWO) {
+          const uint64_t c1 = pair_of(kLog2E, kLog2E), m1 = pair_of(-(k * kLog2E), -(k * kLog2E));
+#pragma unroll
+          for (int i = 0; i < NV; ++i) add(v[i], c1, m1, so);
+        }
+        if (huge) {   // (as they were: the gradient is relative to the whole row's largest)
+#pragma unroll
+          for (int i = 0; i < NV; ++i) {
+            const uint32_t w = w0 + i * THREADS + threadIdx.x;
+            if (w < w1) v[i] = load_word<TYPE>(b, a.vocab, w);
+          }
+        }
+        const float2 t = floats_of(st), o = floats_of(so);
+        mine.t = (t.x + t.y) * unround(k, per);
+        mine.one = TWO ? (o.x + o.y) * unround(k, kLog2E) : 0.f;
       } else {
-        float max = -INFINITY;   // of the words so far, which the sums are relative to
         for (uint32_t w = w0 + threadIdx.x; w < w1; w += THREADS) {
           const uint4 word = load_word<TYPE>(b, a.vocab, w);
-          mine.max = max;
-          largest(word);
-          const float shift = finite_shift(mine.max), down = finite_shift(max) - shift;
-          if (down != 0.f) {
-            mine.t *= exp2_of(down * per);
-            mine.one *= exp2_of(down * kLog2E);
+          const float max = fmaxf(mine.max, largest_of<TYPE>(word));
+          const float shift = finite_shift(max);
+          if (max > mine.max && mine.max != -INFINITY) {   // (sums of nothing are 0)
+            mine.t *= exp2_of((mine.max - max) * per);
+            mine.one *= exp2_of((mine.max - max) * kLog2E);
           }
-          max = mine.max;
-          add(word, shift);
-        }
-        float top = max;
+          mine.max = max;
+          float x[E];
+          unpack_word<TYPE>(word, x);
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-        const float down = finite_shift(max) - finite_shift(top);
-        mine.t *= exp2_of(down * per);
-        mine.one *= exp2_of(down * kLog2E);
+          for (int j = 0; j < E; ++j) {
+            mine.t += exp2_of((x[j] - shift) * per);
+            if (TWO) mine.one += exp2_of((x[j] - shift) * kLog2E);
+          }
+        }
+        const float top = lanes_max(mine.max);
+        if (mine.max != -INFINITY) {
+          mine.t *= exp2_of((mine.max - top) * per);
+          mine.one *= exp2_of((mine.max - top) * kLog2E);
+        }
         mine.max = top;
       }
       mine.t = lanes_sum(mine.t, 32);
@@ -322,127 +472,110 @@ distill_kernel(const __grid_constant__ DistillArgs a, int split, uint32_t table)
       if (lane == 0) sums[turn][warp] = mine;
       __syncthreads();
     }
-    Sums all{-INFINITY, 0.f, 0.f};
+    RowSums all{-INFINITY, 0.f, 0.f};
     if (live) {
       for (int i = lane; i < split * WARPS; i += 32) all.max = fmaxf(all.max, sums[turn][i].max);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) all.max = fmaxf(all.max, __shfl_xor_sync(0xFFFFFFFFu, all.max, o));
+      all.max = lanes_max(all.max);
       for (int i = lane; i < split * WARPS; i += 32) {
-        const Sums& s = sums[turn][i];
+        const RowSums& s = sums[turn][i];
         const float down = s.max - all.max;   // (-inf: the warp has no logit above -inf, its sums are 0)
         all.t += s.t * exp2_of(down * per);
         if (TWO) all.one += s.one * exp2_of(down * kLog2E);
       }
       all.t = lanes_sum(all.t, 32);
       if (TWO) all.one = lanes_sum(all.one, 32);
+      if (rank == 0 && threadIdx.x == 0) static_cast<RowSums*>(a.sums)[row] = all;
     }
-    const bool some = live && teacher_part[turn][0] != 0.f && a.top > 0;
-    const float factor = a.weights != nullptr ? a.scale * a.weights[row] : a.scale;
-    const float soft = some ? a.soft * a.temperature : 0.f, hard = task.label >= 0 ? a.hard : 0.f;
-    const bool any = some || task.label >= 0;
-    // coefficients of the two exponentials
-    const float ct = TWO ? soft * factor / all.t : (soft + hard) * factor / all.t;
-    const float co = TWO ? hard * factor / all.one : 0.f;
-    RowWords g{};
-    uint32_t w1g = 0;
-    if (a.grad.data != nullptr) {
-      g = row_words<TYPE>(a.grad, row, a.vocab);
-      w1g = rank == split - 1 ? g.words : min(g.words, w0 + slice);
-      auto gradient = [&](const uint4& word) {
-        float x[E];
-        unpack_word<TYPE>(word, x);
-#pragma unroll
-        for (int j = 0; j < E; ++j) {
-          const float d = x[j] - all.max;
-          x[j] = exp2_of(d * per) * ct;
-          if (TWO) x[j] = fmaf(exp2_of(d * kLog2E), co, x[j]);
-        }
-        return pack_word<TYPE>(x);
-      };
-      if (!any) {
-        for (uint32_t w = w0 + threadIdx.x; w < w1g; w += THREADS) store_word<TYPE>(g, a.vocab, w, make_uint4(0, 0, 0, 0));
-      } else if (NV > 0 && g.head == b.head) {
-#pragma unroll
-        for (int i = 0; i < KEPT; ++i) {
-          const uint32_t w = w0 + i * THREADS + threadIdx.x;
-          if (w < w1) store_word<TYPE>(g, a.vocab, w, gradient(v[i]));
-        }
-      } else {
-        // words of the gradient that begin elsewhere: the row again, from L2
-        const uint32_t shift = (b.head - g.head) & (E - 1), back = b.head < g.head ? 1 : 0;
-        for (uint32_t w = w0 + threadIdx.x; w < w1g; w += THREADS)
-          store_word<TYPE>(g, a.vocab, w, gradient(load_shifted<TYPE>(b, a.vocab, w - back, shift)));
-      }
-      if (any) __syncthreads();   // the elements below are written over
-    }
-    if (warp != 0) continue;
-    if (!any) {
-      if (rank == 0 && lane == 0) a.loss[row] = 0.f;
+    if (a.grad.data == nullptr) continue;
+    const RowWords g = row_words<TYPE>(a.grad, row, a.vocab);
+    const uint32_t w1g = rank == split - 1 ? g.words : min(g.words, w0 + slice);
+    if (!live) {
+      for (uint32_t w = w0 + threadIdx.x; w < w1g; w += THREADS) store_word<TYPE>(g, a.vocab, w, make_uint4(0, 0, 0, 0));
       continue;
     }
-    const float tm = teacher_part[turn][1], ts = teacher_part[turn][2];
-    const float inv_t = 1.f / a.temperature;
-    const float log_st = logf(all.t), log_s1 = TWO ? logf(all.one) : log_st, log_ts = logf(ts);
-    // entries that share an id: the first of them speaks for all
-    bool doubled = false;
-    if (some && a.grad.data != nullptr) {
-      __syncwarp();
-      for (uint32_t j = lane; j < a.top; j += 32) {
-        const uint32_t id = l_id[j];
-        if (id == kNoKey) continue;
-        uint32_t h = (id * 2654435761u) & (table - 1);
-        while (true) {   // (the table has twice as many slots as there are entries)
-          const uint32_t old = atomicCAS(&l_table[h], kEmpty, j);
-          if (old == kEmpty) break;
-          if (l_id[old] == id) {
-            atomicMin(&l_table[h], j);
-            doubled = true;
-            break;
-          }
-          h = (h + 1) & (table - 1);
+    const RowScale scale = row_scale(a, row, task, all, TWO);
+    const bool huge = fabsf(all.max * kLog2E) > kHuge || fabsf(all.max * per) > kHuge;
+    const float k = huge ? 0.f : all.max;
+    const uint64_t c = pair_of(per, per), m = pair_of(-(k * per), -(k * per)), ct = pair_of(scale.t * unround(k, per), scale.t * unround(k, per));
+    const uint64_t c1 = pair_of(kLog2E, kLog2E), m1 = pair_of(-(k * kLog2E), -(k * kLog2E)), co = pair_of(scale.one * unround(k, kLog2E), scale.one * unround(k, kLog2E));
+    auto gradient = [&](uint4 word) {
+      if (huge) take_off<TYPE>(word, all.max);
+      float x[E];
+#pragma unroll
+      for (int j = 0; j < E / 2; ++j) {
+        const uint64_t s = pair_at<TYPE>(word, j);
+        const float2 d = floats_of(fma_pair(s, c, m));
+        uint64_t y = mul_pair(pair_of(exp2_of(d.x), exp2_of(d.y)), ct);
+        if (TWO) {
+          const float2 d1 = floats_of(fma_pair(s, c1, m1));
+          y = fma_pair(pair_of(exp2_of(d1.x), exp2_of(d1.y)), co, y);
         }
-        l_slot[j] = h;
+        const float2 f = floats_of(y);
+        x[2 * j] = f.x;
+        x[2 * j + 1] = f.y;
       }
-      doubled = __any_sync(0xFFFFFFFFu, doubled);
-      __syncwarp();
+      return pack_word<TYPE>(x);
+    };
+    if (NV > 0 && g.head == b.head) {
+#pragma unroll
+      for (int i = 0; i < KEPT; ++i) {
+        const uint32_t w = w0 + i * THREADS + threadIdx.x;
+        if (w < w1) store_word<TYPE>(g, a.vocab, w, gradient(v[i]));
+      }
+    } else {
+      // words of the gradient that begin elsewhere: the row again, from L2
+      const uint32_t shift = (b.head - g.head) & (E - 1), back = b.head < g.head ? 1 : 0;
+      for (uint32_t w = w0 + threadIdx.x; w < w1g; w += THREADS)
+        store_word<TYPE>(g, a.vocab, w, gradient(load_shifted<TYPE>(b, a.vocab, w - back, shift)));
     }
-    float kl = 0.f;
-    bool label_met = false;
-    auto mine_to_write = [&](uint32_t id) {
-      const uint32_t w = (g.head + id) / E;
-      return a.grad.data != nullptr && w >= w0 && w < w1g;
-    };
-    auto dense = [&](float s) {   // the part of every element, as written above
+  }
+}
+
+// The loss, and the elements that list and label change.
+template <int TYPE>
+__global__ void __launch_bounds__(kListWarps * 32)
+distill_marks_kernel(const __grid_constant__ DistillArgs a, bool two) {
+  after_previous();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const float per = a.top > 0 ? kLog2E / a.temperature : kLog2E;
+  const float inv_t = 1.f / a.temperature;
+  for (uint64_t row = (uint64_t)blockIdx.x * kListWarps + warp; row < a.n; row += (uint64_t)gridDim.x * kListWarps) {
+    const RowTask task = static_cast<const RowTask*>(a.tasks)[row];
+    if (!task.some && task.label < 0) {
+      if (lane == 0) a.loss[row] = 0.f;
+      continue;
+    }
+    const RowSums all = static_cast<const RowSums*>(a.sums)[row];
+    const RowScale scale = row_scale(a, row, task, all, two);
+    const float f = a.weights != nullptr ? a.scale * a.weights[row] : a.scale;
+    const float log_st = logf(all.t), log_s1 = two ? logf(all.one) : log_st;
+    const bool write = a.grad.data != nullptr;
+    char* const grad = write ? a.grad.data + row_offset(a.grad, (uint32_t)row) * Word<TYPE>::kSize : nullptr;
+    auto dense = [&](float s) {   // the part that every element has
       const float d = s - all.max;
-      const float x = exp2_of(d * per) * ct;
-      return TWO ? fmaf(exp2_of(d * kLog2E), co, x) : x;
+      const float x = exp2_of(d * per) * scale.t;
+      return two ? fmaf(exp2_of(d * kLog2E), scale.one, x) : x;
     };
-    if (some) {
+    float cross = 0.f;   // sum of p ln q
+    bool label_met = false;
+    if (task.some) {
       for (uint32_t j = lane; j < a.top; j += 32) {
-        const uint32_t id = l_id[j];
-        if (id == kNoKey) continue;
-        const float log_p = (l_t[j] - tm) * inv_t - log_ts;
-        float p = exp2_of((l_t[j] - tm) * per_t) / ts;
-        if (rank == 0 && p != 0.f) kl += p * (log_p - ((l_s[j] - all.max) * inv_t - log_st));
-        const bool labelled = task.label == (int64_t)id;
+        const Entry e = static_cast<const Entry*>(a.entries)[row * a.top + j];
+        if (e.id == kNoKey) continue;
+        if (e.p != 0.f) cross += e.p * ((e.s - all.max) * inv_t - log_st);
+        const bool labelled = task.label == (int32_t)e.id;
         label_met = label_met || labelled;
-        if (!mine_to_write(id)) continue;
-        if (doubled) {
-          if (l_table[l_slot[j]] != j) continue;
-          for (uint32_t i = j + 1; i < a.top; ++i)
-            if (l_id[i] == id) p += exp2_of((l_t[i] - tm) * per_t) / ts;
-        }
-        store_as(g.base, TYPE, (int64_t)g.head + id, dense(l_s[j]) - factor * (soft * p + (labelled ? hard : 0.f)));
+        if (write) store_as(grad, TYPE, e.id, dense(e.s) - f * (a.soft * a.temperature * e.p + (labelled ? a.hard : 0.f)));
       }
       label_met = __any_sync(0xFFFFFFFFu, label_met);
+      cross = lanes_sum(cross, 32);
     }
-    if (rank == 0) kl = lanes_sum(kl, 32);
     if (lane != 0) continue;
-    if (task.label >= 0 && !label_met && mine_to_write((uint32_t)task.label))
-      store_as(g.base, TYPE, g.head + task.label, dense(label_s) - factor * hard);
-    if (rank != 0) continue;
-    float loss = some ? a.soft * a.temperature * a.temperature * kl : 0.f;
-    if (task.label >= 0) loss -= a.hard * ((label_s - all.max) - log_s1);
+    float loss = task.some ? a.soft * a.temperature * a.temperature * (task.plogp - cross) : 0.f;
+    if (task.label >= 0) {
+      loss -= a.hard * ((task.label_s - all.max) - log_s1);
+      if (write && !label_met) store_as(grad, TYPE, task.label, dense(task.label_s) - f * a.hard);
+    }
     a.loss[row] = loss;
   }
 }
@@ -453,12 +586,11 @@ inline uint32_t power_of_two(uint64_t n) {
   while (p < n) p *= 2;
   return p;
 }
+inline bool distill_two(const DistillArgs& a) { return a.top > 0 && a.labels != nullptr && a.temperature != 1.f; }
 
 template <int TYPE, int THREADS, int NV>
-void launch_distill_as(const DistillArgs& a, int split, int sms, cudaStream_t stream) {
-  const bool two = a.top > 0 && a.labels != nullptr && a.temperature != 1.f;
-  const uint32_t table = a.top > 0 ? power_of_two(2 * a.top) : 0;
-  void (*kernel)(DistillArgs, int, uint32_t) = two ? distill_kernel<TYPE, THREADS, NV, true> : distill_kernel<TYPE, THREADS, NV, false>;
+void launch_rows_as(const DistillArgs& a, int split, int sms, cudaStream_t stream) {
+  void (*kernel)(DistillArgs, int) = distill_two(a) ? distill_rows_kernel<TYPE, THREADS, NV, true> : distill_rows_kernel<TYPE, THREADS, NV, false>;
   cudaLaunchAttribute at[2]{};
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
@@ -470,25 +602,36 @@ void launch_distill_as(const DistillArgs& a, int split, int sms, cudaStream_t st
   cudaLaunchConfig_t c{};
   c.gridDim = dim3((unsigned)(std::min<uint64_t>(a.n, clusters) * split));
   c.blockDim = dim3(THREADS);
-  c.dynamicSmemBytes = (4 * (size_t)a.top + table) * sizeof(uint32_t);
   c.stream = stream;
   c.attrs = at;
   c.numAttrs = split > 1 ? 2 : 1;
-  note_launches(1);
-  cudaLaunchKernelEx(&c, kernel, a, split, table);
+  cudaLaunchKernelEx(&c, kernel, a, split);
+}
+
+template <int TYPE>
+void launch_rows(const DistillArgs& a, int sms, cudaStream_t stream) {
+  const uint64_t words = ((uint64_t)a.vocab * Word<TYPE>::kSize + 15) / 16 + 1;   // (a row may begin inside a word)
+  if (words <= 256) return launch_rows_as<TYPE, 128, 2>(a, 1, sms, stream);
+  if (words <= 1024) return launch_rows_as<TYPE, 128, 8>(a, 1, sms, stream);
+  if (words <= 2048) return launch_rows_as<TYPE, 512, 4>(a, 1, sms, stream);
+  uint32_t split = power_of_two((words + 4095) / 4096);
+  if (split > kMaxCluster) return launch_rows_as<TYPE, 512, 0>(a, 8, sms, stream);
+  // few rows: more blocks for each
+  while (split < 8 && a.n * split * 2 <= (uint64_t)sms && words / split > 1024) split *= 2;
+  launch_rows_as<TYPE, 512, 8>(a, (int)split, sms, stream);
 }
 
 template <int TYPE>
 void launch_distill_type(const DistillArgs& a, int sms, cudaStream_t stream) {
-  const uint64_t words = ((uint64_t)a.vocab * Word<TYPE>::kSize + 15) / 16 + 1;   // (a row may begin inside a word)
-  if (words <= 256) return launch_distill_as<TYPE, 128, 2>(a, 1, sms, stream);
-  if (words <= 1024) return launch_distill_as<TYPE, 128, 8>(a, 1, sms, stream);
-  if (words <= 2048) return launch_distill_as<TYPE, 512, 4>(a, 1, sms, stream);
-  uint32_t split = power_of_two((words + 4095) / 4096);
-  if (split > kMaxCluster) return launch_distill_as<TYPE, 512, 0>(a, 8, sms, stream);
-  // few rows: more blocks for each
-  while (split < 8 && a.n * split * 2 <= (uint64_t)sms && words / split > 1024) split *= 2;
-  launch_distill_as<TYPE, 512, 8>(a, (int)split, sms, stream);
+  const uint32_t table = a.top > 0 ? power_of_two(2 * a.top) : 0;
+  const unsigned grid = (unsigned)std::min<uint64_t>((a.n + kListWarps - 1) / kListWarps, (uint64_t)sms * 16);
+  const size_t smem = kListWarps * (2 * (size_t)a.top + table) * sizeof(uint32_t);
+  if (smem > 48 * 1024)
+    cudaFuncSetAttribute(distill_lists_kernel<TYPE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  note_launches(3);
+  launch_after(distill_lists_kernel<TYPE>, grid, kListWarps * 32, smem, stream, a, table);
+  launch_rows<TYPE>(a, sms, stream);
+  launch_after(distill_marks_kernel<TYPE>, grid, kListWarps * 32, 0, stream, a, distill_two(a));
 }
 
 }  // namespace

@@ -19,33 +19,34 @@ namespace adapm {
 
 namespace {
 
-constexpr int kUnit = 8;             // elements of a lane
-constexpr uint32_t kBlockRow = 1024 * kUnit;   // elements of a row that one block holds
-constexpr int kSmallBlock = 256;     // threads where several rows share a block
-
-// How a row is spread: `lanes` lanes per row (a power of two up to 32, or whole
-// warps), `rows` rows per block of `threads` threads.
+// A row is taken by `lanes` lanes (a power of two up to 32, or whole warps up
+// to kMaxLanes), of which lane l holds elements ((j / VEC) * lanes + l) * VEC + j % VEC
+// for j < EL; blocks of kSmallBlock threads hold several rows of few lanes.
+constexpr int kMaxLanes = 512;
+constexpr int kSmallBlock = 128;
 struct Spread {
-  int lanes, rows, threads;
+  int lanes, threads;
 };
-Spread spread_of(uint32_t dim) {
-  const uint32_t units = (dim + kUnit - 1) / kUnit;
-  Spread s{};
+Spread spread_of(uint32_t dim, int el) {
+  const uint32_t units = (dim + el - 1) / el;
+  Spread s{1, kSmallBlock};
   if (units <= 32) {
-    s.lanes = 1;
     while ((uint32_t)s.lanes < units) s.lanes *= 2;
-    s.threads = kSmallBlock;
-    s.rows = kSmallBlock / s.lanes;
   } else {
     s.lanes = s.threads = (int)((units + 31) / 32 * 32);
-    s.rows = 1;
   }
   return s;
 }
 
-// Sums of two numbers over a row's lanes; `part` is shared memory of two
-// float2 per warp, used in turn by successive calls (`turn` 0 and 1), so that
-// one barrier a call is enough.
+// Elements of a lane: 8 where a warp's lanes are enough for the row; else as
+// many as the registers hold beside the parameters (and, backward, their sums).
+constexpr int kFew = 8;
+constexpr int many(int type, int vec, bool backward) {
+  return backward || type < 0 || type == ADAPM_F32 || vec == 1 ? 16 : 32;
+}
+
+// Sums of two numbers over a row's lanes; `part` is shared memory that
+// successive calls use in turn (`turn` 0 and 1), so that one barrier a call is enough.
 __device__ __forceinline__ float2 row_sum2(float a, float b, int lanes, float2 (*part)[32], int turn) {
   const int w = lanes < 32 ? lanes : 32;
   a = lanes_sum(a, w);
@@ -54,116 +55,181 @@ __device__ __forceinline__ float2 row_sum2(float a, float b, int lanes, float2 (
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = lanes >> 5;
   if (lane == 0) part[turn][warp] = make_float2(a, b);
   __syncthreads();
-  const float2 v = lane < warps ? part[turn][lane] : make_float2(0.f, 0.f);
-  return make_float2(lanes_sum(v.x, 32), lanes_sum(v.y, 32));
-}
-
-// Mean and sum of squared differences from it over a row's lanes.  Warps find
-// both for their own elements first, so one exchange serves both: with n_w
-// elements of mean m_w, the row's sum is sum S_w + sum n_w (m_w - m)^2.
-template <int N>
-__device__ __forceinline__ float2 row_moments(const float (&x)[N], const bool (&has)[N], float own, float warp_n, uint32_t dim,
-                                              int lanes, float2 (*part)[32], int turn) {
-  const int w = lanes < 32 ? lanes : 32;
-  float s = 0.f;
-#pragma unroll
-  for (int j = 0; j < N; ++j) s += x[j];   // (absent elements are zero)
-  s = lanes_sum(s, w);
-  const float mean_w = warp_n > 0.f ? s / warp_n : 0.f;
-  float q = 0.f;
-#pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const float d = has[j] ? x[j] - mean_w : 0.f;
-    q = fmaf(d, d, q);
+  if (warps > 8) {
+    const float2 v = lane < warps ? part[turn][lane] : make_float2(0.f, 0.f);
+    return make_float2(lanes_sum(v.x, 32), lanes_sum(v.y, 32));
   }
-  q = lanes_sum(q, w);
-  if (lanes <= 32) return make_float2(mean_w, q);
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = lanes >> 5;
-  if (lane == 0) part[turn][warp] = make_float2(s, q);
-  __syncthreads();
-  const float2 v = lane < warps ? part[turn][lane] : make_float2(0.f, 0.f);
-  const float mean = lanes_sum(v.x, 32) / (float)dim;
-  // `own`: elements of the warp whose sums this lane looks at
-  const float d = own > 0.f ? v.x / own - mean : 0.f;
-  return make_float2(mean, lanes_sum(fmaf(own * d, d, v.y), 32));
+  float2 s = part[turn][0];
+  for (int i = 1; i < warps; ++i) {
+    s.x += part[turn][i].x;
+    s.y += part[turn][i].y;
+  }
+  return s;
 }
 
-// Elements of a row that warp `warp` of `lanes` holds, in accesses of VEC.
-template <int VEC>
+// Elements of a row that warp `warp` of its lanes holds, in accesses of VEC.
+template <int VEC, int EL>
 __device__ __forceinline__ float warp_elements(uint32_t dim, int lanes, int warp) {
   const int w = lanes < 32 ? lanes : 32;
   int n = 0;
 #pragma unroll
-  for (int i = 0; i < kUnit / VEC; ++i) {
-    const int64_t first = ((int64_t)i * lanes + warp * w) * VEC;
-    const int64_t left = (int64_t)dim - first;
+  for (int i = 0; i < EL / VEC; ++i) {
+    const int64_t left = (int64_t)dim - ((int64_t)i * lanes + warp * w) * VEC;
     n += left <= 0 ? 0 : (left < w * VEC ? (int)left : w * VEC);
   }
   return (float)n;
 }
 
-// Lane `lane` of `lanes` holds elements ((j / VEC) * lanes + lane) * VEC + j % VEC.
-// TYPE -1: types are known at run time alone.
-template <int TYPE, int VEC>
-__device__ __forceinline__ void load_row(const RowView& v, uint64_t row, uint32_t dim, int lane, int lanes, float (&x)[kUnit]) {
+// Mean and sum of squared differences from it over a row's lanes.  Warps find
+// both for their own elements first, so one exchange serves both: with n_w
+// elements of sum s_w, the row's sum is sum q_w + sum n_w (s_w / n_w - m)^2.
+// counts: n_w of every warp.
+template <int VEC, int EL>
+__device__ __forceinline__ float2 row_moments(const float (&x)[EL], float mine, const float* counts, uint32_t dim, int lane,
+                                              int lanes, float2 (*part)[32], int turn) {
+  const int w = lanes < 32 ? lanes : 32;
+  float s = 0.f;
+#pragma unroll
+  for (int j = 0; j < EL; ++j) s += x[j];   // (absent elements are zero)
+  s = lanes_sum(s, w);
+  const float mean_w = mine > 0.f ? s / mine : 0.f;
+  float q = 0.f;
+#pragma unroll
+  for (int j = 0; j < EL; ++j) {
+    const float d = (uint32_t)((j / VEC) * lanes + lane) * VEC < dim ? x[j] - mean_w : 0.f;
+    q = fmaf(d, d, q);
+  }
+  q = lanes_sum(q, w);
+  if (lanes <= 32) return make_float2(mean_w, q);
+  const int wl = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = lanes >> 5;
+  if (wl == 0) part[turn][warp] = make_float2(s, q);
+  __syncthreads();
+  float total = 0.f;
+  for (int i = 0; i < warps; ++i) total += part[turn][i].x;
+  const float mean = total / (float)dim;
+  float all = 0.f;
+  for (int i = 0; i < warps; ++i) {
+    const float2 v = part[turn][i];
+    const float n = counts[i], d = n > 0.f ? v.x / n - mean : 0.f;
+    all += fmaf(n * d, d, v.y);
+  }
+  return make_float2(mean, all);
+}
+
+// A lane's elements as they come from memory (TYPE -1: a type known at run
+// time alone, as floats), so that the next row's can be on their way while
+// this one is worked on.
+template <int TYPE, int VEC, int EL>
+struct Raw {
+  static constexpr int kSize = TYPE == ADAPM_F32 || TYPE < 0 ? 4 : 2;
+  static constexpr int kWords = VEC == 1 ? EL : EL * kSize / 4;
+  uint32_t w[kWords];
+};
+template <int TYPE, int VEC, int EL>
+__device__ __forceinline__ void fetch(const RowView& v, uint64_t row, uint32_t dim, int lane, int lanes, Raw<TYPE, VEC, EL>& r) {
   const int type = TYPE < 0 ? v.type : TYPE;
-  const char* p = v.data + row_offset(v, (uint32_t)row) * type_size(type);
+  const char* p = v.data + (row_offset(v, (uint32_t)row) + (int64_t)lane * VEC) * type_size(type);
+  constexpr int A = EL / VEC, W = Raw<TYPE, VEC, EL>::kWords / A;   // accesses; words of one
 #pragma unroll
-  for (int i = 0; i < kUnit / VEC; ++i) {
-    const uint32_t c = (uint32_t)(i * lanes + lane) * VEC;
-    if (c < dim) {
-      if constexpr (TYPE < 0) load_n_as<VEC>(p + (uint64_t)c * type_size(type), type, x + i * VEC);
-      else load_n<TYPE, VEC>(p + (uint64_t)c * type_size(type), x + i * VEC);
-    } else {
+  for (int j = 0; j < Raw<TYPE, VEC, EL>::kWords; ++j) r.w[j] = 0u;
+  auto all = [&](auto kind) {
+    constexpr int T = decltype(kind)::value, S = T == ADAPM_F32 ? 4 : 2;
+    const char* q = p;
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) x[i * VEC + j] = 0.f;
+    for (int i = 0; i < A; ++i, q += (int64_t)lanes * VEC * S) {
+      if ((uint32_t)(i * lanes + lane) * VEC >= dim) continue;
+      if constexpr (W == 4) {
+        const uint4 x = *reinterpret_cast<const uint4*>(q);
+        r.w[4 * i] = x.x; r.w[4 * i + 1] = x.y; r.w[4 * i + 2] = x.z; r.w[4 * i + 3] = x.w;
+      } else if constexpr (W == 2) {
+        const uint2 x = *reinterpret_cast<const uint2*>(q);
+        r.w[2 * i] = x.x; r.w[2 * i + 1] = x.y;
+      } else if constexpr (TYPE < 0) {
+        r.w[i] = __float_as_uint(load_as(q, T, 0));
+      } else {
+        static_assert(W == 1 && VEC == 1);
+        if constexpr (S == 4) r.w[i] = *reinterpret_cast<const uint32_t*>(q);
+        else r.w[i] = *reinterpret_cast<const uint16_t*>(q);
+      }
+    }
+  };
+  by_type<TYPE>(type, all);
+}
+template <int TYPE, int VEC, int EL>
+__device__ __forceinline__ void unpack_raw(const Raw<TYPE, VEC, EL>& r, float (&x)[EL]) {
+  if constexpr (TYPE == ADAPM_F32 || TYPE < 0) {
+#pragma unroll
+    for (int j = 0; j < EL; ++j) x[j] = __uint_as_float(r.w[j]);
+  } else if constexpr (VEC == 1) {
+#pragma unroll
+    for (int j = 0; j < EL; ++j) x[j] = unpack2<TYPE>(r.w[j]).x;
+  } else {
+#pragma unroll
+    for (int j = 0; j < EL / 2; ++j) {
+      const float2 f = unpack2<TYPE>(r.w[j]);
+      x[2 * j] = f.x;
+      x[2 * j + 1] = f.y;
     }
   }
 }
-template <int VEC>
-__device__ __forceinline__ void store_row(const RowView& v, uint64_t row, uint32_t dim, int lane, int lanes, const float (&y)[kUnit]) {
-  char* p = v.data + row_offset(v, (uint32_t)row) * type_size(v.type);
+template <int VEC, int EL>
+__device__ __forceinline__ void store_row(const RowView& v, uint64_t row, uint32_t dim, int lane, int lanes, const float (&y)[EL]) {
+  auto all = [&](auto kind) {
+    constexpr int T = decltype(kind)::value, S = T == ADAPM_F32 ? 4 : 2;
+    char* p = v.data + (row_offset(v, (uint32_t)row) + (int64_t)lane * VEC) * S;
 #pragma unroll
-  for (int i = 0; i < kUnit / VEC; ++i) {
-    const uint32_t c = (uint32_t)(i * lanes + lane) * VEC;
-    if (c < dim) store_n_as<VEC>(p + (uint64_t)c * type_size(v.type), v.type, y + i * VEC);
-  }
+    for (int i = 0; i < EL / VEC; ++i, p += (int64_t)lanes * VEC * S)
+      if ((uint32_t)(i * lanes + lane) * VEC < dim) store_n<T, VEC>(p, y + i * VEC);
+  };
+  by_type<-1>(v.type, all);
 }
-template <int VEC>
-__device__ __forceinline__ void load_params(const VectorView& v, uint32_t dim, int lane, int lanes, float none, float (&w)[kUnit]) {
+template <int VEC, int EL>
+__device__ __forceinline__ void load_params(const VectorView& v, uint32_t dim, int lane, int lanes, float none, float (&w)[EL]) {
+  if (v.data == nullptr) {
 #pragma unroll
-  for (int j = 0; j < kUnit; ++j) {
-    const uint32_t c = (uint32_t)((j / VEC) * lanes + lane) * VEC + j % VEC;
-    w[j] = v.data == nullptr ? none : (c < dim ? load_as(v.data, v.type, c) : 0.f);
+    for (int j = 0; j < EL; ++j) w[j] = none;
+    return;
   }
+  auto all = [&](auto kind) {
+    constexpr int T = decltype(kind)::value;
+#pragma unroll
+    for (int j = 0; j < EL; ++j) {
+      const uint32_t c = (uint32_t)((j / VEC) * lanes + lane) * VEC + j % VEC;
+      w[j] = c < dim ? load_as(v.data, T, c) : 0.f;
+    }
+  };
+  by_type<-1>(v.type, all);
 }
 
-template <int TYPE, int VEC>
-__global__ void __launch_bounds__(1024)
+template <int TYPE, int VEC, int EL>
+__global__ void __launch_bounds__(kMaxLanes)
 norm_kernel(const __grid_constant__ NormArgs a, int lanes) {
   after_previous();
   __shared__ float2 part[2][32];
+  __shared__ float counts[32];
   const int lane = threadIdx.x % lanes, group = threadIdx.x / lanes, rows = blockDim.x / lanes;
-  float w[kUnit], b[kUnit];
+  const uint64_t step = (uint64_t)gridDim.x * rows;
+  // (the rows of a warp are taken together: lanes without a row take the last one, and leave it)
+  uint64_t row = (uint64_t)blockIdx.x * rows + group;
+  auto held = [&](uint64_t r) { return r < a.n ? r : a.n - 1; };
+  Raw<TYPE, VEC, EL> raw;
+  fetch(a.x, held(row), a.dim, lane, lanes, raw);
+  float w[EL], b[EL];
   load_params<VEC>(a.weight, a.dim, lane, lanes, 1.f, w);
   load_params<VEC>(a.bias, a.dim, lane, lanes, 0.f, b);
-  bool has[kUnit];
-#pragma unroll
-  for (int j = 0; j < kUnit; ++j) has[j] = (uint32_t)((j / VEC) * lanes + lane) * VEC + j % VEC < a.dim;
-  const float mine = warp_elements<VEC>(a.dim, lanes, lane >> 5);
-  const float own = (threadIdx.x & 31) * 32 < lanes ? warp_elements<VEC>(a.dim, lanes, threadIdx.x & 31) : 0.f;
+  if (threadIdx.x < 32) counts[threadIdx.x] = (int)threadIdx.x * 32 < lanes ? warp_elements<VEC, EL>(a.dim, lanes, threadIdx.x) : 0.f;
+  const float mine = warp_elements<VEC, EL>(a.dim, lanes, lane >> 5);
+  if (lanes > 32) __syncthreads();
   int turn = 0;
-  // (the rows of a warp are taken together: a lane without a row follows with zeros)
-  for (uint64_t r0 = (uint64_t)blockIdx.x * rows; r0 < a.n; r0 += (uint64_t)gridDim.x * rows, turn ^= 1) {
-    const uint64_t row = r0 + group;
-    const bool live = row < a.n;
-    float x[kUnit];
-    load_row<TYPE, VEC>(a.x, live ? row : r0, a.dim, lane, lanes, x);
-    const float2 m = row_moments(x, has, own, mine, a.dim, lanes, part, turn);
+  for (uint64_t r0 = (uint64_t)blockIdx.x * rows; r0 < a.n; r0 += step, row += step, turn ^= 1) {
+    float x[EL];
+    unpack_raw(raw, x);
+    if (r0 + step < a.n) fetch(a.x, held(row + step), a.dim, lane, lanes, raw);
+    const float2 m = row_moments<VEC>(x, mine, counts, a.dim, lane, lanes, part, turn);
     const float r = 1.f / sqrtf(m.y / (float)a.dim + a.eps);
-    if (!live) continue;
+    if (row >= a.n) continue;
 #pragma unroll
-    for (int j = 0; j < kUnit; ++j) x[j] = fmaf((x[j] - m.x) * r, w[j], b[j]);
+    for (int j = 0; j < EL; ++j) x[j] = fmaf((x[j] - m.x) * r, w[j], b[j]);
     store_row<VEC>(a.out, row, a.dim, lane, lanes, x);
     if (a.stats != nullptr && lane == 0) reinterpret_cast<float2*>(a.stats)[row] = make_float2(m.x, r);
   }
@@ -197,70 +263,78 @@ norm_long_kernel(const __grid_constant__ NormArgs a) {
 }
 
 // dx, and every block's sums of dy h and dy over its rows.
-template <int TYPE, int VEC>
-__global__ void __launch_bounds__(1024)
+template <int TYPE, int VEC, int EL>
+__global__ void __launch_bounds__(kMaxLanes)
 norm_grad_kernel(const __grid_constant__ NormArgs a, int lanes) {
   after_previous();
   __shared__ float2 part[2][32];
-  __shared__ float sums[kSmallBlock * kUnit];
+  __shared__ float sums[kSmallBlock * EL];
   const int lane = threadIdx.x % lanes, group = threadIdx.x / lanes, rows = blockDim.x / lanes;
-  float w[kUnit], dw[kUnit], db[kUnit];
+  const uint64_t step = (uint64_t)gridDim.x * rows;
+  uint64_t row = (uint64_t)blockIdx.x * rows + group;
+  auto held = [&](uint64_t r) { return r < a.n ? r : a.n - 1; };
+  Raw<TYPE, VEC, EL> rx, rg;
+  fetch(a.x, held(row), a.dim, lane, lanes, rx);
+  fetch(a.grad, held(row), a.dim, lane, lanes, rg);
+  float2 next = reinterpret_cast<const float2*>(a.stats)[held(row)];
+  float w[EL], dw[EL], db[EL];
   load_params<VEC>(a.weight, a.dim, lane, lanes, 1.f, w);
 #pragma unroll
-  for (int j = 0; j < kUnit; ++j) dw[j] = db[j] = 0.f;
+  for (int j = 0; j < EL; ++j) dw[j] = db[j] = 0.f;
   const float inv = 1.f / (float)a.dim;
   int turn = 0;
-  for (uint64_t r0 = (uint64_t)blockIdx.x * rows; r0 < a.n; r0 += (uint64_t)gridDim.x * rows, turn ^= 1) {
-    const uint64_t row = r0 + group;
+  for (uint64_t r0 = (uint64_t)blockIdx.x * rows; r0 < a.n; r0 += step, row += step, turn ^= 1) {
     const bool live = row < a.n;
-    float x[kUnit], g[kUnit];
-    load_row<TYPE, VEC>(a.x, live ? row : r0, a.dim, lane, lanes, x);
-    load_row<TYPE, VEC>(a.grad, live ? row : r0, a.dim, lane, lanes, g);
-    const float2 st = reinterpret_cast<const float2*>(a.stats)[live ? row : r0];
+    const float2 st = next;
+    float x[EL], g[EL];
+    unpack_raw(rx, x);
+    unpack_raw(rg, g);
+    if (r0 + step < a.n) {
+      fetch(a.x, held(row + step), a.dim, lane, lanes, rx);
+      fetch(a.grad, held(row + step), a.dim, lane, lanes, rg);
+      next = reinterpret_cast<const float2*>(a.stats)[held(row + step)];
+    }
     float s0 = 0.f, s1 = 0.f;
 #pragma unroll
-    for (int j = 0; j < kUnit; ++j) {
-      const float h = (x[j] - st.x) * st.y;
+    for (int j = 0; j < EL; ++j) {
+      x[j] = (x[j] - st.x) * st.y;   // h
       if (live) {
-        dw[j] = fmaf(g[j], h, dw[j]);
+        dw[j] = fmaf(g[j], x[j], dw[j]);
         db[j] += g[j];
       }
-      const float gw = g[j] * w[j];   // (zero where there is no element)
-      s0 += gw;
-      s1 = fmaf(gw, h, s1);
+      g[j] *= w[j];   // (zero where there is no element)
+      s0 += g[j];
+      s1 = fmaf(g[j], x[j], s1);
     }
     if (a.out.data == nullptr) continue;
     const float2 s = row_sum2(s0, s1, lanes, part, turn);
     if (!live) continue;
     const float c0 = s.x * inv, c1 = s.y * inv;
 #pragma unroll
-    for (int j = 0; j < kUnit; ++j) {
-      const float h = (x[j] - st.x) * st.y;
-      x[j] = st.y * (g[j] * w[j] - c0 - h * c1);
-    }
+    for (int j = 0; j < EL; ++j) x[j] = st.y * (g[j] - c0 - x[j] * c1);
     store_row<VEC>(a.out, row, a.dim, lane, lanes, x);
   }
   if (a.parts == nullptr) return;
   // the block's rows together, group after group
   float* out = a.parts + (uint64_t)blockIdx.x * 2 * a.dim;
+#pragma unroll
   for (int which = 0; which < 2; ++which) {
-    const float(&d)[kUnit] = which ? db : dw;
     if (lanes > 32) {   // one row at a time
 #pragma unroll
-      for (int j = 0; j < kUnit; ++j) {
+      for (int j = 0; j < EL; ++j) {
         const uint32_t c = (uint32_t)((j / VEC) * lanes + lane) * VEC + j % VEC;
-        if (c < a.dim) out[which * a.dim + c] = d[j];
+        if (c < a.dim) out[which * a.dim + c] = which ? db[j] : dw[j];
       }
       continue;
     }
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < kUnit; ++j)
-      sums[group * lanes * kUnit + ((j / VEC) * lanes + lane) * VEC + j % VEC] = d[j];
+    for (int j = 0; j < EL; ++j)
+      sums[group * lanes * EL + ((j / VEC) * lanes + lane) * VEC + j % VEC] = which ? db[j] : dw[j];
     __syncthreads();
     for (uint32_t c = threadIdx.x; c < a.dim; c += blockDim.x) {
       float s = 0.f;
-      for (int g = 0; g < rows; ++g) s += sums[g * lanes * kUnit + c];
+      for (int g = 0; g < rows; ++g) s += sums[g * lanes * EL + c];
       out[which * a.dim + c] = s;
     }
   }
@@ -314,31 +388,39 @@ norm_columns_kernel(const __grid_constant__ NormArgs a) {
 }
 
 // The sums of `count` blocks, in a fixed order: 32 columns a block, every warp
-// takes each 8th block's sums.
-__global__ void __launch_bounds__(256)
+// takes each 32nd block's sums, four of them on their way at a time.
+__global__ void __launch_bounds__(1024)
 norm_join_kernel(const float* parts, uint32_t count, uint32_t dim, VectorView dweight, VectorView dbias) {
   after_previous();
-  __shared__ float sums[8][32];
+  __shared__ float sums[32][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const uint64_t c = (uint64_t)blockIdx.x * 32 + lane;   // of 2 dim columns
-  const uint64_t width = 2ull * dim;
+  const uint64_t width = 2ull * dim;   // columns of both
+  const uint64_t c = (uint64_t)blockIdx.x * 32 + lane;
   float s = 0.f;
-  if (c < width)
-    for (uint32_t p = warp; p < count; p += 8) s += parts[p * width + c];
+  if (c < width) {
+    uint32_t p = warp;
+    for (; p + 96 < count; p += 128) {
+      const float x0 = parts[p * width + c], x1 = parts[(p + 32) * width + c], x2 = parts[(p + 64) * width + c],
+                  x3 = parts[(p + 96) * width + c];
+      s = (((s + x0) + x1) + x2) + x3;
+    }
+    for (; p < count; p += 32) s += parts[p * width + c];
+  }
   sums[warp][lane] = s;
   __syncthreads();
-  if (warp != 0 || c >= width) return;
-  for (int w = 1; w < 8; ++w) s += sums[w][lane];
-  const VectorView& v = c < dim ? dweight : dbias;
-  if (v.data != nullptr) store_as(v.data, v.type, c < dim ? c : c - dim, s);
+  // warp w adds up column w
+  s = lanes_sum(sums[lane][warp], 32);
+  const uint64_t mine = (uint64_t)blockIdx.x * 32 + warp;
+  if (lane != 0 || mine >= width) return;
+  const VectorView& v = mine < dim ? dweight : dbias;
+  if (v.data != nullptr) store_as(v.data, v.type, mine < dim ? mine : mine - dim, s);
 }
 
-// Elements that every access of the vectors kernels takes: rows begin and end on a multiple of it.
+// Elements that every access takes: rows begin and end on a multiple of it.
 template <class... V>
-uint32_t width_of(const NormArgs& a, const V&... views) {
-  const int type = a.x.type;
-  for (uint32_t vec : {8u, 4u}) {
-    if (type == ADAPM_F32 && vec == 8) continue;
+int width_of(const NormArgs& a, const V&... views) {
+  for (int vec : {8, 4}) {
+    if (a.x.type == ADAPM_F32 && vec == 8) continue;
     bool ok = a.dim % vec == 0;
     ((ok = ok && rows_on(views, a.n, vec)), ...);
     if (ok) return vec;
@@ -346,61 +428,77 @@ uint32_t width_of(const NormArgs& a, const V&... views) {
   return 1;
 }
 
-unsigned grid_of(uint64_t n, const Spread& s, int sms, int threads_per_sm) {
-  const uint64_t per_sm = std::min(32, std::max(1, threads_per_sm / s.threads));
-  return (unsigned)std::max<uint64_t>(1, std::min<uint64_t>((n + s.rows - 1) / s.rows, (uint64_t)sms * per_sm));
+// How the kernels take the rows: types known when compiled or not, the width of
+// an access, elements of a lane.
+struct Plan {
+  int type, vec, el;
+  Spread s;
+  unsigned grid;
+  bool wide;   // too wide for a block
+};
+Plan plan_of(const NormArgs& a, bool backward, int sms) {
+  Plan p{};
+  const bool mixed = backward && a.grad.type != a.x.type;
+  p.type = mixed ? -1 : a.x.type;
+  p.vec = mixed ? 1 : (!backward ? width_of(a, a.x, a.out) : (a.out.data ? width_of(a, a.x, a.grad, a.out) : width_of(a, a.x, a.grad)));
+  p.el = a.dim <= 32 * kFew ? kFew : many(p.type, p.vec, backward);
+  p.s = spread_of(a.dim, p.el);
+  p.wide = p.s.lanes > kMaxLanes;
+  const uint64_t rows = p.s.threads / p.s.lanes;
+  // blocks per SM that the registers hold
+  const uint64_t per_sm = std::max(1, (p.el == kFew ? 1024 : 512) / p.s.threads);
+  p.grid = (unsigned)std::max<uint64_t>(1, std::min<uint64_t>((a.n + rows - 1) / rows, (uint64_t)sms * per_sm));
+  return p;
 }
-
-constexpr int kNormThreads = 1536, kNormGradThreads = 1024;   // per SM
 constexpr int kLongRows = 64;   // row classes of norm_columns_kernel
+uint64_t part_count(const NormArgs& a, const Plan& p) { return p.wide ? std::min<uint64_t>(a.n, kLongRows) : p.grid; }
 
-bool long_rows(const NormArgs& a) { return a.dim > kBlockRow; }
-uint64_t part_count(const NormArgs& a, int sms) {
-  if (long_rows(a)) return std::min<uint64_t>(a.n, kLongRows);
-  return grid_of(a.n, spread_of(a.dim), sms, kNormGradThreads);
-}
-
-template <int TYPE>
-void launch_norm_type(const NormArgs& a, uint32_t vec, const Spread& s, unsigned grid, cudaStream_t stream) {
-  if (vec == 8) {
-    if constexpr (TYPE != ADAPM_F32) launch_after(norm_kernel<TYPE, 8>, grid, s.threads, 0, stream, a, s.lanes);
+template <bool BACK, int TYPE, int VEC>
+void launch_as(const NormArgs& a, const Plan& p, cudaStream_t stream) {
+  constexpr int MANY = many(TYPE, VEC, BACK);
+  if constexpr (BACK) {
+    if (p.el == kFew) launch_after(norm_grad_kernel<TYPE, VEC, kFew>, p.grid, p.s.threads, 0, stream, a, p.s.lanes);
+    else launch_after(norm_grad_kernel<TYPE, VEC, MANY>, p.grid, p.s.threads, 0, stream, a, p.s.lanes);
   } else {
-    launch_after(norm_kernel<TYPE, 4>, grid, s.threads, 0, stream, a, s.lanes);
+    if (p.el == kFew) launch_after(norm_kernel<TYPE, VEC, kFew>, p.grid, p.s.threads, 0, stream, a, p.s.lanes);
+    else launch_after(norm_kernel<TYPE, VEC, MANY>, p.grid, p.s.threads, 0, stream, a, p.s.lanes);
   }
 }
-template <int TYPE>
-void launch_grad_type(const NormArgs& a, uint32_t vec, const Spread& s, unsigned grid, cudaStream_t stream) {
-  if (vec == 8) {
-    if constexpr (TYPE != ADAPM_F32) launch_after(norm_grad_kernel<TYPE, 8>, grid, s.threads, 0, stream, a, s.lanes);
-  } else {
-    launch_after(norm_grad_kernel<TYPE, 4>, grid, s.threads, 0, stream, a, s.lanes);
-  }
+template <bool BACK, int TYPE>
+void launch_type(const NormArgs& a, const Plan& p, cudaStream_t stream) {
+  if constexpr (TYPE == ADAPM_F16 || TYPE == ADAPM_BF16)
+    if (p.vec == 8) return launch_as<BACK, TYPE, 8>(a, p, stream);
+  if (p.vec == 4) launch_as<BACK, TYPE, 4>(a, p, stream);
+  else launch_as<BACK, TYPE, 1>(a, p, stream);
+}
+template <bool BACK>
+void launch(const NormArgs& a, const Plan& p, cudaStream_t stream) {
+  note_launches(1);
+  if (p.type == ADAPM_F32) launch_type<BACK, ADAPM_F32>(a, p, stream);
+  else if (p.type == ADAPM_F16) launch_type<BACK, ADAPM_F16>(a, p, stream);
+  else if (p.type == ADAPM_BF16) launch_type<BACK, ADAPM_BF16>(a, p, stream);
+  else if constexpr (BACK) launch_as<BACK, -1, 1>(a, p, stream);
 }
 
 }  // namespace
 
 void launch_layer_norm(const NormArgs& a, int sms, cudaStream_t stream) {
+  const Plan p = plan_of(a, false, sms);
+  if (!p.wide) return launch<false>(a, p, stream);
   note_launches(1);
-  if (long_rows(a)) {
-    launch_after(norm_long_kernel, (unsigned)std::min<uint64_t>(a.n, (uint64_t)sms * 2), 1024, 0, stream, a);
-    return;
-  }
-  const Spread s = spread_of(a.dim);
-  const unsigned grid = grid_of(a.n, s, sms, kNormThreads);
-  const uint32_t vec = width_of(a, a.x, a.out);
-  if (vec == 1) launch_after(norm_kernel<-1, 1>, grid, s.threads, 0, stream, a, s.lanes);
-  else if (a.x.type == ADAPM_F32) launch_norm_type<ADAPM_F32>(a, vec, s, grid, stream);
-  else if (a.x.type == ADAPM_F16) launch_norm_type<ADAPM_F16>(a, vec, s, grid, stream);
-  else launch_norm_type<ADAPM_BF16>(a, vec, s, grid, stream);
+  launch_after(norm_long_kernel, (unsigned)std::min<uint64_t>(a.n, (uint64_t)sms * 2), 1024, 0, stream, a);
 }
 
 size_t norm_grad_scratch(const NormArgs& a, int sms) {
-  return a.dweight.data || a.dbias.data ? part_count(a, sms) * 2 * a.dim : 0;
+  return a.dweight.data || a.dbias.data ? part_count(a, plan_of(a, true, sms)) * 2 * a.dim : 0;
 }
 
 void launch_layer_norm_grad(const NormArgs& a, int sms, cudaStream_t stream) {
-  const uint64_t count = part_count(a, sms);
-  if (long_rows(a)) {
+  const Plan p = plan_of(a, true, sms);
+  const uint64_t count = part_count(a, p);
+  if (!p.wide) {
+    launch<true>(a, p, stream);
+  } else {
     if (a.parts != nullptr) {
       note_launches(1);
       // (the grid has two dimensions: launched plainly)
@@ -410,19 +508,11 @@ void launch_layer_norm_grad(const NormArgs& a, int sms, cudaStream_t stream) {
       note_launches(1);
       launch_after(norm_grad_long_kernel, (unsigned)std::min<uint64_t>(a.n, (uint64_t)sms * 2), 1024, 0, stream, a);
     }
-  } else {
-    const Spread s = spread_of(a.dim);
-    uint32_t vec = a.grad.type != a.x.type ? 1 : (a.out.data ? width_of(a, a.x, a.grad, a.out) : width_of(a, a.x, a.grad));
-    note_launches(1);
-    if (vec == 1) launch_after(norm_grad_kernel<-1, 1>, (unsigned)count, s.threads, 0, stream, a, s.lanes);
-    else if (a.x.type == ADAPM_F32) launch_grad_type<ADAPM_F32>(a, vec, s, (unsigned)count, stream);
-    else if (a.x.type == ADAPM_F16) launch_grad_type<ADAPM_F16>(a, vec, s, (unsigned)count, stream);
-    else launch_grad_type<ADAPM_BF16>(a, vec, s, (unsigned)count, stream);
   }
   if (a.parts != nullptr) {
     note_launches(1);
-    launch_after(norm_join_kernel, (unsigned)((2ull * a.dim + 31) / 32), 256, 0, stream, (const float*)a.parts, (uint32_t)count, a.dim,
-                 a.dweight, a.dbias);
+    launch_after(norm_join_kernel, (unsigned)((2ull * a.dim + 31) / 32), 1024, 0, stream, (const float*)a.parts, (uint32_t)count,
+                 a.dim, a.dweight, a.dbias);
   }
 }
 

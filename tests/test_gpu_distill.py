@@ -245,6 +245,15 @@ def test_far_logits(gpu_lib, pm):
     assert not loss.isnan().any()
 
 
+def test_logits_far_from_zero(gpu_lib, pm):
+    """An offset of all logits of a row changes nothing but their own rounding."""
+    for V in (300, 20_000, 300_001):
+        logits = torch.randn(4, V, device="cuda") * 2 + torch.tensor([[1000.0], [-3000.0], [30.0], [20_000.0]], device="cuda")
+        ids, teacher = lists((4,), V, 8)
+        check(pm, logits, ids, teacher, 1.0, long=V > 270_000)
+        check(pm, logits, ids, teacher, 1.7, 0.5, ids[:, 0].contiguous(), 0.5, long=V > 270_000)
+
+
 def test_ids_outside_the_vocabulary_are_reported(gpu_lib):
     pm = gpu_lib.ParameterManager(4, 4, 1)
     V = 50
