@@ -33,6 +33,11 @@ size_t norm_grad_scratch(const NormArgs& a, int sms);
 void launch_layer_norm(const NormArgs& a, int sms, cudaStream_t stream);
 void launch_layer_norm_grad(const NormArgs& a, int sms, cudaStream_t stream);
 
+// Columns of `count` rows of sums (`width` floats each) added up in a fixed
+// order; the first `dim` go to low, the others to high.
+void launch_column_join(const float* parts, uint32_t count, uint64_t width, uint32_t dim, const VectorView& low,
+                        const VectorView& high, cudaStream_t stream);
+
 // ---- distillation (distill.cuh) ---------------------------------------------------
 constexpr uint32_t kMaxTop = 1024;   // entries of a teacher's list
 struct DistillArgs {

@@ -28,8 +28,7 @@ struct GemmArgs {
   uint32_t bn, stages;
   uint32_t tiles_m, tiles_n;
   uint32_t k_blocks, splits, per_split;   // blocks of k: all, parts they are summed in, of one part
-  bool bf16;
-  float* parts;              // splits > 1: the parts' sums, each laid out like the product without gaps
+  bool aligned;              // rows of what is written and of the residual begin on four elements
   Epilogue e;
   DevState* st;
 };

@@ -12,8 +12,9 @@
 // address (rows that do not begin on 16 bytes) is copied first.
 // Bound by the tensor cores where all three sizes are large, by memory where
 // one is small: then k is summed in parts, so that every SM reads.
+#include <cooperative_groups.h>
+
 #include <algorithm>
-#include <cmath>
 
 #include "gemm.cuh"
 
@@ -21,85 +22,201 @@ namespace adapm {
 
 namespace {
 
-constexpr int kGemmThreads = 192;
+namespace cg = cooperative_groups;
+
+constexpr int kFinishWarps = 8, kGemmThreads = 32 * (2 + kFinishWarps);
 constexpr uint32_t kMaxStages = 12;
 constexpr uint32_t kStage = 32 * 36;        // floats of a warp's staging tile (rows of 32, apart by 36)
 constexpr uint32_t kSmem = 232448;          // shared memory of a block
 constexpr uint32_t kGroupM = 16;            // tiles of m taken together, for L2
 constexpr uint32_t kTurnedRows = 64;        // up to so many rows the weight's columns are m
+constexpr uint32_t kMostSplits = 8;         // parts of k: the blocks of a cluster
 
 // ---- activations -----------------------------------------------------------------
-__device__ __forceinline__ float act(float z, int kind) {
-  switch (kind) {
-    case ADAPM_ACTIVATION_RELU: return fmaxf(z, 0.f) + (z != z ? z : 0.f);   // (a NaN stays one)
-    case ADAPM_ACTIVATION_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678f));
-    case ADAPM_ACTIVATION_GELU_TANH: return 0.5f * z * (1.f + tanhf(0.79788456f * (z + 0.044715f * z * z * z)));
-    case ADAPM_ACTIVATION_SILU: return z / (1.f + expf(-z));
-    case ADAPM_ACTIVATION_TANH: return tanhf(z);
-    default: return z;
-  }
-}
-__device__ __forceinline__ float slope(float z, int kind) {
-  switch (kind) {
-    case ADAPM_ACTIVATION_RELU: return z > 0.f ? 1.f : (z != z ? z : 0.f);
-    case ADAPM_ACTIVATION_GELU: return 0.5f * (1.f + erff(z * 0.70710678f)) + z * 0.39894228f * expf(-0.5f * z * z);
-    case ADAPM_ACTIVATION_GELU_TANH: {
-      const float t = tanhf(0.79788456f * (z + 0.044715f * z * z * z));
-      return 0.5f * (1.f + t) + 0.5f * z * (1.f - t * t) * 0.79788456f * (1.f + 0.134145f * z * z);
-    }
-    case ADAPM_ACTIVATION_SILU: {
-      const float s = 1.f / (1.f + expf(-z));
-      return s * (1.f + z * (1.f - s));
-    }
-    case ADAPM_ACTIVATION_TANH: {
-      const float t = tanhf(z);
-      return 1.f - t * t;
-    }
-    default: return 1.f;
-  }
-}
+// z / (1 + e^-z); 0 where e^-z is beyond fp32, as in the limit.
+__device__ __forceinline__ float over_one_plus_exp(float z, float minus) { return __fdividef(z, 1.f + __expf(minus)); }
 
-// One element of a product.
-__device__ __forceinline__ void finish_one(const Epilogue& e, uint64_t r, uint64_t c, float z) {
-  if (e.bias.data) z += load_as(e.bias.data, e.bias.type, c);
-  if (e.pre.data) store_as(e.pre.data, e.pre.type, r * e.pre.row_stride + c, z);
-  z = act(z, e.activation);
-  if (e.residual.data) z += load_as(e.residual.data, e.residual.type, r * e.residual.row_stride + c);
-  store_as(e.out.data, e.out.type, r * e.out.row_stride + c, z);
+// act(z) of N numbers; the branch stands outside of the loop.
+template <int N>
+__device__ __forceinline__ void activate(float (&z)[N], int kind) {
+  switch (kind) {
+    case ADAPM_ACTIVATION_RELU:
+#pragma unroll
+      for (int j = 0; j < N; ++j) z[j] = z[j] < 0.f ? 0.f : z[j];   // (a NaN stays one)
+      break;
+    case ADAPM_ACTIVATION_GELU:
+#pragma unroll
+      for (int j = 0; j < N; ++j) z[j] = 0.5f * z[j] * (1.f + erff(z[j] * 0.70710678f));
+      break;
+    case ADAPM_ACTIVATION_GELU_TANH:   // 1/2 (1 + tanh u) = 1 / (1 + e^-2u)
+#pragma unroll
+      for (int j = 0; j < N; ++j) z[j] = over_one_plus_exp(z[j], z[j] * fmaf(-0.0713548163f, z[j] * z[j], -1.59576912f));
+      break;
+    case ADAPM_ACTIVATION_SILU:
+#pragma unroll
+      for (int j = 0; j < N; ++j) z[j] = over_one_plus_exp(z[j], -z[j]);
+      break;
+    case ADAPM_ACTIVATION_TANH:
+#pragma unroll
+      for (int j = 0; j < N; ++j) z[j] = tanhf(z[j]);
+      break;
+    default: break;
+  }
 }
-// Four neighbours of a row, on addresses that are multiples of four elements.
-__device__ __forceinline__ void finish_four(const Epilogue& e, uint64_t r, uint64_t c, float (&z)[4], const float (&bias)[4]) {
-  float add[4] = {0.f, 0.f, 0.f, 0.f};
-  if (e.residual.data) load_n_as<4>(e.residual.data + (r * e.residual.row_stride + c) * type_size(e.residual.type), e.residual.type, add);
+// d times act'(z), N of them.
+template <int N>
+__device__ __forceinline__ void times_slope(float (&d)[N], const float (&z)[N], int kind) {
+  switch (kind) {
+    case ADAPM_ACTIVATION_RELU:
 #pragma unroll
-  for (int j = 0; j < 4; ++j) z[j] += bias[j];
-  if (e.pre.data) store_n_as<4>(e.pre.data + (r * e.pre.row_stride + c) * type_size(e.pre.type), e.pre.type, z);
+      for (int j = 0; j < N; ++j) d[j] = z[j] > 0.f ? d[j] : (z[j] != z[j] ? z[j] : d[j] * 0.f);
+      break;
+    case ADAPM_ACTIVATION_GELU:
 #pragma unroll
-  for (int j = 0; j < 4; ++j) z[j] = act(z[j], e.activation) + add[j];
-  store_n_as<4>(e.out.data + (r * e.out.row_stride + c) * type_size(e.out.type), e.out.type, z);
+      for (int j = 0; j < N; ++j)
+        d[j] *= 0.5f * (1.f + erff(z[j] * 0.70710678f)) + z[j] * 0.39894228f * __expf(-0.5f * z[j] * z[j]);
+      break;
+    case ADAPM_ACTIVATION_GELU_TANH:
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        // s = 1/2 (1 + tanh u), its slope 2 s (1 - s) u'
+        const float q = z[j] * z[j];
+        const float s = over_one_plus_exp(1.f, z[j] * fmaf(-0.0713548163f, q, -1.59576912f));
+        d[j] *= fmaf(s * (1.f - s) * z[j], fmaf(0.214064449f, q, 1.59576912f), s);
+      }
+      break;
+    case ADAPM_ACTIVATION_SILU:
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const float s = over_one_plus_exp(1.f, -z[j]);
+        d[j] *= s * fmaf(z[j], 1.f - s, 1.f);
+      }
+      break;
+    case ADAPM_ACTIVATION_TANH:
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const float t = tanhf(z[j]);
+        d[j] *= 1.f - t * t;
+      }
+      break;
+    default: break;
+  }
 }
 
 // ---- the product -------------------------------------------------------------------
-struct Item {
-  uint32_t m0, n0, k0, k1, split;
+struct Tile {
+  uint32_t m0, n0;
 };
-__device__ __forceinline__ Item item_of(const GemmArgs& g, uint32_t i) {
-  Item t;
-  const uint32_t tiles = g.tiles_m * g.tiles_n;
-  t.split = i / tiles;
-  const uint32_t tile = i - t.split * tiles;
+__device__ __forceinline__ Tile tile_of(const GemmArgs& g, uint32_t tile) {
+  Tile t;
   // groups of kGroupM tiles of m, n by n inside
   const uint32_t in_group = kGroupM * g.tiles_n, group = tile / in_group, at = tile - group * in_group;
   const uint32_t height = min(kGroupM, g.tiles_m - group * kGroupM);
   t.m0 = (group * kGroupM + at % height) * kTileM;
   t.n0 = at / height * g.bn;
-  t.k0 = t.split * g.per_split;
-  t.k1 = min(g.k_blocks, t.k0 + g.per_split);
   return t;
 }
 
+// ---- epilogue ------------------------------------------------------------------------
+// N elements of a row from (r, c) on, that follow each other in memory on a multiple of N.
+template <int TYPE, bool OUT32, int N>
+struct Finish {
+  static constexpr int kOut = OUT32 ? ADAPM_F32 : TYPE;
+  static __device__ __forceinline__ void load_residual(const Epilogue& e, uint64_t r, uint32_t c, float (&add)[N]) {
+    load_n<kOut, N>(e.residual.data + (r * e.residual.row_stride + c) * type_size(kOut), add);
+  }
+  static __device__ __forceinline__ void store_pre(const Epilogue& e, uint64_t r, uint32_t c, const float* z) {
+    store_n<TYPE, N>(e.pre.data + (r * e.pre.row_stride + c) * type_size(TYPE), z);
+  }
+  static __device__ __forceinline__ void store_out(const Epilogue& e, uint64_t r, uint32_t c, const float* z) {
+    store_n<kOut, N>(e.out.data + (r * e.out.row_stride + c) * type_size(kOut), z);
+  }
+};
+// ROWS places (r_i, c) of one column block: z becomes what is stored; bias: of
+// the N columns.  has: which of the places exist.
+template <int TYPE, bool OUT32, int N, int ROWS>
+__device__ __forceinline__ void finish(const Epilogue& e, const uint64_t (&r)[ROWS], uint32_t c, const bool (&has)[ROWS],
+                                       const float (&bias)[N], float (&z)[ROWS * N]) {
+  using F = Finish<TYPE, OUT32, N>;
+  float add[ROWS][N];
+  const bool more = e.residual.data != nullptr;
+  if (more) {
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i)
+      if (has[i]) F::load_residual(e, r[i], c, add[i]);
+  }
+#pragma unroll
+  for (int j = 0; j < ROWS * N; ++j) z[j] += bias[j % N];
+  if (e.pre.data != nullptr) {
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i)
+      if (has[i]) F::store_pre(e, r[i], c, z + i * N);
+  }
+  activate(z, e.activation);
+  if (more) {
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+      for (int j = 0; j < N; ++j) z[i * N + j] += add[i][j];
+  }
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i)
+    if (has[i]) F::store_out(e, r[i], c, z + i * N);
+}
+
+// 32 x 32 elements that a warp has staged, rows apart by 36: rows [m0, m0 + 32),
+// columns [n0, n0 + 32) of m x n.
+template <int TYPE, bool OUT32>
+__device__ __forceinline__ void finish_tile(const GemmArgs& g, const float* tile, uint32_t m0, uint32_t n0) {
+  const int lane = threadIdx.x & 31;
+  if (g.aligned && n0 + 32 <= g.n) {
+    // a lane holds four neighbours of each fourth row
+    const uint32_t c = n0 + (lane & 7) * 4;
+    float bias[4] = {0.f, 0.f, 0.f, 0.f};
+    if (g.e.bias.data)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) bias[j] = load_as(g.e.bias.data, g.e.bias.type, c + j);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      float z[16];
+      uint64_t r[4];
+      bool has[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t row = half * 16 + i * 4 + (lane >> 3);
+        const float4 q = *reinterpret_cast<const float4*>(tile + row * 36 + (lane & 7) * 4);
+        z[4 * i] = q.x; z[4 * i + 1] = q.y; z[4 * i + 2] = q.z; z[4 * i + 3] = q.w;
+        r[i] = m0 + row;
+        has[i] = m0 + row < g.m;
+      }
+      finish<TYPE, OUT32, 4, 4>(g.e, r, c, has, bias, z);
+    }
+  } else {
+    // a lane holds a column: whatever the alignment, a row's stores are neighbours
+    const uint32_t c = n0 + lane;
+    float bias[1] = {0.f};
+    if (g.e.bias.data && c < g.n) bias[0] = load_as(g.e.bias.data, g.e.bias.type, c);
+#pragma unroll 1
+    for (int r0 = 0; r0 < 32; r0 += 8) {
+      float z[8];
+      uint64_t r[8];
+      bool has[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        z[i] = tile[(r0 + i) * 36 + lane];
+        r[i] = m0 + r0 + i;
+        has[i] = c < g.n && m0 + r0 + i < g.m;
+      }
+      finish<TYPE, OUT32, 1, 8>(g.e, r, c, has, bias, z);
+    }
+  }
+}
+
+// kGemmThreads threads: warp 0 copies, warp 1 multiplies, the others finish.
+template <bool BF16, bool OUT32>
 __global__ void __launch_bounds__(kGemmThreads, 1)
-gemm_kernel(const __grid_constant__ GemmArgs g, bool aligned) {
+gemm_kernel(const __grid_constant__ GemmArgs g) {
+  constexpr int TYPE = BF16 ? ADAPM_BF16 : ADAPM_F16;
   extern __shared__ uint8_t smem[];
   __shared__ uint64_t bars[2 * kMaxStages + 4];
   __shared__ uint32_t tmem_at;
@@ -107,9 +224,10 @@ gemm_kernel(const __grid_constant__ GemmArgs g, bool aligned) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t a_bytes = kTileM * 128, stage_bytes = a_bytes + g.bn * 128;
   const uint32_t ring = (shared_at(smem) + 1023u) & ~1023u;
-  float* const staging = reinterpret_cast<float*>(smem + (ring - shared_at(smem)) + g.stages * stage_bytes);
+  float* const ring_floats = reinterpret_cast<float*>(smem + (ring - shared_at(smem)));
+  float* const staging = ring_floats + g.stages * stage_bytes / 4;
   const uint32_t full = shared_at(bars), empty = full + 8 * kMaxStages, sum_full = empty + 8 * kMaxStages, sum_empty = sum_full + 16;
-  const uint32_t columns = 2 * max(16u, g.bn) <= 32 ? 32 : 2 * g.bn;   // (bn is a power of two)
+  const uint32_t columns = 2 * g.bn;   // (bn is a power of two, at least 16)
   if (threadIdx.x == 0) {
     for (uint32_t s = 0; s < g.stages; ++s) {
       barrier_init(full + 8 * s, 1);
@@ -117,7 +235,7 @@ gemm_kernel(const __grid_constant__ GemmArgs g, bool aligned) {
     }
     for (int b = 0; b < 2; ++b) {
       barrier_init(sum_full + 8 * b, 1);
-      barrier_init(sum_empty + 8 * b, 4);
+      barrier_init(sum_empty + 8 * b, kFinishWarps);
     }
     gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -128,15 +246,18 @@ gemm_kernel(const __grid_constant__ GemmArgs g, bool aligned) {
   tmem_fence_after();
   after_previous();
   const uint32_t tmem = tmem_at;
-  const uint32_t items = g.tiles_m * g.tiles_n * g.splits;
+  // with parts of k, each block of a cluster sums one part of one tile
+  const uint32_t items = g.tiles_m * g.tiles_n, part = g.splits > 1 ? blockIdx.x % g.splits : 0;
+  const uint32_t first = g.splits > 1 ? blockIdx.x / g.splits : blockIdx.x, step = g.splits > 1 ? items : gridDim.x;
+  const uint32_t k0 = part * g.per_split, k1 = min(g.k_blocks, k0 + g.per_split);
   if (warp == 0) {
     if (lane == 0) {
       asm volatile("fence.proxy.async;" ::: "memory");
       uint32_t n = 0, stage = 0, parity = 1;   // copies issued; a fresh ring is empty
       bool ok = true;
-      for (uint32_t i = blockIdx.x; i < items && ok; i += gridDim.x) {
-        const Item t = item_of(g, i);
-        for (uint32_t k = t.k0; k < t.k1; ++k) {
+      for (uint32_t i = first; i < items && ok; i += step) {
+        const Tile t = tile_of(g, i);
+        for (uint32_t k = k0; k < k1; ++k) {
           if (!(ok = barrier_wait(empty + 8 * stage, parity))) break;
           const uint32_t bar = full + 8 * stage, at = ring + stage * stage_bytes;
           barrier_expect(bar, stage_bytes);
@@ -166,23 +287,22 @@ gemm_kernel(const __grid_constant__ GemmArgs g, bool aligned) {
     }
   } else if (warp == 1) {
     if (lane == 0) {
-      const uint32_t shape = mma_shape(g.bf16, g.a_across, g.b_across, g.bn);
+      const uint32_t shape = mma_shape(BF16, g.a_across, g.b_across, g.bn);
       const uint32_t a_step = tile_step(g.a_across), b_step = tile_step(g.b_across);
       uint32_t stage = 0, parity = 0, turn = 0;
       bool ok = true;
-      for (uint32_t i = blockIdx.x; i < items && ok; i += gridDim.x, ++turn) {
-        const Item t = item_of(g, i);
+      for (uint32_t i = first; i < items && ok; i += step, ++turn) {
         const uint32_t b = turn & 1u;
         if (!(ok = barrier_wait(sum_empty + 8 * b, ((turn >> 1) & 1u) ^ 1u))) break;
         tmem_fence_after();
-        for (uint32_t k = t.k0; k < t.k1; ++k) {
+        for (uint32_t k = k0; k < k1; ++k) {
           if (!(ok = barrier_wait(full + 8 * stage, parity))) break;
           tmem_fence_after();
           const uint32_t at = ring + stage * stage_bytes;
           const uint64_t da = tile_descriptor(at, g.a_across), db = tile_descriptor(at + a_bytes, g.b_across);
 #pragma unroll
           for (uint32_t j = 0; j < kBlockK / 16; ++j)
-            mma(tmem + b * g.bn, da + j * a_step, db + j * b_step, shape, k > t.k0 || j > 0);
+            mma(tmem + b * g.bn, da + j * a_step, db + j * b_step, shape, k > k0 || j > 0);
           mma_commit(empty + 8 * stage);
           if (++stage == g.stages) {
             stage = 0;
@@ -194,11 +314,12 @@ gemm_kernel(const __grid_constant__ GemmArgs g, bool aligned) {
       if (!ok) atomicExch(&gave_up, 1u);
     }
   } else {
-    const uint32_t quarter = (uint32_t)warp & 3u;   // of the rows of tensor memory that this warp reaches
+    const uint32_t quarter = (uint32_t)warp & 3u;      // of the rows of tensor memory that this warp reaches
+    const uint32_t half = (uint32_t)(warp - 2) >> 2;   // of their columns, by turns
     float* const tile = staging + (warp - 2) * kStage;
     uint32_t turn = 0;
-    for (uint32_t i = blockIdx.x; i < items; i += gridDim.x, ++turn) {
-      const Item t = item_of(g, i);
+    for (uint32_t i = first; i < items; i += step, ++turn) {
+      const Tile t = tile_of(g, i);
       const uint32_t b = turn & 1u;
       if (!barrier_wait(sum_full + 8 * b, (turn >> 1) & 1u)) {
         if (lane == 0) atomicExch(&gave_up, 1u);
@@ -207,25 +328,24 @@ gemm_kernel(const __grid_constant__ GemmArgs g, bool aligned) {
       __syncwarp();
       tmem_fence_after();
       const uint32_t from = tmem + ((quarter * 32u) << 16) + b * g.bn;
-      const uint32_t m1 = t.m0 + quarter * 32;   // the warp's first row
-      float* const part = g.splits > 1 ? g.parts + (uint64_t)t.split * g.m * g.n : nullptr;
-      if (g.turned) {
-        // lanes are neighbours in the product's rows
-        for (uint32_t c0 = 0; c0 < g.bn; c0 += 16) {
+      if (g.splits > 1 || g.turned) {
+        // to shared memory (the ring is no longer read: there is one tile): see below
+        const uint32_t row = quarter * 32 + lane;
+        for (uint32_t c0 = half * 16; c0 < g.bn; c0 += 32) {
           float v[16];
           __syncwarp();
           tmem_load16(from + c0, v);
-          const uint64_t c = m1 + lane;
+          if (g.turned) {
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const uint64_t r = t.n0 + c0 + j;
-            if (c >= g.m || r >= g.n) continue;
-            if (part) part[r * g.m + c] = v[j];
-            else finish_one(g.e, r, c, v[j]);
+            for (int j = 0; j < 16; ++j) ring_floats[(c0 + j) * kTileM + row] = v[j];
+          } else {
+#pragma unroll
+            for (int j = 0; j < 16; j += 4)
+              *reinterpret_cast<float4*>(ring_floats + row * (g.bn + 4) + c0 + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
           }
         }
       } else {
-        for (uint32_t c0 = 0; c0 < g.bn && t.n0 + c0 < g.n; c0 += 32) {
+        for (uint32_t c0 = half * 32; c0 < g.bn && t.n0 + c0 < g.n; c0 += 64) {
           float v[32];
           __syncwarp();
           tmem_load(from + c0, v);
@@ -234,30 +354,7 @@ gemm_kernel(const __grid_constant__ GemmArgs g, bool aligned) {
           for (int j = 0; j < 32; j += 4)
             *reinterpret_cast<float4*>(tile + lane * 36 + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
           __syncwarp();
-          const uint32_t c = t.n0 + c0 + (lane & 7) * 4;
-          float bias[4] = {0.f, 0.f, 0.f, 0.f};
-          if (!part && g.e.bias.data)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (c + j < g.n) bias[j] = load_as(g.e.bias.data, g.e.bias.type, c + j);
-          for (int p = 0; p < 8; ++p) {
-            const uint32_t row = p * 4 + (lane >> 3);
-            const uint64_t r = m1 + row;
-            const float4 q = *reinterpret_cast<const float4*>(tile + row * 36 + (lane & 7) * 4);
-            if (r >= g.m) break;
-            float z[4] = {q.x, q.y, q.z, q.w};
-            if (aligned && c + 4 <= g.n) {
-              if (part) *reinterpret_cast<float4*>(part + r * g.n + c) = q;
-              else finish_four(g.e, r, c, z, bias);
-            } else {
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                if (c + j >= g.n) break;
-                if (part) part[r * g.n + c + j] = z[j];
-                else finish_one(g.e, r, c + j, z[j]);
-              }
-            }
-          }
+          finish_tile<TYPE, OUT32>(g, tile, t.m0 + quarter * 32, t.n0 + c0);
         }
       }
       tmem_fence_before();
@@ -266,6 +363,54 @@ gemm_kernel(const __grid_constant__ GemmArgs g, bool aligned) {
     }
   }
   __syncwarp();
+  if (g.splits > 1 || g.turned) {
+    // One tile per block, or one part of it: the cluster's blocks add up a
+    // share each, in the order of the parts.
+    cg::cluster_group cluster = cg::this_cluster();
+    if (g.splits > 1) cluster.sync();
+    else __syncthreads();
+    const Tile t = tile_of(g, first);
+    const uint32_t shift = 31 - __clz(g.bn);
+    // four neighbours at a time, of all parts at once
+    for (uint32_t j = 4 * (part * kGemmThreads + threadIdx.x); j < kTileM * g.bn; j += 4 * g.splits * kGemmThreads) {
+      const uint32_t m = g.turned ? j & (kTileM - 1) : j >> shift, n = g.turned ? j / kTileM : j & (g.bn - 1);
+      const uint32_t at = g.turned ? j : m * (g.bn + 4) + n;
+      if (t.m0 + m >= g.m || t.n0 + n >= g.n) continue;
+      float4 v[kMostSplits];
+#pragma unroll
+      for (uint32_t s = 0; s < kMostSplits; ++s)
+        if (s < g.splits)
+          v[s] = *reinterpret_cast<const float4*>((g.splits > 1 ? cluster.map_shared_rank(ring_floats, s) : ring_floats) + at);
+      float z[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+#pragma unroll
+      for (uint32_t s = 1; s < kMostSplits; ++s) {
+        if (s >= g.splits) break;
+        z[0] += v[s].x; z[1] += v[s].y; z[2] += v[s].z; z[3] += v[s].w;
+      }
+      const uint32_t c = g.turned ? t.m0 + m : t.n0 + n, width = g.turned ? g.m : g.n;   // (columns of the product)
+      const uint64_t r = g.turned ? t.n0 + n : t.m0 + m;
+      float bias[4] = {0.f, 0.f, 0.f, 0.f};
+      if (g.e.bias.data)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (c + i < width) bias[i] = load_as(g.e.bias.data, g.e.bias.type, c + i);
+      if (g.aligned && c + 4 <= width) {
+        const uint64_t rows[1] = {r};
+        const bool has[1] = {true};
+        finish<TYPE, OUT32, 4, 1>(g.e, rows, c, has, bias, z);
+      } else {
+#pragma unroll 1
+        for (int i = 0; i < 4 && c + i < width; ++i) {
+          const uint64_t rows[1] = {r};
+          const bool has[1] = {true};
+          const float b1[1] = {i == 0 ? bias[0] : (i == 1 ? bias[1] : (i == 2 ? bias[2] : bias[3]))};
+          float z1[1] = {i == 0 ? z[0] : (i == 1 ? z[1] : (i == 2 ? z[2] : z[3]))};
+          finish<TYPE, OUT32, 1, 1>(g.e, rows, c + i, has, b1, z1);
+        }
+      }
+    }
+    if (g.splits > 1) cluster.sync();   // (others may still read here)
+  }
   tmem_fence_before();
   __syncthreads();
   tmem_fence_after();
@@ -273,26 +418,38 @@ gemm_kernel(const __grid_constant__ GemmArgs g, bool aligned) {
   if (warp == 1) tmem_give(tmem, columns);
 }
 
-// The parts of a product of rows x columns, in order, and what becomes of their sum.
-__global__ void __launch_bounds__(256)
-gemm_join_kernel(const float* parts, uint32_t splits, uint64_t rows, uint32_t columns, const __grid_constant__ Epilogue e) {
-  after_previous();
-  const uint64_t count = rows * columns;
-  for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (uint64_t)gridDim.x * 256) {
-    float z = 0.f;
-    for (uint32_t s = 0; s < splits; ++s) z += parts[s * count + i];
-    const uint64_t r = i / columns;
-    finish_one(e, r, i - r * columns, z);
-  }
-}
-
 // ---- operands ------------------------------------------------------------------------
-// rows x columns elements of a 16-bit type to rows without gaps but for `pitch`.
+// rows x columns elements of a 16-bit type to rows that begin `pitch` apart;
+// blocks of kPackRows rows x kPackColumns columns, of up to two matrices.
+constexpr uint32_t kPackRows = 4, kPackColumns = 512;
+struct PackJob {
+  const uint16_t* from;
+  uint16_t* to;
+  int64_t row_stride, col_stride;
+  uint64_t rows;
+  uint32_t columns, pitch, across;   // across: blocks of columns
+  uint32_t blocks;
+};
 __global__ void __launch_bounds__(256)
-pack_kernel(const uint16_t* from, int64_t row_stride, int64_t col_stride, uint16_t* to, uint64_t rows, uint32_t columns, uint32_t pitch) {
+pack_kernel(const PackJob x, const PackJob y) {
   after_previous();
-  for (uint64_t r = blockIdx.x; r < rows; r += gridDim.x)
-    for (uint32_t c = threadIdx.x; c < columns; c += 256) to[r * pitch + c] = from[(int64_t)r * row_stride + (int64_t)c * col_stride];
+  const bool second = blockIdx.x >= x.blocks;
+  const PackJob& p = second ? y : x;
+  const uint32_t b = second ? blockIdx.x - x.blocks : blockIdx.x;
+  const uint64_t r0 = (uint64_t)(b / p.across) * kPackRows;
+  const uint32_t c0 = b % p.across * kPackColumns + threadIdx.x;
+  uint16_t v[kPackRows][2];
+#pragma unroll
+  for (uint32_t i = 0; i < kPackRows; ++i)
+#pragma unroll
+    for (uint32_t j = 0; j < 2; ++j)
+      if (r0 + i < p.rows && c0 + j * 256 < p.columns)
+        v[i][j] = p.from[(int64_t)(r0 + i) * p.row_stride + (int64_t)(c0 + j * 256) * p.col_stride];
+#pragma unroll
+  for (uint32_t i = 0; i < kPackRows; ++i)
+#pragma unroll
+    for (uint32_t j = 0; j < 2; ++j)
+      if (r0 + i < p.rows && c0 + j * 256 < p.columns) p.to[(r0 + i) * p.pitch + c0 + j * 256] = v[i][j];
 }
 
 // A matrix of mn x k elements as an operand: how it is stored, and whether it
@@ -333,17 +490,31 @@ Operand operand(const char* data, uint64_t mn, uint32_t k, int64_t mn_stride, in
 
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
-// Copies the operand to `at` if it has to be; returns what it takes there.
-size_t pack(Operand& o, char* at, int sms, cudaStream_t stream) {
-  if (!o.packed) return 0;
-  const uint64_t rows = o.across ? o.k : o.mn;
-  const uint32_t columns = (uint32_t)(o.across ? o.mn : o.k);
+// Copies those of two operands to `at` that have to be.
+void pack(Operand& x, Operand& y, char* at, cudaStream_t stream) {
+  PackJob jobs[2]{};
+  uint64_t blocks = 0;
+  int i = 0;
+  for (Operand* o : {&x, &y}) {
+    PackJob& j = jobs[i++];
+    j.across = 1;
+    if (!o->packed) continue;
+    j.from = reinterpret_cast<const uint16_t*>(o->data);
+    j.to = reinterpret_cast<uint16_t*>(at);
+    j.row_stride = o->across ? o->k_stride : o->mn_stride;
+    j.col_stride = o->across ? o->mn_stride : o->k_stride;
+    j.rows = o->across ? o->k : o->mn;
+    j.columns = (uint32_t)(o->across ? o->mn : o->k);
+    j.pitch = (uint32_t)o->pitch;
+    j.across = (j.columns + kPackColumns - 1) / kPackColumns;
+    j.blocks = (uint32_t)((j.rows + kPackRows - 1) / kPackRows * j.across);
+    blocks += j.blocks;
+    o->data = at;
+    at += round256(o->bytes);
+  }
+  if (blocks == 0) return;
   note_launches(1);
-  launch_after(pack_kernel, (unsigned)std::min<uint64_t>(rows, (uint64_t)sms * 8), 256, 0, stream,
-               reinterpret_cast<const uint16_t*>(o.data), o.across ? o.k_stride : o.mn_stride, o.across ? o.mn_stride : o.k_stride,
-               reinterpret_cast<uint16_t*>(at), rows, columns, (uint32_t)o.pitch);
-  o.data = at;
-  return round256(o.bytes);
+  launch_after(pack_kernel, (unsigned)blocks, 256, 0, stream, jobs[0], jobs[1]);
 }
 
 // The tensor map of an operand whose tiles have `height` rows of mn.
@@ -375,7 +546,6 @@ cudaError_t tensor_map(const Operand& o, bool bf16, uint32_t height, CUtensorMap
 struct GemmPlan {
   bool turned;
   uint32_t bn, tiles_m, tiles_n, k_blocks, splits, per_split, stages;
-  size_t part_bytes;
 };
 // The product of `rows` x `columns` elements over k.
 GemmPlan gemm_plan(uint64_t rows, uint32_t columns, uint64_t k, int sms) {
@@ -389,14 +559,13 @@ GemmPlan gemm_plan(uint64_t rows, uint32_t columns, uint64_t k, int sms) {
   while (!p.turned && p.bn > 64 && (uint64_t)p.tiles_m * ((n + p.bn - 1) / p.bn) < (uint64_t)sms) p.bn /= 2;
   p.tiles_n = (uint32_t)((n + p.bn - 1) / p.bn);
   p.k_blocks = (uint32_t)((k + kBlockK - 1) / kBlockK);
-  // parts of k, of at least four blocks, while SMs are idle
+  // parts of k, of at least two blocks, while SMs are idle
   const uint64_t tiles = (uint64_t)p.tiles_m * p.tiles_n;
-  const uint64_t want = std::max<uint64_t>(1, std::min<uint64_t>((uint64_t)sms / tiles, p.k_blocks / 4));
+  const uint64_t want = std::max<uint64_t>(1, std::min<uint64_t>({(uint64_t)sms / tiles, p.k_blocks / 2, kMostSplits}));
   p.per_split = (uint32_t)((p.k_blocks + want - 1) / want);
   p.splits = (p.k_blocks + p.per_split - 1) / p.per_split;
-  p.part_bytes = p.splits > 1 ? (size_t)p.splits * rows * columns * sizeof(float) : 0;
   const uint32_t stage = kTileM * 128 + p.bn * 128;
-  p.stages = std::min(kMaxStages, (kSmem - 1024 - 512 - 4 * kStage * (uint32_t)sizeof(float)) / stage);
+  p.stages = std::min(kMaxStages, (kSmem - 1024 - 512 - kFinishWarps * kStage * (uint32_t)sizeof(float)) / stage);
   return p;
 }
 
@@ -404,9 +573,9 @@ bool on_four(const MatrixView& v, uint64_t rows) {
   return v.data == nullptr || (reinterpret_cast<uintptr_t>(v.data) % (4 * type_size(v.type)) == 0 && (rows <= 1 || v.row_stride % 4 == 0));
 }
 
-// rows x columns = left (rows x k) right (k x columns); `at`: scratch for the parts.
-cudaError_t launch_gemm(const GemmPlan& p, const Operand& left, const Operand& right, bool bf16, const Epilogue& e, char* at,
-                        DevState* st, int sms, cudaStream_t stream) {
+// rows x columns = left (rows x k) right (k x columns).
+cudaError_t launch_gemm(const GemmPlan& p, const Operand& left, const Operand& right, bool bf16, const Epilogue& e, DevState* st,
+                        int sms, cudaStream_t stream) {
   GemmArgs g{};
   const Operand& a = p.turned ? right : left;
   const Operand& b = p.turned ? left : right;
@@ -425,61 +594,87 @@ cudaError_t launch_gemm(const GemmPlan& p, const Operand& left, const Operand& r
   g.k_blocks = p.k_blocks;
   g.splits = p.splits;
   g.per_split = p.per_split;
-  g.bf16 = bf16;
-  g.parts = p.splits > 1 ? reinterpret_cast<float*>(at) : nullptr;
+  g.aligned = on_four(e.out, left.mn) && on_four(e.pre, left.mn) && on_four(e.residual, left.mn);
   g.e = e;
   g.st = st;
-  const uint64_t rows = left.mn;
-  const uint32_t columns = (uint32_t)right.mn;
-  const bool aligned = p.splits > 1 ? columns % 4 == 0
-                                    : on_four(e.out, rows) && on_four(e.pre, rows) && on_four(e.residual, rows);
-  const size_t smem = 1024 + (size_t)p.stages * (kTileM + p.bn) * 128 + 4 * kStage * sizeof(float);
-  err = cudaFuncSetAttribute(gemm_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kSmem - 1024));
+  const bool out32 = e.out.type == ADAPM_F32;
+  void (*kernel)(GemmArgs) = bf16 ? (out32 ? gemm_kernel<true, true> : gemm_kernel<true, false>)
+                                  : (out32 ? gemm_kernel<false, true> : gemm_kernel<false, false>);
+  err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kSmem - 1024));
   if (err != cudaSuccess) return err;
-  const uint64_t items = (uint64_t)p.tiles_m * p.tiles_n * p.splits;
+  // (a block whose tile goes through the ring to its epilogue takes one tile)
+  const uint64_t tiles = (uint64_t)p.tiles_m * p.tiles_n;
+  const bool single = p.splits > 1 || p.turned;
+  cudaLaunchAttribute at[2]{};
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = p.splits;
+  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t c{};
+  c.gridDim = dim3((unsigned)(single ? tiles * p.splits : std::min<uint64_t>(tiles, (uint64_t)sms)));
+  c.blockDim = dim3(kGemmThreads);
+  c.dynamicSmemBytes = 1024 + (size_t)p.stages * (kTileM + p.bn) * 128 + kFinishWarps * kStage * sizeof(float);
+  c.stream = stream;
+  c.attrs = at;
+  c.numAttrs = p.splits > 1 ? 2 : 1;
   note_launches(1);
-  launch_after(gemm_kernel, (unsigned)std::min<uint64_t>(items, (uint64_t)sms), kGemmThreads, smem, stream, g, aligned);
-  if (p.splits > 1) {
-    note_launches(1);
-    launch_after(gemm_join_kernel, (unsigned)std::min<uint64_t>((rows * columns + 255) / 256, (uint64_t)sms * 8), 256, 0, stream,
-                 (const float*)g.parts, p.splits, rows, columns, e);
-  }
-  return cudaSuccess;
+  return cudaLaunchKernelEx(&c, kernel, g);
 }
 
 // ---- the gradient of z ----------------------------------------------------------------------
-// dz = grad act'(pre) to rows of `pitch` elements (to null: grad itself serves),
-// and sums of its columns over every gridDim.y-th group of 8 rows.
-__global__ void __launch_bounds__(256)
-dz_kernel(const MatrixView grad, const MatrixView pre, int activation, char* to, uint32_t pitch, uint64_t rows, uint32_t columns, float* parts) {
+// dz = grad act'(pre) to rows of `pitch` elements (to null: grad itself
+// serves), and the sums of its columns over a block's rows: 32 N columns a
+// block, N neighbours a lane, warps take rows by turns, kDzRows at a time.
+constexpr int kDzRows = 2;
+template <int TYPE, int N>
+__global__ void __launch_bounds__(256, 4)
+dz_kernel(const MatrixView grad, const MatrixView pre, int activation, char* to, uint32_t pitch, uint64_t rows, uint32_t columns,
+          uint32_t per_block, float* parts) {
   after_previous();
-  __shared__ float sums[8][32];
+  __shared__ float sums[8][32 * N];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const uint64_t c = (uint64_t)blockIdx.x * 32 + lane;
-  float sum = 0.f;
-  if (c < columns)
-    for (uint64_t r = (uint64_t)blockIdx.y * 8 + warp; r < rows; r += (uint64_t)gridDim.y * 8) {
-      float d = load_as(grad.data, grad.type, (int64_t)r * grad.row_stride + (int64_t)c * grad.col_stride);
-      if (activation != ADAPM_ACTIVATION_NONE)
-        d *= slope(load_as(pre.data, pre.type, (int64_t)r * pre.row_stride + (int64_t)c * pre.col_stride), activation);
-      if (to != nullptr) store_as(to, grad.type, r * pitch + c, d);
-      sum += d;
+  const uint32_t across = (columns + 32 * N - 1) / (32 * N);
+  const uint32_t block = blockIdx.x / across;
+  const uint64_t c = (uint64_t)(blockIdx.x % across) * 32 * N + lane * N;
+  const uint64_t r1 = min(rows, (uint64_t)(block + 1) * per_block);
+  float sum[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) sum[j] = 0.f;
+  if (c < columns) {
+    for (uint64_t r0 = (uint64_t)block * per_block + warp; r0 < r1; r0 += 8 * kDzRows) {
+      float d[kDzRows][N], z[kDzRows][N];
+#pragma unroll
+      for (int i = 0; i < kDzRows; ++i)
+        if (r0 + i * 8 < r1)
+          load_n<TYPE, N>(grad.data + ((int64_t)(r0 + i * 8) * grad.row_stride + (int64_t)c * grad.col_stride) * 2, d[i]);
+      if (activation != ADAPM_ACTIVATION_NONE) {
+#pragma unroll
+        for (int i = 0; i < kDzRows; ++i)
+          if (r0 + i * 8 < r1)
+            load_n<TYPE, N>(pre.data + ((int64_t)(r0 + i * 8) * pre.row_stride + (int64_t)c * pre.col_stride) * 2, z[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < kDzRows; ++i) {
+        if (r0 + i * 8 >= r1) continue;
+        times_slope(d[i], z[i], activation);
+        if (to != nullptr) store_n<TYPE, N>(to + ((r0 + i * 8) * pitch + c) * 2, d[i]);
+#pragma unroll
+        for (int j = 0; j < N; ++j) sum[j] += d[i][j];
+      }
     }
+  }
   if (parts == nullptr) return;
-  sums[warp][lane] = sum;
+#pragma unroll
+  for (int j = 0; j < N; ++j) sums[warp][lane * N + j] = sum[j];
   __syncthreads();
-  if (warp != 0 || c >= columns) return;
-  for (int w = 1; w < 8; ++w) sum += sums[w][lane];
-  parts[blockIdx.y * (uint64_t)columns + c] = sum;
-}
-__global__ void __launch_bounds__(256)
-bias_join_kernel(const float* parts, uint32_t count, uint32_t columns, VectorView out) {
-  after_previous();
-  const uint64_t c = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-  if (c >= columns) return;
-  float s = 0.f;
-  for (uint32_t p = 0; p < count; ++p) s += parts[p * (uint64_t)columns + c];
-  store_as(out.data, out.type, c, s);
+  for (int i = threadIdx.x; i < 32 * N; i += 256) {
+    const uint64_t column = (uint64_t)(blockIdx.x % across) * 32 * N + i;
+    if (column >= columns) continue;
+    float s = 0.f;
+    for (int w = 0; w < 8; ++w) s += sums[w][i];
+    parts[block * (uint64_t)columns + column] = s;
+  }
 }
 
 bool by_rows(const MatrixView& m, uint64_t rows, uint32_t columns) {   // stored with a row's elements contiguous
@@ -492,17 +687,16 @@ size_t linear_scratch(const LinearArgs& a, int sms) {
   const GemmPlan p = gemm_plan(a.rows, a.outs, a.ins, sms);
   const Operand x = operand(a.x.data, a.rows, a.ins, a.x.row_stride, a.x.col_stride, p.turned);
   const Operand w = operand(a.weight.data, a.outs, a.ins, a.weight.col_stride, a.weight.row_stride, false);
-  return round256(x.bytes) + round256(w.bytes) + p.part_bytes;
+  return round256(x.bytes) + round256(w.bytes);
 }
 
 cudaError_t launch_linear(const LinearArgs& a, char* scratch, int sms, cudaStream_t stream) {
   const GemmPlan p = gemm_plan(a.rows, a.outs, a.ins, sms);
   Operand x = operand(a.x.data, a.rows, a.ins, a.x.row_stride, a.x.col_stride, p.turned);
   Operand w = operand(a.weight.data, a.outs, a.ins, a.weight.col_stride, a.weight.row_stride, false);
-  scratch += pack(x, scratch, sms, stream);
-  scratch += pack(w, scratch, sms, stream);
+  pack(x, w, scratch, stream);
   const Epilogue e{a.bias, a.residual, a.out, a.pre, a.activation};
-  return launch_gemm(p, x, w, a.x.type == ADAPM_BF16, e, scratch, a.st, sms, stream);
+  return launch_gemm(p, x, w, a.x.type == ADAPM_BF16, e, a.st, sms, stream);
 }
 
 namespace {
@@ -511,27 +705,37 @@ namespace {
 // products, and their scratch, one after the other.
 struct Backward {
   bool own_dz;
-  uint32_t pitch, chunks;
+  uint32_t pitch;
   MatrixView dz;
-  bool across_out;   // dweight is stored by output: its transpose is computed
+  bool across_out;     // dweight is stored by output: its transpose is computed
+  int vec;             // elements of an access of dz_kernel
+  uint32_t across, blocks, per_block;   // its blocks: of columns, of rows, and their rows
   size_t dz_bytes, sum_bytes;
 };
-constexpr uint32_t kRowChunks = 64;
-Backward backward_of(const LinearArgs& a, char* scratch) {
+Backward backward_of(const LinearArgs& a, char* scratch, int sms) {
   Backward b{};
   b.own_dz = a.activation != ADAPM_ACTIVATION_NONE && (a.dx.data || a.dweight.data);
   b.pitch = (a.outs + 7) / 8 * 8;
   b.dz_bytes = b.own_dz ? round256(a.rows * (size_t)b.pitch * 2) : 0;
-  b.chunks = (uint32_t)std::min<uint64_t>((a.rows + 7) / 8, kRowChunks);
-  b.sum_bytes = a.dbias.data ? round256((size_t)b.chunks * a.outs * sizeof(float)) : 0;
   b.dz = b.own_dz ? MatrixView{scratch, a.grad.type, (int64_t)b.pitch, 1} : a.grad;
   b.across_out = a.dweight.data && !by_rows(a.dweight, a.ins, a.outs);
+  // eight neighbours where rows begin and end on them, else one
+  auto on_eight = [&](const MatrixView& m) {
+    return m.data == nullptr || (m.col_stride == 1 && reinterpret_cast<uintptr_t>(m.data) % 16 == 0 && (a.rows <= 1 || m.row_stride % 8 == 0));
+  };
+  b.vec = a.outs % 8 == 0 && on_eight(a.grad) && on_eight(a.pre) ? 8 : 1;
+  b.across = (a.outs + 32 * b.vec - 1) / (32 * b.vec);
+  // about eight blocks an SM, of at least 32 rows
+  const uint64_t want = std::max<uint64_t>(1, (uint64_t)sms * 8 / b.across);
+  b.per_block = (uint32_t)std::max<uint64_t>(32, (a.rows + want - 1) / want);
+  b.blocks = (uint32_t)((a.rows + b.per_block - 1) / b.per_block);
+  b.sum_bytes = a.dbias.data ? round256((size_t)b.blocks * a.outs * sizeof(float)) : 0;
   return b;
 }
 struct Product {
   GemmPlan p;
   Operand left, right;
-  size_t bytes() const { return round256(left.bytes) + round256(right.bytes) + round256(p.part_bytes); }
+  size_t bytes() const { return round256(left.bytes) + round256(right.bytes); }
 };
 Product dx_product(const LinearArgs& a, const Backward& b, int sms) {   // rows x ins over outs
   Product q;
@@ -552,10 +756,19 @@ Product dweight_product(const LinearArgs& a, const Backward& b, int sms) {   // 
   return q;
 }
 
+template <int TYPE>
+void launch_dz(const LinearArgs& a, const Backward& b, float* sums, cudaStream_t stream) {
+  note_launches(1);
+  char* const to = b.own_dz ? b.dz.data : nullptr;
+  const unsigned grid = b.across * b.blocks;
+  if (b.vec == 8) launch_after(dz_kernel<TYPE, 8>, grid, 256, 0, stream, a.grad, a.pre, a.activation, to, b.pitch, a.rows, a.outs, b.per_block, sums);
+  else launch_after(dz_kernel<TYPE, 1>, grid, 256, 0, stream, a.grad, a.pre, a.activation, to, b.pitch, a.rows, a.outs, b.per_block, sums);
+}
+
 }  // namespace
 
 size_t linear_grad_scratch(const LinearArgs& a, int sms) {
-  const Backward b = backward_of(a, nullptr);
+  const Backward b = backward_of(a, nullptr, sms);
   size_t most = 0;   // (the products follow each other: they share)
   if (a.dx.data) most = std::max(most, dx_product(a, b, sms).bytes());
   if (a.dweight.data) most = std::max(most, dweight_product(a, b, sms).bytes());
@@ -563,30 +776,23 @@ size_t linear_grad_scratch(const LinearArgs& a, int sms) {
 }
 
 cudaError_t launch_linear_grad(const LinearArgs& a, char* scratch, int sms, cudaStream_t stream) {
-  const Backward b = backward_of(a, scratch);
+  const Backward b = backward_of(a, scratch, sms);
   float* const sums = a.dbias.data ? reinterpret_cast<float*>(scratch + b.dz_bytes) : nullptr;
   char* const rest = scratch + b.dz_bytes + b.sum_bytes;
   const bool bf16 = a.x.type == ADAPM_BF16;
   if (b.own_dz || a.dbias.data) {
-    note_launches(1);
-    // (the grid has two dimensions: launched plainly)
-    dz_kernel<<<dim3((a.outs + 31) / 32, b.chunks), 256, 0, stream>>>(a.grad, a.pre, a.activation, b.own_dz ? b.dz.data : nullptr,
-                                                                      b.pitch, a.rows, a.outs, sums);
+    if (bf16) launch_dz<ADAPM_BF16>(a, b, sums, stream);
+    else launch_dz<ADAPM_F16>(a, b, sums, stream);
   }
-  if (a.dbias.data) {
-    note_launches(1);
-    launch_after(bias_join_kernel, (a.outs + 255) / 256, 256, 0, stream, (const float*)sums, b.chunks, a.outs, a.dbias);
-  }
+  if (a.dbias.data) launch_column_join(sums, b.blocks, a.outs, a.outs, a.dbias, VectorView{nullptr, ADAPM_F32}, stream);
   for (int which = 0; which < 2; ++which) {
     if ((which ? a.dweight.data : a.dx.data) == nullptr) continue;
     Product q = which ? dweight_product(a, b, sms) : dx_product(a, b, sms);
-    char* at = rest;
-    at += pack(q.left, at, sms, stream);
-    at += pack(q.right, at, sms, stream);
+    pack(q.left, q.right, rest, stream);
     Epilogue e{};
     e.out = which ? a.dweight : a.dx;
     if (which && b.across_out) std::swap(e.out.row_stride, e.out.col_stride);
-    const cudaError_t err = launch_gemm(q.p, q.left, q.right, bf16, e, at, a.st, sms, stream);
+    const cudaError_t err = launch_gemm(q.p, q.left, q.right, bf16, e, a.st, sms, stream);
     if (err != cudaSuccess) return err;
   }
   return cudaSuccess;

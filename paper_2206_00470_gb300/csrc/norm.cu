@@ -387,14 +387,14 @@ norm_columns_kernel(const __grid_constant__ NormArgs a) {
   out[a.dim + c] = db;
 }
 
-// The sums of `count` blocks, in a fixed order: 32 columns a block, every warp
-// takes each 32nd block's sums, four of them on their way at a time.
+// The sums of `count` blocks over `width` columns, in a fixed order: 32 columns
+// a block, every warp takes each 32nd block's sums, four of them on their way
+// at a time.
 __global__ void __launch_bounds__(1024)
-norm_join_kernel(const float* parts, uint32_t count, uint32_t dim, VectorView dweight, VectorView dbias) {
+column_join_kernel(const float* parts, uint32_t count, uint64_t width, uint32_t dim, VectorView low, VectorView high) {
   after_previous();
   __shared__ float sums[32][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const uint64_t width = 2ull * dim;   // columns of both
   const uint64_t c = (uint64_t)blockIdx.x * 32 + lane;
   float s = 0.f;
   if (c < width) {
@@ -412,7 +412,7 @@ norm_join_kernel(const float* parts, uint32_t count, uint32_t dim, VectorView dw
   s = lanes_sum(sums[lane][warp], 32);
   const uint64_t mine = (uint64_t)blockIdx.x * 32 + warp;
   if (lane != 0 || mine >= width) return;
-  const VectorView& v = mine < dim ? dweight : dbias;
+  const VectorView& v = mine < dim ? low : high;
   if (v.data != nullptr) store_as(v.data, v.type, mine < dim ? mine : mine - dim, s);
 }
 
@@ -510,10 +510,14 @@ void launch_layer_norm_grad(const NormArgs& a, int sms, cudaStream_t stream) {
     }
   }
   if (a.parts != nullptr) {
-    note_launches(1);
-    launch_after(norm_join_kernel, (unsigned)((2ull * a.dim + 31) / 32), 1024, 0, stream, (const float*)a.parts, (uint32_t)count,
-                 a.dim, a.dweight, a.dbias);
+    launch_column_join(a.parts, (uint32_t)count, 2ull * a.dim, a.dim, a.dweight, a.dbias, stream);
   }
+}
+
+void launch_column_join(const float* parts, uint32_t count, uint64_t width, uint32_t dim, const VectorView& low,
+                        const VectorView& high, cudaStream_t stream) {
+  note_launches(1);
+  launch_after(column_join_kernel, (unsigned)((width + 31) / 32), 1024, 0, stream, parts, count, width, dim, low, high);
 }
 
 }  // namespace adapm
