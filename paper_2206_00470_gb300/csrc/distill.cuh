@@ -13,17 +13,21 @@
 // that every element has, from one reading.  distill_marks, a warp per row:
 // the loss, and the few elements that list and label change.
 //
-// distill_rows keeps a row in registers, packed as it came: eight 16-byte
-// words a thread, and where a block is too small the blocks of a cluster take
-// a slice of the row each and exchange their warps' sums through shared
-// memory.  Every warp sums relative to its own maximum, so one exchange per row
-// is enough.  Bound by memory: a read and a write of the logits.
+// The second launch comes in three forms.  distill_rows, for rows of up to 32
+// KB: a block keeps its row in registers, packed as it came.  distill_slices,
+// up to 1 MB: the blocks of a cluster keep a slice of the row each, which was
+// copied to shared memory while they worked on the row before it, and exchange
+// their sums.  distill_long: the blocks of a cluster read a slice twice, the
+// second time from L2.
+// Every warp sums relative to its own maximum, so one exchange per row is
+// enough.  Bound by memory: a read and a write of the logits.
 #pragma once
 
 #include <cooperative_groups.h>
 
 #include <algorithm>
 
+#include "barrier.cuh"
 #include "dense.cuh"
 
 namespace adapm {
@@ -107,13 +111,10 @@ __device__ __forceinline__ uint4 load_word(const RowWords& b, uint32_t vocab, ui
   if (w < b.words) return load_edge<TYPE>(b.base, b.head, vocab, w);
   return make_uint4(Word<TYPE>::kNone, Word<TYPE>::kNone, Word<TYPE>::kNone, Word<TYPE>::kNone);
 }
-// The elements of word w of another row of the same elements, whose words
-// begin `shift` elements (less than a word's) further on in b's.
+// A word's worth of elements from number `shift` (less than a word's) of two
+// words on.
 template <int TYPE>
-__device__ __forceinline__ uint4 load_shifted(const RowWords& b, uint32_t vocab, uint32_t w, uint32_t shift) {
-  const uint4 lo = load_word<TYPE>(b, vocab, w);
-  if (shift == 0) return lo;
-  const uint4 hi = load_word<TYPE>(b, vocab, w + 1);
+__device__ __forceinline__ uint4 shift_words(const uint4& lo, const uint4& hi, uint32_t shift) {
   uint32_t x[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
   const uint32_t bytes = shift * Word<TYPE>::kSize;
   if (bytes & 8u)
@@ -125,6 +126,14 @@ __device__ __forceinline__ uint4 load_shifted(const RowWords& b, uint32_t vocab,
   const uint32_t bits = (bytes & 3u) * 8u;
   return make_uint4(__funnelshift_r(x[0], x[1], bits), __funnelshift_r(x[1], x[2], bits), __funnelshift_r(x[2], x[3], bits),
                     __funnelshift_r(x[3], x[4], bits));
+}
+// The elements of word w of another row of the same elements, whose words
+// begin `shift` elements further on in b's.
+template <int TYPE>
+__device__ __forceinline__ uint4 load_shifted(const RowWords& b, uint32_t vocab, uint32_t w, uint32_t shift) {
+  const uint4 lo = load_word<TYPE>(b, vocab, w);
+  if (shift == 0) return lo;
+  return shift_words<TYPE>(lo, load_word<TYPE>(b, vocab, w + 1), shift);
 }
 template <int TYPE>
 __device__ __noinline__ void store_edge(char* base, uint32_t head, uint32_t vocab, uint32_t w, uint4 v) {
@@ -320,18 +329,34 @@ __device__ __forceinline__ uint64_t pair_at(const uint4& v, int j) {
     return pair_of(f.x, f.y);
   }
 }
+// The largest of the elements seen, kept packed.
 template <int TYPE>
-__device__ __forceinline__ float largest_of(const uint4& v) {
-  if constexpr (TYPE == ADAPM_F32) {
-    return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
-  } else {
-    using H = typename std::conditional<TYPE == ADAPM_BF16, __nv_bfloat162, __half2>::type;
-    auto h = [](uint32_t w) { return *reinterpret_cast<const H*>(&w); };
-    const H m = __hmax2(__hmax2(h(v.x), h(v.y)), __hmax2(h(v.z), h(v.w)));
-    const float2 f = unpack2<TYPE>(*reinterpret_cast<const uint32_t*>(&m));
-    return fmaxf(f.x, f.y);
+struct Largest {
+  using H = typename std::conditional<TYPE == ADAPM_BF16, __nv_bfloat162, __half2>::type;
+  uint32_t m = Word<TYPE>::kNone;
+  __device__ __forceinline__ void see(uint32_t w) {
+    if constexpr (TYPE == ADAPM_F32) {
+      m = __float_as_uint(fmaxf(__uint_as_float(m), __uint_as_float(w)));
+    } else {
+      const H x = __hmax2(*reinterpret_cast<const H*>(&m), *reinterpret_cast<const H*>(&w));
+      m = *reinterpret_cast<const uint32_t*>(&x);
+    }
   }
-}
+  __device__ __forceinline__ void see(const uint4& v) {
+    see(v.x);
+    see(v.y);
+    see(v.z);
+    see(v.w);
+  }
+  __device__ __forceinline__ float value() const {
+    if constexpr (TYPE == ADAPM_F32) {
+      return __uint_as_float(m);
+    } else {
+      const float2 f = unpack2<TYPE>(m);
+      return fmaxf(f.x, f.y);
+    }
+  }
+};
 // Where max c is this large, logits are taken relative to the largest before
 // they are multiplied (which would lose too much, or overflow).  Those within
 // the exponential's range of it share its leading bits, so their differences
@@ -359,176 +384,506 @@ __device__ __forceinline__ float unround(float max, float c) {
   return exp2_of(-fmaf(max, c, -k));
 }
 
-// Blocks per SM that the registers allow: 32 of a thread hold eight words.
-constexpr int resident_blocks(int threads, int words) { return (words == 8 ? 1024 : 1536) / threads; }
 __device__ __forceinline__ float finite_shift(float m) { return m == -INFINITY ? 0.f : m; }
+__device__ __forceinline__ bool is_huge(float max, float per) { return fabsf(max * kLog2E) > kHuge || fabsf(max * per) > kHuge; }
 
-// NV words a thread in registers (0: the row is read again for its gradient).
-// TWO: sums at both temperatures.  Launched in clusters of `split` blocks per row.
-template <int TYPE, int THREADS, int NV, bool TWO>
-__global__ void __launch_bounds__(THREADS, resident_blocks(THREADS, NV))
-distill_rows_kernel(const __grid_constant__ DistillArgs a, int split) {
-  after_previous();
-  constexpr int E = Word<TYPE>::kElements, WARPS = THREADS / 32, KEPT = NV > 0 ? NV : 1;
-  __shared__ RowSums sums[2][kMaxCluster * WARPS];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int rank = split > 1 ? (int)(blockIdx.x % split) : 0;
-  const uint64_t rows = gridDim.x / split;
-  // exp((s - m) / T) = 2^((s - m) per); the one temperature of a row without TWO
-  const float per = a.top > 0 ? kLog2E / a.temperature : kLog2E;
-  const RowTask* const tasks = static_cast<const RowTask*>(a.tasks);
-  uint64_t row = blockIdx.x / split;
-  RowTask next = tasks[row < a.n ? row : 0];
-  for (int turn = 0; row < a.n; row += rows, turn ^= 1) {
-    const RowTask task = next;
-    const bool live = task.some || task.label >= 0;
-    const RowWords b = row_words<TYPE>(a.logits, row, a.vocab);
-    const uint32_t slice = (b.words + split - 1) / split;
-    const uint32_t w0 = rank * slice, w1 = min(b.words, w0 + slice);
-    uint4 v[KEPT];
-    RowSums mine{-INFINITY, 0.f, 0.f};
-    if (live && NV > 0) {
+// Adds the sums of 2^(s c - k) over the elements of a word, two by two.
+template <int TYPE>
+__device__ __forceinline__ void add_word(const uint4& word, uint64_t c, uint64_t minus_k, uint64_t& to) {
 #pragma unroll
-      for (int i = 0; i < KEPT; ++i) {
-        const uint32_t w = w0 + i * THREADS + threadIdx.x;
-        v[i] = make_uint4(Word<TYPE>::kNone, Word<TYPE>::kNone, Word<TYPE>::kNone, Word<TYPE>::kNone);
-        if (w < w1) v[i] = load_word<TYPE>(b, a.vocab, w);
-      }
-    }
-    if (row + rows < a.n) next = tasks[row + rows];
-    if (live) {
-      // sums of 2^(s c - k), two by two; k = max c
-      auto add = [&](const uint4& word, uint64_t c, uint64_t minus_k, uint64_t& to) {
+  for (int j = 0; j < Word<TYPE>::kElements / 2; ++j) {
+    const float2 d = floats_of(fma_pair(pair_at<TYPE>(word, j), c, minus_k));
+    to = add_pair(to, pair_of(exp2_of(d.x), exp2_of(d.y)));
+  }
+}
+
+// What turns a row's logits into the part of the gradient that every element
+// has: st 2^(s per - k) + so 2^(s log2(e) - k1).
+struct RowFactors {
+  float minus_k, st, minus_k1, so;
+  float max;
+  bool huge;
+  bool folded;   // st is part of the exponent
+};
+template <int TYPE, bool TWO>
+__device__ __forceinline__ RowFactors row_factors(const DistillArgs& a, uint64_t row, const RowTask& task, const RowSums& all, float per) {
+  const RowScale scale = row_scale(a, row, task, all, TWO);
+  RowFactors f;
+  f.max = all.max;
+  f.huge = is_huge(all.max, per);
+  const float k = f.huge ? 0.f : all.max;
+  f.st = scale.t * unround(k, per);
+  f.so = TWO ? scale.one * unround(k, kLog2E) : 0.f;
+  // 16-bit gradients of one exponential: the factor is added to the exponent (off by 2^-18 of the result at most)
+  f.folded = !TWO && TYPE != ADAPM_F32 && f.st >= 0.f;
+  f.minus_k = -(k * per) + (f.folded ? log2f(f.st) : 0.f);
+  f.minus_k1 = -(k * kLog2E);
+  return f;
+}
+template <int TYPE, bool TWO, bool FOLD>
+struct Gradient {
+  uint64_t c, m, ct, c1, m1, co;
+  __device__ __forceinline__ Gradient(const RowFactors& f, float per)
+      : c(pair_of(per, per)), m(pair_of(f.minus_k, f.minus_k)), ct(pair_of(f.st, f.st)), c1(pair_of(kLog2E, kLog2E)),
+        m1(pair_of(f.minus_k1, f.minus_k1)), co(pair_of(f.so, f.so)) {}
+  __device__ __forceinline__ uint4 of(const uint4& word) const {
+    constexpr int E = Word<TYPE>::kElements;
+    float x[E];
 #pragma unroll
-        for (int j = 0; j < E / 2; ++j) {
-          const float2 d = floats_of(fma_pair(pair_at<TYPE>(word, j), c, minus_k));
-          to = add_pair(to, pair_of(exp2_of(d.x), exp2_of(d.y)));
-        }
-      };
-      uint64_t st = 0, so = 0;
-      if constexpr (NV > 0) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i) mine.max = fmaxf(mine.max, largest_of<TYPE>(v[i]));
-        mine.max = lanes_max(mine.max);
-        float shift = finite_shift(mine.max);
-        const bool huge = fabsf(shift * kLog2E) > kHuge || fabsf(shift * per) > kHuge;
-        if (huge) {
-#pragma unroll
-          for (int i = 0; i < NV; ++i) take_off<TYPE>(v[i], shift);
-        }
-        const float k = huge ? 0.f : shift;
-        const uint64_t c = pair_of(per, per), m = pair_of(-(k * per), -(k * per));
-#pragma unroll
-        for (int i = 0; i < NV; ++i) add(v[i], c, m, st);
-        if (TWO) {
-          const uint64_t c1 = pair_of(kLog2E, kLog2E), m1 = pair_of(-(k * kLog2E), -(k * kLog2E));
-#pragma unroll
-          for (int i = 0; i < NV; ++i) add(v[i], c1, m1, so);
-        }
-        if (huge) {   // (as they were: the gradient is relative to the whole row's largest)
-#pragma unroll
-          for (int i = 0; i < NV; ++i) {
-            const uint32_t w = w0 + i * THREADS + threadIdx.x;
-            if (w < w1) v[i] = load_word<TYPE>(b, a.vocab, w);
-          }
-        }
-        const float2 t = floats_of(st), o = floats_of(so);
-        mine.t = (t.x + t.y) * unround(k, per);
-        mine.one = TWO ? (o.x + o.y) * unround(k, kLog2E) : 0.f;
-      } else {
-        for (uint32_t w = w0 + threadIdx.x; w < w1; w += THREADS) {
-          const uint4 word = load_word<TYPE>(b, a.vocab, w);
-          const float max = fmaxf(mine.max, largest_of<TYPE>(word));
-          const float shift = finite_shift(max);
-          if (max > mine.max && mine.max != -INFINITY) {   // (sums of nothing are 0)
-            mine.t *= exp2_of((mine.max - max) * per);
-            mine.one *= exp2_of((mine.max - max) * kLog2E);
-          }
-          mine.max = max;
-          float x[E];
-          unpack_word<TYPE>(word, x);
-#pragma unroll
-          for (int j = 0; j < E; ++j) {
-            mine.t += exp2_of((x[j] - shift) * per);
-            if (TWO) mine.one += exp2_of((x[j] - shift) * kLog2E);
-          }
-        }
-        const float top = lanes_max(mine.max);
-        if (mine.max != -INFINITY) {
-          mine.t *= exp2_of((mine.max - top) * per);
-          mine.one *= exp2_of((mine.max - top) * kLog2E);
-        }
-        mine.max = top;
-      }
-      mine.t = lanes_sum(mine.t, 32);
-      if (TWO) mine.one = lanes_sum(mine.one, 32);
-    }
-    // one exchange: every warp's sums to every block of the cluster
-    if (split > 1) {
-      cg::cluster_group cluster = cg::this_cluster();
-      if (lane < split) cluster.map_shared_rank(&sums[turn][0], lane)[rank * WARPS + warp] = mine;
-      cluster.sync();
-    } else {
-      if (lane == 0) sums[turn][warp] = mine;
-      __syncthreads();
-    }
-    RowSums all{-INFINITY, 0.f, 0.f};
-    if (live) {
-      for (int i = lane; i < split * WARPS; i += 32) all.max = fmaxf(all.max, sums[turn][i].max);
-      all.max = lanes_max(all.max);
-      for (int i = lane; i < split * WARPS; i += 32) {
-        const RowSums& s = sums[turn][i];
-        const float down = s.max - all.max;   // (-inf: the warp has no logit above -inf, its sums are 0)
-        all.t += s.t * exp2_of(down * per);
-        if (TWO) all.one += s.one * exp2_of(down * kLog2E);
-      }
-      all.t = lanes_sum(all.t, 32);
-      if (TWO) all.one = lanes_sum(all.one, 32);
-      if (rank == 0 && threadIdx.x == 0) static_cast<RowSums*>(a.sums)[row] = all;
-    }
-    if (a.grad.data == nullptr) continue;
-    const RowWords g = row_words<TYPE>(a.grad, row, a.vocab);
-    const uint32_t w1g = rank == split - 1 ? g.words : min(g.words, w0 + slice);
-    if (!live) {
-      for (uint32_t w = w0 + threadIdx.x; w < w1g; w += THREADS) store_word<TYPE>(g, a.vocab, w, make_uint4(0, 0, 0, 0));
-      continue;
-    }
-    const RowScale scale = row_scale(a, row, task, all, TWO);
-    const bool huge = fabsf(all.max * kLog2E) > kHuge || fabsf(all.max * per) > kHuge;
-    const float k = huge ? 0.f : all.max;
-    const uint64_t c = pair_of(per, per), m = pair_of(-(k * per), -(k * per)), ct = pair_of(scale.t * unround(k, per), scale.t * unround(k, per));
-    const uint64_t c1 = pair_of(kLog2E, kLog2E), m1 = pair_of(-(k * kLog2E), -(k * kLog2E)), co = pair_of(scale.one * unround(k, kLog2E), scale.one * unround(k, kLog2E));
-    auto gradient = [&](uint4 word) {
-      if (huge) take_off<TYPE>(word, all.max);
-      float x[E];
-#pragma unroll
-      for (int j = 0; j < E / 2; ++j) {
-        const uint64_t s = pair_at<TYPE>(word, j);
-        const float2 d = floats_of(fma_pair(s, c, m));
-        uint64_t y = mul_pair(pair_of(exp2_of(d.x), exp2_of(d.y)), ct);
+    for (int j = 0; j < E / 2; ++j) {
+      const uint64_t s = pair_at<TYPE>(word, j);
+      const float2 d = floats_of(fma_pair(s, c, m));
+      float2 f = make_float2(exp2_of(d.x), exp2_of(d.y));
+      if (!FOLD) {
+        uint64_t y = mul_pair(pair_of(f.x, f.y), ct);
         if (TWO) {
           const float2 d1 = floats_of(fma_pair(s, c1, m1));
           y = fma_pair(pair_of(exp2_of(d1.x), exp2_of(d1.y)), co, y);
         }
-        const float2 f = floats_of(y);
-        x[2 * j] = f.x;
-        x[2 * j + 1] = f.y;
+        f = floats_of(y);
       }
-      return pack_word<TYPE>(x);
-    };
-    if (NV > 0 && g.head == b.head) {
-#pragma unroll
-      for (int i = 0; i < KEPT; ++i) {
-        const uint32_t w = w0 + i * THREADS + threadIdx.x;
-        if (w < w1) store_word<TYPE>(g, a.vocab, w, gradient(v[i]));
-      }
-    } else {
-      // words of the gradient that begin elsewhere: the row again, from L2
-      const uint32_t shift = (b.head - g.head) & (E - 1), back = b.head < g.head ? 1 : 0;
-      for (uint32_t w = w0 + threadIdx.x; w < w1g; w += THREADS)
-        store_word<TYPE>(g, a.vocab, w, gradient(load_shifted<TYPE>(b, a.vocab, w - back, shift)));
+      x[2 * j] = f.x;
+      x[2 * j + 1] = f.y;
     }
+    return pack_word<TYPE>(x);
   }
+};
+// fn(Gradient) in the form that the row's factors ask for.
+template <int TYPE, bool TWO, class F>
+__device__ __forceinline__ void with_gradient(const RowFactors& f, float per, F&& fn) {
+  if constexpr (!TWO && TYPE != ADAPM_F32) {
+    if (f.folded) return fn(Gradient<TYPE, TWO, true>(f, per));
+  }
+  fn(Gradient<TYPE, TWO, false>(f, per));
+}
+
+// Sums of several parts of a row, relative to the largest of all: `count` of
+// them, of which the lane has number `lane` (at most 32).
+template <bool TWO>
+__device__ __forceinline__ RowSums merge_sums(const RowSums& s, int count, float per) {
+  const int lane = threadIdx.x & 31;
+  RowSums all;
+  all.max = lanes_max(lane < count ? s.max : -INFINITY);
+  // (-inf: a part without logits above it, its sums are 0; all of -inf: NaN, as a softmax of nothing is)
+  const float down = s.max - all.max;
+  all.t = lanes_sum(lane < count ? s.t * exp2_of(down * per) : 0.f, 32);
+  all.one = TWO ? lanes_sum(lane < count ? s.one * exp2_of(down * kLog2E) : 0.f, 32) : 0.f;
+  return all;
+}
+
+// ---- rows in registers ------------------------------------------------------------
+// Blocks per SM that the registers allow: 32 of a thread hold eight words.
+constexpr int resident_blocks(int threads, int words) { return (words == 8 ? 1024 : 1536) / threads; }
+
+// NV words a thread; TWO: sums at both temperatures.
+template <int TYPE, int THREADS, int NV, bool TWO>
+__global__ void __launch_bounds__(THREADS, resident_blocks(THREADS, NV))
+distill_rows_kernel(const __grid_constant__ DistillArgs a) {
+  after_previous();
+  constexpr int E = Word<TYPE>::kElements, WARPS = THREADS / 32;
+  __shared__ RowSums warps[2][WARPS];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  // exp((s - m) / T) = 2^((s - m) per); the one temperature of a row without TWO
+  const float per = a.top > 0 ? kLog2E / a.temperature : kLog2E;
+  const RowTask* const tasks = static_cast<const RowTask*>(a.tasks);
+  uint64_t row = blockIdx.x;
+  RowTask next = tasks[row];
+  for (int turn = 0; row < a.n; row += gridDim.x, turn ^= 1) {
+    const RowTask task = next;
+    const bool live = task.some || task.label >= 0;
+    const RowWords b = row_words<TYPE>(a.logits, row, a.vocab);
+    uint4 v[NV];
+    if (live) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) v[i] = load_word<TYPE>(b, a.vocab, i * THREADS + threadIdx.x);
+    }
+    if (row + gridDim.x < a.n) next = tasks[row + gridDim.x];
+    RowSums all{-INFINITY, 0.f, 0.f};
+    if (live) {
+      Largest<TYPE> largest;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) largest.see(v[i]);
+      RowSums mine;
+      mine.max = lanes_max(largest.value());
+      const float shift = finite_shift(mine.max);
+      const bool huge = is_huge(shift, per);
+      if (huge) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) take_off<TYPE>(v[i], shift);
+      }
+      const float k = huge ? 0.f : shift;
+      uint64_t st = 0, so = 0;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) add_word<TYPE>(v[i], pair_of(per, per), pair_of(-(k * per), -(k * per)), st);
+      if (TWO) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) add_word<TYPE>(v[i], pair_of(kLog2E, kLog2E), pair_of(-(k * kLog2E), -(k * kLog2E)), so);
+      }
+      if (huge) {   // (as they were: the gradient is relative to the whole row's largest)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) v[i] = load_word<TYPE>(b, a.vocab, i * THREADS + threadIdx.x);
+      }
+      const float2 t = floats_of(st), o = floats_of(so);
+      mine.t = lanes_sum((t.x + t.y) * unround(k, per), 32);
+      mine.one = TWO ? lanes_sum((o.x + o.y) * unround(k, kLog2E), 32) : 0.f;
+      if (lane == 0) warps[turn][warp] = mine;
+    }
+    __syncthreads();
+    if (live) {
+      all = merge_sums<TWO>(lane < WARPS ? warps[turn][lane] : RowSums{-INFINITY, 0.f, 0.f}, WARPS, per);
+      if (threadIdx.x == 0) static_cast<RowSums*>(a.sums)[row] = all;
+    }
+    if (a.grad.data == nullptr) continue;
+    const RowWords g = row_words<TYPE>(a.grad, row, a.vocab);
+    if (!live) {
+      for (uint32_t w = threadIdx.x; w < g.words; w += THREADS) store_word<TYPE>(g, a.vocab, w, make_uint4(0, 0, 0, 0));
+      continue;
+    }
+    const RowFactors f = row_factors<TYPE, TWO>(a, row, task, all, per);
+    with_gradient<TYPE, TWO>(f, per, [&](const auto& gradient) {
+      if (g.head == b.head) {
+        if (f.huge) {
+#pragma unroll
+          for (int i = 0; i < NV; ++i) take_off<TYPE>(v[i], f.max);
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) store_word<TYPE>(g, a.vocab, i * THREADS + threadIdx.x, gradient.of(v[i]));
+      } else {
+        // words of the gradient that begin elsewhere: the row again, from L1 and L2
+        const uint32_t shift = (b.head - g.head) & (E - 1), back = b.head < g.head ? 1 : 0;
+        for (uint32_t w = threadIdx.x; w < g.words; w += THREADS) {
+          uint4 word = load_shifted<TYPE>(b, a.vocab, w - back, shift);
+          if (f.huge) take_off<TYPE>(word, f.max);
+          store_word<TYPE>(g, a.vocab, w, gradient.of(word));
+        }
+      }
+    });
+  }
+}
+
+// ---- rows in slices -----------------------------------------------------------------
+// A cluster of `split` blocks takes a row, each a slice of it: kSliceWarps warps
+// work, one copies the next row's slice to shared memory as soon as they have
+// taken this one's to their registers (NV words a thread), adds up their sums,
+// exchanges the blocks', and prepares the row's factors.  With two or three
+// blocks an SM, one's exchange and stores run beside another's sums.
+constexpr int kSliceWarps = 7, kSliceWork = 32 * kSliceWarps, kSliceThreads = kSliceWork + 32;
+// Words of a thread, and blocks per SM: of the 128 registers that eight warps of
+// two blocks have 72 hold words, of the 80 of three blocks' 36.
+constexpr int kManyWords = 18, kFewWords = 9;
+constexpr int slice_blocks(int words) { return words == kManyWords ? 2 : 3; }
+constexpr uint32_t kNap = 40;
+// A block's part of a row: words [g0, g1) of the gradient, whose elements lie in
+// words [e0, e1) of the logits, in which they begin `shift` elements further on.
+struct Slice {
+  char* to;            // the gradient's words
+  uint32_t head, full0, full1;   // of the gradient's row
+  uint32_t g0, g1, e0, held;
+  uint32_t shift, back;
+  bool live;
+};
+struct SliceShared {
+  uint64_t full, taken;                // of the place that slices are copied to
+  uint64_t summed, arrived[2], ready;  // of the live rows; arrivals by turns
+  RowSums warps[kSliceWarps];
+  float4 blocks[2][kMaxCluster];
+  RowFactors factors;
+  Slice slice;
+  int gave_up;
+};
+// Who writes where while others may still read: the warps write their sums of a
+// row after they have read the factors of the row before, which were made
+// from the sums before; the copier writes a slice's description after all have
+// taken the slice before, and its factors when all have summed, behind the
+// stores of the row before.  A block sends sums of row r + 2 when all have sent
+// those of row r + 1, behind their reading of row r's.
+template <int TYPE, int NV, bool TWO>
+__global__ void __launch_bounds__(kSliceThreads) __maxnreg__(NV == kManyWords ? 128 : 80)
+distill_slices_kernel(const __grid_constant__ DistillArgs a, int split) {
+  extern __shared__ __align__(128) uint8_t place_bytes[];
+  __shared__ SliceShared sh;
+  constexpr int E = Word<TYPE>::kElements;
+  uint4* const place = reinterpret_cast<uint4*>(place_bytes);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int rank = split > 1 ? (int)(blockIdx.x % split) : 0;
+  const uint64_t rows = gridDim.x / split, first = blockIdx.x / split;
+  const uint32_t full = shared_at(&sh.full), taken = shared_at(&sh.taken), summed = shared_at(&sh.summed), ready = shared_at(&sh.ready);
+  if (threadIdx.x == 0) {
+    barrier_init(full, 1);
+    barrier_init(taken, kSliceWarps);
+    barrier_init(summed, kSliceWarps);
+    barrier_init(ready, 1);
+    for (int i = 0; i < 2; ++i) {
+      barrier_init(shared_at(&sh.arrived[i]), 1);
+      barrier_expect(shared_at(&sh.arrived[i]), split * 16);
+    }
+    sh.gave_up = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (split > 1) cg::this_cluster().sync();
+  else __syncthreads();
+  after_previous();
+  const float per = a.top > 0 ? kLog2E / a.temperature : kLog2E;
+  bool ok = true;
+  if (warp == kSliceWarps) {
+    const RowTask* const tasks = static_cast<const RowTask*>(a.tasks);
+    uint32_t copies = 0, landed = 0;   // (those that somebody has waited for)
+    // copies the slice of `row` and describes it
+    auto copy = [&](uint64_t row, const RowTask& task) {
+      const RowWords b = row_words<TYPE>(a.logits, row, a.vocab);
+      const RowWords g = a.grad.data != nullptr ? row_words<TYPE>(a.grad, row, a.vocab) : b;
+      Slice s;
+      s.to = g.base;
+      s.head = g.head;
+      s.full0 = g.full0;
+      s.full1 = g.full1;
+      const uint32_t size = (g.words + split - 1) / split;
+      s.g0 = min(g.words, rank * size);
+      s.g1 = min(g.words, s.g0 + size);
+      s.shift = (b.head - g.head) & (E - 1);
+      s.back = b.head < g.head ? 1 : 0;
+      s.e0 = s.g0 - (s.g0 > 0 ? s.back : 0);
+      const uint32_t e1 = min(b.words, s.g1 + (s.shift != 0 && s.back == 0 ? 1 : 0));
+      s.held = e1 > s.e0 ? e1 - s.e0 : 0;
+      s.live = task.some || task.label >= 0;
+      uint32_t bytes = 0, in0 = 0;
+      if (s.live && s.held > 0) {
+        in0 = max(s.e0, b.full0);
+        const uint32_t in1 = min(e1, b.full1);
+        bytes = in1 > in0 ? (in1 - in0) * 16 : 0;
+        // the row's first and last word, where they hold other elements too
+        if (lane == 0 && s.e0 < b.full0) place[0] = load_word<TYPE>(b, a.vocab, s.e0);
+        if (lane == 1 && e1 > b.full1) place[e1 - 1 - s.e0] = load_word<TYPE>(b, a.vocab, e1 - 1);
+      }
+      __syncwarp();
+      if (lane == 0) {
+        sh.slice = s;
+        barrier_expect(full, bytes);
+        if (bytes > 0)
+          asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                           shared_at(place + (in0 - s.e0))),
+                       "l"(b.base + (uint64_t)in0 * 16), "r"(bytes), "r"(full)
+                       : "memory");
+      }
+      ++copies;
+      __syncwarp();
+    };
+    uint32_t it = 0, lives = 0;
+    RowTask task = tasks[first < a.n ? first : 0];
+    if (first < a.n) copy(first, task);
+    for (uint64_t row = first; row < a.n; row += rows, ++it) {
+      const bool more = row + rows < a.n;
+      const RowTask next = tasks[more ? row + rows : row];
+      if (!(ok = barrier_wait(taken, it & 1u, kNap))) break;
+      ++landed;
+      if (more) copy(row + rows, next);
+      if (task.some || task.label >= 0) {
+        const uint32_t parity = lives & 1u, q = lives & 1u;
+        if (!(ok = barrier_wait(summed, parity, kNap))) break;
+        RowSums all = merge_sums<TWO>(lane < kSliceWarps ? sh.warps[lane] : RowSums{-INFINITY, 0.f, 0.f}, kSliceWarps, per);
+        if (split > 1) {
+          if (all.max == -INFINITY) all.t = all.one = 0.f;   // (a part of -inf alone has no NaN for the others)
+          const uint32_t bar = shared_at(&sh.arrived[q]);
+          if (lane < split)
+            store_and_count(shared_of(shared_at(&sh.blocks[q][rank]), lane), make_float4(all.max, all.t, all.one, 0.f), shared_of(bar, lane));
+          if (!(ok = barrier_wait(bar, (lives >> 1) & 1u))) break;
+          if (lane == 0) barrier_expect(bar, split * 16);   // (for two live rows on)
+          const float4 v = lane < split ? sh.blocks[q][lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+          all = merge_sums<TWO>(RowSums{v.x, v.y, v.z}, split, per);
+        }
+        ++lives;
+        if (lane == 0) {
+          if (rank == 0) static_cast<RowSums*>(a.sums)[row] = all;
+          sh.factors = row_factors<TYPE, TWO>(a, row, task, all, per);
+          barrier_arrive(ready);
+        }
+        __syncwarp();
+      }
+      task = next;
+    }
+    if (!ok) {
+      if (lane == 0) atomicExch(&sh.gave_up, 1);
+      if (copies > landed) barrier_wait(full, landed & 1u);   // (it lands before the block ends)
+    }
+  } else {
+    uint32_t it = 0, lives = 0;
+    for (uint64_t row = first; row < a.n; row += rows, ++it) {
+      if (!(ok = barrier_wait(full, it & 1u))) break;
+      const Slice& s = sh.slice;
+      const uint32_t g0 = s.g0 + threadIdx.x, g1 = s.g1, full0 = s.full0, full1 = s.full1, head = s.head;
+      char* const to = s.to;
+      const bool live = s.live;
+      uint4 v[NV];
+      if (live) {
+        const uint32_t shift = s.shift, held = s.held, from = g0 - s.back - s.e0;
+        if (shift == 0) {
+#pragma unroll
+          for (int i = 0; i < NV; ++i) {
+            v[i] = make_uint4(Word<TYPE>::kNone, Word<TYPE>::kNone, Word<TYPE>::kNone, Word<TYPE>::kNone);
+            if (from + i * kSliceWork < held) v[i] = place[from + i * kSliceWork];
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < NV; ++i) {
+            const uint4 none = make_uint4(Word<TYPE>::kNone, Word<TYPE>::kNone, Word<TYPE>::kNone, Word<TYPE>::kNone);
+            const uint32_t w = from + i * kSliceWork;
+            v[i] = none;
+            if (g0 + i * kSliceWork < g1)
+              v[i] = shift_words<TYPE>(w < held ? place[w] : none, w + 1 < held ? place[w + 1] : none, shift);
+          }
+        }
+      }
+      __syncwarp();
+      if (lane == 0) barrier_arrive(taken);
+      if (!live) {
+        if (a.grad.data != nullptr) {
+          for (uint32_t w = g0; w < g1; w += kSliceWork) {
+            if (w >= full0 && w < full1) *reinterpret_cast<uint4*>(to + (uint64_t)w * 16) = make_uint4(0, 0, 0, 0);
+            else store_edge<TYPE>(to, head, a.vocab, w, make_uint4(0, 0, 0, 0));
+          }
+        }
+        continue;
+      }
+      Largest<TYPE> largest;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) largest.see(v[i]);
+      RowSums mine;
+      mine.max = lanes_max(largest.value());
+      const float shift = finite_shift(mine.max);
+      const bool huge = is_huge(shift, per);
+      const float k = huge ? 0.f : shift;
+      uint64_t st = 0, so = 0;
+      auto add = [&](const uint4& word) {
+        add_word<TYPE>(word, pair_of(per, per), pair_of(-(k * per), -(k * per)), st);
+        if (TWO) add_word<TYPE>(word, pair_of(kLog2E, kLog2E), pair_of(-(k * kLog2E), -(k * kLog2E)), so);
+      };
+      if (!huge) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) add(v[i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          uint4 word = v[i];
+          take_off<TYPE>(word, shift);
+          add(word);
+        }
+      }
+      const float2 t = floats_of(st), o = floats_of(so);
+      mine.t = lanes_sum((t.x + t.y) * unround(k, per), 32);
+      mine.one = TWO ? lanes_sum((o.x + o.y) * unround(k, kLog2E), 32) : 0.f;
+      if (lane == 0) {
+        sh.warps[warp] = mine;
+        barrier_arrive(summed);
+      }
+      if (!(ok = barrier_wait(ready, lives & 1u))) break;
+      ++lives;
+      if (a.grad.data == nullptr) continue;
+      const RowFactors f = sh.factors;
+      if (f.huge) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) take_off<TYPE>(v[i], f.max);
+      }
+      with_gradient<TYPE, TWO>(f, per, [&](const auto& gradient) {
+        char* const p = to + (uint64_t)g0 * 16;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          const uint32_t w = g0 + i * kSliceWork;
+          if (w >= g1) continue;
+          const uint4 y = gradient.of(v[i]);
+          if (w >= full0 && w < full1) *reinterpret_cast<uint4*>(p + i * kSliceWork * 16) = y;
+          else store_edge<TYPE>(to, head, a.vocab, w, y);
+        }
+      });
+    }
+    if (!ok && lane == 0) atomicExch(&sh.gave_up, 1);
+  }
+  __syncwarp();
+  if (split > 1) cg::this_cluster().sync();   // (no block leaves while others send to it)
+  else __syncthreads();
+  if (threadIdx.x == 0 && sh.gave_up) set_error(a.st, ERR_TIMEOUT);
+}
+
+// ---- rows read twice ---------------------------------------------------------------
+constexpr int kLongThreads = 512, kLongBlocks = 8;   // of a cluster
+template <int TYPE, bool TWO>
+__global__ void __launch_bounds__(kLongThreads, 2) __cluster_dims__(kLongBlocks)
+distill_long_kernel(const __grid_constant__ DistillArgs a) {
+  after_previous();
+  constexpr int E = Word<TYPE>::kElements, WARPS = kLongThreads / 32;
+  __shared__ RowSums warps[WARPS];
+  __shared__ RowSums blocks[2][kLongBlocks];
+  cg::cluster_group cluster = cg::this_cluster();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rank = blockIdx.x % kLongBlocks;
+  const float per = a.top > 0 ? kLog2E / a.temperature : kLog2E;
+  int turn = 0;
+  for (uint64_t row = blockIdx.x / kLongBlocks; row < a.n; row += gridDim.x / kLongBlocks) {
+    const RowTask task = static_cast<const RowTask*>(a.tasks)[row];
+    const bool live = task.some || task.label >= 0;
+    const RowWords b = row_words<TYPE>(a.logits, row, a.vocab);
+    const uint32_t size = (b.words + kLongBlocks - 1) / kLongBlocks;
+    const uint32_t w0 = min(b.words, rank * size), w1 = min(b.words, w0 + size);
+    RowSums all{-INFINITY, 0.f, 0.f};
+    if (live) {
+      RowSums mine{-INFINITY, 0.f, 0.f};   // relative to the largest so far
+#pragma unroll 4
+      for (uint32_t w = w0 + threadIdx.x; w < w1; w += kLongThreads) {
+        const uint4 word = load_word<TYPE>(b, a.vocab, w);
+        Largest<TYPE> here;
+        here.see(word);
+        const float max = fmaxf(mine.max, here.value());
+        if (max > mine.max && mine.max != -INFINITY) {   // (sums of nothing are 0)
+          mine.t *= exp2_of((mine.max - max) * per);
+          mine.one *= exp2_of((mine.max - max) * kLog2E);
+        }
+        mine.max = max;
+        const float shift = finite_shift(max);
+        float x[E];
+        unpack_word<TYPE>(word, x);
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+          mine.t += exp2_of((x[j] - shift) * per);
+          if (TWO) mine.one += exp2_of((x[j] - shift) * kLog2E);
+        }
+      }
+      const float top = lanes_max(mine.max);
+      if (mine.max != -INFINITY) {
+        mine.t *= exp2_of((mine.max - top) * per);
+        mine.one *= exp2_of((mine.max - top) * kLog2E);
+      }
+      mine.max = top;
+      mine.t = lanes_sum(mine.t, 32);
+      mine.one = lanes_sum(mine.one, 32);
+      if (lane == 0) warps[warp] = mine;
+      __syncthreads();
+      if (warp == 0) {
+        RowSums ours = merge_sums<TWO>(lane < WARPS ? warps[lane] : RowSums{-INFINITY, 0.f, 0.f}, WARPS, per);
+        if (ours.max == -INFINITY) ours.t = ours.one = 0.f;
+        if (lane < kLongBlocks) cluster.map_shared_rank(&blocks[turn][0], lane)[rank] = ours;
+      }
+      cluster.sync();
+      all = merge_sums<TWO>(lane < kLongBlocks ? blocks[turn][lane] : RowSums{-INFINITY, 0.f, 0.f}, kLongBlocks, per);
+      if (rank == 0 && threadIdx.x == 0) static_cast<RowSums*>(a.sums)[row] = all;
+      turn ^= 1;
+    }
+    if (a.grad.data == nullptr) continue;
+    const RowWords g = row_words<TYPE>(a.grad, row, a.vocab);
+    const uint32_t g0 = min(g.words, rank * size), g1 = rank == kLongBlocks - 1 ? g.words : min(g.words, (rank + 1) * size);
+    if (!live) {
+      for (uint32_t w = g0 + threadIdx.x; w < g1; w += kLongThreads) store_word<TYPE>(g, a.vocab, w, make_uint4(0, 0, 0, 0));
+      continue;
+    }
+    const RowFactors f = row_factors<TYPE, TWO>(a, row, task, all, per);
+    const uint32_t shift = (b.head - g.head) & (E - 1), back = b.head < g.head ? 1 : 0;
+    with_gradient<TYPE, TWO>(f, per, [&](const auto& gradient) {
+#pragma unroll 4
+      for (uint32_t w = g0 + threadIdx.x; w < g1; w += kLongThreads) {
+        uint4 word = load_shifted<TYPE>(b, a.vocab, w - back, shift);
+        if (f.huge) take_off<TYPE>(word, f.max);
+        store_word<TYPE>(g, a.vocab, w, gradient.of(word));
+      }
+    });
+  }
+  cluster.sync();   // (others may still write here)
 }
 
 // The loss, and the elements that list and label change.
@@ -589,36 +944,74 @@ inline uint32_t power_of_two(uint64_t n) {
 inline bool distill_two(const DistillArgs& a) { return a.top > 0 && a.labels != nullptr && a.temperature != 1.f; }
 
 template <int TYPE, int THREADS, int NV>
-void launch_rows_as(const DistillArgs& a, int split, int sms, cudaStream_t stream) {
-  void (*kernel)(DistillArgs, int) = distill_two(a) ? distill_rows_kernel<TYPE, THREADS, NV, true> : distill_rows_kernel<TYPE, THREADS, NV, false>;
+void launch_rows_as(const DistillArgs& a, int sms, cudaStream_t stream) {
+  const unsigned grid = (unsigned)std::min<uint64_t>(a.n, (uint64_t)sms * resident_blocks(THREADS, NV));
+  if (distill_two(a)) launch_after(distill_rows_kernel<TYPE, THREADS, NV, true>, grid, THREADS, 0, stream, a);
+  else launch_after(distill_rows_kernel<TYPE, THREADS, NV, false>, grid, THREADS, 0, stream, a);
+}
+
+// As many clusters of a kernel as run at once: rows are dealt out beforehand,
+// and one cluster more would double the time.  (Not all SMs of a GPC fill up
+// with clusters.  Asked for once per kernel and size.)
+inline int clusters_at_once(const void* kernel, const cudaLaunchConfig_t& c, int split, int otherwise) {
+  struct Known {
+    const void* kernel;
+    size_t smem;
+    int split, clusters;
+  };
+  static thread_local Known known[8]{};
+  static thread_local unsigned next = 0;
+  for (const Known& k : known)
+    if (k.kernel == kernel && k.smem == c.dynamicSmemBytes && k.split == split) return k.clusters;
+  int clusters = 0;
+  if (split == 1 || cudaOccupancyMaxActiveClusters(&clusters, kernel, &c) != cudaSuccess || clusters < 1) {
+    cudaGetLastError();
+    clusters = std::max(1, otherwise / split);
+  }
+  known[next++ % 8] = Known{kernel, c.dynamicSmemBytes, split, clusters};
+  return clusters;
+}
+
+template <int TYPE, int NV>
+void launch_slices(const DistillArgs& a, int split, int sms, cudaStream_t stream) {
+  void (*kernel)(DistillArgs, int) = distill_two(a) ? distill_slices_kernel<TYPE, NV, true> : distill_slices_kernel<TYPE, NV, false>;
   cudaLaunchAttribute at[2]{};
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
   at[1].id = cudaLaunchAttributeClusterDimension;
   at[1].val.clusterDim.x = (unsigned)split;
   at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
-  if (split > 8) cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-  const uint64_t clusters = std::max<uint64_t>(1, (uint64_t)sms * resident_blocks(THREADS, NV) / split);
   cudaLaunchConfig_t c{};
-  c.gridDim = dim3((unsigned)(std::min<uint64_t>(a.n, clusters) * split));
-  c.blockDim = dim3(THREADS);
+  c.gridDim = dim3((unsigned)split);
+  c.blockDim = dim3(kSliceThreads);
+  c.dynamicSmemBytes = (NV * kSliceWork + 2) * 16;   // (a neighbour where the gradient's words begin elsewhere)
   c.stream = stream;
   c.attrs = at;
   c.numAttrs = split > 1 ? 2 : 1;
+  cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)c.dynamicSmemBytes);
+  if (split > 8) cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  const int clusters = clusters_at_once((const void*)kernel, c, split, sms * slice_blocks(NV));
+  c.gridDim = dim3((unsigned)(std::min<uint64_t>(a.n, clusters) * split));
   cudaLaunchKernelEx(&c, kernel, a, split);
 }
 
 template <int TYPE>
 void launch_rows(const DistillArgs& a, int sms, cudaStream_t stream) {
   const uint64_t words = ((uint64_t)a.vocab * Word<TYPE>::kSize + 15) / 16 + 1;   // (a row may begin inside a word)
-  if (words <= 256) return launch_rows_as<TYPE, 128, 2>(a, 1, sms, stream);
-  if (words <= 1024) return launch_rows_as<TYPE, 128, 8>(a, 1, sms, stream);
-  if (words <= 2048) return launch_rows_as<TYPE, 512, 4>(a, 1, sms, stream);
-  uint32_t split = power_of_two((words + 4095) / 4096);
-  if (split > kMaxCluster) return launch_rows_as<TYPE, 512, 0>(a, 8, sms, stream);
-  // few rows: more blocks for each
-  while (split < 8 && a.n * split * 2 <= (uint64_t)sms && words / split > 1024) split *= 2;
-  launch_rows_as<TYPE, 512, 8>(a, (int)split, sms, stream);
+  if (words <= 256) return launch_rows_as<TYPE, 128, 2>(a, sms, stream);
+  if (words <= 1024) return launch_rows_as<TYPE, 128, 8>(a, sms, stream);
+  if (words <= 2048) return launch_rows_as<TYPE, 512, 4>(a, sms, stream);
+  constexpr uint64_t most = kManyWords * kSliceWork, few = kFewWords * kSliceWork;   // words of a slice
+  if (words <= kMaxCluster * most) {
+    uint32_t split = (uint32_t)((words + most - 1) / most);
+    // few rows: more blocks for each
+    while (split <= 4 && a.n * split * 2 <= (uint64_t)sms && words / split > 1024) split *= 2;
+    if (words <= split * few) return launch_slices<TYPE, kFewWords>(a, (int)split, sms, stream);
+    return launch_slices<TYPE, kManyWords>(a, (int)split, sms, stream);
+  }
+  const unsigned grid = (unsigned)std::min<uint64_t>(a.n, std::max(1, sms * 2 / kLongBlocks)) * kLongBlocks;
+  if (distill_two(a)) launch_after(distill_long_kernel<TYPE, true>, grid, kLongThreads, 0, stream, a);
+  else launch_after(distill_long_kernel<TYPE, false>, grid, kLongThreads, 0, stream, a);
 }
 
 template <int TYPE>

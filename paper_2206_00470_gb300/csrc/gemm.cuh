@@ -5,6 +5,7 @@
 
 #include <cuda.h>
 
+#include "barrier.cuh"
 #include "dense.cuh"
 
 namespace adapm {
@@ -35,41 +36,6 @@ struct GemmArgs {
 
 #ifdef __CUDACC__
 namespace {
-
-__device__ __forceinline__ uint32_t shared_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-__device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void barrier_expect(uint32_t bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void barrier_arrive(uint32_t bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity) {
-  uint32_t done;
-  asm volatile(
-      "{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
-      : "=r"(done)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return done != 0;
-}
-__device__ __forceinline__ uint64_t now_ns() {
-  uint64_t t;
-  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-  return t;
-}
-// Waits for a phase of a barrier, two seconds at most; false: it gave up.
-__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity) {
-  if (barrier_try(bar, parity)) return true;
-  const uint64_t start = now_ns();
-  for (uint32_t i = 1;; ++i) {
-    if (barrier_try(bar, parity)) return true;
-    if ((i & 63u) == 0u && now_ns() - start > 2000000000ull) return false;
-  }
-}
 
 __device__ __forceinline__ void copy_tile(uint32_t to, const CUtensorMap* map, int x, int y, uint32_t bar) {
   asm volatile(
