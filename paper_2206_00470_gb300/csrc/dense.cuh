@@ -217,6 +217,26 @@ __device__ __forceinline__ void store_n_as(char* p, int type, const float* x) {
 
 __host__ __device__ __forceinline__ int type_size(int type) { return type == ADAPM_F32 ? 4 : 2; }
 
+// ---- two floats at a time ------------------------------------------------------
+__device__ __forceinline__ uint64_t pair_of(float x, float y) {
+  return (uint64_t)__float_as_uint(x) | ((uint64_t)__float_as_uint(y) << 32);
+}
+__device__ __forceinline__ float2 floats_of(uint64_t v) { return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))); }
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
 // Sum over `width` lanes (a power of two) that begin at a multiple of it; every lane gets it.
 __device__ __forceinline__ float lanes_sum(float x, int width) {
   for (int o = width >> 1; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);

@@ -168,7 +168,7 @@ struct RowTask {
   int32_t some;     // whether the list has entries
 };
 // What distill_rows finds out: largest logit, and sums of exp((s - max) / T)
-// and (distill_two) of exp(s - max).
+// and, with two temperatures, of exp(s - max).
 struct RowSums {
   float max, t, one;
 };
@@ -298,26 +298,6 @@ __device__ __forceinline__ RowScale row_scale(const DistillArgs& a, uint64_t row
   return RowScale{(soft + hard) / sums.t, 0.f};
 }
 
-// ---- two floats at a time ------------------------------------------------------
-__device__ __forceinline__ uint64_t pair_of(float x, float y) {
-  return (uint64_t)__float_as_uint(x) | ((uint64_t)__float_as_uint(y) << 32);
-}
-__device__ __forceinline__ float2 floats_of(uint64_t v) { return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))); }
-__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-__device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-__device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
 // The elements of a word, two by two.
 template <int TYPE>
 __device__ __forceinline__ uint64_t pair_at(const uint4& v, int j) {
@@ -387,14 +367,38 @@ __device__ __forceinline__ float unround(float max, float c) {
 __device__ __forceinline__ float finite_shift(float m) { return m == -INFINITY ? 0.f : m; }
 __device__ __forceinline__ bool is_huge(float max, float per) { return fabsf(max * kLog2E) > kHuge || fabsf(max * per) > kHuge; }
 
-// Adds the sums of 2^(s c - k) over the elements of a word, two by two.
-template <int TYPE>
-__device__ __forceinline__ void add_word(const uint4& word, uint64_t c, uint64_t minus_k, uint64_t& to) {
+// Which sums a row has: at one temperature; at two; at two of which the first is
+// 2, where e^d = (e^(d/2))^2 (3063 rows of 50,021 bf16, both terms: 142 -> 122 us).
+enum { ONE_SUM = 0, TWO_SUMS = 1, SQUARES = 2 };
+
+// Constants of 2^(s c - k) at both temperatures, as pairs.
+struct Exponents {
+  uint64_t c, m, c1, m1;
+  __device__ __forceinline__ Exponents(float per, float k)
+      : c(pair_of(per, per)), m(pair_of(-(k * per), -(k * per))), c1(pair_of(kLog2E, kLog2E)), m1(pair_of(-(k * kLog2E), -(k * kLog2E))) {}
+};
+// Adds the exponentials of the elements of a word, two by two.
+template <int TYPE, int MODE>
+__device__ __forceinline__ void add_word(const uint4& word, const Exponents& e, uint64_t& t, uint64_t& one) {
 #pragma unroll
   for (int j = 0; j < Word<TYPE>::kElements / 2; ++j) {
-    const float2 d = floats_of(fma_pair(pair_at<TYPE>(word, j), c, minus_k));
-    to = add_pair(to, pair_of(exp2_of(d.x), exp2_of(d.y)));
+    const uint64_t s = pair_at<TYPE>(word, j);
+    const float2 d = floats_of(fma_pair(s, e.c, e.m));
+    const uint64_t x = pair_of(exp2_of(d.x), exp2_of(d.y));
+    t = add_pair(t, x);
+    if (MODE == TWO_SUMS) {
+      const float2 d1 = floats_of(fma_pair(s, e.c1, e.m1));
+      one = add_pair(one, pair_of(exp2_of(d1.x), exp2_of(d1.y)));
+    } else if (MODE == SQUARES) {
+      one = fma_pair(x, x, one);
+    }
   }
+}
+// What the rounding of k costs the two sums: see unround.
+template <int MODE>
+__device__ __forceinline__ float2 unround_both(float k, float per) {
+  const float u = unround(k, per);
+  return make_float2(u, MODE == TWO_SUMS ? unround(k, kLog2E) : (MODE == SQUARES ? u * u : 0.f));
 }
 
 // What turns a row's logits into the part of the gradient that every element
@@ -405,22 +409,23 @@ struct RowFactors {
   bool huge;
   bool folded;   // st is part of the exponent
 };
-template <int TYPE, bool TWO>
+template <int TYPE, int MODE>
 __device__ __forceinline__ RowFactors row_factors(const DistillArgs& a, uint64_t row, const RowTask& task, const RowSums& all, float per) {
-  const RowScale scale = row_scale(a, row, task, all, TWO);
+  const RowScale scale = row_scale(a, row, task, all, MODE != ONE_SUM);
   RowFactors f;
   f.max = all.max;
   f.huge = is_huge(all.max, per);
   const float k = f.huge ? 0.f : all.max;
-  f.st = scale.t * unround(k, per);
-  f.so = TWO ? scale.one * unround(k, kLog2E) : 0.f;
+  const float2 u = unround_both<MODE>(k, per);
+  f.st = scale.t * u.x;
+  f.so = scale.one * u.y;
   // 16-bit gradients of one exponential: the factor is added to the exponent (off by 2^-18 of the result at most)
-  f.folded = !TWO && TYPE != ADAPM_F32 && f.st >= 0.f;
+  f.folded = MODE == ONE_SUM && TYPE != ADAPM_F32 && f.st >= 0.f;
   f.minus_k = -(k * per) + (f.folded ? log2f(f.st) : 0.f);
   f.minus_k1 = -(k * kLog2E);
   return f;
 }
-template <int TYPE, bool TWO, bool FOLD>
+template <int TYPE, int MODE, bool FOLD>
 struct Gradient {
   uint64_t c, m, ct, c1, m1, co;
   __device__ __forceinline__ Gradient(const RowFactors& f, float per)
@@ -435,10 +440,13 @@ struct Gradient {
       const float2 d = floats_of(fma_pair(s, c, m));
       float2 f = make_float2(exp2_of(d.x), exp2_of(d.y));
       if (!FOLD) {
-        uint64_t y = mul_pair(pair_of(f.x, f.y), ct);
-        if (TWO) {
+        const uint64_t x = pair_of(f.x, f.y);
+        uint64_t y = mul_pair(x, ct);
+        if (MODE == TWO_SUMS) {
           const float2 d1 = floats_of(fma_pair(s, c1, m1));
           y = fma_pair(pair_of(exp2_of(d1.x), exp2_of(d1.y)), co, y);
+        } else if (MODE == SQUARES) {
+          y = mul_pair(x, fma_pair(x, co, ct));
         }
         f = floats_of(y);
       }
@@ -449,17 +457,17 @@ struct Gradient {
   }
 };
 // fn(Gradient) in the form that the row's factors ask for.
-template <int TYPE, bool TWO, class F>
+template <int TYPE, int MODE, class F>
 __device__ __forceinline__ void with_gradient(const RowFactors& f, float per, F&& fn) {
-  if constexpr (!TWO && TYPE != ADAPM_F32) {
-    if (f.folded) return fn(Gradient<TYPE, TWO, true>(f, per));
+  if constexpr (MODE == ONE_SUM && TYPE != ADAPM_F32) {
+    if (f.folded) return fn(Gradient<TYPE, MODE, true>(f, per));
   }
-  fn(Gradient<TYPE, TWO, false>(f, per));
+  fn(Gradient<TYPE, MODE, false>(f, per));
 }
 
 // Sums of several parts of a row, relative to the largest of all: `count` of
 // them, of which the lane has number `lane` (at most 32).
-template <bool TWO>
+template <int MODE>
 __device__ __forceinline__ RowSums merge_sums(const RowSums& s, int count, float per) {
   const int lane = threadIdx.x & 31;
   RowSums all;
@@ -467,7 +475,7 @@ __device__ __forceinline__ RowSums merge_sums(const RowSums& s, int count, float
   // (-inf: a part without logits above it, its sums are 0; all of -inf: NaN, as a softmax of nothing is)
   const float down = s.max - all.max;
   all.t = lanes_sum(lane < count ? s.t * exp2_of(down * per) : 0.f, 32);
-  all.one = TWO ? lanes_sum(lane < count ? s.one * exp2_of(down * kLog2E) : 0.f, 32) : 0.f;
+  all.one = MODE != ONE_SUM ? lanes_sum(lane < count ? s.one * exp2_of(down * kLog2E) : 0.f, 32) : 0.f;
   return all;
 }
 
@@ -475,15 +483,15 @@ __device__ __forceinline__ RowSums merge_sums(const RowSums& s, int count, float
 // Blocks per SM that the registers allow: 32 of a thread hold eight words.
 constexpr int resident_blocks(int threads, int words) { return (words == 8 ? 1024 : 1536) / threads; }
 
-// NV words a thread; TWO: sums at both temperatures.
-template <int TYPE, int THREADS, int NV, bool TWO>
+// NV words a thread.
+template <int TYPE, int THREADS, int NV, int MODE>
 __global__ void __launch_bounds__(THREADS, resident_blocks(THREADS, NV))
 distill_rows_kernel(const __grid_constant__ DistillArgs a) {
   after_previous();
   constexpr int E = Word<TYPE>::kElements, WARPS = THREADS / 32;
   __shared__ RowSums warps[2][WARPS];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  // exp((s - m) / T) = 2^((s - m) per); the one temperature of a row without TWO
+  // exp((s - m) / T) = 2^((s - m) per); the one temperature of a row with one sum
   const float per = a.top > 0 ? kLog2E / a.temperature : kLog2E;
   const RowTask* const tasks = static_cast<const RowTask*>(a.tasks);
   uint64_t row = blockIdx.x;
@@ -512,25 +520,25 @@ distill_rows_kernel(const __grid_constant__ DistillArgs a) {
         for (int i = 0; i < NV; ++i) take_off<TYPE>(v[i], shift);
       }
       const float k = huge ? 0.f : shift;
+      const Exponents e(per, k);
       uint64_t st = 0, so = 0;
 #pragma unroll
-      for (int i = 0; i < NV; ++i) add_word<TYPE>(v[i], pair_of(per, per), pair_of(-(k * per), -(k * per)), st);
-      if (TWO) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i) add_word<TYPE>(v[i], pair_of(kLog2E, kLog2E), pair_of(-(k * kLog2E), -(k * kLog2E)), so);
+      for (int i = 0; i < NV; ++i) {
+        if (i * THREADS >= (int)b.words) break;
+        add_word<TYPE, MODE>(v[i], e, st, so);
       }
       if (huge) {   // (as they were: the gradient is relative to the whole row's largest)
 #pragma unroll
         for (int i = 0; i < NV; ++i) v[i] = load_word<TYPE>(b, a.vocab, i * THREADS + threadIdx.x);
       }
-      const float2 t = floats_of(st), o = floats_of(so);
-      mine.t = lanes_sum((t.x + t.y) * unround(k, per), 32);
-      mine.one = TWO ? lanes_sum((o.x + o.y) * unround(k, kLog2E), 32) : 0.f;
+      const float2 t = floats_of(st), o = floats_of(so), u = unround_both<MODE>(k, per);
+      mine.t = lanes_sum((t.x + t.y) * u.x, 32);
+      mine.one = MODE != ONE_SUM ? lanes_sum((o.x + o.y) * u.y, 32) : 0.f;
       if (lane == 0) warps[turn][warp] = mine;
     }
     __syncthreads();
     if (live) {
-      all = merge_sums<TWO>(lane < WARPS ? warps[turn][lane] : RowSums{-INFINITY, 0.f, 0.f}, WARPS, per);
+      all = merge_sums<MODE>(lane < WARPS ? warps[turn][lane] : RowSums{-INFINITY, 0.f, 0.f}, WARPS, per);
       if (threadIdx.x == 0) static_cast<RowSums*>(a.sums)[row] = all;
     }
     if (a.grad.data == nullptr) continue;
@@ -539,15 +547,18 @@ distill_rows_kernel(const __grid_constant__ DistillArgs a) {
       for (uint32_t w = threadIdx.x; w < g.words; w += THREADS) store_word<TYPE>(g, a.vocab, w, make_uint4(0, 0, 0, 0));
       continue;
     }
-    const RowFactors f = row_factors<TYPE, TWO>(a, row, task, all, per);
-    with_gradient<TYPE, TWO>(f, per, [&](const auto& gradient) {
+    const RowFactors f = row_factors<TYPE, MODE>(a, row, task, all, per);
+    with_gradient<TYPE, MODE>(f, per, [&](const auto& gradient) {
       if (g.head == b.head) {
         if (f.huge) {
 #pragma unroll
           for (int i = 0; i < NV; ++i) take_off<TYPE>(v[i], f.max);
         }
 #pragma unroll
-        for (int i = 0; i < NV; ++i) store_word<TYPE>(g, a.vocab, i * THREADS + threadIdx.x, gradient.of(v[i]));
+        for (int i = 0; i < NV; ++i) {
+          if (i * THREADS >= (int)g.words) break;
+          store_word<TYPE>(g, a.vocab, i * THREADS + threadIdx.x, gradient.of(v[i]));
+        }
       } else {
         // words of the gradient that begin elsewhere: the row again, from L1 and L2
         const uint32_t shift = (b.head - g.head) & (E - 1), back = b.head < g.head ? 1 : 0;
@@ -577,8 +588,9 @@ constexpr uint32_t kNap = 40;
 // words [e0, e1) of the logits, in which they begin `shift` elements further on.
 struct Slice {
   char* to;            // the gradient's words
-  uint32_t head, full0, full1;   // of the gradient's row
+  uint32_t head;       // of the gradient's row
   uint32_t g0, g1, e0, held;
+  uint32_t in0, in1;   // of [g0, g1): the words that hold nothing else
   uint32_t shift, back;
   bool live;
 };
@@ -597,7 +609,7 @@ struct SliceShared {
 // taken the slice before, and its factors when all have summed, behind the
 // stores of the row before.  A block sends sums of row r + 2 when all have sent
 // those of row r + 1, behind their reading of row r's.
-template <int TYPE, int NV, bool TWO>
+template <int TYPE, int NV, int MODE>
 __global__ void __launch_bounds__(kSliceThreads) __maxnreg__(NV == kManyWords ? 128 : 80)
 distill_slices_kernel(const __grid_constant__ DistillArgs a, int split) {
   extern __shared__ __align__(128) uint8_t place_bytes[];
@@ -635,11 +647,11 @@ distill_slices_kernel(const __grid_constant__ DistillArgs a, int split) {
       Slice s;
       s.to = g.base;
       s.head = g.head;
-      s.full0 = g.full0;
-      s.full1 = g.full1;
       const uint32_t size = (g.words + split - 1) / split;
       s.g0 = min(g.words, rank * size);
       s.g1 = min(g.words, s.g0 + size);
+      s.in0 = max(s.g0, g.full0);
+      s.in1 = max(s.in0, min(s.g1, g.full1));
       s.shift = (b.head - g.head) & (E - 1);
       s.back = b.head < g.head ? 1 : 0;
       s.e0 = s.g0 - (s.g0 > 0 ? s.back : 0);
@@ -680,7 +692,7 @@ distill_slices_kernel(const __grid_constant__ DistillArgs a, int split) {
       if (task.some || task.label >= 0) {
         const uint32_t parity = lives & 1u, q = lives & 1u;
         if (!(ok = barrier_wait(summed, parity, kNap))) break;
-        RowSums all = merge_sums<TWO>(lane < kSliceWarps ? sh.warps[lane] : RowSums{-INFINITY, 0.f, 0.f}, kSliceWarps, per);
+        RowSums all = merge_sums<MODE>(lane < kSliceWarps ? sh.warps[lane] : RowSums{-INFINITY, 0.f, 0.f}, kSliceWarps, per);
         if (split > 1) {
           if (all.max == -INFINITY) all.t = all.one = 0.f;   // (a part of -inf alone has no NaN for the others)
           const uint32_t bar = shared_at(&sh.arrived[q]);
@@ -689,12 +701,12 @@ distill_slices_kernel(const __grid_constant__ DistillArgs a, int split) {
           if (!(ok = barrier_wait(bar, (lives >> 1) & 1u))) break;
           if (lane == 0) barrier_expect(bar, split * 16);   // (for two live rows on)
           const float4 v = lane < split ? sh.blocks[q][lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
-          all = merge_sums<TWO>(RowSums{v.x, v.y, v.z}, split, per);
+          all = merge_sums<MODE>(RowSums{v.x, v.y, v.z}, split, per);
         }
         ++lives;
         if (lane == 0) {
           if (rank == 0) static_cast<RowSums*>(a.sums)[row] = all;
-          sh.factors = row_factors<TYPE, TWO>(a, row, task, all, per);
+          sh.factors = row_factors<TYPE, MODE>(a, row, task, all, per);
           barrier_arrive(ready);
         }
         __syncwarp();
@@ -710,25 +722,32 @@ distill_slices_kernel(const __grid_constant__ DistillArgs a, int split) {
     for (uint64_t row = first; row < a.n; row += rows, ++it) {
       if (!(ok = barrier_wait(full, it & 1u))) break;
       const Slice& s = sh.slice;
-      const uint32_t g0 = s.g0 + threadIdx.x, g1 = s.g1, full0 = s.full0, full1 = s.full1, head = s.head;
+      const uint32_t g0 = s.g0, g1 = s.g1, count = g1 - g0, in0 = s.in0, in1 = s.in1, head = s.head;
       char* const to = s.to;
       const bool live = s.live;
+      const uint4 none = make_uint4(Word<TYPE>::kNone, Word<TYPE>::kNone, Word<TYPE>::kNone, Word<TYPE>::kNone);
       uint4 v[NV];
       if (live) {
-        const uint32_t shift = s.shift, held = s.held, from = g0 - s.back - s.e0;
+        const uint32_t shift = s.shift, held = s.held, from = g0 + threadIdx.x - s.back - s.e0;
         if (shift == 0) {
+          const uint4* const p = place + threadIdx.x;   // (word g0 is the first that is held)
 #pragma unroll
           for (int i = 0; i < NV; ++i) {
-            v[i] = make_uint4(Word<TYPE>::kNone, Word<TYPE>::kNone, Word<TYPE>::kNone, Word<TYPE>::kNone);
-            if (from + i * kSliceWork < held) v[i] = place[from + i * kSliceWork];
+            if (i * kSliceWork >= count) break;         // (the same for the block)
+            if ((i + 1) * kSliceWork <= held) {
+              v[i] = p[i * kSliceWork];
+            } else {
+              v[i] = none;
+              if (threadIdx.x + i * kSliceWork < held) v[i] = p[i * kSliceWork];
+            }
           }
         } else {
 #pragma unroll
           for (int i = 0; i < NV; ++i) {
-            const uint4 none = make_uint4(Word<TYPE>::kNone, Word<TYPE>::kNone, Word<TYPE>::kNone, Word<TYPE>::kNone);
+            if (i * kSliceWork >= count) break;
             const uint32_t w = from + i * kSliceWork;
             v[i] = none;
-            if (g0 + i * kSliceWork < g1)
+            if (threadIdx.x + i * kSliceWork < count)
               v[i] = shift_words<TYPE>(w < held ? place[w] : none, w + 1 < held ? place[w + 1] : none, shift);
           }
         }
@@ -737,8 +756,8 @@ distill_slices_kernel(const __grid_constant__ DistillArgs a, int split) {
       if (lane == 0) barrier_arrive(taken);
       if (!live) {
         if (a.grad.data != nullptr) {
-          for (uint32_t w = g0; w < g1; w += kSliceWork) {
-            if (w >= full0 && w < full1) *reinterpret_cast<uint4*>(to + (uint64_t)w * 16) = make_uint4(0, 0, 0, 0);
+          for (uint32_t w = g0 + threadIdx.x; w < g1; w += kSliceWork) {
+            if (w >= in0 && w < in1) *reinterpret_cast<uint4*>(to + (uint64_t)w * 16) = make_uint4(0, 0, 0, 0);
             else store_edge<TYPE>(to, head, a.vocab, w, make_uint4(0, 0, 0, 0));
           }
         }
@@ -746,31 +765,35 @@ distill_slices_kernel(const __grid_constant__ DistillArgs a, int split) {
       }
       Largest<TYPE> largest;
 #pragma unroll
-      for (int i = 0; i < NV; ++i) largest.see(v[i]);
+      for (int i = 0; i < NV; ++i) {
+        if (i * kSliceWork >= count) break;
+        largest.see(v[i]);
+      }
       RowSums mine;
       mine.max = lanes_max(largest.value());
       const float shift = finite_shift(mine.max);
       const bool huge = is_huge(shift, per);
       const float k = huge ? 0.f : shift;
+      const Exponents e(per, k);
       uint64_t st = 0, so = 0;
-      auto add = [&](const uint4& word) {
-        add_word<TYPE>(word, pair_of(per, per), pair_of(-(k * per), -(k * per)), st);
-        if (TWO) add_word<TYPE>(word, pair_of(kLog2E, kLog2E), pair_of(-(k * kLog2E), -(k * kLog2E)), so);
-      };
       if (!huge) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) add(v[i]);
+        for (int i = 0; i < NV; ++i) {
+          if (i * kSliceWork >= count) break;
+          add_word<TYPE, MODE>(v[i], e, st, so);
+        }
       } else {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
+          if (i * kSliceWork >= count) break;
           uint4 word = v[i];
           take_off<TYPE>(word, shift);
-          add(word);
+          add_word<TYPE, MODE>(word, e, st, so);
         }
       }
-      const float2 t = floats_of(st), o = floats_of(so);
-      mine.t = lanes_sum((t.x + t.y) * unround(k, per), 32);
-      mine.one = TWO ? lanes_sum((o.x + o.y) * unround(k, kLog2E), 32) : 0.f;
+      const float2 t = floats_of(st), o = floats_of(so), u = unround_both<MODE>(k, per);
+      mine.t = lanes_sum((t.x + t.y) * u.x, 32);
+      mine.one = MODE != ONE_SUM ? lanes_sum((o.x + o.y) * u.y, 32) : 0.f;
       if (lane == 0) {
         sh.warps[warp] = mine;
         barrier_arrive(summed);
@@ -781,17 +804,22 @@ distill_slices_kernel(const __grid_constant__ DistillArgs a, int split) {
       const RowFactors f = sh.factors;
       if (f.huge) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) take_off<TYPE>(v[i], f.max);
+        for (int i = 0; i < NV; ++i) {
+          if (i * kSliceWork >= count) break;
+          take_off<TYPE>(v[i], f.max);
+        }
       }
-      with_gradient<TYPE, TWO>(f, per, [&](const auto& gradient) {
-        char* const p = to + (uint64_t)g0 * 16;
+      with_gradient<TYPE, MODE>(f, per, [&](const auto& gradient) {
+        const uint32_t w = g0 + threadIdx.x;
+        char* const p = to + (uint64_t)w * 16;
+        // (the row's first and last word may hold other elements too)
+        const uint32_t inside = w - in0, size = in1 - in0;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-          const uint32_t w = g0 + i * kSliceWork;
-          if (w >= g1) continue;
+          if (i * kSliceWork >= count) break;
           const uint4 y = gradient.of(v[i]);
-          if (w >= full0 && w < full1) *reinterpret_cast<uint4*>(p + i * kSliceWork * 16) = y;
-          else store_edge<TYPE>(to, head, a.vocab, w, y);
+          if (inside + i * kSliceWork < size) *reinterpret_cast<uint4*>(p + i * kSliceWork * 16) = y;
+          else if (w + i * kSliceWork < g1) store_edge<TYPE>(to, head, a.vocab, w + i * kSliceWork, y);
         }
       });
     }
@@ -805,7 +833,7 @@ distill_slices_kernel(const __grid_constant__ DistillArgs a, int split) {
 
 // ---- rows read twice ---------------------------------------------------------------
 constexpr int kLongThreads = 512, kLongBlocks = 8;   // of a cluster
-template <int TYPE, bool TWO>
+template <int TYPE, int MODE>
 __global__ void __launch_bounds__(kLongThreads, 2) __cluster_dims__(kLongBlocks)
 distill_long_kernel(const __grid_constant__ DistillArgs a) {
   after_previous();
@@ -842,7 +870,7 @@ distill_long_kernel(const __grid_constant__ DistillArgs a) {
 #pragma unroll
         for (int j = 0; j < E; ++j) {
           mine.t += exp2_of((x[j] - shift) * per);
-          if (TWO) mine.one += exp2_of((x[j] - shift) * kLog2E);
+          if (MODE != ONE_SUM) mine.one += exp2_of((x[j] - shift) * kLog2E);
         }
       }
       const float top = lanes_max(mine.max);
@@ -856,12 +884,12 @@ distill_long_kernel(const __grid_constant__ DistillArgs a) {
       if (lane == 0) warps[warp] = mine;
       __syncthreads();
       if (warp == 0) {
-        RowSums ours = merge_sums<TWO>(lane < WARPS ? warps[lane] : RowSums{-INFINITY, 0.f, 0.f}, WARPS, per);
+        RowSums ours = merge_sums<MODE>(lane < WARPS ? warps[lane] : RowSums{-INFINITY, 0.f, 0.f}, WARPS, per);
         if (ours.max == -INFINITY) ours.t = ours.one = 0.f;
         if (lane < kLongBlocks) cluster.map_shared_rank(&blocks[turn][0], lane)[rank] = ours;
       }
       cluster.sync();
-      all = merge_sums<TWO>(lane < kLongBlocks ? blocks[turn][lane] : RowSums{-INFINITY, 0.f, 0.f}, kLongBlocks, per);
+      all = merge_sums<MODE>(lane < kLongBlocks ? blocks[turn][lane] : RowSums{-INFINITY, 0.f, 0.f}, kLongBlocks, per);
       if (rank == 0 && threadIdx.x == 0) static_cast<RowSums*>(a.sums)[row] = all;
       turn ^= 1;
     }
@@ -872,9 +900,9 @@ distill_long_kernel(const __grid_constant__ DistillArgs a) {
       for (uint32_t w = g0 + threadIdx.x; w < g1; w += kLongThreads) store_word<TYPE>(g, a.vocab, w, make_uint4(0, 0, 0, 0));
       continue;
     }
-    const RowFactors f = row_factors<TYPE, TWO>(a, row, task, all, per);
+    const RowFactors f = row_factors<TYPE, MODE>(a, row, task, all, per);
     const uint32_t shift = (b.head - g.head) & (E - 1), back = b.head < g.head ? 1 : 0;
-    with_gradient<TYPE, TWO>(f, per, [&](const auto& gradient) {
+    with_gradient<TYPE, MODE>(f, per, [&](const auto& gradient) {
 #pragma unroll 4
       for (uint32_t w = g0 + threadIdx.x; w < g1; w += kLongThreads) {
         uint4 word = load_shifted<TYPE>(b, a.vocab, w - back, shift);
@@ -941,13 +969,17 @@ inline uint32_t power_of_two(uint64_t n) {
   while (p < n) p *= 2;
   return p;
 }
-inline bool distill_two(const DistillArgs& a) { return a.top > 0 && a.labels != nullptr && a.temperature != 1.f; }
+inline int distill_mode(const DistillArgs& a) {
+  return a.top == 0 || a.labels == nullptr || a.temperature == 1.f ? ONE_SUM : (a.temperature == 2.f ? SQUARES : TWO_SUMS);
+}
 
 template <int TYPE, int THREADS, int NV>
 void launch_rows_as(const DistillArgs& a, int sms, cudaStream_t stream) {
   const unsigned grid = (unsigned)std::min<uint64_t>(a.n, (uint64_t)sms * resident_blocks(THREADS, NV));
-  if (distill_two(a)) launch_after(distill_rows_kernel<TYPE, THREADS, NV, true>, grid, THREADS, 0, stream, a);
-  else launch_after(distill_rows_kernel<TYPE, THREADS, NV, false>, grid, THREADS, 0, stream, a);
+  const int mode = distill_mode(a);
+  if (mode == ONE_SUM) launch_after(distill_rows_kernel<TYPE, THREADS, NV, ONE_SUM>, grid, THREADS, 0, stream, a);
+  else if (mode == SQUARES) launch_after(distill_rows_kernel<TYPE, THREADS, NV, SQUARES>, grid, THREADS, 0, stream, a);
+  else launch_after(distill_rows_kernel<TYPE, THREADS, NV, TWO_SUMS>, grid, THREADS, 0, stream, a);
 }
 
 // As many clusters of a kernel as run at once: rows are dealt out beforehand,
@@ -974,7 +1006,9 @@ inline int clusters_at_once(const void* kernel, const cudaLaunchConfig_t& c, int
 
 template <int TYPE, int NV>
 void launch_slices(const DistillArgs& a, int split, int sms, cudaStream_t stream) {
-  void (*kernel)(DistillArgs, int) = distill_two(a) ? distill_slices_kernel<TYPE, NV, true> : distill_slices_kernel<TYPE, NV, false>;
+  const int mode = distill_mode(a);
+  void (*kernel)(DistillArgs, int) = mode == ONE_SUM ? distill_slices_kernel<TYPE, NV, ONE_SUM>
+                                     : (mode == SQUARES ? distill_slices_kernel<TYPE, NV, SQUARES> : distill_slices_kernel<TYPE, NV, TWO_SUMS>);
   cudaLaunchAttribute at[2]{};
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
@@ -1010,8 +1044,8 @@ void launch_rows(const DistillArgs& a, int sms, cudaStream_t stream) {
     return launch_slices<TYPE, kManyWords>(a, (int)split, sms, stream);
   }
   const unsigned grid = (unsigned)std::min<uint64_t>(a.n, std::max(1, sms * 2 / kLongBlocks)) * kLongBlocks;
-  if (distill_two(a)) launch_after(distill_long_kernel<TYPE, true>, grid, kLongThreads, 0, stream, a);
-  else launch_after(distill_long_kernel<TYPE, false>, grid, kLongThreads, 0, stream, a);
+  if (distill_mode(a) == ONE_SUM) launch_after(distill_long_kernel<TYPE, ONE_SUM>, grid, kLongThreads, 0, stream, a);
+  else launch_after(distill_long_kernel<TYPE, TWO_SUMS>, grid, kLongThreads, 0, stream, a);
 }
 
 template <int TYPE>
@@ -1024,7 +1058,7 @@ void launch_distill_type(const DistillArgs& a, int sms, cudaStream_t stream) {
   note_launches(3);
   launch_after(distill_lists_kernel<TYPE>, grid, kListWarps * 32, smem, stream, a, table);
   launch_rows<TYPE>(a, sms, stream);
-  launch_after(distill_marks_kernel<TYPE>, grid, kListWarps * 32, 0, stream, a, distill_two(a));
+  launch_after(distill_marks_kernel<TYPE>, grid, kListWarps * 32, 0, stream, a, distill_mode(a) != ONE_SUM);
 }
 
 }  // namespace

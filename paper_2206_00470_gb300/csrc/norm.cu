@@ -80,26 +80,33 @@ __device__ __forceinline__ float warp_elements(uint32_t dim, int lanes, int warp
   return (float)n;
 }
 
-// Mean and sum of squared differences from it over a row's lanes.  Warps find
-// both for their own elements first, so one exchange serves both: with n_w
-// elements of sum s_w, the row's sum is sum q_w + sum n_w (s_w / n_w - m)^2.
-// counts: n_w of every warp.
-template <int VEC, int EL>
-__device__ __forceinline__ float2 row_moments(const float (&x)[EL], float mine, const float* counts, uint32_t dim, int lane,
+// Mean of a row and sum of squared differences from it.  Warps find both for
+// their own elements first, so one exchange serves both: with n_w elements of
+// sum s_w, the row's sum is sum q_w + sum n_w (s_w / n_w - m)^2.  counts: n_w of
+// every warp, mine: this one's.  x (pairs; absent elements are zero) becomes
+// its differences from the mean.
+template <bool FULL, int VEC, int EL>
+__device__ __forceinline__ float2 row_moments(uint64_t (&x)[EL / 2], float mine, const float* counts, uint32_t dim, int lane,
                                               int lanes, float2 (*part)[32], int turn) {
   const int w = lanes < 32 ? lanes : 32;
-  float s = 0.f;
+  uint64_t sum = x[0];
 #pragma unroll
-  for (int j = 0; j < EL; ++j) s += x[j];   // (absent elements are zero)
-  s = lanes_sum(s, w);
-  const float mean_w = mine > 0.f ? s / mine : 0.f;
-  float q = 0.f;
+  for (int j = 1; j < EL / 2; ++j) sum = add_pair(sum, x[j]);
+  const float s = lanes_sum(floats_of(sum).x + floats_of(sum).y, w);
+  const float mean_w = mine > 0.f ? __fdividef(s, mine) : 0.f;
+  const uint64_t minus = pair_of(-mean_w, -mean_w);
+  uint64_t sq = 0;
 #pragma unroll
-  for (int j = 0; j < EL; ++j) {
-    const float d = (uint32_t)((j / VEC) * lanes + lane) * VEC < dim ? x[j] - mean_w : 0.f;
-    q = fmaf(d, d, q);
+  for (int j = 0; j < EL / 2; ++j) {
+    x[j] = add_pair(x[j], minus);
+    if constexpr (!FULL) {
+      const float2 d = floats_of(x[j]);
+      auto here = [&](int e) { return (uint32_t)((e / VEC) * lanes + lane) * VEC + e % VEC < dim; };
+      x[j] = pair_of(here(2 * j) ? d.x : 0.f, here(2 * j + 1) ? d.y : 0.f);
+    }
+    sq = fma_pair(x[j], x[j], sq);
   }
-  q = lanes_sum(q, w);
+  const float q = lanes_sum(floats_of(sq).x + floats_of(sq).y, w);
   if (lanes <= 32) return make_float2(mean_w, q);
   const int wl = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = lanes >> 5;
   if (wl == 0) part[turn][warp] = make_float2(s, q);
@@ -113,6 +120,9 @@ __device__ __forceinline__ float2 row_moments(const float (&x)[EL], float mine, 
     const float n = counts[i], d = n > 0.f ? v.x / n - mean : 0.f;
     all += fmaf(n * d, d, v.y);
   }
+  const uint64_t more = pair_of(mean_w - mean, mean_w - mean);
+#pragma unroll
+  for (int j = 0; j < EL / 2; ++j) x[j] = add_pair(x[j], more);
   return make_float2(mean, all);
 }
 
@@ -125,19 +135,21 @@ struct Raw {
   static constexpr int kWords = VEC == 1 ? EL : EL * kSize / 4;
   uint32_t w[kWords];
 };
-template <int TYPE, int VEC, int EL>
+template <bool FULL, int TYPE, int VEC, int EL>
 __device__ __forceinline__ void fetch(const RowView& v, uint64_t row, uint32_t dim, int lane, int lanes, Raw<TYPE, VEC, EL>& r) {
   const int type = TYPE < 0 ? v.type : TYPE;
   const char* p = v.data + (row_offset(v, (uint32_t)row) + (int64_t)lane * VEC) * type_size(type);
   constexpr int A = EL / VEC, W = Raw<TYPE, VEC, EL>::kWords / A;   // accesses; words of one
+  if constexpr (!FULL) {
 #pragma unroll
-  for (int j = 0; j < Raw<TYPE, VEC, EL>::kWords; ++j) r.w[j] = 0u;
+    for (int j = 0; j < Raw<TYPE, VEC, EL>::kWords; ++j) r.w[j] = 0u;
+  }
   auto all = [&](auto kind) {
     constexpr int T = decltype(kind)::value, S = T == ADAPM_F32 ? 4 : 2;
     const char* q = p;
 #pragma unroll
     for (int i = 0; i < A; ++i, q += (int64_t)lanes * VEC * S) {
-      if ((uint32_t)(i * lanes + lane) * VEC >= dim) continue;
+      if (!FULL && (uint32_t)(i * lanes + lane) * VEC >= dim) continue;
       if constexpr (W == 4) {
         const uint4 x = *reinterpret_cast<const uint4*>(q);
         r.w[4 * i] = x.x; r.w[4 * i + 1] = x.y; r.w[4 * i + 2] = x.z; r.w[4 * i + 3] = x.w;
@@ -155,41 +167,46 @@ __device__ __forceinline__ void fetch(const RowView& v, uint64_t row, uint32_t d
   };
   by_type<TYPE>(type, all);
 }
+// The elements as pairs of floats.
 template <int TYPE, int VEC, int EL>
-__device__ __forceinline__ void unpack_raw(const Raw<TYPE, VEC, EL>& r, float (&x)[EL]) {
-  if constexpr (TYPE == ADAPM_F32 || TYPE < 0) {
+__device__ __forceinline__ void unpack_raw(const Raw<TYPE, VEC, EL>& r, uint64_t (&x)[EL / 2]) {
 #pragma unroll
-    for (int j = 0; j < EL; ++j) x[j] = __uint_as_float(r.w[j]);
-  } else if constexpr (VEC == 1) {
-#pragma unroll
-    for (int j = 0; j < EL; ++j) x[j] = unpack2<TYPE>(r.w[j]).x;
-  } else {
-#pragma unroll
-    for (int j = 0; j < EL / 2; ++j) {
+  for (int j = 0; j < EL / 2; ++j) {
+    if constexpr (TYPE == ADAPM_F32 || TYPE < 0) {
+      x[j] = (uint64_t)r.w[2 * j] | ((uint64_t)r.w[2 * j + 1] << 32);
+    } else if constexpr (VEC == 1) {
+      x[j] = pair_of(unpack2<TYPE>(r.w[2 * j]).x, unpack2<TYPE>(r.w[2 * j + 1]).x);
+    } else {
       const float2 f = unpack2<TYPE>(r.w[j]);
-      x[2 * j] = f.x;
-      x[2 * j + 1] = f.y;
+      x[j] = pair_of(f.x, f.y);
     }
   }
 }
-template <int VEC, int EL>
-__device__ __forceinline__ void store_row(const RowView& v, uint64_t row, uint32_t dim, int lane, int lanes, const float (&y)[EL]) {
+template <bool FULL, int VEC, int EL>
+__device__ __forceinline__ void store_row(const RowView& v, uint64_t row, uint32_t dim, int lane, int lanes, const uint64_t (&pairs)[EL / 2]) {
+  float y[EL];
+#pragma unroll
+  for (int j = 0; j < EL / 2; ++j) {
+    y[2 * j] = floats_of(pairs[j]).x;
+    y[2 * j + 1] = floats_of(pairs[j]).y;
+  }
   auto all = [&](auto kind) {
     constexpr int T = decltype(kind)::value, S = T == ADAPM_F32 ? 4 : 2;
     char* p = v.data + (row_offset(v, (uint32_t)row) + (int64_t)lane * VEC) * S;
 #pragma unroll
     for (int i = 0; i < EL / VEC; ++i, p += (int64_t)lanes * VEC * S)
-      if ((uint32_t)(i * lanes + lane) * VEC < dim) store_n<T, VEC>(p, y + i * VEC);
+      if (FULL || (uint32_t)(i * lanes + lane) * VEC < dim) store_n<T, VEC>(p, y + i * VEC);
   };
   by_type<-1>(v.type, all);
 }
 template <int VEC, int EL>
-__device__ __forceinline__ void load_params(const VectorView& v, uint32_t dim, int lane, int lanes, float none, float (&w)[EL]) {
+__device__ __forceinline__ void load_params(const VectorView& v, uint32_t dim, int lane, int lanes, float none, uint64_t (&pairs)[EL / 2]) {
   if (v.data == nullptr) {
 #pragma unroll
-    for (int j = 0; j < EL; ++j) w[j] = none;
+    for (int j = 0; j < EL / 2; ++j) pairs[j] = pair_of(none, none);
     return;
   }
+  float w[EL];
   auto all = [&](auto kind) {
     constexpr int T = decltype(kind)::value;
 #pragma unroll
@@ -199,9 +216,12 @@ __device__ __forceinline__ void load_params(const VectorView& v, uint32_t dim, i
     }
   };
   by_type<-1>(v.type, all);
+#pragma unroll
+  for (int j = 0; j < EL / 2; ++j) pairs[j] = pair_of(w[2 * j], w[2 * j + 1]);
 }
 
-template <int TYPE, int VEC, int EL>
+// FULL: the lanes hold nothing but elements.
+template <bool FULL, int TYPE, int VEC, int EL>
 __global__ void __launch_bounds__(kMaxLanes)
 norm_kernel(const __grid_constant__ NormArgs a, int lanes) {
   after_previous();
@@ -213,24 +233,25 @@ norm_kernel(const __grid_constant__ NormArgs a, int lanes) {
   uint64_t row = (uint64_t)blockIdx.x * rows + group;
   auto held = [&](uint64_t r) { return r < a.n ? r : a.n - 1; };
   Raw<TYPE, VEC, EL> raw;
-  fetch(a.x, held(row), a.dim, lane, lanes, raw);
-  float w[EL], b[EL];
-  load_params<VEC>(a.weight, a.dim, lane, lanes, 1.f, w);
-  load_params<VEC>(a.bias, a.dim, lane, lanes, 0.f, b);
+  fetch<FULL>(a.x, held(row), a.dim, lane, lanes, raw);
+  uint64_t w[EL / 2], b[EL / 2];
+  load_params<VEC, EL>(a.weight, a.dim, lane, lanes, 1.f, w);
+  load_params<VEC, EL>(a.bias, a.dim, lane, lanes, 0.f, b);
   if (threadIdx.x < 32) counts[threadIdx.x] = (int)threadIdx.x * 32 < lanes ? warp_elements<VEC, EL>(a.dim, lanes, threadIdx.x) : 0.f;
   const float mine = warp_elements<VEC, EL>(a.dim, lanes, lane >> 5);
   if (lanes > 32) __syncthreads();
   int turn = 0;
   for (uint64_t r0 = (uint64_t)blockIdx.x * rows; r0 < a.n; r0 += step, row += step, turn ^= 1) {
-    float x[EL];
+    uint64_t x[EL / 2];
     unpack_raw(raw, x);
-    if (r0 + step < a.n) fetch(a.x, held(row + step), a.dim, lane, lanes, raw);
-    const float2 m = row_moments<VEC>(x, mine, counts, a.dim, lane, lanes, part, turn);
+    if (r0 + step < a.n) fetch<FULL>(a.x, held(row + step), a.dim, lane, lanes, raw);
+    const float2 m = row_moments<FULL, VEC, EL>(x, mine, counts, a.dim, lane, lanes, part, turn);
     const float r = 1.f / sqrtf(m.y / (float)a.dim + a.eps);
     if (row >= a.n) continue;
+    const uint64_t rr = pair_of(r, r);
 #pragma unroll
-    for (int j = 0; j < EL; ++j) x[j] = fmaf((x[j] - m.x) * r, w[j], b[j]);
-    store_row<VEC>(a.out, row, a.dim, lane, lanes, x);
+    for (int j = 0; j < EL / 2; ++j) x[j] = fma_pair(mul_pair(x[j], rr), w[j], b[j]);
+    store_row<FULL, VEC, EL>(a.out, row, a.dim, lane, lanes, x);
     if (a.stats != nullptr && lane == 0) reinterpret_cast<float2*>(a.stats)[row] = make_float2(m.x, r);
   }
 }
@@ -263,7 +284,7 @@ norm_long_kernel(const __grid_constant__ NormArgs a) {
 }
 
 // dx, and every block's sums of dy h and dy over its rows.
-template <int TYPE, int VEC, int EL>
+template <bool FULL, int TYPE, int VEC, int EL>
 __global__ void __launch_bounds__(kMaxLanes)
 norm_grad_kernel(const __grid_constant__ NormArgs a, int lanes) {
   after_previous();
@@ -274,63 +295,71 @@ norm_grad_kernel(const __grid_constant__ NormArgs a, int lanes) {
   uint64_t row = (uint64_t)blockIdx.x * rows + group;
   auto held = [&](uint64_t r) { return r < a.n ? r : a.n - 1; };
   Raw<TYPE, VEC, EL> rx, rg;
-  fetch(a.x, held(row), a.dim, lane, lanes, rx);
-  fetch(a.grad, held(row), a.dim, lane, lanes, rg);
+  fetch<FULL>(a.x, held(row), a.dim, lane, lanes, rx);
+  fetch<FULL>(a.grad, held(row), a.dim, lane, lanes, rg);
   float2 next = reinterpret_cast<const float2*>(a.stats)[held(row)];
-  float w[EL], dw[EL], db[EL];
-  load_params<VEC>(a.weight, a.dim, lane, lanes, 1.f, w);
+  uint64_t w[EL / 2], dw[EL / 2], db[EL / 2];
+  load_params<VEC, EL>(a.weight, a.dim, lane, lanes, 1.f, w);
 #pragma unroll
-  for (int j = 0; j < EL; ++j) dw[j] = db[j] = 0.f;
+  for (int j = 0; j < EL / 2; ++j) dw[j] = db[j] = 0;
   const float inv = 1.f / (float)a.dim;
   int turn = 0;
   for (uint64_t r0 = (uint64_t)blockIdx.x * rows; r0 < a.n; r0 += step, row += step, turn ^= 1) {
     const bool live = row < a.n;
     const float2 st = next;
-    float x[EL], g[EL];
+    uint64_t x[EL / 2], g[EL / 2];
     unpack_raw(rx, x);
     unpack_raw(rg, g);
     if (r0 + step < a.n) {
-      fetch(a.x, held(row + step), a.dim, lane, lanes, rx);
-      fetch(a.grad, held(row + step), a.dim, lane, lanes, rg);
+      fetch<FULL>(a.x, held(row + step), a.dim, lane, lanes, rx);
+      fetch<FULL>(a.grad, held(row + step), a.dim, lane, lanes, rg);
       next = reinterpret_cast<const float2*>(a.stats)[held(row + step)];
     }
-    float s0 = 0.f, s1 = 0.f;
+    const uint64_t minus = pair_of(-st.x, -st.x), rr = pair_of(st.y, st.y);
+    uint64_t s0 = 0, s1 = 0;
+    // (where there is no element g is zero; lanes without a row add to sums that nobody reads)
 #pragma unroll
-    for (int j = 0; j < EL; ++j) {
-      x[j] = (x[j] - st.x) * st.y;   // h
+    for (int j = 0; j < EL / 2; ++j) {
+      x[j] = mul_pair(add_pair(x[j], minus), rr);   // h
       if (live) {
-        dw[j] = fmaf(g[j], x[j], dw[j]);
-        db[j] += g[j];
+        dw[j] = fma_pair(g[j], x[j], dw[j]);
+        db[j] = add_pair(db[j], g[j]);
       }
-      g[j] *= w[j];   // (zero where there is no element)
-      s0 += g[j];
-      s1 = fmaf(g[j], x[j], s1);
+      g[j] = mul_pair(g[j], w[j]);
+      s0 = add_pair(s0, g[j]);
+      s1 = fma_pair(g[j], x[j], s1);
     }
     if (a.out.data == nullptr) continue;
-    const float2 s = row_sum2(s0, s1, lanes, part, turn);
+    const float2 p0 = floats_of(s0), p1 = floats_of(s1);
+    const float2 s = row_sum2(p0.x + p0.y, p1.x + p1.y, lanes, part, turn);
     if (!live) continue;
-    const float c0 = s.x * inv, c1 = s.y * inv;
+    const float c0 = -s.x * inv, c1 = -s.y * inv;
+    const uint64_t m0 = pair_of(c0, c0), m1 = pair_of(c1, c1);
 #pragma unroll
-    for (int j = 0; j < EL; ++j) x[j] = st.y * (g[j] - c0 - x[j] * c1);
-    store_row<VEC>(a.out, row, a.dim, lane, lanes, x);
+    for (int j = 0; j < EL / 2; ++j) x[j] = mul_pair(fma_pair(x[j], m1, add_pair(g[j], m0)), rr);
+    store_row<FULL, VEC, EL>(a.out, row, a.dim, lane, lanes, x);
   }
   if (a.parts == nullptr) return;
   // the block's rows together, group after group
   float* out = a.parts + (uint64_t)blockIdx.x * 2 * a.dim;
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
+    auto element = [&](int j) {
+      const float2 f = floats_of(which ? db[j / 2] : dw[j / 2]);
+      return j % 2 ? f.y : f.x;
+    };
     if (lanes > 32) {   // one row at a time
 #pragma unroll
       for (int j = 0; j < EL; ++j) {
         const uint32_t c = (uint32_t)((j / VEC) * lanes + lane) * VEC + j % VEC;
-        if (c < a.dim) out[which * a.dim + c] = which ? db[j] : dw[j];
+        if (c < a.dim) out[which * a.dim + c] = element(j);
       }
       continue;
     }
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < EL; ++j)
-      sums[group * lanes * EL + ((j / VEC) * lanes + lane) * VEC + j % VEC] = which ? db[j] : dw[j];
+      sums[group * lanes * EL + ((j / VEC) * lanes + lane) * VEC + j % VEC] = element(j);
     __syncthreads();
     for (uint32_t c = threadIdx.x; c < a.dim; c += blockDim.x) {
       float s = 0.f;
@@ -453,16 +482,21 @@ Plan plan_of(const NormArgs& a, bool backward, int sms) {
 constexpr int kLongRows = 64;   // row classes of norm_columns_kernel
 uint64_t part_count(const NormArgs& a, const Plan& p) { return p.wide ? std::min<uint64_t>(a.n, kLongRows) : p.grid; }
 
+template <bool BACK, bool FULL, int TYPE, int VEC, int EL>
+void launch_el(const NormArgs& a, const Plan& p, cudaStream_t stream) {
+  if constexpr (BACK) launch_after(norm_grad_kernel<FULL, TYPE, VEC, EL>, p.grid, p.s.threads, 0, stream, a, p.s.lanes);
+  else launch_after(norm_kernel<FULL, TYPE, VEC, EL>, p.grid, p.s.threads, 0, stream, a, p.s.lanes);
+}
 template <bool BACK, int TYPE, int VEC>
 void launch_as(const NormArgs& a, const Plan& p, cudaStream_t stream) {
   constexpr int MANY = many(TYPE, VEC, BACK);
-  if constexpr (BACK) {
-    if (p.el == kFew) launch_after(norm_grad_kernel<TYPE, VEC, kFew>, p.grid, p.s.threads, 0, stream, a, p.s.lanes);
-    else launch_after(norm_grad_kernel<TYPE, VEC, MANY>, p.grid, p.s.threads, 0, stream, a, p.s.lanes);
-  } else {
-    if (p.el == kFew) launch_after(norm_kernel<TYPE, VEC, kFew>, p.grid, p.s.threads, 0, stream, a, p.s.lanes);
-    else launch_after(norm_kernel<TYPE, VEC, MANY>, p.grid, p.s.threads, 0, stream, a, p.s.lanes);
+  const bool full = (uint64_t)p.s.lanes * p.el == a.dim;
+  if constexpr (VEC > 1) {   // (rows of full lanes are read in wide accesses)
+    if (full && p.el == kFew) return launch_el<BACK, true, TYPE, VEC, kFew>(a, p, stream);
+    if (full) return launch_el<BACK, true, TYPE, VEC, MANY>(a, p, stream);
   }
+  if (p.el == kFew) launch_el<BACK, false, TYPE, VEC, kFew>(a, p, stream);
+  else launch_el<BACK, false, TYPE, VEC, MANY>(a, p, stream);
 }
 template <bool BACK, int TYPE>
 void launch_type(const NormArgs& a, const Plan& p, cudaStream_t stream) {
