@@ -237,6 +237,18 @@ __device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b) {
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
+// 2^x and 1 / x, off by a few units in the last place; 2^x is 0 below the normal numbers.
+__device__ __forceinline__ float exp2_of(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float over(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 // Sum over `width` lanes (a power of two) that begin at a multiple of it; every lane gets it.
 __device__ __forceinline__ float lanes_sum(float x, int width) {
   for (int o = width >> 1; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);

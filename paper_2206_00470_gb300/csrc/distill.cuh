@@ -41,12 +41,6 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kMaxCluster = 16;
 constexpr uint32_t kEmpty = 0x7FFFFFFFu;
 
-__device__ __forceinline__ float exp2_of(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
 template <int TYPE>
 struct Word {
   static constexpr int kSize = TYPE == ADAPM_F32 ? 4 : 2;

@@ -30,11 +30,16 @@ constexpr uint32_t kStage = 32 * 36;        // floats of a warp's staging tile (
 constexpr uint32_t kSmem = 232448;          // shared memory of a block
 constexpr uint32_t kGroupM = 16;            // tiles of m taken together, for L2
 constexpr uint32_t kTurnedRows = 64;        // up to so many rows the weight's columns are m
+constexpr double kPairGain = 1.3;           // the rate of pairs of blocks over that of single ones: 8192 x 4096 x 4096 in
+                                            // 193 us by tiles of 128 x 256, 145 by pairs; across 240, 181
 constexpr uint32_t kMostSplits = 8;         // parts of k: the blocks of a cluster
 
 // ---- activations -----------------------------------------------------------------
-// z / (1 + e^-z); 0 where e^-z is beyond fp32, as in the limit.
-__device__ __forceinline__ float over_one_plus_exp(float z, float minus) { return __fdividef(z, 1.f + __expf(minus)); }
+// 1 / (1 + 2^x); 0 where 2^x is beyond fp32, as in the limit.
+__device__ __forceinline__ float logistic(float x) { return over(1.f + exp2_of(x)); }
+constexpr float kLog2E = 1.4426950408889634f;
+// 1/2 (1 + tanh u) = 1 / (1 + e^-2u); -2 u log2(e) = z (kTanhA z^2 + kTanhB) with u = sqrt(2 / pi) (z + 0.044715 z^3)
+constexpr float kTanhB = -2.f * 0.7978845608f * kLog2E, kTanhA = 0.044715f * kTanhB;
 
 // act(z) of N numbers; the branch stands outside of the loop.
 template <int N>
@@ -48,13 +53,13 @@ __device__ __forceinline__ void activate(float (&z)[N], int kind) {
 #pragma unroll
       for (int j = 0; j < N; ++j) z[j] = 0.5f * z[j] * (1.f + erff(z[j] * 0.70710678f));
       break;
-    case ADAPM_ACTIVATION_GELU_TANH:   // 1/2 (1 + tanh u) = 1 / (1 + e^-2u)
+    case ADAPM_ACTIVATION_GELU_TANH:
 #pragma unroll
-      for (int j = 0; j < N; ++j) z[j] = over_one_plus_exp(z[j], z[j] * fmaf(-0.0713548163f, z[j] * z[j], -1.59576912f));
+      for (int j = 0; j < N; ++j) z[j] *= logistic(z[j] * fmaf(kTanhA, z[j] * z[j], kTanhB));
       break;
     case ADAPM_ACTIVATION_SILU:
 #pragma unroll
-      for (int j = 0; j < N; ++j) z[j] = over_one_plus_exp(z[j], -z[j]);
+      for (int j = 0; j < N; ++j) z[j] *= logistic(-kLog2E * z[j]);
       break;
     case ADAPM_ACTIVATION_TANH:
 #pragma unroll
@@ -74,22 +79,22 @@ __device__ __forceinline__ void times_slope(float (&d)[N], const float (&z)[N], 
     case ADAPM_ACTIVATION_GELU:
 #pragma unroll
       for (int j = 0; j < N; ++j)
-        d[j] *= 0.5f * (1.f + erff(z[j] * 0.70710678f)) + z[j] * 0.39894228f * __expf(-0.5f * z[j] * z[j]);
+        d[j] *= 0.5f * (1.f + erff(z[j] * 0.70710678f)) + z[j] * 0.39894228f * exp2_of(-0.5f * kLog2E * z[j] * z[j]);
       break;
     case ADAPM_ACTIVATION_GELU_TANH:
 #pragma unroll
       for (int j = 0; j < N; ++j) {
-        // s = 1/2 (1 + tanh u), its slope 2 s (1 - s) u'
+        // s = 1 / (1 + e^-2u), its slope s (1 - s) 2 u'
         const float q = z[j] * z[j];
-        const float s = over_one_plus_exp(1.f, z[j] * fmaf(-0.0713548163f, q, -1.59576912f));
-        d[j] *= fmaf(s * (1.f - s) * z[j], fmaf(0.214064449f, q, 1.59576912f), s);
+        const float s = logistic(z[j] * fmaf(kTanhA, q, kTanhB)), t = s * z[j];
+        d[j] *= fmaf(fmaf(-s, t, t), fmaf(-3.f * kTanhA / kLog2E, q, -kTanhB / kLog2E), s);
       }
       break;
     case ADAPM_ACTIVATION_SILU:
 #pragma unroll
       for (int j = 0; j < N; ++j) {
-        const float s = over_one_plus_exp(1.f, -z[j]);
-        d[j] *= s * fmaf(z[j], 1.f - s, 1.f);
+        const float s = logistic(-kLog2E * z[j]), t = s * z[j];
+        d[j] *= fmaf(-s, t, t) + s;
       }
       break;
     case ADAPM_ACTIVATION_TANH:
@@ -107,12 +112,13 @@ __device__ __forceinline__ void times_slope(float (&d)[N], const float (&z)[N], 
 struct Tile {
   uint32_t m0, n0;
 };
+template <bool PAIR>
 __device__ __forceinline__ Tile tile_of(const GemmArgs& g, uint32_t tile) {
   Tile t;
   // groups of kGroupM tiles of m, n by n inside
   const uint32_t in_group = kGroupM * g.tiles_n, group = tile / in_group, at = tile - group * in_group;
   const uint32_t height = min(kGroupM, g.tiles_m - group * kGroupM);
-  t.m0 = (group * kGroupM + at % height) * kTileM;
+  t.m0 = (group * kGroupM + at % height) * (PAIR ? 2 * kTileM : kTileM);
   t.n0 = at / height * g.bn;
   return t;
 }
@@ -213,7 +219,12 @@ __device__ __forceinline__ void finish_tile(const GemmArgs& g, const float* tile
 }
 
 // kGemmThreads threads: warp 0 copies, warp 1 multiplies, the others finish.
-template <bool BF16, bool OUT32>
+// PAIR: tiles of 256 x bn by two blocks; each copies its halves of the operands
+// and finishes its half of the rows, the first one multiplies.  An SM then
+// holds, and writes to its shared memory, half of b's tile: with tiles of 128 x
+// 256 copies and products move 96 KB through it per block of k, 188 bytes a clock at
+// full rate, with pairs 64 KB.
+template <bool BF16, bool OUT32, bool PAIR>
 __global__ void __launch_bounds__(kGemmThreads, 1)
 gemm_kernel(const __grid_constant__ GemmArgs g) {
   constexpr int TYPE = BF16 ? ADAPM_BF16 : ADAPM_F16;
@@ -222,12 +233,14 @@ gemm_kernel(const __grid_constant__ GemmArgs g) {
   __shared__ uint32_t tmem_at;
   __shared__ uint32_t gave_up;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t a_bytes = kTileM * 128, stage_bytes = a_bytes + g.bn * 128;
+  const uint32_t b_rows = PAIR ? g.bn / 2 : g.bn;   // of b's tile, in this block
+  const uint32_t a_bytes = kTileM * 128, stage_bytes = a_bytes + b_rows * 128;
   const uint32_t ring = (shared_at(smem) + 1023u) & ~1023u;
   float* const ring_floats = reinterpret_cast<float*>(smem + (ring - shared_at(smem)));
   float* const staging = ring_floats + g.stages * stage_bytes / 4;
   const uint32_t full = shared_at(bars), empty = full + 8 * kMaxStages, sum_full = empty + 8 * kMaxStages, sum_empty = sum_full + 16;
   const uint32_t columns = 2 * g.bn;   // (bn is a power of two, at least 16)
+  const uint32_t rank = PAIR ? blockIdx.x & 1u : 0;
   if (threadIdx.x == 0) {
     for (uint32_t s = 0; s < g.stages; ++s) {
       barrier_init(full + 8 * s, 1);
@@ -235,20 +248,23 @@ gemm_kernel(const __grid_constant__ GemmArgs g) {
     }
     for (int b = 0; b < 2; ++b) {
       barrier_init(sum_full + 8 * b, 1);
-      barrier_init(sum_empty + 8 * b, kFinishWarps);
+      barrier_init(sum_empty + 8 * b, (PAIR ? 2 : 1) * kFinishWarps);
     }
     gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 1) tmem_take(&tmem_at, columns);
+  if constexpr (PAIR) cg::this_cluster().sync();
+  if (warp == 1) tmem_take<PAIR>(&tmem_at, columns);
   tmem_fence_before();
-  __syncthreads();
+  if constexpr (PAIR) cg::this_cluster().sync();
+  else __syncthreads();
   tmem_fence_after();
   after_previous();
   const uint32_t tmem = tmem_at;
   // with parts of k, each block of a cluster sums one part of one tile
   const uint32_t items = g.tiles_m * g.tiles_n, part = g.splits > 1 ? blockIdx.x % g.splits : 0;
-  const uint32_t first = g.splits > 1 ? blockIdx.x / g.splits : blockIdx.x, step = g.splits > 1 ? items : gridDim.x;
+  const uint32_t first = PAIR ? blockIdx.x / 2 : (g.splits > 1 ? blockIdx.x / g.splits : blockIdx.x);
+  const uint32_t step = PAIR ? gridDim.x / 2 : (g.splits > 1 ? items : gridDim.x);
   const uint32_t k0 = part * g.per_split, k1 = min(g.k_blocks, k0 + g.per_split);
   if (warp == 0) {
     if (lane == 0) {
@@ -256,20 +272,28 @@ gemm_kernel(const __grid_constant__ GemmArgs g) {
       uint32_t n = 0, stage = 0, parity = 1;   // copies issued; a fresh ring is empty
       bool ok = true;
       for (uint32_t i = first; i < items && ok; i += step) {
-        const Tile t = tile_of(g, i);
+        const Tile t = tile_of<PAIR>(g, i);
+        const uint32_t m0 = t.m0 + rank * kTileM, n0 = t.n0 + rank * b_rows;
         for (uint32_t k = k0; k < k1; ++k) {
           if (!(ok = barrier_wait(empty + 8 * stage, parity))) break;
-          const uint32_t bar = full + 8 * stage, at = ring + stage * stage_bytes;
-          barrier_expect(bar, stage_bytes);
+          const uint32_t at = ring + stage * stage_bytes;
+          uint32_t bar = full + 8 * stage;
+          // (the first block's barrier counts both blocks' bytes, before or after it expects them)
+          if (!PAIR || rank == 0) barrier_expect(bar, (PAIR ? 2 : 1) * stage_bytes);
+          if (PAIR) bar = shared_of(bar, 0);
+          auto copy = [&](uint32_t to, const CUtensorMap* map, uint32_t x, uint32_t y) {
+            if constexpr (PAIR) copy_tile_pair(to, map, (int)x, (int)y, bar);
+            else copy_tile(to, map, (int)x, (int)y, bar);
+          };
           if (!g.a_across) {
-            copy_tile(at, &g.a, (int)(k * kBlockK), (int)t.m0, bar);
+            copy(at, &g.a, k * kBlockK, m0);
           } else {
-            for (uint32_t j = 0; j < kTileM; j += 64) copy_tile(at + j * 128, &g.a, (int)(t.m0 + j), (int)(k * kBlockK), bar);
+            for (uint32_t j = 0; j < kTileM; j += 64) copy(at + j * 128, &g.a, m0 + j, k * kBlockK);
           }
           if (!g.b_across) {
-            copy_tile(at + a_bytes, &g.b, (int)(k * kBlockK), (int)t.n0, bar);
+            copy(at + a_bytes, &g.b, k * kBlockK, n0);
           } else {
-            for (uint32_t j = 0; j < g.bn; j += 64) copy_tile(at + a_bytes + j * 128, &g.b, (int)(t.n0 + j), (int)(k * kBlockK), bar);
+            for (uint32_t j = 0; j < b_rows; j += 64) copy(at + a_bytes + j * 128, &g.b, n0 + j, k * kBlockK);
           }
           ++n;
           if (++stage == g.stages) {
@@ -280,14 +304,14 @@ gemm_kernel(const __grid_constant__ GemmArgs g) {
       }
       if (!ok) {
         atomicExch(&gave_up, 1u);
-        // copies in flight land before the block ends
+        // copies in flight land before the block ends (of a pair's second block: its share of the first one's barriers)
         for (uint32_t j = n > g.stages ? n - g.stages : 0; j < n; ++j)
-          if (!barrier_wait(full + 8 * (j % g.stages), (j / g.stages) & 1u)) break;
+          if (!barrier_wait(rank == 0 ? full + 8 * (j % g.stages) : empty + 8 * (j % g.stages), (j / g.stages) & 1u)) break;
       }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      const uint32_t shape = mma_shape(BF16, g.a_across, g.b_across, g.bn);
+    if (lane == 0 && rank == 0) {
+      const uint32_t shape = mma_shape(BF16, g.a_across, g.b_across, PAIR ? 2 * kTileM : kTileM, g.bn);
       const uint32_t a_step = tile_step(g.a_across), b_step = tile_step(g.b_across);
       uint32_t stage = 0, parity = 0, turn = 0;
       bool ok = true;
@@ -302,14 +326,14 @@ gemm_kernel(const __grid_constant__ GemmArgs g) {
           const uint64_t da = tile_descriptor(at, g.a_across), db = tile_descriptor(at + a_bytes, g.b_across);
 #pragma unroll
           for (uint32_t j = 0; j < kBlockK / 16; ++j)
-            mma(tmem + b * g.bn, da + j * a_step, db + j * b_step, shape, k > k0 || j > 0);
-          mma_commit(empty + 8 * stage);
+            mma<PAIR>(tmem + b * g.bn, da + j * a_step, db + j * b_step, shape, k > k0 || j > 0);
+          mma_commit<PAIR>(empty + 8 * stage);
           if (++stage == g.stages) {
             stage = 0;
             parity ^= 1u;
           }
         }
-        mma_commit(sum_full + 8 * b);
+        mma_commit<PAIR>(sum_full + 8 * b);
       }
       if (!ok) atomicExch(&gave_up, 1u);
     }
@@ -319,7 +343,7 @@ gemm_kernel(const __grid_constant__ GemmArgs g) {
     float* const tile = staging + (warp - 2) * kStage;
     uint32_t turn = 0;
     for (uint32_t i = first; i < items; i += step, ++turn) {
-      const Tile t = tile_of(g, i);
+      const Tile t = tile_of<PAIR>(g, i);
       const uint32_t b = turn & 1u;
       if (!barrier_wait(sum_full + 8 * b, (turn >> 1) & 1u)) {
         if (lane == 0) atomicExch(&gave_up, 1u);
@@ -328,7 +352,7 @@ gemm_kernel(const __grid_constant__ GemmArgs g) {
       __syncwarp();
       tmem_fence_after();
       const uint32_t from = tmem + ((quarter * 32u) << 16) + b * g.bn;
-      if (g.splits > 1 || g.turned) {
+      if (!PAIR && (g.splits > 1 || g.turned)) {
         // to shared memory (the ring is no longer read: there is one tile): see below
         const uint32_t row = quarter * 32 + lane;
         for (uint32_t c0 = half * 16; c0 < g.bn; c0 += 32) {
@@ -354,22 +378,25 @@ gemm_kernel(const __grid_constant__ GemmArgs g) {
           for (int j = 0; j < 32; j += 4)
             *reinterpret_cast<float4*>(tile + lane * 36 + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
           __syncwarp();
-          finish_tile<TYPE, OUT32>(g, tile, t.m0 + quarter * 32, t.n0 + c0);
+          finish_tile<TYPE, OUT32>(g, tile, t.m0 + rank * kTileM + quarter * 32, t.n0 + c0);
         }
       }
       tmem_fence_before();
       __syncwarp();
-      if (lane == 0) barrier_arrive(sum_empty + 8 * b);
+      if (lane == 0) {
+        if constexpr (PAIR) barrier_arrive_at(shared_of(sum_empty + 8 * b, 0));
+        else barrier_arrive(sum_empty + 8 * b);
+      }
     }
   }
   __syncwarp();
-  if (g.splits > 1 || g.turned) {
+  if (!PAIR && (g.splits > 1 || g.turned)) {
     // One tile per block, or one part of it: the cluster's blocks add up a
     // share each, in the order of the parts.
     cg::cluster_group cluster = cg::this_cluster();
     if (g.splits > 1) cluster.sync();
     else __syncthreads();
-    const Tile t = tile_of(g, first);
+    const Tile t = tile_of<PAIR>(g, first);
     const uint32_t shift = 31 - __clz(g.bn);
     // four neighbours at a time, of all parts at once
     for (uint32_t j = 4 * (part * kGemmThreads + threadIdx.x); j < kTileM * g.bn; j += 4 * g.splits * kGemmThreads) {
@@ -412,10 +439,11 @@ gemm_kernel(const __grid_constant__ GemmArgs g) {
     if (g.splits > 1) cluster.sync();   // (others may still read here)
   }
   tmem_fence_before();
-  __syncthreads();
+  if constexpr (PAIR) cg::this_cluster().sync();
+  else __syncthreads();
   tmem_fence_after();
   if (threadIdx.x == 0 && gave_up) set_error(g.st, ERR_TIMEOUT);
-  if (warp == 1) tmem_give(tmem, columns);
+  if (warp == 1) tmem_give<PAIR>(tmem, columns);
 }
 
 // ---- operands ------------------------------------------------------------------------
@@ -544,7 +572,7 @@ cudaError_t tensor_map(const Operand& o, bool bf16, uint32_t height, CUtensorMap
 
 // ---- sizes of a product -----------------------------------------------------------------
 struct GemmPlan {
-  bool turned;
+  bool turned, pair;
   uint32_t bn, tiles_m, tiles_n, k_blocks, splits, per_split, stages;
 };
 // The product of `rows` x `columns` elements over k.
@@ -558,13 +586,20 @@ GemmPlan gemm_plan(uint64_t rows, uint32_t columns, uint64_t k, int sms) {
   // narrower tiles while there are too few for every SM
   while (!p.turned && p.bn > 64 && (uint64_t)p.tiles_m * ((n + p.bn - 1) / p.bn) < (uint64_t)sms) p.bn /= 2;
   p.tiles_n = (uint32_t)((n + p.bn - 1) / p.bn);
+  // pairs of blocks on tiles of 256 x 256, unless much of their last round stands idle
+  if (!p.turned && p.bn == 256) {
+    const uint64_t pairs = (m + 2 * kTileM - 1) / (2 * kTileM) * p.tiles_n, alone = (uint64_t)p.tiles_m * p.tiles_n;
+    auto busy = [](uint64_t tiles, uint64_t at_once) { return (double)tiles / (double)((tiles + at_once - 1) / at_once * at_once); };
+    p.pair = kPairGain * busy(pairs, sms / 2) >= busy(alone, sms);
+    if (p.pair) p.tiles_m = (uint32_t)((m + 2 * kTileM - 1) / (2 * kTileM));
+  }
   p.k_blocks = (uint32_t)((k + kBlockK - 1) / kBlockK);
   // parts of k, of at least two blocks, while SMs are idle
   const uint64_t tiles = (uint64_t)p.tiles_m * p.tiles_n;
   const uint64_t want = std::max<uint64_t>(1, std::min<uint64_t>({(uint64_t)sms / tiles, p.k_blocks / 2, kMostSplits}));
   p.per_split = (uint32_t)((p.k_blocks + want - 1) / want);
   p.splits = (p.k_blocks + p.per_split - 1) / p.per_split;
-  const uint32_t stage = kTileM * 128 + p.bn * 128;
+  const uint32_t stage = kTileM * 128 + (p.pair ? p.bn / 2 : p.bn) * 128;
   p.stages = std::min(kMaxStages, (kSmem - 1024 - 512 - kFinishWarps * kStage * (uint32_t)sizeof(float)) / stage);
   return p;
 }
@@ -580,7 +615,7 @@ cudaError_t launch_gemm(const GemmPlan& p, const Operand& left, const Operand& r
   const Operand& a = p.turned ? right : left;
   const Operand& b = p.turned ? left : right;
   cudaError_t err = tensor_map(a, bf16, kTileM, &g.a);
-  if (err == cudaSuccess) err = tensor_map(b, bf16, p.bn, &g.b);
+  if (err == cudaSuccess) err = tensor_map(b, bf16, p.pair ? p.bn / 2 : p.bn, &g.b);
   if (err != cudaSuccess) return err;
   g.a_across = a.across;
   g.b_across = b.across;
@@ -598,26 +633,31 @@ cudaError_t launch_gemm(const GemmPlan& p, const Operand& left, const Operand& r
   g.e = e;
   g.st = st;
   const bool out32 = e.out.type == ADAPM_F32;
-  void (*kernel)(GemmArgs) = bf16 ? (out32 ? gemm_kernel<true, true> : gemm_kernel<true, false>)
-                                  : (out32 ? gemm_kernel<false, true> : gemm_kernel<false, false>);
+  using Kernel = void (*)(GemmArgs);
+  static constexpr Kernel kernels[2][2][2] = {
+      {{gemm_kernel<false, false, false>, gemm_kernel<false, false, true>}, {gemm_kernel<false, true, false>, gemm_kernel<false, true, true>}},
+      {{gemm_kernel<true, false, false>, gemm_kernel<true, false, true>}, {gemm_kernel<true, true, false>, gemm_kernel<true, true, true>}}};
+  const Kernel kernel = kernels[bf16][out32][p.pair];
   err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kSmem - 1024));
   if (err != cudaSuccess) return err;
   // (a block whose tile goes through the ring to its epilogue takes one tile)
   const uint64_t tiles = (uint64_t)p.tiles_m * p.tiles_n;
   const bool single = p.splits > 1 || p.turned;
+  const unsigned cluster = p.pair ? 2 : p.splits;
   cudaLaunchAttribute at[2]{};
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
   at[1].id = cudaLaunchAttributeClusterDimension;
-  at[1].val.clusterDim.x = p.splits;
+  at[1].val.clusterDim.x = cluster;
   at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t c{};
-  c.gridDim = dim3((unsigned)(single ? tiles * p.splits : std::min<uint64_t>(tiles, (uint64_t)sms)));
+  c.gridDim = dim3((unsigned)(p.pair ? 2 * std::min<uint64_t>(tiles, (uint64_t)sms / 2)
+                                     : (single ? tiles * p.splits : std::min<uint64_t>(tiles, (uint64_t)sms))));
   c.blockDim = dim3(kGemmThreads);
-  c.dynamicSmemBytes = 1024 + (size_t)p.stages * (kTileM + p.bn) * 128 + kFinishWarps * kStage * sizeof(float);
+  c.dynamicSmemBytes = 1024 + (size_t)p.stages * (kTileM + (p.pair ? p.bn / 2 : p.bn)) * 128 + kFinishWarps * kStage * sizeof(float);
   c.stream = stream;
   c.attrs = at;
-  c.numAttrs = p.splits > 1 ? 2 : 1;
+  c.numAttrs = cluster > 1 ? 2 : 1;
   note_launches(1);
   return cudaLaunchKernelEx(&c, kernel, g);
 }
@@ -626,9 +666,32 @@ cudaError_t launch_gemm(const GemmPlan& p, const Operand& left, const Operand& r
 // dz = grad act'(pre) to rows of `pitch` elements (to null: grad itself
 // serves), and the sums of its columns over a block's rows: 32 N columns a
 // block, N neighbours a lane, warps take rows by turns, kDzRows at a time.
-constexpr int kDzRows = 2;
+constexpr int kDzRows = 4;
+// N elements of a 16-bit type as they come from memory.
+template <int N>
+struct Packed {
+  uint4 v;
+  __device__ __forceinline__ void fetch(const char* p) {
+    if constexpr (N == 8) v = *reinterpret_cast<const uint4*>(p);
+    else v.x = *reinterpret_cast<const uint16_t*>(p);
+  }
+  template <int TYPE>
+  __device__ __forceinline__ void unpack(float (&x)[N]) const {
+    if constexpr (N == 8) {
+      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float2 f = unpack2<TYPE>(w[j]);
+        x[2 * j] = f.x;
+        x[2 * j + 1] = f.y;
+      }
+    } else {
+      x[0] = unpack2<TYPE>(v.x).x;
+    }
+  }
+};
 template <int TYPE, int N>
-__global__ void __launch_bounds__(256, 4)
+__global__ void __launch_bounds__(256, 3)
 dz_kernel(const MatrixView grad, const MatrixView pre, int activation, char* to, uint32_t pitch, uint64_t rows, uint32_t columns,
           uint32_t per_block, float* parts) {
   after_previous();
@@ -643,24 +706,27 @@ dz_kernel(const MatrixView grad, const MatrixView pre, int activation, char* to,
   for (int j = 0; j < N; ++j) sum[j] = 0.f;
   if (c < columns) {
     for (uint64_t r0 = (uint64_t)block * per_block + warp; r0 < r1; r0 += 8 * kDzRows) {
-      float d[kDzRows][N], z[kDzRows][N];
+      Packed<N> d[kDzRows], z[kDzRows];
 #pragma unroll
       for (int i = 0; i < kDzRows; ++i)
-        if (r0 + i * 8 < r1)
-          load_n<TYPE, N>(grad.data + ((int64_t)(r0 + i * 8) * grad.row_stride + (int64_t)c * grad.col_stride) * 2, d[i]);
+        if (r0 + i * 8 < r1) d[i].fetch(grad.data + ((int64_t)(r0 + i * 8) * grad.row_stride + (int64_t)c * grad.col_stride) * 2);
       if (activation != ADAPM_ACTIVATION_NONE) {
 #pragma unroll
         for (int i = 0; i < kDzRows; ++i)
-          if (r0 + i * 8 < r1)
-            load_n<TYPE, N>(pre.data + ((int64_t)(r0 + i * 8) * pre.row_stride + (int64_t)c * pre.col_stride) * 2, z[i]);
+          if (r0 + i * 8 < r1) z[i].fetch(pre.data + ((int64_t)(r0 + i * 8) * pre.row_stride + (int64_t)c * pre.col_stride) * 2);
       }
 #pragma unroll
       for (int i = 0; i < kDzRows; ++i) {
         if (r0 + i * 8 >= r1) continue;
-        times_slope(d[i], z[i], activation);
-        if (to != nullptr) store_n<TYPE, N>(to + ((r0 + i * 8) * pitch + c) * 2, d[i]);
+        float x[N], y[N];
+        d[i].template unpack<TYPE>(x);
+        if (activation != ADAPM_ACTIVATION_NONE) {
+          z[i].template unpack<TYPE>(y);
+          times_slope(x, y, activation);
+        }
+        if (to != nullptr) store_n<TYPE, N>(to + ((r0 + i * 8) * pitch + c) * 2, x);
 #pragma unroll
-        for (int j = 0; j < N; ++j) sum[j] += d[i][j];
+        for (int j = 0; j < N; ++j) sum[j] += x[j];
       }
     }
   }
@@ -725,8 +791,8 @@ Backward backward_of(const LinearArgs& a, char* scratch, int sms) {
   };
   b.vec = a.outs % 8 == 0 && on_eight(a.grad) && on_eight(a.pre) ? 8 : 1;
   b.across = (a.outs + 32 * b.vec - 1) / (32 * b.vec);
-  // about eight blocks an SM, of at least 32 rows
-  const uint64_t want = std::max<uint64_t>(1, (uint64_t)sms * 8 / b.across);
+  // about six blocks an SM, of at least 32 rows
+  const uint64_t want = std::max<uint64_t>(1, (uint64_t)sms * 6 / b.across);
   b.per_block = (uint32_t)std::max<uint64_t>(32, (a.rows + want - 1) / want);
   b.blocks = (uint32_t)((a.rows + b.per_block - 1) / b.per_block);
   b.sum_bytes = a.dbias.data ? round256((size_t)b.blocks * a.outs * sizeof(float)) : 0;

@@ -23,6 +23,8 @@ SIZES = [(1, 1, 1), (1, 64, 128), (1, 8, 5003), (1, 4096, 300), (2, 7, 9), (5, 3
          (33, 1000, 127), (64, 512, 2048), (65, 64, 64), (100, 63, 65), (127, 129, 257), (128, 128, 256), (129, 72, 40),
          (300, 1024, 520), (777, 256, 1000), (1021, 333, 503), (40, 9000, 24), (130, 20_000, 70), (3000, 96, 3),
          (2500, 17, 1100)]
+# enough tiles of 128 x 256 for every SM: pairs of blocks in the product, in dx, in dweight; sizes that nothing divides
+LARGE = [(2600, 200, 4100), (2600, 4100, 200), (100, 2600, 4100), (2601, 1001, 4099), (4096, 512, 4096)]
 
 
 @pytest.fixture(scope="module")
@@ -113,7 +115,7 @@ def stored(w, by_out):
 @pytest.mark.parametrize("size", range(len(SIZES)))
 def test_whole_numbers_are_exact(gpu_lib, pm, size, dtype):
     """Bit for bit, in every way that the operands are stored in."""
-    rows, ins, outs = SIZES[size]
+    rows, ins, outs = size[0] if isinstance(size, tuple) else SIZES[size]
     x, w = small((rows, ins), dtype), small((ins, outs), dtype)
     b, res = small((outs,), dtype), small((rows, outs), torch.float32)
     grad = small((rows, outs), dtype)
@@ -135,10 +137,23 @@ def test_whole_numbers_are_exact(gpu_lib, pm, size, dtype):
             assert torch.equal(into.bias.double(), grad.double().sum(0))
 
 
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("size", range(len(LARGE)))
+def test_large_products_of_whole_numbers_are_exact(gpu_lib, pm, size, dtype):
+    test_whole_numbers_are_exact(gpu_lib, pm, (LARGE[size],), dtype)
+
+
+@pytest.mark.parametrize("act", ["gelu", "tanh"])
+@pytest.mark.parametrize("size", range(len(LARGE)))
+def test_large_sizes(gpu_lib, pm, size, act):
+    test_every_size(gpu_lib, pm, (LARGE[size],), act)
+
+
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("size", range(len(SIZES)))
 def test_every_size(gpu_lib, pm, size, act):
-    rows, ins, outs = SIZES[size]
+    rows, ins, outs = size[0] if isinstance(size, tuple) else SIZES[size]
+    size = rows + ins
     torch.manual_seed(size)
     for dtype in HALVES:
         x = torch.randn(rows, ins, device="cuda").to(dtype)
