@@ -379,7 +379,7 @@ class _Dense:
     """Descriptors that the calls on dense layers refill (making one anew takes longer than filling it)."""
 
     __slots__ = ("shape", "layer", "rows", "matrices", "vectors", "teacher", "labels", "shape_ref", "layer_ref",
-                 "rows_ref", "matrices_ref", "vectors_ref", "teacher_ref", "labels_ref")
+                 "rows_ref", "other_rows", "matrices_ref", "vectors_ref", "teacher_ref", "labels_ref")
 
     def __init__(self):
         self.shape, self.layer, self.teacher, self.labels = _Shape(), _Layer(), _Teacher(), _Labels()
@@ -387,6 +387,7 @@ class _Dense:
         self.matrices = [_Matrix() for _ in range(6)]
         for name in ("shape", "layer", "teacher", "labels"):
             setattr(self, name + "_ref", ctypes.byref(getattr(self, name)))
+        self.other_rows = self.rows[1:]
         for name in ("rows", "vectors", "matrices"):
             setattr(self, name + "_ref", [ctypes.byref(a) for a in getattr(self, name)])
 
@@ -445,9 +446,11 @@ class ParameterManager:
         self._h = h
         self._handle = stream.cuda_stream
         self._device = torch.device("cuda", torch.cuda.current_device())
+        _type_of(torch.float32)   # (fills the table of types)
         self._t, self._r = _Tokens(), _Rows()   # refilled by every call that takes tokens
         self._t_ref, self._r_ref = ctypes.byref(self._t), ctypes.byref(self._r)
         self._d = _Dense()
+        self._index = self._device.index
 
     # -- plumbing ------------------------------------------------------------
     def _check(self, st):
@@ -691,11 +694,28 @@ class ParameterManager:
 
     # -- dense layers --------------------------------------------------------------
     def _gpu(self, t, what, dtype=None):
-        if not t.is_cuda or t.device.index != self._device.index:
+        if t.get_device() != self._index:
             raise ValueError(f"{what} is a tensor on {self._device}, not on {t.device}")
         if dtype is not None and t.dtype is not dtype:
             raise ValueError(f"{what} is {dtype}, not {t.dtype}")
         return t
+
+    def _same_rows(self, x, *others):
+        """_dense_rows where all are of one shape without gaps on the GPU, None where that takes a closer look."""
+        shape, index = x.shape, self._index
+        if not shape or x.get_device() != index or not x.is_contiguous():
+            return None
+        dim = shape[-1]
+        d, n = self._d, x.numel()
+        s = d.shape
+        s.outer, s.inner, s.dim = 1, n // dim if dim else 0, dim
+        r = d.rows[0]
+        r.data, r.type, r.outer_stride, r.inner_stride = x.data_ptr(), _float_types.get(x.dtype, -1), 0, dim
+        for r, t in zip(d.other_rows, others):
+            if t.shape != shape or t.get_device() != index or not t.is_contiguous():
+                return None
+            r.data, r.type, r.outer_stride, r.inner_stride = t.data_ptr(), _float_types.get(t.dtype, -1), 0, dim
+        return dim
 
     def _dense_rows(self, named):
         """Fills the shape and a descriptor of rows for each (tensor, name, written): all (..., dim), of one shape.
@@ -738,11 +758,12 @@ class ParameterManager:
         """The descriptor of a vector of dim elements (None: none)."""
         if t is None:
             return None
-        if self._gpu(t, what).numel() != dim or not t.is_contiguous():
-            raise ValueError(f"{what} holds {dim} elements without gaps")
-        v = self._d.vectors[i]
-        v.data, v.type = t.data_ptr(), _type_of(t.dtype)
-        return self._d.vectors_ref[i]
+        if t.get_device() != self._index or t.numel() != dim or not t.is_contiguous():
+            raise ValueError(f"{what} holds {dim} elements without gaps on {self._device}")
+        d = self._d
+        v = d.vectors[i]
+        v.data, v.type = t.data_ptr(), _float_types.get(t.dtype, -1)   # (the library refuses other types)
+        return d.vectors_ref[i]
 
     def layer_norm(self, x, weight=None, bias=None, eps=1e-5, out=None, dtype=None, stats=None):
         """(x - mean) / sqrt(variance + eps) * weight + bias for every row of x (..., dim), in dtype (x's unless
@@ -754,20 +775,22 @@ class ParameterManager:
                 out = torch.empty(x.shape, dtype=dtype or x.dtype, device=self._device)
         elif dtype is not None and out.dtype != dtype:
             raise ValueError("out has another dtype")
-        keep = self._dense_rows(((x, "x", False), (out, "out", True)))
-        dim = x.shape[-1]
+        dim, keep = self._same_rows(x, out), None
+        if dim is None:
+            keep = self._dense_rows(((x, "x", False), (out, "out", True)))
+            dim = x.shape[-1]
         w, b = self._dense_vector(0, weight, dim, "weight"), self._dense_vector(1, bias, dim, "bias")
         if stats is not None:
-            self._check_stats(stats, x)
+            self._check_stats(stats, x, dim)
         self._check(self._lib.adapm_layer_norm(self._h, d.shape_ref, d.rows_ref[0], w, b, eps, d.rows_ref[1],
                                                None if stats is None else stats.data_ptr()))
         del keep
         return out
 
-    def _check_stats(self, stats, x):
-        self._gpu(stats, "stats", _torch().float32)
-        if stats.numel() != 2 * (x.numel() // max(1, x.shape[-1])) or not stats.is_contiguous():
-            raise ValueError("stats holds two elements for every row, without gaps")
+    def _check_stats(self, stats, x, dim):
+        if (stats.dtype is not _torch().float32 or stats.get_device() != self._index
+                or stats.numel() * dim != 2 * x.numel() or not stats.is_contiguous()):
+            raise ValueError(f"stats holds two float32 elements for every row, without gaps, on {self._device}")
 
     def layer_norm_grad(self, x, grad, stats, weight=None, bias=None, out=None):
         """NormGrads of layer_norm(x, weight, ..., stats=stats) for the gradient of its output: of x in x's dtype, of
@@ -781,46 +804,54 @@ class ParameterManager:
                 dw, db = (torch.empty(dim, dtype=like, device=self._device) if want else None
                           for want in (weight is not None, weight is not None if bias is None else bias))
                 out = NormGrads(torch.empty(x.shape, dtype=x.dtype, device=self._device), dw, db)
-        rows = [(x, "x", False), (grad, "grad", False)]
-        if out.x is not None:
-            rows.append((out.x, "out.x", True))
-        keep = self._dense_rows(rows)
-        self._check_stats(stats, x)
-        w, dw, db = (self._dense_vector(i, t, dim, what) for i, (t, what) in
-                     enumerate(((weight, "weight"), (out.weight, "out.weight"), (out.bias, "out.bias"))))
+        dx, keep = out.x, None
+        if (self._same_rows(x, grad) if dx is None else self._same_rows(x, grad, dx)) is None:
+            rows = [(x, "x", False), (grad, "grad", False)]
+            if dx is not None:
+                rows.append((dx, "out.x", True))
+            keep = self._dense_rows(rows)
+        self._check_stats(stats, x, dim)
+        w = self._dense_vector(0, weight, dim, "weight")
+        dw, db = self._dense_vector(1, out.weight, dim, "out.weight"), self._dense_vector(2, out.bias, dim, "out.bias")
         self._check(self._lib.adapm_layer_norm_grad(self._h, d.shape_ref, d.rows_ref[0], d.rows_ref[1], stats.data_ptr(),
-                                                    w, None if out.x is None else d.rows_ref[2], dw, db))
+                                                    w, None if dx is None else d.rows_ref[2], dw, db))
         del keep
         return out
 
-    def _matrix(self, i, t, shape, what, written=False):
-        """The descriptor of (..., columns) as rows of columns, of which there are shape[0]; an input whose rows are
-        not one step apart is copied.  Returns the descriptor and the tensor that it describes."""
+    def _matrix(self, i, t, rows, columns, what, written=False):
+        """The descriptor of (..., columns), taken as so many rows; an input whose rows are not one step apart is
+        copied, and the copy returned beside it (None otherwise)."""
         if t is None:
             return None, None
-        rows, columns = shape
-        self._gpu(t, what)
-        if t.shape[-1:] != (columns,) or t.numel() != rows * columns:
-            raise ValueError(f"{what} must be (..., {columns}) with {rows} rows, not {tuple(t.shape)}")
-        step = columns if t.is_contiguous() else (t.stride(0) if t.dim() == 2
-                                                  else _one_stride(t.shape[:-1], t.stride()[:-1]))
-        if step is None:
-            if written:
-                raise ValueError(f"rows of {what} are not one step apart")
-            with self._on_stream():
-                t = t.contiguous()
-            step = columns
-        m = self._d.matrices[i]
-        m.data, m.type, m.row_stride, m.col_stride = t.data_ptr(), _type_of(t.dtype), step, t.stride(-1)
-        return self._d.matrices_ref[i], t
+        shape, copy = t.shape, None
+        if not shape or shape[-1] != columns or t.numel() != rows * columns or t.get_device() != self._index:
+            raise ValueError(f"{what} must be (..., {columns}) with {rows} rows on {self._device}, not {tuple(shape)} on "
+                             f"{t.device}")
+        if t.is_contiguous():
+            step, one = columns, 1
+        else:
+            *steps, one = t.stride()
+            step = steps[0] if len(steps) == 1 else _one_stride(shape[:-1], steps)
+            if step is None:
+                if written:
+                    raise ValueError(f"rows of {what} are not one step apart")
+                with self._on_stream():
+                    copy = t = t.contiguous()
+                step, one = columns, 1
+        d = self._d
+        m = d.matrices[i]
+        m.data, m.type, m.row_stride, m.col_stride = t.data_ptr(), _float_types.get(t.dtype, -1), step, one
+        return d.matrices_ref[i], copy
 
     def _layer(self, x, weight):
-        if weight.dim() != 2 or x.dim() < 1 or x.shape[-1] != weight.shape[0]:
-            raise ValueError(f"x (..., ins) and weight (ins, outs) do not fit: {tuple(x.shape)}, {tuple(weight.shape)}")
+        shape = weight.shape
+        if len(shape) != 2 or not x.shape or x.shape[-1] != shape[0]:
+            raise ValueError(f"x (..., ins) and weight (ins, outs) do not fit: {tuple(x.shape)}, {tuple(shape)}")
+        ins, outs = shape
+        n = x.numel() // ins if ins else 0
         layer = self._d.layer
-        layer.ins, layer.outs = weight.shape
-        layer.rows = n = x.numel() // max(1, layer.ins)
-        return n, layer.ins, layer.outs
+        layer.rows, layer.ins, layer.outs = n, ins, outs
+        return n, ins, outs
 
     def linear(self, x, weight, bias=None, activation=None, residual=None, out=None, dtype=None, pre=None):
         """activation(x weight + bias) + residual for x (..., ins) and weight (ins, outs), both float16 or bfloat16,
@@ -834,12 +865,12 @@ class ParameterManager:
                 out = torch.empty((*x.shape[:-1], outs), dtype=dtype or x.dtype, device=self._device)
         elif dtype is not None and out.dtype != dtype:
             raise ValueError("out has another dtype")
-        xm, x = self._matrix(0, x, (n, ins), "x")
-        wm, weight = self._matrix(1, weight, (ins, outs), "weight")
-        rm, residual = self._matrix(2, residual, (n, outs), "residual")
-        om, out = self._matrix(3, out, (n, outs), "out", True)
-        pm, pre = self._matrix(4, pre, (n, outs), "pre", True)
-        b = self._dense_vector(0, bias, outs, "bias")
+        xm, x = self._matrix(0, x, n, ins, "x")          # (copies stay until the call has taken its arguments)
+        wm, weight = self._matrix(1, weight, ins, outs, "weight")
+        rm, residual = self._matrix(2, residual, n, outs, "residual") if residual is not None else (None, None)
+        om, _ = self._matrix(3, out, n, outs, "out", True)
+        pm, _ = self._matrix(4, pre, n, outs, "pre", True) if pre is not None else (None, None)
+        b = None if bias is None else self._dense_vector(0, bias, outs, "bias")
         self._check(self._lib.adapm_linear(self._h, d.layer_ref, xm, wm, b, _activation(activation), rm, om, pm))
         return out
 
@@ -857,12 +888,12 @@ class ParameterManager:
                 out = LinearGrads(torch.empty(x.shape, dtype=x.dtype, device=self._device),
                                   torch.empty_like(weight),
                                   torch.empty(outs, dtype=weight.dtype, device=self._device) if bias in (None, True) else None)
-        xm, x = self._matrix(0, x, (n, ins), "x")
-        wm, weight = self._matrix(1, weight, (ins, outs), "weight")
-        gm, grad = self._matrix(2, grad, (n, outs), "grad")
-        pm, pre = self._matrix(3, pre if kind else None, (n, outs), "pre")
-        dx, _ = self._matrix(4, out.x, (n, ins), "out.x", True)
-        dw, _ = self._matrix(5, out.weight, (ins, outs), "out.weight", True)
+        xm, x = self._matrix(0, x, n, ins, "x")          # (copies stay until the call has taken its arguments)
+        wm, weight = self._matrix(1, weight, ins, outs, "weight")
+        gm, grad = self._matrix(2, grad, n, outs, "grad")
+        pm, pre = self._matrix(3, pre if kind else None, n, outs, "pre")
+        dx, _ = self._matrix(4, out.x, n, ins, "out.x", True)
+        dw, _ = self._matrix(5, out.weight, ins, outs, "out.weight", True)
         db = self._dense_vector(0, out.bias, outs, "out.bias")
         self._check(self._lib.adapm_linear_grad(self._h, d.layer_ref, xm, wm, gm, pm, kind, dx, dw, db))
         return out
@@ -890,10 +921,12 @@ class ParameterManager:
                         gradient of the loss; weights: float32, one factor per row"""
         torch, d = _torch(), self._d
         lead = logits.shape[:-1]
-        rows = [(logits, "logits", False)]
-        if grad is not None:
-            rows.append((grad, "grad", True))
-        keep = [self._dense_rows(rows)]
+        keep = []
+        if (self._same_rows(logits) if grad is None else self._same_rows(logits, grad)) is None:
+            rows = [(logits, "logits", False)]
+            if grad is not None:
+                rows.append((grad, "grad", True))
+            keep.append(self._dense_rows(rows))
         n = logits.numel() // max(1, logits.shape[-1])
         t = y = None
         if teacher is not None or ids is not None:
@@ -904,8 +937,8 @@ class ParameterManager:
             if not self._gpu(teacher, "teacher").is_contiguous():
                 with self._on_stream():
                     teacher = teacher.contiguous()
-            d.teacher.ids, d.teacher.logits, d.teacher.top = at.data_ptr(), teacher.data_ptr(), top
-            d.teacher.type = _type_of(teacher.dtype)
+            e = d.teacher
+            e.ids, e.logits, e.top, e.type = at.data_ptr(), teacher.data_ptr(), top, _float_types.get(teacher.dtype, -1)
             keep.append((at, teacher))
             t = d.teacher_ref
         if labels is not None:

@@ -6,6 +6,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <atomic>
+
 #include "adapm.h"
 #include "embed.cuh"
 
@@ -15,6 +17,23 @@ namespace adapm {
 struct VectorView {
   char* data;
   int type;
+};
+
+// Asks once per device for what a kernel may use beyond the usual (asking takes
+// the host 0.5 us): dynamic shared memory, and clusters of more than 8 blocks.
+struct Asked {
+  std::atomic<uint32_t> devices{0};
+  template <class K>
+  cudaError_t allow(K kernel, size_t smem, bool large_clusters = false) {
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    const uint32_t bit = 1u << (device & 31);
+    if (e != cudaSuccess || (devices.load(std::memory_order_relaxed) & bit) != 0) return e;
+    if (smem > 48 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e == cudaSuccess && large_clusters) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e == cudaSuccess && device < 32) devices.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+  }
 };
 
 // ---- layer norm (norm.cu) -------------------------------------------------------

@@ -13,7 +13,7 @@
 // that every element has, from one reading.  distill_marks, a warp per row:
 // the loss, and the few elements that list and label change.
 //
-// The second launch comes in three forms.  distill_rows, for rows of up to 32
+// The second launch comes in three forms.  distill_rows, for rows of up to 16
 // KB: a block keeps its row in registers, packed as it came.  distill_slices,
 // up to 1 MB: the blocks of a cluster keep a slice of the row each, which was
 // copied to shared memory while they worked on the row before it, and exchange
@@ -185,17 +185,20 @@ __device__ __forceinline__ float lanes_max(float x) {
 
 constexpr int kListWarps = 4;
 
-// Shared memory: for every warp the ids and the table of slots (`table`, a
-// power of two of at least twice as many) that finds those listed twice.
+// Shared memory: for every warp its row's entries, and the table of slots
+// (`table`, a power of two of at least twice as many) that finds ids listed
+// twice.  A row's loads are in two steps, each all at once: entries, then logits.
 template <int TYPE>
 __global__ void __launch_bounds__(kListWarps * 32)
 distill_lists_kernel(const __grid_constant__ DistillArgs a, uint32_t table) {
   after_previous();
   extern __shared__ uint32_t lists[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  uint32_t* const l_id = lists + warp * (2 * a.top + table);
+  uint32_t* const l_id = lists + warp * (4 * a.top + table);
   uint32_t* const l_slot = l_id + a.top;
-  uint32_t* const l_table = l_slot + a.top;
+  float* const l_t = reinterpret_cast<float*>(l_slot + a.top);
+  float* const l_s = l_t + a.top;
+  uint32_t* const l_table = reinterpret_cast<uint32_t*>(l_s + a.top);
   Entry* const entries = static_cast<Entry*>(a.entries);
   for (uint64_t row = (uint64_t)blockIdx.x * kListWarps + warp; row < a.n; row += (uint64_t)gridDim.x * kListWarps) {
     const char* const logits = a.logits.data + row_offset(a.logits, (uint32_t)row) * Word<TYPE>::kSize;
@@ -213,6 +216,7 @@ distill_lists_kernel(const __grid_constant__ DistillArgs a, uint32_t table) {
       for (uint32_t j = lane; j < table; j += 32) l_table[j] = kEmpty;
       // T ln p_j = t_j - t_max - T ln(sum)
       float largest = -INFINITY;
+#pragma unroll 4
       for (uint32_t j = lane; j < a.top; j += 32) {
         const uint64_t at = row * a.top + j;
         const int64_t id = id_at(a.ids, a.wide, at);
@@ -220,6 +224,8 @@ distill_lists_kernel(const __grid_constant__ DistillArgs a, uint32_t table) {
         const bool here = id >= 0 && id < (int64_t)a.vocab && t != -INFINITY;
         bad = bad || id >= (int64_t)a.vocab || id < -1;
         l_id[j] = here ? (uint32_t)id : kNoKey;
+        l_t[j] = t;
+        l_s[j] = here ? load_as(logits, TYPE, id) : 0.f;
         if (here) {
           task.some = 1;
           largest = fmaxf(largest, t);
@@ -234,7 +240,7 @@ distill_lists_kernel(const __grid_constant__ DistillArgs a, uint32_t table) {
       for (uint32_t j = lane; j < a.top; j += 32) {
         const uint32_t id = l_id[j];
         if (id == kNoKey) continue;
-        sum += exp2_of((load_as(static_cast<const char*>(a.teacher), a.teacher_type, row * a.top + j) - largest) * per_t);
+        sum += exp2_of((l_t[j] - largest) * per_t);
         // the first entry of an id speaks for all (the table has twice as many slots as there are entries)
         uint32_t h = (id * 2654435761u) & (table - 1);
         while (true) {
@@ -257,17 +263,16 @@ distill_lists_kernel(const __grid_constant__ DistillArgs a, uint32_t table) {
         const uint64_t at = row * a.top + j;
         Entry e{l_id[j], 0.f, 0.f};
         if (e.id != kNoKey) {
-          auto d_of = [&](uint32_t i) { return load_as(static_cast<const char*>(a.teacher), a.teacher_type, row * a.top + i) - largest; };
-          const float d = d_of(j);
+          const float d = l_t[j] - largest;
           e.p = exp2_of(d * per_t) / sum;
-          e.s = load_as(logits, TYPE, e.id);
+          e.s = l_s[j];
           if (e.p != 0.f) task.plogp += e.p * (d * inv_t - log_sum);
           if (doubled) {
             if (l_table[l_slot[j]] != j) {
               e.id = kNoKey;
             } else {
               for (uint32_t i = j + 1; i < a.top; ++i)
-                if (l_id[i] == e.id) e.p += exp2_of(d_of(i) * per_t) / sum;
+                if (l_id[i] == e.id) e.p += exp2_of((l_t[i] - largest) * per_t) / sum;
             }
           }
         }
@@ -362,7 +367,7 @@ __device__ __forceinline__ float finite_shift(float m) { return m == -INFINITY ?
 __device__ __forceinline__ bool is_huge(float max, float per) { return fabsf(max * kLog2E) > kHuge || fabsf(max * per) > kHuge; }
 
 // Which sums a row has: at one temperature; at two; at two of which the first is
-// 2, where e^d = (e^(d/2))^2 (3063 rows of 50,021 bf16, both terms: 142 -> 122 us).
+// 2, where e^d = (e^(d/2))^2 (3063 rows of 50,021 bf16, both terms: 164 -> 122 us).
 enum { ONE_SUM = 0, TWO_SUMS = 1, SQUARES = 2 };
 
 // Constants of 2^(s c - k) at both temperatures, as pairs.
@@ -936,6 +941,7 @@ distill_marks_kernel(const __grid_constant__ DistillArgs a, bool two) {
     float cross = 0.f;   // sum of p ln q
     bool label_met = false;
     if (task.some) {
+#pragma unroll 4
       for (uint32_t j = lane; j < a.top; j += 32) {
         const Entry e = static_cast<const Entry*>(a.entries)[row * a.top + j];
         if (e.id == kNoKey) continue;
@@ -1016,8 +1022,8 @@ void launch_slices(const DistillArgs& a, int split, int sms, cudaStream_t stream
   c.stream = stream;
   c.attrs = at;
   c.numAttrs = split > 1 ? 2 : 1;
-  cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)c.dynamicSmemBytes);
-  if (split > 8) cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  static Asked asked[3];
+  asked[mode].allow(kernel, c.dynamicSmemBytes, true);   // (an error shows in the launch)
   const int clusters = clusters_at_once((const void*)kernel, c, split, sms * slice_blocks(NV));
   c.gridDim = dim3((unsigned)(std::min<uint64_t>(a.n, clusters) * split));
   cudaLaunchKernelEx(&c, kernel, a, split);
@@ -1028,7 +1034,6 @@ void launch_rows(const DistillArgs& a, int sms, cudaStream_t stream) {
   const uint64_t words = ((uint64_t)a.vocab * Word<TYPE>::kSize + 15) / 16 + 1;   // (a row may begin inside a word)
   if (words <= 256) return launch_rows_as<TYPE, 128, 2>(a, sms, stream);
   if (words <= 1024) return launch_rows_as<TYPE, 128, 8>(a, sms, stream);
-  if (words <= 2048) return launch_rows_as<TYPE, 512, 4>(a, sms, stream);
   constexpr uint64_t most = kManyWords * kSliceWork, few = kFewWords * kSliceWork;   // words of a slice
   if (words <= kMaxCluster * most) {
     uint32_t split = (uint32_t)((words + most - 1) / most);
@@ -1046,9 +1051,9 @@ template <int TYPE>
 void launch_distill_type(const DistillArgs& a, int sms, cudaStream_t stream) {
   const uint32_t table = a.top > 0 ? power_of_two(2 * a.top) : 0;
   const unsigned grid = (unsigned)std::min<uint64_t>((a.n + kListWarps - 1) / kListWarps, (uint64_t)sms * 16);
-  const size_t smem = kListWarps * (2 * (size_t)a.top + table) * sizeof(uint32_t);
-  if (smem > 48 * 1024)
-    cudaFuncSetAttribute(distill_lists_kernel<TYPE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  const size_t smem = kListWarps * (4 * (size_t)a.top + table) * sizeof(uint32_t);
+  static Asked asked;
+  if (smem > 48 * 1024) asked.allow(distill_lists_kernel<TYPE>, kListWarps * 6 * (size_t)kMaxTop * sizeof(uint32_t));
   note_launches(3);
   launch_after(distill_lists_kernel<TYPE>, grid, kListWarps * 32, smem, stream, a, table);
   launch_rows<TYPE>(a, sms, stream);

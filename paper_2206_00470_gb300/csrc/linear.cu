@@ -638,7 +638,8 @@ cudaError_t launch_gemm(const GemmPlan& p, const Operand& left, const Operand& r
       {{gemm_kernel<false, false, false>, gemm_kernel<false, false, true>}, {gemm_kernel<false, true, false>, gemm_kernel<false, true, true>}},
       {{gemm_kernel<true, false, false>, gemm_kernel<true, false, true>}, {gemm_kernel<true, true, false>, gemm_kernel<true, true, true>}}};
   const Kernel kernel = kernels[bf16][out32][p.pair];
-  err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kSmem - 1024));
+  static Asked asked[2][2][2];
+  err = asked[bf16][out32][p.pair].allow(kernel, kSmem - 1024);
   if (err != cudaSuccess) return err;
   // (a block whose tile goes through the ring to its epilogue takes one tile)
   const uint64_t tiles = (uint64_t)p.tiles_m * p.tiles_n;

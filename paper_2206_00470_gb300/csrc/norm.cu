@@ -265,21 +265,31 @@ norm_long_kernel(const __grid_constant__ NormArgs a) {
   for (uint64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
     const char* x = a.x.data + row_offset(a.x, (uint32_t)row) * type_size(a.x.type);
     char* y = a.out.data + row_offset(a.out, (uint32_t)row) * type_size(a.out.type);
-    float s = 0.f;
-    for (uint32_t c = threadIdx.x; c < a.dim; c += 1024) s += load_as(x, a.x.type, c);
-    const float mean = row_sum2(s, 0.f, 1024, part, 0).x / (float)a.dim;
-    float q = 0.f;
-    for (uint32_t c = threadIdx.x; c < a.dim; c += 1024) {
-      const float d = load_as(x, a.x.type, c) - mean;
-      q = fmaf(d, d, q);
-    }
-    const float r = 1.f / sqrtf(row_sum2(q, 0.f, 1024, part, 1).x / (float)a.dim + a.eps);
-    for (uint32_t c = threadIdx.x; c < a.dim; c += 1024) {
-      const float w = a.weight.data ? load_as(a.weight.data, a.weight.type, c) : 1.f;
-      const float b = a.bias.data ? load_as(a.bias.data, a.bias.type, c) : 0.f;
-      store_as(y, a.out.type, c, fmaf((load_as(x, a.x.type, c) - mean) * r, w, b));
-    }
-    if (a.stats != nullptr && threadIdx.x == 0) reinterpret_cast<float2*>(a.stats)[row] = make_float2(mean, r);
+    by_type<-1>(a.x.type, [&](auto kind) {
+      constexpr int T = decltype(kind)::value;
+      float s = 0.f;
+#pragma unroll 8
+      for (uint32_t c = threadIdx.x; c < a.dim; c += 1024) s += load_as(x, T, c);
+      const float mean = row_sum2(s, 0.f, 1024, part, 0).x / (float)a.dim;
+      float q = 0.f;
+#pragma unroll 8
+      for (uint32_t c = threadIdx.x; c < a.dim; c += 1024) {
+        const float d = load_as(x, T, c) - mean;
+        q = fmaf(d, d, q);
+      }
+      const float r = 1.f / sqrtf(row_sum2(q, 0.f, 1024, part, 1).x / (float)a.dim + a.eps);
+      auto write = [&](auto wkind) {
+        constexpr int W = decltype(wkind)::value;
+#pragma unroll 4
+        for (uint32_t c = threadIdx.x; c < a.dim; c += 1024) {
+          const float w = a.weight.data ? load_as(a.weight.data, W, c) : 1.f;
+          const float b = a.bias.data ? load_as(a.bias.data, a.bias.type, c) : 0.f;
+          store_as(y, a.out.type, c, fmaf((load_as(x, T, c) - mean) * r, w, b));
+        }
+      };
+      by_type<-1>(a.weight.type, write);
+      if (a.stats != nullptr && threadIdx.x == 0) reinterpret_cast<float2*>(a.stats)[row] = make_float2(mean, r);
+    });
   }
 }
 
@@ -380,19 +390,26 @@ norm_grad_long_kernel(const __grid_constant__ NormArgs a) {
     const char* g = a.grad.data + row_offset(a.grad, (uint32_t)row) * type_size(a.grad.type);
     char* dx = a.out.data + row_offset(a.out, (uint32_t)row) * type_size(a.out.type);
     const float2 st = reinterpret_cast<const float2*>(a.stats)[row];
-    float s0 = 0.f, s1 = 0.f;
-    for (uint32_t c = threadIdx.x; c < a.dim; c += 1024) {
-      const float gw = load_as(g, a.grad.type, c) * (a.weight.data ? load_as(a.weight.data, a.weight.type, c) : 1.f);
-      s0 += gw;
-      s1 = fmaf(gw, (load_as(x, a.x.type, c) - st.x) * st.y, s1);
-    }
-    const float2 s = row_sum2(s0, s1, 1024, part, turn);
-    const float c0 = s.x / (float)a.dim, c1 = s.y / (float)a.dim;
-    for (uint32_t c = threadIdx.x; c < a.dim; c += 1024) {
-      const float gw = load_as(g, a.grad.type, c) * (a.weight.data ? load_as(a.weight.data, a.weight.type, c) : 1.f);
-      const float h = (load_as(x, a.x.type, c) - st.x) * st.y;
-      store_as(dx, a.out.type, c, st.y * (gw - c0 - h * c1));
-    }
+    auto both = [&](auto xkind, auto gkind) {
+      constexpr int X = decltype(xkind)::value, G = decltype(gkind)::value;
+      auto gw_at = [&](uint32_t c) { return load_as(g, G, c) * (a.weight.data ? load_as(a.weight.data, a.weight.type, c) : 1.f); };
+      float s0 = 0.f, s1 = 0.f;
+#pragma unroll 4
+      for (uint32_t c = threadIdx.x; c < a.dim; c += 1024) {
+        const float gw = gw_at(c);
+        s0 += gw;
+        s1 = fmaf(gw, (load_as(x, X, c) - st.x) * st.y, s1);
+      }
+      const float2 s = row_sum2(s0, s1, 1024, part, turn);
+      const float c0 = s.x / (float)a.dim, c1 = s.y / (float)a.dim;
+#pragma unroll 4
+      for (uint32_t c = threadIdx.x; c < a.dim; c += 1024)
+        store_as(dx, a.out.type, c, st.y * (gw_at(c) - c0 - (load_as(x, X, c) - st.x) * st.y * c1));
+    };
+    by_type<-1>(a.x.type, [&](auto xkind) {
+      if (a.grad.type == a.x.type) both(xkind, xkind);
+      else by_type<-1>(a.grad.type, [&](auto gkind) { both(xkind, gkind); });
+    });
   }
 }
 
@@ -404,13 +421,19 @@ norm_columns_kernel(const __grid_constant__ NormArgs a) {
   const uint64_t c = (uint64_t)blockIdx.x * 256 + threadIdx.x;
   if (c >= a.dim) return;
   float dw = 0.f, db = 0.f;
-  for (uint64_t row = blockIdx.y; row < a.n; row += gridDim.y) {
-    const float2 st = reinterpret_cast<const float2*>(a.stats)[row];
-    const float g = load_as(a.grad.data + row_offset(a.grad, (uint32_t)row) * type_size(a.grad.type), a.grad.type, c);
-    const float x = load_as(a.x.data + row_offset(a.x, (uint32_t)row) * type_size(a.x.type), a.x.type, c);
-    dw = fmaf(g, (x - st.x) * st.y, dw);
-    db += g;
-  }
+  by_type<-1>(a.x.type, [&](auto xkind) {
+    by_type<-1>(a.grad.type, [&](auto gkind) {
+      constexpr int X = decltype(xkind)::value, G = decltype(gkind)::value;
+#pragma unroll 4
+      for (uint64_t row = blockIdx.y; row < a.n; row += gridDim.y) {
+        const float2 st = reinterpret_cast<const float2*>(a.stats)[row];
+        const float g = load_as(a.grad.data + row_offset(a.grad, (uint32_t)row) * type_size(G), G, c);
+        const float x = load_as(a.x.data + row_offset(a.x, (uint32_t)row) * type_size(X), X, c);
+        dw = fmaf(g, (x - st.x) * st.y, dw);
+        db += g;
+      }
+    });
+  });
   float* out = a.parts + (uint64_t)blockIdx.y * 2 * a.dim;
   out[c] = dw;
   out[a.dim + c] = db;

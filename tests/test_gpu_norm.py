@@ -161,6 +161,37 @@ def test_strides(gpu_lib, pm, view, dim, dtype):
     check_grad(x, grad, stats, w, got)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("dim", [65, 97, 333, 1023, 1025, 4001])
+def test_rows_that_begin_anywhere(gpu_lib, pm, dim, dtype):
+    """Rows one after the other that begin on every element of a 16-byte word; what lies around them stays."""
+    for n in (1, 2, 11, 300, 2500 if dim < 1000 else 1300):
+        size = n * dim
+        w, b = params(dim, torch.float32)
+        for a in (0, 1, 3, 6, 7):
+            x, grad = (rows((size + 16,), dtype, m, 1.0)[a:a + size].view(n, dim) for m in (0.2, 0.0))
+            stats = torch.empty(n, 2, device="cuda")
+            for c in (a, 2):   # (the output begins like the input, or does not)
+                bufs = [torch.full((size + 16,), 7.0, device="cuda", dtype=dtype) for _ in range(2)]
+                out, dx = (t[c:c + size].view(n, dim) for t in bufs)
+                pm.layer_norm(x, w, b, out=out, stats=stats)
+                into = gpu_lib.NormGrads(dx, torch.empty_like(w), torch.empty_like(b))
+                pm.layer_norm_grad(x, grad, stats, w, out=into)
+                pm.wait()
+                check_forward(x, w, b, 1e-5, out, stats)
+                check_grad(x, grad, stats, w, into)
+                for t in bufs:
+                    assert (t[:c] == 7).all() and (t[c + size:] == 7).all()
+            y, g = x.clone().view(-1), grad
+            flat = torch.full((size + 16,), 7.0, device="cuda", dtype=dtype)
+            flat[a:a + size] = y
+            over = flat[a:a + size].view(n, dim)
+            pm.layer_norm(over, w, b, out=over)
+            pm.wait()
+            check_forward(x, w, b, 1e-5, over)
+            assert (flat[:a] == 7).all() and (flat[a + size:] == 7).all()
+
+
 @pytest.mark.parametrize("dim", [20, 256, 1003, 4096, 9001])
 def test_in_place(gpu_lib, pm, dim):
     for dtype in DTYPES:
@@ -223,15 +254,21 @@ def test_large_means_and_constant_rows(gpu_lib, pm, dim):
 
 
 def test_what_is_no_number_stays_in_its_row(gpu_lib, pm):
-    for dim in (48, 3000, 10_000):
-        x = rows((20, dim), torch.bfloat16)
-        clean = pm.layer_norm(x)
+    for dim in (48, 97, 1001, 3000, 10_000):
+        x, stats = rows((20, dim), torch.bfloat16), torch.empty(20, 2, device="cuda")
+        clean = pm.layer_norm(x, stats=stats)
+        grad = rows((20, dim), torch.bfloat16)
+        clean_dx = pm.layer_norm_grad(x, grad, stats).x
         x[3, 5], x[11, dim - 1], x[12, 0] = math.nan, math.inf, -math.inf
-        out = pm.layer_norm(x)
+        grad[7, 0], grad[15, dim - 1] = math.nan, math.inf
+        out = pm.layer_norm(x, stats=stats)
+        dx = pm.layer_norm_grad(x, grad, stats).x
         pm.wait()
         bad = torch.zeros(20, dtype=torch.bool, device="cuda")
         bad[[3, 11, 12]] = True
         assert out[bad].isnan().all() and torch.equal(out[~bad], clean[~bad])
+        bad[[7, 15]] = True
+        assert (~torch.isfinite(dx[bad])).all() and torch.equal(dx[~bad], clean_dx[~bad])
 
 
 def test_gradient_against_differences(gpu_lib, pm):
