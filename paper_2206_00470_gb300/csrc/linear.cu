@@ -30,8 +30,6 @@ constexpr uint32_t kStage = 32 * 36;        // floats of a warp's staging tile (
 constexpr uint32_t kSmem = 232448;          // shared memory of a block
 constexpr uint32_t kGroupM = 16;            // tiles of m taken together, for L2
 constexpr uint32_t kTurnedRows = 64;        // up to so many rows the weight's columns are m
-constexpr double kPairGain = 1.3;           // the rate of pairs of blocks over that of single ones: 8192 x 4096 x 4096 in
-                                            // 193 us by tiles of 128 x 256, 145 by pairs; across 240, 181
 constexpr uint32_t kMostSplits = 8;         // parts of k: the blocks of a cluster
 
 // ---- activations -----------------------------------------------------------------
@@ -575,29 +573,63 @@ struct GemmPlan {
   bool turned, pair;
   uint32_t bn, tiles_m, tiles_n, k_blocks, splits, per_split, stages;
 };
+// What a form of the kernel takes: microseconds before the first round of
+// tiles, per block of k and per tile, as measured with fp16 outputs on sizes
+// from 300 x 512 x 2048 to 4096 x 4096 x 4096.  The form is chosen by the sum,
+// which is near what the sizes below take (rows x ins x outs, us):
+//                        pairs  128 x 256  128 x 128  128 x 64
+//   4096 x 4096 x 4096     89      121        125       215
+//   2048 x 2048 x 2048     19       18         23        35
+//   4096 x 4096 x 512      27       27         22        34
+//   1024 x 1024 x 1024     13       12          9         8
+//    256 x 8192 x 1000     47       67         44        15 (in parts)
+struct Form {
+  bool pair;
+  uint32_t bn;
+  double start, block, tile;
+};
+constexpr Form kForms[] = {
+    {true, 256, 7.6, 0.284, 2.1}, {false, 256, 6.6, 0.345, 1.1}, {false, 128, 4.8, 0.24, 1.2}, {false, 64, 3.5, 0.22, 0.9}};
+constexpr double kPartsCost = 3.0;   // of summing k in parts by a cluster
 // The product of `rows` x `columns` elements over k.
 GemmPlan gemm_plan(uint64_t rows, uint32_t columns, uint64_t k, int sms) {
   GemmPlan p{};
   p.turned = rows <= kTurnedRows;
   const uint64_t m = p.turned ? columns : rows, n = p.turned ? rows : columns;
-  if (p.turned) p.bn = n <= 16 ? 16 : (n <= 32 ? 32 : 64);
-  else p.bn = n <= 64 ? 64 : (n <= 128 ? 128 : 256);
-  p.tiles_m = (uint32_t)((m + kTileM - 1) / kTileM);
-  // narrower tiles while there are too few for every SM
-  while (!p.turned && p.bn > 64 && (uint64_t)p.tiles_m * ((n + p.bn - 1) / p.bn) < (uint64_t)sms) p.bn /= 2;
-  p.tiles_n = (uint32_t)((n + p.bn - 1) / p.bn);
-  // pairs of blocks on tiles of 256 x 256, unless much of their last round stands idle
-  if (!p.turned && p.bn == 256) {
-    const uint64_t pairs = (m + 2 * kTileM - 1) / (2 * kTileM) * p.tiles_n, alone = (uint64_t)p.tiles_m * p.tiles_n;
-    auto busy = [](uint64_t tiles, uint64_t at_once) { return (double)tiles / (double)((tiles + at_once - 1) / at_once * at_once); };
-    p.pair = kPairGain * busy(pairs, sms / 2) >= busy(alone, sms);
-    if (p.pair) p.tiles_m = (uint32_t)((m + 2 * kTileM - 1) / (2 * kTileM));
-  }
   p.k_blocks = (uint32_t)((k + kBlockK - 1) / kBlockK);
+  auto tiles_of = [&](uint32_t bn, bool pair) {
+    const uint64_t height = pair ? 2 * kTileM : kTileM;
+    return ((m + height - 1) / height) * ((n + bn - 1) / bn);
+  };
   // parts of k, of at least two blocks, while SMs are idle
-  const uint64_t tiles = (uint64_t)p.tiles_m * p.tiles_n;
-  const uint64_t want = std::max<uint64_t>(1, std::min<uint64_t>({(uint64_t)sms / tiles, p.k_blocks / 2, kMostSplits}));
-  p.per_split = (uint32_t)((p.k_blocks + want - 1) / want);
+  auto parts_of = [&](uint64_t tiles) {
+    return std::max<uint64_t>(1, std::min<uint64_t>({(uint64_t)sms / tiles, p.k_blocks / 2, kMostSplits}));
+  };
+  uint64_t parts = 1;
+  if (p.turned) {
+    p.bn = n <= 16 ? 16 : (n <= 32 ? 32 : 64);
+    parts = parts_of(tiles_of(p.bn, false));
+  } else {
+    double best = 0.0;
+    for (const Form& f : kForms) {
+      const uint64_t tiles = tiles_of(f.bn, f.pair), at_once = f.pair ? sms / 2 : sms;
+      const double rounds = (double)((tiles + at_once - 1) / at_once);
+      for (int in_parts = 0; in_parts < 2; ++in_parts) {
+        const uint64_t s = in_parts ? parts_of(tiles) : 1;
+        if (in_parts && (s == 1 || f.bn > 64)) continue;   // (128 x 128 in parts: 1327 x 3315 x 651 30 -> 35)
+        const double us = f.start + (in_parts ? kPartsCost : 0.0) + rounds * ((double)((p.k_blocks + s - 1) / s) * f.block + f.tile);
+        if (best != 0.0 && us >= best) continue;
+        best = us;
+        p.pair = f.pair;
+        p.bn = f.bn;
+        parts = s;
+      }
+    }
+  }
+  const uint32_t height = p.pair ? 2 * kTileM : kTileM;
+  p.tiles_m = (uint32_t)((m + height - 1) / height);
+  p.tiles_n = (uint32_t)((n + p.bn - 1) / p.bn);
+  p.per_split = (uint32_t)((p.k_blocks + parts - 1) / parts);
   p.splits = (p.k_blocks + p.per_split - 1) / p.per_split;
   const uint32_t stage = kTileM * 128 + (p.pair ? p.bn / 2 : p.bn) * 128;
   p.stages = std::min(kMaxStages, (kSmem - 1024 - 512 - kFinishWarps * kStage * (uint32_t)sizeof(float)) / stage);
