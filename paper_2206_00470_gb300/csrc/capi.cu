@@ -2255,11 +2255,13 @@ adapm_status adapm_distill(adapm_ctx* ctx, const adapm_shape* shape, const adapm
   a.st = ctx->dstate;
   ProfScope ps(ctx, 5);
   char *tasks = nullptr, *entries = nullptr;
-  CK(pool_alloc(ctx, &tasks, n * (kTaskBytes + kRowSumBytes)));
-  if (a.top > 0) CK(pool_alloc(ctx, &entries, n * a.top * kEntryBytes));
-  a.tasks = tasks;
-  a.sums = tasks + n * kTaskBytes;
-  a.entries = entries;
+  if (!distill_in_one(n, a.vocab, a.logits.type, ctx->sms)) {
+    CK(pool_alloc(ctx, &tasks, n * (kTaskBytes + kRowSumBytes)));
+    if (a.top > 0) CK(pool_alloc(ctx, &entries, n * a.top * kEntryBytes));
+    a.tasks = tasks;
+    a.sums = tasks + n * kTaskBytes;
+    a.entries = entries;
+  }
   launch_distill(a, ctx->sms, ctx->stream);
   pool_free(ctx, tasks);
   pool_free(ctx, entries);

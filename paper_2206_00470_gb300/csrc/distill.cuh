@@ -7,11 +7,12 @@
 //   loss = soft T^2 sum_j p_j (ln p_j - ln q_id_j) + hard (-ln c_y)
 //   grad_v = f (soft T (q_v - sum_{id_j = v} p_j) + hard (c_v - [v = y])),  f = scale weights[r]
 //
-// Three launches.  distill_lists, a warp per row: the list's p, one entry for
-// all that share an id, and the logits at its ids and at the label.
-// distill_rows: sums of exponentials of each row and the part of the gradient
-// that every element has, from one reading.  distill_marks, a warp per row:
-// the loss, and the few elements that list and label change.
+// Three launches, or one where there are few rows (distill_few).  distill_lists,
+// a warp per row: the list's p, one entry for all that share an id, and the
+// logits at its ids and at the label.  distill_rows: sums of exponentials of
+// each row and the part of the gradient that every element has, from one
+// reading.  distill_marks, a warp per row: the loss, and the few elements that
+// list and label change.
 //
 // The second launch comes in three forms.  distill_rows, for rows of up to 16
 // KB: a block keeps its row in registers, packed as it came.  distill_slices,
@@ -183,105 +184,118 @@ __device__ __forceinline__ float lanes_max(float x) {
   return x;
 }
 
-constexpr int kListWarps = 4;
+// A warp's entries of a row in shared memory, and the table of slots (`table`,
+// a power of two of at least twice as many) that finds ids listed twice.
+struct Lists {
+  uint32_t *id, *slot, *tab;
+  float *t, *s;
+  static __host__ __device__ constexpr uint32_t words(uint32_t top, uint32_t table) { return 4 * top + table; }
+  __device__ __forceinline__ Lists(uint32_t* at, uint32_t top)
+      : id(at), slot(at + top), tab(at + 4 * top), t(reinterpret_cast<float*>(at + 2 * top)), s(reinterpret_cast<float*>(at + 3 * top)) {}
+};
+// Warp-wide: what there is to learn from a row's list and label.  Afterwards
+// l.id[j] is the id of entry j (kNoKey: none, or another one speaks for it),
+// l.t[j] its p and l.s[j] its logit.  The loads are in two steps, each all at
+// once: entries, then logits.
+template <int TYPE>
+__device__ __forceinline__ RowTask read_lists(const DistillArgs& a, uint64_t row, const Lists& l, uint32_t table) {
+  const int lane = threadIdx.x & 31;
+  const char* const logits = a.logits.data + row_offset(a.logits, (uint32_t)row) * Word<TYPE>::kSize;
+  RowTask task{0.f, 0.f, -1, 0};
+  bool bad = false;
+  if (a.labels != nullptr) {
+    const int64_t y = id_at(a.labels, a.wide_labels, row);
+    if (!(a.has_pad && y == a.pad)) {
+      if (y >= 0 && y < (int64_t)a.vocab) task.label = (int32_t)y;
+      else bad = true;
+    }
+    if (task.label >= 0) task.label_s = load_as(logits, TYPE, task.label);
+  }
+  if (a.top > 0) {
+    for (uint32_t j = lane; j < table; j += 32) l.tab[j] = kEmpty;
+    // T ln p_j = t_j - t_max - T ln(sum)
+    float largest = -INFINITY;
+#pragma unroll 4
+    for (uint32_t j = lane; j < a.top; j += 32) {
+      const uint64_t at = row * a.top + j;
+      const int64_t id = id_at(a.ids, a.wide, at);
+      const float t = load_as(static_cast<const char*>(a.teacher), a.teacher_type, at);
+      const bool here = id >= 0 && id < (int64_t)a.vocab && t != -INFINITY;
+      bad = bad || id >= (int64_t)a.vocab || id < -1;
+      l.id[j] = here ? (uint32_t)id : kNoKey;
+      l.t[j] = t;
+      l.s[j] = here ? load_as(logits, TYPE, id) : 0.f;
+      if (here) {
+        task.some = 1;
+        largest = fmaxf(largest, t);
+      }
+    }
+    __syncwarp();
+    largest = lanes_max(largest);
+    task.some = __any_sync(0xFFFFFFFFu, task.some);
+    const float per_t = kLog2E / a.temperature, inv_t = 1.f / a.temperature;
+    bool doubled = false;
+    float sum = 0.f;
+    for (uint32_t j = lane; j < a.top; j += 32) {
+      const uint32_t id = l.id[j];
+      if (id == kNoKey) continue;
+      sum += exp2_of((l.t[j] - largest) * per_t);
+      // the first entry of an id speaks for all (the table has twice as many slots as there are entries)
+      uint32_t h = (id * 2654435761u) & (table - 1);
+      while (true) {
+        const uint32_t old = atomicCAS(&l.tab[h], kEmpty, j);
+        if (old == kEmpty) break;
+        if (l.id[old] == id) {
+          atomicMin(&l.tab[h], j);
+          doubled = true;
+          break;
+        }
+        h = (h + 1) & (table - 1);
+      }
+      l.slot[j] = h;
+    }
+    __syncwarp();
+    doubled = __any_sync(0xFFFFFFFFu, doubled);
+    sum = lanes_sum(sum, 32);
+    const float log_sum = logf(sum);
+    for (uint32_t j = lane; j < a.top; j += 32) {
+      if (l.id[j] == kNoKey) continue;
+      const float d = l.t[j] - largest, p = exp2_of(d * per_t) / sum;
+      if (p != 0.f) task.plogp += p * (d * inv_t - log_sum);
+      l.t[j] = p;
+    }
+    task.plogp = lanes_sum(task.plogp, 32);
+    __syncwarp();
+    if (doubled) {
+      for (uint32_t j = lane; j < a.top; j += 32) {
+        if (l.id[j] == kNoKey || l.tab[l.slot[j]] != j) continue;
+        float p = l.t[j];
+        for (uint32_t i = j + 1; i < a.top; ++i)
+          if (l.id[i] == l.id[j]) p += l.t[i];
+        l.t[j] = p;   // (an entry that speaks is no other one's)
+      }
+      __syncwarp();
+      for (uint32_t j = lane; j < a.top; j += 32)
+        if (l.id[j] != kNoKey && l.tab[l.slot[j]] != j) l.id[j] = kNoKey;
+      __syncwarp();
+    }
+  }
+  if (bad) set_error(a.st, ERR_KEY_RANGE);
+  return task;
+}
 
-// Shared memory: for every warp its row's entries, and the table of slots
-// (`table`, a power of two of at least twice as many) that finds ids listed
-// twice.  A row's loads are in two steps, each all at once: entries, then logits.
+constexpr int kListWarps = 4;
 template <int TYPE>
 __global__ void __launch_bounds__(kListWarps * 32)
 distill_lists_kernel(const __grid_constant__ DistillArgs a, uint32_t table) {
   after_previous();
   extern __shared__ uint32_t lists[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  uint32_t* const l_id = lists + warp * (4 * a.top + table);
-  uint32_t* const l_slot = l_id + a.top;
-  float* const l_t = reinterpret_cast<float*>(l_slot + a.top);
-  float* const l_s = l_t + a.top;
-  uint32_t* const l_table = reinterpret_cast<uint32_t*>(l_s + a.top);
-  Entry* const entries = static_cast<Entry*>(a.entries);
+  const Lists l(lists + warp * Lists::words(a.top, table), a.top);
   for (uint64_t row = (uint64_t)blockIdx.x * kListWarps + warp; row < a.n; row += (uint64_t)gridDim.x * kListWarps) {
-    const char* const logits = a.logits.data + row_offset(a.logits, (uint32_t)row) * Word<TYPE>::kSize;
-    RowTask task{0.f, 0.f, -1, 0};
-    bool bad = false;
-    if (a.labels != nullptr) {
-      const int64_t y = id_at(a.labels, a.wide_labels, row);
-      if (!(a.has_pad && y == a.pad)) {
-        if (y >= 0 && y < (int64_t)a.vocab) task.label = (int32_t)y;
-        else bad = true;
-      }
-      if (task.label >= 0) task.label_s = load_as(logits, TYPE, task.label);
-    }
-    if (a.top > 0) {
-      for (uint32_t j = lane; j < table; j += 32) l_table[j] = kEmpty;
-      // T ln p_j = t_j - t_max - T ln(sum)
-      float largest = -INFINITY;
-#pragma unroll 4
-      for (uint32_t j = lane; j < a.top; j += 32) {
-        const uint64_t at = row * a.top + j;
-        const int64_t id = id_at(a.ids, a.wide, at);
-        const float t = load_as(static_cast<const char*>(a.teacher), a.teacher_type, at);
-        const bool here = id >= 0 && id < (int64_t)a.vocab && t != -INFINITY;
-        bad = bad || id >= (int64_t)a.vocab || id < -1;
-        l_id[j] = here ? (uint32_t)id : kNoKey;
-        l_t[j] = t;
-        l_s[j] = here ? load_as(logits, TYPE, id) : 0.f;
-        if (here) {
-          task.some = 1;
-          largest = fmaxf(largest, t);
-        }
-      }
-      __syncwarp();
-      largest = lanes_max(largest);
-      task.some = __any_sync(0xFFFFFFFFu, task.some);
-      const float per_t = kLog2E / a.temperature, inv_t = 1.f / a.temperature;
-      bool doubled = false;
-      float sum = 0.f;
-      for (uint32_t j = lane; j < a.top; j += 32) {
-        const uint32_t id = l_id[j];
-        if (id == kNoKey) continue;
-        sum += exp2_of((l_t[j] - largest) * per_t);
-        // the first entry of an id speaks for all (the table has twice as many slots as there are entries)
-        uint32_t h = (id * 2654435761u) & (table - 1);
-        while (true) {
-          const uint32_t old = atomicCAS(&l_table[h], kEmpty, j);
-          if (old == kEmpty) break;
-          if (l_id[old] == id) {
-            atomicMin(&l_table[h], j);
-            doubled = true;
-            break;
-          }
-          h = (h + 1) & (table - 1);
-        }
-        l_slot[j] = h;
-      }
-      __syncwarp();
-      doubled = __any_sync(0xFFFFFFFFu, doubled);
-      sum = lanes_sum(sum, 32);
-      const float log_sum = logf(sum);
-      for (uint32_t j = lane; j < a.top; j += 32) {
-        const uint64_t at = row * a.top + j;
-        Entry e{l_id[j], 0.f, 0.f};
-        if (e.id != kNoKey) {
-          const float d = l_t[j] - largest;
-          e.p = exp2_of(d * per_t) / sum;
-          e.s = l_s[j];
-          if (e.p != 0.f) task.plogp += e.p * (d * inv_t - log_sum);
-          if (doubled) {
-            if (l_table[l_slot[j]] != j) {
-              e.id = kNoKey;
-            } else {
-              for (uint32_t i = j + 1; i < a.top; ++i)
-                if (l_id[i] == e.id) e.p += exp2_of((l_t[i] - largest) * per_t) / sum;
-            }
-          }
-        }
-        entries[at] = e;
-      }
-      task.plogp = lanes_sum(task.plogp, 32);
-      __syncwarp();
-    }
-    if (bad) set_error(a.st, ERR_KEY_RANGE);
+    const RowTask task = read_lists<TYPE>(a, row, l, table);
+    for (uint32_t j = lane; j < a.top; j += 32) static_cast<Entry*>(a.entries)[row * a.top + j] = Entry{l.id[j], l.t[j], l.s[j]};
+    __syncwarp();
     if (lane == 0) static_cast<RowTask*>(a.tasks)[row] = task;
   }
 }
@@ -913,54 +927,137 @@ distill_long_kernel(const __grid_constant__ DistillArgs a) {
   cluster.sync();   // (others may still write here)
 }
 
-// The loss, and the elements that list and label change.
+// Warp-wide: a row's loss, and the elements that list and label change;
+// entry(j): entry j of its list.
+template <int TYPE, class F>
+__device__ __forceinline__ void write_marks(const DistillArgs& a, uint64_t row, const RowTask& task, const RowSums& all, bool two, F&& entry) {
+  const int lane = threadIdx.x & 31;
+  if (!task.some && task.label < 0) {
+    if (lane == 0) a.loss[row] = 0.f;
+    return;
+  }
+  const float per = a.top > 0 ? kLog2E / a.temperature : kLog2E;
+  const float inv_t = 1.f / a.temperature;
+  const RowScale scale = row_scale(a, row, task, all, two);
+  const float f = a.weights != nullptr ? a.scale * a.weights[row] : a.scale;
+  const float log_st = logf(all.t), log_s1 = two ? logf(all.one) : log_st;
+  const bool write = a.grad.data != nullptr;
+  char* const grad = write ? a.grad.data + row_offset(a.grad, (uint32_t)row) * Word<TYPE>::kSize : nullptr;
+  auto dense = [&](float s) {   // the part that every element has
+    const float d = s - all.max;
+    const float x = exp2_of(d * per) * scale.t;
+    return two ? fmaf(exp2_of(d * kLog2E), scale.one, x) : x;
+  };
+  float cross = 0.f;   // sum of p ln q
+  bool label_met = false;
+  if (task.some) {
+#pragma unroll 4
+    for (uint32_t j = lane; j < a.top; j += 32) {
+      const Entry e = entry(j);
+      if (e.id == kNoKey) continue;
+      if (e.p != 0.f) cross += e.p * ((e.s - all.max) * inv_t - log_st);
+      const bool labelled = task.label == (int32_t)e.id;
+      label_met = label_met || labelled;
+      if (write) store_as(grad, TYPE, e.id, dense(e.s) - f * (a.soft * a.temperature * e.p + (labelled ? a.hard : 0.f)));
+    }
+    label_met = __any_sync(0xFFFFFFFFu, label_met);
+    cross = lanes_sum(cross, 32);
+  }
+  if (lane != 0) return;
+  float loss = task.some ? a.soft * a.temperature * a.temperature * (task.plogp - cross) : 0.f;
+  if (task.label >= 0) {
+    loss -= a.hard * ((task.label_s - all.max) - log_s1);
+    if (write && !label_met) store_as(grad, TYPE, task.label, dense(task.label_s) - f * a.hard);
+  }
+  a.loss[row] = loss;
+}
 template <int TYPE>
 __global__ void __launch_bounds__(kListWarps * 32)
 distill_marks_kernel(const __grid_constant__ DistillArgs a, bool two) {
   after_previous();
+  const int warp = threadIdx.x >> 5;
+  for (uint64_t row = (uint64_t)blockIdx.x * kListWarps + warp; row < a.n; row += (uint64_t)gridDim.x * kListWarps)
+    write_marks<TYPE>(a, row, static_cast<const RowTask*>(a.tasks)[row], static_cast<const RowSums*>(a.sums)[row], two,
+                      [&](uint32_t j) { return static_cast<const Entry*>(a.entries)[row * a.top + j]; });
+}
+
+// ---- few rows ---------------------------------------------------------------------------
+// All of it in one launch, a block per row that fits its registers: warp 0 reads
+// the list while the row is on its way, and writes what it changes behind the
+// others' gradient.
+constexpr int kFewThreads = 1024;
+template <int TYPE, int NV, int MODE>
+__global__ void __launch_bounds__(kFewThreads)
+distill_few_kernel(const __grid_constant__ DistillArgs a, uint32_t table) {
+  after_previous();
+  extern __shared__ uint32_t lists[];
+  __shared__ RowSums warps[32];
+  __shared__ RowTask shared_task;
+  constexpr int E = Word<TYPE>::kElements;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const uint64_t row = blockIdx.x;
   const float per = a.top > 0 ? kLog2E / a.temperature : kLog2E;
-  const float inv_t = 1.f / a.temperature;
-  for (uint64_t row = (uint64_t)blockIdx.x * kListWarps + warp; row < a.n; row += (uint64_t)gridDim.x * kListWarps) {
-    const RowTask task = static_cast<const RowTask*>(a.tasks)[row];
-    if (!task.some && task.label < 0) {
-      if (lane == 0) a.loss[row] = 0.f;
-      continue;
-    }
-    const RowSums all = static_cast<const RowSums*>(a.sums)[row];
-    const RowScale scale = row_scale(a, row, task, all, two);
-    const float f = a.weights != nullptr ? a.scale * a.weights[row] : a.scale;
-    const float log_st = logf(all.t), log_s1 = two ? logf(all.one) : log_st;
-    const bool write = a.grad.data != nullptr;
-    char* const grad = write ? a.grad.data + row_offset(a.grad, (uint32_t)row) * Word<TYPE>::kSize : nullptr;
-    auto dense = [&](float s) {   // the part that every element has
-      const float d = s - all.max;
-      const float x = exp2_of(d * per) * scale.t;
-      return two ? fmaf(exp2_of(d * kLog2E), scale.one, x) : x;
-    };
-    float cross = 0.f;   // sum of p ln q
-    bool label_met = false;
-    if (task.some) {
-#pragma unroll 4
-      for (uint32_t j = lane; j < a.top; j += 32) {
-        const Entry e = static_cast<const Entry*>(a.entries)[row * a.top + j];
-        if (e.id == kNoKey) continue;
-        if (e.p != 0.f) cross += e.p * ((e.s - all.max) * inv_t - log_st);
-        const bool labelled = task.label == (int32_t)e.id;
-        label_met = label_met || labelled;
-        if (write) store_as(grad, TYPE, e.id, dense(e.s) - f * (a.soft * a.temperature * e.p + (labelled ? a.hard : 0.f)));
-      }
-      label_met = __any_sync(0xFFFFFFFFu, label_met);
-      cross = lanes_sum(cross, 32);
-    }
-    if (lane != 0) continue;
-    float loss = task.some ? a.soft * a.temperature * a.temperature * (task.plogp - cross) : 0.f;
-    if (task.label >= 0) {
-      loss -= a.hard * ((task.label_s - all.max) - log_s1);
-      if (write && !label_met) store_as(grad, TYPE, task.label, dense(task.label_s) - f * a.hard);
-    }
-    a.loss[row] = loss;
+  const RowWords b = row_words<TYPE>(a.logits, row, a.vocab);
+  uint4 v[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) v[i] = load_word<TYPE>(b, a.vocab, i * kFewThreads + threadIdx.x);
+  const Lists l(lists, a.top);
+  if (warp == 0) {
+    const RowTask task = read_lists<TYPE>(a, row, l, table);
+    if (lane == 0) shared_task = task;
   }
+  Largest<TYPE> largest;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) largest.see(v[i]);
+  RowSums mine;
+  mine.max = lanes_max(largest.value());
+  const float shift = finite_shift(mine.max);
+  const bool huge = is_huge(shift, per);
+  const float k = huge ? 0.f : shift;
+  const Exponents e(per, k);
+  uint64_t st = 0, so = 0;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    uint4 word = v[i];
+    if (huge) take_off<TYPE>(word, shift);
+    add_word<TYPE, MODE>(word, e, st, so);
+  }
+  const float2 t = floats_of(st), o = floats_of(so), u = unround_both<MODE>(k, per);
+  mine.t = lanes_sum((t.x + t.y) * u.x, 32);
+  mine.one = MODE != ONE_SUM ? lanes_sum((o.x + o.y) * u.y, 32) : 0.f;
+  if (lane == 0) warps[warp] = mine;
+  __syncthreads();
+  const RowTask task = shared_task;
+  const bool live = task.some || task.label >= 0;
+  const RowSums all = merge_sums<MODE>(warps[lane], 32, per);
+  if (a.grad.data != nullptr) {
+    const RowWords g = row_words<TYPE>(a.grad, row, a.vocab);
+    if (!live) {
+      for (uint32_t w = threadIdx.x; w < g.words; w += kFewThreads) store_word<TYPE>(g, a.vocab, w, make_uint4(0, 0, 0, 0));
+    } else {
+      const RowFactors f = row_factors<TYPE, MODE>(a, row, task, all, per);
+      with_gradient<TYPE, MODE>(f, per, [&](const auto& gradient) {
+        if (g.head == b.head) {
+          if (f.huge) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) take_off<TYPE>(v[i], f.max);
+          }
+#pragma unroll
+          for (int i = 0; i < NV; ++i) store_word<TYPE>(g, a.vocab, i * kFewThreads + threadIdx.x, gradient.of(v[i]));
+        } else {
+          // words of the gradient that begin elsewhere: the row again, from L2
+          const uint32_t shift_by = (b.head - g.head) & (E - 1), back = b.head < g.head ? 1 : 0;
+          for (uint32_t w = threadIdx.x; w < g.words; w += kFewThreads) {
+            uint4 word = load_shifted<TYPE>(b, a.vocab, w - back, shift_by);
+            if (f.huge) take_off<TYPE>(word, f.max);
+            store_word<TYPE>(g, a.vocab, w, gradient.of(word));
+          }
+        }
+      });
+    }
+    __syncthreads();   // the marks are written over it
+  }
+  if (warp == 0) write_marks<TYPE>(a, row, task, all, MODE != ONE_SUM, [&](uint32_t j) { return Entry{l.id[j], l.t[j], l.s[j]}; });
 }
 
 // Smallest power of two that is at least n.
@@ -1031,7 +1128,7 @@ void launch_slices(const DistillArgs& a, int split, int sms, cudaStream_t stream
 
 template <int TYPE>
 void launch_rows(const DistillArgs& a, int sms, cudaStream_t stream) {
-  const uint64_t words = ((uint64_t)a.vocab * Word<TYPE>::kSize + 15) / 16 + 1;   // (a row may begin inside a word)
+  const uint64_t words = words_of_row(a.vocab, TYPE);
   if (words <= 256) return launch_rows_as<TYPE, 128, 2>(a, sms, stream);
   if (words <= 1024) return launch_rows_as<TYPE, 128, 8>(a, sms, stream);
   constexpr uint64_t most = kManyWords * kSliceWork, few = kFewWords * kSliceWork;   // words of a slice
@@ -1047,11 +1144,25 @@ void launch_rows(const DistillArgs& a, int sms, cudaStream_t stream) {
   else launch_after(distill_long_kernel<TYPE, TWO_SUMS>, grid, kLongThreads, 0, stream, a);
 }
 
+template <int TYPE, int NV>
+void launch_few(const DistillArgs& a, uint32_t table, cudaStream_t stream) {
+  const size_t smem = Lists::words(a.top, table) * sizeof(uint32_t);
+  const int mode = distill_mode(a);
+  note_launches(1);
+  if (mode == ONE_SUM) launch_after(distill_few_kernel<TYPE, NV, ONE_SUM>, (unsigned)a.n, kFewThreads, smem, stream, a, table);
+  else if (mode == SQUARES) launch_after(distill_few_kernel<TYPE, NV, SQUARES>, (unsigned)a.n, kFewThreads, smem, stream, a, table);
+  else launch_after(distill_few_kernel<TYPE, NV, TWO_SUMS>, (unsigned)a.n, kFewThreads, smem, stream, a, table);
+}
+
 template <int TYPE>
 void launch_distill_type(const DistillArgs& a, int sms, cudaStream_t stream) {
   const uint32_t table = a.top > 0 ? power_of_two(2 * a.top) : 0;
+  if (distill_in_one(a.n, a.vocab, TYPE, sms)) {
+    if (words_of_row(a.vocab, TYPE) <= 2 * kFewThreads) return launch_few<TYPE, 2>(a, table, stream);
+    return launch_few<TYPE, 8>(a, table, stream);
+  }
   const unsigned grid = (unsigned)std::min<uint64_t>((a.n + kListWarps - 1) / kListWarps, (uint64_t)sms * 16);
-  const size_t smem = kListWarps * (4 * (size_t)a.top + table) * sizeof(uint32_t);
+  const size_t smem = kListWarps * (size_t)Lists::words(a.top, table) * sizeof(uint32_t);
   static Asked asked;
   if (smem > 48 * 1024) asked.allow(distill_lists_kernel<TYPE>, kListWarps * 6 * (size_t)kMaxTop * sizeof(uint32_t));
   note_launches(3);

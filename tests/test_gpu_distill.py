@@ -146,6 +146,21 @@ def test_rows_that_begin_anywhere(gpu_lib, pm, V, dtype):
             assert (dst[mask] == 3.0).all()
 
 
+@pytest.mark.parametrize("V", [40, 3000, 32_003])
+def test_few_rows_equal_many(gpu_lib, pm, V):
+    """One launch does at most as many rows as there are SMs, three do more: losses and gradients of the same rows."""
+    n = 400
+    for dtype, T in ((torch.bfloat16, 1.0), (torch.float32, 2.0), (torch.float16, 3.0)):
+        logits = (torch.randn(n, V, device="cuda") * 2).to(dtype)
+        ids, teacher = lists((n,), V, min(V, 17))
+        labels = torch.randint(0, V, (n,), device="cuda")
+        labels[5:9], ids[7:12] = -100, -1
+        check(pm, logits, ids, teacher, T, 0.5, labels, 0.5, pad=-100)
+        for a in (0, 150, 300):
+            check(pm, logits[a:a + 100], ids[a:a + 100], teacher[a:a + 100], T, 0.5, labels[a:a + 100], 0.5, pad=-100)
+            check(pm, logits[a:a + 100], ids[a:a + 100], teacher[a:a + 100], T, in_place=True)
+
+
 def test_strides_and_types(gpu_lib, pm):
     B, T, V = 3, 10, 501
     wide = torch.randn(B, T + 1, V, device="cuda")
