@@ -2255,7 +2255,7 @@ adapm_status adapm_distill(adapm_ctx* ctx, const adapm_shape* shape, const adapm
   a.st = ctx->dstate;
   ProfScope ps(ctx, 5);
   char *tasks = nullptr, *entries = nullptr;
-  if (!distill_in_one(n, a.vocab, a.logits.type, ctx->sms)) {
+  if (!distill_in_one(a.logits, n, a.vocab, ctx->sms)) {
     CK(pool_alloc(ctx, &tasks, n * (kTaskBytes + kRowSumBytes)));
     if (a.top > 0) CK(pool_alloc(ctx, &entries, n * a.top * kEntryBytes));
     a.tasks = tasks;

@@ -78,13 +78,19 @@ struct DistillArgs {
   void *tasks, *sums, *entries;   // scratch: n, n and n * top of them
   DevState* st;
 };
-// 16-byte words of a row, which may begin inside one; and whether all rows are
-// done by one launch, which needs no scratch: at most one per SM, of up to 128 KB.
-inline uint64_t words_of_row(uint32_t vocab, int type) { return ((uint64_t)vocab * (type == ADAPM_F32 ? 4 : 2) + 15) / 16 + 1; }
-inline bool distill_in_one(uint64_t n, uint32_t vocab, int type, int sms) {
-  return n <= (uint64_t)sms && words_of_row(vocab, type) <= 8192;
-}
 constexpr size_t kTaskBytes = 16, kRowSumBytes = 12, kEntryBytes = 12;
+// Whether every row of the view begins on a multiple of `elements` elements.
+inline bool rows_on(const RowView& v, uint64_t n, uint32_t elements);
+// 16-byte words of a row, one more where rows may begin inside one; and whether
+// all rows are done by one launch, which needs no scratch: at most one per SM,
+// of up to 128 KB.
+inline uint64_t words_of_row(uint32_t vocab, const RowView& v, uint64_t n) {
+  const uint32_t size = v.type == ADAPM_F32 ? 4 : 2;
+  return ((uint64_t)vocab * size + 15) / 16 + (rows_on(v, n, 16 / size) ? 0 : 1);
+}
+inline bool distill_in_one(const RowView& logits, uint64_t n, uint32_t vocab, int sms) {
+  return n <= (uint64_t)sms && words_of_row(vocab, logits, n) <= 8192;
+}
 // The kernels of one type of logits (a translation unit each).
 void launch_distill_f32(const DistillArgs& a, int sms, cudaStream_t stream);
 void launch_distill_f16(const DistillArgs& a, int sms, cudaStream_t stream);

@@ -1128,7 +1128,8 @@ void launch_slices(const DistillArgs& a, int split, int sms, cudaStream_t stream
 
 template <int TYPE>
 void launch_rows(const DistillArgs& a, int sms, cudaStream_t stream) {
-  const uint64_t words = words_of_row(a.vocab, TYPE);
+  // (slices are cut by the gradient's words)
+  const uint64_t words = std::max(words_of_row(a.vocab, a.logits, a.n), a.grad.data ? words_of_row(a.vocab, a.grad, a.n) : 0);
   if (words <= 256) return launch_rows_as<TYPE, 128, 2>(a, sms, stream);
   if (words <= 1024) return launch_rows_as<TYPE, 128, 8>(a, sms, stream);
   constexpr uint64_t most = kManyWords * kSliceWork, few = kFewWords * kSliceWork;   // words of a slice
@@ -1157,8 +1158,8 @@ void launch_few(const DistillArgs& a, uint32_t table, cudaStream_t stream) {
 template <int TYPE>
 void launch_distill_type(const DistillArgs& a, int sms, cudaStream_t stream) {
   const uint32_t table = a.top > 0 ? power_of_two(2 * a.top) : 0;
-  if (distill_in_one(a.n, a.vocab, TYPE, sms)) {
-    if (words_of_row(a.vocab, TYPE) <= 2 * kFewThreads) return launch_few<TYPE, 2>(a, table, stream);
+  if (distill_in_one(a.logits, a.n, a.vocab, sms)) {
+    if (words_of_row(a.vocab, a.logits, a.n) <= 2 * kFewThreads) return launch_few<TYPE, 2>(a, table, stream);
     return launch_few<TYPE, 8>(a, table, stream);
   }
   const unsigned grid = (unsigned)std::min<uint64_t>((a.n + kListWarps - 1) / kListWarps, (uint64_t)sms * 16);

@@ -445,37 +445,55 @@ gemm_kernel(const __grid_constant__ GemmArgs g) {
 }
 
 // ---- operands ------------------------------------------------------------------------
-// rows x columns elements of a 16-bit type to rows that begin `pitch` apart;
-// blocks of kPackRows rows x kPackColumns columns, of up to two matrices.
-constexpr uint32_t kPackRows = 4, kPackColumns = 512;
+// rows x columns elements of a 16-bit type to rows that begin `pitch` (a
+// multiple of eight) apart, of up to two matrices.  A thread writes eight
+// neighbours; where a row's elements are neighbours too they come from the two
+// 16-byte words that hold them, which may hold others of the matrix, but
+// nothing in front of or behind it.
 struct PackJob {
   const uint16_t* from;
   uint16_t* to;
   int64_t row_stride, col_stride;
   uint64_t rows;
-  uint32_t columns, pitch, across;   // across: blocks of columns
+  uint32_t columns, pitch, eights;   // eights: of a row
   uint32_t blocks;
 };
+__device__ __forceinline__ uint4 eight_of(const PackJob& p, uint64_t r, uint32_t c) {
+  const uint16_t* const at = p.from + (int64_t)r * p.row_stride + (int64_t)c * p.col_stride;
+  if (p.col_stride == 1 && c + 8 <= p.columns) {
+    const uint32_t in = (uint32_t)reinterpret_cast<uintptr_t>(at) & 15u;
+    const char* const word = reinterpret_cast<const char*>(at) - in;
+    const char* const end = reinterpret_cast<const char*>(p.from + (int64_t)(p.rows - 1) * p.row_stride + p.columns);
+    if (in == 0) return *reinterpret_cast<const uint4*>(word);
+    if (word >= reinterpret_cast<const char*>(p.from) && word + 32 <= end) {
+      const uint4 lo = *reinterpret_cast<const uint4*>(word), hi = *reinterpret_cast<const uint4*>(word + 16);
+      uint32_t x[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+      if (in & 8u)
+#pragma unroll
+        for (int j = 0; j < 6; ++j) x[j] = x[j + 2];
+      if (in & 4u)
+#pragma unroll
+        for (int j = 0; j < 5; ++j) x[j] = x[j + 1];
+      const uint32_t bits = (in & 3u) * 8u;
+      return make_uint4(__funnelshift_r(x[0], x[1], bits), __funnelshift_r(x[1], x[2], bits), __funnelshift_r(x[2], x[3], bits),
+                        __funnelshift_r(x[3], x[4], bits));
+    }
+  }
+  uint32_t x[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+  for (uint32_t j = 0; j < 8; ++j)
+    if (c + j < p.columns) x[j / 2] |= (uint32_t)at[(int64_t)j * p.col_stride] << (16 * (j & 1));
+  return make_uint4(x[0], x[1], x[2], x[3]);
+}
 __global__ void __launch_bounds__(256)
 pack_kernel(const PackJob x, const PackJob y) {
   after_previous();
   const bool second = blockIdx.x >= x.blocks;
   const PackJob& p = second ? y : x;
   const uint32_t b = second ? blockIdx.x - x.blocks : blockIdx.x;
-  const uint64_t r0 = (uint64_t)(b / p.across) * kPackRows;
-  const uint32_t c0 = b % p.across * kPackColumns + threadIdx.x;
-  uint16_t v[kPackRows][2];
-#pragma unroll
-  for (uint32_t i = 0; i < kPackRows; ++i)
-#pragma unroll
-    for (uint32_t j = 0; j < 2; ++j)
-      if (r0 + i < p.rows && c0 + j * 256 < p.columns)
-        v[i][j] = p.from[(int64_t)(r0 + i) * p.row_stride + (int64_t)(c0 + j * 256) * p.col_stride];
-#pragma unroll
-  for (uint32_t i = 0; i < kPackRows; ++i)
-#pragma unroll
-    for (uint32_t j = 0; j < 2; ++j)
-      if (r0 + i < p.rows && c0 + j * 256 < p.columns) p.to[(r0 + i) * p.pitch + c0 + j * 256] = v[i][j];
+  const uint64_t i = (uint64_t)b * 256 + threadIdx.x, r = i / p.eights;
+  const uint32_t c = (uint32_t)(i - r * p.eights) * 8;
+  if (r < p.rows) *reinterpret_cast<uint4*>(p.to + r * p.pitch + c) = eight_of(p, r, c);
 }
 
 // A matrix of mn x k elements as an operand: how it is stored, and whether it
@@ -523,7 +541,7 @@ void pack(Operand& x, Operand& y, char* at, cudaStream_t stream) {
   int i = 0;
   for (Operand* o : {&x, &y}) {
     PackJob& j = jobs[i++];
-    j.across = 1;
+    j.eights = 1;
     if (!o->packed) continue;
     j.from = reinterpret_cast<const uint16_t*>(o->data);
     j.to = reinterpret_cast<uint16_t*>(at);
@@ -532,8 +550,8 @@ void pack(Operand& x, Operand& y, char* at, cudaStream_t stream) {
     j.rows = o->across ? o->k : o->mn;
     j.columns = (uint32_t)(o->across ? o->mn : o->k);
     j.pitch = (uint32_t)o->pitch;
-    j.across = (j.columns + kPackColumns - 1) / kPackColumns;
-    j.blocks = (uint32_t)((j.rows + kPackRows - 1) / kPackRows * j.across);
+    j.eights = (j.columns + 7) / 8;
+    j.blocks = (uint32_t)((j.rows * j.eights + 255) / 256);
     blocks += j.blocks;
     o->data = at;
     at += round256(o->bytes);
