@@ -432,8 +432,9 @@ typedef struct {
 /* out = (x - m) r weight + bias for every row, m its mean, r = 1 / sqrt(v +
  * eps), v its variance (the mean of the squared differences from m).  weight
  * and bias (NULL: ones, zeros) have types of their own.  stats (NULL: not
- * wanted) receives m and r of every row, two floats a row without gaps.
- * Computed in fp32, rounded once to out's type.  out is x's own memory (same
+ * wanted) receives m and r of every row, two floats a row without gaps,
+ * aligned to 8 bytes.  Computed in fp32, rounded once to out's type; squares
+ * beyond fp32 make v infinite and r 0.  out is x's own memory (same
  * type and strides) or does not overlap it; its rows must not overlap each
  * other (ADAPM_EINVAL where two strides make them).  eps must not be
  * negative.  An infinity or NaN makes its own row NaN, no other. */
@@ -480,8 +481,8 @@ typedef struct {
  * NULL: zeros) has a type of its own; residual (NULL: zeros), out and pre are
  * rows x outs with col_stride 1.  pre (NULL: not wanted) receives z in x's
  * type, for the backward pass.  out is of x's type or fp32, residual has out's
- * type and may be its memory.  Products are summed and all else is computed in
- * fp32, each output is rounded once.  rows, ins and outs are at most 2^31, ins
+ * type and may be its memory; out and pre overlap nothing else.  Products are
+ * summed and all else is computed in fp32, each output is rounded once.  rows, ins and outs are at most 2^31, ins
  * and outs not 0.  Operands whose rows (or columns) do not begin on 16 bytes
  * are copied to scratch memory first. */
 adapm_status adapm_linear(adapm_ctx* ctx, const adapm_layer* shape, const adapm_matrix* x,
@@ -528,7 +529,7 @@ typedef struct {
 /* The loss of every row of student logits s (dim is the vocabulary) against a
  * teacher's list and a label, and its gradient.  With p the softmax of the
  * list's logits / T (over its entries alone), q the softmax of s / T and c that
- * of s, T = temperature > 0:
+ * of s, T = temperature, a positive normal number:
  *   loss = soft T^2 sum_j p_j (ln p_j - ln q_id_j) + hard (-ln c_label)
  *   grad_v = scale weights[row] (soft T (q_v - sum of p_j with id_j = v)
  *                                + hard (c_v - [v = label]))

@@ -2203,8 +2203,8 @@ adapm_status adapm_distill(adapm_ctx* ctx, const adapm_shape* shape, const adapm
   if (st == ADAPM_OK) st = check_rows(ctx, device, logits, n, "logits");
   if (st == ADAPM_OK && grad) st = check_rows(ctx, device, grad, n, "grad");
   if (st != ADAPM_OK) return st;
-  if (!(temperature > 0.f) || !std::isfinite(temperature))
-    return fail(ctx, ADAPM_EINVAL, "the temperature is a positive number, not %g", (double)temperature);
+  if (!(temperature > 0.f) || !std::isnormal(temperature))
+    return fail(ctx, ADAPM_EINVAL, "the temperature is a positive normal number, not %g", (double)temperature);
   if (!std::isfinite(soft) || !std::isfinite(hard)) return fail(ctx, ADAPM_EINVAL, "soft or hard is not a number");
   if (grad && grad->type != logits->type) return fail(ctx, ADAPM_EINVAL, "grad has another type than the logits");
   if (teacher) {

@@ -358,6 +358,7 @@ def test_refusals(gpu_lib, pm):
         lambda: pm.distill(x, big.long(), big),
         lambda: pm.distill(x, ids, t, 0.0),
         lambda: pm.distill(x, ids, t, -1.0),
+        lambda: pm.distill(x, ids, t, 1e-39),
         lambda: pm.distill(x, ids, t, math.nan),
         lambda: pm.distill(x, ids, t, math.inf),
         lambda: pm.distill(x, ids, t, soft=math.nan),
@@ -379,3 +380,22 @@ def test_refusals(gpu_lib, pm):
     pm.wait()
     assert not flat.any()
     assert pm.distill(torch.zeros(0, 8, device="cuda"), ids[:0], t[:0]).shape == (0,)
+
+
+def test_offsets_beyond_32_bits(gpu_lib, pm):
+    """More than 2^31 logits: the rows behind that are like the others."""
+    n, V = 8700, 250_000
+    logits = torch.empty(n, V, dtype=torch.bfloat16, device="cuda")
+    for a in range(0, n, 300):
+        logits[a:a + 300].normal_(0.0, 2.0)
+    ids, teacher = lists((n,), V, 4)
+    part = [0, 1, 8600, 8698, 8699]
+    kept = logits[part].clone()
+    loss = pm.distill(logits, ids, teacher, grad=logits)
+    pm.wait()
+    l64, size, grad, gsize = wanted(kept, ids[part], teacher[part], 1.0, 1.0, None, 0.0, None, 1.0, None)
+    assert ((loss[part].double() - l64).abs() <= 300 * U * (size + 2)).all()
+    ut, tiny = TYPES[torch.bfloat16]
+    assert ((logits[part].double() - grad).abs() <= 300 * U * gsize + grad.abs() * ut + tiny).all()
+    # what the softmax's parts sum to: 1 - 1, but for their roundings
+    assert (logits[8000:].double().sum(1).abs() <= 2.0 ** -8 * 2).all()

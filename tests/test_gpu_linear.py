@@ -23,8 +23,10 @@ SIZES = [(1, 1, 1), (1, 64, 128), (1, 8, 5003), (1, 4096, 300), (2, 7, 9), (5, 3
          (33, 1000, 127), (64, 512, 2048), (65, 64, 64), (100, 63, 65), (127, 129, 257), (128, 128, 256), (129, 72, 40),
          (300, 1024, 520), (777, 256, 1000), (1021, 333, 503), (40, 9000, 24), (130, 20_000, 70), (3000, 96, 3),
          (2500, 17, 1100)]
-# enough tiles of 128 x 256 for every SM: pairs of blocks in the product, in dx, in dweight; sizes that nothing divides
-LARGE = [(2600, 200, 4100), (2600, 4100, 200), (100, 2600, 4100), (2601, 1001, 4099), (4096, 512, 4096)]
+# enough tiles of 128 x 256 for every SM: pairs of blocks in the product, in dx, in dweight; sizes that nothing divides;
+# long sums whose last tiles are halved
+LARGE = [(2600, 200, 4100), (2600, 4100, 200), (100, 2600, 4100), (2601, 1001, 4099), (4096, 512, 4096),
+         (4090, 4100, 4095), (2100, 4096, 4096)]
 
 
 @pytest.fixture(scope="module")
@@ -300,7 +302,7 @@ def test_recorded_in_a_graph_and_the_same_bits(gpu_lib):
     with torch.cuda.stream(s):
         pm = gpu_lib.ParameterManager(4, 4, 1)
         sets = []
-        for rows, ins, outs in ((3, 2048, 300), (500, 333, 260)):
+        for rows, ins, outs in ((3, 2048, 300), (500, 333, 260), (4096, 4096, 4096)):
             x, w = torch.randn(rows, ins, device="cuda").half(), (torch.randn(ins, outs, device="cuda") / 50).half()
             pre, out, grad = (torch.randn(rows, outs, device="cuda").half() for _ in range(3))
             into = gpu_lib.LinearGrads(torch.empty_like(x), torch.empty_like(w), torch.empty(outs, device="cuda"))
@@ -366,3 +368,18 @@ def test_refusals(gpu_lib, pm):
     pm.wait()
     assert not flat.any() and not x.any() and not w.any() and not y.any()
     assert not pm.linear(x, w).any()
+
+
+def test_offsets_beyond_32_bits(gpu_lib, pm):
+    """More than 2^31 outputs: the rows behind that are like the others; and as inputs of the gradient."""
+    rows, ins, outs = 66_000, 40, 32_768
+    x, w = small((rows, ins), torch.bfloat16), small((ins, outs), torch.bfloat16)
+    out = pm.linear(x, w)
+    pm.wait()
+    part = [0, 65_535, 65_536, rows - 1]
+    want = x[part].double() @ w.double()
+    assert ((out[part].double() - want).abs() <= want.abs() * 2.0 ** -8).all()   # (whole sums, rounded once)
+    grad = out.clamp_(-1, 1)
+    got = pm.linear_grad(x, w, grad, out=gpu_lib.LinearGrads(torch.empty(rows, ins, device="cuda"), None, None))
+    pm.wait()
+    assert torch.equal(got.x[part].double(), grad[part].double() @ w.double().t())

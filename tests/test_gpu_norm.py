@@ -373,3 +373,48 @@ def test_refusals(gpu_lib, pm):
     assert not flat.any() and not x.any()
     # what the call refuses leaves the manager as it was
     assert np.isfinite(pm.layer_norm(x).cpu().numpy()).all()
+
+
+def test_offsets_beyond_32_bits(gpu_lib, pm):
+    """More than 2^31 elements: the rows behind that are like the others."""
+    n, dim = 530_000, 4096
+    x = torch.empty(n, dim, dtype=torch.bfloat16, device="cuda")
+    for a in range(0, n, 53_000):
+        x[a:a + 53_000].normal_(0.5, 1.5)
+    w, b = params(dim, torch.float32)
+    stats = torch.empty(n, 2, device="cuda")
+    out = pm.layer_norm(x, w, b, stats=stats)
+    part = [0, 524_287, 524_288, 524_289, n - 1]
+    pm.wait()
+    check_forward(x[part], w, b, 1e-5, out[part], stats[part])
+    got = pm.layer_norm_grad(x, out, stats, w)
+    pm.wait()
+    check_grad(x[part], out[part], stats[part], w, gpu_lib.NormGrads(got.x[part], None, None))
+    want = out[:, 7].double() * (x[:, 7].double() - stats[:, 0].double()) * stats[:, 1].double()
+    assert abs(float(got.weight[7].double() - want.sum())) <= (n / 152 + 300) * U * float(want.abs().sum())
+
+
+def test_two_managers_at_once(gpu_lib):
+    """Calls on two streams, side by side, with inputs that have to be copied first."""
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    pms = []
+    for s in streams:
+        with torch.cuda.stream(s):
+            pms.append(gpu_lib.ParameterManager(4, 4, 1))
+    w, b = params(700, torch.float32)
+    xs = [torch.randn(700, 900, device="cuda").t() for _ in range(2)]        # (elements of a row lie apart)
+    heavy = [torch.randn(3000, 4096, device="cuda").half() for _ in range(2)]
+    weight = torch.randn(4096, 3000, device="cuda").half()
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(3):
+        got = [(pm.layer_norm(x, w, b), pm.linear(h, weight, dtype=torch.float32)) for pm, x, h in zip(pms, xs, heavy)]
+    for pm in pms:
+        pm.wait()
+    for (out, product), x, h in zip(got, xs, heavy):
+        check_forward(x, w, b, 1e-5, out)
+        want = h.double() @ weight.double()
+        size = h.double().abs() @ weight.double().abs()
+        assert ((product.double() - want).abs() <= (4096 / 8 + 16) * 2.0 ** -23 * size).all()
+    for pm in pms:
+        pm.close()
