@@ -304,8 +304,10 @@ distill_lists_kernel(const __grid_constant__ DistillArgs a, uint32_t table) {
 struct RowScale {
   float t, one;
 };
-__device__ __forceinline__ RowScale row_scale(const DistillArgs& a, uint64_t row, const RowTask& task, const RowSums& sums, bool two) {
-  const float f = a.weights != nullptr ? a.scale * a.weights[row] : a.scale;
+__device__ __forceinline__ float row_weight(const DistillArgs& a, uint64_t row) {
+  return a.weights != nullptr ? a.scale * a.weights[row] : a.scale;
+}
+__device__ __forceinline__ RowScale row_scale(const DistillArgs& a, float f, const RowTask& task, const RowSums& sums, bool two) {
   const float soft = task.some ? a.soft * a.temperature * f : 0.f, hard = task.label >= 0 ? a.hard * f : 0.f;
   if (two) return RowScale{soft / sums.t, hard / sums.one};
   return RowScale{(soft + hard) / sums.t, 0.f};
@@ -423,8 +425,8 @@ struct RowFactors {
   bool folded;   // st is part of the exponent
 };
 template <int TYPE, int MODE>
-__device__ __forceinline__ RowFactors row_factors(const DistillArgs& a, uint64_t row, const RowTask& task, const RowSums& all, float per) {
-  const RowScale scale = row_scale(a, row, task, all, MODE != ONE_SUM);
+__device__ __forceinline__ RowFactors row_factors(const DistillArgs& a, float weight, const RowTask& task, const RowSums& all, float per) {
+  const RowScale scale = row_scale(a, weight, task, all, MODE != ONE_SUM);
   RowFactors f;
   f.max = all.max;
   f.huge = is_huge(all.max, per);
@@ -492,6 +494,23 @@ __device__ __forceinline__ RowSums merge_sums(const RowSums& s, int count, float
   return all;
 }
 
+// The same by every lane for itself, for few parts that part(i) reads from
+// shared memory: no lane waits for another.
+template <int MODE, class F>
+__device__ __forceinline__ RowSums merge_few(int count, float per, F&& part) {
+  RowSums all{-INFINITY, 0.f, 0.f};
+#pragma unroll 8
+  for (int i = 0; i < count; ++i) all.max = fmaxf(all.max, part(i).max);
+#pragma unroll 8
+  for (int i = 0; i < count; ++i) {
+    const RowSums s = part(i);
+    const float down = s.max - all.max;
+    all.t = fmaf(s.t, exp2_of(down * per), all.t);
+    if (MODE != ONE_SUM) all.one = fmaf(s.one, exp2_of(down * kLog2E), all.one);
+  }
+  return all;
+}
+
 // ---- rows in registers ------------------------------------------------------------
 // Blocks per SM that the registers allow: 32 of a thread hold eight words.
 constexpr int resident_blocks(int threads, int words) { return (words == 8 ? 1024 : 1536) / threads; }
@@ -551,7 +570,7 @@ distill_rows_kernel(const __grid_constant__ DistillArgs a) {
     }
     __syncthreads();
     if (live) {
-      all = merge_sums<MODE>(lane < WARPS ? warps[turn][lane] : RowSums{-INFINITY, 0.f, 0.f}, WARPS, per);
+      all = merge_few<MODE>(WARPS, per, [&](int i) { return warps[turn][i]; });
       if (threadIdx.x == 0) static_cast<RowSums*>(a.sums)[row] = all;
     }
     if (a.grad.data == nullptr) continue;
@@ -560,7 +579,7 @@ distill_rows_kernel(const __grid_constant__ DistillArgs a) {
       for (uint32_t w = threadIdx.x; w < g.words; w += THREADS) store_word<TYPE>(g, a.vocab, w, make_uint4(0, 0, 0, 0));
       continue;
     }
-    const RowFactors f = row_factors<TYPE, MODE>(a, row, task, all, per);
+    const RowFactors f = row_factors<TYPE, MODE>(a, row_weight(a, row), task, all, per);
     with_gradient<TYPE, MODE>(f, per, [&](const auto& gradient) {
       if (g.head == b.head) {
         if (f.huge) {
@@ -704,8 +723,9 @@ distill_slices_kernel(const __grid_constant__ DistillArgs a, int split) {
       if (more) copy(row + rows, next);
       if (task.some || task.label >= 0) {
         const uint32_t parity = lives & 1u, q = lives & 1u;
-        if (!(ok = barrier_wait(summed, parity, kNap))) break;
-        RowSums all = merge_sums<MODE>(lane < kSliceWarps ? sh.warps[lane] : RowSums{-INFINITY, 0.f, 0.f}, kSliceWarps, per);
+        const float weight = row_weight(a, row);
+        if (!(ok = barrier_wait(summed, parity))) break;
+        RowSums all = merge_few<MODE>(kSliceWarps, per, [&](int i) { return sh.warps[i]; });
         if (split > 1) {
           if (all.max == -INFINITY) all.t = all.one = 0.f;   // (a part of -inf alone has no NaN for the others)
           const uint32_t bar = shared_at(&sh.arrived[q]);
@@ -713,14 +733,16 @@ distill_slices_kernel(const __grid_constant__ DistillArgs a, int split) {
             store_and_count(shared_of(shared_at(&sh.blocks[q][rank]), lane), make_float4(all.max, all.t, all.one, 0.f), shared_of(bar, lane));
           if (!(ok = barrier_wait(bar, (lives >> 1) & 1u))) break;
           if (lane == 0) barrier_expect(bar, split * 16);   // (for two live rows on)
-          const float4 v = lane < split ? sh.blocks[q][lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
-          all = merge_sums<MODE>(RowSums{v.x, v.y, v.z}, split, per);
+          all = merge_few<MODE>(split, per, [&](int i) {
+            const float4 v = sh.blocks[q][i];
+            return RowSums{v.x, v.y, v.z};
+          });
         }
         ++lives;
         if (lane == 0) {
-          if (rank == 0) static_cast<RowSums*>(a.sums)[row] = all;
-          sh.factors = row_factors<TYPE, MODE>(a, row, task, all, per);
+          sh.factors = row_factors<TYPE, MODE>(a, weight, task, all, per);
           barrier_arrive(ready);
+          if (rank == 0) static_cast<RowSums*>(a.sums)[row] = all;
         }
         __syncwarp();
       }
@@ -913,7 +935,7 @@ distill_long_kernel(const __grid_constant__ DistillArgs a) {
       for (uint32_t w = g0 + threadIdx.x; w < g1; w += kLongThreads) store_word<TYPE>(g, a.vocab, w, make_uint4(0, 0, 0, 0));
       continue;
     }
-    const RowFactors f = row_factors<TYPE, MODE>(a, row, task, all, per);
+    const RowFactors f = row_factors<TYPE, MODE>(a, row_weight(a, row), task, all, per);
     const uint32_t shift = (b.head - g.head) & (E - 1), back = b.head < g.head ? 1 : 0;
     with_gradient<TYPE, MODE>(f, per, [&](const auto& gradient) {
 #pragma unroll 4
@@ -938,8 +960,8 @@ __device__ __forceinline__ void write_marks(const DistillArgs& a, uint64_t row, 
   }
   const float per = a.top > 0 ? kLog2E / a.temperature : kLog2E;
   const float inv_t = 1.f / a.temperature;
-  const RowScale scale = row_scale(a, row, task, all, two);
-  const float f = a.weights != nullptr ? a.scale * a.weights[row] : a.scale;
+  const float f = row_weight(a, row);
+  const RowScale scale = row_scale(a, f, task, all, two);
   const float log_st = logf(all.t), log_s1 = two ? logf(all.one) : log_st;
   const bool write = a.grad.data != nullptr;
   char* const grad = write ? a.grad.data + row_offset(a.grad, (uint32_t)row) * Word<TYPE>::kSize : nullptr;
@@ -1035,7 +1057,7 @@ distill_few_kernel(const __grid_constant__ DistillArgs a, uint32_t table) {
     if (!live) {
       for (uint32_t w = threadIdx.x; w < g.words; w += kFewThreads) store_word<TYPE>(g, a.vocab, w, make_uint4(0, 0, 0, 0));
     } else {
-      const RowFactors f = row_factors<TYPE, MODE>(a, row, task, all, per);
+      const RowFactors f = row_factors<TYPE, MODE>(a, row_weight(a, row), task, all, per);
       with_gradient<TYPE, MODE>(f, per, [&](const auto& gradient) {
         if (g.head == b.head) {
           if (f.huge) {
