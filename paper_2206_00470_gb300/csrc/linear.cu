@@ -126,14 +126,31 @@ __device__ __forceinline__ Tile tile_of(const GemmArgs& g, uint32_t tile) {
 template <int TYPE, bool OUT32, int N>
 struct Finish {
   static constexpr int kOut = OUT32 ? ADAPM_F32 : TYPE;
+  // (what is read or written once stays out of the way of the operands in L2)
   static __device__ __forceinline__ void load_residual(const Epilogue& e, uint64_t r, uint32_t c, float (&add)[N]) {
-    load_n<kOut, N>(e.residual.data + (r * e.residual.row_stride + c) * type_size(kOut), add);
+    const char* p = e.residual.data + (r * e.residual.row_stride + c) * type_size(kOut);
+    if constexpr (kOut == ADAPM_F32 && N == 4) {
+      const float4 v = __ldcs(reinterpret_cast<const float4*>(p));
+      add[0] = v.x; add[1] = v.y; add[2] = v.z; add[3] = v.w;
+    } else if constexpr (N == 4) {
+      const uint2 v = __ldcs(reinterpret_cast<const uint2*>(p));
+      const float2 x = unpack2<kOut>(v.x), y = unpack2<kOut>(v.y);
+      add[0] = x.x; add[1] = x.y; add[2] = y.x; add[3] = y.y;
+    } else {
+      load_n<kOut, N>(p, add);
+    }
+  }
+  template <int T>
+  static __device__ __forceinline__ void store_once(char* p, const float* z) {
+    if constexpr (T == ADAPM_F32 && N == 4) __stcs(reinterpret_cast<float4*>(p), make_float4(z[0], z[1], z[2], z[3]));
+    else if constexpr (N == 4) __stcs(reinterpret_cast<uint2*>(p), make_uint2(pack2<T>(z[0], z[1]), pack2<T>(z[2], z[3])));
+    else store_n<T, N>(p, z);
   }
   static __device__ __forceinline__ void store_pre(const Epilogue& e, uint64_t r, uint32_t c, const float* z) {
-    store_n<TYPE, N>(e.pre.data + (r * e.pre.row_stride + c) * type_size(TYPE), z);
+    store_once<TYPE>(e.pre.data + (r * e.pre.row_stride + c) * type_size(TYPE), z);
   }
   static __device__ __forceinline__ void store_out(const Epilogue& e, uint64_t r, uint32_t c, const float* z) {
-    store_n<kOut, N>(e.out.data + (r * e.out.row_stride + c) * type_size(kOut), z);
+    store_once<kOut>(e.out.data + (r * e.out.row_stride + c) * type_size(kOut), z);
   }
 };
 // ROWS places (r_i, c) of one column block: z becomes what is stored; bias: of
