@@ -122,56 +122,58 @@ __device__ __forceinline__ Tile tile_of(const GemmArgs& g, uint32_t tile) {
 }
 
 // ---- epilogue ------------------------------------------------------------------------
-// N elements of a row from (r, c) on, that follow each other in memory on a multiple of N.
-template <int TYPE, bool OUT32, int N>
-struct Finish {
-  static constexpr int kOut = OUT32 ? ADAPM_F32 : TYPE;
-  // (what is read or written once stays out of the way of the operands in L2)
-  static __device__ __forceinline__ void load_residual(const Epilogue& e, uint64_t r, uint32_t c, float (&add)[N]) {
-    const char* p = e.residual.data + (r * e.residual.row_stride + c) * type_size(kOut);
-    if constexpr (kOut == ADAPM_F32 && N == 4) {
-      const float4 v = __ldcs(reinterpret_cast<const float4*>(p));
-      add[0] = v.x; add[1] = v.y; add[2] = v.z; add[3] = v.w;
-    } else if constexpr (N == 4) {
-      const uint2 v = __ldcs(reinterpret_cast<const uint2*>(p));
-      const float2 x = unpack2<kOut>(v.x), y = unpack2<kOut>(v.y);
-      add[0] = x.x; add[1] = x.y; add[2] = y.x; add[3] = y.y;
-    } else {
-      load_n<kOut, N>(p, add);
-    }
+// N neighbours of a row, on a multiple of N where N > 1.  (What is read or
+// written once stays out of the way of the operands in L2.)
+template <int TYPE, int N>
+__device__ __forceinline__ void load_once(const char* p, float* x) {
+  if constexpr (N == 4 && TYPE == ADAPM_F32) {
+    const float4 v = __ldcs(reinterpret_cast<const float4*>(p));
+    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+  } else if constexpr (N == 4) {
+    const uint2 v = __ldcs(reinterpret_cast<const uint2*>(p));
+    const float2 low = unpack2<TYPE>(v.x), high = unpack2<TYPE>(v.y);
+    x[0] = low.x; x[1] = low.y; x[2] = high.x; x[3] = high.y;
+  } else {
+    load_n<TYPE, N>(p, x);
   }
-  template <int T>
-  static __device__ __forceinline__ void store_once(char* p, const float* z) {
-    if constexpr (T == ADAPM_F32 && N == 4) __stcs(reinterpret_cast<float4*>(p), make_float4(z[0], z[1], z[2], z[3]));
-    else if constexpr (N == 4) __stcs(reinterpret_cast<uint2*>(p), make_uint2(pack2<T>(z[0], z[1]), pack2<T>(z[2], z[3])));
-    else store_n<T, N>(p, z);
-  }
-  static __device__ __forceinline__ void store_pre(const Epilogue& e, uint64_t r, uint32_t c, const float* z) {
-    store_once<TYPE>(e.pre.data + (r * e.pre.row_stride + c) * type_size(TYPE), z);
-  }
-  static __device__ __forceinline__ void store_out(const Epilogue& e, uint64_t r, uint32_t c, const float* z) {
-    store_once<kOut>(e.out.data + (r * e.out.row_stride + c) * type_size(kOut), z);
-  }
+}
+template <int TYPE, int N>
+__device__ __forceinline__ void store_once(char* p, const float* x) {
+  if constexpr (N == 4 && TYPE == ADAPM_F32) __stcs(reinterpret_cast<float4*>(p), make_float4(x[0], x[1], x[2], x[3]));
+  else if constexpr (N == 4) __stcs(reinterpret_cast<uint2*>(p), make_uint2(pack2<TYPE>(x[0], x[1]), pack2<TYPE>(x[2], x[3])));
+  else store_n<TYPE, N>(p, x);
+}
+// The places (r + i * step, c), i < ROWS, of a matrix.
+template <int TYPE>
+struct Places {
+  char* at;
+  int64_t step;
+  __device__ __forceinline__ Places(const MatrixView& v, uint64_t r, uint32_t c, uint32_t rows)
+      : at(v.data + ((int64_t)r * v.row_stride + c) * (TYPE == ADAPM_F32 ? 4 : 2)),
+        step((int64_t)rows * v.row_stride * (TYPE == ADAPM_F32 ? 4 : 2)) {}
+  __device__ __forceinline__ char* operator[](int i) const { return at + i * step; }
 };
-// ROWS places (r_i, c) of one column block: z becomes what is stored; bias: of
-// the N columns.  has: which of the places exist.
+// ROWS such places of N columns: z becomes what is stored; bias: of the
+// columns.  Those from `count` on do not exist.
 template <int TYPE, bool OUT32, int N, int ROWS>
-__device__ __forceinline__ void finish(const Epilogue& e, const uint64_t (&r)[ROWS], uint32_t c, const bool (&has)[ROWS],
+__device__ __forceinline__ void finish(const Epilogue& e, uint64_t r, uint32_t step, uint32_t c, uint32_t count,
                                        const float (&bias)[N], float (&z)[ROWS * N]) {
-  using F = Finish<TYPE, OUT32, N>;
+  constexpr int kOut = OUT32 ? ADAPM_F32 : TYPE;
   float add[ROWS][N];
   const bool more = e.residual.data != nullptr;
   if (more) {
+    const Places<kOut> from(e.residual, r, c, step);
 #pragma unroll
     for (int i = 0; i < ROWS; ++i)
-      if (has[i]) F::load_residual(e, r[i], c, add[i]);
+      if (i < (int)count) load_once<kOut, N>(from[i], add[i]);
   }
 #pragma unroll
   for (int j = 0; j < ROWS * N; ++j) z[j] += bias[j % N];
   if (e.pre.data != nullptr) {
+    const Places<TYPE> to(e.pre, r, c, step);
 #pragma unroll
     for (int i = 0; i < ROWS; ++i)
-      if (has[i]) F::store_pre(e, r[i], c, z + i * N);
+      if (i < (int)count) store_once<TYPE, N>(to[i], z + i * N);
   }
   activate(z, e.activation);
   if (more) {
@@ -180,55 +182,44 @@ __device__ __forceinline__ void finish(const Epilogue& e, const uint64_t (&r)[RO
 #pragma unroll
       for (int j = 0; j < N; ++j) z[i * N + j] += add[i][j];
   }
+  const Places<kOut> to(e.out, r, c, step);
 #pragma unroll
   for (int i = 0; i < ROWS; ++i)
-    if (has[i]) F::store_out(e, r[i], c, z + i * N);
+    if (i < (int)count) store_once<kOut, N>(to[i], z + i * N);
 }
 
 // 32 x 32 elements that a warp has staged, rows apart by 36: rows [m0, m0 + 32),
 // columns [n0, n0 + 32) of m x n.
 template <int TYPE, bool OUT32>
 __device__ __forceinline__ void finish_tile(const GemmArgs& g, const float* tile, uint32_t m0, uint32_t n0) {
-  const int lane = threadIdx.x & 31;
+  const uint32_t lane = threadIdx.x & 31u, rows = g.m - m0;
   if (g.aligned && n0 + 32 <= g.n) {
     // a lane holds four neighbours of each fourth row
-    const uint32_t c = n0 + (lane & 7) * 4;
+    const uint32_t c = n0 + (lane & 7u) * 4, mine = lane >> 3;
     float bias[4] = {0.f, 0.f, 0.f, 0.f};
     if (g.e.bias.data)
 #pragma unroll
       for (int j = 0; j < 4; ++j) bias[j] = load_as(g.e.bias.data, g.e.bias.type, c + j);
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
+    for (uint32_t r0 = mine; r0 < 32; r0 += 16) {
       float z[16];
-      uint64_t r[4];
-      bool has[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t row = half * 16 + i * 4 + (lane >> 3);
-        const float4 q = *reinterpret_cast<const float4*>(tile + row * 36 + (lane & 7) * 4);
+      for (uint32_t i = 0; i < 4; ++i) {
+        const float4 q = *reinterpret_cast<const float4*>(tile + (r0 + i * 4) * 36 + (lane & 7u) * 4);
         z[4 * i] = q.x; z[4 * i + 1] = q.y; z[4 * i + 2] = q.z; z[4 * i + 3] = q.w;
-        r[i] = m0 + row;
-        has[i] = m0 + row < g.m;
       }
-      finish<TYPE, OUT32, 4, 4>(g.e, r, c, has, bias, z);
+      finish<TYPE, OUT32, 4, 4>(g.e, (uint64_t)m0 + r0, 4, c, r0 < rows ? (rows - r0 + 3) / 4 : 0, bias, z);
     }
-  } else {
+  } else if (n0 + lane < g.n) {
     // a lane holds a column: whatever the alignment, a row's stores are neighbours
-    const uint32_t c = n0 + lane;
     float bias[1] = {0.f};
-    if (g.e.bias.data && c < g.n) bias[0] = load_as(g.e.bias.data, g.e.bias.type, c);
+    if (g.e.bias.data) bias[0] = load_as(g.e.bias.data, g.e.bias.type, n0 + lane);
 #pragma unroll 1
-    for (int r0 = 0; r0 < 32; r0 += 8) {
-      float z[8];
-      uint64_t r[8];
-      bool has[8];
+    for (uint32_t r0 = 0; r0 < 32; r0 += 16) {
+      float z[16];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        z[i] = tile[(r0 + i) * 36 + lane];
-        r[i] = m0 + r0 + i;
-        has[i] = c < g.n && m0 + r0 + i < g.m;
-      }
-      finish<TYPE, OUT32, 1, 8>(g.e, r, c, has, bias, z);
+      for (uint32_t i = 0; i < 16; ++i) z[i] = tile[(r0 + i) * 36 + lane];
+      finish<TYPE, OUT32, 1, 16>(g.e, (uint64_t)m0 + r0, 1, n0 + lane, r0 < rows ? rows - r0 : 0, bias, z);
     }
   }
 }
@@ -393,7 +384,8 @@ gemm_kernel(const __grid_constant__ GemmArgs g) {
           for (int j = 0; j < 32; j += 4)
             *reinterpret_cast<float4*>(tile + lane * 36 + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
           __syncwarp();
-          finish_tile<TYPE, OUT32>(g, tile, t.m0 + rank * kTileM + quarter * 32, t.n0 + c0);
+          const uint32_t m0 = t.m0 + rank * kTileM + quarter * 32;
+          if (m0 < g.m) finish_tile<TYPE, OUT32>(g, tile, m0, t.n0 + c0);
         }
       }
       tmem_fence_before();
@@ -437,17 +429,13 @@ gemm_kernel(const __grid_constant__ GemmArgs g) {
         for (int i = 0; i < 4; ++i)
           if (c + i < width) bias[i] = load_as(g.e.bias.data, g.e.bias.type, c + i);
       if (g.aligned && c + 4 <= width) {
-        const uint64_t rows[1] = {r};
-        const bool has[1] = {true};
-        finish<TYPE, OUT32, 4, 1>(g.e, rows, c, has, bias, z);
+        finish<TYPE, OUT32, 4, 1>(g.e, r, 0, c, 1, bias, z);
       } else {
 #pragma unroll 1
         for (int i = 0; i < 4 && c + i < width; ++i) {
-          const uint64_t rows[1] = {r};
-          const bool has[1] = {true};
           const float b1[1] = {i == 0 ? bias[0] : (i == 1 ? bias[1] : (i == 2 ? bias[2] : bias[3]))};
           float z1[1] = {i == 0 ? z[0] : (i == 1 ? z[1] : (i == 2 ? z[2] : z[3]))};
-          finish<TYPE, OUT32, 1, 1>(g.e, rows, c + i, has, b1, z1);
+          finish<TYPE, OUT32, 1, 1>(g.e, r, 0, c + i, 1, b1, z1);
         }
       }
     }
