@@ -21,16 +21,23 @@ struct Epilogue {
 // D[m][n] = sum over k of A[m][k] B[n][k], in tiles of 128 x bn, k in blocks of
 // 64 (128 bytes, the width of a swizzled row of shared memory).
 constexpr uint32_t kTileM = 128, kBlockK = 64;
-struct GemmArgs {
+struct GemmProduct {
   CUtensorMap a, b;
   bool a_across, b_across;   // stored with m (n) contiguous instead of k
-  bool turned;               // D is the product's transpose: m counts its columns
-  uint32_t m, n;
-  uint32_t bn, stages;
-  uint32_t tiles_m, tiles_n;
-  uint32_t k_blocks, splits, per_split;   // blocks of k: all, parts they are summed in, of one part
   bool aligned;              // rows of what is written and of the residual begin on four elements
+  uint32_t m, n, k_blocks;
+  uint32_t tiles_m, tiles_n;
   Epilogue e;
+};
+// One product, or two whose tiles the same blocks take, the second one's after
+// the first one's.  In the first one's last round `late` workers have a tile;
+// the others begin with `head` tiles of the second that take as long.
+struct GemmArgs {
+  GemmProduct p[2];          // (one: the second has no tiles)
+  uint32_t late, head;
+  bool turned;               // D is the product's transpose: m counts its columns
+  uint32_t bn, stages;
+  uint32_t splits, per_split;   // parts that one product's k is summed in, and blocks of a part
   DevState* st;
 };
 

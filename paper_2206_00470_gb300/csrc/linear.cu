@@ -111,15 +111,44 @@ struct Tile {
   uint32_t m0, n0;
 };
 template <bool PAIR>
-__device__ __forceinline__ Tile tile_of(const GemmArgs& g, uint32_t tile) {
+__device__ __forceinline__ Tile tile_of(const GemmProduct& p, uint32_t bn, uint32_t tile) {
   Tile t;
   // groups of kGroupM tiles of m, n by n inside
-  const uint32_t in_group = kGroupM * g.tiles_n, group = tile / in_group, at = tile - group * in_group;
-  const uint32_t height = min(kGroupM, g.tiles_m - group * kGroupM);
+  const uint32_t in_group = kGroupM * p.tiles_n, group = tile / in_group, at = tile - group * in_group;
+  const uint32_t height = min(kGroupM, p.tiles_m - group * kGroupM);
   t.m0 = (group * kGroupM + at % height) * (PAIR ? 2 * kTileM : kTileM);
-  t.n0 = at / height * g.bn;
+  t.n0 = at / height * bn;
   return t;
 }
+// The tiles of a worker (a block, or a pair or cluster of them), one after the
+// other; TWO: of both products.
+template <bool TWO>
+struct Items {
+  uint32_t worker, workers;
+  uint32_t which = 0, tile, head = 0;   // of which product, its number, how many before the common rounds
+  bool any;
+  __device__ __forceinline__ Items(const GemmArgs& g, uint32_t w, uint32_t all) : worker(w), workers(all), tile(w) { check(g); }
+  __device__ __forceinline__ void check(const GemmArgs& g) {
+    const GemmProduct& p = g.p[TWO ? which : 0];
+    any = tile < p.tiles_m * p.tiles_n;
+    if (!TWO || any || which == 1) return;
+    which = 1;
+    if (worker >= g.late && ahead(g) != 0 && g.head != 0) {
+      head = g.head;
+      tile = worker - g.late;
+    } else {
+      tile = common(g);
+    }
+    any = tile < g.p[1].tiles_m * g.p[1].tiles_n;
+  }
+  __device__ __forceinline__ uint32_t ahead(const GemmArgs& g) const { return g.late != 0 ? workers - g.late : 0; }
+  __device__ __forceinline__ uint32_t common(const GemmArgs& g) const { return g.head * ahead(g) + (workers - 1 - worker); }
+  __device__ __forceinline__ void next(const GemmArgs& g) {
+    if (!TWO || head == 0) tile += workers;
+    else tile = --head != 0 ? tile + ahead(g) : common(g);
+    check(g);
+  }
+};
 
 // ---- epilogue ------------------------------------------------------------------------
 // N neighbours of a row, on a multiple of N where N > 1.  (What is read or
@@ -191,15 +220,15 @@ __device__ __forceinline__ void finish(const Epilogue& e, uint64_t r, uint32_t s
 // 32 x 32 elements that a warp has staged, rows apart by 36: rows [m0, m0 + 32),
 // columns [n0, n0 + 32) of m x n.
 template <int TYPE, bool OUT32>
-__device__ __forceinline__ void finish_tile(const GemmArgs& g, const float* tile, uint32_t m0, uint32_t n0) {
-  const uint32_t lane = threadIdx.x & 31u, rows = g.m - m0;
-  if (g.aligned && n0 + 32 <= g.n) {
+__device__ __forceinline__ void finish_tile(const Epilogue& e, bool aligned, const float* tile, uint32_t m, uint32_t n, uint32_t m0, uint32_t n0) {
+  const uint32_t lane = threadIdx.x & 31u, rows = m - m0;
+  if (aligned && n0 + 32 <= n) {
     // a lane holds four neighbours of each fourth row
     const uint32_t c = n0 + (lane & 7u) * 4, mine = lane >> 3;
     float bias[4] = {0.f, 0.f, 0.f, 0.f};
-    if (g.e.bias.data)
+    if (e.bias.data)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) bias[j] = load_as(g.e.bias.data, g.e.bias.type, c + j);
+      for (int j = 0; j < 4; ++j) bias[j] = load_as(e.bias.data, e.bias.type, c + j);
 #pragma unroll
     for (uint32_t r0 = mine; r0 < 32; r0 += 16) {
       float z[16];
@@ -208,18 +237,18 @@ __device__ __forceinline__ void finish_tile(const GemmArgs& g, const float* tile
         const float4 q = *reinterpret_cast<const float4*>(tile + (r0 + i * 4) * 36 + (lane & 7u) * 4);
         z[4 * i] = q.x; z[4 * i + 1] = q.y; z[4 * i + 2] = q.z; z[4 * i + 3] = q.w;
       }
-      finish<TYPE, OUT32, 4, 4>(g.e, (uint64_t)m0 + r0, 4, c, r0 < rows ? (rows - r0 + 3) / 4 : 0, bias, z);
+      finish<TYPE, OUT32, 4, 4>(e, (uint64_t)m0 + r0, 4, c, r0 < rows ? (rows - r0 + 3) / 4 : 0, bias, z);
     }
-  } else if (n0 + lane < g.n) {
+  } else if (n0 + lane < n) {
     // a lane holds a column: whatever the alignment, a row's stores are neighbours
     float bias[1] = {0.f};
-    if (g.e.bias.data) bias[0] = load_as(g.e.bias.data, g.e.bias.type, n0 + lane);
+    if (e.bias.data) bias[0] = load_as(e.bias.data, e.bias.type, n0 + lane);
 #pragma unroll 1
     for (uint32_t r0 = 0; r0 < 32; r0 += 16) {
       float z[16];
 #pragma unroll
       for (uint32_t i = 0; i < 16; ++i) z[i] = tile[(r0 + i) * 36 + lane];
-      finish<TYPE, OUT32, 1, 16>(g.e, (uint64_t)m0 + r0, 1, n0 + lane, r0 < rows ? rows - r0 : 0, bias, z);
+      finish<TYPE, OUT32, 1, 16>(e, (uint64_t)m0 + r0, 1, n0 + lane, r0 < rows ? rows - r0 : 0, bias, z);
     }
   }
 }
@@ -230,7 +259,8 @@ __device__ __forceinline__ void finish_tile(const GemmArgs& g, const float* tile
 // holds, and writes to its shared memory, half of b's tile: with tiles of 128 x
 // 256 copies and products move 96 KB through it per block of k, 188 bytes a clock at
 // full rate, with pairs 64 KB.
-template <bool BF16, bool OUT32, bool PAIR>
+// TWO: of two products, both without more of an epilogue than the output, each of a type of its own.
+template <bool BF16, bool OUT32, bool PAIR, bool TWO>
 __global__ void __launch_bounds__(kGemmThreads, 1)
 gemm_kernel(const __grid_constant__ GemmArgs g) {
   constexpr int TYPE = BF16 ? ADAPM_BF16 : ADAPM_F16;
@@ -268,18 +298,18 @@ gemm_kernel(const __grid_constant__ GemmArgs g) {
   after_previous();
   const uint32_t tmem = tmem_at;
   // with parts of k, each block of a cluster sums one part of one tile
-  const uint32_t items = g.tiles_m * g.tiles_n, part = g.splits > 1 ? blockIdx.x % g.splits : 0;
-  const uint32_t first = PAIR ? blockIdx.x / 2 : (g.splits > 1 ? blockIdx.x / g.splits : blockIdx.x);
-  const uint32_t step = PAIR ? gridDim.x / 2 : (g.splits > 1 ? items : gridDim.x);
-  const uint32_t k0 = part * g.per_split, k1 = min(g.k_blocks, k0 + g.per_split);
+  const uint32_t part = g.splits > 1 ? blockIdx.x % g.splits : 0, team = PAIR ? 2 : g.splits;
+  const uint32_t worker = blockIdx.x / team, workers = gridDim.x / team, k0 = part * g.per_split;
+  auto k_end = [&](const GemmProduct& p) { return !TWO && g.splits > 1 ? min(p.k_blocks, k0 + g.per_split) : p.k_blocks; };
   if (warp == 0) {
     if (lane == 0) {
       asm volatile("fence.proxy.async;" ::: "memory");
       uint32_t n = 0, stage = 0, parity = 1;   // copies issued; a fresh ring is empty
       bool ok = true;
-      for (uint32_t i = first; i < items && ok; i += step) {
-        const Tile t = tile_of<PAIR>(g, i);
-        const uint32_t m0 = t.m0 + rank * kTileM, n0 = t.n0 + rank * b_rows;
+      for (Items<TWO> i(g, worker, workers); i.any && ok; i.next(g)) {
+        const GemmProduct& p = g.p[TWO ? i.which : 0];
+        const Tile t = tile_of<PAIR>(p, g.bn, i.tile);
+        const uint32_t m0 = t.m0 + rank * kTileM, n0 = t.n0 + rank * b_rows, k1 = k_end(p);
         for (uint32_t k = k0; k < k1; ++k) {
           if (!(ok = barrier_wait(empty + 8 * stage, parity))) break;
           const uint32_t at = ring + stage * stage_bytes;
@@ -291,15 +321,15 @@ gemm_kernel(const __grid_constant__ GemmArgs g) {
             if constexpr (PAIR) copy_tile_pair(to, map, (int)x, (int)y, bar);
             else copy_tile(to, map, (int)x, (int)y, bar);
           };
-          if (!g.a_across) {
-            copy(at, &g.a, k * kBlockK, m0);
+          if (!p.a_across) {
+            copy(at, &p.a, k * kBlockK, m0);
           } else {
-            for (uint32_t j = 0; j < kTileM; j += 64) copy(at + j * 128, &g.a, m0 + j, k * kBlockK);
+            for (uint32_t j = 0; j < kTileM; j += 64) copy(at + j * 128, &p.a, m0 + j, k * kBlockK);
           }
-          if (!g.b_across) {
-            copy(at + a_bytes, &g.b, k * kBlockK, n0);
+          if (!p.b_across) {
+            copy(at + a_bytes, &p.b, k * kBlockK, n0);
           } else {
-            for (uint32_t j = 0; j < b_rows; j += 64) copy(at + a_bytes + j * 128, &g.b, n0 + j, k * kBlockK);
+            for (uint32_t j = 0; j < b_rows; j += 64) copy(at + a_bytes + j * 128, &p.b, n0 + j, k * kBlockK);
           }
           ++n;
           if (++stage == g.stages) {
@@ -317,11 +347,12 @@ gemm_kernel(const __grid_constant__ GemmArgs g) {
     }
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {
-      const uint32_t shape = mma_shape(BF16, g.a_across, g.b_across, PAIR ? 2 * kTileM : kTileM, g.bn);
-      const uint32_t a_step = tile_step(g.a_across), b_step = tile_step(g.b_across);
       uint32_t stage = 0, parity = 0, turn = 0;
       bool ok = true;
-      for (uint32_t i = first; i < items && ok; i += step, ++turn) {
+      for (Items<TWO> i(g, worker, workers); i.any && ok; i.next(g), ++turn) {
+        const GemmProduct& p = g.p[TWO ? i.which : 0];
+        const uint32_t shape = mma_shape(BF16, p.a_across, p.b_across, PAIR ? 2 * kTileM : kTileM, g.bn);
+        const uint32_t a_step = tile_step(p.a_across), b_step = tile_step(p.b_across), k1 = k_end(p);
         const uint32_t b = turn & 1u;
         if (!(ok = barrier_wait(sum_empty + 8 * b, ((turn >> 1) & 1u) ^ 1u))) break;
         tmem_fence_after();
@@ -329,7 +360,7 @@ gemm_kernel(const __grid_constant__ GemmArgs g) {
           if (!(ok = barrier_wait(full + 8 * stage, parity))) break;
           tmem_fence_after();
           const uint32_t at = ring + stage * stage_bytes;
-          const uint64_t da = tile_descriptor(at, g.a_across), db = tile_descriptor(at + a_bytes, g.b_across);
+          const uint64_t da = tile_descriptor(at, p.a_across), db = tile_descriptor(at + a_bytes, p.b_across);
 #pragma unroll
           for (uint32_t j = 0; j < kBlockK / 16; ++j)
             mma<PAIR>(tmem + b * g.bn, da + j * a_step, db + j * b_step, shape, k > k0 || j > 0);
@@ -348,8 +379,9 @@ gemm_kernel(const __grid_constant__ GemmArgs g) {
     const uint32_t half = (uint32_t)(warp - 2) >> 2;   // of their columns, by turns
     float* const tile = staging + (warp - 2) * kStage;
     uint32_t turn = 0;
-    for (uint32_t i = first; i < items; i += step, ++turn) {
-      const Tile t = tile_of<PAIR>(g, i);
+    for (Items<TWO> i(g, worker, workers); i.any; i.next(g), ++turn) {
+      const GemmProduct& p = g.p[TWO ? i.which : 0];
+      const Tile t = tile_of<PAIR>(p, g.bn, i.tile);
       const uint32_t b = turn & 1u;
       if (!barrier_wait(sum_full + 8 * b, (turn >> 1) & 1u)) {
         if (lane == 0) atomicExch(&gave_up, 1u);
@@ -358,7 +390,7 @@ gemm_kernel(const __grid_constant__ GemmArgs g) {
       __syncwarp();
       tmem_fence_after();
       const uint32_t from = tmem + ((quarter * 32u) << 16) + b * g.bn;
-      if (!PAIR && (g.splits > 1 || g.turned)) {
+      if (!PAIR && !TWO && (g.splits > 1 || g.turned)) {
         // to shared memory (the ring is no longer read: there is one tile): see below
         const uint32_t row = quarter * 32 + lane;
         for (uint32_t c0 = half * 16; c0 < g.bn; c0 += 32) {
@@ -375,7 +407,7 @@ gemm_kernel(const __grid_constant__ GemmArgs g) {
           }
         }
       } else {
-        for (uint32_t c0 = half * 32; c0 < g.bn && t.n0 + c0 < g.n; c0 += 64) {
+        for (uint32_t c0 = half * 32; c0 < g.bn && t.n0 + c0 < p.n; c0 += 64) {
           float v[32];
           __syncwarp();
           tmem_load(from + c0, v);
@@ -385,7 +417,15 @@ gemm_kernel(const __grid_constant__ GemmArgs g) {
             *reinterpret_cast<float4*>(tile + lane * 36 + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
           __syncwarp();
           const uint32_t m0 = t.m0 + rank * kTileM + quarter * 32;
-          if (m0 < g.m) finish_tile<TYPE, OUT32>(g, tile, m0, t.n0 + c0);
+          if (m0 >= p.m) continue;
+          if constexpr (TWO) {
+            Epilogue e{};
+            e.out = p.e.out;
+            if (e.out.type == ADAPM_F32) finish_tile<TYPE, true>(e, p.aligned, tile, p.m, p.n, m0, t.n0 + c0);
+            else finish_tile<TYPE, false>(e, p.aligned, tile, p.m, p.n, m0, t.n0 + c0);
+          } else {
+            finish_tile<TYPE, OUT32>(p.e, p.aligned, tile, p.m, p.n, m0, t.n0 + c0);
+          }
         }
       }
       tmem_fence_before();
@@ -397,19 +437,20 @@ gemm_kernel(const __grid_constant__ GemmArgs g) {
     }
   }
   __syncwarp();
-  if (!PAIR && (g.splits > 1 || g.turned)) {
+  if (!PAIR && !TWO && (g.splits > 1 || g.turned)) {
     // One tile per block, or one part of it: the cluster's blocks add up a
     // share each, in the order of the parts.
     cg::cluster_group cluster = cg::this_cluster();
     if (g.splits > 1) cluster.sync();
     else __syncthreads();
-    const Tile t = tile_of<PAIR>(g, first);
+    const GemmProduct& p = g.p[0];
+    const Tile t = tile_of<PAIR>(p, g.bn, worker);
     const uint32_t shift = 31 - __clz(g.bn);
     // four neighbours at a time, of all parts at once
     for (uint32_t j = 4 * (part * kGemmThreads + threadIdx.x); j < kTileM * g.bn; j += 4 * g.splits * kGemmThreads) {
       const uint32_t m = g.turned ? j & (kTileM - 1) : j >> shift, n = g.turned ? j / kTileM : j & (g.bn - 1);
       const uint32_t at = g.turned ? j : m * (g.bn + 4) + n;
-      if (t.m0 + m >= g.m || t.n0 + n >= g.n) continue;
+      if (t.m0 + m >= p.m || t.n0 + n >= p.n) continue;
       float4 v[kMostSplits];
 #pragma unroll
       for (uint32_t s = 0; s < kMostSplits; ++s)
@@ -421,21 +462,21 @@ gemm_kernel(const __grid_constant__ GemmArgs g) {
         if (s >= g.splits) break;
         z[0] += v[s].x; z[1] += v[s].y; z[2] += v[s].z; z[3] += v[s].w;
       }
-      const uint32_t c = g.turned ? t.m0 + m : t.n0 + n, width = g.turned ? g.m : g.n;   // (columns of the product)
+      const uint32_t c = g.turned ? t.m0 + m : t.n0 + n, width = g.turned ? p.m : p.n;   // (columns of the product)
       const uint64_t r = g.turned ? t.n0 + n : t.m0 + m;
       float bias[4] = {0.f, 0.f, 0.f, 0.f};
-      if (g.e.bias.data)
+      if (p.e.bias.data)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (c + i < width) bias[i] = load_as(g.e.bias.data, g.e.bias.type, c + i);
-      if (g.aligned && c + 4 <= width) {
-        finish<TYPE, OUT32, 4, 1>(g.e, r, 0, c, 1, bias, z);
+          if (c + i < width) bias[i] = load_as(p.e.bias.data, p.e.bias.type, c + i);
+      if (p.aligned && c + 4 <= width) {
+        finish<TYPE, OUT32, 4, 1>(p.e, r, 0, c, 1, bias, z);
       } else {
 #pragma unroll 1
         for (int i = 0; i < 4 && c + i < width; ++i) {
           const float b1[1] = {i == 0 ? bias[0] : (i == 1 ? bias[1] : (i == 2 ? bias[2] : bias[3]))};
           float z1[1] = {i == 0 ? z[0] : (i == 1 ? z[1] : (i == 2 ? z[2] : z[3]))};
-          finish<TYPE, OUT32, 1, 1>(g.e, r, 0, c + i, 1, b1, z1);
+          finish<TYPE, OUT32, 1, 1>(p.e, r, 0, c + i, 1, b1, z1);
         }
       }
     }
@@ -593,8 +634,10 @@ cudaError_t tensor_map(const Operand& o, bool bf16, uint32_t height, CUtensorMap
 
 // ---- sizes of a product -----------------------------------------------------------------
 struct GemmPlan {
+  uint64_t m, n;
   bool turned, pair;
   uint32_t bn, tiles_m, tiles_n, k_blocks, splits, per_split, stages;
+  double us;   // that it takes, by kForms
 };
 // What a form of the kernel takes: microseconds before the first round of
 // tiles, per block of k and per tile, as measured with fp16 outputs on sizes
@@ -614,90 +657,151 @@ struct Form {
 constexpr Form kForms[] = {
     {true, 256, 7.6, 0.284, 2.1}, {false, 256, 6.6, 0.345, 1.1}, {false, 128, 4.8, 0.24, 1.2}, {false, 64, 3.5, 0.22, 0.9}};
 constexpr double kPartsCost = 3.0;   // of summing k in parts by a cluster
+uint64_t tiles_of(const GemmPlan& p, uint32_t bn, bool pair) {
+  const uint64_t height = pair ? 2 * kTileM : kTileM;
+  return ((p.m + height - 1) / height) * ((p.n + bn - 1) / bn);
+}
+void set_form(GemmPlan& p, uint32_t bn, bool pair, uint64_t parts) {
+  const uint32_t height = pair ? 2 * kTileM : kTileM;
+  p.pair = pair;
+  p.bn = bn;
+  p.tiles_m = (uint32_t)((p.m + height - 1) / height);
+  p.tiles_n = (uint32_t)((p.n + bn - 1) / bn);
+  p.per_split = (uint32_t)((p.k_blocks + parts - 1) / parts);
+  p.splits = (p.k_blocks + p.per_split - 1) / p.per_split;
+  const uint32_t stage = kTileM * 128 + (pair ? bn / 2 : bn) * 128;
+  p.stages = std::min(kMaxStages, (kSmem - 1024 - 512 - kFinishWarps * kStage * (uint32_t)sizeof(float)) / stage);
+}
 // The product of `rows` x `columns` elements over k.
 GemmPlan gemm_plan(uint64_t rows, uint32_t columns, uint64_t k, int sms) {
   GemmPlan p{};
   p.turned = rows <= kTurnedRows;
-  const uint64_t m = p.turned ? columns : rows, n = p.turned ? rows : columns;
+  p.m = p.turned ? columns : rows;
+  p.n = p.turned ? rows : columns;
   p.k_blocks = (uint32_t)((k + kBlockK - 1) / kBlockK);
-  auto tiles_of = [&](uint32_t bn, bool pair) {
-    const uint64_t height = pair ? 2 * kTileM : kTileM;
-    return ((m + height - 1) / height) * ((n + bn - 1) / bn);
-  };
   // parts of k, of at least two blocks, while SMs are idle
   auto parts_of = [&](uint64_t tiles) {
     return std::max<uint64_t>(1, std::min<uint64_t>({(uint64_t)sms / tiles, p.k_blocks / 2, kMostSplits}));
   };
-  uint64_t parts = 1;
   if (p.turned) {
-    p.bn = n <= 16 ? 16 : (n <= 32 ? 32 : 64);
-    parts = parts_of(tiles_of(p.bn, false));
-  } else {
-    double best = 0.0;
-    for (const Form& f : kForms) {
-      const uint64_t tiles = tiles_of(f.bn, f.pair), at_once = f.pair ? sms / 2 : sms;
-      const double rounds = (double)((tiles + at_once - 1) / at_once);
-      for (int in_parts = 0; in_parts < 2; ++in_parts) {
-        const uint64_t s = in_parts ? parts_of(tiles) : 1;
-        if (in_parts && (s == 1 || f.bn > 64)) continue;   // (128 x 128 in parts: 1327 x 3315 x 651 30 -> 35)
-        const double us = f.start + (in_parts ? kPartsCost : 0.0) + rounds * ((double)((p.k_blocks + s - 1) / s) * f.block + f.tile);
-        if (best != 0.0 && us >= best) continue;
-        best = us;
-        p.pair = f.pair;
-        p.bn = f.bn;
-        parts = s;
-      }
+    const uint32_t bn = p.n <= 16 ? 16 : (p.n <= 32 ? 32 : 64);
+    set_form(p, bn, false, parts_of(tiles_of(p, bn, false)));
+    return p;
+  }
+  const Form* best = nullptr;
+  uint64_t parts = 1;
+  for (const Form& f : kForms) {
+    const uint64_t tiles = tiles_of(p, f.bn, f.pair), at_once = f.pair ? sms / 2 : sms;
+    const double rounds = (double)((tiles + at_once - 1) / at_once);
+    for (int in_parts = 0; in_parts < 2; ++in_parts) {
+      const uint64_t s = in_parts ? parts_of(tiles) : 1;
+      if (in_parts && (s == 1 || f.bn > 64)) continue;   // (128 x 128 in parts: 1327 x 3315 x 651 30 -> 35)
+      const double us = f.start + (in_parts ? kPartsCost : 0.0) + rounds * ((double)((p.k_blocks + s - 1) / s) * f.block + f.tile);
+      if (best && us >= p.us) continue;
+      best = &f;
+      p.us = us;
+      parts = s;
     }
   }
-  const uint32_t height = p.pair ? 2 * kTileM : kTileM;
-  p.tiles_m = (uint32_t)((m + height - 1) / height);
-  p.tiles_n = (uint32_t)((n + p.bn - 1) / p.bn);
-  p.per_split = (uint32_t)((p.k_blocks + parts - 1) / parts);
-  p.splits = (p.k_blocks + p.per_split - 1) / p.per_split;
-  const uint32_t stage = kTileM * 128 + (p.pair ? p.bn / 2 : p.bn) * 128;
-  p.stages = std::min(kMaxStages, (kSmem - 1024 - 512 - kFinishWarps * kStage * (uint32_t)sizeof(float)) / stage);
+  set_form(p, best->bn, best->pair, parts);
   return p;
+}
+// How two products share a launch.
+struct Shared {
+  uint32_t late, head;
+};
+// Whether one launch of one form does p (of as many blocks of k or more) and q
+// sooner than each one's own: then they have that form.  A round of p that is
+// not full is filled with tiles of q.  By a sixteenth at least, and not in
+// pairs, which leave little idle (both gradients of rows x ins x outs, us):
+//                          apart   one launch   of pairs
+//     777 x  256 x 1000     16.2      10.5
+//    1024 x 1024 x 1024     16.2      10.4
+//    2048 x 2048 x 2048     34.1      30.1       35.0
+//   16384 x 1024 x 1024     99.9      81.6
+//    4096 x 4096 x 4096    185       205        182
+//    8192 x 4096 x 4096    350                  361
+bool share(GemmPlan& p, GemmPlan& q, int sms, Shared* how) {
+  if (p.turned || q.turned) return false;
+  double best = (p.us + q.us) * 15 / 16;
+  const Form* form = nullptr;
+  for (const Form& f : kForms) {
+    if (f.pair) continue;
+    const uint64_t of_p = tiles_of(p, f.bn, false), of_q = tiles_of(q, f.bn, false);
+    const uint64_t workers = std::min<uint64_t>(sms, of_p + of_q);
+    const double each_p = p.k_blocks * f.block + f.tile, each_q = q.k_blocks * f.block + f.tile;
+    const uint64_t late = of_p % workers, head = late ? (uint64_t)(each_p / each_q) : 0;
+    const uint64_t ahead = late ? head * (workers - late) : 0;
+    const double rounds = (double)(of_p / workers), common = (double)(((of_q > ahead ? of_q - ahead : 0) + workers - 1) / workers);
+    const double us = f.start + rounds * each_p + (late ? std::max(each_p, (double)head * each_q) : 0.0) + common * each_q;
+    if (us >= best) continue;
+    best = us;
+    form = &f;
+    *how = {(uint32_t)late, (uint32_t)head};
+  }
+  if (!form) return false;
+  set_form(p, form->bn, false, 1);
+  set_form(q, form->bn, false, 1);
+  return true;
 }
 
 bool on_four(const MatrixView& v, uint64_t rows) {
   return v.data == nullptr || (reinterpret_cast<uintptr_t>(v.data) % (4 * type_size(v.type)) == 0 && (rows <= 1 || v.row_stride % 4 == 0));
 }
 
-// rows x columns = left (rows x k) right (k x columns).
-cudaError_t launch_gemm(const GemmPlan& p, const Operand& left, const Operand& right, bool bf16, const Epilogue& e, DevState* st,
-                        int sms, cudaStream_t stream) {
+// rows x columns = left (rows x k) right (k x columns), with its epilogue.
+struct Product {
+  GemmPlan p;
+  Operand left, right;
+  Epilogue e;
+  size_t bytes() const { return round256(left.bytes) + round256(right.bytes); }
+};
+// One product, or two that share a launch.
+cudaError_t launch_gemm(const Product& first, const Product* second, const Shared& how, bool bf16, DevState* st, int sms, cudaStream_t stream) {
+  const GemmPlan& p = first.p;
   GemmArgs g{};
-  const Operand& a = p.turned ? right : left;
-  const Operand& b = p.turned ? left : right;
-  cudaError_t err = tensor_map(a, bf16, kTileM, &g.a);
-  if (err == cudaSuccess) err = tensor_map(b, bf16, p.pair ? p.bn / 2 : p.bn, &g.b);
-  if (err != cudaSuccess) return err;
-  g.a_across = a.across;
-  g.b_across = b.across;
+  for (int i = 0; i < (second ? 2 : 1); ++i) {
+    const Product& q = i ? *second : first;
+    GemmProduct& to = g.p[i];
+    const Operand& a = p.turned ? q.right : q.left;
+    const Operand& b = p.turned ? q.left : q.right;
+    cudaError_t err = tensor_map(a, bf16, kTileM, &to.a);
+    if (err == cudaSuccess) err = tensor_map(b, bf16, p.pair ? p.bn / 2 : p.bn, &to.b);
+    if (err != cudaSuccess) return err;
+    to.a_across = a.across;
+    to.b_across = b.across;
+    to.aligned = on_four(q.e.out, q.left.mn) && on_four(q.e.pre, q.left.mn) && on_four(q.e.residual, q.left.mn);
+    to.m = (uint32_t)a.mn;
+    to.n = (uint32_t)b.mn;
+    to.k_blocks = q.p.k_blocks;
+    to.tiles_m = q.p.tiles_m;
+    to.tiles_n = q.p.tiles_n;
+    to.e = q.e;
+  }
+  g.late = how.late;
+  g.head = how.head;
   g.turned = p.turned;
-  g.m = (uint32_t)a.mn;
-  g.n = (uint32_t)b.mn;
   g.bn = p.bn;
   g.stages = p.stages;
-  g.tiles_m = p.tiles_m;
-  g.tiles_n = p.tiles_n;
-  g.k_blocks = p.k_blocks;
   g.splits = p.splits;
   g.per_split = p.per_split;
-  g.aligned = on_four(e.out, left.mn) && on_four(e.pre, left.mn) && on_four(e.residual, left.mn);
-  g.e = e;
   g.st = st;
-  const bool out32 = e.out.type == ADAPM_F32;
   using Kernel = void (*)(GemmArgs);
-  static constexpr Kernel kernels[2][2][2] = {
-      {{gemm_kernel<false, false, false>, gemm_kernel<false, false, true>}, {gemm_kernel<false, true, false>, gemm_kernel<false, true, true>}},
-      {{gemm_kernel<true, false, false>, gemm_kernel<true, false, true>}, {gemm_kernel<true, true, false>, gemm_kernel<true, true, true>}}};
-  const Kernel kernel = kernels[bf16][out32][p.pair];
-  static Asked asked[2][2][2];
-  err = asked[bf16][out32][p.pair].allow(kernel, kSmem - 1024);
+  // (two products share no pairs)
+  static constexpr Kernel kernels[2][3][2] = {
+      {{gemm_kernel<false, false, false, false>, gemm_kernel<false, false, true, false>},
+       {gemm_kernel<false, true, false, false>, gemm_kernel<false, true, true, false>},
+       {gemm_kernel<false, false, false, true>, nullptr}},
+      {{gemm_kernel<true, false, false, false>, gemm_kernel<true, false, true, false>},
+       {gemm_kernel<true, true, false, false>, gemm_kernel<true, true, true, false>},
+       {gemm_kernel<true, false, false, true>, nullptr}}};
+  const int what = second ? 2 : (first.e.out.type == ADAPM_F32 ? 1 : 0);
+  const Kernel kernel = kernels[bf16][what][p.pair];
+  static Asked asked[2][3][2];
+  const cudaError_t err = asked[bf16][what][p.pair].allow(kernel, kSmem - 1024);
   if (err != cudaSuccess) return err;
   // (a block whose tile goes through the ring to its epilogue takes one tile)
-  const uint64_t tiles = (uint64_t)p.tiles_m * p.tiles_n;
+  const uint64_t tiles = (uint64_t)p.tiles_m * p.tiles_n + (second ? (uint64_t)second->p.tiles_m * second->p.tiles_n : 0);
   const bool single = p.splits > 1 || p.turned;
   const unsigned cluster = p.pair ? 2 : p.splits;
   cudaLaunchAttribute at[2]{};
@@ -803,22 +907,23 @@ bool by_rows(const MatrixView& m, uint64_t rows, uint32_t columns) {   // stored
   return columns <= 1 || m.col_stride == 1 || !(rows <= 1 || m.row_stride == 1);
 }
 
-}  // namespace
-
-size_t linear_scratch(const LinearArgs& a, int sms) {
-  const GemmPlan p = gemm_plan(a.rows, a.outs, a.ins, sms);
-  const Operand x = operand(a.x.data, a.rows, a.ins, a.x.row_stride, a.x.col_stride, p.turned);
-  const Operand w = operand(a.weight.data, a.outs, a.ins, a.weight.col_stride, a.weight.row_stride, false);
-  return round256(x.bytes) + round256(w.bytes);
+Product out_product(const LinearArgs& a, int sms) {   // rows x outs over ins
+  Product q;
+  q.p = gemm_plan(a.rows, a.outs, a.ins, sms);
+  q.left = operand(a.x.data, a.rows, a.ins, a.x.row_stride, a.x.col_stride, q.p.turned);
+  q.right = operand(a.weight.data, a.outs, a.ins, a.weight.col_stride, a.weight.row_stride, false);
+  q.e = Epilogue{a.bias, a.residual, a.out, a.pre, a.activation};
+  return q;
 }
 
+}  // namespace
+
+size_t linear_scratch(const LinearArgs& a, int sms) { return out_product(a, sms).bytes(); }
+
 cudaError_t launch_linear(const LinearArgs& a, char* scratch, int sms, cudaStream_t stream) {
-  const GemmPlan p = gemm_plan(a.rows, a.outs, a.ins, sms);
-  Operand x = operand(a.x.data, a.rows, a.ins, a.x.row_stride, a.x.col_stride, p.turned);
-  Operand w = operand(a.weight.data, a.outs, a.ins, a.weight.col_stride, a.weight.row_stride, false);
-  pack(x, w, scratch, stream);
-  const Epilogue e{a.bias, a.residual, a.out, a.pre, a.activation};
-  return launch_gemm(p, x, w, a.x.type == ADAPM_BF16, e, a.st, sms, stream);
+  Product q = out_product(a, sms);
+  pack(q.left, q.right, scratch, stream);
+  return launch_gemm(q, nullptr, Shared{}, a.x.type == ADAPM_BF16, a.st, sms, stream);
 }
 
 namespace {
@@ -854,16 +959,13 @@ Backward backward_of(const LinearArgs& a, char* scratch, int sms) {
   b.sum_bytes = a.dbias.data ? round256((size_t)b.blocks * a.outs * sizeof(float)) : 0;
   return b;
 }
-struct Product {
-  GemmPlan p;
-  Operand left, right;
-  size_t bytes() const { return round256(left.bytes) + round256(right.bytes); }
-};
 Product dx_product(const LinearArgs& a, const Backward& b, int sms) {   // rows x ins over outs
   Product q;
   q.p = gemm_plan(a.rows, a.ins, a.outs, sms);
   q.left = operand(b.dz.data, a.rows, a.outs, b.dz.row_stride, b.dz.col_stride, q.p.turned);
   q.right = operand(a.weight.data, a.ins, a.outs, a.weight.row_stride, a.weight.col_stride, false);
+  q.e = Epilogue{};
+  q.e.out = a.dx;
   return q;
 }
 Product dweight_product(const LinearArgs& a, const Backward& b, int sms) {   // ins x outs over rows, or its transpose
@@ -875,7 +977,31 @@ Product dweight_product(const LinearArgs& a, const Backward& b, int sms) {   // 
   const Operand d = operand(b.dz.data, a.outs, k, b.dz.col_stride, b.dz.row_stride, turned && b.across_out);
   q.left = b.across_out ? d : x;
   q.right = b.across_out ? x : d;
+  q.e = Epilogue{};
+  q.e.out = a.dweight;
+  if (b.across_out) std::swap(q.e.out.row_stride, q.e.out.col_stride);
   return q;
+}
+// Both, or the one that is wanted; the one of more blocks of k is the first.
+struct Products {
+  int n = 0;
+  Product q[2];
+  bool shared = false;   // in one launch
+  Shared how{};
+  size_t bytes() const {   // (launches that follow each other share scratch)
+    const size_t x = n > 0 ? q[0].bytes() : 0, y = n > 1 ? q[1].bytes() : 0;
+    return shared ? x + y : std::max(x, y);
+  }
+};
+Products backward_products(const LinearArgs& a, const Backward& b, int sms) {
+  Products all;
+  if (a.dx.data) all.q[all.n++] = dx_product(a, b, sms);
+  if (a.dweight.data) all.q[all.n++] = dweight_product(a, b, sms);
+  if (all.n == 2) {
+    if (all.q[0].p.k_blocks < all.q[1].p.k_blocks) std::swap(all.q[0], all.q[1]);
+    all.shared = share(all.q[0].p, all.q[1].p, sms, &all.how);
+  }
+  return all;
 }
 
 template <int TYPE>
@@ -891,10 +1017,7 @@ void launch_dz(const LinearArgs& a, const Backward& b, float* sums, cudaStream_t
 
 size_t linear_grad_scratch(const LinearArgs& a, int sms) {
   const Backward b = backward_of(a, nullptr, sms);
-  size_t most = 0;   // (the products follow each other: they share)
-  if (a.dx.data) most = std::max(most, dx_product(a, b, sms).bytes());
-  if (a.dweight.data) most = std::max(most, dweight_product(a, b, sms).bytes());
-  return b.dz_bytes + b.sum_bytes + most;
+  return b.dz_bytes + b.sum_bytes + backward_products(a, b, sms).bytes();
 }
 
 cudaError_t launch_linear_grad(const LinearArgs& a, char* scratch, int sms, cudaStream_t stream) {
@@ -907,14 +1030,14 @@ cudaError_t launch_linear_grad(const LinearArgs& a, char* scratch, int sms, cuda
     else launch_dz<ADAPM_F16>(a, b, sums, stream);
   }
   if (a.dbias.data) launch_column_join(sums, b.blocks, a.outs, a.outs, a.dbias, VectorView{nullptr, ADAPM_F32}, stream);
-  for (int which = 0; which < 2; ++which) {
-    if ((which ? a.dweight.data : a.dx.data) == nullptr) continue;
-    Product q = which ? dweight_product(a, b, sms) : dx_product(a, b, sms);
-    pack(q.left, q.right, rest, stream);
-    Epilogue e{};
-    e.out = which ? a.dweight : a.dx;
-    if (which && b.across_out) std::swap(e.out.row_stride, e.out.col_stride);
-    const cudaError_t err = launch_gemm(q.p, q.left, q.right, bf16, e, a.st, sms, stream);
+  Products all = backward_products(a, b, sms);
+  size_t at = 0;
+  for (int i = 0; i < all.n; ++i) {
+    Product& q = all.q[i];
+    pack(q.left, q.right, rest + at, stream);
+    if (all.shared) at += q.bytes();
+    if (all.shared && i == 0) continue;
+    const cudaError_t err = launch_gemm(all.shared ? all.q[0] : q, all.shared ? &q : nullptr, all.how, bf16, a.st, sms, stream);
     if (err != cudaSuccess) return err;
   }
   return cudaSuccess;

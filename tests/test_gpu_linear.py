@@ -145,6 +145,25 @@ def test_large_products_of_whole_numbers_are_exact(gpu_lib, pm, size, dtype):
     test_whole_numbers_are_exact(gpu_lib, pm, (LARGE[size],), dtype)
 
 
+# sizes whose two gradients share a launch (few tiles; a last round with free blocks; both products longer than the
+# other) and some whose do not; one rounding of an exact sum, so that bits are compared
+@pytest.mark.parametrize("size", [(777, 256, 1000), (70, 96, 50), (300, 520, 130), (2600, 4100, 200), (4096, 512, 4096),
+                                  (1300, 4099, 1027), (130, 20_000, 70), (40, 90, 24), (5000, 2048, 2048)])
+def test_gradients_of_two_types(gpu_lib, pm, size):
+    rows, ins, outs = size
+    for dtype in HALVES:
+        x, w, grad = small((rows, ins), dtype), small((ins, outs), dtype), small((rows, outs), dtype)
+        dx, dw = grad.double() @ w.double().t(), x.double().t() @ grad.double()
+        for of_x, of_w in ((dtype, torch.float32), (torch.float32, dtype), (dtype, dtype)):
+            for by_out in (False, True):
+                into = gpu_lib.LinearGrads(torch.empty(rows, ins, device="cuda", dtype=of_x),
+                                           stored(torch.empty(ins, outs, device="cuda", dtype=of_w), by_out), None)
+                pm.linear_grad(x, w, grad, out=into)
+                pm.wait()
+                assert torch.equal(into.x, dx.float().to(of_x))
+                assert torch.equal(into.weight, dw.float().to(of_w))
+
+
 @pytest.mark.parametrize("act", ["gelu", "tanh"])
 @pytest.mark.parametrize("size", range(len(LARGE)))
 def test_large_sizes(gpu_lib, pm, size, act):
