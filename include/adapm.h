@@ -43,7 +43,8 @@
  *     whose keys are out of order (adapm_push_grads).  ADAPM_ETIMEOUT
  *     reports that a bounded device-side wait gave up: the key sort of a
  *     push (or of a large embedding gradient) runs as one cooperative launch
- *     whose blocks meet at grid barriers, and a barrier wait is limited.  Work
+ *     whose blocks meet at grid barriers, and a barrier wait is limited, as
+ *     are the waits for copies and products in a dense layer's kernels.  Work
  *     enqueued after such a failure does not touch the store, and the context
  *     is unusable afterwards (destroy it).
  *   - ADAPM_ECUDA reports a CUDA runtime error; the context is then unusable.
@@ -433,7 +434,7 @@ typedef struct {
  * eps), v its variance (the mean of the squared differences from m).  weight
  * and bias (NULL: ones, zeros) have types of their own.  stats (NULL: not
  * wanted) receives m and r of every row, two floats a row without gaps,
- * aligned to 8 bytes.  Computed in fp32, rounded once to out's type; squares
+ * aligned to 8 bytes; it overlaps nothing.  Computed in fp32, rounded once to out's type; squares
  * beyond fp32 make v infinite and r 0.  out is x's own memory (same
  * type and strides) or does not overlap it; its rows must not overlap each
  * other (ADAPM_EINVAL where two strides make them).  eps must not be
@@ -447,7 +448,8 @@ adapm_status adapm_layer_norm(adapm_ctx* ctx, const adapm_shape* shape, const ad
  * (elementwise) every row of dx is r (g - mean(g) - h mean(g h)); dweight is
  * the sum over rows of grad * h, dbias that of grad (zeros without rows).  dx,
  * dweight and dbias may each be NULL (not wanted); dx is the memory of x or
- * of grad (same type and strides) or overlaps neither. */
+ * of grad (same type and strides) or overlaps neither; else what is written
+ * overlaps nothing. */
 adapm_status adapm_layer_norm_grad(adapm_ctx* ctx, const adapm_shape* shape, const adapm_rows* x,
                                    const adapm_rows* grad, const float* stats, const adapm_vector* weight,
                                    const adapm_rows* dx, const adapm_vector* dweight, const adapm_vector* dbias);
@@ -482,9 +484,9 @@ typedef struct {
  * rows x outs with col_stride 1.  pre (NULL: not wanted) receives z in x's
  * type, for the backward pass.  out is of x's type or fp32, residual has out's
  * type and may be its memory; out and pre overlap nothing else.  Products are
- * summed and all else is computed in fp32, each output is rounded once.  rows, ins and outs are at most 2^31, ins
- * and outs not 0.  Operands whose rows (or columns) do not begin on 16 bytes
- * are copied to scratch memory first. */
+ * summed and all else is computed in fp32, each output is rounded once.  rows,
+ * ins and outs are at most 2^31, ins and outs not 0.  Operands whose rows (or
+ * columns) do not begin on 16 bytes are copied to scratch memory first. */
 adapm_status adapm_linear(adapm_ctx* ctx, const adapm_layer* shape, const adapm_matrix* x,
                           const adapm_matrix* weight, const adapm_vector* bias, int32_t activation,
                           const adapm_matrix* residual, const adapm_matrix* out, const adapm_matrix* pre);
@@ -542,7 +544,7 @@ typedef struct {
  * and weights.  weights (one float a row; NULL: ones) and grad (NULL: not
  * wanted) may be left out.  grad has the logits' type and is their own memory
  * (same strides) or does not overlap them; its rows must not overlap each
- * other.  Computed in fp32 from one reading of the logits; a gradient is
+ * other; else loss and grad overlap nothing.  Computed in fp32 from one reading of the logits; a gradient is
  * rounded once to its type. */
 adapm_status adapm_distill(adapm_ctx* ctx, const adapm_shape* shape, const adapm_rows* logits,
                            const adapm_teacher* teacher, float temperature, float soft,

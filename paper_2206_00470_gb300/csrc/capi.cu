@@ -14,6 +14,7 @@
 #include <cstdio>
 #include <cstring>
 #include <deque>
+#include <initializer_list>
 #include <map>
 #include <new>
 #include <string>
@@ -1002,6 +1003,13 @@ adapm_status check_tensors(adapm_ctx* ctx, const adapm_tensor* t, uint64_t n, co
       return fail(ctx, ADAPM_EINVAL, "%s[%llu] is not a device array", what, at);
   }
   return ADAPM_OK;
+}
+
+// Whether memory that is written is one of the others'.
+bool one_of(const void* written, std::initializer_list<const void*> others) {
+  for (const void* p : others)
+    if (written != nullptr && p == written) return true;
+  return false;
 }
 
 // ---- dense layers --------------------------------------------------------------
@@ -2031,6 +2039,9 @@ adapm_status adapm_layer_norm(adapm_ctx* ctx, const adapm_shape* shape, const ad
   if (n == 0) return ADAPM_OK;
   st = check_written(ctx, shape, out, x, "out");
   if (st != ADAPM_OK) return st;
+  const void *const w = weight ? weight->data : nullptr, *const b = bias ? bias->data : nullptr;
+  if (one_of(out->data, {w, b, stats}) || one_of(stats, {x->data, w, b}))
+    return fail(ctx, ADAPM_EINVAL, "out or stats is the memory of another array");
   const adapm_tokens t = tokens_of(shape);
   NormArgs a{};
   a.n = n;
@@ -2064,6 +2075,11 @@ adapm_status adapm_layer_norm_grad(adapm_ctx* ctx, const adapm_shape* shape, con
   if (st == ADAPM_OK && n > 0 && dx) st = check_written(ctx, shape, dx, x, "dx");
   if (st == ADAPM_OK && n > 0 && dx) st = check_written(ctx, shape, dx, grad, "dx");
   if (st != ADAPM_OK) return st;
+  const void *const w = weight ? weight->data : nullptr, *const dw = dweight ? dweight->data : nullptr;
+  const void* const db = dbias ? dbias->data : nullptr;
+  if (n > 0 && ((dx && one_of(dx->data, {stats, w, dw, db})) || one_of(dw, {x->data, grad->data, stats, w}) ||
+                one_of(db, {x->data, grad->data, stats, w, dw})))
+    return fail(ctx, ADAPM_EINVAL, "dx, dweight or dbias is the memory of another array");
   ProfScope ps(ctx, 5);
   if (n == 0) {
     for (const adapm_vector* v : {dweight, dbias})
@@ -2111,7 +2127,8 @@ adapm_status adapm_linear(adapm_ctx* ctx, const adapm_layer* shape, const adapm_
     return fail(ctx, ADAPM_EINVAL, "residual is of out's type, elements of a row next to each other");
   if (residual && n > 1 && residual->data == out->data && residual->row_stride != out->row_stride)
     return fail(ctx, ADAPM_EINVAL, "out is the residual's memory in another layout");
-  if (n > 0 && (out->data == x->data || out->data == weight->data || (pre && (pre->data == out->data || pre->data == x->data))))
+  if (n > 0 && (one_of(out->data, {x->data, weight->data, bias ? bias->data : nullptr, pre ? pre->data : nullptr}) ||
+                (pre && one_of(pre->data, {x->data, weight->data, bias ? bias->data : nullptr, residual ? residual->data : nullptr}))))
     return fail(ctx, ADAPM_EINVAL, "out or pre is the memory of another array");
   if (n == 0) return ADAPM_OK;
   LinearArgs a{};
@@ -2156,9 +2173,15 @@ adapm_status adapm_linear_grad(adapm_ctx* ctx, const adapm_layer* shape, const a
     return fail(ctx, ADAPM_EINVAL, "grad and pre are of x's type");
   for (const adapm_matrix* m : {dx, dweight})
     if (m && m->type != x->type && m->type != ADAPM_F32) return fail(ctx, ADAPM_EINVAL, "dx and dweight are of x's type or fp32");
-  if (n > 0 && dx && (dx->data == x->data || dx->data == grad->data || (dweight && dx->data == dweight->data)))
+  const void *const of_x = n > 0 ? x->data : nullptr, *const of_grad = n > 0 ? grad->data : nullptr;
+  const void* const of_pre = n > 0 && activation != ADAPM_ACTIVATION_NONE ? pre->data : nullptr;
+  const void *const to_x = dx && n > 0 ? dx->data : nullptr, *const to_weight = dweight ? dweight->data : nullptr;
+  const void* const to_bias = dbias ? dbias->data : nullptr;
+  if (one_of(to_x, {of_x, weight->data, of_grad, of_pre, to_weight, to_bias}))
     return fail(ctx, ADAPM_EINVAL, "dx is the memory of another array");
-  if (dweight && dweight->data == weight->data) return fail(ctx, ADAPM_EINVAL, "dweight is the memory of weight");
+  if (one_of(to_weight, {of_x, weight->data, of_grad, of_pre, to_bias}))
+    return fail(ctx, ADAPM_EINVAL, "dweight is the memory of another array");
+  if (one_of(to_bias, {of_x, weight->data, of_grad, of_pre})) return fail(ctx, ADAPM_EINVAL, "dbias is the memory of another array");
   ProfScope ps(ctx, 5);
   if (n == 0) {
     if (dweight) {
@@ -2227,6 +2250,11 @@ adapm_status adapm_distill(adapm_ctx* ctx, const adapm_shape* shape, const adapm
   if (n == 0) return ADAPM_OK;
   if (grad) st = check_written(ctx, shape, grad, logits, "grad");
   if (st != ADAPM_OK) return st;
+  const void *const ids = teacher ? teacher->ids : nullptr, *const list = teacher ? teacher->logits : nullptr;
+  const void* const of_labels = labels ? labels->ids : nullptr;
+  if (one_of(loss, {logits->data, grad ? grad->data : nullptr, ids, list, of_labels, weights}) ||
+      (grad && one_of(grad->data, {ids, list, of_labels, weights})))
+    return fail(ctx, ADAPM_EINVAL, "loss or grad is the memory of another array");
   const adapm_tokens t = tokens_of(shape);
   DistillArgs a{};
   a.n = n;

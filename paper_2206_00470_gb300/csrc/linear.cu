@@ -7,11 +7,16 @@
 // operands copied by the tensor memory accelerator into a ring of swizzled
 // blocks of 64 k, sums in tensor memory (two accumulators, so that one tile's
 // epilogue runs beside the next one's products), one warp that issues copies,
-// one that issues products, four for the epilogue.  Operands are taken as they
-// lie in memory, with k contiguous or across it; what the accelerator cannot
-// address (rows that do not begin on 16 bytes) is copied first.
+// one that issues products, eight for the epilogue.  Large products are taken
+// by pairs of blocks, 256 x 256 a tile.  Operands are taken as they lie in
+// memory, with k contiguous or across it; what the accelerator cannot address
+// (rows that do not begin on 16 bytes) is copied first.  Up to 64 rows are the
+// columns of a tile whose rows are the weight's columns.
 // Bound by the tensor cores where all three sizes are large, by memory where
-// one is small: then k is summed in parts, so that every SM reads.
+// one is small: then k is summed in parts, so that every SM reads.  bf16, 8192
+// x 4096 x 8192 with bias, activation, z kept and residual 362 to 377 us, 1.5
+// PFLOP/s (320 us alone, 1.7; at full power the clock falls); gradients of 8192
+// x 4096 x 4096 390 us, of which dz 36; one row by 4096 x 4096 9 us, 3.7 TB/s.
 #include <cooperative_groups.h>
 
 #include <algorithm>

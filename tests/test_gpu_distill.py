@@ -372,6 +372,9 @@ def test_refusals(gpu_lib, pm):
         lambda: pm.distill(x, ids, t, grad=flat.as_strided((4, 8), (4, 1))),
         lambda: pm.distill(flat.as_strided((4, 8), (9, 1)), ids, t, grad=flat.as_strided((4, 8), (8, 1))),
         lambda: pm.distill(torch.zeros(4, 0, device="cuda"), ids, t),
+        lambda: pm.distill(x, ids, t, weights=flat[:4], loss=flat[:4]),
+        lambda: pm.distill(x, ids, t, weights=flat[:4], grad=flat.as_strided((4, 8), (8, 1))),
+        lambda: pm.distill(t, ids, t, grad=t),
     ]
     for i, call in enumerate(bad):
         with pytest.raises((ValueError, gpu_lib.AdaPMError)) as e:

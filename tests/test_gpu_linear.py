@@ -351,6 +351,7 @@ def test_recorded_in_a_graph_and_the_same_bits(gpu_lib):
 def test_refusals(gpu_lib, pm):
     x, w = torch.zeros(4, 8, device="cuda").half(), torch.zeros(8, 16, device="cuda").half()
     y, flat = torch.zeros(4, 16, device="cuda").half(), torch.zeros(200, device="cuda").half()
+    square, y16, y17, w16 = (torch.zeros(16, 16, device="cuda").half() for _ in range(4))
     bad = [
         lambda: pm.linear(x.float(), w.float()),
         lambda: pm.linear(x, w.bfloat16()),
@@ -377,6 +378,15 @@ def test_refusals(gpu_lib, pm):
         lambda: pm.linear_grad(x, w, y, y.float(), "relu"),
         lambda: pm.linear_grad(x, w, y, out=gpu_lib.LinearGrads(x, None, None)),
         lambda: pm.linear_grad(x, w, y, out=gpu_lib.LinearGrads(None, w, None)),
+        lambda: pm.linear(square, w16, square[0], out=square),
+        lambda: pm.linear(square, w16, y16[0], out=y16),
+        lambda: pm.linear(square, w16, y16[0], pre=y16),
+        lambda: pm.linear(square, square.clone(), residual=y16, pre=y16),   # (out may be the residual, pre may not)
+        lambda: pm.linear_grad(square, square.clone(), y16, out=gpu_lib.LinearGrads(None, square, None)),
+        lambda: pm.linear_grad(square, square.clone(), y16, out=gpu_lib.LinearGrads(None, y16, None)),
+        lambda: pm.linear_grad(square, square.clone(), y16, y17, "relu", out=gpu_lib.LinearGrads(y17, None, None)),
+        lambda: pm.linear_grad(square, square.clone(), y16, y17, "relu", out=gpu_lib.LinearGrads(None, None, y17[0])),
+        lambda: pm.linear_grad(square, w16, y16, out=gpu_lib.LinearGrads(w16, None, None)),
         lambda: pm.linear_grad(x, w, y, out=gpu_lib.LinearGrads(None, flat.as_strided((8, 16), (2, 3)), None)),
         lambda: pm.linear_grad(x, w, y, out=gpu_lib.LinearGrads(None, torch.zeros(8, 16, device="cuda").bfloat16(), None)),
     ]
@@ -385,7 +395,7 @@ def test_refusals(gpu_lib, pm):
             call()
         assert not isinstance(e.value, gpu_lib.AdaPMError) or e.value.status == gpu_lib.EINVAL, i
     pm.wait()
-    assert not flat.any() and not x.any() and not w.any() and not y.any()
+    assert not any(t.any() for t in (flat, x, w, y, square, y16, y17, w16))
     assert not pm.linear(x, w).any()
 
 

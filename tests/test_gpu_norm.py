@@ -364,6 +364,11 @@ def test_refusals(gpu_lib, pm):
         lambda: pm.layer_norm_grad(x, x, stats[:3]),
         lambda: pm.layer_norm_grad(x, x, stats.cpu()),
         lambda: pm.layer_norm_grad(x, x, stats, out=gpu_lib.NormGrads(torch.zeros(4, 9, device="cuda")[:, :7], None, None)),
+        lambda: pm.layer_norm(x, flat[:8], out=flat.as_strided((4, 8), (8, 1))),   # over what the rows are scaled by
+        lambda: pm.layer_norm(torch.zeros(4, 2, device="cuda"), out=stats, stats=stats),
+        lambda: pm.layer_norm_grad(x, x.clone(), stats, flat[:8], out=gpu_lib.NormGrads(None, flat[:8], None)),
+        lambda: pm.layer_norm_grad(x, x.clone(), stats, out=gpu_lib.NormGrads(None, flat[:8], flat[:8])),
+        lambda: pm.layer_norm_grad(x, x.clone(), stats, out=gpu_lib.NormGrads(None, None, x[0])),
     ]
     for i, call in enumerate(bad):
         with pytest.raises((ValueError, gpu_lib.AdaPMError)) as e:
