@@ -29,12 +29,21 @@ struct GemmProduct {
   uint32_t tiles_m, tiles_n;
   Epilogue e;
 };
+// Sums of columns that blocks without a tile add up meanwhile: `count` rows of
+// `columns` floats to one row (no parts: nothing).
+struct ColumnSums {
+  const float* parts;
+  uint32_t count, columns;
+  VectorView out;
+};
 // One product, or two whose tiles the same blocks take, the second one's after
 // the first one's.  In the first one's last round `late` workers have a tile;
 // the others begin with `head` tiles of the second that take as long.
 struct GemmArgs {
   GemmProduct p[2];          // (one: the second has no tiles)
   uint32_t late, head;
+  uint32_t workers;          // (of two products)
+  ColumnSums sums;           // (beside two products: of the blocks behind the workers)
   bool turned;               // D is the product's transpose: m counts its columns
   uint32_t bn, stages;
   uint32_t splits, per_split;   // parts that one product's k is summed in, and blocks of a part

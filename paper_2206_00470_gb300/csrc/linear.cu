@@ -258,6 +258,27 @@ __device__ __forceinline__ void finish_tile(const Epilogue& e, bool aligned, con
   }
 }
 
+// Block `block` of `blocks`: 32 columns at a time, every warp its share of the
+// rows, the warps' sums in their order.
+__device__ __forceinline__ void add_columns(const ColumnSums& s, float* shared, uint32_t block, uint32_t blocks) {
+  constexpr uint32_t kWarps = kGemmThreads / 32;
+  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+  for (uint32_t c0 = block * 32; c0 < s.columns; c0 += blocks * 32) {
+    const uint32_t c = c0 + lane;
+    float sum = 0.f;
+    if (c < s.columns)
+#pragma unroll 4
+      for (uint32_t i = warp; i < s.count; i += kWarps) sum += s.parts[(uint64_t)i * s.columns + c];
+    shared[warp * 32 + lane] = sum;
+    __syncthreads();
+    if (warp == 0 && c < s.columns) {
+      for (uint32_t w = 1; w < kWarps; ++w) sum += shared[w * 32 + lane];
+      store_as(s.out.data, s.out.type, c, sum);
+    }
+    __syncthreads();
+  }
+}
+
 // kGemmThreads threads: warp 0 copies, warp 1 multiplies, the others finish.
 // PAIR: tiles of 256 x bn by two blocks; each copies its halves of the operands
 // and finishes its half of the rows, the first one multiplies.  An SM then
@@ -304,9 +325,11 @@ gemm_kernel(const __grid_constant__ GemmArgs g) {
   const uint32_t tmem = tmem_at;
   // with parts of k, each block of a cluster sums one part of one tile
   const uint32_t part = g.splits > 1 ? blockIdx.x % g.splits : 0, team = PAIR ? 2 : g.splits;
-  const uint32_t worker = blockIdx.x / team, workers = gridDim.x / team, k0 = part * g.per_split;
+  const uint32_t worker = blockIdx.x / team, workers = TWO ? g.workers : gridDim.x / team, k0 = part * g.per_split;
   auto k_end = [&](const GemmProduct& p) { return !TWO && g.splits > 1 ? min(p.k_blocks, k0 + g.per_split) : p.k_blocks; };
-  if (warp == 0) {
+  if (TWO && worker >= workers) {
+    add_columns(g.sums, staging, worker - workers, gridDim.x - workers);
+  } else if (warp == 0) {
     if (lane == 0) {
       asm volatile("fence.proxy.async;" ::: "memory");
       uint32_t n = 0, stage = 0, parity = 1;   // copies issued; a fresh ring is empty
@@ -760,9 +783,11 @@ struct Product {
   Operand left, right;
   Epilogue e;
   size_t bytes() const { return round256(left.bytes) + round256(right.bytes); }
+  uint64_t tiles() const { return (uint64_t)p.tiles_m * p.tiles_n; }
 };
 // One product, or two that share a launch.
-cudaError_t launch_gemm(const Product& first, const Product* second, const Shared& how, bool bf16, DevState* st, int sms, cudaStream_t stream) {
+cudaError_t launch_gemm(const Product& first, const Product* second, const Shared& how, const ColumnSums& sums, bool bf16, DevState* st, int sms,
+                        cudaStream_t stream) {
   const GemmPlan& p = first.p;
   GemmArgs g{};
   for (int i = 0; i < (second ? 2 : 1); ++i) {
@@ -805,8 +830,11 @@ cudaError_t launch_gemm(const Product& first, const Product* second, const Share
   static Asked asked[2][3][2];
   const cudaError_t err = asked[bf16][what][p.pair].allow(kernel, kSmem - 1024);
   if (err != cudaSuccess) return err;
+  const uint64_t tiles = first.tiles() + (second ? second->tiles() : 0);
+  g.workers = (uint32_t)std::min<uint64_t>(tiles, (uint64_t)sms);
+  g.sums = sums;
+  const uint32_t others = sums.parts ? std::min((uint32_t)sms - g.workers, (sums.columns + 31) / 32) : 0;
   // (a block whose tile goes through the ring to its epilogue takes one tile)
-  const uint64_t tiles = (uint64_t)p.tiles_m * p.tiles_n + (second ? (uint64_t)second->p.tiles_m * second->p.tiles_n : 0);
   const bool single = p.splits > 1 || p.turned;
   const unsigned cluster = p.pair ? 2 : p.splits;
   cudaLaunchAttribute at[2]{};
@@ -817,7 +845,7 @@ cudaError_t launch_gemm(const Product& first, const Product* second, const Share
   at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t c{};
   c.gridDim = dim3((unsigned)(p.pair ? 2 * std::min<uint64_t>(tiles, (uint64_t)sms / 2)
-                                     : (single ? tiles * p.splits : std::min<uint64_t>(tiles, (uint64_t)sms))));
+                                     : (single ? tiles * p.splits : g.workers + others)));
   c.blockDim = dim3(kGemmThreads);
   c.dynamicSmemBytes = 1024 + (size_t)p.stages * (kTileM + (p.pair ? p.bn / 2 : p.bn)) * 128 + kFinishWarps * kStage * sizeof(float);
   c.stream = stream;
@@ -928,7 +956,7 @@ size_t linear_scratch(const LinearArgs& a, int sms) { return out_product(a, sms)
 cudaError_t launch_linear(const LinearArgs& a, char* scratch, int sms, cudaStream_t stream) {
   Product q = out_product(a, sms);
   pack(q.left, q.right, scratch, stream);
-  return launch_gemm(q, nullptr, Shared{}, a.x.type == ADAPM_BF16, a.st, sms, stream);
+  return launch_gemm(q, nullptr, Shared{}, ColumnSums{}, a.x.type == ADAPM_BF16, a.st, sms, stream);
 }
 
 namespace {
@@ -1034,15 +1062,18 @@ cudaError_t launch_linear_grad(const LinearArgs& a, char* scratch, int sms, cuda
     if (bf16) launch_dz<ADAPM_BF16>(a, b, sums, stream);
     else launch_dz<ADAPM_F16>(a, b, sums, stream);
   }
-  if (a.dbias.data) launch_column_join(sums, b.blocks, a.outs, a.outs, a.dbias, VectorView{nullptr, ADAPM_F32}, stream);
   Products all = backward_products(a, b, sms);
+  // the sums of dz's columns: beside the products where they leave blocks free
+  ColumnSums beside{};
+  if (a.dbias.data && all.shared && all.q[0].tiles() + all.q[1].tiles() < (uint64_t)sms) beside = ColumnSums{sums, b.blocks, a.outs, a.dbias};
+  else if (a.dbias.data) launch_column_join(sums, b.blocks, a.outs, a.outs, a.dbias, VectorView{nullptr, ADAPM_F32}, stream);
   size_t at = 0;
   for (int i = 0; i < all.n; ++i) {
     Product& q = all.q[i];
     pack(q.left, q.right, rest + at, stream);
     if (all.shared) at += q.bytes();
     if (all.shared && i == 0) continue;
-    const cudaError_t err = launch_gemm(all.shared ? all.q[0] : q, all.shared ? &q : nullptr, all.how, bf16, a.st, sms, stream);
+    const cudaError_t err = launch_gemm(all.shared ? all.q[0] : q, all.shared ? &q : nullptr, all.how, beside, bf16, a.st, sms, stream);
     if (err != cudaSuccess) return err;
   }
   return cudaSuccess;
