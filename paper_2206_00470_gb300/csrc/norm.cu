@@ -446,30 +446,36 @@ norm_columns_kernel(const __grid_constant__ NormArgs a) {
   out[a.dim + c] = db;
 }
 
-// The sums of `count` blocks over `width` columns, in a fixed order: 32 columns
-// a block, every warp takes each 32nd block's sums, four of them on their way
-// at a time.
+// The sums of `count` blocks over `width` columns, in a fixed order: a block
+// takes kJoinColumns of them, each by kJoinRows threads, which take every
+// kJoinRows-th block's sums, four of them on their way at a time.  Few columns a
+// block: more blocks, and fewer loads one after the other.
+constexpr uint32_t kJoinColumns = 16, kJoinRows = 1024 / kJoinColumns;
 __global__ void __launch_bounds__(1024)
 column_join_kernel(const float* parts, uint32_t count, uint64_t width, uint32_t dim, VectorView low, VectorView high) {
   after_previous();
-  __shared__ float sums[32][33];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const uint64_t c = (uint64_t)blockIdx.x * 32 + lane;
+  __shared__ float sums[kJoinColumns][kJoinRows + 1];
+  const uint32_t column = threadIdx.x % kJoinColumns, first = threadIdx.x / kJoinColumns;
+  const uint64_t c = (uint64_t)blockIdx.x * kJoinColumns + column;
   float s = 0.f;
   if (c < width) {
-    uint32_t p = warp;
-    for (; p + 96 < count; p += 128) {
-      const float x0 = parts[p * width + c], x1 = parts[(p + 32) * width + c], x2 = parts[(p + 64) * width + c],
-                  x3 = parts[(p + 96) * width + c];
+    uint32_t p = first;
+    for (; p + 3 * kJoinRows < count; p += 4 * kJoinRows) {
+      const float x0 = parts[p * width + c], x1 = parts[(p + kJoinRows) * width + c], x2 = parts[(p + 2 * kJoinRows) * width + c],
+                  x3 = parts[(p + 3 * kJoinRows) * width + c];
       s = (((s + x0) + x1) + x2) + x3;
     }
-    for (; p < count; p += 32) s += parts[p * width + c];
+    for (; p < count; p += kJoinRows) s += parts[p * width + c];
   }
-  sums[warp][lane] = s;
+  sums[column][first] = s;
   __syncthreads();
-  // warp w adds up column w
-  s = lanes_sum(sums[lane][warp], 32);
-  const uint64_t mine = (uint64_t)blockIdx.x * 32 + warp;
+  // a warp adds up a column
+  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+  if (warp >= kJoinColumns) return;
+  s = 0.f;
+  for (uint32_t i = lane; i < kJoinRows; i += 32) s += sums[warp][i];
+  s = lanes_sum(s, 32);
+  const uint64_t mine = (uint64_t)blockIdx.x * kJoinColumns + warp;
   if (lane != 0 || mine >= width) return;
   const VectorView& v = mine < dim ? low : high;
   if (v.data != nullptr) store_as(v.data, v.type, mine < dim ? mine : mine - dim, s);
@@ -581,7 +587,7 @@ void launch_layer_norm_grad(const NormArgs& a, int sms, cudaStream_t stream) {
 void launch_column_join(const float* parts, uint32_t count, uint64_t width, uint32_t dim, const VectorView& low,
                         const VectorView& high, cudaStream_t stream) {
   note_launches(1);
-  launch_after(column_join_kernel, (unsigned)((width + 31) / 32), 1024, 0, stream, parts, count, width, dim, low, high);
+  launch_after(column_join_kernel, (unsigned)((width + kJoinColumns - 1) / kJoinColumns), 1024, 0, stream, parts, count, width, dim, low, high);
 }
 
 }  // namespace adapm
