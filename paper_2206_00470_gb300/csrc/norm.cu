@@ -17,7 +17,7 @@
 // Bound by memory: 65,472 rows of 1024 bf16 forward 48 us, 5.5 TB/s, 262,144
 // rows backward 271 us, 6.0 TB/s; one row of 4096 by the launch, 6.9 us.  Odd
 // rows of fp16, which no wide access fits, are bound by instructions: 5105 rows
-// of 1001 backward 16 us.
+// of 1001 backward 15 us.
 #include <algorithm>
 
 #include "dense.cuh"
