@@ -707,11 +707,13 @@ distill_slices_kernel(const __grid_constant__ DistillArgs a, int split) {
       if (lane == 0) {
         sh.slice = s;
         barrier_expect(full, bytes);
-        if (bytes > 0)
+        if (bytes > 0) {
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (words written plainly for the row before)
           asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
                            shared_at(place + (in0 - s.e0))),
                        "l"(b.base + (uint64_t)in0 * 16), "r"(bytes), "r"(full)
                        : "memory");
+        }
       }
       ++copies;
       __syncwarp();
