@@ -484,7 +484,8 @@ typedef struct {
  * rows x outs with col_stride 1.  pre (NULL: not wanted) receives z in x's
  * type, for the backward pass.  out is of x's type or fp32, residual has out's
  * type and may be its memory; out and pre overlap nothing else.  Products are
- * summed and all else is computed in fp32, each output is rounded once.  rows,
+ * summed and all else is computed in fp32 (for an fp32 output at most 512 of
+ * them in the tensor cores, which do not round to nearest), each output is rounded once.  rows,
  * ins and outs are at most 2^31, ins and outs not 0.  Operands whose rows (or
  * columns) do not begin on 16 bytes are copied to scratch memory first. */
 adapm_status adapm_linear(adapm_ctx* ctx, const adapm_layer* shape, const adapm_matrix* x,

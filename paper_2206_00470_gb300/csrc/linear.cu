@@ -36,6 +36,14 @@ constexpr uint32_t kSmem = 232448;          // shared memory of a block
 constexpr uint32_t kGroupM = 16;            // tiles of m taken together, for L2 (8192 x 4096 x 8192: 4 384 us, 8 381, 16 366, 32 372)
 constexpr uint32_t kTurnedRows = 64;        // up to so many rows the weight's columns are m
 constexpr uint32_t kMostSplits = 8;         // parts of k: the blocks of a cluster
+// Blocks of k that the tensor cores add up for an output of 32 bits; such
+// chains' sums are added by the epilogue's warps.  The tensor cores cut what
+// does not fit fp32 towards zero, which grows with the number of additions:
+// 4096 x 4096 x 4096 is off by 4.8e-6 in one chain, by 6.5e-7 in eight, of 12
+// blocks each by 9.2e-7 (96, 141 and 137 us: tiles of 256 columns leave the
+// chains' sums no registers; 133 x 4096 x 2048 16.1, 17.5 and 17.2).  A 16-bit
+// output's rounding is hundreds of times that.
+constexpr uint32_t kChain = 8;
 
 // ---- activations -----------------------------------------------------------------
 // 1 / (1 + 2^x); 0 where 2^x is beyond fp32, as in the limit.
@@ -285,8 +293,9 @@ __device__ __forceinline__ void add_columns(const ColumnSums& s, float* shared, 
 // holds, and writes to its shared memory, half of b's tile: with tiles of 128 x
 // 256 copies and products move 96 KB through it per block of k, 188 bytes a clock at
 // full rate, with pairs 64 KB.
+// CHAIN: for fp32 outputs of more than kChain blocks of k, tiles of up to 128 columns.
 // TWO: of two products, both without more of an epilogue than the output, each of a type of its own.
-template <bool BF16, bool OUT32, bool PAIR, bool TWO>
+template <bool BF16, bool OUT32, bool PAIR, bool TWO, bool CHAIN>
 __global__ void __launch_bounds__(kGemmThreads, 1)
 gemm_kernel(const __grid_constant__ GemmArgs g) {
   constexpr int TYPE = BF16 ? ADAPM_BF16 : ADAPM_F16;
@@ -377,28 +386,31 @@ gemm_kernel(const __grid_constant__ GemmArgs g) {
     if (lane == 0 && rank == 0) {
       uint32_t stage = 0, parity = 0, turn = 0;
       bool ok = true;
-      for (Items<TWO> i(g, worker, workers); i.any && ok; i.next(g), ++turn) {
+      for (Items<TWO> i(g, worker, workers); i.any && ok; i.next(g)) {
         const GemmProduct& p = g.p[TWO ? i.which : 0];
         const uint32_t shape = mma_shape(BF16, p.a_across, p.b_across, PAIR ? 2 * kTileM : kTileM, g.bn);
         const uint32_t a_step = tile_step(p.a_across), b_step = tile_step(p.b_across), k1 = k_end(p);
-        const uint32_t b = turn & 1u;
-        if (!(ok = barrier_wait(sum_empty + 8 * b, ((turn >> 1) & 1u) ^ 1u))) break;
-        tmem_fence_after();
-        for (uint32_t k = k0; k < k1; ++k) {
-          if (!(ok = barrier_wait(full + 8 * stage, parity))) break;
+        for (uint32_t from = k0, to; from < k1 && ok; from = to, ++turn) {   // a chain of them
+          to = CHAIN ? min(k1, from + kChain) : k1;
+          const uint32_t b = turn & 1u;
+          if (!(ok = barrier_wait(sum_empty + 8 * b, ((turn >> 1) & 1u) ^ 1u))) break;
           tmem_fence_after();
-          const uint32_t at = ring + stage * stage_bytes;
-          const uint64_t da = tile_descriptor(at, p.a_across), db = tile_descriptor(at + a_bytes, p.b_across);
+          for (uint32_t k = from; k < to; ++k) {
+            if (!(ok = barrier_wait(full + 8 * stage, parity))) break;
+            tmem_fence_after();
+            const uint32_t at = ring + stage * stage_bytes;
+            const uint64_t da = tile_descriptor(at, p.a_across), db = tile_descriptor(at + a_bytes, p.b_across);
 #pragma unroll
-          for (uint32_t j = 0; j < kBlockK / 16; ++j)
-            mma<PAIR>(tmem + b * g.bn, da + j * a_step, db + j * b_step, shape, k > k0 || j > 0);
-          mma_commit<PAIR>(empty + 8 * stage);
-          if (++stage == g.stages) {
-            stage = 0;
-            parity ^= 1u;
+            for (uint32_t j = 0; j < kBlockK / 16; ++j)
+              mma<PAIR>(tmem + b * g.bn, da + j * a_step, db + j * b_step, shape, k > from || j > 0);
+            mma_commit<PAIR>(empty + 8 * stage);
+            if (++stage == g.stages) {
+              stage = 0;
+              parity ^= 1u;
+            }
           }
+          mma_commit<PAIR>(sum_full + 8 * b);
         }
-        mma_commit<PAIR>(sum_full + 8 * b);
       }
       if (!ok) atomicExch(&gave_up, 1u);
     }
@@ -407,60 +419,101 @@ gemm_kernel(const __grid_constant__ GemmArgs g) {
     const uint32_t half = (uint32_t)(warp - 2) >> 2;   // of their columns, by turns
     float* const tile = staging + (warp - 2) * kStage;
     uint32_t turn = 0;
-    for (Items<TWO> i(g, worker, workers); i.any; i.next(g), ++turn) {
+    float run[CHAIN ? 2 : 1][32];   // sums of the chains so far
+    bool ok = true;
+    for (Items<TWO> i(g, worker, workers); i.any && ok; i.next(g)) {
       const GemmProduct& p = g.p[TWO ? i.which : 0];
       const Tile t = tile_of<PAIR>(p, g.bn, i.tile);
-      const uint32_t b = turn & 1u;
-      if (!barrier_wait(sum_full + 8 * b, (turn >> 1) & 1u)) {
-        if (lane == 0) atomicExch(&gave_up, 1u);
-        break;
-      }
-      __syncwarp();
-      tmem_fence_after();
-      const uint32_t from = tmem + ((quarter * 32u) << 16) + b * g.bn;
-      if (!PAIR && !TWO && (g.splits > 1 || g.turned)) {
-        // to shared memory (the ring is no longer read: there is one tile): see below
-        const uint32_t row = quarter * 32 + lane;
-        for (uint32_t c0 = half * 16; c0 < g.bn; c0 += 32) {
-          float v[16];
-          __syncwarp();
-          tmem_load16(from + c0, v);
-          if (g.turned) {
+      const uint32_t m0 = t.m0 + rank * kTileM + quarter * 32, k1 = k_end(p);
+      for (uint32_t k = k0, to; k < k1; k = to, ++turn) {
+        to = CHAIN ? min(k1, k + kChain) : k1;
+        const bool more = CHAIN && k > k0, last = !CHAIN || to == k1;
+        const uint32_t b = turn & 1u;
+        if (!(ok = barrier_wait(sum_full + 8 * b, (turn >> 1) & 1u))) {
+          if (lane == 0) atomicExch(&gave_up, 1u);
+          break;
+        }
+        __syncwarp();
+        tmem_fence_after();
+        const uint32_t from = tmem + ((quarter * 32u) << 16) + b * g.bn;
+        if (!PAIR && !TWO && (g.splits > 1 || g.turned)) {
+          // to shared memory (the ring is no longer read: there is one tile): see below
+          const uint32_t row = quarter * 32 + lane;
 #pragma unroll
-            for (int j = 0; j < 16; ++j) ring_floats[(c0 + j) * kTileM + row] = v[j];
-          } else {
+          for (uint32_t n = 0; n < 2; ++n) {
+            const uint32_t c0 = half * 16 + n * 32;
+            if (c0 >= g.bn) break;
+            float v[16];
+            __syncwarp();
+            tmem_load16(from + c0, v);
+            if constexpr (CHAIN) {
 #pragma unroll
-            for (int j = 0; j < 16; j += 4)
-              *reinterpret_cast<float4*>(ring_floats + row * (g.bn + 4) + c0 + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+              for (int j = 0; j < 16; ++j) {
+                if (more) v[j] += run[0][n * 16 + j];
+                run[0][n * 16 + j] = v[j];
+              }
+            }
+            if (!last) continue;
+            if (g.turned) {
+#pragma unroll
+              for (int j = 0; j < 16; ++j) ring_floats[(c0 + j) * kTileM + row] = v[j];
+            } else {
+#pragma unroll
+              for (int j = 0; j < 16; j += 4)
+                *reinterpret_cast<float4*>(ring_floats + row * (g.bn + 4) + c0 + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+            }
+          }
+        } else if (!last) {
+          if constexpr (CHAIN) {
+#pragma unroll
+            for (uint32_t n = 0; n < 2; ++n) {
+              const uint32_t c0 = half * 32 + n * 64;
+              if (c0 >= g.bn || t.n0 + c0 >= p.n) break;
+              float v[32];
+              __syncwarp();
+              tmem_load(from + c0, v);
+#pragma unroll
+              for (int j = 0; j < 32; ++j) run[n][j] = more ? run[n][j] + v[j] : v[j];
+            }
+          }
+        } else {
+          for (uint32_t c0 = half * 32, n = 0; c0 < g.bn && t.n0 + c0 < p.n; c0 += 64, ++n) {
+            float v[32];
+            __syncwarp();
+            tmem_load(from + c0, v);
+            if constexpr (CHAIN) {
+              // (an array of registers has no index)
+              auto add = [&](const float (&sums)[32]) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] += sums[j];
+              };
+              if (more) {
+                if (n == 0) add(run[0]);
+                else add(run[1]);
+              }
+            }
+            // through shared memory, so that neighbouring lanes hold neighbouring columns
+#pragma unroll
+            for (int j = 0; j < 32; j += 4)
+              *reinterpret_cast<float4*>(tile + lane * 36 + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+            __syncwarp();
+            if (m0 >= p.m) continue;
+            if constexpr (TWO) {
+              Epilogue e{};
+              e.out = p.e.out;
+              if (e.out.type == ADAPM_F32) finish_tile<TYPE, true>(e, p.aligned, tile, p.m, p.n, m0, t.n0 + c0);
+              else finish_tile<TYPE, false>(e, p.aligned, tile, p.m, p.n, m0, t.n0 + c0);
+            } else {
+              finish_tile<TYPE, OUT32>(p.e, p.aligned, tile, p.m, p.n, m0, t.n0 + c0);
+            }
           }
         }
-      } else {
-        for (uint32_t c0 = half * 32; c0 < g.bn && t.n0 + c0 < p.n; c0 += 64) {
-          float v[32];
-          __syncwarp();
-          tmem_load(from + c0, v);
-          // through shared memory, so that neighbouring lanes hold neighbouring columns
-#pragma unroll
-          for (int j = 0; j < 32; j += 4)
-            *reinterpret_cast<float4*>(tile + lane * 36 + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-          __syncwarp();
-          const uint32_t m0 = t.m0 + rank * kTileM + quarter * 32;
-          if (m0 >= p.m) continue;
-          if constexpr (TWO) {
-            Epilogue e{};
-            e.out = p.e.out;
-            if (e.out.type == ADAPM_F32) finish_tile<TYPE, true>(e, p.aligned, tile, p.m, p.n, m0, t.n0 + c0);
-            else finish_tile<TYPE, false>(e, p.aligned, tile, p.m, p.n, m0, t.n0 + c0);
-          } else {
-            finish_tile<TYPE, OUT32>(p.e, p.aligned, tile, p.m, p.n, m0, t.n0 + c0);
-          }
+        tmem_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if constexpr (PAIR) barrier_arrive_at(shared_of(sum_empty + 8 * b, 0));
+          else barrier_arrive(sum_empty + 8 * b);
         }
-      }
-      tmem_fence_before();
-      __syncwarp();
-      if (lane == 0) {
-        if constexpr (PAIR) barrier_arrive_at(shared_of(sum_empty + 8 * b, 0));
-        else barrier_arrive(sum_empty + 8 * b);
       }
     }
   }
@@ -664,6 +717,7 @@ cudaError_t tensor_map(const Operand& o, bool bf16, uint32_t height, CUtensorMap
 struct GemmPlan {
   uint64_t m, n;
   bool turned, pair;
+  bool chained;   // in chains of kChain blocks of k
   uint32_t bn, tiles_m, tiles_n, k_blocks, splits, per_split, stages;
   double us;   // that it takes, by kForms
 };
@@ -701,12 +755,13 @@ void set_form(GemmPlan& p, uint32_t bn, bool pair, uint64_t parts) {
   p.stages = std::min(kMaxStages, (kSmem - 1024 - 512 - kFinishWarps * kStage * (uint32_t)sizeof(float)) / stage);
 }
 // The product of `rows` x `columns` elements over k.
-GemmPlan gemm_plan(uint64_t rows, uint32_t columns, uint64_t k, int sms) {
+GemmPlan gemm_plan(uint64_t rows, uint32_t columns, uint64_t k, bool out32, int sms) {
   GemmPlan p{};
   p.turned = rows <= kTurnedRows;
   p.m = p.turned ? columns : rows;
   p.n = p.turned ? rows : columns;
   p.k_blocks = (uint32_t)((k + kBlockK - 1) / kBlockK);
+  p.chained = out32 && p.k_blocks > kChain;
   // parts of k, of at least two blocks, while SMs are idle
   auto parts_of = [&](uint64_t tiles) {
     return std::max<uint64_t>(1, std::min<uint64_t>({(uint64_t)sms / tiles, p.k_blocks / 2, kMostSplits}));
@@ -719,6 +774,7 @@ GemmPlan gemm_plan(uint64_t rows, uint32_t columns, uint64_t k, int sms) {
   const Form* best = nullptr;
   uint64_t parts = 1;
   for (const Form& f : kForms) {
+    if (p.chained && f.bn > 128) continue;   // (sums of chains that the registers hold)
     const uint64_t tiles = tiles_of(p, f.bn, f.pair), at_once = f.pair ? sms / 2 : sms;
     const double rounds = (double)((tiles + at_once - 1) / at_once);
     for (int in_parts = 0; in_parts < 2; ++in_parts) {
@@ -750,7 +806,7 @@ struct Shared {
 //    4096 x 4096 x 4096    185       205        182
 //    8192 x 4096 x 4096    350                  361
 bool share(GemmPlan& p, GemmPlan& q, int sms, Shared* how) {
-  if (p.turned || q.turned) return false;
+  if (p.turned || q.turned || p.chained || q.chained) return false;
   double best = (p.us + q.us) * 15 / 16;
   const Form* form = nullptr;
   for (const Form& f : kForms) {
@@ -817,17 +873,19 @@ cudaError_t launch_gemm(const Product& first, const Product* second, const Share
   g.per_split = p.per_split;
   g.st = st;
   using Kernel = void (*)(GemmArgs);
-  // (two products share no pairs)
-  static constexpr Kernel kernels[2][3][2] = {
-      {{gemm_kernel<false, false, false, false>, gemm_kernel<false, false, true, false>},
-       {gemm_kernel<false, true, false, false>, gemm_kernel<false, true, true, false>},
-       {gemm_kernel<false, false, false, true>, nullptr}},
-      {{gemm_kernel<true, false, false, false>, gemm_kernel<true, false, true, false>},
-       {gemm_kernel<true, true, false, false>, gemm_kernel<true, true, true, false>},
-       {gemm_kernel<true, false, false, true>, nullptr}}};
-  const int what = second ? 2 : (first.e.out.type == ADAPM_F32 ? 1 : 0);
+  // (two products share no pairs, and chains are none of theirs)
+  static constexpr Kernel kernels[2][4][2] = {
+      {{gemm_kernel<false, false, false, false, false>, gemm_kernel<false, false, true, false, false>},
+       {gemm_kernel<false, true, false, false, false>, gemm_kernel<false, true, true, false, false>},
+       {gemm_kernel<false, false, false, true, false>, nullptr},
+       {gemm_kernel<false, true, false, false, true>, nullptr}},
+      {{gemm_kernel<true, false, false, false, false>, gemm_kernel<true, false, true, false, false>},
+       {gemm_kernel<true, true, false, false, false>, gemm_kernel<true, true, true, false, false>},
+       {gemm_kernel<true, false, false, true, false>, nullptr},
+       {gemm_kernel<true, true, false, false, true>, nullptr}}};
+  const int what = second ? 2 : (p.chained ? 3 : (first.e.out.type == ADAPM_F32 ? 1 : 0));
   const Kernel kernel = kernels[bf16][what][p.pair];
-  static Asked asked[2][3][2];
+  static Asked asked[2][4][2];
   const cudaError_t err = asked[bf16][what][p.pair].allow(kernel, kSmem - 1024);
   if (err != cudaSuccess) return err;
   const uint64_t tiles = first.tiles() + (second ? second->tiles() : 0);
@@ -942,7 +1000,7 @@ bool by_rows(const MatrixView& m, uint64_t rows, uint32_t columns) {   // stored
 
 Product out_product(const LinearArgs& a, int sms) {   // rows x outs over ins
   Product q;
-  q.p = gemm_plan(a.rows, a.outs, a.ins, sms);
+  q.p = gemm_plan(a.rows, a.outs, a.ins, a.out.type == ADAPM_F32, sms);
   q.left = operand(a.x.data, a.rows, a.ins, a.x.row_stride, a.x.col_stride, q.p.turned);
   q.right = operand(a.weight.data, a.outs, a.ins, a.weight.col_stride, a.weight.row_stride, false);
   q.e = Epilogue{a.bias, a.residual, a.out, a.pre, a.activation};
@@ -994,7 +1052,7 @@ Backward backward_of(const LinearArgs& a, char* scratch, int sms) {
 }
 Product dx_product(const LinearArgs& a, const Backward& b, int sms) {   // rows x ins over outs
   Product q;
-  q.p = gemm_plan(a.rows, a.ins, a.outs, sms);
+  q.p = gemm_plan(a.rows, a.ins, a.outs, a.dx.type == ADAPM_F32, sms);
   q.left = operand(b.dz.data, a.rows, a.outs, b.dz.row_stride, b.dz.col_stride, q.p.turned);
   q.right = operand(a.weight.data, a.ins, a.outs, a.weight.row_stride, a.weight.col_stride, false);
   q.e = Epilogue{};
@@ -1004,7 +1062,8 @@ Product dx_product(const LinearArgs& a, const Backward& b, int sms) {   // rows 
 Product dweight_product(const LinearArgs& a, const Backward& b, int sms) {   // ins x outs over rows, or its transpose
   Product q;
   const uint32_t k = (uint32_t)a.rows;
-  q.p = b.across_out ? gemm_plan(a.outs, a.ins, k, sms) : gemm_plan(a.ins, a.outs, k, sms);
+  const bool out32 = a.dweight.type == ADAPM_F32;
+  q.p = b.across_out ? gemm_plan(a.outs, a.ins, k, out32, sms) : gemm_plan(a.ins, a.outs, k, out32, sms);
   const bool turned = q.p.turned;
   const Operand x = operand(a.x.data, a.ins, k, a.x.col_stride, a.x.row_stride, turned && !b.across_out);
   const Operand d = operand(b.dz.data, a.outs, k, b.dz.col_stride, b.dz.row_stride, turned && b.across_out);

@@ -255,6 +255,28 @@ def test_residual_in_place(gpu_lib, pm):
         assert torch.equal(y, want)
 
 
+@pytest.mark.parametrize("size", [(1, 4096, 300), (40, 9000, 24), (130, 20_000, 70), (2600, 4100, 200), (300, 1024, 520),
+                                  (9000, 65, 130), (20_000, 300, 40), (4096, 2100, 1500), (500, 577, 3000)])
+def test_long_sums_in_32_bits(gpu_lib, pm, size):
+    """Positive numbers, whose sums' errors add up. At most 512 products are summed in the tensor cores, 16 at a time, by
+    two units in the last place each (and 16 more, as above): 80 * 2^-23; the chains' sums by a half each: k / 512 * 2^-24,
+    and parts of k and the rest of the epilogue by 16 * 2^-24."""
+    rows, ins, outs = size
+    for dtype in HALVES:
+        x, w, g = (torch.rand(s, device="cuda").add_(1).to(dtype) for s in ((rows, ins), (ins, outs), (rows, outs)))
+        for by_out in (False, True):
+            ws = stored(w, by_out)
+            out = pm.linear(x, ws, dtype=torch.float32)
+            into = gpu_lib.LinearGrads(torch.empty(rows, ins, device="cuda"),
+                                       stored(torch.empty(ins, outs, device="cuda"), by_out), None)
+            pm.linear_grad(x, ws, g, out=into)
+            pm.wait()
+            for got, a, b in ((out, x, w), (into.x, g, w.t()), (into.weight, x.t(), g)):
+                want = a.double() @ b.double()
+                k = a.shape[1]
+                assert ((got.double() - want).abs() <= want * (80 * 2.0 ** -23 + (k / 512 + 16) * 2.0 ** -24)).all()
+
+
 def test_parts_of_the_gradient(gpu_lib, pm):
     x, w, grad = torch.randn(70, 96, device="cuda").half(), torch.randn(96, 50, device="cuda").half(), \
         torch.randn(70, 50, device="cuda").half()
