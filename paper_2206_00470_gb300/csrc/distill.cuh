@@ -438,9 +438,16 @@ __device__ __forceinline__ RowFactors row_factors(const DistillArgs& a, float we
   const float2 u = unround_both<MODE>(k, per);
   f.st = scale.t * u.x;
   f.so = scale.one * u.y;
-  // 16-bit gradients of one exponential: the factor is added to the exponent (off by 2^-18 of the result at most)
-  f.folded = MODE == ONE_SUM && TYPE != ADAPM_F32 && f.st >= 0.f;
-  f.minus_k = -(k * per) + (f.folded ? log2f(f.st) : 0.f);
+  // 16-bit gradients of one exponential: the factor is added to the exponent, where the sum is below 128 and its
+  // logarithm at most 64: both round by 2^-18, so a gradient is off by 2^-17 of itself at most, a 64th of a half step
+  // of fp16.  (Around 20,000 it would be 7e-4, more than that half step.)
+  f.minus_k = -(k * per);
+  f.folded = false;
+  if (MODE == ONE_SUM && TYPE != ADAPM_F32 && f.st >= 0x1p-64f && f.st <= 0x1p64f) {
+    const float sum = f.minus_k + log2f(f.st);
+    f.folded = fabsf(sum) < 128.f;
+    if (f.folded) f.minus_k = sum;
+  }
   f.minus_k1 = -(k * kLog2E);
   return f;
 }
