@@ -356,25 +356,10 @@ struct Largest {
     }
   }
 };
-// Where max c is this large, logits are taken relative to the largest before
-// they are multiplied (which would lose too much, or overflow).  Those within
-// the exponential's range of it share its leading bits, so their differences
-// are exact in 16 bits too.
+// Where max c is this large, for one of the temperatures, logits are taken
+// relative to the largest before they are multiplied (which would lose too
+// much, or overflow): in fp32, so that a difference serves both temperatures.
 constexpr float kHuge = 1e5f;
-template <int TYPE>
-__device__ __forceinline__ void take_off(uint4& v, float max) {
-  uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    if constexpr (TYPE == ADAPM_F32) {
-      w[j] = __float_as_uint(__uint_as_float(w[j]) - max);
-    } else {
-      const float2 f = unpack2<TYPE>(w[j]);
-      w[j] = pack2<TYPE>(f.x - max, f.y - max);
-    }
-  }
-  v = make_uint4(w[0], w[1], w[2], w[3]);
-}
 
 // 2^(s c - k) with k = max c, rounded, is off by the rounding of k alone; times
 // this it is 2^((s - max) c).
@@ -384,24 +369,30 @@ __device__ __forceinline__ float unround(float max, float c) {
 }
 
 __device__ __forceinline__ float finite_shift(float m) { return m == -INFINITY ? 0.f : m; }
-__device__ __forceinline__ bool is_huge(float max, float per) { return fabsf(max * kLog2E) > kHuge || fabsf(max * per) > kHuge; }
 
 // Which sums a row has: at one temperature; at two; at two of which the first is
 // 2, where e^d = (e^(d/2))^2 (3063 rows of 50,021 bf16, both terms: 164 -> 122 us).
 enum { ONE_SUM = 0, TWO_SUMS = 1, SQUARES = 2 };
+template <int MODE>
+__device__ __forceinline__ bool is_huge(float max, float per) {
+  return fabsf(max * per) > kHuge || (MODE == TWO_SUMS && fabsf(max * kLog2E) > kHuge);
+}
 
-// Constants of 2^(s c - k) at both temperatures, as pairs.
+// Constants of 2^(s c - k) at both temperatures, as pairs; off: what is taken
+// off first where the largest is huge (k: 0).
 struct Exponents {
-  uint64_t c, m, c1, m1;
-  __device__ __forceinline__ Exponents(float per, float k)
-      : c(pair_of(per, per)), m(pair_of(-(k * per), -(k * per))), c1(pair_of(kLog2E, kLog2E)), m1(pair_of(-(k * kLog2E), -(k * kLog2E))) {}
+  uint64_t c, m, c1, m1, off;
+  __device__ __forceinline__ Exponents(float per, float k, float largest)
+      : c(pair_of(per, per)), m(pair_of(-(k * per), -(k * per))), c1(pair_of(kLog2E, kLog2E)), m1(pair_of(-(k * kLog2E), -(k * kLog2E))),
+        off(pair_of(-largest, -largest)) {}
 };
 // Adds the exponentials of the elements of a word, two by two.
-template <int TYPE, int MODE>
+template <int TYPE, int MODE, bool HUGE>
 __device__ __forceinline__ void add_word(const uint4& word, const Exponents& e, uint64_t& t, uint64_t& one) {
 #pragma unroll
   for (int j = 0; j < Word<TYPE>::kElements / 2; ++j) {
-    const uint64_t s = pair_at<TYPE>(word, j);
+    uint64_t s = pair_at<TYPE>(word, j);
+    if (HUGE) s = add_pair(s, e.off);
     const float2 d = floats_of(fma_pair(s, e.c, e.m));
     const uint64_t x = pair_of(exp2_of(d.x), exp2_of(d.y));
     t = add_pair(t, x);
@@ -433,7 +424,7 @@ __device__ __forceinline__ RowFactors row_factors(const DistillArgs& a, float we
   const RowScale scale = row_scale(a, weight, task, all, MODE != ONE_SUM);
   RowFactors f;
   f.max = all.max;
-  f.huge = is_huge(all.max, per);
+  f.huge = is_huge<MODE>(all.max, per);
   const float k = f.huge ? 0.f : all.max;
   const float2 u = unround_both<MODE>(k, per);
   f.st = scale.t * u.x;
@@ -443,7 +434,7 @@ __device__ __forceinline__ RowFactors row_factors(const DistillArgs& a, float we
   // of fp16.  (Around 20,000 it would be 7e-4, more than that half step.)
   f.minus_k = -(k * per);
   f.folded = false;
-  if (MODE == ONE_SUM && TYPE != ADAPM_F32 && f.st >= 0x1p-64f && f.st <= 0x1p64f) {
+  if (MODE == ONE_SUM && TYPE != ADAPM_F32 && !f.huge && f.st >= 0x1p-64f && f.st <= 0x1p64f) {
     const float sum = f.minus_k + log2f(f.st);
     f.folded = fabsf(sum) < 128.f;
     if (f.folded) f.minus_k = sum;
@@ -451,18 +442,19 @@ __device__ __forceinline__ RowFactors row_factors(const DistillArgs& a, float we
   f.minus_k1 = -(k * kLog2E);
   return f;
 }
-template <int TYPE, int MODE, bool FOLD>
+template <int TYPE, int MODE, bool FOLD, bool HUGE>
 struct Gradient {
-  uint64_t c, m, ct, c1, m1, co;
+  uint64_t c, m, ct, c1, m1, co, off;
   __device__ __forceinline__ Gradient(const RowFactors& f, float per)
       : c(pair_of(per, per)), m(pair_of(f.minus_k, f.minus_k)), ct(pair_of(f.st, f.st)), c1(pair_of(kLog2E, kLog2E)),
-        m1(pair_of(f.minus_k1, f.minus_k1)), co(pair_of(f.so, f.so)) {}
+        m1(pair_of(f.minus_k1, f.minus_k1)), co(pair_of(f.so, f.so)), off(pair_of(-f.max, -f.max)) {}
   __device__ __forceinline__ uint4 of(const uint4& word) const {
     constexpr int E = Word<TYPE>::kElements;
     float x[E];
 #pragma unroll
     for (int j = 0; j < E / 2; ++j) {
-      const uint64_t s = pair_at<TYPE>(word, j);
+      uint64_t s = pair_at<TYPE>(word, j);
+      if (HUGE) s = add_pair(s, off);
       const float2 d = floats_of(fma_pair(s, c, m));
       float2 f = make_float2(exp2_of(d.x), exp2_of(d.y));
       if (!FOLD) {
@@ -485,10 +477,11 @@ struct Gradient {
 // fn(Gradient) in the form that the row's factors ask for.
 template <int TYPE, int MODE, class F>
 __device__ __forceinline__ void with_gradient(const RowFactors& f, float per, F&& fn) {
+  if (f.huge) return fn(Gradient<TYPE, MODE, false, true>(f, per));
   if constexpr (MODE == ONE_SUM && TYPE != ADAPM_F32) {
-    if (f.folded) return fn(Gradient<TYPE, MODE, true>(f, per));
+    if (f.folded) return fn(Gradient<TYPE, MODE, true, false>(f, per));
   }
-  fn(Gradient<TYPE, MODE, false>(f, per));
+  fn(Gradient<TYPE, MODE, false, false>(f, per));
 }
 
 // Sums of several parts of a row, relative to the largest of all: `count` of
@@ -557,22 +550,22 @@ distill_rows_kernel(const __grid_constant__ DistillArgs a) {
       RowSums mine;
       mine.max = lanes_max(largest.value());
       const float shift = finite_shift(mine.max);
-      const bool huge = is_huge(shift, per);
-      if (huge) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i) take_off<TYPE>(v[i], shift);
-      }
+      const bool huge = is_huge<MODE>(shift, per);
       const float k = huge ? 0.f : shift;
-      const Exponents e(per, k);
+      const Exponents e(per, k, shift);
       uint64_t st = 0, so = 0;
+      if (!huge) {
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        if (i * THREADS >= (int)b.words) break;
-        add_word<TYPE, MODE>(v[i], e, st, so);
-      }
-      if (huge) {   // (as they were: the gradient is relative to the whole row's largest)
+        for (int i = 0; i < NV; ++i) {
+          if (i * THREADS >= (int)b.words) break;
+          add_word<TYPE, MODE, false>(v[i], e, st, so);
+        }
+      } else {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) v[i] = load_word<TYPE>(b, a.vocab, i * THREADS + threadIdx.x);
+        for (int i = 0; i < NV; ++i) {
+          if (i * THREADS >= (int)b.words) break;
+          add_word<TYPE, MODE, true>(v[i], e, st, so);
+        }
       }
       const float2 t = floats_of(st), o = floats_of(so), u = unround_both<MODE>(k, per);
       mine.t = lanes_sum((t.x + t.y) * u.x, 32);
@@ -593,10 +586,6 @@ distill_rows_kernel(const __grid_constant__ DistillArgs a) {
     const RowFactors f = row_factors<TYPE, MODE>(a, row_weight(a, row), task, all, per);
     with_gradient<TYPE, MODE>(f, per, [&](const auto& gradient) {
       if (g.head == b.head) {
-        if (f.huge) {
-#pragma unroll
-          for (int i = 0; i < NV; ++i) take_off<TYPE>(v[i], f.max);
-        }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
           if (i * THREADS >= (int)g.words) break;
@@ -606,9 +595,7 @@ distill_rows_kernel(const __grid_constant__ DistillArgs a) {
         // words of the gradient that begin elsewhere: the row again, from L1 and L2
         const uint32_t shift = (b.head - g.head) & (E - 1), back = b.head < g.head ? 1 : 0;
         for (uint32_t w = threadIdx.x; w < g.words; w += THREADS) {
-          uint4 word = load_shifted<TYPE>(b, a.vocab, w - back, shift);
-          if (f.huge) take_off<TYPE>(word, f.max);
-          store_word<TYPE>(g, a.vocab, w, gradient.of(word));
+          store_word<TYPE>(g, a.vocab, w, gradient.of(load_shifted<TYPE>(b, a.vocab, w - back, shift)));
         }
       }
     });
@@ -820,23 +807,21 @@ distill_slices_kernel(const __grid_constant__ DistillArgs a, int split) {
       RowSums mine;
       mine.max = lanes_max(largest.value());
       const float shift = finite_shift(mine.max);
-      const bool huge = is_huge(shift, per);
+      const bool huge = is_huge<MODE>(shift, per);
       const float k = huge ? 0.f : shift;
-      const Exponents e(per, k);
+      const Exponents e(per, k, shift);
       uint64_t st = 0, so = 0;
       if (!huge) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
           if (i * kSliceWork >= count) break;
-          add_word<TYPE, MODE>(v[i], e, st, so);
+          add_word<TYPE, MODE, false>(v[i], e, st, so);
         }
       } else {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
           if (i * kSliceWork >= count) break;
-          uint4 word = v[i];
-          take_off<TYPE>(word, shift);
-          add_word<TYPE, MODE>(word, e, st, so);
+          add_word<TYPE, MODE, true>(v[i], e, st, so);
         }
       }
       const float2 t = floats_of(st), o = floats_of(so), u = unround_both<MODE>(k, per);
@@ -850,13 +835,6 @@ distill_slices_kernel(const __grid_constant__ DistillArgs a, int split) {
       ++lives;
       if (a.grad.data == nullptr) continue;
       const RowFactors f = sh.factors;
-      if (f.huge) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-          if (i * kSliceWork >= count) break;
-          take_off<TYPE>(v[i], f.max);
-        }
-      }
       with_gradient<TYPE, MODE>(f, per, [&](const auto& gradient) {
         const uint32_t w = g0 + threadIdx.x;
         char* const p = to + (uint64_t)w * 16;
@@ -953,9 +931,7 @@ distill_long_kernel(const __grid_constant__ DistillArgs a) {
     with_gradient<TYPE, MODE>(f, per, [&](const auto& gradient) {
 #pragma unroll 4
       for (uint32_t w = g0 + threadIdx.x; w < g1; w += kLongThreads) {
-        uint4 word = load_shifted<TYPE>(b, a.vocab, w - back, shift);
-        if (f.huge) take_off<TYPE>(word, f.max);
-        store_word<TYPE>(g, a.vocab, w, gradient.of(word));
+        store_word<TYPE>(g, a.vocab, w, gradient.of(load_shifted<TYPE>(b, a.vocab, w - back, shift)));
       }
     });
   }
@@ -1047,15 +1023,16 @@ distill_few_kernel(const __grid_constant__ DistillArgs a, uint32_t table) {
   RowSums mine;
   mine.max = lanes_max(largest.value());
   const float shift = finite_shift(mine.max);
-  const bool huge = is_huge(shift, per);
+  const bool huge = is_huge<MODE>(shift, per);
   const float k = huge ? 0.f : shift;
-  const Exponents e(per, k);
+  const Exponents e(per, k, shift);
   uint64_t st = 0, so = 0;
+  if (!huge) {
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    uint4 word = v[i];
-    if (huge) take_off<TYPE>(word, shift);
-    add_word<TYPE, MODE>(word, e, st, so);
+    for (int i = 0; i < NV; ++i) add_word<TYPE, MODE, false>(v[i], e, st, so);
+  } else {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) add_word<TYPE, MODE, true>(v[i], e, st, so);
   }
   const float2 t = floats_of(st), o = floats_of(so), u = unround_both<MODE>(k, per);
   mine.t = lanes_sum((t.x + t.y) * u.x, 32);
@@ -1073,19 +1050,13 @@ distill_few_kernel(const __grid_constant__ DistillArgs a, uint32_t table) {
       const RowFactors f = row_factors<TYPE, MODE>(a, row_weight(a, row), task, all, per);
       with_gradient<TYPE, MODE>(f, per, [&](const auto& gradient) {
         if (g.head == b.head) {
-          if (f.huge) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) take_off<TYPE>(v[i], f.max);
-          }
 #pragma unroll
           for (int i = 0; i < NV; ++i) store_word<TYPE>(g, a.vocab, i * kFewThreads + threadIdx.x, gradient.of(v[i]));
         } else {
           // words of the gradient that begin elsewhere: the row again, from L2
           const uint32_t shift_by = (b.head - g.head) & (E - 1), back = b.head < g.head ? 1 : 0;
           for (uint32_t w = threadIdx.x; w < g.words; w += kFewThreads) {
-            uint4 word = load_shifted<TYPE>(b, a.vocab, w - back, shift_by);
-            if (f.huge) take_off<TYPE>(word, f.max);
-            store_word<TYPE>(g, a.vocab, w, gradient.of(word));
+            store_word<TYPE>(g, a.vocab, w, gradient.of(load_shifted<TYPE>(b, a.vocab, w - back, shift_by)));
           }
         }
       });

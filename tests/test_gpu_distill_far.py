@@ -1,4 +1,4 @@
-"""Distillation of rows far from zero, against the formula in 64 bits.
+"""Distillation of rows far from zero, and at temperatures far from one, against the formula in 64 bits.
 
 Tolerances (u = 2^-24).  As in test_gpu_distill.py an exponential errs by 4 u of itself and 3 u D, D at most 88 where it
 counts in fp32 (e^-88 is the smallest normal number), 268 u, and its sum by 64 u (4000 u for rows read twice).  A factor
@@ -55,3 +55,19 @@ def test_a_factor_in_the_exponent(gpu_lib, pm, n, V, dtype):
         ids, teacher = lists((n,), V, 9)
         check(pm, logits, ids, teacher, T, scale=4096.0)
         check(pm, logits, None, None, 1.0, labels=ids[:, 0].contiguous(), hard=1.0, scale=4096.0)
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("n,V", SHAPES)
+def test_temperatures_far_from_one(gpu_lib, pm, n, V, dtype):
+    """Differences that one temperature needs where the other one, or the plain exponential, sees nothing but the largest."""
+    torch.manual_seed(n + V + 1)
+    ids, teacher = lists((n,), V, 9)
+    labels = ids[:, 2].contiguous()
+    near = (torch.randn(n, V, device="cuda") * 2).to(dtype)
+    for T in (1e-5, 3e-6):
+        check(pm, near, ids, teacher, T, 1.0, labels, 1.0, scale=4096.0)
+    far = (torch.rand(n, V, device="cuda") * (100_000 if dtype is torch.bfloat16 else 60_000)).to(dtype)
+    for T in (4000.0, 30_000.0):
+        check(pm, far, ids, teacher * 1000, T, 1.0, None, 0.0, scale=1 / 16)
+        check(pm, far, ids, teacher * 1000, T, 1.0, labels, 1.0, scale=1 / 16)
