@@ -484,6 +484,12 @@ __device__ __forceinline__ void with_gradient(const RowFactors& f, float per, F&
   fn(Gradient<TYPE, MODE, false, false>(f, per));
 }
 
+// How far a part's largest lies below that of all (-inf: a part without logits
+// above it, whose sums are 0).  Parts of -inf alone stay as they are: their
+// sums are 0, or NaN where they hold one, and a row of nothing else becomes NaN
+// by the division by its sum.
+__device__ __forceinline__ float below(float part, float all) { return all == -INFINITY ? 0.f : part - all; }
+
 // Sums of several parts of a row, relative to the largest of all: `count` of
 // them, of which the lane has number `lane` (at most 32).
 template <int MODE>
@@ -491,8 +497,7 @@ __device__ __forceinline__ RowSums merge_sums(const RowSums& s, int count, float
   const int lane = threadIdx.x & 31;
   RowSums all;
   all.max = lanes_max(lane < count ? s.max : -INFINITY);
-  // (-inf: a part without logits above it, its sums are 0; all of -inf: NaN, as a softmax of nothing is)
-  const float down = s.max - all.max;
+  const float down = below(s.max, all.max);
   all.t = lanes_sum(lane < count ? s.t * exp2_of(down * per) : 0.f, 32);
   all.one = MODE != ONE_SUM ? lanes_sum(lane < count ? s.one * exp2_of(down * kLog2E) : 0.f, 32) : 0.f;
   return all;
@@ -508,7 +513,7 @@ __device__ __forceinline__ RowSums merge_few(int count, float per, F&& part) {
 #pragma unroll 8
   for (int i = 0; i < count; ++i) {
     const RowSums s = part(i);
-    const float down = s.max - all.max;
+    const float down = below(s.max, all.max);
     all.t = fmaf(s.t, exp2_of(down * per), all.t);
     if (MODE != ONE_SUM) all.one = fmaf(s.one, exp2_of(down * kLog2E), all.one);
   }
@@ -727,7 +732,6 @@ distill_slices_kernel(const __grid_constant__ DistillArgs a, int split) {
         if (!(ok = barrier_wait(summed, parity))) break;
         RowSums all = merge_few<MODE>(kSliceWarps, per, [&](int i) { return sh.warps[i]; });
         if (split > 1) {
-          if (all.max == -INFINITY) all.t = all.one = 0.f;   // (a part of -inf alone has no NaN for the others)
           const uint32_t bar = shared_at(&sh.arrived[q]);
           if (lane < split)
             store_and_count(shared_of(shared_at(&sh.blocks[q][rank]), lane), make_float4(all.max, all.t, all.one, 0.f), shared_of(bar, lane));
@@ -910,8 +914,7 @@ distill_long_kernel(const __grid_constant__ DistillArgs a) {
       if (lane == 0) warps[warp] = mine;
       __syncthreads();
       if (warp == 0) {
-        RowSums ours = merge_sums<MODE>(lane < WARPS ? warps[lane] : RowSums{-INFINITY, 0.f, 0.f}, WARPS, per);
-        if (ours.max == -INFINITY) ours.t = ours.one = 0.f;
+        const RowSums ours = merge_sums<MODE>(lane < WARPS ? warps[lane] : RowSums{-INFINITY, 0.f, 0.f}, WARPS, per);
         if (lane < kLongBlocks) cluster.map_shared_rank(&blocks[turn][0], lane)[rank] = ours;
       }
       cluster.sync();

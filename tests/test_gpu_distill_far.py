@@ -1,4 +1,5 @@
-"""Distillation of rows far from zero, and at temperatures far from one, against the formula in 64 bits.
+"""Distillation of rows far from zero, at temperatures far from one, and of rows whose parts hold nothing: against the
+formula in 64 bits.
 
 Tolerances (u = 2^-24).  As in test_gpu_distill.py an exponential errs by 4 u of itself and 3 u D, D at most 88 where it
 counts in fp32 (e^-88 is the smallest normal number), 268 u, and its sum by 64 u (4000 u for rows read twice).  A factor
@@ -71,3 +72,27 @@ def test_temperatures_far_from_one(gpu_lib, pm, n, V, dtype):
     for T in (4000.0, 30_000.0):
         check(pm, far, ids, teacher * 1000, T, 1.0, None, 0.0, scale=1 / 16)
         check(pm, far, ids, teacher * 1000, T, 1.0, labels, 1.0, scale=1 / 16)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("n,V", SHAPES)
+def test_no_number_among_masked_words(gpu_lib, pm, n, V, dtype):
+    """A NaN whose part of the row holds nothing but -infinity beside it makes the row NaN, and no other row; parts of
+    -infinity alone, or of rows of nothing else, do as they did."""
+    torch.manual_seed(n + V + 2)
+    logits = torch.randn(n, V, device="cuda").to(dtype)
+    ids, teacher = lists((n,), 90, 5)
+    logits[:3, 100:] = -math.inf
+    logits[0, V - 1] = math.nan
+    logits[1, V // 2:] = math.nan
+    if n > 4:
+        logits[3] = -math.inf
+        logits[4] = math.nan
+    bad = [0, 1] + ([3, 4] if n > 4 else [])
+    good = [i for i in range(n) if i not in bad]
+    for T, labels, hard in ((1.0, None, 0.0), (2.0, ids[:, 0].contiguous(), 0.5), (0.7, ids[:, 0].contiguous(), 0.5)):
+        into = torch.zeros_like(logits)
+        loss = pm.distill(logits, ids, teacher, T, 1.0, labels, hard, grad=into)
+        pm.wait()
+        assert loss[bad].isnan().all() and into[bad].isnan().all()
+        assert torch.isfinite(loss[good]).all() and torch.isfinite(into[good]).all()
