@@ -95,8 +95,8 @@ __device__ __forceinline__ void times_slope(float (&d)[N], const float (&z)[N], 
     case ADAPM_ACTIVATION_GELU_TANH:
 #pragma unroll
       for (int j = 0; j < N; ++j) {
-        // s = 1 / (1 + e^-2u), its slope s (1 - s) 2 u'
-        const float q = z[j] * z[j];
+        // s = 1 / (1 + e^-2u), its slope s (1 - s) 2 u'; where z^2 is beyond 10^30, s is 0 or 1 and its slope 0
+        const float q = fminf(z[j] * z[j], 1e30f);
         const float s = logistic(z[j] * fmaf(kTanhA, q, kTanhB)), t = s * z[j];
         d[j] *= fmaf(fmaf(-s, t, t), fmaf(-3.f * kTanhA / kLog2E, q, -kTanhB / kLog2E), s);
       }
