@@ -26,6 +26,7 @@ struct GemmProduct {
   bool a_across, b_across;   // stored with m (n) contiguous instead of k
   bool aligned;              // rows of what is written and of the residual begin on four elements
   uint32_t m, n, k_blocks;
+  uint32_t chain;            // blocks of k that the tensor cores add up; such chains' sums are added in fp32
   uint32_t tiles_m, tiles_n;
   Epilogue e;
 };
@@ -47,6 +48,7 @@ struct GemmArgs {
   bool turned;               // D is the product's transpose: m counts its columns
   uint32_t bn, stages;
   uint32_t splits, per_split;   // parts that one product's k is summed in, and blocks of a part
+  float* chains;                // for the sums of chains that registers do not hold: bn x kTileM floats a block
   DevState* st;
 };
 

@@ -36,14 +36,20 @@ constexpr uint32_t kSmem = 232448;          // shared memory of a block
 constexpr uint32_t kGroupM = 16;            // tiles of m taken together, for L2 (8192 x 4096 x 8192: 4 384 us, 8 381, 16 366, 32 372)
 constexpr uint32_t kTurnedRows = 64;        // up to so many rows the weight's columns are m
 constexpr uint32_t kMostSplits = 8;         // parts of k: the blocks of a cluster
-// Blocks of k that the tensor cores add up for an output of 32 bits; such
+// Blocks of k that the tensor cores add up at most, by the output's type; such
 // chains' sums are added by the epilogue's warps.  The tensor cores cut what
-// does not fit fp32 towards zero, which grows with the number of additions:
-// 4096 x 4096 x 4096 is off by 4.8e-6 in one chain, by 6.5e-7 in eight, of 12
-// blocks each by 9.2e-7 (96, 141 and 137 us: tiles of 256 columns leave the
-// chains' sums no registers; 133 x 4096 x 2048 16.1, 17.5 and 17.2).  A 16-bit
-// output's rounding is hundreds of times that.
-constexpr uint32_t kChain = 8;
+// does not fit fp32 towards zero, which grows with the number of products:
+// positive fp16 numbers lose 2.6e-6 of a sum of 512, 2.5e-5 of 4096, 4.1e-4 of
+// 65,536, 1.7e-3 of 262,144; bf16 up to as much.
+// fp32 outputs: short chains, whose sums stay in registers, for which tiles of
+// 256 columns leave no room (4096 x 4096 x 4096 96 -> 141 us, 8192 x 4096 x
+// 8192 351 -> 538, 133 x 4096 x 2048 16.1 -> 17.5).
+// 16-bit outputs: up to a tenth of the half step that they are rounded by, 8192
+// products for fp16's 4.9e-4 and 65,536 for bf16's 3.9e-3; sums of chains that
+// long wait in memory, written and read beside the next chain's products.
+constexpr uint32_t chain_of(int type) { return type == ADAPM_F32 ? 8 : (type == ADAPM_F16 ? 128 : 1024); }
+// Where the sums of chains stay.
+enum { ONE_CHAIN = 0, IN_REGISTERS = 1, IN_MEMORY = 2 };
 
 // ---- activations -----------------------------------------------------------------
 // 1 / (1 + 2^x); 0 where 2^x is beyond fp32, as in the limit.
@@ -293,9 +299,10 @@ __device__ __forceinline__ void add_columns(const ColumnSums& s, float* shared, 
 // holds, and writes to its shared memory, half of b's tile: with tiles of 128 x
 // 256 copies and products move 96 KB through it per block of k, 188 bytes a clock at
 // full rate, with pairs 64 KB.
-// CHAIN: for fp32 outputs of more than kChain blocks of k, tiles of up to 128 columns.
+// CHAIN: for more blocks of k than a chain has: fp32 outputs in tiles of up to
+// 128 columns (IN_REGISTERS), 16-bit ones (IN_MEMORY).
 // TWO: of two products, both without more of an epilogue than the output, each of a type of its own.
-template <bool BF16, bool OUT32, bool PAIR, bool TWO, bool CHAIN>
+template <bool BF16, bool OUT32, bool PAIR, bool TWO, int CHAIN>
 __global__ void __launch_bounds__(kGemmThreads, 1)
 gemm_kernel(const __grid_constant__ GemmArgs g) {
   constexpr int TYPE = BF16 ? ADAPM_BF16 : ADAPM_F16;
@@ -391,7 +398,7 @@ gemm_kernel(const __grid_constant__ GemmArgs g) {
         const uint32_t shape = mma_shape(BF16, p.a_across, p.b_across, PAIR ? 2 * kTileM : kTileM, g.bn);
         const uint32_t a_step = tile_step(p.a_across), b_step = tile_step(p.b_across), k1 = k_end(p);
         for (uint32_t from = k0, to; from < k1 && ok; from = to, ++turn) {   // a chain of them
-          to = CHAIN ? min(k1, from + kChain) : k1;
+          to = CHAIN ? min(k1, from + p.chain) : k1;
           const uint32_t b = turn & 1u;
           if (!(ok = barrier_wait(sum_empty + 8 * b, ((turn >> 1) & 1u) ^ 1u))) break;
           tmem_fence_after();
@@ -419,14 +426,14 @@ gemm_kernel(const __grid_constant__ GemmArgs g) {
     const uint32_t half = (uint32_t)(warp - 2) >> 2;   // of their columns, by turns
     float* const tile = staging + (warp - 2) * kStage;
     uint32_t turn = 0;
-    float run[CHAIN ? 2 : 1][32];   // sums of the chains so far
+    float run[CHAIN == IN_REGISTERS ? 2 : 1][32];   // sums of the chains so far
     bool ok = true;
     for (Items<TWO> i(g, worker, workers); i.any && ok; i.next(g)) {
       const GemmProduct& p = g.p[TWO ? i.which : 0];
       const Tile t = tile_of<PAIR>(p, g.bn, i.tile);
       const uint32_t m0 = t.m0 + rank * kTileM + quarter * 32, k1 = k_end(p);
       for (uint32_t k = k0, to; k < k1; k = to, ++turn) {
-        to = CHAIN ? min(k1, k + kChain) : k1;
+        to = CHAIN ? min(k1, k + p.chain) : k1;
         const bool more = CHAIN && k > k0, last = !CHAIN || to == k1;
         const uint32_t b = turn & 1u;
         if (!(ok = barrier_wait(sum_full + 8 * b, (turn >> 1) & 1u))) {
@@ -436,6 +443,8 @@ gemm_kernel(const __grid_constant__ GemmArgs g) {
         __syncwarp();
         tmem_fence_after();
         const uint32_t from = tmem + ((quarter * 32u) << 16) + b * g.bn;
+        // (column c of the lane's row: read and written by this lane alone)
+        float* const waiting = CHAIN == IN_MEMORY ? g.chains + (uint64_t)blockIdx.x * g.bn * kTileM + quarter * 32 + lane : nullptr;
         if (!PAIR && !TWO && (g.splits > 1 || g.turned)) {
           // to shared memory (the ring is no longer read: there is one tile): see below
           const uint32_t row = quarter * 32 + lane;
@@ -464,7 +473,21 @@ gemm_kernel(const __grid_constant__ GemmArgs g) {
             }
           }
         } else if (!last) {
-          if constexpr (CHAIN) {
+          if constexpr (CHAIN == IN_MEMORY) {
+            for (uint32_t c0 = half * 32; c0 < g.bn && t.n0 + c0 < p.n; c0 += 64) {
+              float v[32];
+              float* const at = waiting + c0 * kTileM;
+              __syncwarp();
+              tmem_load(from + c0, v);
+              if (more) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] += at[j * kTileM];
+              }
+#pragma unroll
+              for (int j = 0; j < 32; ++j) at[j * kTileM] = v[j];
+            }
+          }
+          if constexpr (CHAIN == IN_REGISTERS) {
 #pragma unroll
             for (uint32_t n = 0; n < 2; ++n) {
               const uint32_t c0 = half * 32 + n * 64;
@@ -481,7 +504,13 @@ gemm_kernel(const __grid_constant__ GemmArgs g) {
             float v[32];
             __syncwarp();
             tmem_load(from + c0, v);
-            if constexpr (CHAIN) {
+            if constexpr (CHAIN == IN_MEMORY) {
+              if (more) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] += waiting[(c0 + j) * kTileM];
+              }
+            }
+            if constexpr (CHAIN == IN_REGISTERS) {
               // (an array of registers has no index)
               auto add = [&](const float (&sums)[32]) {
 #pragma unroll
@@ -717,7 +746,8 @@ cudaError_t tensor_map(const Operand& o, bool bf16, uint32_t height, CUtensorMap
 struct GemmPlan {
   uint64_t m, n;
   bool turned, pair;
-  bool chained;   // in chains of kChain blocks of k
+  int chained;   // where the sums of chains stay (ONE_CHAIN, ...)
+  uint32_t chain;   // blocks of k of one
   uint32_t bn, tiles_m, tiles_n, k_blocks, splits, per_split, stages;
   double us;   // that it takes, by kForms
 };
@@ -754,14 +784,19 @@ void set_form(GemmPlan& p, uint32_t bn, bool pair, uint64_t parts) {
   const uint32_t stage = kTileM * 128 + (pair ? bn / 2 : bn) * 128;
   p.stages = std::min(kMaxStages, (kSmem - 1024 - 512 - kFinishWarps * kStage * (uint32_t)sizeof(float)) / stage);
 }
-// The product of `rows` x `columns` elements over k.
-GemmPlan gemm_plan(uint64_t rows, uint32_t columns, uint64_t k, bool out32, int sms) {
+// The product of `rows` x `columns` elements of `type` over k.
+GemmPlan gemm_plan(uint64_t rows, uint32_t columns, uint64_t k, int type, int sms) {
   GemmPlan p{};
   p.turned = rows <= kTurnedRows;
   p.m = p.turned ? columns : rows;
   p.n = p.turned ? rows : columns;
   p.k_blocks = (uint32_t)((k + kBlockK - 1) / kBlockK);
-  p.chained = out32 && p.k_blocks > kChain;
+  p.chain = chain_of(type);
+  if (type != ADAPM_F32 && p.k_blocks > p.chain) {   // chains of one length: none too short for the sums of the one before
+    const uint32_t chains = (p.k_blocks + p.chain - 1) / p.chain;
+    p.chain = (p.k_blocks + chains - 1) / chains;
+  }
+  p.chained = p.k_blocks <= chain_of(type) ? ONE_CHAIN : (type == ADAPM_F32 ? IN_REGISTERS : IN_MEMORY);
   // parts of k, of at least two blocks, while SMs are idle
   auto parts_of = [&](uint64_t tiles) {
     return std::max<uint64_t>(1, std::min<uint64_t>({(uint64_t)sms / tiles, p.k_blocks / 2, kMostSplits}));
@@ -774,7 +809,7 @@ GemmPlan gemm_plan(uint64_t rows, uint32_t columns, uint64_t k, bool out32, int 
   const Form* best = nullptr;
   uint64_t parts = 1;
   for (const Form& f : kForms) {
-    if (p.chained && f.bn > 128) continue;   // (sums of chains that the registers hold)
+    if (p.chained == IN_REGISTERS && f.bn > 128) continue;   // (sums of chains that the registers hold)
     const uint64_t tiles = tiles_of(p, f.bn, f.pair), at_once = f.pair ? sms / 2 : sms;
     const double rounds = (double)((tiles + at_once - 1) / at_once);
     for (int in_parts = 0; in_parts < 2; ++in_parts) {
@@ -806,7 +841,7 @@ struct Shared {
 //    4096 x 4096 x 4096    185       205        182
 //    8192 x 4096 x 4096    350                  361
 bool share(GemmPlan& p, GemmPlan& q, int sms, Shared* how) {
-  if (p.turned || q.turned || p.chained || q.chained) return false;
+  if (p.turned || q.turned || p.chained == IN_REGISTERS || q.chained == IN_REGISTERS) return false;
   double best = (p.us + q.us) * 15 / 16;
   const Form* form = nullptr;
   for (const Form& f : kForms) {
@@ -838,12 +873,21 @@ struct Product {
   GemmPlan p;
   Operand left, right;
   Epilogue e;
-  size_t bytes() const { return round256(left.bytes) + round256(right.bytes); }
+  size_t bytes() const { return round256(left.bytes) + round256(right.bytes); }   // of copies
   uint64_t tiles() const { return (uint64_t)p.tiles_m * p.tiles_n; }
 };
-// One product, or two that share a launch.
-cudaError_t launch_gemm(const Product& first, const Product* second, const Shared& how, const ColumnSums& sums, bool bf16, DevState* st, int sms,
-                        cudaStream_t stream) {
+// (a block whose tile goes through the ring to its epilogue takes one tile)
+bool single(const GemmPlan& p) { return p.splits > 1 || p.turned; }
+bool chains_wait(const Product& first, const Product* second) {
+  return first.p.chained == IN_MEMORY || (second && second->p.chained == IN_MEMORY);
+}
+// Bytes of memory for the sums of chains (those of single tiles stay in registers).
+size_t chain_bytes(const Product& first, const Product* second, int sms) {
+  return chains_wait(first, second) && !single(first.p) ? (size_t)sms * first.p.bn * kTileM * sizeof(float) : 0;
+}
+// One product, or two that share a launch; chains: chain_bytes of memory.
+cudaError_t launch_gemm(const Product& first, const Product* second, const Shared& how, const ColumnSums& sums, bool bf16, char* chains,
+                        DevState* st, int sms, cudaStream_t stream) {
   const GemmPlan& p = first.p;
   GemmArgs g{};
   for (int i = 0; i < (second ? 2 : 1); ++i) {
@@ -860,6 +904,7 @@ cudaError_t launch_gemm(const Product& first, const Product* second, const Share
     to.m = (uint32_t)a.mn;
     to.n = (uint32_t)b.mn;
     to.k_blocks = q.p.k_blocks;
+    to.chain = q.p.chain;
     to.tiles_m = q.p.tiles_m;
     to.tiles_n = q.p.tiles_n;
     to.e = q.e;
@@ -871,29 +916,33 @@ cudaError_t launch_gemm(const Product& first, const Product* second, const Share
   g.stages = p.stages;
   g.splits = p.splits;
   g.per_split = p.per_split;
+  g.chains = reinterpret_cast<float*>(chains);
   g.st = st;
   using Kernel = void (*)(GemmArgs);
-  // (two products share no pairs, and chains are none of theirs)
-  static constexpr Kernel kernels[2][4][2] = {
-      {{gemm_kernel<false, false, false, false, false>, gemm_kernel<false, false, true, false, false>},
-       {gemm_kernel<false, true, false, false, false>, gemm_kernel<false, true, true, false, false>},
-       {gemm_kernel<false, false, false, true, false>, nullptr},
-       {gemm_kernel<false, true, false, false, true>, nullptr}},
-      {{gemm_kernel<true, false, false, false, false>, gemm_kernel<true, false, true, false, false>},
-       {gemm_kernel<true, true, false, false, false>, gemm_kernel<true, true, true, false, false>},
-       {gemm_kernel<true, false, false, true, false>, nullptr},
-       {gemm_kernel<true, true, false, false, true>, nullptr}}};
-  const int what = second ? 2 : (p.chained ? 3 : (first.e.out.type == ADAPM_F32 ? 1 : 0));
+  // (two products share no pairs, and chains in registers are none of theirs)
+  static constexpr Kernel kernels[2][6][2] = {
+      {{gemm_kernel<false, false, false, false, ONE_CHAIN>, gemm_kernel<false, false, true, false, ONE_CHAIN>},
+       {gemm_kernel<false, true, false, false, ONE_CHAIN>, gemm_kernel<false, true, true, false, ONE_CHAIN>},
+       {gemm_kernel<false, false, false, true, ONE_CHAIN>, nullptr},
+       {gemm_kernel<false, true, false, false, IN_REGISTERS>, nullptr},
+       {gemm_kernel<false, false, false, false, IN_MEMORY>, gemm_kernel<false, false, true, false, IN_MEMORY>},
+       {gemm_kernel<false, false, false, true, IN_MEMORY>, nullptr}},
+      {{gemm_kernel<true, false, false, false, ONE_CHAIN>, gemm_kernel<true, false, true, false, ONE_CHAIN>},
+       {gemm_kernel<true, true, false, false, ONE_CHAIN>, gemm_kernel<true, true, true, false, ONE_CHAIN>},
+       {gemm_kernel<true, false, false, true, ONE_CHAIN>, nullptr},
+       {gemm_kernel<true, true, false, false, IN_REGISTERS>, nullptr},
+       {gemm_kernel<true, false, false, false, IN_MEMORY>, gemm_kernel<true, false, true, false, IN_MEMORY>},
+       {gemm_kernel<true, false, false, true, IN_MEMORY>, nullptr}}};
+  const bool wait = chains_wait(first, second);
+  const int what = second ? (wait ? 5 : 2) : (wait ? 4 : (p.chained ? 3 : (first.e.out.type == ADAPM_F32 ? 1 : 0)));
   const Kernel kernel = kernels[bf16][what][p.pair];
-  static Asked asked[2][4][2];
+  static Asked asked[2][6][2];
   const cudaError_t err = asked[bf16][what][p.pair].allow(kernel, kSmem - 1024);
   if (err != cudaSuccess) return err;
   const uint64_t tiles = first.tiles() + (second ? second->tiles() : 0);
   g.workers = (uint32_t)std::min<uint64_t>(tiles, (uint64_t)sms);
   g.sums = sums;
   const uint32_t others = sums.parts ? std::min((uint32_t)sms - g.workers, (sums.columns + 31) / 32) : 0;
-  // (a block whose tile goes through the ring to its epilogue takes one tile)
-  const bool single = p.splits > 1 || p.turned;
   const unsigned cluster = p.pair ? 2 : p.splits;
   cudaLaunchAttribute at[2]{};
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -903,7 +952,7 @@ cudaError_t launch_gemm(const Product& first, const Product* second, const Share
   at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t c{};
   c.gridDim = dim3((unsigned)(p.pair ? 2 * std::min<uint64_t>(tiles, (uint64_t)sms / 2)
-                                     : (single ? tiles * p.splits : g.workers + others)));
+                                     : (single(p) ? tiles * p.splits : g.workers + others)));
   c.blockDim = dim3(kGemmThreads);
   c.dynamicSmemBytes = 1024 + (size_t)p.stages * (kTileM + (p.pair ? p.bn / 2 : p.bn)) * 128 + kFinishWarps * kStage * sizeof(float);
   c.stream = stream;
@@ -1000,7 +1049,7 @@ bool by_rows(const MatrixView& m, uint64_t rows, uint32_t columns) {   // stored
 
 Product out_product(const LinearArgs& a, int sms) {   // rows x outs over ins
   Product q;
-  q.p = gemm_plan(a.rows, a.outs, a.ins, a.out.type == ADAPM_F32, sms);
+  q.p = gemm_plan(a.rows, a.outs, a.ins, a.out.type, sms);
   q.left = operand(a.x.data, a.rows, a.ins, a.x.row_stride, a.x.col_stride, q.p.turned);
   q.right = operand(a.weight.data, a.outs, a.ins, a.weight.col_stride, a.weight.row_stride, false);
   q.e = Epilogue{a.bias, a.residual, a.out, a.pre, a.activation};
@@ -1009,12 +1058,15 @@ Product out_product(const LinearArgs& a, int sms) {   // rows x outs over ins
 
 }  // namespace
 
-size_t linear_scratch(const LinearArgs& a, int sms) { return out_product(a, sms).bytes(); }
+size_t linear_scratch(const LinearArgs& a, int sms) {
+  const Product q = out_product(a, sms);
+  return q.bytes() + chain_bytes(q, nullptr, sms);
+}
 
 cudaError_t launch_linear(const LinearArgs& a, char* scratch, int sms, cudaStream_t stream) {
   Product q = out_product(a, sms);
   pack(q.left, q.right, scratch, stream);
-  return launch_gemm(q, nullptr, Shared{}, ColumnSums{}, a.x.type == ADAPM_BF16, a.st, sms, stream);
+  return launch_gemm(q, nullptr, Shared{}, ColumnSums{}, a.x.type == ADAPM_BF16, scratch + q.bytes(), a.st, sms, stream);
 }
 
 namespace {
@@ -1052,7 +1104,7 @@ Backward backward_of(const LinearArgs& a, char* scratch, int sms) {
 }
 Product dx_product(const LinearArgs& a, const Backward& b, int sms) {   // rows x ins over outs
   Product q;
-  q.p = gemm_plan(a.rows, a.ins, a.outs, a.dx.type == ADAPM_F32, sms);
+  q.p = gemm_plan(a.rows, a.ins, a.outs, a.dx.type, sms);
   q.left = operand(b.dz.data, a.rows, a.outs, b.dz.row_stride, b.dz.col_stride, q.p.turned);
   q.right = operand(a.weight.data, a.ins, a.outs, a.weight.row_stride, a.weight.col_stride, false);
   q.e = Epilogue{};
@@ -1062,8 +1114,7 @@ Product dx_product(const LinearArgs& a, const Backward& b, int sms) {   // rows 
 Product dweight_product(const LinearArgs& a, const Backward& b, int sms) {   // ins x outs over rows, or its transpose
   Product q;
   const uint32_t k = (uint32_t)a.rows;
-  const bool out32 = a.dweight.type == ADAPM_F32;
-  q.p = b.across_out ? gemm_plan(a.outs, a.ins, k, out32, sms) : gemm_plan(a.ins, a.outs, k, out32, sms);
+  q.p = b.across_out ? gemm_plan(a.outs, a.ins, k, a.dweight.type, sms) : gemm_plan(a.ins, a.outs, k, a.dweight.type, sms);
   const bool turned = q.p.turned;
   const Operand x = operand(a.x.data, a.ins, k, a.x.col_stride, a.x.row_stride, turned && !b.across_out);
   const Operand d = operand(b.dz.data, a.outs, k, b.dz.col_stride, b.dz.row_stride, turned && b.across_out);
@@ -1080,9 +1131,11 @@ struct Products {
   Product q[2];
   bool shared = false;   // in one launch
   Shared how{};
-  size_t bytes() const {   // (launches that follow each other share scratch)
-    const size_t x = n > 0 ? q[0].bytes() : 0, y = n > 1 ? q[1].bytes() : 0;
-    return shared ? x + y : std::max(x, y);
+  size_t bytes(int sms) const {   // (launches that follow each other share scratch)
+    if (shared) return q[0].bytes() + q[1].bytes() + chain_bytes(q[0], &q[1], sms);
+    size_t most = 0;
+    for (int i = 0; i < n; ++i) most = std::max(most, q[i].bytes() + chain_bytes(q[i], nullptr, sms));
+    return most;
   }
 };
 Products backward_products(const LinearArgs& a, const Backward& b, int sms) {
@@ -1109,7 +1162,7 @@ void launch_dz(const LinearArgs& a, const Backward& b, float* sums, cudaStream_t
 
 size_t linear_grad_scratch(const LinearArgs& a, int sms) {
   const Backward b = backward_of(a, nullptr, sms);
-  return b.dz_bytes + b.sum_bytes + backward_products(a, b, sms).bytes();
+  return b.dz_bytes + b.sum_bytes + backward_products(a, b, sms).bytes(sms);
 }
 
 cudaError_t launch_linear_grad(const LinearArgs& a, char* scratch, int sms, cudaStream_t stream) {
@@ -1130,10 +1183,11 @@ cudaError_t launch_linear_grad(const LinearArgs& a, char* scratch, int sms, cuda
   for (int i = 0; i < all.n; ++i) {
     Product& q = all.q[i];
     pack(q.left, q.right, rest + at, stream);
-    if (all.shared) at += q.bytes();
+    at += q.bytes();
     if (all.shared && i == 0) continue;
-    const cudaError_t err = launch_gemm(all.shared ? all.q[0] : q, all.shared ? &q : nullptr, all.how, beside, bf16, a.st, sms, stream);
+    const cudaError_t err = launch_gemm(all.shared ? all.q[0] : q, all.shared ? &q : nullptr, all.how, beside, bf16, rest + at, a.st, sms, stream);
     if (err != cudaSuccess) return err;
+    at = 0;
   }
   return cudaSuccess;
 }

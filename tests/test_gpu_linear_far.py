@@ -1,8 +1,10 @@
-"""Dense layers at the ends of their ranges: numbers whose squares leave fp32."""
+"""Dense layers at the ends of their ranges: 16-bit outputs of very long sums, numbers whose squares leave fp32."""
+import math
+
 import pytest
 import torch
 
-from .test_gpu_linear import ACTS, check, check_grad
+from .test_gpu_linear import ACTS, TYPES, check, check_grad, stored
 
 pytestmark = pytest.mark.gpu
 
@@ -12,6 +14,99 @@ def pm(gpu_lib):
     pm = gpu_lib.ParameterManager(4, 4, 1)
     yield pm
     pm.close()
+
+
+def spread(rows, columns, dtype, size=1.0):
+    """Positive numbers whose sums over rows (or products of two such) are spread over the steps of a 16-bit type."""
+    x = torch.rand(rows, columns, device="cuda").add_(1).mul_(0.5 * size)
+    return x.mul_(torch.rand(columns, device="cuda") / 2 + 0.5).to(dtype)
+
+
+# Products that the tensor cores add up for a 16-bit output before the sum is added to others in fp32.
+CHAIN = {torch.float16: 8192, torch.bfloat16: 65_536}
+
+
+def check_long(got, a, b):
+    """got = a b, of positive numbers.  The tensor cores add 16 products at a time, each time off by two units in the last
+    place (2 * 2^-23 of the sum so far) at most, all of one sign: chain / 8 * 2^-23 of the whole sum, and half of that,
+    chain / 16 * 2^-23, of one that grows evenly; the chains' sums and parts of k err by half a unit each.  Then one
+    rounding.  On average that rounding is off by nothing: 5 of its standard deviations (below a half step) over the root
+    of the number of elements."""
+    ut, _ = TYPES[got.dtype]
+    k = a.shape[1]
+    off = CHAIN[got.dtype] / 16 * 2.0 ** -23 + (k / CHAIN[got.dtype] + 24) * 2.0 ** -24
+    for c0 in sorted({0, got.shape[1] // 128 * 64, max(0, got.shape[1] - 64)}):
+        want = a.double() @ b[:, c0:c0 + 64].double()
+        error = (got[:, c0:c0 + 64].double() - want) / want
+        assert error.abs().max() <= off + ut * (1 + off)
+        assert error.mean().abs() <= off + 5 * ut / math.sqrt(want.numel())
+
+
+@pytest.mark.parametrize("rows,ins,outs", [(1 << 18, 300, 520), (1 << 18, 520, 40), (1 << 18, 24, 200), (1 << 18, 2600, 2600),
+                                           (100_001, 129, 333)])
+def test_long_sums_over_rows(gpu_lib, pm, rows, ins, outs):
+    """dweight of many rows: tiles of every form, pairs of blocks, either order."""
+    torch.manual_seed(rows + ins)
+    x, g = spread(rows, ins, torch.float16, 2.0 ** -4), spread(rows, outs, torch.float16, 2.0 ** -4)
+    for by_out in (False, True):
+        w = stored(torch.ones(ins, outs, device="cuda", dtype=torch.float16), by_out)
+        got = pm.linear_grad(x, w, g, out=gpu_lib.LinearGrads(None, torch.empty_like(w), None))
+        pm.wait()
+        check_long(got.weight, x.t(), g)
+
+
+def test_long_sums_over_rows_bf16(gpu_lib, pm):
+    torch.manual_seed(8)
+    x, g = spread(1 << 20, 136, torch.bfloat16), spread(1 << 20, 328, torch.bfloat16)
+    w = torch.ones(136, 328, device="cuda", dtype=torch.bfloat16)
+    got = pm.linear_grad(x, w, g, out=gpu_lib.LinearGrads(None, torch.empty_like(w), None))
+    pm.wait()
+    check_long(got.weight, x.t(), g)
+
+
+@pytest.mark.parametrize("rows", [1, 7, 64, 65, 300, 2600])
+@pytest.mark.parametrize("k", [250_008, 50_021])
+def test_long_sums_over_a_vocabulary(gpu_lib, pm, rows, k):
+    """A product over as many words as a vocabulary has (the gradient of what its logits were made from), and the same
+    with z kept, bias, activation and residual behind it; rows of 50,021 are no multiple of 16 bytes."""
+    torch.manual_seed(rows)
+    n = 200 if rows < 2600 else 2600
+    if n == 2600 and k != 250_008:
+        n = 1000
+    g = spread(k, rows, torch.float16, 2.0 ** -4).t()
+    if rows % 2:
+        g = g.contiguous()
+    w = spread(k, n, torch.float16, 2.0 ** -4)
+    x = torch.ones(rows, n, device="cuda", dtype=torch.float16)
+    got = pm.linear_grad(x, w.t(), g, out=gpu_lib.LinearGrads(torch.empty_like(x), None, None))
+    pre, res = torch.empty(rows, n, device="cuda", dtype=torch.float16), torch.zeros(rows, n, device="cuda", dtype=torch.float16)
+    out = pm.linear(g, w, torch.zeros(n, device="cuda"), "relu", res, pre=pre)
+    pm.wait()
+    check_long(got.x, g, w)
+    check_long(pre, g, w)
+    assert torch.equal(out, pre)
+
+
+def test_long_sums_give_the_same_bits(gpu_lib):
+    """Eager twice, and recorded in a graph and replayed twice."""
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        pm = gpu_lib.ParameterManager(4, 4, 1)
+        x, g = torch.randn(70_000, 2600, device="cuda").half(), torch.randn(70_000, 2600, device="cuda").mul_(2.0 ** -8).half()
+        w = torch.zeros(2600, 2600, device="cuda", dtype=torch.float16)
+        into = [gpu_lib.LinearGrads(None, torch.empty_like(w), None) for _ in range(3)]
+        for o in into[:2]:
+            pm.linear_grad(x, w, g, out=o)
+        pm.wait()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            pm.linear_grad(x, w, g, out=into[2])
+        for _ in range(2):
+            into[2].weight.zero_()
+            graph.replay()
+            pm.wait()
+            assert torch.equal(into[2].weight, into[0].weight) and torch.equal(into[1].weight, into[0].weight)
+        pm.close()
 
 
 @pytest.mark.parametrize("act", ACTS)
