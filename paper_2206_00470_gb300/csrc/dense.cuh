@@ -232,19 +232,6 @@ __device__ __forceinline__ void store_n(char* p, const float* x) {
     *reinterpret_cast<uint2*>(p) = make_uint2(pack2<TYPE>(x[0], x[1]), pack2<TYPE>(x[2], x[3]));
   }
 }
-// The same for a type known at run time (the branch is the same for a whole launch).
-template <int N>
-__device__ __forceinline__ void load_n_as(const char* p, int type, float* x) {
-  if (type == ADAPM_F32) load_n<ADAPM_F32, N>(p, x);
-  else if (type == ADAPM_BF16) load_n<ADAPM_BF16, N>(p, x);
-  else load_n<ADAPM_F16, N>(p, x);
-}
-template <int N>
-__device__ __forceinline__ void store_n_as(char* p, int type, const float* x) {
-  if (type == ADAPM_F32) store_n<ADAPM_F32, N>(p, x);
-  else if (type == ADAPM_BF16) store_n<ADAPM_BF16, N>(p, x);
-  else store_n<ADAPM_F16, N>(p, x);
-}
 
 __host__ __device__ __forceinline__ int type_size(int type) { return type == ADAPM_F32 ? 4 : 2; }
 
@@ -295,9 +282,6 @@ inline bool rows_on(const RowView& v, uint64_t n, uint32_t elements) {
   const bool one = n <= 1;
   if (!one && v.inner_stride % (int64_t)elements != 0) return false;
   return v.flat || v.outer_stride % (int64_t)elements == 0;
-}
-inline bool vector_on(const VectorView& v, uint32_t elements) {
-  return reinterpret_cast<uintptr_t>(v.data) % ((uint64_t)elements * type_size(v.type)) == 0;
 }
 #endif
 

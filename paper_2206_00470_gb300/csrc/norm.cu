@@ -8,12 +8,12 @@
 // A row is taken by a group of lanes, 8 to 32 elements each, that stay in
 // registers, so that both sums are over values already there: the squares are
 // of differences from the mean, which costs no second pass over memory and
-// loses nothing where the mean is large.  Rows of up to 256 elements are taken
-// by (parts of) a warp, of up to 8192 (16-bit, forward: 16,384) by a block,
-// which has its next row on the way while it works on one; longer ones are
-// read again from L2.  Arithmetic is on pairs of floats: one issue for two.
-// dweight and dbias are summed by every block over its rows, in registers, and
-// joined in the order of the blocks.
+// loses nothing where the mean is large.  Rows of up to 512 elements are taken
+// by (parts of) a warp, of up to 8192 by a block (forward, 16-bit rows in wide
+// accesses: 1024 and 16,384), which has its next row on the way while it works
+// on one; longer ones are read again from L2.  Arithmetic is on pairs of floats:
+// one issue for two.  dweight and dbias are summed by every block over its rows,
+// in registers, and joined in the order of the blocks.
 // Bound by memory: 65,472 rows of 1024 bf16 forward 48 us, 5.5 TB/s, 262,144
 // rows backward 271 us, 6.0 TB/s; one row of 4096 by the launch, 6.9 us.  Odd
 // rows of fp16, which no wide access fits, are bound by instructions: 5105 rows
