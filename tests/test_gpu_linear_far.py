@@ -1,10 +1,11 @@
-"""Dense layers at the ends of their ranges: 16-bit outputs of very long sums, numbers whose squares leave fp32."""
+"""Dense layers at the ends of their ranges: 16-bit outputs of very long sums, numbers whose squares leave fp32, gradients
+that are one value for a whole row, and gradients against differences."""
 import math
 
 import pytest
 import torch
 
-from .test_gpu_linear import ACTS, TYPES, check, check_grad, stored
+from .test_gpu_linear import ACTS, HALVES, TYPES, U, act64, check, check_grad, stored
 
 pytestmark = pytest.mark.gpu
 
@@ -127,3 +128,53 @@ def test_numbers_whose_squares_leave_fp32(gpu_lib, pm, act):
     pm.linear_grad(x, w, grad, pre, act, out=into)
     pm.wait()
     check_grad(x, w, grad, pre, act, into)
+
+
+@pytest.mark.parametrize("rows,ins,outs", [(6, 40, 72), (150, 136, 264), (90, 77, 131)])
+def test_gradients_that_are_expanded(gpu_lib, pm, rows, ins, outs):
+    """One value for a row, one row for all, one value for everything; inputs likewise."""
+    torch.manual_seed(rows)
+    for dtype in HALVES:
+        for of in ((rows, 1), (1, outs), (1, 1)):
+            grad = torch.randn(of, device="cuda").to(dtype).expand(rows, outs)
+            x = torch.randn(1 if of[0] == 1 else rows, ins, device="cuda").to(dtype).expand(rows, ins)
+            for by_out in (False, True):
+                w = stored((torch.randn(ins, outs, device="cuda") / math.sqrt(ins)).to(dtype), by_out)
+                got = pm.linear_grad(x, w, grad)
+                pre = torch.randn(rows, 1, device="cuda").to(dtype).expand(rows, outs)
+                curved = pm.linear_grad(x, w, grad, pre, "silu")
+                pm.wait()
+                check_grad(x, w, grad, None, None, got)
+                check_grad(x, w, grad, pre, "silu", curved)
+
+
+@pytest.mark.parametrize("act", ACTS)
+def test_every_gradient_against_differences(gpu_lib, pm, act):
+    """Central differences of act(z) in 64 bits at the z that the forward pass kept, times grad, through plain products.
+
+    Differences over 2^-14: a third derivative (below 4) times 2^-28 / 6, and 2^-52 / 2^-14 of rounding.  dz is rounded to 16
+    bits, a half step of each term, after a slope that is off by 32 u of grad; sums of at most 64 terms in fp32 by
+    (64 / 8 + 16) 2^-23 of their magnitudes.  relu's kink lies at zero: no z is nearer to it than the difference."""
+    torch.manual_seed(4)
+    for dtype in HALVES:
+        x, w = torch.randn(64, 24, device="cuda").to(dtype), (torch.randn(24, 40, device="cuda") / 5).to(dtype)
+        b, grad = torch.randn(40, device="cuda").to(dtype), torch.randn(64, 40, device="cuda").to(dtype)
+        pre = torch.empty_like(grad)
+        pm.linear(x, w, b, act, pre=pre)
+        pm.wait()
+        pre = torch.where(pre.abs() < 2.0 ** -10, torch.full_like(pre, 2.0 ** -10), pre)
+        into = gpu_lib.LinearGrads(torch.empty(64, 24, device="cuda"), torch.empty(24, 40, device="cuda"),
+                                   torch.empty(40, device="cuda"))
+        pm.linear_grad(x, w, grad, pre, act, out=into)
+        pm.wait()
+        h, z, g = 2.0 ** -14, pre.double(), grad.double()
+        slope = (act64(z + h, act) - act64(z - h, act)) / (2 * h)
+        dz = g * slope
+        off = g.abs() * (4 * 2.0 ** -28 / 6 + 2.0 ** -37 * (1 + z.abs()) + 32 * U)
+        rounded = off + (dz.abs() + off) * TYPES[dtype][0] + TYPES[dtype][1]
+        more = (64 / 8 + 16) * 2.0 ** -23
+        for got, left, right, of in ((into.x, dz, w.t(), 0), (into.weight, x.t(), dz, 1)):
+            error = rounded @ w.double().t().abs() if of == 0 else x.double().t().abs() @ rounded
+            size = left.double().abs() @ right.double().abs()
+            assert ((got.double() - left.double() @ right.double()).abs() <= error + more * (size + error)).all()
+        assert ((into.bias.double() - dz.sum(0)).abs() <= off.sum(0) + more * (dz.abs() + off).sum(0)).all()
