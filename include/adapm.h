@@ -484,9 +484,10 @@ typedef struct {
  * rows x outs with col_stride 1.  pre (NULL: not wanted) receives z in x's
  * type, for the backward pass.  out is of x's type or fp32, residual has out's
  * type and may be its memory; out and pre overlap nothing else.  Products are
- * summed and all else is computed in fp32 (for an fp32 output at most 512 of
- * them in the tensor cores, which do not round to nearest), each output is rounded once.  rows,
- * ins and outs are at most 2^31, ins and outs not 0.  Operands whose rows (or
+ * summed and all else is computed in fp32, each output is rounded once.  (The
+ * tensor cores do not round to nearest: they add up at most 512 products for an
+ * fp32 output, 8192 for fp16, 65,536 for bf16; such sums are added to nearest.)
+ * rows, ins and outs are at most 2^31, ins and outs not 0.  Operands whose rows (or
  * columns) do not begin on 16 bytes are copied to scratch memory first. */
 adapm_status adapm_linear(adapm_ctx* ctx, const adapm_layer* shape, const adapm_matrix* x,
                           const adapm_matrix* weight, const adapm_vector* bias, int32_t activation,
@@ -545,8 +546,9 @@ typedef struct {
  * and weights.  weights (one float a row; NULL: ones) and grad (NULL: not
  * wanted) may be left out.  grad has the logits' type and is their own memory
  * (same strides) or does not overlap them; its rows must not overlap each
- * other; else loss and grad overlap nothing.  Computed in fp32 from one reading of the logits; a gradient is
- * rounded once to its type. */
+ * other; else loss and grad overlap nothing.  Computed in fp32 (exponentials below
+ * 2^-126 are 0) from one reading of the logits, two for rows above 1 MB; a
+ * gradient is rounded once to its type. */
 adapm_status adapm_distill(adapm_ctx* ctx, const adapm_shape* shape, const adapm_rows* logits,
                            const adapm_teacher* teacher, float temperature, float soft,
                            const adapm_labels* labels, float hard, float scale, const float* weights,

@@ -22,10 +22,12 @@
 // second time from L2.
 // Every warp sums relative to its own maximum, so one exchange per row is
 // enough.  Bound by memory, a read and a write of the logits: 4096 rows of
-// 250,000 bf16 645 us, 6.4 TB/s.  3060 rows of 50,021, a quarter of them padding,
-// each by two blocks: 123 to 143 us, 79 at the memory's rate; a row's exchange
-// takes as long as its slices' work, and only two blocks an SM run beside it.
-// Seven rows of 32,000 by the one launch 8.7 us.
+// 250,000 bf16 646 to 655 us, 6.3 TB/s.  3060 rows of 50,021, a quarter of them
+// padding, each by two blocks: 134 to 143 us (two exponentials: 152), 79 at the
+// memory's rate; a row's exchange takes as long as its slices' work, and only two
+// blocks an SM run beside it.  Seven rows of 32,000 by the one launch 9 us.  Far
+// from that rate: short rows by their lists (34,584 rows of 384 bf16 92 us, 9 at
+// the rate), rows read twice (16 of 700,000 fp32 54, 13).
 #pragma once
 
 #include <cooperative_groups.h>

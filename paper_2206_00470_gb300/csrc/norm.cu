@@ -16,8 +16,11 @@
 // in registers, and joined in the order of the blocks.
 // Bound by memory: 65,472 rows of 1024 bf16 forward 48 us, 5.5 TB/s, 262,144
 // rows backward 271 us, 6.0 TB/s; one row of 4096 by the launch, 6.9 us.  Odd
-// rows of fp16, which no wide access fits, are bound by instructions: 5105 rows
-// of 1001 backward 15 us.
+// rows of 16 bits, which no wide access fits, are bound by instructions: 5105
+// rows of 1001 fp16 backward 15 us, 8011 of 6511 bf16 133 forward (31 at the
+// memory's rate) and 120 backward (46).  So are rows beyond a block's registers,
+// which are read three times in such accesses: 1617 of 38,946 bf16 139 (37) and
+// 504 (56), 4096 of 12,000 backward 346 (43).
 #include <algorithm>
 
 #include "dense.cuh"
