@@ -88,6 +88,23 @@ def test_long_sums_over_a_vocabulary(gpu_lib, pm, rows, k):
     assert torch.equal(out, pre)
 
 
+@pytest.mark.parametrize("act", [None, "tanh"])
+@pytest.mark.parametrize("rows,ins,outs", [(9000, 256, 1000), (20_000, 1024, 1024), (65_472, 200, 328), (30_001, 333, 129)])
+def test_long_sums_beside_short_ones(gpu_lib, pm, rows, ins, outs, act):
+    """Both gradients of a layer, which may share a launch (dweight's sums are long, dx's are not), and the bias's."""
+    torch.manual_seed(rows)
+    x, g = spread(rows, ins, torch.float16, 2.0 ** -4), spread(rows, outs, torch.float16, 2.0 ** -4)
+    pre = torch.randn(rows, outs, device="cuda").half() if act else None
+    for by_out in (False, True):
+        w = stored((torch.rand(ins, outs, device="cuda") / 8).half(), by_out)
+        got, again = (pm.linear_grad(x, w, g, pre, act) for _ in range(2))
+        pm.wait()
+        if act is None:
+            check_long(got.weight, x.t(), g)
+        check_grad(x, w, g, pre, act, got)
+        assert all(torch.equal(a, b) for a, b in zip(got, again))
+
+
 def test_long_sums_give_the_same_bits(gpu_lib):
     """Eager twice, and recorded in a graph and replayed twice."""
     s = torch.cuda.Stream()
